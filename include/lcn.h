@@ -79,7 +79,7 @@ typedef enum {
 typedef enum { LCN_COST_SQEUCLID = 0, LCN_COST_EUCLID = 1, LCN_COST_COSINE = 2 } lcn_cost;
 typedef enum { LCN_MODE_DENSE = 0, LCN_MODE_SPARSE = 1, LCN_MODE_NYSTROM = 2, LCN_MODE_LCN = 3 } lcn_mode;
 typedef enum { LCN_HASH_KMEANS = 0, LCN_HASH_CROSSPOLYTOPE = 1 } lcn_hash;
-typedef enum { LCN_F32 = 0, LCN_BF16 = 1 } lcn_dtype; /* storage type of X and Y only */
+typedef enum { LCN_F32 = 0, LCN_BF16 = 1 } lcn_dtype; /* storage type of X and Y, and of the encoder operators' tensors */
 
 typedef enum {
     LCN_INIT_SAMPLE = 0,   /* num_landmarks distinct points by a splitmix64-driven partial Fisher-Yates shuffle */
@@ -360,6 +360,74 @@ typedef enum {
     LCN_CAL_LAUNCH_US = 4
 } lcn_calibration;
 lcn_status lcn_calibrate(int32_t what, void *workspace, size_t workspace_bytes, void *hip_stream, double *value_host);
+
+/* ---- operators that produce and train the points ---------------------------
+ * Layers and a loss for the model behind X and Y: a matrix product with its
+ * epilogue, attention inside the sets of a ragged batch, and softmax cross
+ * entropy against a large vocabulary of points.  They need no handle.
+ *
+ *   - Tensors are device memory, row-major and dense unless a stride is named,
+ *     of type `dtype` where no other is; any alignment that the type has (with
+ *     rows of a multiple of 16 bytes from 16-byte aligned addresses bf16 tensors
+ *     are read as they lie, others are first laid out in the workspace).
+ *     Outputs must not overlap inputs or each other, except where noted.
+ *   - Sums, softmax statistics and z are in 32 bits; a bf16 output is rounded
+ *     once.  float products are formed from three bf16 planes per operand (six
+ *     products of planes; as exact as single precision), so a float input that
+ *     is infinite makes the sums it enters NaN.
+ *   - Asynchronous on hip_stream, no synchronisation, no device allocation, no
+ *     atomics: same inputs, same bits.  The workspace (device, 256-byte aligned,
+ *     at least the bytes that the matching *_workspace_bytes call says for the
+ *     same sizes, else LCN_ERR_ALLOC) is free again when the call's work is done.
+ *     The calls may be captured into a graph.
+ *   - LCN_ERR_INVALID_ARG: a null pointer that is not called nullable, a size out
+ *     of its range, an unknown dtype or activation; nothing has been launched.
+ *     With rows == 0 nothing is read, and gradients of parameters become zero. */
+typedef enum { LCN_ACT_NONE = 0, LCN_ACT_TANH = 1, LCN_ACT_RELU = 2, LCN_ACT_GELU = 3, LCN_ACT_SILU = 4 } lcn_activation;
+
+/* y = act(x W^T + bias) + residual: x rows x d_in, W d_out x d_in, bias d_out
+ * (nullable), residual rows x d_out (nullable; y may be the same memory), y rows x
+ * d_out.  pre (nullable): the fp32 values z = x W^T + bias for the backward pass,
+ * rows x d_out.  GELU is z Phi(z) with the error function, SILU z / (1 + e^-z).
+ * Sizes: 0 <= rows <= 2^30, 1 <= d_in, d_out <= 2^20.  Up to 8 rows need no
+ * workspace. */
+lcn_status lcn_linear_workspace_bytes(int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype, int32_t backward,
+                                      size_t *bytes);
+lcn_status lcn_linear(const void *x, const void *W, const void *bias, const void *residual, int64_t rows, int32_t d_in,
+                      int32_t d_out, int32_t dtype, int32_t activation, void *y, float *pre, void *workspace,
+                      size_t workspace_bytes, void *hip_stream);
+/* Its gradients for a given dy: with dz = dy .* act'(pre),
+ *   dx = dz W (rows x d_in),  dW = dz^T x (d_out x d_in),  dbias = column sums of dz;
+ * the residual's gradient is dy itself.  dx, dW, dbias are nullable; pre may be
+ * NULL for LCN_ACT_NONE, x if dW is, W if dx is. */
+lcn_status lcn_linear_backward(const void *x, const void *W, const float *pre, const void *dy, int64_t rows, int32_t d_in,
+                               int32_t d_out, int32_t dtype, int32_t activation, void *dx, void *dW, void *dbias,
+                               void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Softmax cross entropy over a vocabulary, without keeping the rows x vocab scores
+ *   z_nv = scale x_n . W_v + bias_v    (x rows x dim, W vocab x dim, bias fp32, nullable):
+ *   lse_n = log sum_v exp z_nv,  loss_n = lse_n - z_n,target(n)   (fp32, rows each).
+ * With scale = 1/lambda and bias = log v this is the negative log likelihood of known
+ * pairs under the row-normalised plan.  A row with a negative target has loss 0
+ * (its lse is still formed) and adds nothing to any gradient, whatever its x
+ * holds; a target >= vocab makes its loss NaN.  A bias of -inf takes a word out.
+ * target: int64.  Sizes: 0 <= rows <= 2^30, 1 <= vocab <= 2^30, 1 <= dim <= 2^20;
+ * scale finite. */
+lcn_status lcn_cross_entropy_workspace_bytes(int64_t rows, int32_t vocab, int32_t dim, int32_t dtype, int32_t backward,
+                                             size_t *bytes);
+lcn_status lcn_cross_entropy(const void *x, const void *W, const float *bias, const int64_t *target, int64_t rows,
+                             int32_t vocab, int32_t dim, int32_t dtype, float scale, float *loss, float *lse, void *workspace,
+                             size_t workspace_bytes, void *hip_stream);
+/* Gradients of sum_n grad_loss_n loss_n for given grad_loss (fp32) and the lse of the
+ * forward call: with G_nv = grad_loss_n (exp(z_nv - lse_n) - [v = target(n)]),
+ *   dx = scale G W,  dW = scale G^T x  (of type dtype),  dbias_v = sum_n G_nv  (fp32).
+ * dx, dW, dbias are nullable.  The vocabulary is worked off in pieces; the
+ * workspace holds G of one piece (up to 512 MiB, or 256 words where more rows
+ * need more). */
+lcn_status lcn_cross_entropy_backward(const void *x, const void *W, const float *bias, const int64_t *target, const float *lse,
+                                      const float *grad_loss, int64_t rows, int32_t vocab, int32_t dim, int32_t dtype,
+                                      float scale, void *dx, void *dW, float *dbias, void *workspace, size_t workspace_bytes,
+                                      void *hip_stream);
 
 void lcn_destroy(lcn_handle h); /* frees host memory only; the workspace is the caller's */
 const char *lcn_status_string(int32_t status);

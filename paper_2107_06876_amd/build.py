@@ -24,6 +24,9 @@ SOURCES = {
     "kernels_dense.hip": [],
     "kernels_buckets.hip": [],
     "kernels_batched.hip": ["-ffp-contract=off"],  # bucket rule again
+    "kernels_planes.hip": [],
+    "kernels_linear.hip": [],
+    "kernels_entropy.hip": [],
     "lcn_api.hip": [],
     "calibrate.hip": [],
 }

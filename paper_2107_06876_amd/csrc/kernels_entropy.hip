@@ -1,0 +1,501 @@
+// Softmax cross entropy of rows x against a vocabulary W, z = scale x W^T + b, without keeping z:
+//   loss_n = lse_n - z_n,t(n),  lse_n = log sum_v exp z_nv;   G = g_n (exp(z_nv - lse_n) - [v = t(n)]),
+//   dx = scale G W,  dW = scale G^T x,  db_v = sum_n G_nv.
+//
+// Forward: one product whose epilogue leaves the maximum and the sum of exponentials of its 256 (or fewer) words for
+// every row; a second launch joins them.  Backward: for a piece of the vocabulary at a time the product is formed again,
+// its epilogue writes G of the piece (planes of bf16) into the workspace, and two products read it from there, G by rows for
+// dx and by columns for dW.  8 N V D operations, against 6 N V D with z kept at 4 bytes a value (N V values).
+//
+// Statistics, sums and z are in 32 bits; G is rounded to bf16 for bf16 tensors (its error is that of rounding the result
+// once more) and kept as three planes for float ones.
+#include "operators.h"
+
+namespace lcn {
+
+constexpr float LOG2E = 1.4426950408889634f;
+
+struct EntropyRow {
+    const float *bias;        // nullable
+    const int64_t *target;
+    float scale;
+    int vocab;
+};
+
+// joins (m, s) with another pair: the sum of exponentials relative to the larger maximum.  -inf: nothing yet.
+__device__ __forceinline__ void join(float &m, float &s, float om, float os)
+{
+    const float top = fmaxf(m, om);
+    const float a = m == top ? 1.f : exp2f((m - top) * LOG2E), b = om == top ? 1.f : exp2f((om - top) * LOG2E);
+    s = s * a + os * b;
+    m = top;
+}
+
+struct EntropyForward {
+    struct Args {
+        EntropyRow r;
+        float2 *part;    // [tile][row]
+        float *at_target;
+    };
+    template <int TM, int TN, int WM, int WN>
+    static __device__ void run(const Args &e, const ProductArgs &p, f32x4 (&acc)[TM][TN], long long m0, long long n0, int,
+                               char *lds, int tm, int tn)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g4 = 4 * (lane >> 4);
+        float2 *joined = (float2 *)lds;   // [WM][WN * TN * 16]
+        f32x4 bias[TM];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            bias[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (e.r.bias) bias[i] = load_four(e.r.bias + m0 + i * 16 + g4, (int)(p.m - (m0 + i * 16 + g4)), false);
+        }
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const long long n = n0 + j * 16 + (lane & 15);
+            const long long t = n < p.n ? e.r.target[n] - (m0 + g4) : -1;
+            float top = -__builtin_huge_valf();
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    float z = acc[i][j][u] * e.r.scale + bias[i][u];
+                    if (m0 + i * 16 + g4 + u >= p.m) z = -__builtin_huge_valf();
+                    else if (t == i * 16 + u) e.at_target[n] = z;
+                    acc[i][j][u] = z;
+                    top = fmaxf(top, z);
+                }
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            // a row without a finite score: its terms are exp(-inf) = 0, or not a number
+            const float ref = top == -__builtin_huge_valf() ? 0.f : top;
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) sum += exp2f((acc[i][j][u] - ref) * LOG2E);
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            if (lane < 16) joined[(wave % WM) * (WN * TN * 16) + (wave / WM) * (TN * 16) + j * 16 + lane] = make_float2(top, sum);
+        }
+        __syncthreads();
+        const int c = threadIdx.x;
+        const long long n = (long long)tn * (WN * TN * 16) + c;
+        if (c < WN * TN * 16 && n < p.n) {
+            float2 v = joined[c];
+#pragma unroll
+            for (int w = 1; w < WM; ++w) {
+                const float2 o = joined[w * (WN * TN * 16) + c];
+                join(v.x, v.y, o.x, o.y);
+            }
+            e.part[(long long)tm * p.n + n] = v;
+        }
+    }
+};
+
+// One workgroup of `width` x `height` threads: a row per column of threads; joins the parts in a fixed order.
+__global__ __launch_bounds__(256) void entropy_join_kernel(const float2 *__restrict__ part, int parts, long long rows,
+                                                           EntropyRow r, const float *__restrict__ at_target,
+                                                           float *__restrict__ loss, float *__restrict__ lse, int across)
+{
+    __shared__ float2 sums[256];
+    const int c = threadIdx.x % across, q = threadIdx.x / across, down = 256 / across;
+    const long long n = (long long)blockIdx.x * across + c;
+    float m = -__builtin_huge_valf(), s = 0.f;
+    if (n < rows)
+        for (int i = q; i < parts; i += down) {
+            const float2 v = part[(long long)i * rows + n];
+            join(m, s, v.x, v.y);
+        }
+    sums[threadIdx.x] = make_float2(m, s);
+    for (int half = down / 2; half > 0; half >>= 1) {
+        __syncthreads();
+        if (q < half) {
+            const float2 o = sums[threadIdx.x + half * across];
+            join(m, s, o.x, o.y);
+            sums[threadIdx.x] = make_float2(m, s);
+        }
+    }
+    if (q || n >= rows) return;
+    const float total = m + logf(s);
+    const int64_t t = r.target[n];
+    lse[n] = total;
+    // no target: no loss; a target outside the vocabulary: not a number
+    loss[n] = t < 0 ? 0.f : t >= r.vocab ? __builtin_nanf("") : total - at_target[n];
+}
+
+// Few rows: bound by reading W once.  A workgroup goes over a share of the words and leaves one pair per row.
+template <class T, int R, bool VEC>
+__global__ __launch_bounds__(256) void entropy_few_kernel(EntropyRow e, const T *__restrict__ x, const T *__restrict__ w,
+                                                          int rows, int k, float2 *__restrict__ part,
+                                                          float *__restrict__ at_target)
+{
+    __shared__ float2 joined[16][R];
+    const int group = threadIdx.x >> 4;
+    float m[R], s[R];
+    long long t[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        m[r] = -__builtin_huge_valf();
+        s[r] = 0.f;
+        t[r] = r < rows ? e.target[r] : -1;
+    }
+    for (long long f = ((long long)blockIdx.x * 16 + group) * 2; f < e.vocab; f += (long long)gridDim.x * 32) {
+        const bool two = f + 1 < e.vocab;
+        float sum[2][R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) sum[0][r] = sum[1][r] = 0.f;
+        few_rows_dot<T, R, VEC>(w + f * k, w + (two ? f + 1 : f) * k, x, rows, k, sum);
+        const float b0 = e.bias ? e.bias[f] : 0.f, b1 = e.bias && two ? e.bias[f + 1] : 0.f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float z0 = sum[0][r] * e.scale + b0, z1 = two ? sum[1][r] * e.scale + b1 : -__builtin_huge_valf();
+            if ((threadIdx.x & 15) == 0 && r < rows) {
+                if (t[r] == f) at_target[r] = z0;
+                if (t[r] == f + 1 && two) at_target[r] = z1;
+            }
+            const float top = fmaxf(m[r], fmaxf(z0, z1)), ref = top == -__builtin_huge_valf() ? 0.f : top;
+            s[r] = s[r] * exp2f((m[r] - ref) * LOG2E) + exp2f((z0 - ref) * LOG2E) + exp2f((z1 - ref) * LOG2E);
+            m[r] = top;
+        }
+    }
+    if ((threadIdx.x & 15) == 0)
+#pragma unroll
+        for (int r = 0; r < R; ++r) joined[group][r] = make_float2(m[r], s[r]);
+    __syncthreads();
+    if ((int)threadIdx.x < rows) {
+        float2 v = joined[0][threadIdx.x];
+        for (int g = 1; g < 16; ++g) join(v.x, v.y, joined[g][threadIdx.x].x, joined[g][threadIdx.x].y);
+        part[(long long)blockIdx.x * rows + threadIdx.x] = v;
+    }
+}
+
+// G of a piece of the vocabulary, in planes; optionally the sums over this tile's rows.
+template <int PLANES>
+struct EntropyGradient {
+    struct Args {
+        EntropyRow r;        // bias: of this piece
+        long long first;     // the piece's first word
+        const float *lse, *grad;
+        __bf16 *g;
+        long long ldg, plane;   // elements
+        float *sums;         // [tile of rows][word of the piece], nullable
+    };
+    template <int TM, int TN, int WM, int WN>
+    static __device__ void run(const Args &e, const ProductArgs &p, f32x4 (&acc)[TM][TN], long long m0, long long n0, int,
+                               char *lds, int tm, int tn)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g4 = 4 * (lane >> 4);
+        constexpr int BM = WM * TM * 16;
+        float *total = (float *)lds;   // [WN][BM]
+        const long long wide = (p.m + 7) & ~7LL;   // G is read in pieces of eight words
+        float lse[TN], grad[TN];
+        long long t[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const long long n = n0 + j * 16 + (lane & 15);
+            const bool in = n < p.n;
+            t[j] = in ? e.r.target[n] : -1;
+            lse[j] = in ? e.lse[n] : 0.f;
+            // a row without a target adds nothing, whatever it holds
+            grad[j] = in && t[j] >= 0 ? e.grad[n] : 0.f;
+            if (t[j] >= e.r.vocab) grad[j] = __builtin_nanf("");   // no such word
+            t[j] = t[j] < 0 ? -1 : t[j] - e.first;
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const long long m = m0 + i * 16 + g4;
+            f32x4 bias = {0.f, 0.f, 0.f, 0.f}, sum = {0.f, 0.f, 0.f, 0.f};
+            if (e.r.bias) bias = load_four(e.r.bias + m, (int)(p.m - m), false);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const long long n = n0 + j * 16 + (lane & 15);
+                f32x4 v;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const float z = acc[i][j][u] * e.r.scale + bias[u];
+                    float q = exp2f((z - lse[j]) * LOG2E);
+                    if (t[j] == m + u) q -= 1.f;
+                    v[u] = grad[j] == 0.f || m + u >= p.m ? 0.f : q * grad[j];
+                }
+                sum += v;
+                if (n >= p.n || m >= wide) continue;
+                __bf16 *at = e.g + n * e.ldg + m;
+                bf16x4 o[3];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    __bf16 a, b, c;
+                    if (PLANES == 3) {
+                        split_planes(v[u], a, b, c);
+                        o[1][u] = b;
+                        o[2][u] = c;
+                    } else {
+                        a = (__bf16)v[u];
+                    }
+                    o[0][u] = a;
+                }
+                *(bf16x4 *)at = o[0];
+                if (PLANES == 3) {
+                    *(bf16x4 *)(at + e.plane) = o[1];
+                    *(bf16x4 *)(at + 2 * e.plane) = o[2];
+                }
+            }
+            if (e.sums) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+#pragma unroll
+                    for (int o = 8; o > 0; o >>= 1) sum[u] += __shfl_xor(sum[u], o, 16);
+                    if ((lane & 15) == u) total[(wave / WM) * BM + (wave % WM) * (TM * 16) + i * 16 + g4 + u] = sum[u];
+                }
+            }
+        }
+        if (!e.sums) return;
+        __syncthreads();
+        const int c = threadIdx.x;
+        const long long m = (long long)tm * BM + c;
+        if (c < BM && m < p.m) {
+            float v = total[c];
+#pragma unroll
+            for (int w = 1; w < WN; ++w) v += total[w * BM + c];
+            e.sums[(long long)tn * p.m + m] = v;
+        }
+    }
+};
+
+// ---- host ---------------------------------------------------------------------
+
+constexpr int FEW_ROWS = 8, FEW_GROUPS = 1024;
+// G of a piece of the vocabulary takes at most this much of the workspace
+constexpr size_t PIECE_BYTES = (size_t)512 << 20;
+
+static bool entropy_args_fit(int64_t rows, int32_t vocab, int32_t dim, int32_t dtype)
+{
+    return rows >= 0 && rows <= MAX_ROWS && vocab >= 1 && vocab <= (int32_t)MAX_ROWS && dim >= 1 && dim <= MAX_WIDTH &&
+           (dtype == LCN_F32 || dtype == LCN_BF16);
+}
+static int few_groups(int32_t vocab)
+{
+    const int g = (vocab + 31) / 32;
+    return g < FEW_GROUPS ? g : FEW_GROUPS;
+}
+static const int TILE_M[TILE_COUNT] = {256, 128, 64, 320}, TILE_N[TILE_COUNT] = {256, 128, 64, 128};
+
+struct EntropySpace {
+    ProductPlan plan;         // of the scores
+    void *xp, *wp;
+    float2 *part;
+    float *at_target;
+    size_t bytes;
+};
+static EntropySpace entropy_space(char *ws, int64_t rows, int32_t vocab, int32_t dim, int32_t dtype)
+{
+    Carver c{ws};
+    EntropySpace f{};
+    f.at_target = (float *)c.take((size_t)rows * 4);
+    if (rows <= FEW_ROWS) {
+        f.part = (float2 *)c.take((size_t)few_groups(vocab) * rows * 8);
+    } else {
+        f.plan = plan_product(vocab, rows, dim, planes_of(dtype), false);
+        f.part = (float2 *)c.take((size_t)((vocab + TILE_M[f.plan.tile] - 1) / TILE_M[f.plan.tile]) * rows * 8);
+        f.xp = c.take(planes_bytes(rows, dim, dtype));
+        f.wp = c.take(planes_bytes(vocab, dim, dtype));
+    }
+    f.bytes = c.used;
+    return f;
+}
+
+struct EntropyBackward {
+    ProductPlan scores, dx, dw;   // for a piece
+    int32_t piece;                // words
+    void *xp, *xz, *wp, *g;       // xz: x with zeros in the rows without a target
+    float *part_dx, *part_dw, *sums;
+    size_t bytes;
+};
+static EntropyBackward entropy_backward_space(char *ws, int64_t rows, int32_t vocab, int32_t dim, int32_t dtype)
+{
+    Carver c{ws};
+    EntropyBackward b{};
+    const int planes = planes_of(dtype);
+    int64_t most = (int64_t)(PIECE_BYTES / ((size_t)rows * 2 * planes)) & ~(int64_t)255;
+    if (most < 256) most = 256;
+    const int64_t pieces = (vocab + most - 1) / most;
+    int64_t piece = ((vocab + pieces - 1) / pieces + 255) & ~(int64_t)255;   // pieces of about one size
+    if (piece > vocab) piece = vocab;
+    b.piece = (int32_t)piece;
+    b.scores = plan_product(piece, rows, dim, planes, false);
+    b.dx = plan_product(dim, rows, piece, planes, true);
+    b.dw = plan_product(dim, piece, rows, planes, true);
+    b.xp = c.take(planes_bytes(rows, dim, dtype));
+    b.xz = c.take(planes_bytes(rows, dim, dtype));
+    b.wp = c.take(planes_bytes(vocab, dim, dtype));
+    b.g = c.take(planes_bytes(rows, piece, dtype));
+    b.part_dx = (float *)c.take((size_t)b.dx.splits * rows * ((dim + 3) & ~3) * 4);
+    b.part_dw = (float *)c.take(partial_bytes(b.dw, dim, piece));
+    b.sums = (float *)c.take((size_t)((rows + TILE_N[b.scores.tile] - 1) / TILE_N[b.scores.tile]) * piece * 4);
+    b.bytes = c.used;
+    return b;
+}
+
+template <class T, int R>
+static hipError_t launch_few(const EntropyRow &e, const T *x, const T *w, int rows, int k, float2 *part, float *at_target,
+                             hipStream_t s)
+{
+    const unsigned grid = (unsigned)few_groups(e.vocab);
+    if (k % (16 / (int)sizeof(T)) == 0 && (((uintptr_t)x | (uintptr_t)w) & 15) == 0)
+        hipLaunchKernelGGL((entropy_few_kernel<T, R, true>), dim3(grid), dim3(256), 0, s, e, x, w, rows, k, part, at_target);
+    else
+        hipLaunchKernelGGL((entropy_few_kernel<T, R, false>), dim3(grid), dim3(256), 0, s, e, x, w, rows, k, part, at_target);
+    return hipGetLastError();
+}
+
+template <class T>
+static lcn_status entropy_as(const T *x, const T *w, const float *bias, const int64_t *target, int64_t rows, int32_t vocab,
+                             int32_t dim, int32_t dtype, float scale, float *loss, float *lse, char *ws, size_t ws_bytes,
+                             hipStream_t s)
+{
+    const EntropySpace f = entropy_space(ws, rows, vocab, dim, dtype);
+    if (!ws || ((uintptr_t)ws & 255) || ws_bytes < f.bytes) return LCN_ERR_ALLOC;
+    const EntropyRow e{bias, target, scale, vocab};
+    int parts, across;
+    if (rows <= FEW_ROWS) {
+        const int r = (int)rows;
+        hipError_t st = r == 1   ? launch_few<T, 1>(e, x, w, r, dim, f.part, f.at_target, s)
+                        : r == 2 ? launch_few<T, 2>(e, x, w, r, dim, f.part, f.at_target, s)
+                        : r <= 4 ? launch_few<T, 4>(e, x, w, r, dim, f.part, f.at_target, s)
+                                 : launch_few<T, 8>(e, x, w, r, dim, f.part, f.at_target, s);
+        OPCHK(st);
+        parts = few_groups(vocab);
+        across = 1;
+    } else {
+        ProductArgs p{};
+        OPCHK(operand_of(w, vocab, dim, dtype, f.wp, s, &p.a));
+        OPCHK(operand_of(x, rows, dim, dtype, f.xp, s, &p.b));
+        p.m = vocab;
+        p.n = (int)rows;
+        p.k = dim;
+        p.planes = planes_of(dtype);
+        OPCHK((launch_planned<false, false, EntropyForward>(f.plan, p, {e, f.part, f.at_target}, s)));
+        parts = (vocab + TILE_M[f.plan.tile] - 1) / TILE_M[f.plan.tile];
+        across = 16;
+    }
+    hipLaunchKernelGGL(entropy_join_kernel, dim3((unsigned)((rows + across - 1) / across)), dim3(256), 0, s, f.part, parts,
+                       (long long)rows, e, f.at_target, loss, lse, across);
+    OPCHK(hipGetLastError());
+    return LCN_OK;
+}
+
+template <int PLANES>
+static hipError_t launch_gradient(const ProductPlan &plan, const ProductArgs &p, const EntropyRow &r, long long first,
+                                  const float *lse, const float *grad, void *g, long long ldg, float *sums, hipStream_t s)
+{
+    return launch_planned<false, false, EntropyGradient<PLANES>>(plan, p,
+                                                                 {r, first, lse, grad, (__bf16 *)g, ldg, p.n * ldg, sums}, s);
+}
+
+static lcn_status entropy_backward_as(const void *x, const void *w, const float *bias, const int64_t *target, const float *lse,
+                                      const float *grad, int64_t rows, int32_t vocab, int32_t dim, int32_t dtype, float scale,
+                                      void *dx, void *dw, float *dbias, char *ws, size_t ws_bytes, hipStream_t s)
+{
+    const EntropyBackward b = entropy_backward_space(ws, rows, vocab, dim, dtype);
+    if (!ws || ((uintptr_t)ws & 255) || ws_bytes < b.bytes) return LCN_ERR_ALLOC;
+    const int planes = planes_of(dtype);
+    const size_t size = dtype == LCN_F32 ? 4 : 2;
+    Operand wo, xo, xz = plane_operand(b.xz, rows, dim);
+    OPCHK(operand_of(w, vocab, dim, dtype, b.wp, s, &wo));
+    OPCHK(operand_of(x, rows, dim, dtype, b.xp, s, &xo));
+    if (dw) OPCHK(launch_planes(x, rows, dim, dtype, target, b.xz, s));
+    const bool one = b.piece >= vocab;
+    for (int64_t first = 0; first < vocab; first += b.piece) {
+        const int words = (int)(vocab - first < b.piece ? vocab - first : b.piece);
+        const Operand here{(const char *)wo.p + first * wo.ld * 2, wo.plane, wo.ld};
+        const Operand g = plane_operand(b.g, rows, words);
+        const EntropyRow r{bias ? bias + first : nullptr, target, scale, vocab};
+        ProductArgs p{};
+        p.planes = planes;
+        p.a = here;
+        p.b = xo;
+        p.m = words;
+        p.n = (int)rows;
+        p.k = dim;
+        float *sums = dbias ? b.sums : nullptr;
+        if (planes == 3)
+            OPCHK((launch_gradient<3>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, s)));
+        else
+            OPCHK((launch_gradient<1>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, s)));
+        if (dbias) {
+            const int parts = (int)((rows + TILE_N[b.scores.tile] - 1) / TILE_N[b.scores.tile]);
+            OPCHK(launch_column_sums(sums, parts, words, LCN_F32, dbias + first, s));
+        }
+        p.m = dim;
+        if (dx) {   // G by rows x W by columns
+            p.a = here;
+            p.b = g;
+            p.n = (int)rows;
+            p.k = words;
+            if (one)
+                OPCHK((launch_scaled<true, false>(b.dx, p, scale, dtype, dx, b.part_dx, s)));
+            else
+                OPCHK(launch_partials(b.dx, p, b.part_dx, first > 0, s));
+        }
+        if (dw) {   // G by columns x x by columns
+            p.a = xz;
+            p.b = g;
+            p.n = words;
+            p.k = (int)rows;
+            OPCHK((launch_scaled<true, true>(b.dw, p, scale, dtype, (char *)dw + (size_t)first * dim * size, b.part_dw, s)));
+        }
+    }
+    if (dx && !one)
+        OPCHK(launch_add_partials(b.part_dx, b.dx.splits, rows, dim, (dim + 3) & ~3, scale, dtype, dx, s));
+    return LCN_OK;
+}
+
+}  // namespace lcn
+
+using namespace lcn;
+
+extern "C" {
+
+lcn_status lcn_cross_entropy_workspace_bytes(int64_t rows, int32_t vocab, int32_t dim, int32_t dtype, int32_t backward,
+                                             size_t *bytes)
+{
+    if (!bytes || !entropy_args_fit(rows, vocab, dim, dtype)) return LCN_ERR_INVALID_ARG;
+    *bytes = 0;
+    if (rows == 0) return LCN_OK;
+    *bytes = backward ? entropy_backward_space(nullptr, rows, vocab, dim, dtype).bytes
+                      : entropy_space(nullptr, rows, vocab, dim, dtype).bytes;
+    return LCN_OK;
+}
+
+lcn_status lcn_cross_entropy(const void *x, const void *W, const float *bias, const int64_t *target, int64_t rows,
+                             int32_t vocab, int32_t dim, int32_t dtype, float scale, float *loss, float *lse, void *workspace,
+                             size_t workspace_bytes, void *hip_stream)
+{
+    if (!entropy_args_fit(rows, vocab, dim, dtype) || !(scale - scale == 0.f)) return LCN_ERR_INVALID_ARG;
+    if (rows == 0) return LCN_OK;
+    if (!x || !W || !target || !loss || !lse) return LCN_ERR_INVALID_ARG;
+    if (dtype == LCN_F32)
+        return entropy_as((const float *)x, (const float *)W, bias, target, rows, vocab, dim, dtype, scale, loss, lse,
+                          (char *)workspace, workspace_bytes, (hipStream_t)hip_stream);
+    return entropy_as((const __bf16 *)x, (const __bf16 *)W, bias, target, rows, vocab, dim, dtype, scale, loss, lse,
+                      (char *)workspace, workspace_bytes, (hipStream_t)hip_stream);
+}
+
+lcn_status lcn_cross_entropy_backward(const void *x, const void *W, const float *bias, const int64_t *target, const float *lse,
+                                      const float *grad_loss, int64_t rows, int32_t vocab, int32_t dim, int32_t dtype,
+                                      float scale, void *dx, void *dW, float *dbias, void *workspace, size_t workspace_bytes,
+                                      void *hip_stream)
+{
+    if (!entropy_args_fit(rows, vocab, dim, dtype) || !(scale - scale == 0.f)) return LCN_ERR_INVALID_ARG;
+    if (!dx && !dW && !dbias) return LCN_OK;
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (rows == 0) {   // no rows: the parameters' gradients are zero
+        if (dW) OPCHK(launch_zero(dW, (size_t)vocab * dim * (dtype == LCN_F32 ? 4 : 2), s));
+        if (dbias) OPCHK(launch_zero(dbias, (size_t)vocab * 4, s));
+        return LCN_OK;
+    }
+    if (!x || !W || !target || !lse || !grad_loss) return LCN_ERR_INVALID_ARG;
+    return entropy_backward_as(x, W, bias, target, lse, grad_loss, rows, vocab, dim, dtype, scale, dx, dW, dbias,
+                               (char *)workspace, workspace_bytes, s);
+}
+
+}  // extern "C"

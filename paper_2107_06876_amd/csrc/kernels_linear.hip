@@ -1,0 +1,354 @@
+// y = act(x W^T + b) + r and its gradients.
+//
+// One product on the matrix instruction with everything else in its epilogue; the backward pass forms
+// dz = dy act'(z) once (as planes of bf16, with the column sums that are db), then dx = dz W and dW = dz^T x, whose operands
+// are read as they lie: a product takes either index of an operand as the contiguous one.
+//
+// Rounding: z, sums and activations are in 32 bits; with bf16 tensors y, dz, dx, dW and db are rounded once each, the kept
+// z is not (as bf16 it would add an error to dz of the size of dz's own rounding).
+#include "operators.h"
+
+namespace lcn {
+
+template <class T>
+struct LinearArgs {
+    const T *bias, *residual;
+    T *y;
+    float *pre;
+    int act, whole;   // whole: groups of four values of a row are aligned in y, residual, bias and pre
+};
+
+template <class T>
+__device__ __forceinline__ void linear_finish(const LinearArgs<T> &e, f32x4 z, f32x4 b, long long n, long long m, int width)
+{
+    const int left = (int)(width - m);
+    const long long at = n * width + m;
+    z += b;
+    if (e.pre) store_four(e.pre + at, z, left, e.whole);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) z[u] = activate(z[u], e.act);
+    if (e.residual) z += load_four(e.residual + at, left, e.whole);
+    store_four(e.y + at, z, left, e.whole);
+}
+
+template <class T>
+struct LinearEpilogue {
+    typedef LinearArgs<T> Args;
+    template <int TM, int TN, int WM, int WN>
+    static __device__ void run(const Args &e, const ProductArgs &p, f32x4 (&acc)[TM][TN], long long m0, long long n0, int,
+                               char *, int, int)
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const long long m = m0 + i * 16 + 4 * (lane >> 4);
+            if (m >= p.m) continue;
+            f32x4 b = {0.f, 0.f, 0.f, 0.f};
+            if (e.bias) b = load_four(e.bias + m, (int)(p.m - m), e.whole);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const long long n = n0 + j * 16 + (lane & 15);
+                if (n < p.n) linear_finish(e, acc[i][j], b, n, m, p.m);
+            }
+        }
+    }
+};
+
+// the epilogue of a product whose k was shared by workgroups
+template <class T>
+__global__ __launch_bounds__(256) void linear_finish_kernel(LinearArgs<T> e, const float *__restrict__ part, int splits,
+                                                            long long stride, long long rows, int width, long long ldp)
+{
+    const int per_row = (width + 3) / 4;
+    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < rows * per_row; t += (long long)gridDim.x * 256) {
+        const long long n = t / per_row;
+        const int m = (int)(t - n * per_row) * 4;
+        f32x4 z = *(const f32x4 *)(part + n * ldp + m), b = {0.f, 0.f, 0.f, 0.f};
+        for (int u = 1; u < splits; ++u) z += *(const f32x4 *)(part + u * stride + n * ldp + m);
+        if (e.bias) b = load_four(e.bias + m, width - m, e.whole);
+        linear_finish(e, z, b, n, m, width);
+    }
+}
+
+// Few rows: bound by reading W once; 16 lanes read a row of W, a wavefront eight rows.
+template <class T, int R, bool VEC>
+__global__ __launch_bounds__(256) void linear_few_kernel(LinearArgs<T> e, const T *__restrict__ x, const T *__restrict__ w,
+                                                         int rows, int k, int width)
+{
+    const int group = (int)(blockIdx.x * 16 + (threadIdx.x >> 4)), f = group * 2;
+    if (f >= width) return;
+    const int f1 = f + 1 < width ? f + 1 : f;
+    float sum[2][R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) sum[0][r] = sum[1][r] = 0.f;
+    few_rows_dot<T, R, VEC>(w + (long long)f * k, w + (long long)f1 * k, x, rows, k, sum);
+    // lane r * 2 + (which of the two rows of W) finishes one value
+    const int lane = threadIdx.x & 15, r = lane >> 1, which = lane & 1;
+    if (r >= rows || f + which >= width) return;
+    float z = 0.f;
+#pragma unroll
+    for (int u = 0; u < R; ++u)
+        if (u == r) z = which ? sum[1][u] : sum[0][u];
+    const long long at = (long long)r * width + f + which;
+    if (e.bias) z += (float)e.bias[f + which];
+    if (e.pre) e.pre[at] = z;
+    z = activate(z, e.act);
+    if (e.residual) z += (float)e.residual[at];
+    e.y[at] = (T)z;
+}
+
+template <class T, int R>
+static hipError_t launch_few(const LinearArgs<T> &e, const T *x, const T *w, int rows, int k, int width, hipStream_t s)
+{
+    const unsigned grid = (unsigned)((width + 31) / 32);
+    if (k % (16 / (int)sizeof(T)) == 0 && (((uintptr_t)x | (uintptr_t)w) & 15) == 0)
+        hipLaunchKernelGGL((linear_few_kernel<T, R, true>), dim3(grid), dim3(256), 0, s, e, x, w, rows, k, width);
+    else
+        hipLaunchKernelGGL((linear_few_kernel<T, R, false>), dim3(grid), dim3(256), 0, s, e, x, w, rows, k, width);
+    return hipGetLastError();
+}
+
+// dz = dy act'(z) as planes (dst: nullable), and the sums over this workgroup's rows for every column (part: nullable).
+// 32 pieces of eight columns x 8 rows at a time.
+template <class T>
+__global__ __launch_bounds__(256) void slope_kernel(const T *__restrict__ dy, const float *__restrict__ pre, long long rows,
+                                                    int width, int dp, int act, int rows_each, int whole,
+                                                    __bf16 *__restrict__ dst, float *__restrict__ part)
+{
+    __shared__ float sums[8][32][9];
+    const int c = threadIdx.x & 31, q = threadIdx.x >> 5, k = ((int)blockIdx.x * 32 + c) * 8;
+    const long long plane = rows * dp, r0 = (long long)blockIdx.y * rows_each;
+    float total[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) total[e] = 0.f;
+    if (k < dp)
+        for (long long r = r0 + q; r < r0 + rows_each && r < rows; r += 8) {
+            f32x4 v[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int left = width - k - 4 * h;
+                v[h] = load_four(dy + r * width + k + 4 * h, left, whole);
+                if (act != LCN_ACT_NONE) {
+                    const f32x4 z = load_four(pre + r * width + k + 4 * h, left, whole);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) v[h][u] *= activate_slope(z[u], act);
+                }
+            }
+            bf16x8 o[3];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                __bf16 a, b, d;
+                const float y = k + e < width ? v[e >> 2][e & 3] : 0.f;
+                total[e] += y;
+                split_planes(y, a, b, d);
+                o[0][e] = a;
+                o[1][e] = b;
+                o[2][e] = d;
+            }
+            if (dst) {
+                *(bf16x8 *)(dst + r * dp + k) = o[0];
+                if (sizeof(T) == 4) {
+                    *(bf16x8 *)(dst + plane + r * dp + k) = o[1];
+                    *(bf16x8 *)(dst + 2 * plane + r * dp + k) = o[2];
+                }
+            }
+        }
+    if (!part) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[q][c][e] = total[e];
+    __syncthreads();
+    // thread: column threadIdx.x of the 256
+    const int cc = threadIdx.x >> 3, e = threadIdx.x & 7, col = (int)blockIdx.x * 256 + threadIdx.x;
+    float v = 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v += sums[u][cc][e];
+    if (col < width) part[(long long)blockIdx.y * width + col] = v;
+}
+
+// ---- host ---------------------------------------------------------------------
+
+constexpr int FEW_ROWS = 8;
+
+static bool linear_args_fit(int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype)
+{
+    return rows >= 0 && rows <= MAX_ROWS && d_in >= 1 && d_in <= MAX_WIDTH && d_out >= 1 && d_out <= MAX_WIDTH &&
+           (dtype == LCN_F32 || dtype == LCN_BF16);
+}
+
+struct LinearForward {
+    void *xp, *wp;
+    float *part;
+    ProductPlan plan;
+    size_t bytes;
+};
+static LinearForward linear_forward_space(char *ws, int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype)
+{
+    Carver c{ws};
+    LinearForward f;
+    f.plan = plan_product(d_out, rows, d_in, planes_of(dtype), true);
+    f.xp = c.take(planes_bytes(rows, d_in, dtype));
+    f.wp = c.take(planes_bytes(d_out, d_in, dtype));
+    f.part = (float *)c.take(partial_bytes(f.plan, d_out, rows));
+    f.bytes = c.used;
+    return f;
+}
+
+struct LinearBackward {
+    void *xp, *wp, *dz;
+    float *part_dx, *part_dw, *sums;
+    ProductPlan dx, dw;
+    int groups, rows_each;
+    size_t bytes;
+};
+static LinearBackward linear_backward_space(char *ws, int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype)
+{
+    Carver c{ws};
+    LinearBackward b;
+    b.dx = plan_product(d_in, rows, d_out, planes_of(dtype), true);
+    b.dw = plan_product(d_in, d_out, rows, planes_of(dtype), true);
+    // enough workgroups to fill the chip, at most 256 partial sums per column
+    b.rows_each = (int)((((rows + 255) / 256) + 31) & ~31LL);
+    b.groups = (int)((rows + b.rows_each - 1) / b.rows_each);
+    b.xp = c.take(planes_bytes(rows, d_in, dtype));
+    b.wp = c.take(planes_bytes(d_out, d_in, dtype));
+    b.dz = c.take(planes_bytes(rows, d_out, dtype));
+    b.part_dx = (float *)c.take(partial_bytes(b.dx, d_in, rows));
+    b.part_dw = (float *)c.take(partial_bytes(b.dw, d_in, d_out));
+    b.sums = (float *)c.take((size_t)b.groups * d_out * 4);
+    b.bytes = c.used;
+    return b;
+}
+
+template <class T>
+static lcn_status linear_as(const T *x, const T *w, const T *bias, const T *residual, int64_t rows, int32_t d_in,
+                            int32_t d_out, int32_t dtype, int32_t act, T *y, float *pre, char *ws, size_t ws_bytes,
+                            hipStream_t s)
+{
+    LinearArgs<T> e{bias, residual, y, pre, act, 0};
+    if (rows <= FEW_ROWS) {
+        const int r = (int)rows;
+        hipError_t st = r == 1   ? launch_few<T, 1>(e, x, w, r, d_in, d_out, s)
+                        : r == 2 ? launch_few<T, 2>(e, x, w, r, d_in, d_out, s)
+                        : r <= 4 ? launch_few<T, 4>(e, x, w, r, d_in, d_out, s)
+                                 : launch_few<T, 8>(e, x, w, r, d_in, d_out, s);
+        OPCHK(st);
+        return LCN_OK;
+    }
+    const LinearForward f = linear_forward_space(ws, rows, d_in, d_out, dtype);
+    if (!ws || ((uintptr_t)ws & 255) || ws_bytes < f.bytes) return LCN_ERR_ALLOC;
+    const uintptr_t all = (uintptr_t)y | (uintptr_t)bias | (uintptr_t)residual;
+    e.whole = d_out % 4 == 0 && (all & (4 * sizeof(T) - 1)) == 0 && ((uintptr_t)pre & 15) == 0;
+    ProductArgs p{};
+    OPCHK(operand_of(w, d_out, d_in, dtype, f.wp, s, &p.a));
+    OPCHK(operand_of(x, rows, d_in, dtype, f.xp, s, &p.b));
+    p.m = d_out;
+    p.n = (int)rows;
+    p.k = d_in;
+    p.planes = planes_of(dtype);
+    if (f.plan.splits > 1) {
+        const long long ldp = (d_out + 3) & ~3LL, groups = (rows * (ldp / 4) + 255) / 256;
+        OPCHK((launch_planned<false, false, PartialEpilogue>(f.plan, p, {f.part, ldp, rows * ldp, 0}, s)));
+        hipLaunchKernelGGL(linear_finish_kernel<T>, dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(256), 0, s, e, f.part,
+                           f.plan.splits, rows * ldp, (long long)rows, d_out, ldp);
+        OPCHK(hipGetLastError());
+        return LCN_OK;
+    }
+    OPCHK((launch_planned<false, false, LinearEpilogue<T>>(f.plan, p, e, s)));
+    return LCN_OK;
+}
+
+template <class T>
+static lcn_status linear_backward_as(const T *x, const T *w, const float *pre, const T *dy, int64_t rows, int32_t d_in,
+                                     int32_t d_out, int32_t dtype, int32_t act, T *dx, T *dw, T *dbias, char *ws,
+                                     size_t ws_bytes, hipStream_t s)
+{
+    const LinearBackward b = linear_backward_space(ws, rows, d_in, d_out, dtype);
+    if (!ws || ((uintptr_t)ws & 255) || ws_bytes < b.bytes) return LCN_ERR_ALLOC;
+    const int planes = planes_of(dtype);
+    Operand dz = plane_operand(b.dz, rows, d_out);
+    const bool as_is = act == LCN_ACT_NONE && in_place(dy, d_out, dtype);
+    if (as_is) dz = Operand{dy, 0, d_out};
+    if (!as_is || dbias) {
+        const int dp = (int)padded(d_out);
+        const int whole = d_out % 4 == 0 && ((uintptr_t)dy & (4 * sizeof(T) - 1)) == 0 && ((uintptr_t)pre & 15) == 0;
+        hipLaunchKernelGGL(slope_kernel<T>, dim3((unsigned)((dp + 255) / 256), (unsigned)b.groups), dim3(256), 0, s, dy, pre,
+                           (long long)rows, d_out, dp, act, b.rows_each, whole, as_is ? nullptr : (__bf16 *)b.dz,
+                           dbias ? b.sums : nullptr);
+        OPCHK(hipGetLastError());
+        if (dbias) OPCHK(launch_column_sums(b.sums, b.groups, d_out, dtype, dbias, s));
+    }
+    ProductArgs p{};
+    p.planes = planes;
+    p.m = d_in;
+    if (dx) {
+        OPCHK(operand_of(w, d_out, d_in, dtype, b.wp, s, &p.a));
+        p.b = dz;
+        p.n = (int)rows;
+        p.k = d_out;
+        OPCHK((launch_scaled<true, false>(b.dx, p, 1.f, dtype, dx, b.part_dx, s)));
+    }
+    if (dw) {
+        OPCHK(operand_of(x, rows, d_in, dtype, b.xp, s, &p.a));
+        p.b = dz;
+        p.n = d_out;
+        p.k = (int)rows;
+        OPCHK((launch_scaled<true, true>(b.dw, p, 1.f, dtype, dw, b.part_dw, s)));
+    }
+    return LCN_OK;
+}
+
+}  // namespace lcn
+
+using namespace lcn;
+
+extern "C" {
+
+lcn_status lcn_linear_workspace_bytes(int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype, int32_t backward,
+                                      size_t *bytes)
+{
+    if (!bytes || !linear_args_fit(rows, d_in, d_out, dtype)) return LCN_ERR_INVALID_ARG;
+    *bytes = 0;
+    if (rows == 0 || (!backward && rows <= FEW_ROWS)) return LCN_OK;
+    *bytes = backward ? linear_backward_space(nullptr, rows, d_in, d_out, dtype).bytes
+                      : linear_forward_space(nullptr, rows, d_in, d_out, dtype).bytes;
+    return LCN_OK;
+}
+
+lcn_status lcn_linear(const void *x, const void *W, const void *bias, const void *residual, int64_t rows, int32_t d_in,
+                      int32_t d_out, int32_t dtype, int32_t activation, void *y, float *pre, void *workspace,
+                      size_t workspace_bytes, void *hip_stream)
+{
+    if (!linear_args_fit(rows, d_in, d_out, dtype) || activation < LCN_ACT_NONE || activation > LCN_ACT_SILU)
+        return LCN_ERR_INVALID_ARG;
+    if (rows == 0) return LCN_OK;
+    if (!x || !W || !y) return LCN_ERR_INVALID_ARG;
+    if (dtype == LCN_F32)
+        return linear_as((const float *)x, (const float *)W, (const float *)bias, (const float *)residual, rows, d_in, d_out,
+                         dtype, activation, (float *)y, pre, (char *)workspace, workspace_bytes, (hipStream_t)hip_stream);
+    return linear_as((const __bf16 *)x, (const __bf16 *)W, (const __bf16 *)bias, (const __bf16 *)residual, rows, d_in, d_out,
+                     dtype, activation, (__bf16 *)y, pre, (char *)workspace, workspace_bytes, (hipStream_t)hip_stream);
+}
+
+lcn_status lcn_linear_backward(const void *x, const void *W, const float *pre, const void *dy, int64_t rows, int32_t d_in,
+                               int32_t d_out, int32_t dtype, int32_t activation, void *dx, void *dW, void *dbias,
+                               void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (!linear_args_fit(rows, d_in, d_out, dtype) || activation < LCN_ACT_NONE || activation > LCN_ACT_SILU)
+        return LCN_ERR_INVALID_ARG;
+    if (!dx && !dW && !dbias) return LCN_OK;
+    hipStream_t s = (hipStream_t)hip_stream;
+    const size_t e = dtype == LCN_F32 ? 4 : 2;
+    if (rows == 0) {   // no rows: the parameters' gradients are zero
+        if (dW) OPCHK(launch_zero(dW, (size_t)d_in * d_out * e, s));
+        if (dbias) OPCHK(launch_zero(dbias, (size_t)d_out * e, s));
+        return LCN_OK;
+    }
+    if (!dy || (activation != LCN_ACT_NONE && !pre) || (dx && !W) || (dW && !x)) return LCN_ERR_INVALID_ARG;
+    if (dtype == LCN_F32)
+        return linear_backward_as((const float *)x, (const float *)W, pre, (const float *)dy, rows, d_in, d_out, dtype,
+                                  activation, (float *)dx, (float *)dW, (float *)dbias, (char *)workspace, workspace_bytes, s);
+    return linear_backward_as((const __bf16 *)x, (const __bf16 *)W, pre, (const __bf16 *)dy, rows, d_in, d_out, dtype,
+                              activation, (__bf16 *)dx, (__bf16 *)dW, (__bf16 *)dbias, (char *)workspace, workspace_bytes, s);
+}
+
+}  // extern "C"

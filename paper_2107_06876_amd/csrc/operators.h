@@ -1,0 +1,277 @@
+// Shared by the operators that produce and train the points: activations, planes of bf16, host-side choices.
+#pragma once
+
+#include "lcn_internal.h"
+#include "product.h"
+
+namespace lcn {
+
+// what the host takes for granted about sizes: offsets within a tile stay below 2^31 bytes
+constexpr int32_t MAX_WIDTH = 1 << 20;
+constexpr int64_t MAX_ROWS = (int64_t)1 << 30;
+
+template <class T>
+struct Four;   // four consecutive values, one load or store
+template <>
+struct Four<float> {
+    typedef f32x4 type;
+};
+template <>
+struct Four<__bf16> {
+    typedef bf16x4 type;
+};
+
+// Four consecutive values from `p` (only the first `left` exist) and back; `whole`: p is aligned to four values.
+template <class T>
+__device__ __forceinline__ f32x4 load_four(const T *p, int left, bool whole)
+{
+    f32x4 r = {0.f, 0.f, 0.f, 0.f};
+    if (whole && left >= 4) {
+        const typename Four<T>::type v = *(const typename Four<T>::type *)p;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = (float)v[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) r[e] = (float)p[e];
+    }
+    return r;
+}
+template <class T>
+__device__ __forceinline__ void store_four(T *p, f32x4 v, int left, bool whole)
+{
+    if (whole && left >= 4) {
+        typename Four<T>::type o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = (T)v[e];
+        *(typename Four<T>::type *)p = o;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) p[e] = (T)v[e];
+    }
+}
+
+// x as the sum of three bf16 (to 2^-26).  A value beyond the largest bf16 is cut, not rounded to infinity; what
+// is not finite stands in the first plane alone.
+__device__ __forceinline__ void split_planes(float x, __bf16 &a, __bf16 &b, __bf16 &c)
+{
+    a = (__bf16)x;
+    const float whole = __builtin_fabsf(x);
+    if (__builtin_isinf((float)a) && whole < __builtin_huge_valf())
+        a = __builtin_bit_cast(__bf16, (unsigned short)(__builtin_bit_cast(unsigned, x) >> 16));
+    float r = x - (float)a;
+    if (!(whole < __builtin_huge_valf())) r = 0.f;
+    b = (__bf16)r;
+    c = (__bf16)(r - (float)b);
+}
+
+__device__ __forceinline__ float activate(float z, int act)
+{
+    switch (act) {
+    case LCN_ACT_TANH: return tanhf(z);
+    case LCN_ACT_RELU: return z > 0.f ? z : z == z ? 0.f : z;
+    case LCN_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    case LCN_ACT_SILU: return z / (1.f + expf(-z));
+    default: return z;
+    }
+}
+__device__ __forceinline__ float activate_slope(float z, int act)
+{
+    switch (act) {
+    case LCN_ACT_TANH: {
+        const float t = tanhf(z);
+        return 1.f - t * t;
+    }
+    case LCN_ACT_RELU: return z > 0.f ? 1.f : z == z ? 0.f : z;
+    case LCN_ACT_GELU:
+        return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+    case LCN_ACT_SILU: {
+        const float f = 1.f / (1.f + expf(-z));
+        return f * (1.f + z * (1.f - f));
+    }
+    default: return 1.f;
+    }
+}
+
+// ---- planes (kernels_planes.hip) --------------------------------------------
+inline long long padded(long long d) { return (d + 7) & ~7LL; }
+inline int planes_of(int32_t dtype) { return dtype == LCN_F32 ? 3 : 1; }
+// bytes of an operand of rows x d in planes
+inline size_t planes_bytes(long long rows, long long d, int32_t dtype)
+{
+    return ((size_t)rows * (size_t)padded(d) * 2 * planes_of(dtype) + 255) & ~(size_t)255;
+}
+// Whether a bf16 matrix can be an operand as it lies: rows of whole 16-byte pieces, aligned.
+inline bool in_place(const void *p, long long d, int32_t dtype)
+{
+    return dtype == LCN_BF16 && d % 8 == 0 && ((uintptr_t)p & 15) == 0;
+}
+// rows x d of `dtype` into planes at dst, rows padded with zeros to a multiple of 8; rows whose `target` is negative
+// become zero (target: nullable).
+hipError_t launch_planes(const void *src, long long rows, int d, int32_t dtype, const int64_t *target, void *dst,
+                         hipStream_t s);
+Operand plane_operand(const void *dst, long long rows, long long d);
+// the operand of a matrix: as it lies, or its planes at `space`
+hipError_t operand_of(const void *p, long long rows, int d, int32_t dtype, void *space, hipStream_t s, Operand *o);
+
+// out[n][m] (dtype, m dense, width m) = scale * the sum of `splits` partial products (float, [split][n][ldp])
+hipError_t launch_add_partials(const float *part, int splits, long long n, int m, long long ldp, float scale, int32_t dtype,
+                               void *out, hipStream_t s);
+
+// ---- host-side choice of a product's tile and split --------------------------
+struct ProductPlan {
+    int tile;      // index of the tile shape, see launch_planned
+    int splits;
+};
+ProductPlan plan_product(long long m, long long n, long long k, int planes, bool may_split);
+
+// A float product's partial sums: [split][n][ldp]; `add` adds to what is there.
+struct PartialEpilogue {
+    struct Args {
+        float *part;
+        long long ldp, stride;   // elements from a row, from a split to the next
+        int add;
+    };
+    template <int TM, int TN, int WM, int WN>
+    static __device__ void run(const Args &e, const ProductArgs &p, f32x4 (&acc)[TM][TN], long long m0, long long n0,
+                               int split, char *, int, int)
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const long long n = n0 + j * 16 + (lane & 15);
+            if (n >= p.n) continue;
+            float *row = e.part + split * e.stride + n * e.ldp;
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const long long m = m0 + i * 16 + 4 * (lane >> 4);
+                if (m >= p.m) continue;   // ldp is a multiple of 4: a group of four is inside the row
+                f32x4 v = acc[i][j];
+                if (e.add) v += *(f32x4 *)(row + m);
+                *(f32x4 *)(row + m) = v;
+            }
+        }
+    }
+};
+
+// scale * the product, rounded to T, at out[n][m]
+template <class T>
+struct ScaledEpilogue {
+    struct Args {
+        T *out;
+        long long ld;
+        float scale;
+        int whole;   // rows start aligned to four values
+    };
+    template <int TM, int TN, int WM, int WN>
+    static __device__ void run(const Args &e, const ProductArgs &p, f32x4 (&acc)[TM][TN], long long m0, long long n0, int,
+                               char *, int, int)
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const long long n = n0 + j * 16 + (lane & 15);
+            if (n >= p.n) continue;
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const long long m = m0 + i * 16 + 4 * (lane >> 4);
+                if (m >= p.m) continue;
+                store_four(e.out + n * e.ld + m, acc[i][j] * e.scale, (int)(p.m - m), e.whole);
+            }
+        }
+    }
+};
+
+// Tile shapes: index -> BM x BN.  256 x 256 has the best rate; the smaller ones fill the chip where the result is
+// small, 320 x 128 keeps a row of up to 320 values in one tile.
+enum { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2, TILE_320 = 3, TILE_COUNT = 4 };
+template <bool ACOL, bool BCOL, class Epi>
+hipError_t launch_planned(const ProductPlan &plan, ProductArgs p, const typename Epi::Args &e, hipStream_t s)
+{
+    p.splits = plan.splits;
+    switch (plan.tile) {
+    case TILE_256: return launch_product<256, 256, 2, 4, ACOL, BCOL, Epi>(p, e, s);
+    case TILE_320: return launch_product<320, 128, 4, 2, ACOL, BCOL, Epi>(p, e, s);
+    case TILE_128: return launch_product<128, 128, 2, 2, ACOL, BCOL, Epi>(p, e, s);
+    default: return launch_product<64, 64, 2, 2, ACOL, BCOL, Epi>(p, e, s);
+    }
+}
+
+// out[n][m] = scale * product, in one launch or as partial sums in `part` that a second launch adds up.
+template <bool ACOL, bool BCOL>
+hipError_t launch_scaled(const ProductPlan &plan, const ProductArgs &p, float scale, int32_t dtype, void *out, float *part,
+                         hipStream_t s);
+
+// The partial sums alone, A by columns and B by rows; `add`: to what is in `part`.
+hipError_t launch_partials(const ProductPlan &plan, const ProductArgs &p, float *part, int add, hipStream_t s);
+// out[c] (dtype) = sum over r of part[r][c], r = 0 .. parts - 1
+hipError_t launch_column_sums(const float *part, int parts, int width, int32_t dtype, void *out, hipStream_t s);
+// zeros, by a kernel
+hipError_t launch_zero(void *p, size_t bytes, hipStream_t s);
+inline size_t partial_bytes(const ProductPlan &plan, long long m, long long n)
+{
+    return plan.splits > 1 ? (size_t)plan.splits * (size_t)n * (size_t)((m + 3) & ~3LL) * 4 : 0;
+}
+
+// ---- products with few rows: 16 lanes per row of W ---------------------------
+// sums[f][r] += W[f] . x[r] for two rows of W per group of 16 lanes and R rows of x (`rows` of them exist); every lane of
+// the group gets the sums.  Sums are in 32 bits.  VEC: rows of W and x are whole aligned 16-byte pieces.
+template <class T, int R, bool VEC>
+__device__ __forceinline__ void few_rows_dot(const T *__restrict__ w0, const T *__restrict__ w1, const T *__restrict__ x,
+                                             int rows, int k, float (&sum)[2][R])
+{
+    constexpr int V = VEC ? 16 / (int)sizeof(T) : 1;
+    typedef T piece __attribute__((ext_vector_type(V)));
+    const int lane = threadIdx.x & 15;
+#pragma unroll 4
+    for (int c = lane * V; c < k; c += 16 * V) {
+        piece a, b, y[R];
+        if constexpr (VEC) {
+            a = *(const piece *)(w0 + c);
+            b = *(const piece *)(w1 + c);
+#pragma unroll
+            for (int r = 0; r < R; ++r) y[r] = *(const piece *)(x + (long long)(r < rows ? r : 0) * k + c);
+        } else {
+            a[0] = w0[c];
+            b[0] = w1[c];
+#pragma unroll
+            for (int r = 0; r < R; ++r) y[r][0] = x[(long long)(r < rows ? r : 0) * k + c];
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                sum[0][r] += (float)a[e] * (float)y[r][e];
+                sum[1][r] += (float)b[e] * (float)y[r][e];
+            }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) sum[f][r] += __shfl_xor(sum[f][r], o, 16);
+}
+
+// part of the workspace: hands out 256-byte aligned pieces, or only counts them
+struct Carver {
+    char *base;
+    size_t used = 0;
+    void *take(size_t bytes)
+    {
+        void *r = base ? base + used : nullptr;
+        used += (bytes + 255) & ~(size_t)255;
+        return r;
+    }
+};
+
+#define OPCHK(call)                         \
+    do {                                    \
+        if ((call) != hipSuccess) {         \
+            (void)hipGetLastError();        \
+            return LCN_ERR_DEVICE;          \
+        }                                   \
+    } while (0)
+
+}  // namespace lcn

@@ -1,0 +1,248 @@
+// Matrix products of the embedding operators on the bf16 matrix instruction: the sum over k of A[m][k] B[n][k],
+// both operands in memory as planes of bf16, with an epilogue that reads the accumulators in registers.
+//
+// bf16 inputs are one plane.  A float x is three: x1 = bf16(x), x2 = bf16(x - x1), x3 = bf16(x - x1 - x2); what is left
+// is below 2^-26 |x|.  Of the nine products of planes the six with x_i y_j, i + j <= 4, are added (the others are below
+// 2^-25 of the product), the small ones first.  Six bf16 products cost less than one on the fp32 matrix instruction,
+// whose rate is 1/16.
+//
+// An operand is stored either with k contiguous (`rows`: A[m][k] at m * ld + k) or with its own index contiguous
+// (`columns`: A[k][m] at k * ld + m).  Tiles of 64 values of k go from memory straight into LDS (16 bytes a lane; what is
+// outside the operand is read as zero by the buffer's bounds), two tiles of LDS in turn, so that the next tile is on its
+// way while the matrix instructions work on this one.  The 16-byte pieces of a tile are permuted so that neither the
+// 128-bit reads of `rows` tiles nor the transposing 64-bit reads of `columns` tiles meet in a bank.
+//
+// The accumulators' row index (four consecutive values in a lane) is m: outputs are stored with m contiguous.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace lcn {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+struct Operand {
+    const void *p;     // first plane, 16-byte aligned
+    long long plane;   // bytes from one plane to the next
+    long long ld;      // elements from a row (`rows`) or a k (`columns`) to the next, a multiple of 8
+};
+
+struct ProductArgs {
+    Operand a, b;
+    int m, n, k;         // k is padded by zeros up to a multiple of 8 in `rows` operands
+    int planes;          // 1 or 3
+    int splits;          // workgroups that share a tile's k
+    int tiles_m, tiles_n;
+};
+
+enum { STEP_K = 64 };   // values of k per tile in LDS
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// permutation of the 16-byte pieces of a tile: of row r (`rows`), of value k (`columns`, W indices wide)
+__device__ __forceinline__ int rows_swizzle(int r) { return (r >> 1) & 7; }
+template <int W>
+__device__ __forceinline__ int columns_swizzle(int k)
+{
+    if (W % 128 == 0) return ((k & 3) | ((k >> 1) & 4)) << 1;
+    return (((k >> 1) & 1) | ((k >> 2) & 2)) << 1;
+}
+
+// One operand's part of the tiles of a workgroup: W indices from i0, 64 values of k at a time, into LDS.
+template <int W, bool COLUMNS, int THREADS>
+struct TileLoader {
+    static constexpr int LOADS = W * 8 / THREADS;   // 16-byte pieces per thread
+    static_assert(W * 8 % THREADS == 0, "a whole number of pieces per thread");
+    const char *first;        // the workgroup's first index, k = 0, first plane
+    long long k_bytes;        // from one tile's k to the next
+    unsigned row_bytes, tail; // from a row to the next; bytes of the last row that are read
+    int rows;                 // `rows`: rows there are; `columns`: left for the call
+    unsigned off[LOADS];
+    int need[LOADS];          // `rows`: values of k the piece needs to be left
+
+    __device__ __forceinline__ void init(const Operand &o, long long i0, int count, int wave, int lane)
+    {
+        const int left = count - (int)i0;
+        row_bytes = (unsigned)(o.ld * 2);
+        first = (const char *)o.p + (COLUMNS ? i0 : i0 * o.ld) * 2;
+        k_bytes = COLUMNS ? (long long)STEP_K * o.ld * 2 : STEP_K * 2;
+        rows = left < W ? left : W;
+        tail = (unsigned)(((left + 7) & ~7) * 2);
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) {
+            const int c = (u * (THREADS / 64) + wave) * 64 + lane;
+            if (!COLUMNS) {
+                const int row = c >> 3, piece = (c & 7) ^ rows_swizzle(row);
+                off[u] = (unsigned)row * row_bytes + (unsigned)piece * 16;
+                need[u] = piece * 8;
+            } else {
+                const int kk = c / (W / 8), piece = (c % (W / 8)) ^ columns_swizzle<W>(kk);
+                off[u] = piece * 8 < left ? (unsigned)kk * row_bytes + (unsigned)piece * 16 : 0x80000000u;
+            }
+        }
+    }
+    // tile number `step` of the plane that lies `plane` bytes behind the first; k: all values of k
+    __device__ __forceinline__ void load(long long plane, int step, int k, char *lds, int wave) const
+    {
+        const int left = k - step * STEP_K;
+        const char *base = first + plane + step * k_bytes;
+        const int r = COLUMNS ? (left < STEP_K ? left : STEP_K) : rows;
+        const unsigned end = COLUMNS ? tail : (unsigned)(((left + 7) & ~7) * 2);
+        __amdgpu_buffer_rsrc_t res =
+            __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (unsigned)(r - 1) * row_bytes + end, 0x00020000);
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) {
+            unsigned o = off[u];
+            if (!COLUMNS) o = need[u] < left ? o : 0x80000000u;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (lds_void *)(lds + (u * (THREADS / 64) + wave) * 1024), 16, (int)o,
+                                                     0, 0, 0);
+        }
+    }
+};
+
+// The matrix instruction's operand for indices i .. i + 15 (i a multiple of 16) and the 32 values of k from 32 kk: lane l
+// has index i + l % 16 and k = 32 kk + 8 (l / 16) + 0 .. 7.  `at` is the lane's place for i = 0 and kk = 0.
+template <int W, bool COLUMNS>
+__device__ __forceinline__ int fragment_place(int lane)
+{
+    if constexpr (!COLUMNS) {
+        return (lane & 15) * 128 + (((lane >> 4) ^ rows_swizzle(lane & 15)) << 4);
+    } else {
+        // a group of 16 lanes reads 4 values of k x 16 indices, each lane 4 indices of one k, and gets 4 values of
+        // k of one index; the second read is 4 values of k further
+        const int k = (lane >> 4) * 8 + ((lane & 15) >> 2);
+        return k * (W * 2) + ((((lane & 3) >> 1) ^ columns_swizzle<W>(k)) << 4) + (lane & 1) * 8;
+    }
+}
+template <int W, bool COLUMNS>
+__device__ __forceinline__ bf16x8 load_fragment(const char *lds, int at, int i, int kk)
+{
+    if constexpr (!COLUMNS) {
+        return *(const bf16x8 *)(lds + (at ^ (kk * 64)) + i * 128);
+    } else {
+        union {
+            s16x4 h[2];
+            bf16x8 v;
+        } f;
+        static_assert(W % 64 == 0, "a row of the tile is whole units of 128 bytes");
+        constexpr int LOW = W % 128 == 0 ? 255 : 127;   // what the permutation moves within
+        const char *q = lds + (at ^ (i * 2 & LOW)) + (i * 2 & ~LOW) + kk * 32 * (W * 2);
+        f.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)q);
+        f.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(q + 4 * (W * 2)));
+        return f.v;
+    }
+}
+
+// The tile that a workgroup works on.  Workgroups are dealt to the eight dies in turn: a die gets a run of
+// consecutive tiles, and tiles follow each other in strips of four along n, so that the tiles in flight on a die share
+// their operands in its cache.
+__device__ __forceinline__ void tile_of(const ProductArgs &p, int id, int &tm, int &tn)
+{
+    const int total = p.tiles_m * p.tiles_n;
+    const int base = total / 8, more = total % 8, die = id % 8, nth = id / 8;
+    const int t = die * base + (die < more ? die : more) + nth;
+    const int strip = t / (4 * p.tiles_m), in = t % (4 * p.tiles_m);
+    const int wide = p.tiles_n - strip * 4 < 4 ? p.tiles_n - strip * 4 : 4;
+    tm = in / wide;
+    tn = strip * 4 + in % wide;
+}
+
+// WM x WN wavefronts of 64, each BM/WM x BN/WN of the tile.  Epi: struct with Args and
+// run<TM, TN>(args, product args, acc, m0, n0, split, lds) for the wavefront's accumulators.
+template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, class Epi>
+__global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs p, typename Epi::Args e)
+{
+    constexpr int THREADS = WM * WN * 64, TM = BM / WM / 16, TN = BN / WN / 16;
+    constexpr int ABYTES = BM * STEP_K * 2, BBYTES = BN * STEP_K * 2;
+    __shared__ __align__(1024) char lds0[ABYTES + BBYTES];
+    __shared__ __align__(1024) char lds1[ABYTES + BBYTES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int tm, tn;
+    tile_of(p, blockIdx.x, tm, tn);
+    const long long m0 = (long long)tm * BM, n0 = (long long)tn * BN;
+    const int wm = (wave % WM) * (BM / WM), wn = (wave / WM) * (BN / WN);
+
+    const int at_a = fragment_place<BM, ACOL>(lane), at_b = fragment_place<BN, BCOL>(lane);
+    f32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    const int ksteps = (p.k + STEP_K - 1) / STEP_K, pairs = p.planes == 3 ? 6 : 1;
+    const int all = ksteps * pairs, per = (all + p.splits - 1) / p.splits;
+    const int first = (int)blockIdx.y * per, last = first + per < all ? first + per : all;
+
+    TileLoader<BM, ACOL, THREADS> load_a;
+    TileLoader<BN, BCOL, THREADS> load_b;
+    load_a.init(p.a, m0, p.m, wave, lane);
+    load_b.init(p.b, n0, p.n, wave, lane);
+    int pair = first / ksteps, step = first - pair * ksteps;   // of the next fetch
+    auto fetch = [&](char *lds) {
+        long long ia = 0, ib = 0;
+        if (pairs > 1) {   // pairs of planes: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
+            ia = (0x001012 >> (4 * pair)) & 3;
+            ib = (0x010210 >> (4 * pair)) & 3;
+        }
+        load_a.load(ia * p.a.plane, step, p.k, lds, wave);
+        load_b.load(ib * p.b.plane, step, p.k, lds + ABYTES, wave);
+        if (++step == ksteps) {
+            step = 0;
+            ++pair;
+        }
+    };
+    auto work = [&](const char *lds) {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            bf16x8 a[TM], b[TN];
+#pragma unroll
+            for (int i = 0; i < TM; ++i) a[i] = load_fragment<BM, ACOL>(lds, at_a, wm + i * 16, kk);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) b[j] = load_fragment<BN, BCOL>(lds + ABYTES, at_b, wn + j * 16, kk);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
+        }
+    };
+    auto arrived = [&]() {   // this wavefront's loads are in LDS, and so are all others'
+        __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+        __syncthreads();
+    };
+    if (first < last) {
+        fetch(lds0);
+        int t = first;
+        for (; t + 2 <= last; t += 2) {
+            arrived();
+            fetch(lds1);
+            work(lds0);
+            arrived();
+            if (t + 2 < last) fetch(lds0);
+            work(lds1);
+        }
+        if (t < last) {
+            arrived();
+            work(lds0);
+        }
+    }
+    __syncthreads();
+    Epi::template run<TM, TN, WM, WN>(e, p, acc, m0 + wm, n0 + wn, (int)blockIdx.y, lds0, tm, tn);
+}
+
+template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, class Epi>
+hipError_t launch_product(ProductArgs p, const typename Epi::Args &e, hipStream_t s)
+{
+    p.tiles_m = (p.m + BM - 1) / BM;
+    p.tiles_n = (p.n + BN - 1) / BN;
+    hipLaunchKernelGGL((product_kernel<BM, BN, WM, WN, ACOL, BCOL, Epi>), dim3((unsigned)(p.tiles_m * p.tiles_n), p.splits),
+                       dim3(WM * WN * 64), 0, s, p, e);
+    return hipGetLastError();
+}
+
+}  // namespace lcn
