@@ -429,6 +429,54 @@ lcn_status lcn_cross_entropy_backward(const void *x, const void *W, const float 
                                       float scale, void *dx, void *dW, float *dbias, void *workspace, size_t workspace_bytes,
                                       void *hip_stream);
 
+/* Attention inside the sets of a ragged batch.  Set p owns queries q_off[p] .. q_off[p+1]
+ * of q and keys k_off[p] .. k_off[p+1] of k and v (the x_off / y_off of a
+ * lcn_batch_desc, on the device); with nq queries and nk keys, query i of a set has
+ * position i + nk - nq (the last query stands at the last key), and its score
+ * for key j of the same set is
+ *   z = scale q_i . k_j;      cap > 0: z = cap tanh(z / cap);
+ *   slopes: z = z - slopes[head] |position - j|;
+ *   causal: keys with j > position and j >= prefix[p] are not seen.
+ * o_i = sum_j softmax(z)_ij v_j and lse_i = log sum_j exp z_ij; a query that sees no
+ * key has o = 0 and lse = -inf, and no gradient.  Query head h reads key head
+ * h / (heads / kv_heads).  A key that a query does not see has no weight, but
+ * its v (and in the backward pass its k, and a query's q and dy) must be finite
+ * where another token of the set sees it; tokens of other sets may hold anything.
+ *   q       total_q x heads x head_dim;  k, v  total_k x kv_heads x head_dim, by
+ *           the strides given (in elements, 0: dense, at most 2^22; the values of
+ *           a head are contiguous); o, dy and the gradients are dense
+ *   lse     fp32, heads x total_q
+ * Sets may be empty.  Offsets that are not in order or outside 0 .. total are cut
+ * to what exists; queries in no set are not written.  Sizes: num_sets <= 2^24,
+ * heads <= 1024 and a multiple of kv_heads, head_dim <= 128, totals <= 2^30.
+ * slopes are constants (they get no gradient). */
+typedef struct {
+    int32_t num_sets, heads, kv_heads, head_dim;
+    int32_t dtype;            /* lcn_dtype of q, k, v, o and their gradients */
+    int32_t causal;           /* 0 or 1 */
+    float scale;              /* usually 1 / sqrt(head_dim) */
+    float cap;                /* >= 0; 0: none */
+    int64_t total_q, total_k; /* tokens in q and in k, v */
+    int64_t max_q;            /* the largest number of queries of a set where the caller knows it, else 0: with
+                                 few queries per set the keys are then split over workgroups.  A set must
+                                 not have more (what is beyond is not written) */
+    const int64_t *q_off, *k_off; /* device, num_sets + 1 each */
+    const int32_t *prefix;    /* device, num_sets, nullable (0); read if causal */
+    const float *slopes;      /* device, heads, nullable */
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head; /* strides in elements */
+} lcn_attention_desc;
+lcn_status lcn_attention_workspace_bytes(const lcn_attention_desc *desc, int32_t backward, size_t *bytes);
+lcn_status lcn_attention(const lcn_attention_desc *desc, const void *q, const void *k, const void *v, void *o, float *lse,
+                         void *workspace, size_t workspace_bytes, void *hip_stream);
+/* Gradients for a given dy (the gradient of o, dense as o), from the o and lse of the
+ * forward call:  dv = P^T dy,  dS = P .* (dy v^T - rowsum(dy .* o)) (times the cap's
+ * derivative),  dq = scale dS k,  dk = scale dS^T q, dk and dv summed over the
+ * query heads of a key head.  dq, or dk and dv together, may be NULL.  Gradients
+ * of tokens in no set are not written. */
+lcn_status lcn_attention_backward(const lcn_attention_desc *desc, const void *q, const void *k, const void *v, const void *o,
+                                  const float *lse, const void *dy, void *dq, void *dk, void *dv, void *workspace,
+                                  size_t workspace_bytes, void *hip_stream);
+
 void lcn_destroy(lcn_handle h); /* frees host memory only; the workspace is the caller's */
 const char *lcn_status_string(int32_t status);
 

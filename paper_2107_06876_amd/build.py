@@ -27,6 +27,9 @@ SOURCES = {
     "kernels_planes.hip": [],
     "kernels_linear.hip": [],
     "kernels_entropy.hip": [],
+    "kernels_attention_f32.hip": [],
+    "kernels_attention_bf16.hip": [],
+    "attention_api.hip": [],
     "lcn_api.hip": [],
     "calibrate.hip": [],
 }

@@ -1,0 +1,649 @@
+// Attention inside the sets of a ragged batch: forward, and the gradients of q, k and v.
+//
+// For query i and key j of a set (nq queries, nk keys; a query's position is i + nk - nq, so the last query stands at the
+// last key):  z = scale q_i . k_j;  with a cap c: z = c tanh(z / c);  with a slope of the head: z -= slope |position - j|;
+// causal: only j <= position, or j < prefix.  o_i = sum_j softmax(z)_ij v_j,  lse_i = log sum_j exp z_ij.
+//
+// Layout: the matrix instruction's accumulator has its column in lane % 16 and rows 4 (lane / 16) + 0 .. 3.  Scores are formed
+// with keys as rows (forward, dq) or queries as rows (dk, dv), so that two accumulators, converted, ARE the right-hand
+// operand of the next product: the 32 values of its k are keys 4 g + 0 .. 3 and 16 + 4 g + 0 .. 3 in lane group g, and the
+// left-hand operand is read from LDS in the same order, transposed by the reads.  Scores never pass through LDS, and a
+// query's maximum and sum are in its own lanes.
+//
+// bf16 tensors use the 16x16x32 bf16 instruction, float ones eight 16x16x4 float instructions on the same registers.
+// Scores, statistics, sums and dS are in 32 bits; P and dS are rounded to the tensors' type where they enter a product.
+#pragma once
+
+#include "operators.h"
+
+namespace lcn {
+
+struct AttentionArgs {
+    const void *q, *k, *v;
+    const int64_t *q_off, *k_off;
+    const int32_t *prefix;      // nullable
+    const float *slopes;        // nullable
+    long long q_token, q_head, k_token, k_head, v_token, v_head;   // strides in elements
+    long long total_q, total_k;
+    int sets, heads, kv_heads, dim;
+    int causal;
+    float scale, cap;
+    int tiles;                  // of queries (forward, dq) or keys (dk, dv), over all sets
+    // forward
+    void *o;
+    float *lse;                 // [head][query]
+    // backward
+    const void *d_o;
+    const float *lse_in, *delta;
+    void *dq, *dk, *dv;
+};
+
+template <class T>
+struct Frag;
+template <>
+struct Frag<__bf16> {
+    typedef bf16x8 type;
+};
+template <>
+struct Frag<float> {
+    typedef float type __attribute__((ext_vector_type(8)));
+};
+
+__device__ __forceinline__ void mma(f32x4 &c, bf16x8 a, bf16x8 b) { c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ void mma(f32x4 &c, Frag<float>::type a, Frag<float>::type b)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+}
+
+// A tile in LDS: ROWS rows of DP values, in pieces of 16 bytes permuted so that neither 16 rows' pieces of one place nor
+// the transposing reads of eight rows meet in a bank.
+template <class T, int DP>
+struct Tile {
+    static constexpr int PITCH = DP * (int)sizeof(T), PIECES = PITCH / 16, EACH = 16 / (int)sizeof(T);
+    static __device__ __forceinline__ int swizzle(int r)
+    {
+        if (PIECES >= 16) return ((r & 7) << 1) | ((r >> 3) & 1);
+        if (PIECES == 8) return (((r >> 1) & 3) << 1) | ((r >> 3) & 1);
+        return (((r >> 2) & 1) << 1) | ((r >> 3) & 1);
+    }
+    static __device__ __forceinline__ int place(int r, int piece) { return r * PITCH + ((piece ^ swizzle(r)) << 4); }
+
+    // rows r0 .. r0 + 15 (lane % 16), values 32 c + 8 (lane / 16) + 0 .. 7
+    static __device__ __forceinline__ typename Frag<T>::type rows(const char *lds, int r0, int c, int lane)
+    {
+        const int r = r0 + (lane & 15), g = lane >> 4;
+        if constexpr (sizeof(T) == 2) {
+            return *(const bf16x8 *)(lds + place(r, 4 * c + g));
+        } else {
+            union {
+                f32x4 h[2];
+                Frag<float>::type v;
+            } f;
+            f.h[0] = *(const f32x4 *)(lds + place(r, 8 * c + 2 * g));
+            f.h[1] = *(const f32x4 *)(lds + place(r, 8 * c + 2 * g + 1));
+            return f.v;
+        }
+    }
+    // values d0 .. d0 + 15 (lane % 16) of rows r0 + 4 g + 0 .. 3 and r0 + 16 + 4 g + 0 .. 3, g = lane / 16
+    static __device__ __forceinline__ typename Frag<T>::type columns(const char *lds, int r0, int d0, int lane)
+    {
+        const int g = lane >> 4;
+        if constexpr (sizeof(T) == 2) {
+            const int r = r0 + 4 * g + ((lane & 15) >> 2), piece = (d0 >> 3) + ((lane & 3) >> 1), part = (lane & 1) * 8;
+            union {
+                s16x4 h[2];
+                bf16x8 v;
+            } f;
+            f.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(lds + place(r, piece) + part));
+            f.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(lds + place(r + 16, piece) + part));
+            return f.v;
+        } else {
+            Frag<float>::type f;
+            const int d = d0 + (lane & 15), piece = d >> 2, part = (d & 3) * 4;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int r = r0 + 4 * g + (e & 3) + (e >> 2) * 16;
+                f[e] = *(const float *)(lds + place(r, piece) + part);
+            }
+            return f;
+        }
+    }
+};
+
+// Brings rows of a tensor into a tile.  VEC: 16-byte pieces of rows are aligned and whole; they go straight into LDS.
+// Otherwise values are read one by one.  What is outside (rows from `left` on, values from dim on) becomes zero.
+template <class T, int DP, int ROWS, bool VEC, int THREADS>
+struct TileReader {
+    typedef Tile<T, DP> L;
+    static constexpr int ALL = ROWS * L::PIECES, LOADS = (ALL + THREADS - 1) / THREADS;
+    static_assert(ALL % 64 == 0, "whole wavefronts of pieces");
+    static __device__ __forceinline__ void read(const T *first, long long token, int left, int dim, char *lds, int tid)
+    {
+        const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        if constexpr (VEC) {
+            const int rows = left < ROWS ? left : ROWS;
+            const unsigned pitch = (unsigned)token * (unsigned)sizeof(T);
+            __amdgpu_buffer_rsrc_t res = __builtin_amdgcn_make_buffer_rsrc(
+                (void *)first, 0, rows > 0 ? (unsigned)(rows - 1) * pitch + (unsigned)(dim * sizeof(T)) : 0, 0x00020000);
+#pragma unroll
+            for (int u = 0; u < LOADS; ++u) {
+                const int at = (u * (THREADS / 64) + wave) * 64, c = at + lane;
+                if (at >= ALL) break;
+                const int r = c / L::PIECES, piece = (c % L::PIECES) ^ L::swizzle(r);
+                unsigned off = (unsigned)r * pitch + (unsigned)piece * 16;
+                if (r >= rows || piece * L::EACH >= dim) off = 0x80000000u;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (lds_void *)(lds + at * 16), 16, (int)off, 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < LOADS; ++u) {
+                if (u * THREADS + tid >= ALL) break;
+                const int c = u * THREADS + tid, r = c / L::PIECES, piece = (c % L::PIECES) ^ L::swizzle(r);
+                typedef T pieces __attribute__((ext_vector_type(L::EACH)));
+                pieces p;
+#pragma unroll
+                for (int e = 0; e < L::EACH; ++e) {
+                    const int d = piece * L::EACH + e;
+                    p[e] = r < left && d < dim ? first[(long long)r * token + d] : (T)0.f;
+                }
+                *(pieces *)(lds + c * 16) = p;
+            }
+        }
+    }
+};
+
+// A fragment straight from memory: row `row` (nullptr: zeros), values 32 c + 8 g + 0 .. 7.
+template <class T, bool VEC>
+__device__ __forceinline__ typename Frag<T>::type read_fragment(const T *row, int d0, int dim)
+{
+    typename Frag<T>::type f;
+    if constexpr (VEC) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = (T)0.f;
+        if (row && d0 < dim) {
+            constexpr int EACH = 16 / (int)sizeof(T);
+            typedef T pieces __attribute__((ext_vector_type(EACH)));
+#pragma unroll
+            for (int h = 0; h < 8 / EACH; ++h)
+                if (d0 + h * EACH < dim) {
+                    const pieces p = *(const pieces *)(row + d0 + h * EACH);
+#pragma unroll
+                    for (int e = 0; e < EACH; ++e) f[h * EACH + e] = p[e];
+                }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = row && d0 + e < dim ? row[d0 + e] : (T)0.f;
+    }
+    return f;
+}
+
+// The set that a tile of B tokens belongs to: set p's tiles are numbered from off[p] / B + p on.  All lanes search.
+__device__ __forceinline__ int set_of_tile(const int64_t *off, int sets, int B, long long tile)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = sets;
+    while (n > 1) {
+        const int step = (n + 63) >> 6, p = lo + lane * step;
+        const bool below = p < lo + n && off[p] / B + p <= tile;
+        const int count = __popcll(__ballot(below));
+        const int end = lo + n;
+        lo += (count > 0 ? count - 1 : 0) * step;
+        n = end - lo < step ? end - lo : step;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+struct SetRange {
+    long long q0, k0;
+    int nq, nk;
+};
+// A set's tokens; offsets that are not in order or outside the tensors are cut to what exists.
+__device__ __forceinline__ SetRange range_of(const AttentionArgs &a, int p)
+{
+    auto cut = [](long long v, long long lo, long long hi) { return v < lo ? lo : v > hi ? hi : v; };
+    SetRange r;
+    r.q0 = cut(a.q_off[p], 0, a.total_q);
+    r.k0 = cut(a.k_off[p], 0, a.total_k);
+    r.nq = (int)(cut(a.q_off[p + 1], r.q0, a.total_q) - r.q0);
+    r.nk = (int)(cut(a.k_off[p + 1], r.k0, a.total_k) - r.k0);
+    return r;
+}
+
+constexpr float LOG2_E = 1.4426950408889634f, LN_2 = 0.6931471805599453f;
+
+// tanh for bf16 tensors: 1 - 2 / (e^2x + 1), off by about 2^-23 of 1, far below the rounding of P
+__device__ __forceinline__ float cap_tanh(float x, __bf16) { return 1.f - 2.f * __builtin_amdgcn_rcpf(exp2f(2.f * LOG2_E * x) + 1.f); }
+__device__ __forceinline__ float cap_tanh(float x, float) { return tanhf(x); }
+
+// Turns q . k into the score times log2(e).  SHAPED: there is a cap or a slope; `cut`: the cap's derivative.
+template <class T, bool SHAPED>
+struct Scores {
+    float scale, cap, inv_cap, slope;
+    __device__ __forceinline__ void init(const AttentionArgs &a, int head)
+    {
+        scale = SHAPED ? a.scale : a.scale * LOG2_E;
+        cap = a.cap;
+        inv_cap = SHAPED && a.cap > 0.f ? 1.f / a.cap : 0.f;
+        slope = SHAPED && a.slopes ? a.slopes[head] : 0.f;
+    }
+    __device__ __forceinline__ float operator()(float dot, int behind, float *cut) const
+    {
+        if constexpr (!SHAPED) {
+            return dot * scale;
+        } else {
+            float z = dot * scale;
+            if (cap > 0.f) {
+                const float t = cap_tanh(z * inv_cap, T());
+                z = cap * t;
+                if (cut) *cut = 1.f - t * t;
+            }
+            z -= slope * __builtin_fabsf((float)behind);
+            return z * LOG2_E;
+        }
+    }
+};
+
+__device__ __forceinline__ float minus_infinity() { return -__builtin_huge_valf(); }
+
+// Workgroups are dealt to the eight dies in turn; a die gets a run of neighbours, which share keys or queries.
+__device__ __forceinline__ long long die_run(long long id, long long total)
+{
+    const long long base = total / 8, more = total % 8, die = id % 8, nth = id / 8;
+    return die * base + (die < more ? die : more) + nth;
+}
+
+// ---- forward -------------------------------------------------------------------
+// Four wavefronts of 16 QT queries each go over the set's keys, 64 at a time.
+template <class T, int DP, int QT, bool VEC, bool SHAPED>
+__global__ __launch_bounds__(256) void attention_forward_kernel(AttentionArgs a)
+{
+    constexpr int BQ = 64 * QT, BK = 64, C = DP / 32, DT = DP / 16;
+    typedef Tile<T, DP> L;
+    __shared__ __align__(1024) char lds_k[BK * L::PITCH];
+    __shared__ __align__(1024) char lds_v[BK * L::PITCH];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
+    const int group = a.heads / a.kv_heads;
+    const long long t = die_run(blockIdx.x, gridDim.x);
+    const int head = (int)(t / ((long long)a.tiles * group)) * group + (int)(t % group), kv = head / group;
+    const long long tile = a.tiles - 1 - (t / group) % a.tiles;
+    const int p = set_of_tile(a.q_off, a.sets, BQ, tile);
+    const SetRange s = range_of(a, p);
+    const long long first_tile = s.q0 / BQ + p;
+    const long long b0 = (tile - first_tile) * BQ;
+    if (b0 < 0 || b0 >= s.nq) return;
+    const int q_first = (int)b0, shift = s.nk - s.nq;
+    const int prefix = a.causal && a.prefix ? a.prefix[p] : 0;
+    int last = s.nk;   // keys that any query of the tile sees
+    if (a.causal) {
+        const int reach = (q_first + BQ < s.nq ? q_first + BQ : s.nq) + shift;
+        last = reach > prefix ? reach : prefix;
+        last = last < s.nk ? last : s.nk;
+    }
+    Scores<T, SHAPED> score;
+    score.init(a, head);
+
+    const T *qp = (const T *)a.q + s.q0 * a.q_token + head * a.q_head;
+    const T *kp = (const T *)a.k + s.k0 * a.k_token + kv * a.k_head;
+    const T *vp = (const T *)a.v + s.k0 * a.v_token + kv * a.v_head;
+    typename Frag<T>::type fq[QT][C];
+    int qi[QT];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        qi[u] = q_first + (wave * QT + u) * 16 + (lane & 15);
+        const T *row = qi[u] < s.nq ? qp + (long long)qi[u] * a.q_token : nullptr;
+#pragma unroll
+        for (int c = 0; c < C; ++c) fq[u][c] = read_fragment<T, VEC>(row, 32 * c + 8 * g, a.dim);
+    }
+    const int w_first = q_first + wave * QT * 16;   // this wavefront's queries
+    f32x4 o[DT][QT];
+    float top[QT], sum[QT];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        top[u] = minus_infinity();
+        sum[u] = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    for (int j0 = 0; j0 < last; j0 += BK) {
+        __syncthreads();
+        TileReader<T, DP, BK, VEC, 256>::read(kp + (long long)j0 * a.k_token, a.k_token, s.nk - j0, a.dim, lds_k, tid);
+        TileReader<T, DP, BK, VEC, 256>::read(vp + (long long)j0 * a.v_token, a.v_token, s.nk - j0, a.dim, lds_v, tid);
+        __builtin_amdgcn_s_waitcnt(0x0f70);
+        __syncthreads();
+        f32x4 z[4][QT];
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+            for (int u = 0; u < QT; ++u) z[kt][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+                const typename Frag<T>::type fk = L::rows(lds_k, kt * 16, c, lane);
+#pragma unroll
+                for (int u = 0; u < QT; ++u) mma(z[kt][u], fk, fq[u][c]);
+            }
+        const bool whole = j0 + BK <= s.nk && (!a.causal || j0 + BK - 1 <= w_first + shift || j0 + BK <= prefix);
+        typename Frag<T>::type fp[2][QT];
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+            float most = top[u];
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = j0 + kt * 16 + 4 * g + e, at = qi[u] + shift;
+                    float v = score(z[kt][u][e], at - j, nullptr);
+                    if (!whole && (j >= s.nk || (a.causal && j > at && j >= prefix))) v = minus_infinity();
+                    z[kt][u][e] = v;
+                    most = fmaxf(most, v);
+                }
+            most = fmaxf(most, __shfl_xor(most, 16));
+            most = fmaxf(most, __shfl_xor(most, 32));
+            const float ref = most == minus_infinity() ? 0.f : most;
+            const float keep = exp2f(top[u] - ref);
+            top[u] = most;
+            float add = 0.f;
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float v = exp2f(z[kt][u][e] - ref);
+                    add += v;
+                    fp[kt >> 1][u][(kt & 1) * 4 + e] = (T)v;
+                }
+            sum[u] = sum[u] * keep + add;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d][u] *= keep;
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                const typename Frag<T>::type fv = L::columns(lds_v, c * 32, d * 16, lane);
+#pragma unroll
+                for (int u = 0; u < QT; ++u) mma(o[d][u], fv, fp[c][u]);
+            }
+    }
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        float total = sum[u];
+        total += __shfl_xor(total, 16);
+        total += __shfl_xor(total, 32);
+        if (qi[u] >= s.nq) continue;
+        const long long n = s.q0 + qi[u];
+        const float inv = total > 0.f || total != total ? 1.f / total : 0.f;   // no key: zero
+        T *out = (T *)a.o + (n * a.heads + head) * a.dim;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            const int d0 = d * 16 + 4 * g;
+            if (d0 < a.dim) store_four(out + d0, o[d][u] * inv, a.dim - d0, VEC);
+        }
+        if (g == 0) a.lse[head * a.total_q + n] = (top[u] + log2f(total)) * LN_2;
+    }
+}
+
+// ---- backward -------------------------------------------------------------------
+// delta = do . o per query and head: 16 lanes each
+template <class T>
+__global__ __launch_bounds__(256) void attention_delta_kernel(const T *__restrict__ o, const T *__restrict__ d_o, long long total_q,
+                                                              int heads, int dim, float *__restrict__ delta)
+{
+    const long long r = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (r >= total_q * heads) return;
+    float s = 0.f;
+    for (int d = threadIdx.x & 15; d < dim; d += 16) s += (float)o[r * dim + d] * (float)d_o[r * dim + d];
+#pragma unroll
+    for (int x = 8; x > 0; x >>= 1) s += __shfl_xor(s, x, 16);
+    if ((threadIdx.x & 15) == 0) delta[(r % heads) * total_q + r / heads] = s;
+}
+
+// dq: like the forward pass; dS = P (dP - delta) cut, dq = scale sum_j dS_ij k_j.
+template <class T, int DP, int QT, bool VEC, bool SHAPED>
+__global__ __launch_bounds__(256) void attention_dq_kernel(AttentionArgs a)
+{
+    constexpr int BQ = 64 * QT, BK = 64, C = DP / 32, DT = DP / 16;
+    typedef Tile<T, DP> L;
+    __shared__ __align__(1024) char lds_k[BK * L::PITCH];
+    __shared__ __align__(1024) char lds_v[BK * L::PITCH];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
+    const int group = a.heads / a.kv_heads;
+    const long long t = die_run(blockIdx.x, gridDim.x);
+    const int head = (int)(t / ((long long)a.tiles * group)) * group + (int)(t % group), kv = head / group;
+    const long long tile = a.tiles - 1 - (t / group) % a.tiles;
+    const int p = set_of_tile(a.q_off, a.sets, BQ, tile);
+    const SetRange s = range_of(a, p);
+    const long long b0 = (tile - (s.q0 / BQ + p)) * BQ;
+    if (b0 < 0 || b0 >= s.nq) return;
+    const int q_first = (int)b0, shift = s.nk - s.nq;
+    const int prefix = a.causal && a.prefix ? a.prefix[p] : 0;
+    int last = s.nk;
+    if (a.causal) {
+        const int reach = (q_first + BQ < s.nq ? q_first + BQ : s.nq) + shift;
+        last = reach > prefix ? reach : prefix;
+        last = last < s.nk ? last : s.nk;
+    }
+    Scores<T, SHAPED> score;
+    score.init(a, head);
+    const T *kp = (const T *)a.k + s.k0 * a.k_token + kv * a.k_head;
+    const T *vp = (const T *)a.v + s.k0 * a.v_token + kv * a.v_head;
+    typename Frag<T>::type fq[QT][C], fo[QT][C];
+    int qi[QT];
+    float lse[QT], delta[QT];
+    f32x4 dq[DT][QT];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        qi[u] = q_first + (wave * QT + u) * 16 + (lane & 15);
+        const bool in = qi[u] < s.nq;
+        const long long n = s.q0 + (in ? qi[u] : 0);
+        const T *row = in ? (const T *)a.q + n * a.q_token + head * a.q_head : nullptr;
+        const T *orow = in ? (const T *)a.d_o + (n * a.heads + head) * a.dim : nullptr;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            fq[u][c] = read_fragment<T, VEC>(row, 32 * c + 8 * g, a.dim);
+            fo[u][c] = read_fragment<T, VEC>(orow, 32 * c + 8 * g, a.dim);
+        }
+        lse[u] = in ? a.lse_in[head * a.total_q + n] * LOG2_E : 0.f;
+        delta[u] = in ? a.delta[head * a.total_q + n] : 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) dq[d][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int w_first = q_first + wave * QT * 16;
+    for (int j0 = 0; j0 < last; j0 += BK) {
+        __syncthreads();
+        TileReader<T, DP, BK, VEC, 256>::read(kp + (long long)j0 * a.k_token, a.k_token, s.nk - j0, a.dim, lds_k, tid);
+        TileReader<T, DP, BK, VEC, 256>::read(vp + (long long)j0 * a.v_token, a.v_token, s.nk - j0, a.dim, lds_v, tid);
+        __builtin_amdgcn_s_waitcnt(0x0f70);
+        __syncthreads();
+        const bool whole = j0 + BK <= s.nk && (!a.causal || j0 + BK - 1 <= w_first + shift || j0 + BK <= prefix);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {   // 32 keys at a time
+            f32x4 z[2][QT], dp[2][QT];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int u = 0; u < QT; ++u) z[kt][u] = dp[kt][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) {
+                    const typename Frag<T>::type fk = L::rows(lds_k, h * 32 + kt * 16, c, lane);
+                    const typename Frag<T>::type fv = L::rows(lds_v, h * 32 + kt * 16, c, lane);
+#pragma unroll
+                    for (int u = 0; u < QT; ++u) {
+                        mma(z[kt][u], fk, fq[u][c]);
+                        mma(dp[kt][u], fv, fo[u][c]);
+                    }
+                }
+            typename Frag<T>::type fs[QT];
+#pragma unroll
+            for (int u = 0; u < QT; ++u)
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int j = j0 + h * 32 + kt * 16 + 4 * g + e, at = qi[u] + shift;
+                        float cut = 1.f;
+                        const float v = score(z[kt][u][e], at - j, &cut);
+                        float ds = exp2f(v - lse[u]) * (dp[kt][u][e] - delta[u]) * cut;
+                        if (!whole && (j >= s.nk || (a.causal && j > at && j >= prefix))) ds = 0.f;
+                        fs[u][kt * 4 + e] = (T)ds;
+                    }
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                const typename Frag<T>::type fk = L::columns(lds_k, h * 32, d * 16, lane);
+#pragma unroll
+                for (int u = 0; u < QT; ++u) mma(dq[d][u], fk, fs[u]);
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        if (qi[u] >= s.nq) continue;
+        T *out = (T *)a.dq + ((s.q0 + qi[u]) * a.heads + head) * a.dim;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            const int d0 = d * 16 + 4 * g;
+            if (d0 < a.dim) store_four(out + d0, dq[d][u] * a.scale, a.dim - d0, VEC);
+        }
+    }
+}
+
+// dk, dv: four wavefronts of 16 KT keys each go over the queries of all heads that share the key head, 32 at a
+// time; dv = P^T do, dk = scale dS^T q.
+template <class T, int DP, int KT, bool VEC, bool SHAPED>
+__global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
+{
+    constexpr int BK = 64 * KT, BQ = 32, C = DP / 32, DT = DP / 16;
+    typedef Tile<T, DP> L;
+    __shared__ __align__(1024) char lds_q[BQ * L::PITCH];
+    __shared__ __align__(1024) char lds_o[BQ * L::PITCH];
+    __shared__ __align__(16) float lds_lse[BQ], lds_delta[BQ];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
+    const int group = a.heads / a.kv_heads;
+    const long long t = die_run(blockIdx.x, gridDim.x);
+    const int kv = (int)(t / a.tiles);
+    const long long tile = t % a.tiles;
+    const int p = set_of_tile(a.k_off, a.sets, BK, tile);
+    const SetRange s = range_of(a, p);
+    const long long b0 = (tile - (s.k0 / BK + p)) * BK;
+    if (b0 < 0 || b0 >= s.nk) return;
+    const int k_first = (int)b0, shift = s.nk - s.nq;
+    const int prefix = a.causal && a.prefix ? a.prefix[p] : 0;
+    // queries before `begin` see none of these keys
+    int begin = 0;
+    if (a.causal && k_first >= prefix) {
+        begin = k_first - shift;
+        begin = begin > 0 ? begin & ~(BQ - 1) : 0;
+    }
+    typename Frag<T>::type fk[KT][C], fv[KT][C];
+    int kj[KT];
+    f32x4 dk[DT][KT], dv[DT][KT];
+#pragma unroll
+    for (int u = 0; u < KT; ++u) {
+        kj[u] = k_first + (wave * KT + u) * 16 + (lane & 15);
+        const bool in = kj[u] < s.nk;
+        const long long n = s.k0 + (in ? kj[u] : 0);
+        const T *krow = in ? (const T *)a.k + n * a.k_token + kv * a.k_head : nullptr;
+        const T *vrow = in ? (const T *)a.v + n * a.v_token + kv * a.v_head : nullptr;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            fk[u][c] = read_fragment<T, VEC>(krow, 32 * c + 8 * g, a.dim);
+            fv[u][c] = read_fragment<T, VEC>(vrow, 32 * c + 8 * g, a.dim);
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) dk[d][u] = dv[d][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int w_last = k_first + (wave + 1) * KT * 16 - 1;   // this wavefront's last key
+    for (int gh = 0; gh < group; ++gh) {
+        const int head = kv * group + gh;
+        Scores<T, SHAPED> score;
+        score.init(a, head);
+        const T *qp = (const T *)a.q + s.q0 * a.q_token + head * a.q_head;
+        const T *op = (const T *)a.d_o + (s.q0 * a.heads + head) * a.dim;
+        const float *lp = a.lse_in + head * a.total_q + s.q0, *ep = a.delta + head * a.total_q + s.q0;
+        for (int i0 = begin; i0 < s.nq; i0 += BQ) {
+            __syncthreads();
+            TileReader<T, DP, BQ, VEC, 256>::read(qp + (long long)i0 * a.q_token, a.q_token, s.nq - i0, a.dim, lds_q, tid);
+            TileReader<T, DP, BQ, VEC, 256>::read(op + (long long)i0 * a.heads * a.dim, (long long)a.heads * a.dim, s.nq - i0,
+                                                  a.dim, lds_o, tid);
+            if (tid < BQ) {
+                const bool in = i0 + tid < s.nq;
+                lds_lse[tid] = in ? lp[i0 + tid] * LOG2_E : 0.f;
+                lds_delta[tid] = in ? ep[i0 + tid] : 0.f;
+            }
+            __builtin_amdgcn_s_waitcnt(0x0f70);
+            __syncthreads();
+            f32x4 z[2][KT], dp[2][KT];
+#pragma unroll
+            for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+                for (int u = 0; u < KT; ++u) z[qt][u] = dp[qt][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int qt = 0; qt < 2; ++qt) {
+                    const typename Frag<T>::type fq = L::rows(lds_q, qt * 16, c, lane);
+                    const typename Frag<T>::type fo = L::rows(lds_o, qt * 16, c, lane);
+#pragma unroll
+                    for (int u = 0; u < KT; ++u) {
+                        mma(z[qt][u], fq, fk[u][c]);
+                        mma(dp[qt][u], fo, fv[u][c]);
+                    }
+                }
+            const bool whole = i0 + BQ <= s.nq && w_last < s.nk && (!a.causal || w_last <= i0 + shift || w_last < prefix);
+            typename Frag<T>::type fp[KT], fs[KT];
+#pragma unroll
+            for (int qt = 0; qt < 2; ++qt) {
+                const f32x4 lse = *(const f32x4 *)(lds_lse + qt * 16 + 4 * g);
+                const f32x4 delta = *(const f32x4 *)(lds_delta + qt * 16 + 4 * g);
+#pragma unroll
+                for (int u = 0; u < KT; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int i = i0 + qt * 16 + 4 * g + e, at = i + shift, j = kj[u];
+                        float cut = 1.f;
+                        const float v = score(z[qt][u][e], at - j, &cut);
+                        float pr = exp2f(v - lse[e]);
+                        float ds = pr * (dp[qt][u][e] - delta[e]) * cut;
+                        if (!whole && (i >= s.nq || j >= s.nk || (a.causal && j > at && j >= prefix))) pr = ds = 0.f;
+                        fp[u][qt * 4 + e] = (T)pr;
+                        fs[u][qt * 4 + e] = (T)ds;
+                    }
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                const typename Frag<T>::type fo = L::columns(lds_o, 0, d * 16, lane);
+                const typename Frag<T>::type fq = L::columns(lds_q, 0, d * 16, lane);
+#pragma unroll
+                for (int u = 0; u < KT; ++u) {
+                    mma(dv[d][u], fo, fp[u]);
+                    mma(dk[d][u], fq, fs[u]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < KT; ++u) {
+        if (kj[u] >= s.nk) continue;
+        const long long at = ((s.k0 + kj[u]) * a.kv_heads + kv) * a.dim;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            const int d0 = d * 16 + 4 * g;
+            if (d0 >= a.dim) continue;
+            store_four((T *)a.dk + at + d0, dk[d][u] * a.scale, a.dim - d0, VEC);
+            store_four((T *)a.dv + at + d0, dv[d][u], a.dim - d0, VEC);
+        }
+    }
+}
+
+// one translation unit per type (kernels_attention_*.hip)
+template <class T>
+hipError_t attention_forward(AttentionArgs a, bool vec, bool shaped, hipStream_t s);
+template <class T>
+hipError_t attention_backward(AttentionArgs a, bool vec, bool shaped, float *delta, const T *o, hipStream_t s);
+
+}  // namespace lcn

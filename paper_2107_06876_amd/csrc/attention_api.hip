@@ -1,0 +1,118 @@
+// Attention inside the sets of a ragged batch: the C entry points.
+#include "attention.h"
+
+namespace lcn {
+
+static bool attention_desc_fits(const lcn_attention_desc *d)
+{
+    if (!d || d->num_sets < 0 || d->num_sets > (1 << 24) || d->total_q < 0 || d->total_q > MAX_ROWS || d->total_k < 0 ||
+        d->total_k > MAX_ROWS || d->max_q < 0 || d->heads < 1 || d->heads > 1024 || d->kv_heads < 1 || d->heads % d->kv_heads ||
+        d->head_dim < 1 || d->head_dim > 128 || (d->dtype != LCN_F32 && d->dtype != LCN_BF16))
+        return false;
+    if (!(d->scale - d->scale == 0.f) || !(d->cap >= 0.f) || !(d->cap - d->cap == 0.f)) return false;
+    const int64_t strides[6] = {d->q_token, d->q_head, d->k_token, d->k_head, d->v_token, d->v_head};
+    for (int i = 0; i < 6; ++i)
+        if (strides[i] < 0 || strides[i] > (1 << 22)) return false;
+    // a launch has a workgroup per tile of 64 tokens and head
+    if ((d->total_q / 64 + d->num_sets) * (int64_t)d->heads > 0x7fffffff) return false;
+    if ((d->total_k / 64 + d->num_sets) * (int64_t)d->heads > 0x7fffffff) return false;
+    return d->num_sets == 0 || (d->q_off && d->k_off);
+}
+
+static AttentionArgs args_of(const lcn_attention_desc *d, const void *q, const void *k, const void *v)
+{
+    AttentionArgs a{};
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.q_off = d->q_off;
+    a.k_off = d->k_off;
+    a.prefix = d->causal ? d->prefix : nullptr;
+    a.slopes = d->slopes;
+    a.q_head = d->q_head ? d->q_head : d->head_dim;
+    a.k_head = d->k_head ? d->k_head : d->head_dim;
+    a.v_head = d->v_head ? d->v_head : d->head_dim;
+    a.q_token = d->q_token ? d->q_token : (int64_t)d->heads * d->head_dim;
+    a.k_token = d->k_token ? d->k_token : (int64_t)d->kv_heads * d->head_dim;
+    a.v_token = d->v_token ? d->v_token : (int64_t)d->kv_heads * d->head_dim;
+    a.total_q = d->total_q;
+    a.total_k = d->total_k;
+    a.sets = d->num_sets;
+    a.heads = d->heads;
+    a.kv_heads = d->kv_heads;
+    a.dim = d->head_dim;
+    a.causal = d->causal != 0;
+    a.scale = d->scale;
+    a.cap = d->cap;
+    return a;
+}
+
+// Whether every row is whole 16-byte pieces from aligned addresses.
+static bool pieces(const AttentionArgs &a, size_t e, const void *const *more, int count)
+{
+    uintptr_t all = (uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v;
+    for (int i = 0; i < count; ++i) all |= (uintptr_t)more[i];
+    const long long strides = a.q_token | a.q_head | a.k_token | a.k_head | a.v_token | a.v_head | a.dim;
+    return (all & 15) == 0 && (strides & (long long)(16 / e - 1)) == 0;
+}
+
+}  // namespace lcn
+
+using namespace lcn;
+
+extern "C" {
+
+lcn_status lcn_attention_workspace_bytes(const lcn_attention_desc *desc, int32_t backward, size_t *bytes)
+{
+    if (!bytes || !attention_desc_fits(desc)) return LCN_ERR_INVALID_ARG;
+    *bytes = backward ? (size_t)desc->heads * (size_t)desc->total_q * 4 : 0;
+    return LCN_OK;
+}
+
+lcn_status lcn_attention(const lcn_attention_desc *desc, const void *q, const void *k, const void *v, void *o, float *lse,
+                         void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (!attention_desc_fits(desc)) return LCN_ERR_INVALID_ARG;
+    if (desc->num_sets == 0 || desc->total_q == 0) return LCN_OK;
+    if (!q || !o || !lse || (desc->total_k > 0 && (!k || !v))) return LCN_ERR_INVALID_ARG;
+    AttentionArgs a = args_of(desc, q, k, v);
+    a.o = o;
+    a.lse = lse;
+    const void *more[1] = {o};
+    const bool vec = pieces(a, desc->dtype == LCN_F32 ? 4 : 2, more, 1), shaped = a.cap > 0.f || a.slopes;
+    (void)workspace;
+    (void)workspace_bytes;
+    if (desc->dtype == LCN_F32)
+        OPCHK(attention_forward<float>(a, vec, shaped, (hipStream_t)hip_stream));
+    else
+        OPCHK(attention_forward<__bf16>(a, vec, shaped, (hipStream_t)hip_stream));
+    return LCN_OK;
+}
+
+lcn_status lcn_attention_backward(const lcn_attention_desc *desc, const void *q, const void *k, const void *v, const void *o,
+                                  const float *lse, const void *d_o, void *dq, void *dk, void *dv, void *workspace,
+                                  size_t workspace_bytes, void *hip_stream)
+{
+    if (!attention_desc_fits(desc) || !dk != !dv) return LCN_ERR_INVALID_ARG;
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (desc->num_sets == 0 || (!dq && !dk)) return LCN_OK;
+    if (desc->total_q > 0 && (!q || !o || !lse || !d_o)) return LCN_ERR_INVALID_ARG;
+    if (desc->total_k > 0 && (!k || !v)) return LCN_ERR_INVALID_ARG;
+    const size_t need = (size_t)desc->heads * (size_t)desc->total_q * 4;
+    if (need && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return LCN_ERR_ALLOC;
+    AttentionArgs a = args_of(desc, q, k, v);
+    a.d_o = d_o;
+    a.lse_in = lse;
+    a.dq = dq;
+    a.dk = dk;
+    a.dv = dv;
+    const void *more[4] = {d_o, dq, dk, dv};
+    const bool vec = pieces(a, desc->dtype == LCN_F32 ? 4 : 2, more, 4), shaped = a.cap > 0.f || a.slopes;
+    if (desc->dtype == LCN_F32)
+        OPCHK(attention_backward<float>(a, vec, shaped, (float *)workspace, (const float *)o, s));
+    else
+        OPCHK(attention_backward<__bf16>(a, vec, shaped, (float *)workspace, (const __bf16 *)o, s));
+    return LCN_OK;
+}
+
+}  // extern "C"

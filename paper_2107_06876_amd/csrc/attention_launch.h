@@ -1,0 +1,79 @@
+// Instantiates the attention kernels of one type and chooses among them.
+#pragma once
+
+#include "attention.h"
+
+namespace lcn {
+
+// Tiles of B tokens that sets with `total` tokens can have (see set_of_tile).
+inline long long tiles_of(long long total, int sets, int B) { return total / B + sets; }
+
+// Sets of up to 64 tokens on average: wavefronts of 16 instead of 32 queries (or keys) each, so that a set fills a workgroup.
+inline bool short_sets(long long total, int sets) { return total <= 64LL * sets; }
+
+template <class T, int DP, int QT, bool VEC, bool SHAPED>
+static hipError_t forward_one(AttentionArgs a, hipStream_t s)
+{
+    const long long tiles = tiles_of(a.total_q, a.sets, 64 * QT);
+    a.tiles = (int)tiles;
+    hipLaunchKernelGGL((attention_forward_kernel<T, DP, QT, VEC, SHAPED>), dim3((unsigned)(tiles * a.heads)), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+template <class T, int DP, int QT, bool VEC, bool SHAPED>
+static hipError_t backward_one(AttentionArgs a, bool dq, hipStream_t s)
+{
+    if (dq) {
+        const long long tiles = tiles_of(a.total_q, a.sets, 64 * QT);
+        a.tiles = (int)tiles;
+        hipLaunchKernelGGL((attention_dq_kernel<T, DP, QT, VEC, SHAPED>), dim3((unsigned)(tiles * a.heads)), dim3(256), 0, s, a);
+    } else {
+        const long long tiles = tiles_of(a.total_k, a.sets, 64 * QT);
+        a.tiles = (int)tiles;
+        hipLaunchKernelGGL((attention_dkv_kernel<T, DP, QT, VEC, SHAPED>), dim3((unsigned)(tiles * a.kv_heads)), dim3(256), 0, s, a);
+    }
+    return hipGetLastError();
+}
+
+// what: 0 forward, 1 dq, 2 dk and dv
+template <class T, int DP, int QT>
+static hipError_t by_form(const AttentionArgs &a, int what, bool vec, bool shaped, hipStream_t s)
+{
+    if (what == 0) {
+        if (vec) return shaped ? forward_one<T, DP, QT, true, true>(a, s) : forward_one<T, DP, QT, true, false>(a, s);
+        return forward_one<T, DP, QT, false, true>(a, s);
+    }
+    if (vec) return shaped ? backward_one<T, DP, QT, true, true>(a, what == 1, s) : backward_one<T, DP, QT, true, false>(a, what == 1, s);
+    return backward_one<T, DP, QT, false, true>(a, what == 1, s);
+}
+template <class T>
+static hipError_t by_size(const AttentionArgs &a, int what, bool vec, bool shaped, hipStream_t s)
+{
+    const bool few = what == 2 ? short_sets(a.total_k, a.sets) : short_sets(a.total_q, a.sets);
+    if (a.dim <= 32) return few ? by_form<T, 32, 1>(a, what, vec, shaped, s) : by_form<T, 32, 2>(a, what, vec, shaped, s);
+    if (a.dim <= 64) return few ? by_form<T, 64, 1>(a, what, vec, shaped, s) : by_form<T, 64, 2>(a, what, vec, shaped, s);
+    return few ? by_form<T, 128, 1>(a, what, vec, shaped, s) : by_form<T, 128, 2>(a, what, vec, shaped, s);
+}
+
+template <class T>
+hipError_t attention_forward(AttentionArgs a, bool vec, bool shaped, hipStream_t s)
+{
+    return by_size<T>(a, 0, vec, shaped, s);
+}
+template <class T>
+hipError_t attention_backward(AttentionArgs a, bool vec, bool shaped, float *delta, const T *o, hipStream_t s)
+{
+    if (a.total_q > 0) {
+        const long long rows = a.total_q * a.heads;
+        hipLaunchKernelGGL(attention_delta_kernel<T>, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, s, o, (const T *)a.d_o,
+                           a.total_q, a.heads, a.dim, delta);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        a.delta = delta;
+        if (a.dq && (e = by_size<T>(a, 1, vec, shaped, s)) != hipSuccess) return e;
+    }
+    a.delta = delta;
+    if (a.dk && a.total_k > 0) return by_size<T>(a, 2, vec, shaped, s);
+    return hipSuccess;
+}
+
+}  // namespace lcn

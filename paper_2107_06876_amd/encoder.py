@@ -17,6 +17,16 @@ _TYPES = {torch.float32: F32, torch.bfloat16: BF16}
 _lib = None
 
 
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [("num_sets", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("cap", ctypes.c_float), ("total_q", ctypes.c_int64),
+                ("total_k", ctypes.c_int64), ("max_q", ctypes.c_int64), ("q_off", ctypes.c_void_p),
+                ("k_off", ctypes.c_void_p), ("prefix", ctypes.c_void_p), ("slopes", ctypes.c_void_p),
+                ("q_token", ctypes.c_int64), ("q_head", ctypes.c_int64), ("k_token", ctypes.c_int64),
+                ("k_head", ctypes.c_int64), ("v_token", ctypes.c_int64), ("v_head", ctypes.c_int64)]
+
+
 def _library():
     global _lib
     if _lib is None:
@@ -29,7 +39,11 @@ def _library():
         lib.lcn_cross_entropy_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, out]
         lib.lcn_cross_entropy.argtypes = [vp, vp, vp, vp, i64, i32, i32, i32, f32, vp, vp, vp, sz, vp]
         lib.lcn_cross_entropy_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, f32, vp, vp, vp, vp, sz, vp]
-        for name in ("lcn_linear_workspace_bytes", "lcn_linear", "lcn_linear_backward", "lcn_cross_entropy_workspace_bytes",
+        desc = ctypes.POINTER(AttentionDesc)
+        lib.lcn_attention_workspace_bytes.argtypes = [desc, i32, out]
+        lib.lcn_attention.argtypes = [desc, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.lcn_attention_backward.argtypes = [desc, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        for name in ("lcn_attention_workspace_bytes", "lcn_attention", "lcn_attention_backward", "lcn_linear_workspace_bytes", "lcn_linear", "lcn_linear_backward", "lcn_cross_entropy_workspace_bytes",
                      "lcn_cross_entropy", "lcn_cross_entropy_backward"):
             getattr(lib, name).restype = i32
         _lib = lib
@@ -157,3 +171,85 @@ def lcn_cross_entropy_backward(x, w, target, lse, grad_loss, bias=None, scale=1.
     if st != OK:
         raise LcnError(st, "lcn_cross_entropy_backward")
     return dx, dw, db
+
+
+def _heads(t, name, like=None):
+    """Checks a (tokens, heads, dim) device tensor whose last dimension is contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 3 or t.dtype not in _TYPES:
+        raise ValueError("%s: expected a float32 or bfloat16 device tensor (tokens, heads, dim)" % name)
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError("%s: the values of a head must be contiguous" % name)
+    if like is not None and (t.dtype != like.dtype or t.device != like.device or t.shape[2] != like.shape[2]):
+        raise ValueError("%s: q, k and v must agree in type, device and dim" % name)
+    return t
+
+
+def _attention_desc(q, k, v, q_off, k_off, scale, causal, prefix, slopes, cap, max_q):
+    _heads(q, "q"), _heads(k, "k", q), _heads(v, "v", q)
+    if k.shape != v.shape or k.shape[1] == 0 or q.shape[1] % k.shape[1]:
+        raise ValueError("k and v must have one shape, and q a multiple of their heads")
+    dev = q.device
+    if q_off.dim() != 1 or q_off.shape[0] < 1:
+        raise ValueError("q_off: expected num_sets + 1 offsets")
+    sets = q_off.shape[0] - 1
+    if causal is False and prefix is not None:
+        raise ValueError("prefix: only a causal mask has one")
+
+    def strides(t):   # of a dimension with one entry: any
+        dense = t.shape[1] * t.shape[2]
+        token, head = t.stride(0), t.stride(1)
+        if (t.shape[0] > 1 and token < 1) or (t.shape[1] > 1 and head < 1):
+            raise ValueError("tensors that are broadcast over tokens or heads are not taken: make them whole")
+        return token if t.shape[0] > 1 else dense, head if t.shape[1] > 1 else t.shape[2]
+
+    return AttentionDesc(sets, q.shape[1], k.shape[1], q.shape[2], _TYPES[q.dtype], 1 if causal else 0,
+                         float(q.shape[2] ** -0.5 if scale is None else scale), float(cap), q.shape[0], k.shape[0], int(max_q),
+                         _tensor(q_off, "q_off", (sets + 1,), torch.int64, dev),
+                         _tensor(k_off, "k_off", (sets + 1,), torch.int64, dev),
+                         _tensor(prefix, "prefix", (sets,), torch.int32, dev),
+                         _tensor(slopes, "slopes", (q.shape[1],), torch.float32, dev), *strides(q), *strides(k), *strides(v))
+
+
+def lcn_attention(q, k, v, q_off, k_off, scale=None, causal=False, prefix=None, slopes=None, cap=0.0, max_q=0,
+                  workspace=None):
+    """(o, lse): attention of the queries of every set to the keys of the same set.  q: (tokens, heads, dim), k and v:
+    (tokens, key heads, dim), views with strides are taken; q_off, k_off: int64 offsets of the sets on the device; scale:
+    1 / sqrt(dim) where None; prefix: int32 per set; slopes: float32 per head; max_q: the largest number of queries of
+    a set, where known.  o is dense like q, lse float32 (heads, tokens); queries in no set are left as they are."""
+    lib = _library()
+    d = _attention_desc(q, k, v, q_off, k_off, scale, causal, prefix, slopes, cap, max_q)
+    dev = q.device
+    o = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=dev)
+    ref = ctypes.byref(d)
+    ws = _space(lib.lcn_attention_workspace_bytes, (ref, 0), workspace, dev)
+    with torch.cuda.device(dev):
+        st = lib.lcn_attention(ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), ws.data_ptr(),
+                               ws.numel(), torch.cuda.current_stream(dev).cuda_stream)
+    if st != OK:
+        raise LcnError(st, "lcn_attention")
+    return o, lse
+
+
+def lcn_attention_backward(q, k, v, o, lse, dy, q_off, k_off, scale=None, causal=False, prefix=None, slopes=None, cap=0.0,
+                           max_q=0, with_q=True, with_kv=True, workspace=None):
+    """(dq, dk, dv) for a given dy, the gradient of o; o and lse as lcn_attention returned them, the rest as it was
+    given.  Gradients are dense; those that are not asked for are None."""
+    lib = _library()
+    d = _attention_desc(q, k, v, q_off, k_off, scale, causal, prefix, slopes, cap, max_q)
+    dev = q.device
+    shape = tuple(q.shape)
+    dq = torch.empty(shape, dtype=q.dtype, device=dev) if with_q else None
+    dk = torch.empty(k.shape, dtype=q.dtype, device=dev) if with_kv else None
+    dv = torch.empty(k.shape, dtype=q.dtype, device=dev) if with_kv else None
+    ref = ctypes.byref(d)
+    ws = _space(lib.lcn_attention_workspace_bytes, (ref, 1), workspace, dev)
+    with torch.cuda.device(dev):
+        st = lib.lcn_attention_backward(ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), _tensor(o, "o", shape, q.dtype, dev),
+                                        _tensor(lse, "lse", (shape[1], shape[0]), torch.float32, dev),
+                                        _tensor(dy, "dy", shape, q.dtype, dev),
+                                        *[None if t is None else t.data_ptr() for t in (dq, dk, dv)], ws.data_ptr(),
+                                        ws.numel(), torch.cuda.current_stream(dev).cuda_stream)
+    if st != OK:
+        raise LcnError(st, "lcn_attention_backward")
+    return dq, dk, dv
