@@ -214,7 +214,7 @@ __device__ __forceinline__ SetRange range_of(const AttentionArgs &a, int p)
 constexpr float LOG2_E = 1.4426950408889634f, LN_2 = 0.6931471805599453f;
 
 // tanh for bf16 tensors: 1 - 2 / (e^2x + 1), off by about 2^-23 of 1, far below the rounding of P
-__device__ __forceinline__ float cap_tanh(float x, __bf16) { return 1.f - 2.f * __builtin_amdgcn_rcpf(exp2f(2.f * LOG2_E * x) + 1.f); }
+__device__ __forceinline__ float cap_tanh(float x, __bf16) { return 1.f - 2.f * __builtin_amdgcn_rcpf(exp2_fast(2.f * LOG2_E * x) + 1.f); }
 __device__ __forceinline__ float cap_tanh(float x, float) { return tanhf(x); }
 
 // Turns q . k into the score times log2(e).  SHAPED: there is a cap or a slope; `cut`: the cap's derivative.
@@ -344,14 +344,14 @@ __global__ __launch_bounds__(256) void attention_forward_kernel(AttentionArgs a)
             most = fmaxf(most, __shfl_xor(most, 16));
             most = fmaxf(most, __shfl_xor(most, 32));
             const float ref = most == minus_infinity() ? 0.f : most;
-            const float keep = exp2f(top[u] - ref);
+            const float keep = exp2_fast(top[u] - ref);
             top[u] = most;
             float add = 0.f;
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float v = exp2f(z[kt][u][e] - ref);
+                    const float v = exp2_fast(z[kt][u][e] - ref);
                     add += v;
                     fp[kt >> 1][u][(kt & 1) * 4 + e] = (T)v;
                 }
@@ -488,7 +488,7 @@ __global__ __launch_bounds__(256) void attention_dq_kernel(AttentionArgs a)
                         const int j = j0 + h * 32 + kt * 16 + 4 * g + e, at = qi[u] + shift;
                         float cut = 1.f;
                         const float v = score(z[kt][u][e], at - j, &cut);
-                        float ds = exp2f(v - lse[u]) * (dp[kt][u][e] - delta[u]) * cut;
+                        float ds = exp2_fast(v - lse[u]) * (dp[kt][u][e] - delta[u]) * cut;
                         if (!whole && (j >= s.nk || (a.causal && j > at && j >= prefix))) ds = 0.f;
                         fs[u][kt * 4 + e] = (T)ds;
                     }
@@ -607,7 +607,7 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
                         const int i = i0 + qt * 16 + 4 * g + e, at = i + shift, j = kj[u];
                         float cut = 1.f;
                         const float v = score(z[qt][u][e], at - j, &cut);
-                        float pr = exp2f(v - lse[e]);
+                        float pr = exp2_fast(v - lse[e]);
                         float ds = pr * (dp[qt][u][e] - delta[e]) * cut;
                         if (!whole && (i >= s.nq || j >= s.nk || (a.causal && j > at && j >= prefix))) pr = ds = 0.f;
                         fp[u][qt * 4 + e] = (T)pr;

@@ -13,7 +13,7 @@
 
 namespace lcn {
 
-constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct EntropyRow {
     const float *bias;        // nullable
@@ -22,11 +22,12 @@ struct EntropyRow {
     int vocab;
 };
 
-// joins (m, s) with another pair: the sum of exponentials relative to the larger maximum.  -inf: nothing yet.
+// Maxima are kept times log2(e).  Joins (m, s) with another pair: the sum of exponentials relative to the larger
+// maximum.  -inf: nothing yet.
 __device__ __forceinline__ void join(float &m, float &s, float om, float os)
 {
     const float top = fmaxf(m, om);
-    const float a = m == top ? 1.f : exp2f((m - top) * LOG2E), b = om == top ? 1.f : exp2f((om - top) * LOG2E);
+    const float a = m == top ? 1.f : exp2_fast(m - top), b = om == top ? 1.f : exp2_fast(om - top);
     s = s * a + os * b;
     m = top;
 }
@@ -49,21 +50,38 @@ struct EntropyForward {
             bias[i] = f32x4{0.f, 0.f, 0.f, 0.f};
             if (e.r.bias) bias[i] = load_four(e.r.bias + m0 + i * 16 + g4, (int)(p.m - (m0 + i * 16 + g4)), false);
         }
+        const float to_log2 = e.r.scale * LOG2E;
+        const bool edge = m0 + TM * 16 > p.m;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) bias[i] *= LOG2E;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             const long long n = n0 + j * 16 + (lane & 15);
             const long long t = n < p.n ? e.r.target[n] - (m0 + g4) : -1;
-            float top = -__builtin_huge_valf();
+            const bool mine = t >= 0 && t < TM * 16 && (t & 15) < 4 && t + m0 + g4 < p.m;
+            if (__any(mine)) {   // the target is among this lane's words
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+                for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    float z = acc[i][j][u] * e.r.scale + bias[i][u];
-                    if (m0 + i * 16 + g4 + u >= p.m) z = -__builtin_huge_valf();
-                    else if (t == i * 16 + u) e.at_target[n] = z;
-                    acc[i][j][u] = z;
-                    top = fmaxf(top, z);
+                    for (int u = 0; u < 4; ++u)
+                        if (mine && t == i * 16 + u) {
+                            float z = acc[i][j][u] * e.r.scale;
+                            if (e.r.bias) z += e.r.bias[m0 + g4 + t];
+                            e.at_target[n] = z;
+                        }
+            }
+            float top = -__builtin_huge_valf();   // in units of log2(e)
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                acc[i][j] = acc[i][j] * to_log2 + bias[i];
+                if (edge) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        if (m0 + i * 16 + g4 + u >= p.m) acc[i][j][u] = -__builtin_huge_valf();
                 }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) top = fmaxf(top, acc[i][j][u]);
+            }
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             // a row without a finite score: its terms are exp(-inf) = 0, or not a number
@@ -72,7 +90,7 @@ struct EntropyForward {
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int u = 0; u < 4; ++u) sum += exp2f((acc[i][j][u] - ref) * LOG2E);
+                for (int u = 0; u < 4; ++u) sum += exp2_fast(acc[i][j][u] - ref);
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
             if (lane < 16) joined[(wave % WM) * (WN * TN * 16) + (wave / WM) * (TN * 16) + j * 16 + lane] = make_float2(top, sum);
@@ -116,7 +134,7 @@ __global__ __launch_bounds__(256) void entropy_join_kernel(const float2 *__restr
         }
     }
     if (q || n >= rows) return;
-    const float total = m + logf(s);
+    const float total = m * LN2 + logf(s);
     const int64_t t = r.target[n];
     lse[n] = total;
     // no target: no loss; a target outside the vocabulary: not a number
@@ -148,13 +166,15 @@ __global__ __launch_bounds__(256) void entropy_few_kernel(EntropyRow e, const T 
         const float b0 = e.bias ? e.bias[f] : 0.f, b1 = e.bias && two ? e.bias[f + 1] : 0.f;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const float z0 = sum[0][r] * e.scale + b0, z1 = two ? sum[1][r] * e.scale + b1 : -__builtin_huge_valf();
+            float z0 = sum[0][r] * e.scale + b0, z1 = two ? sum[1][r] * e.scale + b1 : -__builtin_huge_valf();
             if ((threadIdx.x & 15) == 0 && r < rows) {
                 if (t[r] == f) at_target[r] = z0;
                 if (t[r] == f + 1 && two) at_target[r] = z1;
             }
+            z0 *= LOG2E;
+            z1 *= LOG2E;
             const float top = fmaxf(m[r], fmaxf(z0, z1)), ref = top == -__builtin_huge_valf() ? 0.f : top;
-            s[r] = s[r] * exp2f((m[r] - ref) * LOG2E) + exp2f((z0 - ref) * LOG2E) + exp2f((z1 - ref) * LOG2E);
+            s[r] = s[r] * exp2_fast(m[r] - ref) + exp2_fast(z0 - ref) + exp2_fast(z1 - ref);
             m[r] = top;
         }
     }
@@ -187,68 +207,84 @@ struct EntropyGradient {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g4 = 4 * (lane >> 4);
         constexpr int BM = WM * TM * 16;
         float *total = (float *)lds;   // [WN][BM]
-        const long long wide = (p.m + 7) & ~7LL;   // G is read in pieces of eight words
-        float lse[TN], grad[TN];
-        long long t[TN];
+        const long long wide = padded(p.m);   // G is read in pieces of eight words
+        char *region = lds + wave * RowRegion<TM>::BYTES;
+        // float tensors: z - lse is formed before it is rounded to units of log2(e); for bf16 ones the rounding of both does
+        // not show, and scores come out of the product in these units
+        const float unit = PLANES == 3 ? 1.f : LOG2E, scale = e.r.scale * unit;
+        const bool edge = m0 + TM * 16 > p.m;
+        f32x4 bias[TM], sum[TM];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const long long m = m0 + i * 16 + g4;
+            bias[i] = sum[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (e.r.bias) bias[i] = load_four(e.r.bias + m, (int)(p.m - m), false) * unit;
+        }
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             const long long n = n0 + j * 16 + (lane & 15);
             const bool in = n < p.n;
-            t[j] = in ? e.r.target[n] : -1;
-            lse[j] = in ? e.lse[n] : 0.f;
-            // a row without a target adds nothing, whatever it holds
-            grad[j] = in && t[j] >= 0 ? e.grad[n] : 0.f;
-            if (t[j] >= e.r.vocab) grad[j] = __builtin_nanf("");   // no such word
-            t[j] = t[j] < 0 ? -1 : t[j] - e.first;
-        }
+            const long long t = in ? e.r.target[n] : -1;
+            const float lse = in ? e.lse[n] * unit : 0.f;
+            // a row without a target adds nothing, whatever it holds: min(x, NaN) is x, min(NaN, 0) is 0
+            const bool none = t < 0;
+            const float grad = none ? 0.f : t >= e.r.vocab ? __builtin_nanf("") : e.grad[n];   // >= vocab: no such word
+            const float most = none ? 0.f : __builtin_nanf("");
+            const long long here = none ? -1 : t - e.first - (m0 + g4);   // the target among this lane's words
+            const int at = here >= 0 && here < TM * 16 ? (int)here : -1;
+            f32x4 col[TM];
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const long long m = m0 + i * 16 + g4;
-            f32x4 bias = {0.f, 0.f, 0.f, 0.f}, sum = {0.f, 0.f, 0.f, 0.f};
-            if (e.r.bias) bias = load_four(e.r.bias + m, (int)(p.m - m), false);
+            for (int i = 0; i < TM; ++i) {
+                f32x4 v = acc[i][j] * scale + bias[i];
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const long long n = n0 + j * 16 + (lane & 15);
-                f32x4 v;
+                for (int u = 0; u < 4; ++u)
+                    v[u] = __builtin_fminf(exp2_fast(PLANES == 3 ? (v[u] - lse) * LOG2E : v[u] - lse), most);
+                if (__any((unsigned)(at - i * 16) < 4u)) {
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const float z = acc[i][j][u] * e.r.scale + bias[u];
-                    float q = exp2f((z - lse[j]) * LOG2E);
-                    if (t[j] == m + u) q -= 1.f;
-                    v[u] = grad[j] == 0.f || m + u >= p.m ? 0.f : q * grad[j];
+                    for (int u = 0; u < 4; ++u)
+                        if (at == i * 16 + u) v[u] -= 1.f;
                 }
-                sum += v;
-                if (n >= p.n || m >= wide) continue;
-                __bf16 *at = e.g + n * e.ldg + m;
-                bf16x4 o[3];
+                v *= grad;
+                if (edge) {
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    __bf16 a, b, c;
-                    if (PLANES == 3) {
-                        split_planes(v[u], a, b, c);
+                    for (int u = 0; u < 4; ++u)
+                        if (m0 + i * 16 + g4 + u >= p.m) v[u] = 0.f;
+                }
+                sum[i] += v;
+                col[i] = v;
+            }
+            by_rows<TM>(
+                region, col, lane, [](int, int) { return Nothing{}; },
+                [&](int r, int c, f32x4 (&v)[2], Nothing) {
+                    const long long row = n0 + j * 16 + r, m = m0 + c;
+                    if (row >= p.n || m >= wide) return;
+                    __bf16 *to = e.g + row * e.ldg + m;
+                    bf16x8 o[3];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        const float x = v[u >> 2][u & 3];
+                        __bf16 a = (__bf16)x, b = a, c3 = a;
+                        if (PLANES == 2) b = (__bf16)(x - (float)a);
+                        if (PLANES == 3) split_planes(x, a, b, c3);
+                        o[0][u] = a;
                         o[1][u] = b;
-                        o[2][u] = c;
-                    } else {
-                        a = (__bf16)v[u];
+                        o[2][u] = c3;
                     }
-                    o[0][u] = a;
-                }
-                *(bf16x4 *)at = o[0];
-                if (PLANES == 3) {
-                    *(bf16x4 *)(at + e.plane) = o[1];
-                    *(bf16x4 *)(at + 2 * e.plane) = o[2];
-                }
-            }
-            if (e.sums) {
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-#pragma unroll
-                    for (int o = 8; o > 0; o >>= 1) sum[u] += __shfl_xor(sum[u], o, 16);
-                    if ((lane & 15) == u) total[(wave / WM) * BM + (wave % WM) * (TM * 16) + i * 16 + g4 + u] = sum[u];
-                }
-            }
+                    *(bf16x8 *)to = o[0];
+                    if (PLANES > 1) *(bf16x8 *)(to + e.plane) = o[1];
+                    if (PLANES > 2) *(bf16x8 *)(to + 2 * e.plane) = o[2];
+                });
         }
         if (!e.sums) return;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) sum[i][u] += __shfl_xor(sum[i][u], o, 16);
+                if ((lane & 15) == u) total[(wave / WM) * BM + (wave % WM) * (TM * 16) + i * 16 + g4 + u] = sum[i][u];
+            }
         __syncthreads();
         const int c = threadIdx.x;
         const long long m = (long long)tm * BM + c;
@@ -296,8 +332,8 @@ static EntropySpace entropy_space(char *ws, int64_t rows, int32_t vocab, int32_t
     } else {
         f.plan = plan_product(vocab, rows, dim, planes_of(dtype), false);
         f.part = (float2 *)c.take((size_t)((vocab + TILE_M[f.plan.tile] - 1) / TILE_M[f.plan.tile]) * rows * 8);
-        f.xp = c.take(planes_bytes(rows, dim, dtype));
-        f.wp = c.take(planes_bytes(vocab, dim, dtype));
+        f.xp = c.take(planes_bytes(rows, dim, planes_of(dtype)));
+        f.wp = c.take(planes_bytes(vocab, dim, planes_of(dtype)));
     }
     f.bytes = c.used;
     return f;
@@ -306,6 +342,7 @@ static EntropySpace entropy_space(char *ws, int64_t rows, int32_t vocab, int32_t
 struct EntropyBackward {
     ProductPlan scores, dx, dw;   // for a piece
     int32_t piece;                // words
+    int planes;                   // of G
     void *xp, *xz, *wp, *g;       // xz: x with zeros in the rows without a target
     float *part_dx, *part_dw, *sums;
     size_t bytes;
@@ -314,21 +351,21 @@ static EntropyBackward entropy_backward_space(char *ws, int64_t rows, int32_t vo
 {
     Carver c{ws};
     EntropyBackward b{};
-    const int planes = planes_of(dtype);
+    const int planes = b.planes = gradient_planes(rows, dtype);
     int64_t most = (int64_t)(PIECE_BYTES / ((size_t)rows * 2 * planes)) & ~(int64_t)255;
     if (most < 256) most = 256;
     const int64_t pieces = (vocab + most - 1) / most;
     int64_t piece = ((vocab + pieces - 1) / pieces + 255) & ~(int64_t)255;   // pieces of about one size
     if (piece > vocab) piece = vocab;
     b.piece = (int32_t)piece;
-    b.scores = plan_product(piece, rows, dim, planes, false);
+    b.scores = plan_product(piece, rows, dim, planes_of(dtype), false);
     b.dx = plan_product(dim, rows, piece, planes, true);
     b.dw = plan_product(dim, piece, rows, planes, true);
-    b.xp = c.take(planes_bytes(rows, dim, dtype));
-    b.xz = c.take(planes_bytes(rows, dim, dtype));
-    b.wp = c.take(planes_bytes(vocab, dim, dtype));
-    b.g = c.take(planes_bytes(rows, piece, dtype));
-    b.part_dx = (float *)c.take((size_t)b.dx.splits * rows * ((dim + 3) & ~3) * 4);
+    b.xp = c.take(planes_bytes(rows, dim, planes_of(dtype)));
+    b.xz = c.take(planes_bytes(rows, dim, planes_of(dtype)));
+    b.wp = c.take(planes_bytes(vocab, dim, planes_of(dtype)));
+    b.g = c.take(planes_bytes(rows, piece, b.planes));
+    b.part_dx = (float *)c.take((size_t)b.dx.splits * rows * padded(dim) * 4);
     b.part_dw = (float *)c.take(partial_bytes(b.dw, dim, piece));
     b.sums = (float *)c.take((size_t)((rows + TILE_N[b.scores.tile] - 1) / TILE_N[b.scores.tile]) * piece * 4);
     b.bytes = c.used;
@@ -397,7 +434,6 @@ static lcn_status entropy_backward_as(const void *x, const void *w, const float 
 {
     const EntropyBackward b = entropy_backward_space(ws, rows, vocab, dim, dtype);
     if (!ws || ((uintptr_t)ws & 255) || ws_bytes < b.bytes) return LCN_ERR_ALLOC;
-    const int planes = planes_of(dtype);
     const size_t size = dtype == LCN_F32 ? 4 : 2;
     Operand wo, xo, xz = plane_operand(b.xz, rows, dim);
     OPCHK(operand_of(w, vocab, dim, dtype, b.wp, s, &wo));
@@ -410,22 +446,22 @@ static lcn_status entropy_backward_as(const void *x, const void *w, const float 
         const Operand g = plane_operand(b.g, rows, words);
         const EntropyRow r{bias ? bias + first : nullptr, target, scale, vocab};
         ProductArgs p{};
-        p.planes = planes;
+        p.planes = planes_of(dtype);
         p.a = here;
         p.b = xo;
         p.m = words;
         p.n = (int)rows;
         p.k = dim;
         float *sums = dbias ? b.sums : nullptr;
-        if (planes == 3)
-            OPCHK((launch_gradient<3>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, s)));
-        else
-            OPCHK((launch_gradient<1>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, s)));
+        OPCHK(b.planes == 3   ? launch_gradient<3>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, s)
+              : b.planes == 2 ? launch_gradient<2>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, s)
+                              : launch_gradient<1>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, s));
         if (dbias) {
             const int parts = (int)((rows + TILE_N[b.scores.tile] - 1) / TILE_N[b.scores.tile]);
             OPCHK(launch_column_sums(sums, parts, words, LCN_F32, dbias + first, s));
         }
         p.m = dim;
+        p.planes = b.planes;
         if (dx) {   // G by rows x W by columns
             p.a = here;
             p.b = g;
@@ -445,7 +481,7 @@ static lcn_status entropy_backward_as(const void *x, const void *w, const float 
         }
     }
     if (dx && !one)
-        OPCHK(launch_add_partials(b.part_dx, b.dx.splits, rows, dim, (dim + 3) & ~3, scale, dtype, dx, s));
+        OPCHK(launch_add_partials(b.part_dx, b.dx.splits, rows, dim, padded(dim), scale, dtype, dx, s));
     return LCN_OK;
 }
 

@@ -15,58 +15,86 @@ struct LinearArgs {
     const T *bias, *residual;
     T *y;
     float *pre;
-    int act, whole;   // whole: groups of four values of a row are aligned in y, residual, bias and pre
+    int act, whole;   // whole: rows of y, residual, bias and pre are whole 16-byte pieces
 };
 
-template <class T>
-__device__ __forceinline__ void linear_finish(const LinearArgs<T> &e, f32x4 z, f32x4 b, long long n, long long m, int width)
+template <class T, int ACT>
+__device__ __forceinline__ void linear_finish(const LinearArgs<T> &e, f32x4 (&z)[2], const f32x4 (&residual)[2], long long at,
+                                              int left)
 {
-    const int left = (int)(width - m);
-    const long long at = n * width + m;
-    z += b;
-    if (e.pre) store_four(e.pre + at, z, left, e.whole);
+    if (e.pre) store_eight(e.pre + at, z, left, e.whole);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) z[u] = activate(z[u], e.act);
-    if (e.residual) z += load_four(e.residual + at, left, e.whole);
-    store_four(e.y + at, z, left, e.whole);
+    for (int u = 0; u < 8; ++u) z[u >> 2][u & 3] = activate<ACT>(z[u >> 2][u & 3]);
+    if (e.residual) {
+        z[0] += residual[0];
+        z[1] += residual[1];
+    }
+    store_eight(e.y + at, z, left, e.whole);
 }
 
-template <class T>
+template <class T, int ACT>
 struct LinearEpilogue {
     typedef LinearArgs<T> Args;
     template <int TM, int TN, int WM, int WN>
     static __device__ void run(const Args &e, const ProductArgs &p, f32x4 (&acc)[TM][TN], long long m0, long long n0, int,
-                               char *, int, int)
+                               char *lds, int, int)
     {
         const int lane = threadIdx.x & 63;
+        char *region = lds + (threadIdx.x >> 6) * RowRegion<TM>::BYTES;
+        f32x4 bias[TM];
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const long long m = m0 + i * 16 + 4 * (lane >> 4);
-            if (m >= p.m) continue;
-            f32x4 b = {0.f, 0.f, 0.f, 0.f};
-            if (e.bias) b = load_four(e.bias + m, (int)(p.m - m), e.whole);
+            bias[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (e.bias && m < p.m) bias[i] = load_four(e.bias + m, (int)(p.m - m), e.whole);
+        }
+        struct Eight {
+            f32x4 v[2];
+        };
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const long long n = n0 + j * 16 + (lane & 15);
-                if (n < p.n) linear_finish(e, acc[i][j], b, n, m, p.m);
-            }
+        for (int j = 0; j < TN; ++j) {
+            f32x4 col[TM];
+#pragma unroll
+            for (int i = 0; i < TM; ++i) col[i] = acc[i][j] + bias[i];
+            by_rows<TM>(
+                region, col, lane,
+                [&](int r, int c) {
+                    Eight o = {};
+                    const long long n = n0 + j * 16 + r, m = m0 + c;
+                    if (e.residual && n < p.n && m < p.m) load_eight(e.residual + n * p.m + m, (int)(p.m - m), e.whole, o.v);
+                    return o;
+                },
+                [&](int r, int c, f32x4 (&v)[2], const Eight &o) {
+                    const long long n = n0 + j * 16 + r, m = m0 + c;
+                    if (n < p.n && m < p.m) linear_finish<T, ACT>(e, v, o.v, n * p.m + m, (int)(p.m - m));
+                });
         }
     }
 };
 
 // the epilogue of a product whose k was shared by workgroups
-template <class T>
+template <class T, int ACT>
 __global__ __launch_bounds__(256) void linear_finish_kernel(LinearArgs<T> e, const float *__restrict__ part, int splits,
                                                             long long stride, long long rows, int width, long long ldp)
 {
-    const int per_row = (width + 3) / 4;
+    const int per_row = (width + 7) / 8;
     for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < rows * per_row; t += (long long)gridDim.x * 256) {
         const long long n = t / per_row;
-        const int m = (int)(t - n * per_row) * 4;
-        f32x4 z = *(const f32x4 *)(part + n * ldp + m), b = {0.f, 0.f, 0.f, 0.f};
-        for (int u = 1; u < splits; ++u) z += *(const f32x4 *)(part + u * stride + n * ldp + m);
-        if (e.bias) b = load_four(e.bias + m, width - m, e.whole);
-        linear_finish(e, z, b, n, m, width);
+        const int m = (int)(t - n * per_row) * 8, left = width - m;
+        f32x4 z[2], v[2], r[2] = {};
+        load_eight(part + n * ldp + m, 8, true, z);
+        for (int u = 1; u < splits; ++u) {
+            load_eight(part + u * stride + n * ldp + m, 8, true, v);
+            z[0] += v[0];
+            z[1] += v[1];
+        }
+        if (e.bias) {
+            load_eight(e.bias + m, left, e.whole, v);
+            z[0] += v[0];
+            z[1] += v[1];
+        }
+        if (e.residual) load_eight(e.residual + n * width + m, left, e.whole, r);
+        linear_finish<T, ACT>(e, z, r, n * width + m, left);
     }
 }
 
@@ -92,7 +120,12 @@ __global__ __launch_bounds__(256) void linear_few_kernel(LinearArgs<T> e, const 
     const long long at = (long long)r * width + f + which;
     if (e.bias) z += (float)e.bias[f + which];
     if (e.pre) e.pre[at] = z;
-    z = activate(z, e.act);
+    switch (e.act) {
+    case LCN_ACT_TANH: z = activate<LCN_ACT_TANH>(z); break;
+    case LCN_ACT_RELU: z = activate<LCN_ACT_RELU>(z); break;
+    case LCN_ACT_GELU: z = activate<LCN_ACT_GELU>(z); break;
+    case LCN_ACT_SILU: z = activate<LCN_ACT_SILU>(z); break;
+    }
     if (e.residual) z += (float)e.residual[at];
     e.y[at] = (T)z;
 }
@@ -110,10 +143,10 @@ static hipError_t launch_few(const LinearArgs<T> &e, const T *x, const T *w, int
 
 // dz = dy act'(z) as planes (dst: nullable), and the sums over this workgroup's rows for every column (part: nullable).
 // 32 pieces of eight columns x 8 rows at a time.
-template <class T>
+template <class T, int ACT>
 __global__ __launch_bounds__(256) void slope_kernel(const T *__restrict__ dy, const float *__restrict__ pre, long long rows,
-                                                    int width, int dp, int act, int rows_each, int whole,
-                                                    __bf16 *__restrict__ dst, float *__restrict__ part)
+                                                    int width, int dp, int rows_each, int whole,
+                                                    int planes, __bf16 *__restrict__ dst, float *__restrict__ part)
 {
     __shared__ float sums[8][32][9];
     const int c = threadIdx.x & 31, q = threadIdx.x >> 5, k = ((int)blockIdx.x * 32 + c) * 8;
@@ -124,15 +157,12 @@ __global__ __launch_bounds__(256) void slope_kernel(const T *__restrict__ dy, co
     if (k < dp)
         for (long long r = r0 + q; r < r0 + rows_each && r < rows; r += 8) {
             f32x4 v[2];
+            load_eight(dy + r * width + k, width - k, whole, v);
+            if constexpr (ACT != LCN_ACT_NONE) {
+                f32x4 z[2];
+                load_eight(pre + r * width + k, width - k, whole, z);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int left = width - k - 4 * h;
-                v[h] = load_four(dy + r * width + k + 4 * h, left, whole);
-                if (act != LCN_ACT_NONE) {
-                    const f32x4 z = load_four(pre + r * width + k + 4 * h, left, whole);
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) v[h][u] *= activate_slope(z[u], act);
-                }
+                for (int u = 0; u < 8; ++u) v[u >> 2][u & 3] *= activate_slope<ACT>(z[u >> 2][u & 3]);
             }
             bf16x8 o[3];
 #pragma unroll
@@ -147,10 +177,8 @@ __global__ __launch_bounds__(256) void slope_kernel(const T *__restrict__ dy, co
             }
             if (dst) {
                 *(bf16x8 *)(dst + r * dp + k) = o[0];
-                if (sizeof(T) == 4) {
-                    *(bf16x8 *)(dst + plane + r * dp + k) = o[1];
-                    *(bf16x8 *)(dst + 2 * plane + r * dp + k) = o[2];
-                }
+                if (planes > 1) *(bf16x8 *)(dst + plane + r * dp + k) = o[1];
+                if (planes > 2) *(bf16x8 *)(dst + 2 * plane + r * dp + k) = o[2];
             }
         }
     if (!part) return;
@@ -169,6 +197,23 @@ __global__ __launch_bounds__(256) void slope_kernel(const T *__restrict__ dy, co
 
 constexpr int FEW_ROWS = 8;
 
+template <int ACT>
+struct Activation {
+    static constexpr int value = ACT;
+};
+// calls f with the activation as a type
+template <class F>
+static hipError_t by_activation(int act, F f)
+{
+    switch (act) {
+    case LCN_ACT_TANH: return f(Activation<LCN_ACT_TANH>());
+    case LCN_ACT_RELU: return f(Activation<LCN_ACT_RELU>());
+    case LCN_ACT_GELU: return f(Activation<LCN_ACT_GELU>());
+    case LCN_ACT_SILU: return f(Activation<LCN_ACT_SILU>());
+    default: return f(Activation<LCN_ACT_NONE>());
+    }
+}
+
 static bool linear_args_fit(int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype)
 {
     return rows >= 0 && rows <= MAX_ROWS && d_in >= 1 && d_in <= MAX_WIDTH && d_out >= 1 && d_out <= MAX_WIDTH &&
@@ -186,8 +231,8 @@ static LinearForward linear_forward_space(char *ws, int64_t rows, int32_t d_in, 
     Carver c{ws};
     LinearForward f;
     f.plan = plan_product(d_out, rows, d_in, planes_of(dtype), true);
-    f.xp = c.take(planes_bytes(rows, d_in, dtype));
-    f.wp = c.take(planes_bytes(d_out, d_in, dtype));
+    f.xp = c.take(planes_bytes(rows, d_in, planes_of(dtype)));
+    f.wp = c.take(planes_bytes(d_out, d_in, planes_of(dtype)));
     f.part = (float *)c.take(partial_bytes(f.plan, d_out, rows));
     f.bytes = c.used;
     return f;
@@ -197,21 +242,22 @@ struct LinearBackward {
     void *xp, *wp, *dz;
     float *part_dx, *part_dw, *sums;
     ProductPlan dx, dw;
-    int groups, rows_each;
+    int planes, groups, rows_each;   // planes of dz
     size_t bytes;
 };
 static LinearBackward linear_backward_space(char *ws, int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype)
 {
     Carver c{ws};
     LinearBackward b;
-    b.dx = plan_product(d_in, rows, d_out, planes_of(dtype), true);
-    b.dw = plan_product(d_in, d_out, rows, planes_of(dtype), true);
+    b.planes = gradient_planes(rows, dtype);
+    b.dx = plan_product(d_in, rows, d_out, b.planes, true);
+    b.dw = plan_product(d_in, d_out, rows, b.planes, true);
     // enough workgroups to fill the chip, at most 256 partial sums per column
     b.rows_each = (int)((((rows + 255) / 256) + 31) & ~31LL);
     b.groups = (int)((rows + b.rows_each - 1) / b.rows_each);
-    b.xp = c.take(planes_bytes(rows, d_in, dtype));
-    b.wp = c.take(planes_bytes(d_out, d_in, dtype));
-    b.dz = c.take(planes_bytes(rows, d_out, dtype));
+    b.xp = c.take(planes_bytes(rows, d_in, planes_of(dtype)));
+    b.wp = c.take(planes_bytes(d_out, d_in, planes_of(dtype)));
+    b.dz = c.take(planes_bytes(rows, d_out, b.planes));
     b.part_dx = (float *)c.take(partial_bytes(b.dx, d_in, rows));
     b.part_dw = (float *)c.take(partial_bytes(b.dw, d_in, d_out));
     b.sums = (float *)c.take((size_t)b.groups * d_out * 4);
@@ -236,8 +282,7 @@ static lcn_status linear_as(const T *x, const T *w, const T *bias, const T *resi
     }
     const LinearForward f = linear_forward_space(ws, rows, d_in, d_out, dtype);
     if (!ws || ((uintptr_t)ws & 255) || ws_bytes < f.bytes) return LCN_ERR_ALLOC;
-    const uintptr_t all = (uintptr_t)y | (uintptr_t)bias | (uintptr_t)residual;
-    e.whole = d_out % 4 == 0 && (all & (4 * sizeof(T) - 1)) == 0 && ((uintptr_t)pre & 15) == 0;
+    e.whole = whole_rows<T>((const void *)((uintptr_t)y | (uintptr_t)bias | (uintptr_t)residual | (uintptr_t)pre), d_out);
     ProductArgs p{};
     OPCHK(operand_of(w, d_out, d_in, dtype, f.wp, s, &p.a));
     OPCHK(operand_of(x, rows, d_in, dtype, f.xp, s, &p.b));
@@ -246,14 +291,18 @@ static lcn_status linear_as(const T *x, const T *w, const T *bias, const T *resi
     p.k = d_in;
     p.planes = planes_of(dtype);
     if (f.plan.splits > 1) {
-        const long long ldp = (d_out + 3) & ~3LL, groups = (rows * (ldp / 4) + 255) / 256;
+        const long long ldp = padded(d_out), groups = (rows * (ldp / 8) + 255) / 256;
         OPCHK((launch_planned<false, false, PartialEpilogue>(f.plan, p, {f.part, ldp, rows * ldp, 0}, s)));
-        hipLaunchKernelGGL(linear_finish_kernel<T>, dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(256), 0, s, e, f.part,
-                           f.plan.splits, rows * ldp, (long long)rows, d_out, ldp);
-        OPCHK(hipGetLastError());
+        OPCHK(by_activation(act, [&](auto a) {
+            hipLaunchKernelGGL((linear_finish_kernel<T, decltype(a)::value>), dim3((unsigned)(groups < 8192 ? groups : 8192)),
+                               dim3(256), 0, s, e, f.part, f.plan.splits, rows * ldp, (long long)rows, d_out, ldp);
+            return hipGetLastError();
+        }));
         return LCN_OK;
     }
-    OPCHK((launch_planned<false, false, LinearEpilogue<T>>(f.plan, p, e, s)));
+    OPCHK(by_activation(act, [&](auto a) {
+        return launch_planned<false, false, LinearEpilogue<T, decltype(a)::value>>(f.plan, p, e, s);
+    }));
     return LCN_OK;
 }
 
@@ -264,17 +313,22 @@ static lcn_status linear_backward_as(const T *x, const T *w, const float *pre, c
 {
     const LinearBackward b = linear_backward_space(ws, rows, d_in, d_out, dtype);
     if (!ws || ((uintptr_t)ws & 255) || ws_bytes < b.bytes) return LCN_ERR_ALLOC;
-    const int planes = planes_of(dtype);
     Operand dz = plane_operand(b.dz, rows, d_out);
     const bool as_is = act == LCN_ACT_NONE && in_place(dy, d_out, dtype);
-    if (as_is) dz = Operand{dy, 0, d_out};
+    int planes = b.planes;
+    if (as_is) {   // dy itself: nothing is rounded
+        dz = Operand{dy, 0, d_out};
+        planes = 1;
+    }
     if (!as_is || dbias) {
         const int dp = (int)padded(d_out);
-        const int whole = d_out % 4 == 0 && ((uintptr_t)dy & (4 * sizeof(T) - 1)) == 0 && ((uintptr_t)pre & 15) == 0;
-        hipLaunchKernelGGL(slope_kernel<T>, dim3((unsigned)((dp + 255) / 256), (unsigned)b.groups), dim3(256), 0, s, dy, pre,
-                           (long long)rows, d_out, dp, act, b.rows_each, whole, as_is ? nullptr : (__bf16 *)b.dz,
-                           dbias ? b.sums : nullptr);
-        OPCHK(hipGetLastError());
+        const int whole = whole_rows<T>((const void *)((uintptr_t)dy | (uintptr_t)pre), d_out);
+        OPCHK(by_activation(act, [&](auto a) {
+            hipLaunchKernelGGL((slope_kernel<T, decltype(a)::value>), dim3((unsigned)((dp + 255) / 256), (unsigned)b.groups),
+                               dim3(256), 0, s, dy, pre, (long long)rows, d_out, dp, b.rows_each, whole, b.planes,
+                               as_is ? nullptr : (__bf16 *)b.dz, dbias ? b.sums : nullptr);
+            return hipGetLastError();
+        }));
         if (dbias) OPCHK(launch_column_sums(b.sums, b.groups, d_out, dtype, dbias, s));
     }
     ProductArgs p{};

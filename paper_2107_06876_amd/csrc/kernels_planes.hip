@@ -102,7 +102,7 @@ ProductPlan plan_product(long long m, long long n, long long k, int planes, bool
         int bm, bn, resident;
         double step_us;   // of one workgroup's 64 values of k with the chip full
     } shape[TILE_COUNT] = {{256, 256, 1, 1.8}, {128, 128, 2, 1.03}, {64, 64, 4, 0.77}, {320, 128, 1, 1.25}};
-    const long long steps = (k + 63) / 64 * (planes == 3 ? 6 : 1);
+    const long long steps = (k + 63) / 64 * pairs_of(planes);
     ProductPlan best{TILE_256, 1};
     double least = 1e300;
     for (int t = 0; t < TILE_COUNT; ++t) {
@@ -131,16 +131,14 @@ hipError_t launch_scaled(const ProductPlan &plan, const ProductArgs &p, float sc
                          hipStream_t s)
 {
     if (plan.splits > 1) {
-        const long long ldp = (p.m + 3) & ~3LL;
+        const long long ldp = padded(p.m);
         const hipError_t e = launch_planned<ACOL, BCOL, PartialEpilogue>(plan, p, {part, ldp, p.n * ldp, 0}, s);
         if (e != hipSuccess) return e;
         return launch_add_partials(part, plan.splits, p.n, p.m, ldp, scale, dtype, out, s);
     }
-    const size_t e = dtype == LCN_F32 ? 4 : 2;
-    const int whole = p.m % 4 == 0 && ((uintptr_t)out & (4 * e - 1)) == 0;
     if (dtype == LCN_F32)
-        return launch_planned<ACOL, BCOL, ScaledEpilogue<float>>(plan, p, {(float *)out, p.m, scale, whole}, s);
-    return launch_planned<ACOL, BCOL, ScaledEpilogue<__bf16>>(plan, p, {(__bf16 *)out, p.m, scale, whole}, s);
+        return launch_planned<ACOL, BCOL, ScaledEpilogue<float>>(plan, p, {(float *)out, p.m, scale, whole_rows<float>(out, p.m)}, s);
+    return launch_planned<ACOL, BCOL, ScaledEpilogue<__bf16>>(plan, p, {(__bf16 *)out, p.m, scale, whole_rows<__bf16>(out, p.m)}, s);
 }
 template hipError_t launch_scaled<true, false>(const ProductPlan &, const ProductArgs &, float, int32_t, void *, float *,
                                                hipStream_t);
@@ -148,7 +146,7 @@ template hipError_t launch_scaled<true, true>(const ProductPlan &, const Product
                                               hipStream_t);
 hipError_t launch_partials(const ProductPlan &plan, const ProductArgs &p, float *part, int add, hipStream_t s)
 {
-    const long long ldp = (p.m + 3) & ~3LL;
+    const long long ldp = padded(p.m);
     return launch_planned<true, false, PartialEpilogue>(plan, p, {part, ldp, p.n * ldp, add}, s);
 }
 

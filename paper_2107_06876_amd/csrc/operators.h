@@ -52,6 +52,43 @@ __device__ __forceinline__ void store_four(T *p, f32x4 v, int left, bool whole)
     }
 }
 
+// The same for eight values in two halves; `whole`: 16-byte pieces are aligned.
+template <class T>
+__device__ __forceinline__ void load_eight(const T *p, int left, bool whole, f32x4 (&r)[2])
+{
+    if constexpr (sizeof(T) == 2) {
+        if (whole && left >= 8) {
+            const bf16x8 v = *(const bf16x8 *)p;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r[e >> 2][e & 3] = (float)v[e];
+            return;
+        }
+    }
+    r[0] = load_four(p, left, whole);
+    r[1] = load_four(p + 4, left - 4, whole);
+}
+template <class T>
+__device__ __forceinline__ void store_eight(T *p, const f32x4 (&v)[2], int left, bool whole)
+{
+    if constexpr (sizeof(T) == 2) {
+        if (whole && left >= 8) {
+            bf16x8 o;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = (T)v[e >> 2][e & 3];
+            *(bf16x8 *)p = o;
+            return;
+        }
+    }
+    store_four(p, v[0], left, whole);
+    store_four(p + 4, v[1], left - 4, whole);
+}
+// Whether rows of `width` values at p are whole aligned 16-byte pieces (of four floats, eight bf16).
+template <class T>
+inline bool whole_rows(const void *p, long long width)
+{
+    return ((uintptr_t)p & 15) == 0 && width % (16 / (int)sizeof(T)) == 0;
+}
+
 // x as the sum of three bf16 (to 2^-26).  A value beyond the largest bf16 is cut, not rounded to infinity; what
 // is not finite stands in the first plane alone.
 __device__ __forceinline__ void split_planes(float x, __bf16 &a, __bf16 &b, __bf16 &c)
@@ -66,42 +103,48 @@ __device__ __forceinline__ void split_planes(float x, __bf16 &a, __bf16 &b, __bf
     c = (__bf16)(r - (float)b);
 }
 
-__device__ __forceinline__ float activate(float z, int act)
+// 2^x by the instruction alone: results below the smallest normal float are zero
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <int ACT>
+__device__ __forceinline__ float activate(float z)
 {
-    switch (act) {
-    case LCN_ACT_TANH: return tanhf(z);
-    case LCN_ACT_RELU: return z > 0.f ? z : z == z ? 0.f : z;
-    case LCN_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-    case LCN_ACT_SILU: return z / (1.f + expf(-z));
-    default: return z;
-    }
+    if constexpr (ACT == LCN_ACT_TANH) return tanhf(z);
+    if constexpr (ACT == LCN_ACT_RELU) return z > 0.f ? z : z == z ? 0.f : z;
+    if constexpr (ACT == LCN_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    if constexpr (ACT == LCN_ACT_SILU) return z / (1.f + expf(-z));
+    return z;
 }
-__device__ __forceinline__ float activate_slope(float z, int act)
+template <int ACT>
+__device__ __forceinline__ float activate_slope(float z)
 {
-    switch (act) {
-    case LCN_ACT_TANH: {
+    if constexpr (ACT == LCN_ACT_TANH) {
         const float t = tanhf(z);
         return 1.f - t * t;
     }
-    case LCN_ACT_RELU: return z > 0.f ? 1.f : z == z ? 0.f : z;
-    case LCN_ACT_GELU:
+    if constexpr (ACT == LCN_ACT_RELU) return z > 0.f ? 1.f : z == z ? 0.f : z;
+    if constexpr (ACT == LCN_ACT_GELU)
         return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
-    case LCN_ACT_SILU: {
+    if constexpr (ACT == LCN_ACT_SILU) {
         const float f = 1.f / (1.f + expf(-z));
         return f * (1.f + z * (1.f - f));
     }
-    default: return 1.f;
-    }
+    return 1.f;
 }
 
 // ---- planes (kernels_planes.hip) --------------------------------------------
-inline long long padded(long long d) { return (d + 7) & ~7LL; }
+inline __host__ __device__ long long padded(long long d) { return (d + 7) & ~7LL; }
 inline int planes_of(int32_t dtype) { return dtype == LCN_F32 ? 3 : 1; }
 // bytes of an operand of rows x d in planes
-inline size_t planes_bytes(long long rows, long long d, int32_t dtype)
+inline size_t planes_bytes(long long rows, long long d, int planes)
 {
-    return ((size_t)rows * (size_t)padded(d) * 2 * planes_of(dtype) + 255) & ~(size_t)255;
+    return ((size_t)rows * (size_t)padded(d) * 2 * planes + 255) & ~(size_t)255;
 }
+// Planes of the gradients dz and G on the way into their products.  One rounding of them to bf16 is as large as that of
+// the result; where few rows are added it can be larger than it in some of the result, so up to FEW_GRADIENT_ROWS rows
+// they have a second plane (the products are then bound by the other operand's bytes).
+constexpr int64_t FEW_GRADIENT_ROWS = 256;
+inline int gradient_planes(int64_t rows, int32_t dtype) { return dtype == LCN_F32 ? 3 : rows <= FEW_GRADIENT_ROWS ? 2 : 1; }
 // Whether a bf16 matrix can be an operand as it lies: rows of whole 16-byte pieces, aligned.
 inline bool in_place(const void *p, long long d, int32_t dtype)
 {
@@ -130,27 +173,38 @@ ProductPlan plan_product(long long m, long long n, long long k, int planes, bool
 struct PartialEpilogue {
     struct Args {
         float *part;
-        long long ldp, stride;   // elements from a row, from a split to the next
+        long long ldp, stride;   // elements from a row, from a split to the next; ldp is a multiple of 8
         int add;
     };
     template <int TM, int TN, int WM, int WN>
     static __device__ void run(const Args &e, const ProductArgs &p, f32x4 (&acc)[TM][TN], long long m0, long long n0,
-                               int split, char *, int, int)
+                               int split, char *lds, int, int)
     {
         const int lane = threadIdx.x & 63;
+        char *region = lds + (threadIdx.x >> 6) * RowRegion<TM>::BYTES;
+        float *first = e.part + split * e.stride + m0;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
-            const long long n = n0 + j * 16 + (lane & 15);
-            if (n >= p.n) continue;
-            float *row = e.part + split * e.stride + n * e.ldp;
+            f32x4 col[TM];
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const long long m = m0 + i * 16 + 4 * (lane >> 4);
-                if (m >= p.m) continue;   // ldp is a multiple of 4: a group of four is inside the row
-                f32x4 v = acc[i][j];
-                if (e.add) v += *(f32x4 *)(row + m);
-                *(f32x4 *)(row + m) = v;
-            }
+            for (int i = 0; i < TM; ++i) col[i] = acc[i][j];
+            struct Eight {
+                f32x4 v[2];
+            };
+            by_rows<TM>(
+                region, col, lane,
+                [&](int r, int c) {
+                    Eight o = {};
+                    const long long n = n0 + j * 16 + r;
+                    if (e.add && n < p.n && m0 + c < p.m) load_eight(first + n * e.ldp + c, 8, true, o.v);
+                    return o;
+                },
+                [&](int r, int c, f32x4 (&v)[2], const Eight &o) {
+                    const long long n = n0 + j * 16 + r;
+                    if (n >= p.n || m0 + c >= p.m) return;
+                    const f32x4 w[2] = {v[0] + o.v[0], v[1] + o.v[1]};
+                    store_eight(first + n * e.ldp + c, w, 8, true);
+                });
         }
     }
 };
@@ -162,23 +216,25 @@ struct ScaledEpilogue {
         T *out;
         long long ld;
         float scale;
-        int whole;   // rows start aligned to four values
+        int whole;   // rows are whole 16-byte pieces
     };
     template <int TM, int TN, int WM, int WN>
     static __device__ void run(const Args &e, const ProductArgs &p, f32x4 (&acc)[TM][TN], long long m0, long long n0, int,
-                               char *, int, int)
+                               char *lds, int, int)
     {
         const int lane = threadIdx.x & 63;
+        char *region = lds + (threadIdx.x >> 6) * RowRegion<TM>::BYTES;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
-            const long long n = n0 + j * 16 + (lane & 15);
-            if (n >= p.n) continue;
+            f32x4 col[TM];
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const long long m = m0 + i * 16 + 4 * (lane >> 4);
-                if (m >= p.m) continue;
-                store_four(e.out + n * e.ld + m, acc[i][j] * e.scale, (int)(p.m - m), e.whole);
-            }
+            for (int i = 0; i < TM; ++i) col[i] = acc[i][j] * e.scale;
+            by_rows<TM>(
+                region, col, lane, [](int, int) { return Nothing{}; },
+                [&](int r, int c, f32x4 (&v)[2], Nothing) {
+                    const long long n = n0 + j * 16 + r, m = m0 + c;
+                    if (n < p.n && m < p.m) store_eight(e.out + n * e.ld + m, v, (int)(p.m - m), e.whole);
+                });
         }
     }
 };
@@ -211,7 +267,7 @@ hipError_t launch_column_sums(const float *part, int parts, int width, int32_t d
 hipError_t launch_zero(void *p, size_t bytes, hipStream_t s);
 inline size_t partial_bytes(const ProductPlan &plan, long long m, long long n)
 {
-    return plan.splits > 1 ? (size_t)plan.splits * (size_t)n * (size_t)((m + 3) & ~3LL) * 4 : 0;
+    return plan.splits > 1 ? (size_t)plan.splits * (size_t)n * (size_t)padded(m) * 4 : 0;
 }
 
 // ---- products with few rows: 16 lanes per row of W ---------------------------

@@ -4,7 +4,8 @@
 // bf16 inputs are one plane.  A float x is three: x1 = bf16(x), x2 = bf16(x - x1), x3 = bf16(x - x1 - x2); what is left
 // is below 2^-26 |x|.  Of the nine products of planes the six with x_i y_j, i + j <= 4, are added (the others are below
 // 2^-25 of the product), the small ones first.  Six bf16 products cost less than one on the fp32 matrix instruction,
-// whose rate is 1/16.
+// whose rate is 1/16.  Two planes of the second operand alone (two products) serve where a rounding of it to one would
+// show in the result.
 //
 // An operand is stored either with k contiguous (`rows`: A[m][k] at m * ld + k) or with its own index contiguous
 // (`columns`: A[k][m] at k * ld + m).  Tiles of 64 values of k go from memory straight into LDS (16 bytes a lane; what is
@@ -34,10 +35,12 @@ struct Operand {
 struct ProductArgs {
     Operand a, b;
     int m, n, k;         // k is padded by zeros up to a multiple of 8 in `rows` operands
-    int planes;          // 1 or 3
+    int planes;          // 1; 2: two of the second operand; 3: three of both
     int splits;          // workgroups that share a tile's k
     int tiles_m, tiles_n;
 };
+
+inline __host__ __device__ int pairs_of(int planes) { return planes == 3 ? 6 : planes; }
 
 enum { STEP_K = 64 };   // values of k per tile in LDS
 
@@ -58,12 +61,17 @@ template <int W, bool COLUMNS, int THREADS>
 struct TileLoader {
     static constexpr int LOADS = W * 8 / THREADS;   // 16-byte pieces per thread
     static_assert(W * 8 % THREADS == 0, "a whole number of pieces per thread");
+    static constexpr int ROW = COLUMNS ? W / 8 : 8;   // pieces of a row of the tile
+    // From one of a thread's pieces to the next: so many rows, the same place in them where that is a whole number that
+    // the permutation does not see.
+    static constexpr bool EVEN = THREADS % ROW == 0 && THREADS / ROW % 16 == 0;
+    static constexpr int KEPT = EVEN ? 1 : LOADS;
     const char *first;        // the workgroup's first index, k = 0, first plane
     long long k_bytes;        // from one tile's k to the next
     unsigned row_bytes, tail; // from a row to the next; bytes of the last row that are read
-    int rows;                 // `rows`: rows there are; `columns`: left for the call
-    unsigned off[LOADS];
-    int need[LOADS];          // `rows`: values of k the piece needs to be left
+    int rows;                 // `rows`: rows there are
+    unsigned off[KEPT];
+    int need[KEPT];           // `rows`: values of k the piece needs to be left
 
     __device__ __forceinline__ void init(const Operand &o, long long i0, int count, int wave, int lane)
     {
@@ -74,16 +82,12 @@ struct TileLoader {
         rows = left < W ? left : W;
         tail = (unsigned)(((left + 7) & ~7) * 2);
 #pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            const int c = (u * (THREADS / 64) + wave) * 64 + lane;
-            if (!COLUMNS) {
-                const int row = c >> 3, piece = (c & 7) ^ rows_swizzle(row);
-                off[u] = (unsigned)row * row_bytes + (unsigned)piece * 16;
-                need[u] = piece * 8;
-            } else {
-                const int kk = c / (W / 8), piece = (c % (W / 8)) ^ columns_swizzle<W>(kk);
-                off[u] = piece * 8 < left ? (unsigned)kk * row_bytes + (unsigned)piece * 16 : 0x80000000u;
-            }
+        for (int u = 0; u < KEPT; ++u) {
+            const int c = (u * (THREADS / 64) + wave) * 64 + lane, row = c / ROW;
+            const int piece = (c % ROW) ^ (COLUMNS ? columns_swizzle<W>(row) : rows_swizzle(row));
+            off[u] = (unsigned)row * row_bytes + (unsigned)piece * 16;
+            need[u] = piece * 8;
+            if (COLUMNS && piece * 8 >= left) off[u] = 0x80000000u;   // outside, also with rows added
         }
     }
     // tile number `step` of the plane that lies `plane` bytes behind the first; k: all values of k
@@ -97,8 +101,9 @@ struct TileLoader {
             __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (unsigned)(r - 1) * row_bytes + end, 0x00020000);
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
-            unsigned o = off[u];
-            if (!COLUMNS) o = need[u] < left ? o : 0x80000000u;
+            unsigned o = off[EVEN ? 0 : u];
+            if (!COLUMNS) o = need[EVEN ? 0 : u] < left ? o : 0x80000000u;
+            if (EVEN) o += u * (THREADS / ROW) * row_bytes;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (lds_void *)(lds + (u * (THREADS / 64) + wave) * 1024), 16, (int)o,
                                                      0, 0, 0);
         }
@@ -152,14 +157,48 @@ __device__ __forceinline__ void tile_of(const ProductArgs &p, int id, int &tm, i
     tn = strip * 4 + in % wide;
 }
 
+// Row by row through LDS: a wavefront's accumulators of 16 columns n (v[i]: rows 16 i + 4 (lane / 16) + 0 .. 3 of column
+// lane % 16) come back as pieces of eight consecutive m, neighbours in neighbouring lanes, so that memory is read and written
+// in whole lines.  ahead(r, c) is called for every piece before (loads that its store will need), then
+// store(r, c, values, what ahead returned), r: column 0 .. 15, c: first m.  `region`: RowRegion<TM>::BYTES of the
+// wavefront's own.
+template <int TM>
+struct RowRegion {
+    static constexpr int PITCH = TM * 16 + 4, BYTES = 16 * PITCH * 4;   // 16 rows of a 128-bit write meet in no bank
+};
+struct Nothing {};
+template <int TM, class Ahead, class Store>
+__device__ __forceinline__ void by_rows(char *region, const f32x4 (&v)[TM], int lane, Ahead ahead, Store store)
+{
+    constexpr int PITCH = RowRegion<TM>::PITCH, ROW = 2 * TM, PIECES = 16 * ROW;
+    float *f = (float *)region;
+    auto next = ahead(lane / ROW, lane % ROW * 8);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) *(f32x4 *)(f + (lane & 15) * PITCH + i * 16 + 4 * (lane >> 4)) = v[i];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // LDS serves a wavefront in order
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1   // a loop: unrolled, epilogues with an activation no longer fit beside unrolled accumulators
+    for (int q = lane; q < PIECES; q += 64) {
+        const auto now = next;
+        if (q + 64 < PIECES) next = ahead((q + 64) / ROW, (q + 64) % ROW * 8);
+        f32x4 w[2];
+        w[0] = *(const f32x4 *)(f + q / ROW * PITCH + q % ROW * 8);
+        w[1] = *(const f32x4 *)(f + q / ROW * PITCH + q % ROW * 8 + 4);
+        store(q / ROW, q % ROW * 8, w, now);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // WM x WN wavefronts of 64, each BM/WM x BN/WN of the tile.  Epi: struct with Args and
-// run<TM, TN>(args, product args, acc, m0, n0, split, lds) for the wavefront's accumulators.
+// run<TM, TN, WM, WN>(args, product args, acc, m0, n0, split, lds, tile) for the wavefront's accumulators.
 template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, class Epi>
 __global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs p, typename Epi::Args e)
 {
     constexpr int THREADS = WM * WN * 64, TM = BM / WM / 16, TN = BN / WN / 16;
     constexpr int ABYTES = BM * STEP_K * 2, BBYTES = BN * STEP_K * 2;
-    __shared__ __align__(1024) char lds0[ABYTES + BBYTES];
+    constexpr int ROWS = WM * WN * RowRegion<TM>::BYTES, TILE = ABYTES + BBYTES;
+    __shared__ __align__(1024) char lds0[TILE > ROWS ? TILE : ROWS];
     __shared__ __align__(1024) char lds1[ABYTES + BBYTES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int tm, tn;
@@ -174,7 +213,7 @@ __global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs p, typ
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    const int ksteps = (p.k + STEP_K - 1) / STEP_K, pairs = p.planes == 3 ? 6 : 1;
+    const int ksteps = (p.k + STEP_K - 1) / STEP_K, pairs = pairs_of(p.planes);
     const int all = ksteps * pairs, per = (all + p.splits - 1) / p.splits;
     const int first = (int)blockIdx.y * per, last = first + per < all ? first + per : all;
 
@@ -185,9 +224,11 @@ __global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs p, typ
     int pair = first / ksteps, step = first - pair * ksteps;   // of the next fetch
     auto fetch = [&](char *lds) {
         long long ia = 0, ib = 0;
-        if (pairs > 1) {   // pairs of planes: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
+        if (pairs == 6) {   // pairs of planes: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
             ia = (0x001012 >> (4 * pair)) & 3;
             ib = (0x010210 >> (4 * pair)) & 3;
+        } else if (pairs == 2) {
+            ib = 1 - pair;
         }
         load_a.load(ia * p.a.plane, step, p.k, lds, wave);
         load_b.load(ib * p.b.plane, step, p.k, lds + ABYTES, wave);
@@ -197,13 +238,16 @@ __global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs p, typ
         }
     };
     auto work = [&](const char *lds) {
+        // places are formed anew for every tile: kept in registers they would not fit beside the accumulators
+        int pa = at_a, pb = at_b;
+        asm volatile("" : "+v"(pa), "+v"(pb));
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
             bf16x8 a[TM], b[TN];
 #pragma unroll
-            for (int i = 0; i < TM; ++i) a[i] = load_fragment<BM, ACOL>(lds, at_a, wm + i * 16, kk);
+            for (int i = 0; i < TM; ++i) a[i] = load_fragment<BM, ACOL>(lds, pa, wm + i * 16, kk);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) b[j] = load_fragment<BN, BCOL>(lds + ABYTES, at_b, wn + j * 16, kk);
+            for (int j = 0; j < TN; ++j) b[j] = load_fragment<BN, BCOL>(lds + ABYTES, pb, wn + j * 16, kk);
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
