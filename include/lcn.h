@@ -422,7 +422,7 @@ lcn_status lcn_cross_entropy(const void *x, const void *W, const float *bias, co
  * forward call: with G_nv = grad_loss_n (exp(z_nv - lse_n) - [v = target(n)]),
  *   dx = scale G W,  dW = scale G^T x  (of type dtype),  dbias_v = sum_n G_nv  (fp32).
  * dx, dW, dbias are nullable.  The vocabulary is worked off in pieces; the
- * workspace holds G of one piece (up to 512 MiB, or 256 words where more rows
+ * workspace holds G of one piece (up to 128 MiB, or 256 words where more rows
  * need more). */
 lcn_status lcn_cross_entropy_backward(const void *x, const void *W, const float *bias, const int64_t *target, const float *lse,
                                       const float *grad_loss, int64_t rows, int32_t vocab, int32_t dim, int32_t dtype,

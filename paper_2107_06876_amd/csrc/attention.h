@@ -32,6 +32,10 @@ struct AttentionArgs {
     // forward
     void *o;
     float *lse;                 // [head][query]
+    // keys split over workgroups: chunks of `chunk` keys, `rows` = max_q * (heads / kv_heads)
+    int chunk, rows;
+    float *part_o;              // [chunk][kv head][row][dim]
+    float2 *part_ml;            // [chunk][kv head][row]: maximum (times log2(e)) and sum
     // backward
     const void *d_o;
     const float *lse_in, *delta;
@@ -179,20 +183,26 @@ __device__ __forceinline__ typename Frag<T>::type read_fragment(const T *row, in
     return f;
 }
 
-// The set that a tile of B tokens belongs to: set p's tiles are numbered from off[p] / B + p on.  All lanes search.
-__device__ __forceinline__ int set_of_tile(const int64_t *off, int sets, int B, long long tile)
+// The last set p of `sets` with below(p), which holds for the first ones; 0 where it holds for none.  All lanes search.
+template <class Below>
+__device__ __forceinline__ int last_set(int sets, Below is_below)
 {
     const int lane = threadIdx.x & 63;
     int lo = 0, n = sets;
     while (n > 1) {
         const int step = (n + 63) >> 6, p = lo + lane * step;
-        const bool below = p < lo + n && off[p] / B + p <= tile;
+        const bool below = p < lo + n && is_below(p);
         const int count = __popcll(__ballot(below));
         const int end = lo + n;
         lo += (count > 0 ? count - 1 : 0) * step;
         n = end - lo < step ? end - lo : step;
     }
     return __builtin_amdgcn_readfirstlane(lo);
+}
+// The set that a tile of B tokens belongs to: set p's tiles are numbered from off[p] / B + p on.
+__device__ __forceinline__ int set_of_tile(const int64_t *off, int sets, int B, long long tile)
+{
+    return last_set(sets, [&](int p) { return off[p] / B + p <= tile; });
 }
 
 struct SetRange {
@@ -384,6 +394,210 @@ __global__ __launch_bounds__(256) void attention_forward_kernel(AttentionArgs a)
         }
         if (g == 0) a.lse[head * a.total_q + n] = (top[u] + log2f(total)) * LN_2;
     }
+}
+
+// Few queries per set (new tokens): the keys of a set are cut into chunks, a workgroup per chunk and key head, so that every
+// key is read once for all query heads that share it.  Bound by reading the keys: each wavefront goes over its own 32 keys at
+// a time, through its own two buffers of LDS without waiting for the others.  A row is a query and one of the heads of
+// the group: row = query * group + head of the group.
+template <class T, int DP, int QT, int WAVES, bool VEC, bool SHAPED>
+__global__ __launch_bounds__(WAVES * 64) void attention_chunk_kernel(AttentionArgs a)
+{
+    constexpr int C = DP / 32, DT = DP / 16, BK = 32;
+    typedef Tile<T, DP> L;
+    constexpr int BYTES = 2 * BK * L::PITCH;   // keys and values of one wavefront
+    __shared__ __align__(1024) char lds0[WAVES * BYTES];
+    __shared__ __align__(1024) char lds1[WAVES * BYTES];
+    __shared__ float2 lds_ml[WAVES][QT * 16];
+    static_assert(WAVES * BYTES >= WAVES * QT * DP * 16 * 4, "the wavefronts' sums fit");
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
+    const int group = a.heads / a.kv_heads;
+    const long long t = die_run(blockIdx.x, gridDim.x);
+    const int kv = (int)(t / a.tiles);
+    const long long tile = t % a.tiles;
+    const int p = set_of_tile(a.k_off, a.sets, a.chunk, tile);
+    SetRange s = range_of(a, p);
+    const long long b0 = (tile - (s.k0 / a.chunk + p)) * a.chunk;
+    if (b0 < 0 || b0 >= s.nk || s.nq <= 0) return;
+    const int shift = s.nk - s.nq, rows = s.nq * group < a.rows ? s.nq * group : a.rows;
+    const int prefix = a.causal && a.prefix ? a.prefix[p] : 0;
+    const int k_first = (int)b0, k_end = k_first + a.chunk < s.nk ? k_first + a.chunk : s.nk;
+    const T *kp = (const T *)a.k + s.k0 * a.k_token + kv * a.k_head;
+    const T *vp = (const T *)a.v + s.k0 * a.v_token + kv * a.v_head;
+
+    typename Frag<T>::type fq[QT][C];
+    Scores<T, SHAPED> score[QT];
+    int qi[QT];
+    f32x4 o[DT][QT];
+    float top[QT], sum[QT];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        const int r = u * 16 + (lane & 15), head = kv * group + r % group;
+        qi[u] = r / group;
+        const T *row = r < rows ? (const T *)a.q + (s.q0 + qi[u]) * a.q_token + head * a.q_head : nullptr;
+#pragma unroll
+        for (int c = 0; c < C; ++c) fq[u][c] = read_fragment<T, VEC>(row, 32 * c + 8 * g, a.dim);
+        score[u].init(a, head);
+        top[u] = minus_infinity();
+        sum[u] = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    constexpr int LOADS = BYTES / 1024;   // of a wavefront for one step
+    auto fetch = [&](int j0, char *lds) {
+        char *own = lds + wave * BYTES;
+        // always the same number of loads: past the end they read nothing
+        const int left = j0 < k_end ? k_end - j0 : 0;
+        const long long at = j0 < k_end ? j0 : 0;
+        TileReader<T, DP, BK, VEC, 64>::read(kp + at * a.k_token, a.k_token, left, a.dim, own, lane);
+        TileReader<T, DP, BK, VEC, 64>::read(vp + at * a.v_token, a.v_token, left, a.dim, own + BK * L::PITCH, lane);
+    };
+    auto work = [&](int j0, const char *lds) {
+        const char *lds_k = lds + wave * BYTES, *lds_v = lds_k + BK * L::PITCH;
+        f32x4 z[2][QT];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int u = 0; u < QT; ++u) z[kt][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+                const typename Frag<T>::type fk = L::rows(lds_k, kt * 16, c, lane);
+#pragma unroll
+                for (int u = 0; u < QT; ++u) mma(z[kt][u], fk, fq[u][c]);
+            }
+        const bool whole = j0 + BK <= k_end && (!a.causal || j0 + BK - 1 <= shift || j0 + BK <= prefix);
+        typename Frag<T>::type fp[QT];
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+            float most = top[u];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = j0 + kt * 16 + 4 * g + e, at = qi[u] + shift;
+                    float v = score[u](z[kt][u][e], at - j, nullptr);
+                    if (!whole && (j >= k_end || (a.causal && j > at && j >= prefix))) v = minus_infinity();
+                    z[kt][u][e] = v;
+                    most = fmaxf(most, v);
+                }
+            most = fmaxf(most, __shfl_xor(most, 16));
+            most = fmaxf(most, __shfl_xor(most, 32));
+            const float ref = most == minus_infinity() ? 0.f : most, keep = exp2_fast(top[u] - ref);
+            top[u] = most;
+            float add = 0.f;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float v = exp2_fast(z[kt][u][e] - ref);
+                    add += v;
+                    fp[u][kt * 4 + e] = (T)v;
+                }
+            sum[u] = sum[u] * keep + add;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d][u] *= keep;
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            const typename Frag<T>::type fv = L::columns(lds_v, 0, d * 16, lane);
+#pragma unroll
+            for (int u = 0; u < QT; ++u) mma(o[d][u], fv, fp[u]);
+        }
+    };
+    auto arrived = [&]() {   // all but the loads of the step after are in LDS
+        if (VEC) __builtin_amdgcn_s_waitcnt((LOADS & 15) | (LOADS >> 4) << 14 | 0x0f70);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+    constexpr int STEP = WAVES * BK;
+    int j0 = k_first + wave * BK;
+    fetch(j0, lds0);
+    for (; j0 < k_end; j0 += 2 * STEP) {
+        fetch(j0 + STEP, lds1);
+        arrived();
+        work(j0, lds0);
+        __builtin_amdgcn_wave_barrier();
+        fetch(j0 + 2 * STEP, lds0);
+        arrived();
+        if (j0 + STEP < k_end) work(j0 + STEP, lds1);
+        __builtin_amdgcn_wave_barrier();
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // no load is under way to LDS that is used again
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        sum[u] += __shfl_xor(sum[u], 16);
+        sum[u] += __shfl_xor(sum[u], 32);
+        if (g == 0) lds_ml[wave][u * 16 + lane] = make_float2(top[u], sum[u]);
+    }
+    __syncthreads();
+    float *all = (float *)lds0;   // [wave][row][dim]
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        float most = minus_infinity();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) most = fmaxf(most, lds_ml[w][u * 16 + (lane & 15)].x);
+        const float keep = most == minus_infinity() ? 0.f : exp2_fast(top[u] - most);
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+            *(f32x4 *)(all + ((long long)wave * QT * 16 + u * 16 + (lane & 15)) * DP + d * 16 + 4 * g) = o[d][u] * keep;
+    }
+    __syncthreads();
+    const long long first = (tile * a.kv_heads + kv) * a.rows;
+    for (int r = wave; r < rows; r += WAVES) {
+        float most = minus_infinity(), total = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) most = fmaxf(most, lds_ml[w][r].x);
+        // a row whose scores here are not numbers has no maximum, but a sum that is not a number
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float2 ml = lds_ml[w][r];
+            total += ml.x == minus_infinity() ? ml.y : ml.y * exp2_fast(ml.x - most);
+        }
+        for (int d = lane; d < a.dim; d += 64) {
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) v += all[((long long)w * QT * 16 + r) * DP + d];
+            a.part_o[(first + r) * a.dim + d] = v;
+        }
+        if (lane == 0) a.part_ml[first + r] = make_float2(most, total);
+    }
+}
+
+// Joins the chunks of a query and head: a wavefront each, in the order of the chunks.
+template <class T>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a)
+{
+    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), n = row / a.heads;
+    const int head = (int)(row % a.heads), lane = threadIdx.x & 63, group = a.heads / a.kv_heads, kv = head / group;
+    if (n >= a.total_q) return;
+    const int p = last_set(a.sets, [&](int q) { return a.q_off[q] <= n; });
+    const SetRange s = range_of(a, p);
+    const long long i = n - s.q0, r = i * group + head % group;
+    if (i < 0 || i >= s.nq || r >= a.rows) return;
+    const long long first = s.k0 / a.chunk + p;
+    const int chunks = (s.nk + a.chunk - 1) / a.chunk;
+    const long long stride = (long long)a.kv_heads * a.rows, at = (first * a.kv_heads + kv) * a.rows + r;
+    float most = minus_infinity();
+    for (int c = lane; c < chunks; c += 64) most = fmaxf(most, a.part_ml[at + c * stride].x);
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) most = fmaxf(most, __shfl_xor(most, x));
+    float total = 0.f, v0 = 0.f, v1 = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < chunks; ++c) {
+        const float2 ml = a.part_ml[at + c * stride];
+        const float keep = ml.x == minus_infinity() ? (ml.y == ml.y ? 0.f : ml.y) : exp2_fast(ml.x - most);
+        const float *o = a.part_o + (at + c * stride) * a.dim;
+        total += ml.y * keep;
+        if (lane < a.dim) v0 += o[lane] * keep;
+        if (lane + 64 < a.dim) v1 += o[lane + 64] * keep;
+    }
+    const float inv = total > 0.f || total != total ? 1.f / total : 0.f;   // no key: zero
+    T *out = (T *)a.o + row * a.dim;
+    if (lane < a.dim) out[lane] = (T)(v0 * inv);
+    if (lane + 64 < a.dim) out[lane + 64] = (T)(v1 * inv);
+    if (lane == 0) a.lse[head * a.total_q + n] = (most + log2f(total)) * LN_2;
 }
 
 // ---- backward -------------------------------------------------------------------
@@ -643,6 +857,8 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
 // one translation unit per type (kernels_attention_*.hip)
 template <class T>
 hipError_t attention_forward(AttentionArgs a, bool vec, bool shaped, hipStream_t s);
+template <class T>
+hipError_t attention_by_chunks(AttentionArgs a, bool vec, bool shaped, hipStream_t s);
 template <class T>
 hipError_t attention_backward(AttentionArgs a, bool vec, bool shaped, float *delta, const T *o, hipStream_t s);
 

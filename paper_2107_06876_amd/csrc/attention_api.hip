@@ -56,6 +56,39 @@ static bool pieces(const AttentionArgs &a, size_t e, const void *const *more, in
     return (all & 15) == 0 && (strides & (long long)(16 / e - 1)) == 0;
 }
 
+// Where a set has few queries, its keys are split over workgroups: up to 32 rows (queries times the heads that share a key
+// head) fit a wavefront.  Chunks of keys are so long that there are some eight workgroups per compute unit, from 128 keys (a
+// step of a workgroup's wavefronts) to 2048.  0: not split, as also where a set has less than 128 keys on average or
+// the plain kernel's workgroups fill the chip several times and sets are short.
+static int chunk_of(const lcn_attention_desc *d)
+{
+    const int64_t rows = d->max_q * (d->heads / d->kv_heads);
+    if (d->max_q == 0 || rows > 32 || d->total_k < 128LL * d->num_sets) return 0;
+    const int64_t keys = d->total_k * d->kv_heads / 2048;
+    const int64_t chunk = (keys + 127) / 128 * 128;
+    return (int)(chunk < 128 ? 128 : chunk > 2048 ? 2048 : chunk);
+}
+struct ChunkSpace {
+    int chunk, rows;
+    float *part_o;
+    float2 *part_ml;
+    size_t bytes;
+};
+static ChunkSpace chunk_space(char *ws, const lcn_attention_desc *d)
+{
+    Carver c{ws};
+    ChunkSpace f{};
+    f.chunk = chunk_of(d);
+    if (f.chunk) {
+        f.rows = (int)(d->max_q * (d->heads / d->kv_heads));
+        const size_t n = (size_t)(d->total_k / f.chunk + d->num_sets) * d->kv_heads * f.rows;
+        f.part_o = (float *)c.take(n * d->head_dim * 4);
+        f.part_ml = (float2 *)c.take(n * 8);
+    }
+    f.bytes = c.used;
+    return f;
+}
+
 }  // namespace lcn
 
 using namespace lcn;
@@ -65,7 +98,7 @@ extern "C" {
 lcn_status lcn_attention_workspace_bytes(const lcn_attention_desc *desc, int32_t backward, size_t *bytes)
 {
     if (!bytes || !attention_desc_fits(desc)) return LCN_ERR_INVALID_ARG;
-    *bytes = backward ? (size_t)desc->heads * (size_t)desc->total_q * 4 : 0;
+    *bytes = backward ? (size_t)desc->heads * (size_t)desc->total_q * 4 : chunk_space(nullptr, desc).bytes;
     return LCN_OK;
 }
 
@@ -80,8 +113,19 @@ lcn_status lcn_attention(const lcn_attention_desc *desc, const void *q, const vo
     a.lse = lse;
     const void *more[1] = {o};
     const bool vec = pieces(a, desc->dtype == LCN_F32 ? 4 : 2, more, 1), shaped = a.cap > 0.f || a.slopes;
-    (void)workspace;
-    (void)workspace_bytes;
+    const ChunkSpace f = chunk_space((char *)workspace, desc);
+    if (f.chunk) {
+        if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < f.bytes) return LCN_ERR_ALLOC;
+        a.chunk = f.chunk;
+        a.rows = f.rows;
+        a.part_o = f.part_o;
+        a.part_ml = f.part_ml;
+        if (desc->dtype == LCN_F32)
+            OPCHK(attention_by_chunks<float>(a, vec, shaped, (hipStream_t)hip_stream));
+        else
+            OPCHK(attention_by_chunks<__bf16>(a, vec, shaped, (hipStream_t)hip_stream));
+        return LCN_OK;
+    }
     if (desc->dtype == LCN_F32)
         OPCHK(attention_forward<float>(a, vec, shaped, (hipStream_t)hip_stream));
     else

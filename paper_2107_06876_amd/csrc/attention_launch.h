@@ -59,6 +59,35 @@ hipError_t attention_forward(AttentionArgs a, bool vec, bool shaped, hipStream_t
 {
     return by_size<T>(a, 0, vec, shaped, s);
 }
+template <class T, int DP, int QT>
+static hipError_t chunks_one(const AttentionArgs &a, bool vec, bool shaped, hipStream_t s)
+{
+    constexpr int WAVES = DP * sizeof(T) > 256 ? 2 : 4;   // two buffers of each wavefront fit into LDS
+    const dim3 grid((unsigned)((long long)a.tiles * a.kv_heads)), block(WAVES * 64);
+    if (vec && !shaped)
+        hipLaunchKernelGGL((attention_chunk_kernel<T, DP, QT, WAVES, true, false>), grid, block, 0, s, a);
+    else if (vec)
+        hipLaunchKernelGGL((attention_chunk_kernel<T, DP, QT, WAVES, true, true>), grid, block, 0, s, a);
+    else
+        hipLaunchKernelGGL((attention_chunk_kernel<T, DP, QT, WAVES, false, true>), grid, block, 0, s, a);
+    return hipGetLastError();
+}
+template <class T, int QT>
+static hipError_t chunks_by_dim(const AttentionArgs &a, bool vec, bool shaped, hipStream_t s)
+{
+    if (a.dim <= 32) return chunks_one<T, 32, QT>(a, vec, shaped, s);
+    if (a.dim <= 64) return chunks_one<T, 64, QT>(a, vec, shaped, s);
+    return chunks_one<T, 128, QT>(a, vec, shaped, s);
+}
+template <class T>
+hipError_t attention_by_chunks(AttentionArgs a, bool vec, bool shaped, hipStream_t s)
+{
+    a.tiles = (int)tiles_of(a.total_k, a.sets, a.chunk);
+    hipError_t e = a.rows <= 16 ? chunks_by_dim<T, 1>(a, vec, shaped, s) : chunks_by_dim<T, 2>(a, vec, shaped, s);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)((a.total_q * a.heads + 3) / 4)), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
 template <class T>
 hipError_t attention_backward(AttentionArgs a, bool vec, bool shaped, float *delta, const T *o, hipStream_t s)
 {

@@ -300,8 +300,9 @@ struct EntropyGradient {
 // ---- host ---------------------------------------------------------------------
 
 constexpr int FEW_ROWS = 8, FEW_GROUPS = 1024;
-// G of a piece of the vocabulary takes at most this much of the workspace
-constexpr size_t PIECE_BYTES = (size_t)512 << 20;
+// G of a piece of the vocabulary takes at most this much of the workspace: what is written stays in the last-level cache until
+// both products have read it (8192 rows against 200 000 words: 6.11 ms; with 64 MiB 7.23, with 256 MiB 6.46, with 512 MiB 6.23)
+constexpr size_t PIECE_BYTES = (size_t)128 << 20;
 
 static bool entropy_args_fit(int64_t rows, int32_t vocab, int32_t dim, int32_t dtype)
 {

@@ -247,10 +247,10 @@ hipError_t launch_planned(const ProductPlan &plan, ProductArgs p, const typename
 {
     p.splits = plan.splits;
     switch (plan.tile) {
-    case TILE_256: return launch_product<256, 256, 2, 4, ACOL, BCOL, Epi>(p, e, s);
-    case TILE_320: return launch_product<320, 128, 4, 2, ACOL, BCOL, Epi>(p, e, s);
-    case TILE_128: return launch_product<128, 128, 2, 2, ACOL, BCOL, Epi>(p, e, s);
-    default: return launch_product<64, 64, 2, 2, ACOL, BCOL, Epi>(p, e, s);
+    case TILE_256: return launch_product<256, 256, 64, 2, 4, ACOL, BCOL, Epi>(p, e, s);
+    case TILE_320: return launch_product<320, 128, 64, 4, 2, ACOL, BCOL, Epi>(p, e, s);
+    case TILE_128: return launch_product<128, 128, 64, 2, 2, ACOL, BCOL, Epi>(p, e, s);
+    default: return launch_product<64, 64, 64, 2, 2, ACOL, BCOL, Epi>(p, e, s);
     }
 }
 

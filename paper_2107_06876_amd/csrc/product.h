@@ -8,7 +8,7 @@
 // show in the result.
 //
 // An operand is stored either with k contiguous (`rows`: A[m][k] at m * ld + k) or with its own index contiguous
-// (`columns`: A[k][m] at k * ld + m).  Tiles of 64 values of k go from memory straight into LDS (16 bytes a lane; what is
+// (`columns`: A[k][m] at k * ld + m).  Tiles of 32 or 64 values of k go from memory straight into LDS (16 bytes a lane; what is
 // outside the operand is read as zero by the buffer's bounds), two tiles of LDS in turn, so that the next tile is on its
 // way while the matrix instructions work on this one.  The 16-byte pieces of a tile are permuted so that neither the
 // 128-bit reads of `rows` tiles nor the transposing 64-bit reads of `columns` tiles meet in a bank.
@@ -42,13 +42,12 @@ struct ProductArgs {
 
 inline __host__ __device__ int pairs_of(int planes) { return planes == 3 ? 6 : planes; }
 
-enum { STEP_K = 64 };   // values of k per tile in LDS
-
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-// permutation of the 16-byte pieces of a tile: of row r (`rows`), of value k (`columns`, W indices wide)
-__device__ __forceinline__ int rows_swizzle(int r) { return (r >> 1) & 7; }
+// permutation of the 16-byte pieces of a tile of BK values of k: of row r (`rows`), of value k (`columns`, W indices wide)
+template <int BK>
+__device__ __forceinline__ int rows_swizzle(int r) { return BK == 64 ? (r >> 1) & 7 : (r >> 2) & 3; }
 template <int W>
 __device__ __forceinline__ int columns_swizzle(int k)
 {
@@ -56,12 +55,12 @@ __device__ __forceinline__ int columns_swizzle(int k)
     return (((k >> 1) & 1) | ((k >> 2) & 2)) << 1;
 }
 
-// One operand's part of the tiles of a workgroup: W indices from i0, 64 values of k at a time, into LDS.
-template <int W, bool COLUMNS, int THREADS>
+// One operand's part of the tiles of a workgroup: W indices from i0, BK values of k at a time, into LDS.
+template <int W, int BK, bool COLUMNS, int THREADS>
 struct TileLoader {
-    static constexpr int LOADS = W * 8 / THREADS;   // 16-byte pieces per thread
-    static_assert(W * 8 % THREADS == 0, "a whole number of pieces per thread");
-    static constexpr int ROW = COLUMNS ? W / 8 : 8;   // pieces of a row of the tile
+    static constexpr int LOADS = W * BK / 8 / THREADS;   // 16-byte pieces per thread
+    static_assert(W * BK / 8 % THREADS == 0, "a whole number of pieces per thread");
+    static constexpr int ROW = COLUMNS ? W / 8 : BK / 8;   // pieces of a row of the tile
     // From one of a thread's pieces to the next: so many rows, the same place in them where that is a whole number that
     // the permutation does not see.
     static constexpr bool EVEN = THREADS % ROW == 0 && THREADS / ROW % 16 == 0;
@@ -78,13 +77,13 @@ struct TileLoader {
         const int left = count - (int)i0;
         row_bytes = (unsigned)(o.ld * 2);
         first = (const char *)o.p + (COLUMNS ? i0 : i0 * o.ld) * 2;
-        k_bytes = COLUMNS ? (long long)STEP_K * o.ld * 2 : STEP_K * 2;
+        k_bytes = COLUMNS ? (long long)BK * o.ld * 2 : BK * 2;
         rows = left < W ? left : W;
         tail = (unsigned)(((left + 7) & ~7) * 2);
 #pragma unroll
         for (int u = 0; u < KEPT; ++u) {
             const int c = (u * (THREADS / 64) + wave) * 64 + lane, row = c / ROW;
-            const int piece = (c % ROW) ^ (COLUMNS ? columns_swizzle<W>(row) : rows_swizzle(row));
+            const int piece = (c % ROW) ^ (COLUMNS ? columns_swizzle<W>(row) : rows_swizzle<BK>(row));
             off[u] = (unsigned)row * row_bytes + (unsigned)piece * 16;
             need[u] = piece * 8;
             if (COLUMNS && piece * 8 >= left) off[u] = 0x80000000u;   // outside, also with rows added
@@ -93,9 +92,9 @@ struct TileLoader {
     // tile number `step` of the plane that lies `plane` bytes behind the first; k: all values of k
     __device__ __forceinline__ void load(long long plane, int step, int k, char *lds, int wave) const
     {
-        const int left = k - step * STEP_K;
+        const int left = k - step * BK;
         const char *base = first + plane + step * k_bytes;
-        const int r = COLUMNS ? (left < STEP_K ? left : STEP_K) : rows;
+        const int r = COLUMNS ? (left < BK ? left : BK) : rows;
         const unsigned end = COLUMNS ? tail : (unsigned)(((left + 7) & ~7) * 2);
         __amdgpu_buffer_rsrc_t res =
             __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (unsigned)(r - 1) * row_bytes + end, 0x00020000);
@@ -112,11 +111,11 @@ struct TileLoader {
 
 // The matrix instruction's operand for indices i .. i + 15 (i a multiple of 16) and the 32 values of k from 32 kk: lane l
 // has index i + l % 16 and k = 32 kk + 8 (l / 16) + 0 .. 7.  `at` is the lane's place for i = 0 and kk = 0.
-template <int W, bool COLUMNS>
+template <int W, int BK, bool COLUMNS>
 __device__ __forceinline__ int fragment_place(int lane)
 {
     if constexpr (!COLUMNS) {
-        return (lane & 15) * 128 + (((lane >> 4) ^ rows_swizzle(lane & 15)) << 4);
+        return (lane & 15) * (BK * 2) + (((lane >> 4) ^ rows_swizzle<BK>(lane & 15)) << 4);
     } else {
         // a group of 16 lanes reads 4 values of k x 16 indices, each lane 4 indices of one k, and gets 4 values of
         // k of one index; the second read is 4 values of k further
@@ -124,11 +123,11 @@ __device__ __forceinline__ int fragment_place(int lane)
         return k * (W * 2) + ((((lane & 3) >> 1) ^ columns_swizzle<W>(k)) << 4) + (lane & 1) * 8;
     }
 }
-template <int W, bool COLUMNS>
+template <int W, int BK, bool COLUMNS>
 __device__ __forceinline__ bf16x8 load_fragment(const char *lds, int at, int i, int kk)
 {
     if constexpr (!COLUMNS) {
-        return *(const bf16x8 *)(lds + (at ^ (kk * 64)) + i * 128);
+        return *(const bf16x8 *)(lds + (at ^ (kk * 64)) + i * (BK * 2));
     } else {
         union {
             s16x4 h[2];
@@ -192,11 +191,11 @@ __device__ __forceinline__ void by_rows(char *region, const f32x4 (&v)[TM], int 
 
 // WM x WN wavefronts of 64, each BM/WM x BN/WN of the tile.  Epi: struct with Args and
 // run<TM, TN, WM, WN>(args, product args, acc, m0, n0, split, lds, tile) for the wavefront's accumulators.
-template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, class Epi>
-__global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs p, typename Epi::Args e)
+template <int BM, int BN, int BK, int WM, int WN, bool ACOL, bool BCOL, class Epi>
+__global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs p, typename Epi::Args e)
 {
     constexpr int THREADS = WM * WN * 64, TM = BM / WM / 16, TN = BN / WN / 16;
-    constexpr int ABYTES = BM * STEP_K * 2, BBYTES = BN * STEP_K * 2;
+    constexpr int ABYTES = BM * BK * 2, BBYTES = BN * BK * 2;
     constexpr int ROWS = WM * WN * RowRegion<TM>::BYTES, TILE = ABYTES + BBYTES;
     __shared__ __align__(1024) char lds0[TILE > ROWS ? TILE : ROWS];
     __shared__ __align__(1024) char lds1[ABYTES + BBYTES];
@@ -206,19 +205,19 @@ __global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs p, typ
     const long long m0 = (long long)tm * BM, n0 = (long long)tn * BN;
     const int wm = (wave % WM) * (BM / WM), wn = (wave / WM) * (BN / WN);
 
-    const int at_a = fragment_place<BM, ACOL>(lane), at_b = fragment_place<BN, BCOL>(lane);
+    const int at_a = fragment_place<BM, BK, ACOL>(lane), at_b = fragment_place<BN, BK, BCOL>(lane);
     f32x4 acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    const int ksteps = (p.k + STEP_K - 1) / STEP_K, pairs = pairs_of(p.planes);
+    const int ksteps = (p.k + BK - 1) / BK, pairs = pairs_of(p.planes);
     const int all = ksteps * pairs, per = (all + p.splits - 1) / p.splits;
     const int first = (int)blockIdx.y * per, last = first + per < all ? first + per : all;
 
-    TileLoader<BM, ACOL, THREADS> load_a;
-    TileLoader<BN, BCOL, THREADS> load_b;
+    TileLoader<BM, BK, ACOL, THREADS> load_a;
+    TileLoader<BN, BK, BCOL, THREADS> load_b;
     load_a.init(p.a, m0, p.m, wave, lane);
     load_b.init(p.b, n0, p.n, wave, lane);
     int pair = first / ksteps, step = first - pair * ksteps;   // of the next fetch
@@ -242,12 +241,12 @@ __global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs p, typ
         int pa = at_a, pb = at_b;
         asm volatile("" : "+v"(pa), "+v"(pb));
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
+        for (int kk = 0; kk < BK / 32; ++kk) {
             bf16x8 a[TM], b[TN];
 #pragma unroll
-            for (int i = 0; i < TM; ++i) a[i] = load_fragment<BM, ACOL>(lds, pa, wm + i * 16, kk);
+            for (int i = 0; i < TM; ++i) a[i] = load_fragment<BM, BK, ACOL>(lds, pa, wm + i * 16, kk);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) b[j] = load_fragment<BN, BCOL>(lds + ABYTES, pb, wn + j * 16, kk);
+            for (int j = 0; j < TN; ++j) b[j] = load_fragment<BN, BK, BCOL>(lds + ABYTES, pb, wn + j * 16, kk);
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -279,12 +278,12 @@ __global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs p, typ
     Epi::template run<TM, TN, WM, WN>(e, p, acc, m0 + wm, n0 + wn, (int)blockIdx.y, lds0, tm, tn);
 }
 
-template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, class Epi>
+template <int BM, int BN, int BK, int WM, int WN, bool ACOL, bool BCOL, class Epi>
 hipError_t launch_product(ProductArgs p, const typename Epi::Args &e, hipStream_t s)
 {
     p.tiles_m = (p.m + BM - 1) / BM;
     p.tiles_n = (p.n + BN - 1) / BN;
-    hipLaunchKernelGGL((product_kernel<BM, BN, WM, WN, ACOL, BCOL, Epi>), dim3((unsigned)(p.tiles_m * p.tiles_n), p.splits),
+    hipLaunchKernelGGL((product_kernel<BM, BN, BK, WM, WN, ACOL, BCOL, Epi>), dim3((unsigned)(p.tiles_m * p.tiles_n), p.splits),
                        dim3(WM * WN * 64), 0, s, p, e);
     return hipGetLastError();
 }

@@ -54,7 +54,7 @@ def _tensor(t, name, shape, dtype, device):
     """The address of a contiguous device tensor of this shape and type; None stays None."""
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or tuple(t.shape) != shape or t.device != device:
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         raise ValueError("%s: expected a contiguous %s tensor of shape %s on %s, got %s %s on %s"
                          % (name, dtype, shape, device, t.dtype, tuple(t.shape), t.device))
     return t.data_ptr()
@@ -66,16 +66,49 @@ def _matrix(t, name):
     return t
 
 
+_sizes = {}   # bytes of workspace by call and sizes
+
+
 def _space(call, sizes, workspace, device):
-    need = ctypes.c_size_t(0)
-    st = call(*sizes, ctypes.byref(need))
-    if st != OK:
-        raise LcnError(st, call.__name__)
+    """The address and size of a workspace, and the tensor that holds it."""
+    need = _sizes.get((call, sizes))
+    if need is None:
+        out = ctypes.c_size_t(0)
+        st = getattr(_library(), call)(*sizes, ctypes.byref(out))
+        if st != OK:
+            raise LcnError(st, call)
+        if len(_sizes) > 4096:
+            _sizes.clear()
+        need = _sizes[(call, sizes)] = out.value
+    return _workspace(need, workspace, device)
+
+
+def _workspace(need, workspace, device):
     if workspace is None:
-        workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
-    elif not workspace.is_contiguous() or workspace.dtype != torch.uint8 or workspace.device != device:
+        if need == 0:
+            return None, 0, None
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        return workspace.data_ptr(), need, workspace
+    if not workspace.is_contiguous() or workspace.dtype != torch.uint8 or workspace.device != device:
         raise ValueError("workspace: expected a contiguous uint8 tensor on %s" % device)
-    return workspace
+    return workspace.data_ptr(), workspace.numel(), workspace
+
+
+def _call(name, device, *args):
+    """Calls an entry point with torch's current stream of `device` as its last argument, on that device."""
+    stream = torch.cuda.current_stream(device).cuda_stream
+    f = getattr(_library(), name)
+    if device.index == torch.cuda.current_device():
+        st = f(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            st = f(*args, stream)
+    if st != OK:
+        raise LcnError(st, name)
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
 
 
 def _linear_shapes(x, w):
@@ -88,40 +121,29 @@ def _linear_shapes(x, w):
 def lcn_linear(x, w, bias=None, residual=None, activation=ACT_NONE, keep_pre=False, out=None, workspace=None):
     """act(x W^T + bias) + residual as a (rows, d_out) tensor; with keep_pre also z = x W^T + bias in float32, which
     lcn_linear_backward takes."""
-    lib = _library()
     rows, d_in, d_out, dtype = _linear_shapes(x, w)
     dev = x.device
     y = torch.empty((rows, d_out), dtype=x.dtype, device=dev) if out is None else out
     pre = torch.empty((rows, d_out), dtype=torch.float32, device=dev) if keep_pre else None
-    ws = _space(lib.lcn_linear_workspace_bytes, (rows, d_in, d_out, dtype, 0), workspace, dev)
-    with torch.cuda.device(dev):
-        st = lib.lcn_linear(x.data_ptr(), w.data_ptr(), _tensor(bias, "bias", (d_out,), x.dtype, dev),
-                            _tensor(residual, "residual", (rows, d_out), x.dtype, dev), rows, d_in, d_out, dtype,
-                            int(activation), _tensor(y, "out", (rows, d_out), x.dtype, dev),
-                            None if pre is None else pre.data_ptr(), ws.data_ptr(), ws.numel(),
-                            torch.cuda.current_stream(dev).cuda_stream)
-    if st != OK:
-        raise LcnError(st, "lcn_linear")
+    at, size, space = _space("lcn_linear_workspace_bytes", (rows, d_in, d_out, dtype, 0), workspace, dev)
+    _call("lcn_linear", dev, x.data_ptr(), w.data_ptr(), _tensor(bias, "bias", (d_out,), x.dtype, dev),
+          _tensor(residual, "residual", (rows, d_out), x.dtype, dev), rows, d_in, d_out, dtype, int(activation),
+          _tensor(y, "out", (rows, d_out), x.dtype, dev), _address(pre), at, size)
     return (y, pre) if keep_pre else y
 
 
 def lcn_linear_backward(x, w, pre, dy, activation=ACT_NONE, with_bias=True, with_x=True, with_w=True, workspace=None):
     """(dx, dw, dbias) for a given dy; pre: what lcn_linear kept (may be None without an activation).  Gradients that
     are not asked for are None."""
-    lib = _library()
     rows, d_in, d_out, dtype = _linear_shapes(x, w)
     dev = x.device
     dx = torch.empty_like(x) if with_x else None
     dw = torch.empty_like(w) if with_w else None
     db = torch.empty(d_out, dtype=x.dtype, device=dev) if with_bias else None
-    ws = _space(lib.lcn_linear_workspace_bytes, (rows, d_in, d_out, dtype, 1), workspace, dev)
-    with torch.cuda.device(dev):
-        st = lib.lcn_linear_backward(x.data_ptr(), w.data_ptr(), _tensor(pre, "pre", (rows, d_out), torch.float32, dev),
-                                     _tensor(dy, "dy", (rows, d_out), x.dtype, dev), rows, d_in, d_out, dtype,
-                                     int(activation), *[None if t is None else t.data_ptr() for t in (dx, dw, db)],
-                                     ws.data_ptr(), ws.numel(), torch.cuda.current_stream(dev).cuda_stream)
-    if st != OK:
-        raise LcnError(st, "lcn_linear_backward")
+    at, size, space = _space("lcn_linear_workspace_bytes", (rows, d_in, d_out, dtype, 1), workspace, dev)
+    _call("lcn_linear_backward", dev, x.data_ptr(), w.data_ptr(), _tensor(pre, "pre", (rows, d_out), torch.float32, dev),
+          _tensor(dy, "dy", (rows, d_out), x.dtype, dev), rows, d_in, d_out, dtype, int(activation), _address(dx),
+          _address(dw), _address(db), at, size)
     return dx, dw, db
 
 
@@ -134,19 +156,14 @@ def _entropy_shapes(x, w):
 
 def lcn_cross_entropy(x, w, target, bias=None, scale=1.0, workspace=None):
     """(loss, lse), float32 per row, of the scores scale x W^T + bias; target: int64, negative where a row has none."""
-    lib = _library()
     rows, vocab, dim, dtype = _entropy_shapes(x, w)
     dev = x.device
     loss = torch.empty(rows, dtype=torch.float32, device=dev)
     lse = torch.empty(rows, dtype=torch.float32, device=dev)
-    ws = _space(lib.lcn_cross_entropy_workspace_bytes, (rows, vocab, dim, dtype, 0), workspace, dev)
-    with torch.cuda.device(dev):
-        st = lib.lcn_cross_entropy(x.data_ptr(), w.data_ptr(), _tensor(bias, "bias", (vocab,), torch.float32, dev),
-                                   _tensor(target, "target", (rows,), torch.int64, dev), rows, vocab, dim, dtype,
-                                   float(scale), loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(),
-                                   torch.cuda.current_stream(dev).cuda_stream)
-    if st != OK:
-        raise LcnError(st, "lcn_cross_entropy")
+    at, size, space = _space("lcn_cross_entropy_workspace_bytes", (rows, vocab, dim, dtype, 0), workspace, dev)
+    _call("lcn_cross_entropy", dev, x.data_ptr(), w.data_ptr(), _tensor(bias, "bias", (vocab,), torch.float32, dev),
+          _tensor(target, "target", (rows,), torch.int64, dev), rows, vocab, dim, dtype, float(scale), loss.data_ptr(),
+          lse.data_ptr(), at, size)
     return loss, lse
 
 
@@ -154,22 +171,16 @@ def lcn_cross_entropy_backward(x, w, target, lse, grad_loss, bias=None, scale=1.
                                workspace=None):
     """(dx, dw, dbias) of sum(grad_loss * loss); lse as lcn_cross_entropy returned it.  dbias is None without a
     bias, dx and dw where they are not asked for."""
-    lib = _library()
     rows, vocab, dim, dtype = _entropy_shapes(x, w)
     dev = x.device
     dx = torch.empty_like(x) if with_x else None
     dw = torch.empty_like(w) if with_w else None
     db = torch.empty(vocab, dtype=torch.float32, device=dev) if bias is not None else None
-    ws = _space(lib.lcn_cross_entropy_workspace_bytes, (rows, vocab, dim, dtype, 1), workspace, dev)
-    with torch.cuda.device(dev):
-        st = lib.lcn_cross_entropy_backward(
-            x.data_ptr(), w.data_ptr(), _tensor(bias, "bias", (vocab,), torch.float32, dev),
-            _tensor(target, "target", (rows,), torch.int64, dev), _tensor(lse, "lse", (rows,), torch.float32, dev),
-            _tensor(grad_loss, "grad_loss", (rows,), torch.float32, dev), rows, vocab, dim, dtype, float(scale),
-            *[None if t is None else t.data_ptr() for t in (dx, dw, db)], ws.data_ptr(), ws.numel(),
-            torch.cuda.current_stream(dev).cuda_stream)
-    if st != OK:
-        raise LcnError(st, "lcn_cross_entropy_backward")
+    at, size, space = _space("lcn_cross_entropy_workspace_bytes", (rows, vocab, dim, dtype, 1), workspace, dev)
+    _call("lcn_cross_entropy_backward", dev, x.data_ptr(), w.data_ptr(), _tensor(bias, "bias", (vocab,), torch.float32, dev),
+          _tensor(target, "target", (rows,), torch.int64, dev), _tensor(lse, "lse", (rows,), torch.float32, dev),
+          _tensor(grad_loss, "grad_loss", (rows,), torch.float32, dev), rows, vocab, dim, dtype, float(scale), _address(dx),
+          _address(dw), _address(db), at, size)
     return dx, dw, db
 
 
@@ -210,24 +221,26 @@ def _attention_desc(q, k, v, q_off, k_off, scale, causal, prefix, slopes, cap, m
                          _tensor(slopes, "slopes", (q.shape[1],), torch.float32, dev), *strides(q), *strides(k), *strides(v))
 
 
+def _attention_space(desc, backward, workspace, device):
+    out = ctypes.c_size_t(0)
+    st = _library().lcn_attention_workspace_bytes(ctypes.byref(desc), backward, ctypes.byref(out))
+    if st != OK:
+        raise LcnError(st, "lcn_attention_workspace_bytes")
+    return _workspace(out.value, workspace, device)
+
+
 def lcn_attention(q, k, v, q_off, k_off, scale=None, causal=False, prefix=None, slopes=None, cap=0.0, max_q=0,
                   workspace=None):
     """(o, lse): attention of the queries of every set to the keys of the same set.  q: (tokens, heads, dim), k and v:
     (tokens, key heads, dim), views with strides are taken; q_off, k_off: int64 offsets of the sets on the device; scale:
     1 / sqrt(dim) where None; prefix: int32 per set; slopes: float32 per head; max_q: the largest number of queries of
     a set, where known.  o is dense like q, lse float32 (heads, tokens); queries in no set are left as they are."""
-    lib = _library()
     d = _attention_desc(q, k, v, q_off, k_off, scale, causal, prefix, slopes, cap, max_q)
     dev = q.device
     o = torch.empty(q.shape, dtype=q.dtype, device=dev)
     lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=dev)
-    ref = ctypes.byref(d)
-    ws = _space(lib.lcn_attention_workspace_bytes, (ref, 0), workspace, dev)
-    with torch.cuda.device(dev):
-        st = lib.lcn_attention(ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), ws.data_ptr(),
-                               ws.numel(), torch.cuda.current_stream(dev).cuda_stream)
-    if st != OK:
-        raise LcnError(st, "lcn_attention")
+    at, size, space = _attention_space(d, 0, workspace, dev)
+    _call("lcn_attention", dev, ctypes.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), at, size)
     return o, lse
 
 
@@ -235,21 +248,14 @@ def lcn_attention_backward(q, k, v, o, lse, dy, q_off, k_off, scale=None, causal
                            max_q=0, with_q=True, with_kv=True, workspace=None):
     """(dq, dk, dv) for a given dy, the gradient of o; o and lse as lcn_attention returned them, the rest as it was
     given.  Gradients are dense; those that are not asked for are None."""
-    lib = _library()
     d = _attention_desc(q, k, v, q_off, k_off, scale, causal, prefix, slopes, cap, max_q)
     dev = q.device
     shape = tuple(q.shape)
     dq = torch.empty(shape, dtype=q.dtype, device=dev) if with_q else None
     dk = torch.empty(k.shape, dtype=q.dtype, device=dev) if with_kv else None
     dv = torch.empty(k.shape, dtype=q.dtype, device=dev) if with_kv else None
-    ref = ctypes.byref(d)
-    ws = _space(lib.lcn_attention_workspace_bytes, (ref, 1), workspace, dev)
-    with torch.cuda.device(dev):
-        st = lib.lcn_attention_backward(ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), _tensor(o, "o", shape, q.dtype, dev),
-                                        _tensor(lse, "lse", (shape[1], shape[0]), torch.float32, dev),
-                                        _tensor(dy, "dy", shape, q.dtype, dev),
-                                        *[None if t is None else t.data_ptr() for t in (dq, dk, dv)], ws.data_ptr(),
-                                        ws.numel(), torch.cuda.current_stream(dev).cuda_stream)
-    if st != OK:
-        raise LcnError(st, "lcn_attention_backward")
+    at, size, space = _attention_space(d, 1, workspace, dev)
+    _call("lcn_attention_backward", dev, ctypes.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+          _tensor(o, "o", shape, q.dtype, dev), _tensor(lse, "lse", (shape[1], shape[0]), torch.float32, dev),
+          _tensor(dy, "dy", shape, q.dtype, dev), _address(dq), _address(dk), _address(dv), at, size)
     return dq, dk, dv
