@@ -314,7 +314,12 @@ static int few_groups(int32_t vocab)
     const int g = (vocab + 31) / 32;
     return g < FEW_GROUPS ? g : FEW_GROUPS;
 }
-static const int TILE_M[TILE_COUNT] = {256, 128, 64, 320}, TILE_N[TILE_COUNT] = {256, 128, 64, 128};
+
+static int64_t row_tiles(const ProductPlan &plan, int64_t rows, int32_t dtype)
+{
+    const int bn = tile_n(plan.tile, planes_of(dtype));
+    return (rows + bn - 1) / bn;
+}
 
 struct EntropySpace {
     ProductPlan plan;         // of the scores
@@ -332,7 +337,7 @@ static EntropySpace entropy_space(char *ws, int64_t rows, int32_t vocab, int32_t
         f.part = (float2 *)c.take((size_t)few_groups(vocab) * rows * 8);
     } else {
         f.plan = plan_product(vocab, rows, dim, planes_of(dtype), false);
-        f.part = (float2 *)c.take((size_t)((vocab + TILE_M[f.plan.tile] - 1) / TILE_M[f.plan.tile]) * rows * 8);
+        f.part = (float2 *)c.take((size_t)((vocab + tile_m(f.plan.tile) - 1) / tile_m(f.plan.tile)) * rows * 8);
         f.xp = c.take(planes_bytes(rows, dim, planes_of(dtype)));
         f.wp = c.take(planes_bytes(vocab, dim, planes_of(dtype)));
     }
@@ -368,7 +373,7 @@ static EntropyBackward entropy_backward_space(char *ws, int64_t rows, int32_t vo
     b.g = c.take(planes_bytes(rows, piece, b.planes));
     b.part_dx = (float *)c.take((size_t)b.dx.splits * rows * padded(dim) * 4);
     b.part_dw = (float *)c.take(partial_bytes(b.dw, dim, piece));
-    b.sums = (float *)c.take((size_t)((rows + TILE_N[b.scores.tile] - 1) / TILE_N[b.scores.tile]) * piece * 4);
+    b.sums = (float *)c.take((size_t)(row_tiles(b.scores, rows, dtype)) * piece * 4);
     b.bytes = c.used;
     return b;
 }
@@ -405,14 +410,16 @@ static lcn_status entropy_as(const T *x, const T *w, const float *bias, const in
         across = 1;
     } else {
         ProductArgs p{};
-        OPCHK(operand_of(w, vocab, dim, dtype, f.wp, s, &p.a));
-        OPCHK(operand_of(x, rows, dim, dtype, f.xp, s, &p.b));
+        PlaneJobs jobs;
+        p.a = add_operand(jobs, w, vocab, dim, dtype, f.wp);
+        p.b = add_operand(jobs, x, rows, dim, dtype, f.xp);
+        OPCHK(launch_planes(jobs, dtype, s));
         p.m = vocab;
         p.n = (int)rows;
         p.k = dim;
         p.planes = planes_of(dtype);
-        OPCHK((launch_planned<false, false, EntropyForward>(f.plan, p, {e, f.part, f.at_target}, s)));
-        parts = (vocab + TILE_M[f.plan.tile] - 1) / TILE_M[f.plan.tile];
+        OPCHK((launch_planned<sizeof(T) == 4 ? 3 : 1, false, false, EntropyForward>(f.plan, p, {e, f.part, f.at_target}, s)));
+        parts = (vocab + tile_m(f.plan.tile) - 1) / tile_m(f.plan.tile);
         across = 16;
     }
     hipLaunchKernelGGL(entropy_join_kernel, dim3((unsigned)((rows + across - 1) / across)), dim3(256), 0, s, f.part, parts,
@@ -425,7 +432,7 @@ template <int PLANES>
 static hipError_t launch_gradient(const ProductPlan &plan, const ProductArgs &p, const EntropyRow &r, long long first,
                                   const float *lse, const float *grad, void *g, long long ldg, float *sums, hipStream_t s)
 {
-    return launch_planned<false, false, EntropyGradient<PLANES>>(plan, p,
+    return launch_planned<PLANES == 3 ? 3 : 1, false, false, EntropyGradient<PLANES>>(plan, p,
                                                                  {r, first, lse, grad, (__bf16 *)g, ldg, p.n * ldg, sums}, s);
 }
 
@@ -436,10 +443,12 @@ static lcn_status entropy_backward_as(const void *x, const void *w, const float 
     const EntropyBackward b = entropy_backward_space(ws, rows, vocab, dim, dtype);
     if (!ws || ((uintptr_t)ws & 255) || ws_bytes < b.bytes) return LCN_ERR_ALLOC;
     const size_t size = dtype == LCN_F32 ? 4 : 2;
-    Operand wo, xo, xz = plane_operand(b.xz, rows, dim);
-    OPCHK(operand_of(w, vocab, dim, dtype, b.wp, s, &wo));
-    OPCHK(operand_of(x, rows, dim, dtype, b.xp, s, &xo));
-    if (dw) OPCHK(launch_planes(x, rows, dim, dtype, target, b.xz, s));
+    PlaneJobs jobs;
+    const Operand wo = add_operand(jobs, w, vocab, dim, dtype, b.wp);
+    const Operand xo = add_operand(jobs, x, rows, dim, dtype, b.xp);
+    Operand xz{};
+    if (dw) xz = add_masked(jobs, x, rows, dim, dtype, target, b.xz);
+    OPCHK(launch_planes(jobs, dtype, s));
     const bool one = b.piece >= vocab;
     for (int64_t first = 0; first < vocab; first += b.piece) {
         const int words = (int)(vocab - first < b.piece ? vocab - first : b.piece);
@@ -458,7 +467,7 @@ static lcn_status entropy_backward_as(const void *x, const void *w, const float 
               : b.planes == 2 ? launch_gradient<2>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, s)
                               : launch_gradient<1>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, s));
         if (dbias) {
-            const int parts = (int)((rows + TILE_N[b.scores.tile] - 1) / TILE_N[b.scores.tile]);
+            const int parts = (int)(row_tiles(b.scores, rows, dtype));
             OPCHK(launch_column_sums(sums, parts, words, LCN_F32, dbias + first, s));
         }
         p.m = dim;

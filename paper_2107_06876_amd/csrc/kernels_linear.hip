@@ -6,7 +6,7 @@
 //
 // Rounding: z, sums and activations are in 32 bits; with bf16 tensors y, dz, dx, dW and db are rounded once each, the kept
 // z is not (as bf16 it would add an error to dz of the size of dz's own rounding).
-#include "operators.h"
+#include "fragments.h"
 
 namespace lcn {
 
@@ -141,6 +141,54 @@ static hipError_t launch_few(const LinearArgs<T> &e, const T *x, const T *w, int
     return hipGetLastError();
 }
 
+// Narrow layers (d_in up to 128, few outputs) on many rows: bound by reading x and writing y, so nothing is laid out first.
+// A workgroup has 64 outputs, their weights in registers, and a wavefront goes over rows 16 at a time, straight from
+// memory into the matrix instruction (float: the float one, whose rate suffices here).
+template <class T, int KP, int ACT, bool VEC>
+__global__ __launch_bounds__(256) void linear_narrow_kernel(LinearArgs<T> e, const T *__restrict__ x, const T *__restrict__ w,
+                                                            long long rows, int k, int width)
+{
+    constexpr int C = KP / 32;
+    const int lane = threadIdx.x & 63, g = lane >> 4, m0 = (int)blockIdx.y * 64;
+    typename Frag<T>::type fw[4][C];
+    f32x4 bias[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int m = m0 + i * 16 + (lane & 15), mb = m0 + i * 16 + 4 * g;
+#pragma unroll
+        for (int c = 0; c < C; ++c) fw[i][c] = read_fragment<T, VEC>(m < width ? w + (long long)m * k : nullptr, 32 * c + 8 * g, k);
+        bias[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (e.bias && mb < width) bias[i] = load_four(e.bias + mb, width - mb, e.whole);
+    }
+    const long long tiles = (rows + 15) / 16, step = (long long)gridDim.x * 4;
+    for (long long t = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); t < tiles; t += step) {
+        const long long n = t * 16 + (lane & 15);
+        const T *row = n < rows ? x + n * k : nullptr;
+        f32x4 acc[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = bias[i];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const typename Frag<T>::type fx = read_fragment<T, VEC>(row, 32 * c + 8 * g, k);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma(acc[i], fw[i][c], fx);
+        }
+        if (n >= rows) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int m = m0 + i * 16 + 4 * g;
+            if (m >= width) continue;
+            const long long at = n * width + m;
+            if (e.pre) store_four(e.pre + at, acc[i], width - m, e.whole);
+            f32x4 y;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) y[u] = activate<ACT>(acc[i][u]);
+            if (e.residual) y += load_four(e.residual + at, width - m, e.whole);
+            store_four(e.y + at, y, width - m, e.whole);
+        }
+    }
+}
+
 // dz = dy act'(z) as planes (dst: nullable), and the sums over this workgroup's rows for every column (part: nullable).
 // 32 pieces of eight columns x 8 rows at a time.
 template <class T, int ACT>
@@ -214,6 +262,20 @@ static hipError_t by_activation(int act, F f)
     }
 }
 
+static bool narrow(int64_t rows, int32_t d_in, int32_t d_out) { return rows >= 128 && d_in <= 128 && d_out <= 256; }
+
+template <class T, int KP, bool VEC>
+static hipError_t launch_narrow(const LinearArgs<T> &e, const T *x, const T *w, int64_t rows, int k, int width, hipStream_t s)
+{
+    const long long groups = (rows + 63) / 64, tiles = (width + 63) / 64, most = 2048 / tiles;
+    return by_activation(e.act, [&](auto a) {
+        hipLaunchKernelGGL((linear_narrow_kernel<T, KP, decltype(a)::value, VEC>),
+                           dim3((unsigned)(groups < most ? groups : most), (unsigned)tiles), dim3(256), 0, s, e, x, w,
+                           (long long)rows, k, width);
+        return hipGetLastError();
+    });
+}
+
 static bool linear_args_fit(int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype)
 {
     return rows >= 0 && rows <= MAX_ROWS && d_in >= 1 && d_in <= MAX_WIDTH && d_out >= 1 && d_out <= MAX_WIDTH &&
@@ -280,19 +342,29 @@ static lcn_status linear_as(const T *x, const T *w, const T *bias, const T *resi
         OPCHK(st);
         return LCN_OK;
     }
+    e.whole = whole_rows<T>((const void *)((uintptr_t)y | (uintptr_t)bias | (uintptr_t)residual | (uintptr_t)pre), d_out);
+    if (narrow(rows, d_in, d_out)) {
+        const bool vec = whole_rows<T>((const void *)((uintptr_t)x | (uintptr_t)w), d_in);
+        OPCHK(!vec          ? launch_narrow<T, 128, false>(e, x, w, rows, d_in, d_out, s)
+              : d_in <= 32 ? launch_narrow<T, 32, true>(e, x, w, rows, d_in, d_out, s)
+              : d_in <= 64 ? launch_narrow<T, 64, true>(e, x, w, rows, d_in, d_out, s)
+                           : launch_narrow<T, 128, true>(e, x, w, rows, d_in, d_out, s));
+        return LCN_OK;
+    }
     const LinearForward f = linear_forward_space(ws, rows, d_in, d_out, dtype);
     if (!ws || ((uintptr_t)ws & 255) || ws_bytes < f.bytes) return LCN_ERR_ALLOC;
-    e.whole = whole_rows<T>((const void *)((uintptr_t)y | (uintptr_t)bias | (uintptr_t)residual | (uintptr_t)pre), d_out);
     ProductArgs p{};
-    OPCHK(operand_of(w, d_out, d_in, dtype, f.wp, s, &p.a));
-    OPCHK(operand_of(x, rows, d_in, dtype, f.xp, s, &p.b));
+    PlaneJobs jobs;
+    p.a = add_operand(jobs, w, d_out, d_in, dtype, f.wp);
+    p.b = add_operand(jobs, x, rows, d_in, dtype, f.xp);
+    OPCHK(launch_planes(jobs, dtype, s));
     p.m = d_out;
     p.n = (int)rows;
     p.k = d_in;
     p.planes = planes_of(dtype);
     if (f.plan.splits > 1) {
         const long long ldp = padded(d_out), groups = (rows * (ldp / 8) + 255) / 256;
-        OPCHK((launch_planned<false, false, PartialEpilogue>(f.plan, p, {f.part, ldp, rows * ldp, 0}, s)));
+        OPCHK((launch_planned<sizeof(T) == 4 ? 3 : 1, false, false, PartialEpilogue>(f.plan, p, {f.part, ldp, rows * ldp, 0}, s)));
         OPCHK(by_activation(act, [&](auto a) {
             hipLaunchKernelGGL((linear_finish_kernel<T, decltype(a)::value>), dim3((unsigned)(groups < 8192 ? groups : 8192)),
                                dim3(256), 0, s, e, f.part, f.plan.splits, rows * ldp, (long long)rows, d_out, ldp);
@@ -301,7 +373,7 @@ static lcn_status linear_as(const T *x, const T *w, const T *bias, const T *resi
         return LCN_OK;
     }
     OPCHK(by_activation(act, [&](auto a) {
-        return launch_planned<false, false, LinearEpilogue<T, decltype(a)::value>>(f.plan, p, e, s);
+        return launch_planned<sizeof(T) == 4 ? 3 : 1, false, false, LinearEpilogue<T, decltype(a)::value>>(f.plan, p, e, s);
     }));
     return LCN_OK;
 }
@@ -332,17 +404,22 @@ static lcn_status linear_backward_as(const T *x, const T *w, const float *pre, c
         if (dbias) OPCHK(launch_column_sums(b.sums, b.groups, d_out, dtype, dbias, s));
     }
     ProductArgs p{};
+    PlaneJobs jobs;
+    Operand xo{}, wo{};
+    if (dx) wo = add_operand(jobs, w, d_out, d_in, dtype, b.wp);
+    if (dw) xo = add_operand(jobs, x, rows, d_in, dtype, b.xp);
+    OPCHK(launch_planes(jobs, dtype, s));
     p.planes = planes;
     p.m = d_in;
     if (dx) {
-        OPCHK(operand_of(w, d_out, d_in, dtype, b.wp, s, &p.a));
+        p.a = wo;
         p.b = dz;
         p.n = (int)rows;
         p.k = d_out;
         OPCHK((launch_scaled<true, false>(b.dx, p, 1.f, dtype, dx, b.part_dx, s)));
     }
     if (dw) {
-        OPCHK(operand_of(x, rows, d_in, dtype, b.xp, s, &p.a));
+        p.a = xo;
         p.b = dz;
         p.n = d_out;
         p.k = (int)rows;
@@ -362,7 +439,7 @@ lcn_status lcn_linear_workspace_bytes(int64_t rows, int32_t d_in, int32_t d_out,
 {
     if (!bytes || !linear_args_fit(rows, d_in, d_out, dtype)) return LCN_ERR_INVALID_ARG;
     *bytes = 0;
-    if (rows == 0 || (!backward && rows <= FEW_ROWS)) return LCN_OK;
+    if (rows == 0 || (!backward && (rows <= FEW_ROWS || narrow(rows, d_in, d_out)))) return LCN_OK;
     *bytes = backward ? linear_backward_space(nullptr, rows, d_in, d_out, dtype).bytes
                       : linear_forward_space(nullptr, rows, d_in, d_out, dtype).bytes;
     return LCN_OK;

@@ -3,21 +3,25 @@
 
 namespace lcn {
 
-// A thread writes 8 values of every plane.  Bound by memory; VEC: source rows are aligned to four values.
-template <class T, bool VEC>
-__global__ __launch_bounds__(256) void planes_kernel(const T *__restrict__ src, long long rows, int d, int dp,
-                                                     const int64_t *__restrict__ target, __bf16 *__restrict__ dst)
+// A thread writes 8 values of every plane.  Bound by memory.
+template <class T>
+__global__ __launch_bounds__(256) void planes_kernel(PlaneJobs jobs)
 {
-    const int per_row = dp / 8;
-    const long long pieces = rows * per_row, plane = rows * dp;
-    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < pieces; t += (long long)gridDim.x * 256) {
+    int at = 0;
+    while (at + 1 < jobs.count && blockIdx.x >= jobs.job[at].end) ++at;
+    const PlaneJobs::Job &j = jobs.job[at];
+    const unsigned begin = at ? jobs.job[at - 1].end : 0, groups = j.end - begin;
+    const int per_row = j.dp / 8;
+    const long long pieces = j.rows * per_row, plane = j.rows * j.dp;
+    __bf16 *dst = (__bf16 *)j.dst;
+    for (long long t = (long long)(blockIdx.x - begin) * 256 + threadIdx.x; t < pieces; t += (long long)groups * 256) {
         const long long r = t / per_row;
         const int k = (int)(t - r * per_row) * 8;
-        const T *p = src + r * d + k;
+        const T *p = (const T *)j.src + r * j.d + k;
         f32x4 v[2];
-        v[0] = load_four(p, d - k, VEC);
-        v[1] = load_four(p + 4, d - k - 4, VEC);
-        if (target && target[r] < 0) v[0] = v[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        v[0] = load_four(p, j.d - k, j.vec);
+        v[1] = load_four(p + 4, j.d - k - 4, j.vec);
+        if (j.target && j.target[r] < 0) v[0] = v[1] = f32x4{0.f, 0.f, 0.f, 0.f};
         bf16x8 o[3];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -35,29 +39,38 @@ __global__ __launch_bounds__(256) void planes_kernel(const T *__restrict__ src, 
     }
 }
 
-template <class T>
-static hipError_t planes_as(const T *src, long long rows, int d, const int64_t *target, void *dst, hipStream_t s)
+Operand add_masked(PlaneJobs &jobs, const void *p, long long rows, int d, int32_t dtype, const int64_t *target, void *space)
 {
-    const int dp = (int)padded(d);
-    const long long groups = (rows * (dp / 8) + 255) / 256;
-    const unsigned grid = (unsigned)(groups < 8192 ? groups : 8192);
-    if (d % 4 == 0 && ((uintptr_t)src & (4 * sizeof(T) - 1)) == 0)
-        hipLaunchKernelGGL((planes_kernel<T, true>), dim3(grid), dim3(256), 0, s, src, rows, d, dp, target, (__bf16 *)dst);
+    const size_t e = dtype == LCN_F32 ? 4 : 2;
+    const long long groups = (rows * (padded(d) / 8) + 255) / 256;
+    PlaneJobs::Job &j = jobs.job[jobs.count];
+    j.src = p;
+    j.dst = space;
+    j.target = target;
+    j.rows = rows;
+    j.d = d;
+    j.dp = (int)padded(d);
+    j.vec = d % 4 == 0 && ((uintptr_t)p & (4 * e - 1)) == 0;
+    j.end = (jobs.count ? jobs.job[jobs.count - 1].end : 0) + (unsigned)(groups < 8192 ? groups : 8192);
+    ++jobs.count;
+    return plane_operand(space, rows, d);
+}
+
+Operand add_operand(PlaneJobs &jobs, const void *p, long long rows, int d, int32_t dtype, void *space)
+{
+    if (in_place(p, d, dtype)) return Operand{p, 0, d};
+    return add_masked(jobs, p, rows, d, dtype, nullptr, space);
+}
+
+hipError_t launch_planes(const PlaneJobs &jobs, int32_t dtype, hipStream_t s)
+{
+    if (!jobs.count) return hipSuccess;
+    const dim3 grid(jobs.job[jobs.count - 1].end);
+    if (dtype == LCN_F32)
+        hipLaunchKernelGGL(planes_kernel<float>, grid, dim3(256), 0, s, jobs);
     else
-        hipLaunchKernelGGL((planes_kernel<T, false>), dim3(grid), dim3(256), 0, s, src, rows, d, dp, target, (__bf16 *)dst);
+        hipLaunchKernelGGL(planes_kernel<__bf16>, grid, dim3(256), 0, s, jobs);
     return hipGetLastError();
-}
-
-hipError_t launch_planes(const void *src, long long rows, int d, int32_t dtype, const int64_t *target, void *dst,
-                         hipStream_t s)
-{
-    if (dtype == LCN_F32) return planes_as((const float *)src, rows, d, target, dst, s);
-    return planes_as((const __bf16 *)src, rows, d, target, dst, s);
-}
-
-Operand plane_operand(const void *dst, long long rows, long long d)
-{
-    return Operand{dst, rows * padded(d) * 2, padded(d)};
 }
 
 // A thread adds four values of a row over all splits, in their order.
@@ -93,21 +106,25 @@ hipError_t launch_add_partials(const float *part, int splits, long long n, int m
 }
 
 // The tile shape and the split with the least estimated time.  A workgroup's step costs its tile's area at the rate
-// that the shape reaches (256 x 256: 1.2 PFLOP/s on 8192^3, 128 x 128: 1.05, 64 x 64: 0.7); `overhead` steps stand for a
-// workgroup's start and epilogue; the chip takes 256 workgroups of the large shapes at a time, 512 and 1024 of the
-// small ones; the partial sums of a split are written and read once at the rate of memory.
+// that the shape reaches on large products (bf16: 256 x 256 1.25 PFLOP/s, 128 x 128 1.1, 64 x 64 0.7; three planes, six
+// products counted: 256 x 128 1.4, 320 x 64 1.1, 128 x 128 1.03, 64 x 64 1.2); two steps stand for a workgroup's start and epilogue; the chip takes 256 workgroups of the large shapes at a
+// time and several times as many small ones; the partial sums of a split are written and read once at the rate of memory.
 ProductPlan plan_product(long long m, long long n, long long k, int planes, bool may_split)
 {
-    static const struct {
-        int bm, bn, resident;
-        double step_us;   // of one workgroup's 64 values of k with the chip full
-    } shape[TILE_COUNT] = {{256, 256, 1, 1.8}, {128, 128, 2, 1.03}, {64, 64, 4, 0.77}, {320, 128, 1, 1.25}};
-    const long long steps = (k + 63) / 64 * pairs_of(planes);
+    struct Shape {
+        int resident;
+        double step_us;   // of one workgroup's step with the chip full: 64 values of k, or 32 in three planes
+    };
+    static const Shape one[TILE_COUNT] = {{1, 1.8}, {2, 1.03}, {4, 0.77}, {1, 1.25}};
+    static const Shape three[TILE_COUNT] = {{1, 2.3}, {1, 1.56}, {3, 1.0}, {1, 1.81}};
+    const Shape *shape = planes == 3 ? three : one;
+    const long long steps = planes == 3 ? (k + 31) / 32 : (k + 63) / 64 * planes;
     ProductPlan best{TILE_256, 1};
     double least = 1e300;
     for (int t = 0; t < TILE_COUNT; ++t) {
-        const long long tiles = ((m + shape[t].bm - 1) / shape[t].bm) * ((n + shape[t].bn - 1) / shape[t].bn);
-        for (int splits = 1; splits <= 64; splits *= 2) {
+        const int bm = tile_m(t), bn = tile_n(t, planes);
+        const long long tiles = ((m + bm - 1) / bm) * ((n + bn - 1) / bn);
+        for (int splits = 1; splits <= 64; splits += splits < 16 ? 1 : 16) {
             if (splits > 1 && (!may_split || steps / splits < 4)) break;
             const long long groups = tiles * splits, room = 256 * shape[t].resident;
             const double rounds = (double)((groups + room - 1) / room);
@@ -132,13 +149,15 @@ hipError_t launch_scaled(const ProductPlan &plan, const ProductArgs &p, float sc
 {
     if (plan.splits > 1) {
         const long long ldp = padded(p.m);
-        const hipError_t e = launch_planned<ACOL, BCOL, PartialEpilogue>(plan, p, {part, ldp, p.n * ldp, 0}, s);
+        const PartialEpilogue::Args a{part, ldp, p.n * ldp, 0};
+        const hipError_t e = p.planes == 3 ? launch_planned<3, ACOL, BCOL, PartialEpilogue>(plan, p, a, s)
+                                           : launch_planned<1, ACOL, BCOL, PartialEpilogue>(plan, p, a, s);
         if (e != hipSuccess) return e;
         return launch_add_partials(part, plan.splits, p.n, p.m, ldp, scale, dtype, out, s);
     }
     if (dtype == LCN_F32)
-        return launch_planned<ACOL, BCOL, ScaledEpilogue<float>>(plan, p, {(float *)out, p.m, scale, whole_rows<float>(out, p.m)}, s);
-    return launch_planned<ACOL, BCOL, ScaledEpilogue<__bf16>>(plan, p, {(__bf16 *)out, p.m, scale, whole_rows<__bf16>(out, p.m)}, s);
+        return launch_planned<3, ACOL, BCOL, ScaledEpilogue<float>>(plan, p, {(float *)out, p.m, scale, whole_rows<float>(out, p.m)}, s);
+    return launch_planned<1, ACOL, BCOL, ScaledEpilogue<__bf16>>(plan, p, {(__bf16 *)out, p.m, scale, whole_rows<__bf16>(out, p.m)}, s);
 }
 template hipError_t launch_scaled<true, false>(const ProductPlan &, const ProductArgs &, float, int32_t, void *, float *,
                                                hipStream_t);
@@ -147,7 +166,9 @@ template hipError_t launch_scaled<true, true>(const ProductPlan &, const Product
 hipError_t launch_partials(const ProductPlan &plan, const ProductArgs &p, float *part, int add, hipStream_t s)
 {
     const long long ldp = padded(p.m);
-    return launch_planned<true, false, PartialEpilogue>(plan, p, {part, ldp, p.n * ldp, add}, s);
+    const PartialEpilogue::Args a{part, ldp, p.n * ldp, add};
+    return p.planes == 3 ? launch_planned<3, true, false, PartialEpilogue>(plan, p, a, s)
+                         : launch_planned<1, true, false, PartialEpilogue>(plan, p, a, s);
 }
 
 // column sums: part is [parts][width]; 32 columns per workgroup, 8 threads each, in a fixed order
@@ -175,17 +196,6 @@ hipError_t launch_column_sums(const float *part, int parts, int width, int32_t d
     else
         hipLaunchKernelGGL(column_sums_kernel<__bf16>, dim3(grid), dim3(256), 0, s, part, parts, width, (__bf16 *)out);
     return hipGetLastError();
-}
-
-// the operand of a matrix: as it lies, or its planes at `space`
-hipError_t operand_of(const void *p, long long rows, int d, int32_t dtype, void *space, hipStream_t s, Operand *o)
-{
-    if (in_place(p, d, dtype)) {
-        *o = Operand{p, 0, d};
-        return hipSuccess;
-    }
-    *o = plane_operand(space, rows, d);
-    return launch_planes(p, rows, d, dtype, nullptr, space, s);
 }
 
 // zeros by a kernel: a fill of memory that a caller may capture into a graph

@@ -150,13 +150,27 @@ inline bool in_place(const void *p, long long d, int32_t dtype)
 {
     return dtype == LCN_BF16 && d % 8 == 0 && ((uintptr_t)p & 15) == 0;
 }
-// rows x d of `dtype` into planes at dst, rows padded with zeros to a multiple of 8; rows whose `target` is negative
-// become zero (target: nullable).
-hipError_t launch_planes(const void *src, long long rows, int d, int32_t dtype, const int64_t *target, void *dst,
-                         hipStream_t s);
-Operand plane_operand(const void *dst, long long rows, long long d);
-// the operand of a matrix: as it lies, or its planes at `space`
-hipError_t operand_of(const void *p, long long rows, int d, int32_t dtype, void *space, hipStream_t s, Operand *o);
+// Matrices to lay out in planes, all by one launch: rows x d into planes at dst, rows padded with zeros to a multiple of 8;
+// rows whose `target` is negative become zero (target: nullable).
+struct PlaneJobs {
+    enum { MOST = 3 };
+    struct Job {
+        const void *src;
+        void *dst;
+        const int64_t *target;
+        long long rows;
+        int d, dp, vec;
+        unsigned end;   // workgroups of this job and those before
+    } job[MOST];
+    int count = 0;
+};
+// The operand of a matrix: as it lies where that can be, else its planes at `space`, which become one of the jobs.
+Operand add_operand(PlaneJobs &jobs, const void *p, long long rows, int d, int32_t dtype, void *space);
+// The same, always in planes, with the rows whose target is negative zero.
+Operand add_masked(PlaneJobs &jobs, const void *p, long long rows, int d, int32_t dtype, const int64_t *target, void *space);
+hipError_t launch_planes(const PlaneJobs &jobs, int32_t dtype, hipStream_t s);
+// planes that a kernel has written to dst
+inline Operand plane_operand(const void *dst, long long rows, long long d) { return Operand{dst, rows * padded(d) * 2, padded(d)}; }
 
 // out[n][m] (dtype, m dense, width m) = scale * the sum of `splits` partial products (float, [split][n][ldp])
 hipError_t launch_add_partials(const float *part, int splits, long long n, int m, long long ldp, float scale, int32_t dtype,
@@ -240,17 +254,33 @@ struct ScaledEpilogue {
 };
 
 // Tile shapes: index -> BM x BN.  256 x 256 has the best rate; the smaller ones fill the chip where the result is
-// small, 320 x 128 keeps a row of up to 320 values in one tile.
+// small, the 320 wide one keeps a row of up to 320 values in one tile.  With three planes a tile has 32 values of k and
+// all planes of both operands in LDS, so the large ones are half as wide in n.
 enum { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2, TILE_320 = 3, TILE_COUNT = 4 };
-template <bool ACOL, bool BCOL, class Epi>
+inline int tile_m(int tile) { return tile == TILE_256 ? 256 : tile == TILE_128 ? 128 : tile == TILE_64 ? 64 : 320; }
+inline int tile_n(int tile, int planes)
+{
+    if (planes == 3) return tile == TILE_256 || tile == TILE_128 ? 128 : 64;
+    return tile == TILE_256 ? 256 : tile == TILE_64 ? 64 : 128;
+}
+template <int NP, bool ACOL, bool BCOL, class Epi>
 hipError_t launch_planned(const ProductPlan &plan, ProductArgs p, const typename Epi::Args &e, hipStream_t s)
 {
     p.splits = plan.splits;
-    switch (plan.tile) {
-    case TILE_256: return launch_product<256, 256, 64, 2, 4, ACOL, BCOL, Epi>(p, e, s);
-    case TILE_320: return launch_product<320, 128, 64, 4, 2, ACOL, BCOL, Epi>(p, e, s);
-    case TILE_128: return launch_product<128, 128, 64, 2, 2, ACOL, BCOL, Epi>(p, e, s);
-    default: return launch_product<64, 64, 64, 2, 2, ACOL, BCOL, Epi>(p, e, s);
+    if constexpr (NP == 3) {
+        switch (plan.tile) {
+        case TILE_256: return launch_product<256, 128, 32, 4, 2, 3, ACOL, BCOL, Epi>(p, e, s);
+        case TILE_320: return launch_product<320, 64, 32, 4, 2, 3, ACOL, BCOL, Epi>(p, e, s);
+        case TILE_128: return launch_product<128, 128, 32, 2, 2, 3, ACOL, BCOL, Epi>(p, e, s);
+        default: return launch_product<64, 64, 32, 2, 2, 3, ACOL, BCOL, Epi>(p, e, s);
+        }
+    } else {
+        switch (plan.tile) {
+        case TILE_256: return launch_product<256, 256, 64, 2, 4, 1, ACOL, BCOL, Epi>(p, e, s);
+        case TILE_320: return launch_product<320, 128, 64, 4, 2, 1, ACOL, BCOL, Epi>(p, e, s);
+        case TILE_128: return launch_product<128, 128, 64, 2, 2, 1, ACOL, BCOL, Epi>(p, e, s);
+        default: return launch_product<64, 64, 64, 2, 2, 1, ACOL, BCOL, Epi>(p, e, s);
+        }
     }
 }
 
@@ -322,12 +352,12 @@ struct Carver {
     }
 };
 
-#define OPCHK(call)                         \
-    do {                                    \
-        if ((call) != hipSuccess) {         \
-            (void)hipGetLastError();        \
-            return LCN_ERR_DEVICE;          \
-        }                                   \
+#define OPCHK(...)                            \
+    do {                                      \
+        if ((__VA_ARGS__) != hipSuccess) {    \
+            (void)hipGetLastError();          \
+            return LCN_ERR_DEVICE;            \
+        }                                     \
     } while (0)
 
 }  // namespace lcn

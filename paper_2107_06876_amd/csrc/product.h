@@ -40,8 +40,6 @@ struct ProductArgs {
     int tiles_m, tiles_n;
 };
 
-inline __host__ __device__ int pairs_of(int planes) { return planes == 3 ? 6 : planes; }
-
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
@@ -58,8 +56,8 @@ __device__ __forceinline__ int columns_swizzle(int k)
 // One operand's part of the tiles of a workgroup: W indices from i0, BK values of k at a time, into LDS.
 template <int W, int BK, bool COLUMNS, int THREADS>
 struct TileLoader {
-    static constexpr int LOADS = W * BK / 8 / THREADS;   // 16-byte pieces per thread
-    static_assert(W * BK / 8 % THREADS == 0, "a whole number of pieces per thread");
+    static constexpr int PIECES = W * BK / 8, LOADS = (PIECES + THREADS - 1) / THREADS;   // 16 bytes each
+    static_assert(PIECES % 64 == 0, "whole wavefronts of pieces");
     static constexpr int ROW = COLUMNS ? W / 8 : BK / 8;   // pieces of a row of the tile
     // From one of a thread's pieces to the next: so many rows, the same place in them where that is a whole number that
     // the permutation does not see.
@@ -100,6 +98,7 @@ struct TileLoader {
             __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (unsigned)(r - 1) * row_bytes + end, 0x00020000);
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
+            if (PIECES % THREADS && (u * (THREADS / 64) + wave) * 64 >= PIECES) break;
             unsigned o = off[EVEN ? 0 : u];
             if (!COLUMNS) o = need[EVEN ? 0 : u] < left ? o : 0x80000000u;
             if (EVEN) o += u * (THREADS / ROW) * row_bytes;
@@ -140,6 +139,11 @@ __device__ __forceinline__ bf16x8 load_fragment(const char *lds, int at, int i, 
         f.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(q + 4 * (W * 2)));
         return f.v;
     }
+}
+
+__device__ __forceinline__ f32x4 mfma_bf16(bf16x8 a, bf16x8 b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
 // The tile that a workgroup works on.  Workgroups are dealt to the eight dies in turn: a die gets a run of
@@ -189,16 +193,16 @@ __device__ __forceinline__ void by_rows(char *region, const f32x4 (&v)[TM], int 
     __builtin_amdgcn_wave_barrier();
 }
 
-// WM x WN wavefronts of 64, each BM/WM x BN/WN of the tile.  Epi: struct with Args and
+// WM x WN wavefronts of 64, each BM/WM x BN/WN of the tile; NP: 3 planes of both operands at a time, or 1.  Epi: struct with Args and
 // run<TM, TN, WM, WN>(args, product args, acc, m0, n0, split, lds, tile) for the wavefront's accumulators.
-template <int BM, int BN, int BK, int WM, int WN, bool ACOL, bool BCOL, class Epi>
+template <int BM, int BN, int BK, int WM, int WN, int NP, bool ACOL, bool BCOL, class Epi>
 __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs p, typename Epi::Args e)
 {
     constexpr int THREADS = WM * WN * 64, TM = BM / WM / 16, TN = BN / WN / 16;
     constexpr int ABYTES = BM * BK * 2, BBYTES = BN * BK * 2;
-    constexpr int ROWS = WM * WN * RowRegion<TM>::BYTES, TILE = ABYTES + BBYTES;
+    constexpr int ROWS = WM * WN * RowRegion<TM>::BYTES, TILE = NP * (ABYTES + BBYTES);
     __shared__ __align__(1024) char lds0[TILE > ROWS ? TILE : ROWS];
-    __shared__ __align__(1024) char lds1[ABYTES + BBYTES];
+    __shared__ __align__(1024) char lds1[TILE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int tm, tn;
     tile_of(p, blockIdx.x, tm, tn);
@@ -212,7 +216,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs p, 
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    const int ksteps = (p.k + BK - 1) / BK, pairs = pairs_of(p.planes);
+    const int ksteps = (p.k + BK - 1) / BK, pairs = NP == 3 ? 1 : p.planes;
     const int all = ksteps * pairs, per = (all + p.splits - 1) / p.splits;
     const int first = (int)blockIdx.y * per, last = first + per < all ? first + per : all;
 
@@ -222,18 +226,20 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs p, 
     load_b.init(p.b, n0, p.n, wave, lane);
     int pair = first / ksteps, step = first - pair * ksteps;   // of the next fetch
     auto fetch = [&](char *lds) {
-        long long ia = 0, ib = 0;
-        if (pairs == 6) {   // pairs of planes: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
-            ia = (0x001012 >> (4 * pair)) & 3;
-            ib = (0x010210 >> (4 * pair)) & 3;
-        } else if (pairs == 2) {
-            ib = 1 - pair;
-        }
-        load_a.load(ia * p.a.plane, step, p.k, lds, wave);
-        load_b.load(ib * p.b.plane, step, p.k, lds + ABYTES, wave);
-        if (++step == ksteps) {
-            step = 0;
-            ++pair;
+        if constexpr (NP == 3) {
+#pragma unroll
+            for (int u = 0; u < 3; ++u) {
+                load_a.load(u * p.a.plane, step, p.k, lds + u * ABYTES, wave);
+                load_b.load(u * p.b.plane, step, p.k, lds + 3 * ABYTES + u * BBYTES, wave);
+            }
+            ++step;
+        } else {   // two planes of B: the second one first
+            load_a.load(0, step, p.k, lds, wave);
+            load_b.load(pairs == 2 ? (1 - pair) * p.b.plane : 0, step, p.k, lds + ABYTES, wave);
+            if (++step == ksteps) {
+                step = 0;
+                ++pair;
+            }
         }
     };
     auto work = [&](const char *lds) {
@@ -242,16 +248,44 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs p, 
         asm volatile("" : "+v"(pa), "+v"(pb));
 #pragma unroll
         for (int kk = 0; kk < BK / 32; ++kk) {
-            bf16x8 a[TM], b[TN];
+            if constexpr (NP == 3) {
+                bf16x8 b[3][TN];
 #pragma unroll
-            for (int i = 0; i < TM; ++i) a[i] = load_fragment<BM, BK, ACOL>(lds, pa, wm + i * 16, kk);
+                for (int u = 0; u < 3; ++u)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) b[j] = load_fragment<BN, BK, BCOL>(lds + ABYTES, pb, wn + j * 16, kk);
+                    for (int j = 0; j < TN; ++j)
+                        b[u][j] = load_fragment<BN, BK, BCOL>(lds + 3 * ABYTES + u * BBYTES, pb, wn + j * 16, kk);
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+                for (int i = 0; i < TM; ++i) {
+                    bf16x8 a[3];
 #pragma unroll
-                for (int j = 0; j < TN; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
+                    for (int u = 0; u < 3; ++u) a[u] = load_fragment<BM, BK, ACOL>(lds + u * ABYTES, pa, wm + i * 16, kk);
+                    // the five small products are added up by themselves, so that the sum is rounded twice in a step
+                    f32x4 t[TN];
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) t[j] = mfma_bf16(a[2], b[0][j], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) t[j] = mfma_bf16(a[1], b[1][j], t[j]);
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) t[j] = mfma_bf16(a[0], b[2][j], t[j]);
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) t[j] = mfma_bf16(a[1], b[0][j], t[j]);
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) t[j] = mfma_bf16(a[0], b[1][j], t[j]);
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = mfma_bf16(a[0], b[0][j], acc[i][j]) + t[j];
+                }
+            } else {
+                bf16x8 a[TM], b[TN];
+#pragma unroll
+                for (int i = 0; i < TM; ++i) a[i] = load_fragment<BM, BK, ACOL>(lds, pa, wm + i * 16, kk);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) b[j] = load_fragment<BN, BK, BCOL>(lds + ABYTES, pb, wn + j * 16, kk);
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = mfma_bf16(a[i], b[j], acc[i][j]);
+            }
         }
     };
     auto arrived = [&]() {   // this wavefront's loads are in LDS, and so are all others'
@@ -278,12 +312,12 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs p, 
     Epi::template run<TM, TN, WM, WN>(e, p, acc, m0 + wm, n0 + wn, (int)blockIdx.y, lds0, tm, tn);
 }
 
-template <int BM, int BN, int BK, int WM, int WN, bool ACOL, bool BCOL, class Epi>
+template <int BM, int BN, int BK, int WM, int WN, int NP, bool ACOL, bool BCOL, class Epi>
 hipError_t launch_product(ProductArgs p, const typename Epi::Args &e, hipStream_t s)
 {
     p.tiles_m = (p.m + BM - 1) / BM;
     p.tiles_n = (p.n + BN - 1) / BN;
-    hipLaunchKernelGGL((product_kernel<BM, BN, BK, WM, WN, ACOL, BCOL, Epi>), dim3((unsigned)(p.tiles_m * p.tiles_n), p.splits),
+    hipLaunchKernelGGL((product_kernel<BM, BN, BK, WM, WN, NP, ACOL, BCOL, Epi>), dim3((unsigned)(p.tiles_m * p.tiles_n), p.splits),
                        dim3(WM * WN * 64), 0, s, p, e);
     return hipGetLastError();
 }

@@ -60,12 +60,6 @@ def _tensor(t, name, shape, dtype, device):
     return t.data_ptr()
 
 
-def _matrix(t, name):
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2 or t.dtype not in _TYPES or not t.is_contiguous():
-        raise ValueError("%s: expected a contiguous float32 or bfloat16 device matrix" % name)
-    return t
-
-
 _sizes = {}   # bytes of workspace by call and sizes
 
 
@@ -94,9 +88,17 @@ def _workspace(need, workspace, device):
     return workspace.data_ptr(), workspace.numel(), workspace
 
 
+def _raw_stream(index):
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# the same without the object around it, where torch has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)
+
+
 def _call(name, device, *args):
     """Calls an entry point with torch's current stream of `device` as its last argument, on that device."""
-    stream = torch.cuda.current_stream(device).cuda_stream
+    stream = _raw_stream(device.index)
     f = getattr(_library(), name)
     if device.index == torch.cuda.current_device():
         st = f(*args, stream)
@@ -111,17 +113,22 @@ def _address(t):
     return None if t is None else t.data_ptr()
 
 
-def _linear_shapes(x, w):
-    x, w = _matrix(x, "x"), _matrix(w, "w")
-    if x.dtype != w.dtype or x.device != w.device or x.shape[1] != w.shape[1]:
-        raise ValueError("x (rows, d_in) and w (d_out, d_in) must agree in type, device and d_in")
-    return x.shape[0], x.shape[1], w.shape[0], _TYPES[x.dtype]
+def _matrices(x, w, inner):
+    """Rows of x and w, their common width and type: contiguous device matrices."""
+    dtype = _TYPES.get(x.dtype)
+    if (dtype is None or w.dtype is not x.dtype or x.dim() != 2 or w.dim() != 2 or not x.is_cuda or w.device != x.device
+            or not x.is_contiguous() or not w.is_contiguous()):
+        raise ValueError("x and w: expected contiguous float32 or bfloat16 matrices of one type on one device")
+    rows, width = x.shape
+    if w.shape[1] != width:
+        raise ValueError("x and w must agree in %s" % inner)
+    return rows, w.shape[0], width, dtype
 
 
 def lcn_linear(x, w, bias=None, residual=None, activation=ACT_NONE, keep_pre=False, out=None, workspace=None):
     """act(x W^T + bias) + residual as a (rows, d_out) tensor; with keep_pre also z = x W^T + bias in float32, which
     lcn_linear_backward takes."""
-    rows, d_in, d_out, dtype = _linear_shapes(x, w)
+    rows, d_out, d_in, dtype = _matrices(x, w, "d_in")
     dev = x.device
     y = torch.empty((rows, d_out), dtype=x.dtype, device=dev) if out is None else out
     pre = torch.empty((rows, d_out), dtype=torch.float32, device=dev) if keep_pre else None
@@ -135,7 +142,7 @@ def lcn_linear(x, w, bias=None, residual=None, activation=ACT_NONE, keep_pre=Fal
 def lcn_linear_backward(x, w, pre, dy, activation=ACT_NONE, with_bias=True, with_x=True, with_w=True, workspace=None):
     """(dx, dw, dbias) for a given dy; pre: what lcn_linear kept (may be None without an activation).  Gradients that
     are not asked for are None."""
-    rows, d_in, d_out, dtype = _linear_shapes(x, w)
+    rows, d_out, d_in, dtype = _matrices(x, w, "d_in")
     dev = x.device
     dx = torch.empty_like(x) if with_x else None
     dw = torch.empty_like(w) if with_w else None
@@ -147,16 +154,9 @@ def lcn_linear_backward(x, w, pre, dy, activation=ACT_NONE, with_bias=True, with
     return dx, dw, db
 
 
-def _entropy_shapes(x, w):
-    x, w = _matrix(x, "x"), _matrix(w, "w")
-    if x.dtype != w.dtype or x.device != w.device or x.shape[1] != w.shape[1]:
-        raise ValueError("x (rows, dim) and w (vocab, dim) must agree in type, device and dim")
-    return x.shape[0], w.shape[0], x.shape[1], _TYPES[x.dtype]
-
-
 def lcn_cross_entropy(x, w, target, bias=None, scale=1.0, workspace=None):
     """(loss, lse), float32 per row, of the scores scale x W^T + bias; target: int64, negative where a row has none."""
-    rows, vocab, dim, dtype = _entropy_shapes(x, w)
+    rows, vocab, dim, dtype = _matrices(x, w, "dim")
     dev = x.device
     loss = torch.empty(rows, dtype=torch.float32, device=dev)
     lse = torch.empty(rows, dtype=torch.float32, device=dev)
@@ -171,7 +171,7 @@ def lcn_cross_entropy_backward(x, w, target, lse, grad_loss, bias=None, scale=1.
                                workspace=None):
     """(dx, dw, dbias) of sum(grad_loss * loss); lse as lcn_cross_entropy returned it.  dbias is None without a
     bias, dx and dw where they are not asked for."""
-    rows, vocab, dim, dtype = _entropy_shapes(x, w)
+    rows, vocab, dim, dtype = _matrices(x, w, "dim")
     dev = x.device
     dx = torch.empty_like(x) if with_x else None
     dw = torch.empty_like(w) if with_w else None
