@@ -29,6 +29,8 @@ SOURCES = {
     "kernels_entropy.hip": [],
     "kernels_attention_f32.hip": [],
     "kernels_attention_bf16.hip": [],
+    "kernels_attention_grad_f32.hip": [],
+    "kernels_attention_grad_bf16.hip": [],
     "attention_api.hip": [],
     "lcn_api.hip": [],
     "calibrate.hip": [],

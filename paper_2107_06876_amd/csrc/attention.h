@@ -30,7 +30,7 @@ struct AttentionArgs {
     float scale, cap;
     int tiles;                  // of queries (forward, dq) or keys (dk, dv), over all sets
     // forward
-    void *o;
+    void *o;                    // read in the backward pass
     float *lse;                 // [head][query]
     // keys split over workgroups: chunks of `chunk` keys, `rows` = max_q * (heads / kv_heads)
     int chunk, rows;
@@ -38,7 +38,8 @@ struct AttentionArgs {
     float2 *part_ml;            // [chunk][kv head][row]: maximum (times log2(e)) and sum
     // backward
     const void *d_o;
-    const float *lse_in, *delta;
+    const float *lse_in;
+    float *delta;               // [head][query]
     void *dq, *dk, *dv;
 };
 
@@ -86,35 +87,70 @@ constexpr float LOG2_E = 1.4426950408889634f, LN_2 = 0.6931471805599453f;
 __device__ __forceinline__ float cap_tanh(float x, __bf16) { return 1.f - 2.f * __builtin_amdgcn_rcpf(exp2_fast(2.f * LOG2_E * x) + 1.f); }
 __device__ __forceinline__ float cap_tanh(float x, float) { return tanhf(x); }
 
-// Turns q . k into the score times log2(e).  SHAPED: there is a cap or a slope; `cut`: the cap's derivative.
+// Turns q . k into the score times log2(e), four at a time.  SHAPED: there is a cap or a slope (or a scale that is not
+// positive); without, the scale is left for the exponential's argument, `unit`: scores are monotonous in q . k.
 template <class T, bool SHAPED>
 struct Scores {
-    float scale, cap, inv_cap, slope;
+    float unit, scale, cap, inv_cap, slope;
     __device__ __forceinline__ void init(const AttentionArgs &a, int head)
     {
-        scale = SHAPED ? a.scale : a.scale * LOG2_E;
-        cap = a.cap;
-        inv_cap = SHAPED && a.cap > 0.f ? 1.f / a.cap : 0.f;
-        slope = SHAPED && a.slopes ? a.slopes[head] : 0.f;
+        unit = SHAPED ? 1.f : a.scale * LOG2_E;
+        scale = a.scale * LOG2_E;
+        cap = a.cap * LOG2_E;
+        inv_cap = SHAPED && a.cap > 0.f ? a.scale / a.cap : 0.f;
+        slope = SHAPED && a.slopes ? a.slopes[head] * LOG2_E : 0.f;
     }
-    __device__ __forceinline__ float operator()(float dot, int behind, float *cut) const
+    // z: q . k of a query and four keys (STEP = -1) or a key and four queries (STEP = 1), `ahead`: how far the first query
+    // is ahead of the first key; cut: the cap's derivative, where not nullptr
+    template <int STEP>
+    __device__ __forceinline__ void shape(f32x4 &z, int ahead, f32x4 *cut) const
     {
-        if constexpr (!SHAPED) {
-            return dot * scale;
-        } else {
-            float z = dot * scale;
+        if constexpr (SHAPED) {
             if (cap > 0.f) {
-                const float t = cap_tanh(z * inv_cap, T());
-                z = cap * t;
-                if (cut) *cut = 1.f - t * t;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float t = cap_tanh(z[e] * inv_cap, T());
+                    z[e] = cap * t;
+                    if (cut) (*cut)[e] = 1.f - t * t;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[e] *= scale;
+                if (cut) *cut = f32x4{1.f, 1.f, 1.f, 1.f};
             }
-            z -= slope * __builtin_fabsf((float)behind);
-            return z * LOG2_E;
+            const float far = (float)ahead;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[e] -= slope * __builtin_fabsf(far + (float)(STEP * e));
         }
     }
 };
 
+template <int N>
+struct Buffer {
+    static constexpr int value = N;
+};
+
 __device__ __forceinline__ float minus_infinity() { return -__builtin_huge_valf(); }
+
+// The accumulators are in general registers from here on.  Without, the compiler (AMD clang 22, ROCm 7.2) has left out the wait between the
+// last matrix instruction and a read of its result behind a branch (attention_chunk_kernel: a wait of 1 to 6 cycles
+// where 8 are due, wrong scores); in one stretch of code it puts it in.
+template <int N, int M>
+__device__ __forceinline__ void settle(f32x4 (&z)[N][M])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < M; ++j) asm volatile("" : "+v"(z[i][j]));
+}
+
+// The same behind a loop whose last instructions are matrix instructions.
+__device__ __forceinline__ void settle_loop()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15");
+    __builtin_amdgcn_sched_barrier(0);
+}
 
 // Workgroups are dealt to the eight dies in turn; a die gets a run of neighbours, which share keys or queries.
 __device__ __forceinline__ long long die_run(long long id, long long total)
@@ -123,65 +159,109 @@ __device__ __forceinline__ long long die_run(long long id, long long total)
     return die * base + (die < more ? die : more) + nth;
 }
 
+// What a workgroup of the forward and dq kernels works on: a tile of BQ queries of a set, for one head.
+struct QueryTile {
+    SetRange s;
+    int head, kv, first, shift, prefix, last;   // last: behind the last key that any query of the tile sees
+    bool any;
+};
+template <int BQ>
+__device__ __forceinline__ QueryTile query_tile(const AttentionArgs &a)
+{
+    QueryTile w;
+    const int group = a.heads / a.kv_heads;
+    const long long t = die_run(blockIdx.x, gridDim.x);
+    w.head = (int)(t / ((long long)a.tiles * group)) * group + (int)(t % group);
+    w.kv = w.head / group;
+    const long long tile = a.tiles - 1 - (t / group) % a.tiles;   // causal: the long ones first
+    const int p = set_of_tile(a.q_off, a.sets, BQ, tile);
+    w.s = range_of(a, p);
+    const long long b0 = (tile - (w.s.q0 / BQ + p)) * BQ;
+    w.any = b0 >= 0 && b0 < w.s.nq;
+    w.first = (int)b0;
+    w.shift = w.s.nk - w.s.nq;
+    w.prefix = a.causal && a.prefix ? a.prefix[p] : 0;
+    w.last = w.s.nk;
+    if (a.causal) {
+        const int reach = (w.first + BQ < w.s.nq ? w.first + BQ : w.s.nq) + w.shift;
+        w.last = reach > w.prefix ? reach : w.prefix;
+        w.last = w.last < w.s.nk ? w.last : w.s.nk;
+    }
+    return w;
+}
+
+// Steps 0 .. steps - 1 with two buffers in turn: step t + 1 is on its way while t is worked on.  fetch(t, which),
+// landed(t, which): what is left to do when step t's loads have arrived (before all wavefronts meet), work(t, which).
+template <class Fetch, class Landed, class Work>
+__device__ __forceinline__ void two_buffers(int steps, Fetch fetch, Landed landed, Work work)
+{
+    auto arrived = [&](int t, auto which) {
+        __builtin_amdgcn_s_waitcnt(0x0f70);
+        landed(t, which);
+        __syncthreads();
+    };
+    if (steps <= 0) return;
+    fetch(0, Buffer<0>());
+    int t = 0;
+    for (; t + 2 <= steps; t += 2) {
+        arrived(t, Buffer<0>());
+        fetch(t + 1, Buffer<1>());
+        work(t, Buffer<0>());
+        arrived(t + 1, Buffer<1>());
+        if (t + 2 < steps) fetch(t + 2, Buffer<0>());
+        work(t + 1, Buffer<1>());
+    }
+    if (t < steps) {
+        arrived(t, Buffer<0>());
+        work(t, Buffer<0>());
+    }
+}
+
 // ---- forward -------------------------------------------------------------------
 // Four wavefronts of 16 QT queries each go over the set's keys, 64 at a time.
 template <class T, int DP, int QT, bool VEC, bool SHAPED>
-__global__ __launch_bounds__(256) void attention_forward_kernel(AttentionArgs a)
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward_kernel(AttentionArgs a)
 {
     constexpr int BQ = 64 * QT, BK = 64, C = DP / 32, DT = DP / 16;
     typedef Tile<T, DP> L;
-    __shared__ __align__(1024) char lds_k[BK * L::PITCH];
-    __shared__ __align__(1024) char lds_v[BK * L::PITCH];
+    __shared__ __align__(1024) char lds0[2 * BK * L::PITCH];
+    __shared__ __align__(1024) char lds1[2 * BK * L::PITCH];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
-    const int group = a.heads / a.kv_heads;
-    const long long t = die_run(blockIdx.x, gridDim.x);
-    const int head = (int)(t / ((long long)a.tiles * group)) * group + (int)(t % group), kv = head / group;
-    const long long tile = a.tiles - 1 - (t / group) % a.tiles;
-    const int p = set_of_tile(a.q_off, a.sets, BQ, tile);
-    const SetRange s = range_of(a, p);
-    const long long first_tile = s.q0 / BQ + p;
-    const long long b0 = (tile - first_tile) * BQ;
-    if (b0 < 0 || b0 >= s.nq) return;
-    const int q_first = (int)b0, shift = s.nk - s.nq;
-    const int prefix = a.causal && a.prefix ? a.prefix[p] : 0;
-    int last = s.nk;   // keys that any query of the tile sees
-    if (a.causal) {
-        const int reach = (q_first + BQ < s.nq ? q_first + BQ : s.nq) + shift;
-        last = reach > prefix ? reach : prefix;
-        last = last < s.nk ? last : s.nk;
-    }
+    const QueryTile w = query_tile<BQ>(a);
+    if (!w.any) return;
+    const SetRange s = w.s;
     Scores<T, SHAPED> score;
-    score.init(a, head);
+    score.init(a, w.head);
 
-    const T *qp = (const T *)a.q + s.q0 * a.q_token + head * a.q_head;
-    const T *kp = (const T *)a.k + s.k0 * a.k_token + kv * a.k_head;
-    const T *vp = (const T *)a.v + s.k0 * a.v_token + kv * a.v_head;
+    const T *qp = (const T *)a.q + s.q0 * a.q_token + w.head * a.q_head;
+    const T *kp = (const T *)a.k + s.k0 * a.k_token + w.kv * a.k_head;
+    const T *vp = (const T *)a.v + s.k0 * a.v_token + w.kv * a.v_head;
     typename Frag<T>::type fq[QT][C];
     int qi[QT];
+    f32x4 o[DT][QT];
+    float top[QT], sum[QT];   // top: in the score's units
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
-        qi[u] = q_first + (wave * QT + u) * 16 + (lane & 15);
+        qi[u] = w.first + (wave * QT + u) * 16 + (lane & 15);
         const T *row = qi[u] < s.nq ? qp + (long long)qi[u] * a.q_token : nullptr;
 #pragma unroll
         for (int c = 0; c < C; ++c) fq[u][c] = read_fragment<T, VEC>(row, 32 * c + 8 * g, a.dim);
-    }
-    const int w_first = q_first + wave * QT * 16;   // this wavefront's queries
-    f32x4 o[DT][QT];
-    float top[QT], sum[QT];
-#pragma unroll
-    for (int u = 0; u < QT; ++u) {
         top[u] = minus_infinity();
         sum[u] = 0.f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d][u] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    const int w_first = w.first + wave * QT * 16;   // this wavefront's queries
 
-    for (int j0 = 0; j0 < last; j0 += BK) {
-        __syncthreads();
-        TileReader<T, DP, BK, VEC, 256>::read(kp + (long long)j0 * a.k_token, a.k_token, s.nk - j0, a.dim, lds_k, tid);
-        TileReader<T, DP, BK, VEC, 256>::read(vp + (long long)j0 * a.v_token, a.v_token, s.nk - j0, a.dim, lds_v, tid);
-        __builtin_amdgcn_s_waitcnt(0x0f70);
-        __syncthreads();
+    auto fetch = [&](int t, auto which) {
+        char *lds = decltype(which)::value ? lds1 : lds0;
+        const int j0 = t * BK;
+        TileReader<T, DP, BK, VEC, 256>::read(kp + (long long)j0 * a.k_token, a.k_token, s.nk - j0, a.dim, lds, tid);
+        TileReader<T, DP, BK, VEC, 256>::read(vp + (long long)j0 * a.v_token, a.v_token, s.nk - j0, a.dim, lds + BK * L::PITCH, tid);
+    };
+    auto work = [&](int t, auto which) {
+        const char *lds_k = decltype(which)::value ? lds1 : lds0, *lds_v = lds_k + BK * L::PITCH;
+        const int j0 = t * BK;
         f32x4 z[4][QT];
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt)
@@ -195,38 +275,48 @@ __global__ __launch_bounds__(256) void attention_forward_kernel(AttentionArgs a)
 #pragma unroll
                 for (int u = 0; u < QT; ++u) mma(z[kt][u], fk, fq[u][c]);
             }
-        const bool whole = j0 + BK <= s.nk && (!a.causal || j0 + BK - 1 <= w_first + shift || j0 + BK <= prefix);
+        settle(z);
+        const bool whole = j0 + BK <= s.nk && (!a.causal || j0 + BK - 1 <= w_first + w.shift || j0 + BK <= w.prefix);
         typename Frag<T>::type fp[2][QT];
 #pragma unroll
         for (int u = 0; u < QT; ++u) {
+            const int at = qi[u] + w.shift;
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) score.template shape<-1>(z[kt][u], at - (j0 + kt * 16 + 4 * g), nullptr);
+            if (!whole) {
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int j = j0 + kt * 16 + 4 * g + e;
+                        if (j >= s.nk || (a.causal && j > at && j >= w.prefix)) z[kt][u][e] = minus_infinity();
+                    }
+            }
             float most = top[u];
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int j = j0 + kt * 16 + 4 * g + e, at = qi[u] + shift;
-                    float v = score(z[kt][u][e], at - j, nullptr);
-                    if (!whole && (j >= s.nk || (a.causal && j > at && j >= prefix))) v = minus_infinity();
-                    z[kt][u][e] = v;
-                    most = fmaxf(most, v);
-                }
+                for (int e = 0; e < 4; ++e) most = fmaxf(most, z[kt][u][e]);
             most = fmaxf(most, __shfl_xor(most, 16));
             most = fmaxf(most, __shfl_xor(most, 32));
-            const float ref = most == minus_infinity() ? 0.f : most;
-            const float keep = exp2_fast(top[u] - ref);
-            top[u] = most;
+            const float ref = most == minus_infinity() ? 0.f : most * score.unit;
+            if (__any(most != top[u])) {   // else nothing is scaled down
+                const float keep = exp2_fast(top[u] * score.unit - ref);
+                top[u] = most;
+                sum[u] *= keep;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[d][u] *= keep;
+            }
             float add = 0.f;
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float v = exp2_fast(z[kt][u][e] - ref);
+                    const float v = exp2_fast(z[kt][u][e] * score.unit - ref);
                     add += v;
                     fp[kt >> 1][u][(kt & 1) * 4 + e] = (T)v;
                 }
-            sum[u] = sum[u] * keep + add;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[d][u] *= keep;
+            sum[u] += add;
         }
 #pragma unroll
         for (int c = 0; c < 2; ++c)
@@ -236,7 +326,9 @@ __global__ __launch_bounds__(256) void attention_forward_kernel(AttentionArgs a)
 #pragma unroll
                 for (int u = 0; u < QT; ++u) mma(o[d][u], fv, fp[c][u]);
             }
-    }
+    };
+    two_buffers((w.last + BK - 1) / BK, fetch, [](int, auto) {}, work);
+    settle_loop();
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         float total = sum[u];
@@ -245,13 +337,13 @@ __global__ __launch_bounds__(256) void attention_forward_kernel(AttentionArgs a)
         if (qi[u] >= s.nq) continue;
         const long long n = s.q0 + qi[u];
         const float inv = total > 0.f || total != total ? 1.f / total : 0.f;   // no key: zero
-        T *out = (T *)a.o + (n * a.heads + head) * a.dim;
+        T *out = (T *)a.o + (n * a.heads + w.head) * a.dim;
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             const int d0 = d * 16 + 4 * g;
             if (d0 < a.dim) store_four(out + d0, o[d][u] * inv, a.dim - d0, VEC);
         }
-        if (g == 0) a.lse[head * a.total_q + n] = (top[u] + log2f(total)) * LN_2;
+        if (g == 0) a.lse[w.head * a.total_q + n] = (top[u] * score.unit + log2f(total)) * LN_2;
     }
 }
 
@@ -305,11 +397,9 @@ __global__ __launch_bounds__(WAVES * 64) void attention_chunk_kernel(AttentionAr
     constexpr int LOADS = BYTES / 1024;   // of a wavefront for one step
     auto fetch = [&](int j0, char *lds) {
         char *own = lds + wave * BYTES;
-        // always the same number of loads: past the end they read nothing
-        const int left = j0 < k_end ? k_end - j0 : 0;
-        const long long at = j0 < k_end ? j0 : 0;
-        TileReader<T, DP, BK, VEC, 64>::read(kp + at * a.k_token, a.k_token, left, a.dim, own, lane);
-        TileReader<T, DP, BK, VEC, 64>::read(vp + at * a.v_token, a.v_token, left, a.dim, own + BK * L::PITCH, lane);
+        TileReader<T, DP, BK, VEC, 64, true>::read(kp + (long long)j0 * a.k_token, a.k_token, k_end - j0, a.dim, own, lane);
+        TileReader<T, DP, BK, VEC, 64, true>::read(vp + (long long)j0 * a.v_token, a.v_token, k_end - j0, a.dim,
+                                                   own + BK * L::PITCH, lane);
     };
     auto work = [&](int j0, const char *lds) {
         const char *lds_k = lds + wave * BYTES, *lds_v = lds_k + BK * L::PITCH;
@@ -326,21 +416,24 @@ __global__ __launch_bounds__(WAVES * 64) void attention_chunk_kernel(AttentionAr
 #pragma unroll
                 for (int u = 0; u < QT; ++u) mma(z[kt][u], fk, fq[u][c]);
             }
+        settle(z);
         const bool whole = j0 + BK <= k_end && (!a.causal || j0 + BK - 1 <= shift || j0 + BK <= prefix);
         typename Frag<T>::type fp[QT];
 #pragma unroll
         for (int u = 0; u < QT; ++u) {
+            const int at = qi[u] + shift;
             float most = top[u];
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
+            for (int kt = 0; kt < 2; ++kt) {
+                score[u].template shape<-1>(z[kt][u], at - (j0 + kt * 16 + 4 * g), nullptr);
+                z[kt][u] *= score[u].unit;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int j = j0 + kt * 16 + 4 * g + e, at = qi[u] + shift;
-                    float v = score[u](z[kt][u][e], at - j, nullptr);
-                    if (!whole && (j >= k_end || (a.causal && j > at && j >= prefix))) v = minus_infinity();
-                    z[kt][u][e] = v;
-                    most = fmaxf(most, v);
+                    const int j = j0 + kt * 16 + 4 * g + e;
+                    if (!whole && (j >= k_end || (a.causal && j > at && j >= prefix))) z[kt][u][e] = minus_infinity();
+                    most = fmaxf(most, z[kt][u][e]);
                 }
+            }
             most = fmaxf(most, __shfl_xor(most, 16));
             most = fmaxf(most, __shfl_xor(most, 32));
             const float ref = most == minus_infinity() ? 0.f : most, keep = exp2_fast(top[u] - ref);
@@ -365,25 +458,32 @@ __global__ __launch_bounds__(WAVES * 64) void attention_chunk_kernel(AttentionAr
             for (int u = 0; u < QT; ++u) mma(o[d][u], fv, fp[u]);
         }
     };
-    auto arrived = [&]() {   // all but the loads of the step after are in LDS
-        if (VEC) __builtin_amdgcn_s_waitcnt((LOADS & 15) | (LOADS >> 4) << 14 | 0x0f70);
+    // A step's loads are in LDS when no more than those of the step after, if there is one, are under way.
+    auto arrived = [&](bool more) {
+        if (VEC && more)
+            __builtin_amdgcn_s_waitcnt((LOADS & 15) | (LOADS >> 4) << 14 | 0x0f70);
+        else
+            __builtin_amdgcn_s_waitcnt(0x0f70);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     };
     constexpr int STEP = WAVES * BK;
     int j0 = k_first + wave * BK;
-    fetch(j0, lds0);
+    if (j0 < k_end) fetch(j0, lds0);
     for (; j0 < k_end; j0 += 2 * STEP) {
-        fetch(j0 + STEP, lds1);
-        arrived();
+        const bool second = j0 + STEP < k_end, third = j0 + 2 * STEP < k_end;
+        if (second) fetch(j0 + STEP, lds1);
+        arrived(second);
         work(j0, lds0);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // the buffer has been read
         __builtin_amdgcn_wave_barrier();
-        fetch(j0 + 2 * STEP, lds0);
-        arrived();
-        if (j0 + STEP < k_end) work(j0 + STEP, lds1);
+        if (!second) break;
+        if (third) fetch(j0 + 2 * STEP, lds0);
+        arrived(third);
+        work(j0 + STEP, lds1);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_s_waitcnt(0x0f70);   // no load is under way to LDS that is used again
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         sum[u] += __shfl_xor(sum[u], 16);
@@ -460,7 +560,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a)
 }
 
 // ---- backward -------------------------------------------------------------------
-// delta = do . o per query and head: 16 lanes each
+// delta = do . o per query and head, where dq is not asked for: 16 lanes each
 template <class T>
 __global__ __launch_bounds__(256) void attention_delta_kernel(const T *__restrict__ o, const T *__restrict__ d_o, long long total_q,
                                                               int heads, int dim, float *__restrict__ delta)
@@ -475,96 +575,140 @@ __global__ __launch_bounds__(256) void attention_delta_kernel(const T *__restric
 }
 
 // dq: like the forward pass; dS = P (dP - delta) cut, dq = scale sum_j dS_ij k_j.
+// delta_i = do_i . o_i = sum_j P_ij dP_ij.  Where a tile sees up to EXACT_KEYS keys it is formed as the second sum, in a pass of
+// its own: o is large there, and its rounding to bf16 would count in dS as much as that of dS itself (with more keys o is
+// an average of many v, and small).  The delta that is used goes to a.delta for dk and dv.
+constexpr int EXACT_KEYS = 256;
 template <class T, int DP, int QT, bool VEC, bool SHAPED>
-__global__ __launch_bounds__(256) void attention_dq_kernel(AttentionArgs a)
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kernel(AttentionArgs a)
 {
     constexpr int BQ = 64 * QT, BK = 64, C = DP / 32, DT = DP / 16;
     typedef Tile<T, DP> L;
-    __shared__ __align__(1024) char lds_k[BK * L::PITCH];
-    __shared__ __align__(1024) char lds_v[BK * L::PITCH];
+    __shared__ __align__(1024) char lds0[2 * BK * L::PITCH];
+    __shared__ __align__(1024) char lds1[2 * BK * L::PITCH];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
-    const int group = a.heads / a.kv_heads;
-    const long long t = die_run(blockIdx.x, gridDim.x);
-    const int head = (int)(t / ((long long)a.tiles * group)) * group + (int)(t % group), kv = head / group;
-    const long long tile = a.tiles - 1 - (t / group) % a.tiles;
-    const int p = set_of_tile(a.q_off, a.sets, BQ, tile);
-    const SetRange s = range_of(a, p);
-    const long long b0 = (tile - (s.q0 / BQ + p)) * BQ;
-    if (b0 < 0 || b0 >= s.nq) return;
-    const int q_first = (int)b0, shift = s.nk - s.nq;
-    const int prefix = a.causal && a.prefix ? a.prefix[p] : 0;
-    int last = s.nk;
-    if (a.causal) {
-        const int reach = (q_first + BQ < s.nq ? q_first + BQ : s.nq) + shift;
-        last = reach > prefix ? reach : prefix;
-        last = last < s.nk ? last : s.nk;
-    }
+    const QueryTile w = query_tile<BQ>(a);
+    if (!w.any) return;
+    const SetRange s = w.s;
     Scores<T, SHAPED> score;
-    score.init(a, head);
-    const T *kp = (const T *)a.k + s.k0 * a.k_token + kv * a.k_head;
-    const T *vp = (const T *)a.v + s.k0 * a.v_token + kv * a.v_head;
+    score.init(a, w.head);
+    const T *kp = (const T *)a.k + s.k0 * a.k_token + w.kv * a.k_head;
+    const T *vp = (const T *)a.v + s.k0 * a.v_token + w.kv * a.v_head;
     typename Frag<T>::type fq[QT][C], fo[QT][C];
     int qi[QT];
     float lse[QT], delta[QT];
     f32x4 dq[DT][QT];
+    const bool exact = w.last <= EXACT_KEYS;
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
-        qi[u] = q_first + (wave * QT + u) * 16 + (lane & 15);
+        qi[u] = w.first + (wave * QT + u) * 16 + (lane & 15);
         const bool in = qi[u] < s.nq;
         const long long n = s.q0 + (in ? qi[u] : 0);
-        const T *row = in ? (const T *)a.q + n * a.q_token + head * a.q_head : nullptr;
-        const T *orow = in ? (const T *)a.d_o + (n * a.heads + head) * a.dim : nullptr;
+        const T *row = in ? (const T *)a.q + n * a.q_token + w.head * a.q_head : nullptr;
+        const T *dorow = in ? (const T *)a.d_o + (n * a.heads + w.head) * a.dim : nullptr;
+        const T *orow = in ? (const T *)a.o + (n * a.heads + w.head) * a.dim : nullptr;
+        delta[u] = 0.f;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             fq[u][c] = read_fragment<T, VEC>(row, 32 * c + 8 * g, a.dim);
-            fo[u][c] = read_fragment<T, VEC>(orow, 32 * c + 8 * g, a.dim);
+            fo[u][c] = read_fragment<T, VEC>(dorow, 32 * c + 8 * g, a.dim);
+            if (!exact) {
+                const typename Frag<T>::type f = read_fragment<T, VEC>(orow, 32 * c + 8 * g, a.dim);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) delta[u] += (float)f[e] * (float)fo[u][c][e];
+            }
         }
-        lse[u] = in ? a.lse_in[head * a.total_q + n] * LOG2_E : 0.f;
-        delta[u] = in ? a.delta[head * a.total_q + n] : 0.f;
+        lse[u] = in ? a.lse_in[w.head * a.total_q + n] * LOG2_E : 0.f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) dq[d][u] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int w_first = q_first + wave * QT * 16;
-    for (int j0 = 0; j0 < last; j0 += BK) {
-        __syncthreads();
-        TileReader<T, DP, BK, VEC, 256>::read(kp + (long long)j0 * a.k_token, a.k_token, s.nk - j0, a.dim, lds_k, tid);
-        TileReader<T, DP, BK, VEC, 256>::read(vp + (long long)j0 * a.v_token, a.v_token, s.nk - j0, a.dim, lds_v, tid);
-        __builtin_amdgcn_s_waitcnt(0x0f70);
-        __syncthreads();
-        const bool whole = j0 + BK <= s.nk && (!a.causal || j0 + BK - 1 <= w_first + shift || j0 + BK <= prefix);
+    const int w_first = w.first + wave * QT * 16;
+    auto fetch = [&](int t, auto which) {
+        char *lds = decltype(which)::value ? lds1 : lds0;
+        const int j0 = t * BK;
+        TileReader<T, DP, BK, VEC, 256>::read(kp + (long long)j0 * a.k_token, a.k_token, s.nk - j0, a.dim, lds, tid);
+        TileReader<T, DP, BK, VEC, 256>::read(vp + (long long)j0 * a.v_token, a.v_token, s.nk - j0, a.dim, lds + BK * L::PITCH, tid);
+    };
+    // P and dP of 32 keys from j0 on, the first of them in row r of the tiles; P is zero where the key is not seen
+    auto scores = [&](const char *lds_k, const char *lds_v, int j0, int r, f32x4 (&z)[2][QT], f32x4 (&dp)[2][QT],
+                      f32x4 (&cut)[2][QT]) {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int u = 0; u < QT; ++u) z[kt][u] = dp[kt][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+                const typename Frag<T>::type fk = L::rows(lds_k, r + kt * 16, c, lane);
+                const typename Frag<T>::type fv = L::rows(lds_v, r + kt * 16, c, lane);
+#pragma unroll
+                for (int u = 0; u < QT; ++u) {
+                    mma(z[kt][u], fk, fq[u][c]);
+                    mma(dp[kt][u], fv, fo[u][c]);
+                }
+            }
+        settle(z);
+        settle(dp);
+        const bool whole = j0 + 32 <= s.nk && (!a.causal || j0 + 31 <= w_first + w.shift || j0 + 32 <= w.prefix);
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+                const int at = qi[u] + w.shift, j = j0 + kt * 16 + 4 * g;
+                score.template shape<-1>(z[kt][u], at - j, &cut[kt][u]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[kt][u][e] = exp2_fast(z[kt][u][e] * score.unit - lse[u]);
+                if (!whole) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (j + e >= s.nk || (a.causal && j + e > at && j + e >= w.prefix)) {
+                            z[kt][u][e] = 0.f;
+                            dp[kt][u][e] = 0.f;
+                        }
+                }
+            }
+    };
+    const int steps = (w.last + BK - 1) / BK;
+    if (exact) {
+        two_buffers(steps, fetch, [](int, auto) {}, [&](int t, auto which) {
+            const char *lds_k = decltype(which)::value ? lds1 : lds0, *lds_v = lds_k + BK * L::PITCH;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                f32x4 z[2][QT], dp[2][QT], cut[2][QT];
+                scores(lds_k, lds_v, t * BK + h * 32, h * 32, z, dp, cut);
+#pragma unroll
+                for (int u = 0; u < QT; ++u)
+#pragma unroll
+                    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) delta[u] += z[kt][u][e] * dp[kt][u][e];
+            }
+        });
+        __syncthreads();   // the first buffer is filled again
+    }
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        delta[u] += __shfl_xor(delta[u], 16);
+        delta[u] += __shfl_xor(delta[u], 32);
+        if (g == 0 && qi[u] < s.nq) a.delta[w.head * a.total_q + s.q0 + qi[u]] = delta[u];
+    }
+    two_buffers(steps, fetch, [](int, auto) {}, [&](int t, auto which) {
+        const char *lds_k = decltype(which)::value ? lds1 : lds0, *lds_v = lds_k + BK * L::PITCH;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {   // 32 keys at a time
-            f32x4 z[2][QT], dp[2][QT];
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int u = 0; u < QT; ++u) z[kt][u] = dp[kt][u] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt) {
-                    const typename Frag<T>::type fk = L::rows(lds_k, h * 32 + kt * 16, c, lane);
-                    const typename Frag<T>::type fv = L::rows(lds_v, h * 32 + kt * 16, c, lane);
-#pragma unroll
-                    for (int u = 0; u < QT; ++u) {
-                        mma(z[kt][u], fk, fq[u][c]);
-                        mma(dp[kt][u], fv, fo[u][c]);
-                    }
-                }
+            f32x4 z[2][QT], dp[2][QT], cut[2][QT];
+            scores(lds_k, lds_v, t * BK + h * 32, h * 32, z, dp, cut);
             typename Frag<T>::type fs[QT];
 #pragma unroll
             for (int u = 0; u < QT; ++u)
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
+                for (int kt = 0; kt < 2; ++kt) {
+                    f32x4 ds = z[kt][u] * (dp[kt][u] - delta[u]);
+                    if (SHAPED) ds *= cut[kt][u];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int j = j0 + h * 32 + kt * 16 + 4 * g + e, at = qi[u] + shift;
-                        float cut = 1.f;
-                        const float v = score(z[kt][u][e], at - j, &cut);
-                        float ds = exp2_fast(v - lse[u]) * (dp[kt][u][e] - delta[u]) * cut;
-                        if (!whole && (j >= s.nk || (a.causal && j > at && j >= prefix))) ds = 0.f;
-                        fs[u][kt * 4 + e] = (T)ds;
-                    }
+                    for (int e = 0; e < 4; ++e) fs[u][kt * 4 + e] = (T)ds[e];
+                }
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
                 const typename Frag<T>::type fk = L::columns(lds_k, h * 32, d * 16, lane);
@@ -572,11 +716,12 @@ __global__ __launch_bounds__(256) void attention_dq_kernel(AttentionArgs a)
                 for (int u = 0; u < QT; ++u) mma(dq[d][u], fk, fs[u]);
             }
         }
-    }
+    });
+    settle_loop();
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         if (qi[u] >= s.nq) continue;
-        T *out = (T *)a.dq + ((s.q0 + qi[u]) * a.heads + head) * a.dim;
+        T *out = (T *)a.dq + ((s.q0 + qi[u]) * a.heads + w.head) * a.dim;
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             const int d0 = d * 16 + 4 * g;
@@ -585,21 +730,21 @@ __global__ __launch_bounds__(256) void attention_dq_kernel(AttentionArgs a)
     }
 }
 
-// dk, dv: four wavefronts of 16 KT keys each go over the queries of all heads that share the key head, 32 at a
+// dk, dv: four wavefronts of 16 KT keys each go over the queries of all heads that share the key head, BQ at a
 // time; dv = P^T do, dk = scale dS^T q.
 template <class T, int DP, int KT, bool VEC, bool SHAPED>
 __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
 {
-    constexpr int BK = 64 * KT, BQ = 32, C = DP / 32, DT = DP / 16;
+    constexpr int BK = 64 * KT, BQ = DP * sizeof(T) > 256 ? 32 : 64, C = DP / 32, DT = DP / 16;
     typedef Tile<T, DP> L;
-    __shared__ __align__(1024) char lds_q[BQ * L::PITCH];
-    __shared__ __align__(1024) char lds_o[BQ * L::PITCH];
-    __shared__ __align__(16) float lds_lse[BQ], lds_delta[BQ];
+    __shared__ __align__(1024) char lds0[2 * BQ * L::PITCH];
+    __shared__ __align__(1024) char lds1[2 * BQ * L::PITCH];
+    __shared__ __align__(16) float lds_lse[2][BQ], lds_delta[2][BQ];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
     const int group = a.heads / a.kv_heads;
-    const long long t = die_run(blockIdx.x, gridDim.x);
-    const int kv = (int)(t / a.tiles);
-    const long long tile = t % a.tiles;
+    const long long t0 = die_run(blockIdx.x, gridDim.x);
+    const int kv = (int)(t0 / a.tiles);
+    const long long tile = t0 % a.tiles;
     const int p = set_of_tile(a.k_off, a.sets, BK, tile);
     const SetRange s = range_of(a, p);
     const long long b0 = (tile - (s.k0 / BK + p)) * BK;
@@ -631,25 +776,37 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
         for (int d = 0; d < DT; ++d) dk[d][u] = dv[d][u] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     const int w_last = k_first + (wave + 1) * KT * 16 - 1;   // this wavefront's last key
-    for (int gh = 0; gh < group; ++gh) {
-        const int head = kv * group + gh;
+    // a step: BQ queries of one head of the group
+    const int each = s.nq > begin ? (s.nq - begin + BQ - 1) / BQ : 0;
+    float next_lse = 0.f, next_delta = 0.f;
+    auto fetch = [&](int t, auto which) {
+        char *lds = decltype(which)::value ? lds1 : lds0;
+        const int head = kv * group + t / each, i0 = begin + t % each * BQ;
+        const T *qp = (const T *)a.q + (s.q0 + i0) * a.q_token + head * a.q_head;
+        const T *op = (const T *)a.d_o + ((s.q0 + i0) * a.heads + head) * a.dim;
+        if (tid < BQ) {
+            const bool in = i0 + tid < s.nq;
+            const long long n = head * a.total_q + s.q0 + (in ? i0 + tid : 0);
+            next_lse = a.lse_in[n];
+            next_delta = a.delta[n];
+        }
+        TileReader<T, DP, BQ, VEC, 256>::read(qp, a.q_token, s.nq - i0, a.dim, lds, tid);
+        TileReader<T, DP, BQ, VEC, 256>::read(op, (long long)a.heads * a.dim, s.nq - i0, a.dim, lds + BQ * L::PITCH, tid);
+    };
+    auto landed = [&](int, auto which) {
+        if (tid < BQ) {
+            lds_lse[decltype(which)::value][tid] = next_lse * LOG2_E;
+            lds_delta[decltype(which)::value][tid] = next_delta;
+        }
+    };
+    auto work = [&](int t, auto which) {
+        const char *lds_q = decltype(which)::value ? lds1 : lds0, *lds_o = lds_q + BQ * L::PITCH;
+        const int head = kv * group + t / each;
         Scores<T, SHAPED> score;
         score.init(a, head);
-        const T *qp = (const T *)a.q + s.q0 * a.q_token + head * a.q_head;
-        const T *op = (const T *)a.d_o + (s.q0 * a.heads + head) * a.dim;
-        const float *lp = a.lse_in + head * a.total_q + s.q0, *ep = a.delta + head * a.total_q + s.q0;
-        for (int i0 = begin; i0 < s.nq; i0 += BQ) {
-            __syncthreads();
-            TileReader<T, DP, BQ, VEC, 256>::read(qp + (long long)i0 * a.q_token, a.q_token, s.nq - i0, a.dim, lds_q, tid);
-            TileReader<T, DP, BQ, VEC, 256>::read(op + (long long)i0 * a.heads * a.dim, (long long)a.heads * a.dim, s.nq - i0,
-                                                  a.dim, lds_o, tid);
-            if (tid < BQ) {
-                const bool in = i0 + tid < s.nq;
-                lds_lse[tid] = in ? lp[i0 + tid] * LOG2_E : 0.f;
-                lds_delta[tid] = in ? ep[i0 + tid] : 0.f;
-            }
-            __builtin_amdgcn_s_waitcnt(0x0f70);
-            __syncthreads();
+#pragma unroll
+        for (int h = 0; h < BQ / 32; ++h) {   // 32 queries at a time
+            const int i0 = begin + t % each * BQ + h * 32;
             f32x4 z[2][KT], dp[2][KT];
 #pragma unroll
             for (int qt = 0; qt < 2; ++qt)
@@ -659,38 +816,48 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int qt = 0; qt < 2; ++qt) {
-                    const typename Frag<T>::type fq = L::rows(lds_q, qt * 16, c, lane);
-                    const typename Frag<T>::type fo = L::rows(lds_o, qt * 16, c, lane);
+                    const typename Frag<T>::type fq = L::rows(lds_q, h * 32 + qt * 16, c, lane);
+                    const typename Frag<T>::type fo = L::rows(lds_o, h * 32 + qt * 16, c, lane);
 #pragma unroll
                     for (int u = 0; u < KT; ++u) {
                         mma(z[qt][u], fq, fk[u][c]);
                         mma(dp[qt][u], fo, fv[u][c]);
                     }
                 }
-            const bool whole = i0 + BQ <= s.nq && w_last < s.nk && (!a.causal || w_last <= i0 + shift || w_last < prefix);
+            settle(z);
+            settle(dp);
+            const bool whole = i0 + 32 <= s.nq && w_last < s.nk && (!a.causal || w_last <= i0 + shift || w_last < prefix);
             typename Frag<T>::type fp[KT], fs[KT];
 #pragma unroll
             for (int qt = 0; qt < 2; ++qt) {
-                const f32x4 lse = *(const f32x4 *)(lds_lse + qt * 16 + 4 * g);
-                const f32x4 delta = *(const f32x4 *)(lds_delta + qt * 16 + 4 * g);
+                const f32x4 lse = *(const f32x4 *)(lds_lse[decltype(which)::value] + h * 32 + qt * 16 + 4 * g);
+                const f32x4 delta = *(const f32x4 *)(lds_delta[decltype(which)::value] + h * 32 + qt * 16 + 4 * g);
 #pragma unroll
-                for (int u = 0; u < KT; ++u)
+                for (int u = 0; u < KT; ++u) {
+                    const int i = i0 + qt * 16 + 4 * g, j = kj[u];
+                    f32x4 cut;
+                    score.template shape<1>(z[qt][u], i + shift - j, &cut);
+                    f32x4 pr, ds;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) pr[e] = exp2_fast(z[qt][u][e] * score.unit - lse[e]);
+                    ds = pr * (dp[qt][u] - delta);
+                    if (SHAPED) ds *= cut;
+                    if (!whole) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (i + e >= s.nq || j >= s.nk || (a.causal && j > i + e + shift && j >= prefix)) pr[e] = ds[e] = 0.f;
+                    }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int i = i0 + qt * 16 + 4 * g + e, at = i + shift, j = kj[u];
-                        float cut = 1.f;
-                        const float v = score(z[qt][u][e], at - j, &cut);
-                        float pr = exp2_fast(v - lse[e]);
-                        float ds = pr * (dp[qt][u][e] - delta[e]) * cut;
-                        if (!whole && (i >= s.nq || j >= s.nk || (a.causal && j > at && j >= prefix))) pr = ds = 0.f;
-                        fp[u][qt * 4 + e] = (T)pr;
-                        fs[u][qt * 4 + e] = (T)ds;
+                        fp[u][qt * 4 + e] = (T)pr[e];
+                        fs[u][qt * 4 + e] = (T)ds[e];
                     }
+                }
             }
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
-                const typename Frag<T>::type fo = L::columns(lds_o, 0, d * 16, lane);
-                const typename Frag<T>::type fq = L::columns(lds_q, 0, d * 16, lane);
+                const typename Frag<T>::type fo = L::columns(lds_o, h * 32, d * 16, lane);
+                const typename Frag<T>::type fq = L::columns(lds_q, h * 32, d * 16, lane);
 #pragma unroll
                 for (int u = 0; u < KT; ++u) {
                     mma(dv[d][u], fo, fp[u]);
@@ -698,7 +865,9 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
                 }
             }
         }
-    }
+    };
+    two_buffers(group * each, fetch, landed, work);
+    settle_loop();
 #pragma unroll
     for (int u = 0; u < KT; ++u) {
         if (kj[u] >= s.nk) continue;
@@ -719,6 +888,6 @@ hipError_t attention_forward(AttentionArgs a, bool vec, bool shaped, hipStream_t
 template <class T>
 hipError_t attention_by_chunks(AttentionArgs a, bool vec, bool shaped, hipStream_t s);
 template <class T>
-hipError_t attention_backward(AttentionArgs a, bool vec, bool shaped, float *delta, const T *o, hipStream_t s);
+hipError_t attention_backward(AttentionArgs a, bool vec, bool shaped, hipStream_t s);
 
 }  // namespace lcn

@@ -56,6 +56,9 @@ static bool pieces(const AttentionArgs &a, size_t e, const void *const *more, in
     return (all & 15) == 0 && (strides & (long long)(16 / e - 1)) == 0;
 }
 
+// Whether scores are more than a positive multiple of q . k.
+static bool shaped_scores(const AttentionArgs &a) { return a.cap > 0.f || a.slopes || !(a.scale > 0.f); }
+
 // Where a set has few queries, its keys are split over workgroups: up to 32 rows (queries times the heads that share a key
 // head) fit a wavefront.  Chunks of keys are so long that there are some eight workgroups per compute unit, from 128 keys (a
 // step of a workgroup's wavefronts) to 2048.  0: not split, as also where a set has less than 128 keys on average or
@@ -112,7 +115,7 @@ lcn_status lcn_attention(const lcn_attention_desc *desc, const void *q, const vo
     a.o = o;
     a.lse = lse;
     const void *more[1] = {o};
-    const bool vec = pieces(a, desc->dtype == LCN_F32 ? 4 : 2, more, 1), shaped = a.cap > 0.f || a.slopes;
+    const bool vec = pieces(a, desc->dtype == LCN_F32 ? 4 : 2, more, 1), shaped = shaped_scores(a);
     const ChunkSpace f = chunk_space((char *)workspace, desc);
     if (f.chunk) {
         if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < f.bytes) return LCN_ERR_ALLOC;
@@ -146,16 +149,18 @@ lcn_status lcn_attention_backward(const lcn_attention_desc *desc, const void *q,
     if (need && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return LCN_ERR_ALLOC;
     AttentionArgs a = args_of(desc, q, k, v);
     a.d_o = d_o;
+    a.o = const_cast<void *>(o);
     a.lse_in = lse;
+    a.delta = (float *)workspace;
     a.dq = dq;
     a.dk = dk;
     a.dv = dv;
-    const void *more[4] = {d_o, dq, dk, dv};
-    const bool vec = pieces(a, desc->dtype == LCN_F32 ? 4 : 2, more, 4), shaped = a.cap > 0.f || a.slopes;
+    const void *more[5] = {o, d_o, dq, dk, dv};
+    const bool vec = pieces(a, desc->dtype == LCN_F32 ? 4 : 2, more, 5), shaped = shaped_scores(a);
     if (desc->dtype == LCN_F32)
-        OPCHK(attention_backward<float>(a, vec, shaped, (float *)workspace, (const float *)o, s));
+        OPCHK(attention_backward<float>(a, vec, shaped, s));
     else
-        OPCHK(attention_backward<__bf16>(a, vec, shaped, (float *)workspace, (const __bf16 *)o, s));
+        OPCHK(attention_backward<__bf16>(a, vec, shaped, s));
     return LCN_OK;
 }
 

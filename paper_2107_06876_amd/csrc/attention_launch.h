@@ -19,10 +19,10 @@ static hipError_t forward_one(AttentionArgs a, hipStream_t s)
     hipLaunchKernelGGL((attention_forward_kernel<T, DP, QT, VEC, SHAPED>), dim3((unsigned)(tiles * a.heads)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
-template <class T, int DP, int QT, bool VEC, bool SHAPED>
-static hipError_t backward_one(AttentionArgs a, bool dq, hipStream_t s)
+template <class T, int DP, int QT, bool DQ, bool VEC, bool SHAPED>
+static hipError_t backward_one(AttentionArgs a, hipStream_t s)
 {
-    if (dq) {
+    if constexpr (DQ) {
         const long long tiles = tiles_of(a.total_q, a.sets, 64 * QT);
         a.tiles = (int)tiles;
         hipLaunchKernelGGL((attention_dq_kernel<T, DP, QT, VEC, SHAPED>), dim3((unsigned)(tiles * a.heads)), dim3(256), 0, s, a);
@@ -34,30 +34,35 @@ static hipError_t backward_one(AttentionArgs a, bool dq, hipStream_t s)
     return hipGetLastError();
 }
 
-// what: 0 forward, 1 dq, 2 dk and dv
-template <class T, int DP, int QT>
-static hipError_t by_form(const AttentionArgs &a, int what, bool vec, bool shaped, hipStream_t s)
+enum { FORWARD = 0, GRAD_Q = 1, GRAD_KV = 2 };
+
+template <class T, int DP, int QT, int WHAT, bool VEC, bool SHAPED>
+static hipError_t one(const AttentionArgs &a, hipStream_t s)
 {
-    if (what == 0) {
-        if (vec) return shaped ? forward_one<T, DP, QT, true, true>(a, s) : forward_one<T, DP, QT, true, false>(a, s);
-        return forward_one<T, DP, QT, false, true>(a, s);
-    }
-    if (vec) return shaped ? backward_one<T, DP, QT, true, true>(a, what == 1, s) : backward_one<T, DP, QT, true, false>(a, what == 1, s);
-    return backward_one<T, DP, QT, false, true>(a, what == 1, s);
+    if constexpr (WHAT == FORWARD)
+        return forward_one<T, DP, QT, VEC, SHAPED>(a, s);
+    else
+        return backward_one<T, DP, QT, WHAT == GRAD_Q, VEC, SHAPED>(a, s);
 }
-template <class T>
-static hipError_t by_size(const AttentionArgs &a, int what, bool vec, bool shaped, hipStream_t s)
+template <class T, int DP, int QT, int WHAT>
+static hipError_t by_form(const AttentionArgs &a, bool vec, bool shaped, hipStream_t s)
 {
-    const bool few = what == 2 ? short_sets(a.total_k, a.sets) : short_sets(a.total_q, a.sets);
-    if (a.dim <= 32) return few ? by_form<T, 32, 1>(a, what, vec, shaped, s) : by_form<T, 32, 2>(a, what, vec, shaped, s);
-    if (a.dim <= 64) return few ? by_form<T, 64, 1>(a, what, vec, shaped, s) : by_form<T, 64, 2>(a, what, vec, shaped, s);
-    return few ? by_form<T, 128, 1>(a, what, vec, shaped, s) : by_form<T, 128, 2>(a, what, vec, shaped, s);
+    if (vec) return shaped ? one<T, DP, QT, WHAT, true, true>(a, s) : one<T, DP, QT, WHAT, true, false>(a, s);
+    return one<T, DP, QT, WHAT, false, true>(a, s);
+}
+template <class T, int WHAT>
+static hipError_t by_size(const AttentionArgs &a, bool vec, bool shaped, hipStream_t s)
+{
+    const bool few = WHAT == GRAD_KV ? short_sets(a.total_k, a.sets) : short_sets(a.total_q, a.sets);
+    if (a.dim <= 32) return few ? by_form<T, 32, 1, WHAT>(a, vec, shaped, s) : by_form<T, 32, 2, WHAT>(a, vec, shaped, s);
+    if (a.dim <= 64) return few ? by_form<T, 64, 1, WHAT>(a, vec, shaped, s) : by_form<T, 64, 2, WHAT>(a, vec, shaped, s);
+    return few ? by_form<T, 128, 1, WHAT>(a, vec, shaped, s) : by_form<T, 128, 2, WHAT>(a, vec, shaped, s);
 }
 
 template <class T>
 hipError_t attention_forward(AttentionArgs a, bool vec, bool shaped, hipStream_t s)
 {
-    return by_size<T>(a, 0, vec, shaped, s);
+    return by_size<T, FORWARD>(a, vec, shaped, s);
 }
 template <class T, int DP, int QT>
 static hipError_t chunks_one(const AttentionArgs &a, bool vec, bool shaped, hipStream_t s)
@@ -89,20 +94,19 @@ hipError_t attention_by_chunks(AttentionArgs a, bool vec, bool shaped, hipStream
     return hipGetLastError();
 }
 template <class T>
-hipError_t attention_backward(AttentionArgs a, bool vec, bool shaped, float *delta, const T *o, hipStream_t s)
+hipError_t attention_backward(AttentionArgs a, bool vec, bool shaped, hipStream_t s)
 {
-    if (a.total_q > 0) {
+    hipError_t e = hipSuccess;
+    if (a.total_q > 0 && a.dq) {
+        e = by_size<T, GRAD_Q>(a, vec, shaped, s);
+    } else if (a.total_q > 0) {
         const long long rows = a.total_q * a.heads;
-        hipLaunchKernelGGL(attention_delta_kernel<T>, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, s, o, (const T *)a.d_o,
-                           a.total_q, a.heads, a.dim, delta);
-        hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        a.delta = delta;
-        if (a.dq && (e = by_size<T>(a, 1, vec, shaped, s)) != hipSuccess) return e;
+        hipLaunchKernelGGL(attention_delta_kernel<T>, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, s, (const T *)a.o,
+                           (const T *)a.d_o, a.total_q, a.heads, a.dim, a.delta);
+        e = hipGetLastError();
     }
-    a.delta = delta;
-    if (a.dk && a.total_k > 0) return by_size<T>(a, 2, vec, shaped, s);
-    return hipSuccess;
+    if (e == hipSuccess && a.dk && a.total_k > 0) e = by_size<T, GRAD_KV>(a, vec, shaped, s);
+    return e;
 }
 
 }  // namespace lcn

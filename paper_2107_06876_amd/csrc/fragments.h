@@ -83,14 +83,16 @@ struct Tile {
 
 // Brings rows of a tensor into a tile.  VEC: 16-byte pieces of rows are aligned and whole; they go straight into LDS.
 // Otherwise values are read one by one.  What is outside (rows from `left` on, values from dim on) becomes zero.
-template <class T, int DP, int ROWS, bool VEC, int THREADS>
+// REPEAT: rows from `left` on repeat the last one instead (left > 0), so that every load reads something: who waits for
+// loads by counting them need not know in which order loads end that are outside as a whole.
+template <class T, int DP, int ROWS, bool VEC, int THREADS, bool REPEAT = false>
 struct TileReader {
     typedef Tile<T, DP> L;
     static constexpr int ALL = ROWS * L::PIECES, LOADS = (ALL + THREADS - 1) / THREADS;
     static_assert(ALL % 64 == 0, "whole wavefronts of pieces");
     static __device__ __forceinline__ void read(const T *first, long long token, int left, int dim, char *lds, int tid)
     {
-        const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int lane = tid & 63, wave = THREADS > 64 ? __builtin_amdgcn_readfirstlane(tid >> 6) : 0;
         if constexpr (VEC) {
             const int rows = left < ROWS ? left : ROWS;
             const unsigned pitch = (unsigned)token * (unsigned)sizeof(T);
@@ -100,9 +102,9 @@ struct TileReader {
             for (int u = 0; u < LOADS; ++u) {
                 const int at = (u * (THREADS / 64) + wave) * 64, c = at + lane;
                 if (at >= ALL) break;
-                const int r = c / L::PIECES, piece = (c % L::PIECES) ^ L::swizzle(r);
-                unsigned off = (unsigned)r * pitch + (unsigned)piece * 16;
-                if (r >= rows || piece * L::EACH >= dim) off = 0x80000000u;
+                const int r = c / L::PIECES, piece = (c % L::PIECES) ^ L::swizzle(r), from = REPEAT && r >= rows ? rows - 1 : r;
+                unsigned off = (unsigned)from * pitch + (unsigned)piece * 16;
+                off = from < rows && piece * L::EACH < dim ? off : 0x80000000u;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (lds_void *)(lds + at * 16), 16, (int)off, 0, 0, 0);
             }
         } else {

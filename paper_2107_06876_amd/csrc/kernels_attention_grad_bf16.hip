@@ -1,0 +1,6 @@
+// Attention on bf16 tensors, backward.
+#include "attention_launch.h"
+
+namespace lcn {
+template hipError_t attention_backward<__bf16>(AttentionArgs, bool, bool, hipStream_t);
+}  // namespace lcn

@@ -143,7 +143,7 @@ inline size_t planes_bytes(long long rows, long long d, int planes)
 // Planes of the gradients dz and G on the way into their products.  One rounding of them to bf16 is as large as that of
 // the result; where few rows are added it can be larger than it in some of the result, so up to FEW_GRADIENT_ROWS rows
 // they have a second plane (the products are then bound by the other operand's bytes).
-constexpr int64_t FEW_GRADIENT_ROWS = 256;
+constexpr int64_t FEW_GRADIENT_ROWS = 512;
 inline int gradient_planes(int64_t rows, int32_t dtype) { return dtype == LCN_F32 ? 3 : rows <= FEW_GRADIENT_ROWS ? 2 : 1; }
 // Whether a bf16 matrix can be an operand as it lies: rows of whole 16-byte pieces, aligned.
 inline bool in_place(const void *p, long long d, int32_t dtype)
