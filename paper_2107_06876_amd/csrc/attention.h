@@ -41,6 +41,8 @@ struct AttentionArgs {
     const float *lse_in;
     float *delta;               // [head][query]
     void *dq, *dk, *dv;
+    int splits;                 // workgroups that share the heads of a key head
+    float *part_kv;             // [split][dk, dv][key][key head][dim], where splits > 1
 };
 
 // The last set p of `sets` with below(p), which holds for the first ones; 0 where it holds for none.  All lanes search.
@@ -83,33 +85,37 @@ __device__ __forceinline__ SetRange range_of(const AttentionArgs &a, int p)
 
 constexpr float LOG2_E = 1.4426950408889634f, LN_2 = 0.6931471805599453f;
 
-// tanh for bf16 tensors: 1 - 2 / (e^2x + 1), off by about 2^-23 of 1, far below the rounding of P
-__device__ __forceinline__ float cap_tanh(float x, __bf16) { return 1.f - 2.f * __builtin_amdgcn_rcpf(exp2_fast(2.f * LOG2_E * x) + 1.f); }
-__device__ __forceinline__ float cap_tanh(float x, float) { return tanhf(x); }
+// How q . k becomes a score.  PLAIN: a positive multiple.  CAPPED (bf16 tensors, scale > 0, cap up to MOST_CAP, no slopes):
+// cap tanh(scale q.k / cap) = cap - 2 cap r with r = 1 / (e^(2 scale q.k / cap) + 1), off by about 2^-23 of the cap, far
+// below the rounding of P; no score is above the cap, so that is the reference of the exponentials: P' = 2^(-2 cap r
+// log2(e)) >= 2^-116 needs no running maximum, and the cap's derivative is 4 r (1 - r).  SHAPED: anything, by tanhf.
+enum Shape { PLAIN = 0, CAPPED = 1, SHAPED = 2 };
+constexpr float MOST_CAP = 40.f;
 
-// Turns q . k into the score times log2(e), four at a time.  SHAPED: there is a cap or a slope (or a scale that is not
-// positive); without, the scale is left for the exponential's argument, `unit`: scores are monotonous in q . k.
-template <class T, bool SHAPED>
+// Four scores at a time, times log2(e); PLAIN: not yet scaled, `unit` scales them.
+template <class T, int SHAPE>
 struct Scores {
     float unit, scale, cap, inv_cap, slope;
     __device__ __forceinline__ void init(const AttentionArgs &a, int head)
     {
-        unit = SHAPED ? 1.f : a.scale * LOG2_E;
+        unit = SHAPE == PLAIN ? a.scale * LOG2_E : 1.f;
         scale = a.scale * LOG2_E;
         cap = a.cap * LOG2_E;
-        inv_cap = SHAPED && a.cap > 0.f ? a.scale / a.cap : 0.f;
-        slope = SHAPED && a.slopes ? a.slopes[head] * LOG2_E : 0.f;
+        inv_cap = SHAPE == CAPPED ? 2.f * LOG2_E * a.scale / a.cap : SHAPE == SHAPED && a.cap > 0.f ? a.scale / a.cap : 0.f;
+        slope = SHAPE == SHAPED && a.slopes ? a.slopes[head] * LOG2_E : 0.f;
     }
+    // CAPPED: r of q . k; the score is cap - 2 cap r
+    __device__ __forceinline__ float under(float dot) const { return __builtin_amdgcn_rcpf(exp2_fast(dot * inv_cap) + 1.f); }
     // z: q . k of a query and four keys (STEP = -1) or a key and four queries (STEP = 1), `ahead`: how far the first query
     // is ahead of the first key; cut: the cap's derivative, where not nullptr
     template <int STEP>
     __device__ __forceinline__ void shape(f32x4 &z, int ahead, f32x4 *cut) const
     {
-        if constexpr (SHAPED) {
+        if constexpr (SHAPE == SHAPED) {
             if (cap > 0.f) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float t = cap_tanh(z[e] * inv_cap, T());
+                    const float t = tanhf(z[e] * inv_cap);
                     z[e] = cap * t;
                     if (cut) (*cut)[e] = 1.f - t * t;
                 }
@@ -123,6 +129,25 @@ struct Scores {
             for (int e = 0; e < 4; ++e) z[e] -= slope * __builtin_fabsf(far + (float)(STEP * e));
         }
     }
+    // P of four q . k for a query (key) with lse (times log2(e)), and the factor of the cap in dS (CAPPED: without its 4)
+    template <int STEP>
+    __device__ __forceinline__ void weigh(f32x4 &z, int ahead, f32x4 lse, f32x4 &cut) const
+    {
+        if constexpr (SHAPE == CAPPED) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float r = under(z[e]);
+                z[e] = exp2_fast(__builtin_fmaf(r, -2.f * cap, cap - lse[e]));
+                cut[e] = __builtin_fmaf(-r, r, r);
+            }
+        } else {
+            shape<STEP>(z, ahead, &cut);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[e] = exp2_fast(z[e] * unit - lse[e]);
+        }
+    }
+    // what dS is still to be multiplied with
+    __device__ __forceinline__ float rest(const AttentionArgs &a) const { return SHAPE == CAPPED ? 4.f * a.scale : a.scale; }
 };
 
 template <int N>
@@ -170,10 +195,11 @@ __device__ __forceinline__ QueryTile query_tile(const AttentionArgs &a)
 {
     QueryTile w;
     const int group = a.heads / a.kv_heads;
-    const long long t = die_run(blockIdx.x, gridDim.x);
-    w.head = (int)(t / ((long long)a.tiles * group)) * group + (int)(t % group);
+    // Heads are numbered fastest: workgroups are dealt to the eight dies in turn, so a die has the same heads of all tiles, and
+    // their keys in its cache, and long and short tiles alike.
+    w.head = (int)(blockIdx.x % a.heads);
     w.kv = w.head / group;
-    const long long tile = a.tiles - 1 - (t / group) % a.tiles;   // causal: the long ones first
+    const long long tile = a.tiles - 1 - blockIdx.x / a.heads;   // causal: the long ones first
     const int p = set_of_tile(a.q_off, a.sets, BQ, tile);
     w.s = range_of(a, p);
     const long long b0 = (tile - (w.s.q0 / BQ + p)) * BQ;
@@ -219,7 +245,7 @@ __device__ __forceinline__ void two_buffers(int steps, Fetch fetch, Landed lande
 
 // ---- forward -------------------------------------------------------------------
 // Four wavefronts of 16 QT queries each go over the set's keys, 64 at a time.
-template <class T, int DP, int QT, bool VEC, bool SHAPED>
+template <class T, int DP, int QT, bool VEC, int SHAPE>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward_kernel(AttentionArgs a)
 {
     constexpr int BQ = 64 * QT, BK = 64, C = DP / 32, DT = DP / 16;
@@ -230,7 +256,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
     const QueryTile w = query_tile<BQ>(a);
     if (!w.any) return;
     const SetRange s = w.s;
-    Scores<T, SHAPED> score;
+    Scores<T, SHAPE> score;
     score.init(a, w.head);
 
     const T *qp = (const T *)a.q + s.q0 * a.q_token + w.head * a.q_head;
@@ -262,70 +288,93 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
     auto work = [&](int t, auto which) {
         const char *lds_k = decltype(which)::value ? lds1 : lds0, *lds_v = lds_k + BK * L::PITCH;
         const int j0 = t * BK;
+        // sets of a tile or less: what lies behind their ends is left out, 16 queries and 16 keys at a time
+        const int tiles = QT == 1 ? (w.last - j0 + 15) / 16 : 4;
+        if (QT == 1 && w_first >= s.nq) return;
         f32x4 z[4][QT];
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
             for (int u = 0; u < QT; ++u) z[kt][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < C; ++c)
+        for (int kt = 0; kt < 4; ++kt) {
+            if (QT == 1 && kt >= tiles) break;
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt) {
+            for (int c = 0; c < C; ++c) {
                 const typename Frag<T>::type fk = L::rows(lds_k, kt * 16, c, lane);
 #pragma unroll
                 for (int u = 0; u < QT; ++u) mma(z[kt][u], fk, fq[u][c]);
             }
+        }
         settle(z);
         const bool whole = j0 + BK <= s.nk && (!a.causal || j0 + BK - 1 <= w_first + w.shift || j0 + BK <= w.prefix);
+        auto seen = [&](int j, int at) { return j < s.nk && (!a.causal || j <= at || j < w.prefix); };
         typename Frag<T>::type fp[2][QT];
 #pragma unroll
         for (int u = 0; u < QT; ++u) {
             const int at = qi[u] + w.shift;
-#pragma unroll
-            for (int kt = 0; kt < 4; ++kt) score.template shape<-1>(z[kt][u], at - (j0 + kt * 16 + 4 * g), nullptr);
-            if (!whole) {
+            float add = 0.f;
+            if constexpr (SHAPE == CAPPED) {
 #pragma unroll
                 for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int j = j0 + kt * 16 + 4 * g + e;
-                        if (j >= s.nk || (a.causal && j > at && j >= w.prefix)) z[kt][u][e] = minus_infinity();
-                    }
+                    for (int e = 0; e < 4; ++e) z[kt][u][e] = exp2_fast(score.under(z[kt][u][e]) * (-2.f * score.cap));
+                if (!whole) {
+#pragma unroll
+                    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!seen(j0 + kt * 16 + 4 * g + e, at)) z[kt][u][e] = 0.f;
+                }
+            } else {
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt) score.template shape<-1>(z[kt][u], at - (j0 + kt * 16 + 4 * g), nullptr);
+                if (!whole) {
+#pragma unroll
+                    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!seen(j0 + kt * 16 + 4 * g + e, at)) z[kt][u][e] = minus_infinity();
+                }
+                float most = top[u];
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) most = fmaxf(most, z[kt][u][e]);
+                most = fmaxf(most, __shfl_xor(most, 16));
+                most = fmaxf(most, __shfl_xor(most, 32));
+                const float ref = most == minus_infinity() ? 0.f : most * score.unit;
+                if (__any(most != top[u])) {   // else nothing is scaled down
+                    const float keep = exp2_fast(top[u] * score.unit - ref);
+                    top[u] = most;
+                    sum[u] *= keep;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[d][u] *= keep;
+                }
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[kt][u][e] = exp2_fast(z[kt][u][e] * score.unit - ref);
             }
-            float most = top[u];
-#pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) most = fmaxf(most, z[kt][u][e]);
-            most = fmaxf(most, __shfl_xor(most, 16));
-            most = fmaxf(most, __shfl_xor(most, 32));
-            const float ref = most == minus_infinity() ? 0.f : most * score.unit;
-            if (__any(most != top[u])) {   // else nothing is scaled down
-                const float keep = exp2_fast(top[u] * score.unit - ref);
-                top[u] = most;
-                sum[u] *= keep;
-#pragma unroll
-                for (int d = 0; d < DT; ++d) o[d][u] *= keep;
-            }
-            float add = 0.f;
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float v = exp2_fast(z[kt][u][e] * score.unit - ref);
-                    add += v;
-                    fp[kt >> 1][u][(kt & 1) * 4 + e] = (T)v;
+                    add += z[kt][u][e];
+                    fp[kt >> 1][u][(kt & 1) * 4 + e] = (T)z[kt][u][e];
                 }
             sum[u] += add;
         }
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+        for (int c = 0; c < 2; ++c) {
+            if (QT == 1 && 2 * c >= tiles) break;
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
                 const typename Frag<T>::type fv = L::columns(lds_v, c * 32, d * 16, lane);
 #pragma unroll
                 for (int u = 0; u < QT; ++u) mma(o[d][u], fv, fp[c][u]);
             }
+        }
     };
     two_buffers((w.last + BK - 1) / BK, fetch, [](int, auto) {}, work);
     settle_loop();
@@ -343,7 +392,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
             const int d0 = d * 16 + 4 * g;
             if (d0 < a.dim) store_four(out + d0, o[d][u] * inv, a.dim - d0, VEC);
         }
-        if (g == 0) a.lse[w.head * a.total_q + n] = (top[u] * score.unit + log2f(total)) * LN_2;
+        const float reference = SHAPE == CAPPED ? score.cap : top[u] * score.unit;
+        if (g == 0) a.lse[w.head * a.total_q + n] = (reference + log2f(total)) * LN_2;
     }
 }
 
@@ -351,7 +401,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
 // key is read once for all query heads that share it.  Bound by reading the keys: each wavefront goes over its own 32 keys at
 // a time, through its own two buffers of LDS without waiting for the others.  A row is a query and one of the heads of
 // the group: row = query * group + head of the group.
-template <class T, int DP, int QT, int WAVES, bool VEC, bool SHAPED>
+template <class T, int DP, int QT, int WAVES, bool VEC, int SHAPE>
 __global__ __launch_bounds__(WAVES * 64) void attention_chunk_kernel(AttentionArgs a)
 {
     constexpr int C = DP / 32, DT = DP / 16, BK = 32;
@@ -377,7 +427,7 @@ __global__ __launch_bounds__(WAVES * 64) void attention_chunk_kernel(AttentionAr
     const T *vp = (const T *)a.v + s.k0 * a.v_token + kv * a.v_head;
 
     typename Frag<T>::type fq[QT][C];
-    Scores<T, SHAPED> score[QT];
+    Scores<T, SHAPE> score[QT];
     int qi[QT];
     f32x4 o[DT][QT];
     float top[QT], sum[QT];
@@ -543,14 +593,24 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a)
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) most = fmaxf(most, __shfl_xor(most, x));
     float total = 0.f, v0 = 0.f, v1 = 0.f;
-#pragma unroll 4
-    for (int c = 0; c < chunks; ++c) {
-        const float2 ml = a.part_ml[at + c * stride];
-        const float keep = ml.x == minus_infinity() ? (ml.y == ml.y ? 0.f : ml.y) : exp2_fast(ml.x - most);
-        const float *o = a.part_o + (at + c * stride) * a.dim;
-        total += ml.y * keep;
-        if (lane < a.dim) v0 += o[lane] * keep;
-        if (lane + 64 < a.dim) v1 += o[lane + 64] * keep;
+    for (int c0 = 0; c0 < chunks; c0 += 64) {   // a lane has the weight of a chunk
+        float keep = 0.f, sum = 0.f;
+        if (c0 + lane < chunks) {
+            const float2 ml = a.part_ml[at + (c0 + lane) * stride];
+            keep = ml.x == minus_infinity() ? (ml.y == ml.y ? 0.f : ml.y) : exp2_fast(ml.x - most);
+            sum = ml.y * keep;
+        }
+#pragma unroll
+        for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
+        total += sum;
+        const int count = chunks - c0 < 64 ? chunks - c0 : 64;
+#pragma unroll 8
+        for (int c = 0; c < count; ++c) {
+            const float k = __shfl(keep, c);
+            const float *o = a.part_o + (at + (c0 + c) * stride) * a.dim;
+            if (lane < a.dim) v0 += o[lane] * k;
+            if (lane + 64 < a.dim) v1 += o[lane + 64] * k;
+        }
     }
     const float inv = total > 0.f || total != total ? 1.f / total : 0.f;   // no key: zero
     T *out = (T *)a.o + row * a.dim;
@@ -579,7 +639,7 @@ __global__ __launch_bounds__(256) void attention_delta_kernel(const T *__restric
 // its own: o is large there, and its rounding to bf16 would count in dS as much as that of dS itself (with more keys o is
 // an average of many v, and small).  The delta that is used goes to a.delta for dk and dv.
 constexpr int EXACT_KEYS = 256;
-template <class T, int DP, int QT, bool VEC, bool SHAPED>
+template <class T, int DP, int QT, bool VEC, int SHAPE>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kernel(AttentionArgs a)
 {
     constexpr int BQ = 64 * QT, BK = 64, C = DP / 32, DT = DP / 16;
@@ -590,7 +650,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
     const QueryTile w = query_tile<BQ>(a);
     if (!w.any) return;
     const SetRange s = w.s;
-    Scores<T, SHAPED> score;
+    Scores<T, SHAPE> score;
     score.init(a, w.head);
     const T *kp = (const T *)a.k + s.k0 * a.k_token + w.kv * a.k_head;
     const T *vp = (const T *)a.v + s.k0 * a.v_token + w.kv * a.v_head;
@@ -598,7 +658,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
     int qi[QT];
     float lse[QT], delta[QT];
     f32x4 dq[DT][QT];
-    const bool exact = w.last <= EXACT_KEYS;
+    const bool exact = sizeof(T) == 2 && w.last <= EXACT_KEYS;   // float: o is not rounded
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         qi[u] = w.first + (wave * QT + u) * 16 + (lane & 15);
@@ -656,9 +716,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) {
                 const int at = qi[u] + w.shift, j = j0 + kt * 16 + 4 * g;
-                score.template shape<-1>(z[kt][u], at - j, &cut[kt][u]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) z[kt][u][e] = exp2_fast(z[kt][u][e] * score.unit - lse[u]);
+                score.template weigh<-1>(z[kt][u], at - j, f32x4{lse[u], lse[u], lse[u], lse[u]}, cut[kt][u]);
                 if (!whole) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
@@ -673,8 +731,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
     if (exact) {
         two_buffers(steps, fetch, [](int, auto) {}, [&](int t, auto which) {
             const char *lds_k = decltype(which)::value ? lds1 : lds0, *lds_v = lds_k + BK * L::PITCH;
+            if (QT == 1 && w_first >= s.nq) return;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+                if (QT == 1 && t * BK + h * 32 >= w.last) break;
                 f32x4 z[2][QT], dp[2][QT], cut[2][QT];
                 scores(lds_k, lds_v, t * BK + h * 32, h * 32, z, dp, cut);
 #pragma unroll
@@ -695,8 +755,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
     }
     two_buffers(steps, fetch, [](int, auto) {}, [&](int t, auto which) {
         const char *lds_k = decltype(which)::value ? lds1 : lds0, *lds_v = lds_k + BK * L::PITCH;
+        if (QT == 1 && w_first >= s.nq) return;   // short sets: see the forward kernel
 #pragma unroll
         for (int h = 0; h < 2; ++h) {   // 32 keys at a time
+            if (QT == 1 && t * BK + h * 32 >= w.last) break;
             f32x4 z[2][QT], dp[2][QT], cut[2][QT];
             scores(lds_k, lds_v, t * BK + h * 32, h * 32, z, dp, cut);
             typename Frag<T>::type fs[QT];
@@ -705,7 +767,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt) {
                     f32x4 ds = z[kt][u] * (dp[kt][u] - delta[u]);
-                    if (SHAPED) ds *= cut[kt][u];
+                    if (SHAPE != PLAIN) ds *= cut[kt][u];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) fs[u][kt * 4 + e] = (T)ds[e];
                 }
@@ -725,14 +787,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             const int d0 = d * 16 + 4 * g;
-            if (d0 < a.dim) store_four(out + d0, dq[d][u] * a.scale, a.dim - d0, VEC);
+            if (d0 < a.dim) store_four(out + d0, dq[d][u] * score.rest(a), a.dim - d0, VEC);
         }
     }
 }
 
 // dk, dv: four wavefronts of 16 KT keys each go over the queries of all heads that share the key head, BQ at a
-// time; dv = P^T do, dk = scale dS^T q.
-template <class T, int DP, int KT, bool VEC, bool SHAPED>
+// time; dv = P^T do, dk = scale dS^T q.  With few tiles the heads are dealt to a.splits workgroups, whose sums a second launch adds.
+template <class T, int DP, int KT, bool VEC, int SHAPE>
 __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
 {
     constexpr int BK = 64 * KT, BQ = DP * sizeof(T) > 256 ? 32 : 64, C = DP / 32, DT = DP / 16;
@@ -742,9 +804,10 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
     __shared__ __align__(16) float lds_lse[2][BQ], lds_delta[2][BQ];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
     const int group = a.heads / a.kv_heads;
-    const long long t0 = die_run(blockIdx.x, gridDim.x);
-    const int kv = (int)(t0 / a.tiles);
-    const long long tile = t0 % a.tiles;
+    const int share = (int)(blockIdx.x % a.splits), kv = (int)(blockIdx.x / a.splits % a.kv_heads);
+    const long long tile = blockIdx.x / (a.splits * a.kv_heads);
+    // this workgroup's heads of the group
+    const int h_first = group * share / a.splits, h_count = group * (share + 1) / a.splits - h_first;
     const int p = set_of_tile(a.k_off, a.sets, BK, tile);
     const SetRange s = range_of(a, p);
     const long long b0 = (tile - (s.k0 / BK + p)) * BK;
@@ -781,7 +844,7 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
     float next_lse = 0.f, next_delta = 0.f;
     auto fetch = [&](int t, auto which) {
         char *lds = decltype(which)::value ? lds1 : lds0;
-        const int head = kv * group + t / each, i0 = begin + t % each * BQ;
+        const int head = kv * group + h_first + t / each, i0 = begin + t % each * BQ;
         const T *qp = (const T *)a.q + (s.q0 + i0) * a.q_token + head * a.q_head;
         const T *op = (const T *)a.d_o + ((s.q0 + i0) * a.heads + head) * a.dim;
         if (tid < BQ) {
@@ -801,12 +864,14 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
     };
     auto work = [&](int t, auto which) {
         const char *lds_q = decltype(which)::value ? lds1 : lds0, *lds_o = lds_q + BQ * L::PITCH;
-        const int head = kv * group + t / each;
-        Scores<T, SHAPED> score;
+        const int head = kv * group + h_first + t / each;
+        Scores<T, SHAPE> score;
         score.init(a, head);
+        if (KT == 1 && w_last - 15 >= s.nk) return;   // short sets: no key of this wavefront, no query of the 32
 #pragma unroll
         for (int h = 0; h < BQ / 32; ++h) {   // 32 queries at a time
             const int i0 = begin + t % each * BQ + h * 32;
+            if (KT == 1 && i0 >= s.nq) break;
             f32x4 z[2][KT], dp[2][KT];
 #pragma unroll
             for (int qt = 0; qt < 2; ++qt)
@@ -836,12 +901,9 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
                 for (int u = 0; u < KT; ++u) {
                     const int i = i0 + qt * 16 + 4 * g, j = kj[u];
                     f32x4 cut;
-                    score.template shape<1>(z[qt][u], i + shift - j, &cut);
-                    f32x4 pr, ds;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) pr[e] = exp2_fast(z[qt][u][e] * score.unit - lse[e]);
-                    ds = pr * (dp[qt][u] - delta);
-                    if (SHAPED) ds *= cut;
+                    score.template weigh<1>(z[qt][u], i + shift - j, lse, cut);
+                    f32x4 pr = z[qt][u], ds = pr * (dp[qt][u] - delta);
+                    if (SHAPE != PLAIN) ds *= cut;
                     if (!whole) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
@@ -866,8 +928,9 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
             }
         }
     };
-    two_buffers(group * each, fetch, landed, work);
+    two_buffers(h_count * each, fetch, landed, work);
     settle_loop();
+    const float rest = Scores<T, SHAPE>().rest(a);
 #pragma unroll
     for (int u = 0; u < KT; ++u) {
         if (kj[u] >= s.nk) continue;
@@ -876,18 +939,47 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
         for (int d = 0; d < DT; ++d) {
             const int d0 = d * 16 + 4 * g;
             if (d0 >= a.dim) continue;
-            store_four((T *)a.dk + at + d0, dk[d][u] * a.scale, a.dim - d0, VEC);
-            store_four((T *)a.dv + at + d0, dv[d][u], a.dim - d0, VEC);
+            if (a.splits > 1) {
+                const long long all = a.total_k * a.kv_heads * a.dim;
+                store_four(a.part_kv + 2 * share * all + at + d0, dk[d][u] * rest, a.dim - d0, VEC);
+                store_four(a.part_kv + (2 * share + 1) * all + at + d0, dv[d][u], a.dim - d0, VEC);
+            } else {
+                store_four((T *)a.dk + at + d0, dk[d][u] * rest, a.dim - d0, VEC);
+                store_four((T *)a.dv + at + d0, dv[d][u], a.dim - d0, VEC);
+            }
+        }
+    }
+}
+
+// dk and dv from the sums of `splits` workgroups, in their order: a thread adds four values
+template <class T>
+__global__ __launch_bounds__(256) void attention_add_kernel(AttentionArgs a, int whole)
+{
+    const long long all = a.total_k * a.kv_heads * a.dim, fours = (all + 3) / 4;
+    const long long begin = a.k_off[0] < 0 ? 0 : a.k_off[0], end = a.k_off[a.sets] < a.total_k ? a.k_off[a.sets] : a.total_k;
+    const long long width = (long long)a.kv_heads * a.dim;
+    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < 2 * fours; t += (long long)gridDim.x * 256) {
+        const int which = t >= fours;
+        const long long i = (t - which * fours) * 4;
+        T *out = (T *)(which ? a.dv : a.dk);
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < a.splits; ++s)
+            v += load_four(a.part_kv + (2 * s + which) * all + i, all - i < 4 ? (int)(all - i) : 4, whole);
+        if (i >= begin * width && i + 4 <= end * width) {
+            store_four(out + i, v, 4, whole);
+        } else {   // keys in no set are not written
+            for (int e = 0; e < 4; ++e)
+                if (i + e >= begin * width && i + e < end * width) out[i + e] = (T)v[e];
         }
     }
 }
 
 // one translation unit per type (kernels_attention_*.hip)
 template <class T>
-hipError_t attention_forward(AttentionArgs a, bool vec, bool shaped, hipStream_t s);
+hipError_t attention_forward(AttentionArgs a, bool vec, int shape, hipStream_t s);
 template <class T>
-hipError_t attention_by_chunks(AttentionArgs a, bool vec, bool shaped, hipStream_t s);
+hipError_t attention_by_chunks(AttentionArgs a, bool vec, int shape, hipStream_t s);
 template <class T>
-hipError_t attention_backward(AttentionArgs a, bool vec, bool shaped, hipStream_t s);
+hipError_t attention_backward(AttentionArgs a, bool vec, int shape, hipStream_t s);
 
 }  // namespace lcn

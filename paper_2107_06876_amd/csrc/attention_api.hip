@@ -56,8 +56,11 @@ static bool pieces(const AttentionArgs &a, size_t e, const void *const *more, in
     return (all & 15) == 0 && (strides & (long long)(16 / e - 1)) == 0;
 }
 
-// Whether scores are more than a positive multiple of q . k.
-static bool shaped_scores(const AttentionArgs &a) { return a.cap > 0.f || a.slopes || !(a.scale > 0.f); }
+static int shape_of(const AttentionArgs &a)
+{
+    if (a.slopes || !(a.scale > 0.f)) return SHAPED;
+    return a.cap == 0.f ? PLAIN : a.cap <= MOST_CAP ? CAPPED : SHAPED;
+}
 
 // Where a set has few queries, its keys are split over workgroups: up to 32 rows (queries times the heads that share a key
 // head) fit a wavefront.  Chunks of keys are so long that there are some eight workgroups per compute unit, from 128 keys (a
@@ -92,6 +95,31 @@ static ChunkSpace chunk_space(char *ws, const lcn_attention_desc *d)
     return f;
 }
 
+// Workgroups that share the query heads of a key head in the dk, dv kernel: enough for four times the compute units (a causal
+// set's first keys take twice the average time, and sets differ), since the sums of each are written and read once more.
+static int kv_splits(const lcn_attention_desc *d)
+{
+    const int64_t tiles = (d->total_k / 128 + d->num_sets) * d->kv_heads;
+    const int group = d->heads / d->kv_heads;
+    const int64_t wanted = (1024 + tiles - 1) / tiles;
+    return (int)(wanted < group ? wanted : group);
+}
+struct GradSpace {
+    float *delta, *part_kv;
+    int splits;
+    size_t bytes;
+};
+static GradSpace grad_space(char *ws, const lcn_attention_desc *d)
+{
+    Carver c{ws};
+    GradSpace f;
+    f.delta = (float *)c.take((size_t)d->heads * (size_t)d->total_q * 4);
+    f.splits = d->num_sets ? kv_splits(d) : 1;
+    f.part_kv = (float *)c.take(f.splits > 1 ? (size_t)f.splits * 2 * (size_t)d->total_k * d->kv_heads * d->head_dim * 4 : 0);
+    f.bytes = c.used;
+    return f;
+}
+
 }  // namespace lcn
 
 using namespace lcn;
@@ -101,7 +129,7 @@ extern "C" {
 lcn_status lcn_attention_workspace_bytes(const lcn_attention_desc *desc, int32_t backward, size_t *bytes)
 {
     if (!bytes || !attention_desc_fits(desc)) return LCN_ERR_INVALID_ARG;
-    *bytes = backward ? (size_t)desc->heads * (size_t)desc->total_q * 4 : chunk_space(nullptr, desc).bytes;
+    *bytes = backward ? grad_space(nullptr, desc).bytes : chunk_space(nullptr, desc).bytes;
     return LCN_OK;
 }
 
@@ -115,7 +143,8 @@ lcn_status lcn_attention(const lcn_attention_desc *desc, const void *q, const vo
     a.o = o;
     a.lse = lse;
     const void *more[1] = {o};
-    const bool vec = pieces(a, desc->dtype == LCN_F32 ? 4 : 2, more, 1), shaped = shaped_scores(a);
+    const bool vec = pieces(a, desc->dtype == LCN_F32 ? 4 : 2, more, 1);
+    const int shape = shape_of(a);
     const ChunkSpace f = chunk_space((char *)workspace, desc);
     if (f.chunk) {
         if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < f.bytes) return LCN_ERR_ALLOC;
@@ -124,15 +153,15 @@ lcn_status lcn_attention(const lcn_attention_desc *desc, const void *q, const vo
         a.part_o = f.part_o;
         a.part_ml = f.part_ml;
         if (desc->dtype == LCN_F32)
-            OPCHK(attention_by_chunks<float>(a, vec, shaped, (hipStream_t)hip_stream));
+            OPCHK(attention_by_chunks<float>(a, vec, shape, (hipStream_t)hip_stream));
         else
-            OPCHK(attention_by_chunks<__bf16>(a, vec, shaped, (hipStream_t)hip_stream));
+            OPCHK(attention_by_chunks<__bf16>(a, vec, shape, (hipStream_t)hip_stream));
         return LCN_OK;
     }
     if (desc->dtype == LCN_F32)
-        OPCHK(attention_forward<float>(a, vec, shaped, (hipStream_t)hip_stream));
+        OPCHK(attention_forward<float>(a, vec, shape, (hipStream_t)hip_stream));
     else
-        OPCHK(attention_forward<__bf16>(a, vec, shaped, (hipStream_t)hip_stream));
+        OPCHK(attention_forward<__bf16>(a, vec, shape, (hipStream_t)hip_stream));
     return LCN_OK;
 }
 
@@ -145,22 +174,25 @@ lcn_status lcn_attention_backward(const lcn_attention_desc *desc, const void *q,
     if (desc->num_sets == 0 || (!dq && !dk)) return LCN_OK;
     if (desc->total_q > 0 && (!q || !o || !lse || !d_o)) return LCN_ERR_INVALID_ARG;
     if (desc->total_k > 0 && (!k || !v)) return LCN_ERR_INVALID_ARG;
-    const size_t need = (size_t)desc->heads * (size_t)desc->total_q * 4;
-    if (need && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return LCN_ERR_ALLOC;
+    const GradSpace f = grad_space((char *)workspace, desc);
+    if (f.bytes && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < f.bytes)) return LCN_ERR_ALLOC;
     AttentionArgs a = args_of(desc, q, k, v);
     a.d_o = d_o;
     a.o = const_cast<void *>(o);
     a.lse_in = lse;
-    a.delta = (float *)workspace;
+    a.delta = f.delta;
+    a.splits = f.splits;
+    a.part_kv = f.part_kv;
     a.dq = dq;
     a.dk = dk;
     a.dv = dv;
     const void *more[5] = {o, d_o, dq, dk, dv};
-    const bool vec = pieces(a, desc->dtype == LCN_F32 ? 4 : 2, more, 5), shaped = shaped_scores(a);
+    const bool vec = pieces(a, desc->dtype == LCN_F32 ? 4 : 2, more, 5);
+    const int shape = shape_of(a);
     if (desc->dtype == LCN_F32)
-        OPCHK(attention_backward<float>(a, vec, shaped, s));
+        OPCHK(attention_backward<float>(a, vec, shape, s));
     else
-        OPCHK(attention_backward<__bf16>(a, vec, shaped, s));
+        OPCHK(attention_backward<__bf16>(a, vec, shape, s));
     return LCN_OK;
 }
 

@@ -2,5 +2,5 @@
 #include "attention_launch.h"
 
 namespace lcn {
-template hipError_t attention_backward<__bf16>(AttentionArgs, bool, bool, hipStream_t);
+template hipError_t attention_backward<__bf16>(AttentionArgs, bool, int, hipStream_t);
 }  // namespace lcn

@@ -2,5 +2,5 @@
 #include "attention_launch.h"
 
 namespace lcn {
-template hipError_t attention_backward<float>(AttentionArgs, bool, bool, hipStream_t);
+template hipError_t attention_backward<float>(AttentionArgs, bool, int, hipStream_t);
 }  // namespace lcn

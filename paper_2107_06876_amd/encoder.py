@@ -158,8 +158,7 @@ def lcn_cross_entropy(x, w, target, bias=None, scale=1.0, workspace=None):
     """(loss, lse), float32 per row, of the scores scale x W^T + bias; target: int64, negative where a row has none."""
     rows, vocab, dim, dtype = _matrices(x, w, "dim")
     dev = x.device
-    loss = torch.empty(rows, dtype=torch.float32, device=dev)
-    lse = torch.empty(rows, dtype=torch.float32, device=dev)
+    loss, lse = torch.empty((2, rows), dtype=torch.float32, device=dev)
     at, size, space = _space("lcn_cross_entropy_workspace_bytes", (rows, vocab, dim, dtype, 0), workspace, dev)
     _call("lcn_cross_entropy", dev, x.data_ptr(), w.data_ptr(), _tensor(bias, "bias", (vocab,), torch.float32, dev),
           _tensor(target, "target", (rows,), torch.int64, dev), rows, vocab, dim, dtype, float(scale), loss.data_ptr(),
