@@ -232,26 +232,14 @@ struct EntropyGradient {
             const float most = none ? 0.f : __builtin_nanf("");
             const long long here = none ? -1 : t - e.first - (m0 + g4);   // the target among this lane's words
             const int at = here >= 0 && here < TM * 16 ? (int)here : -1;
-            const bool left_out = __any(none), hit = __any(at >= 0);
             f32x4 col[TM];
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
-                f32x4 v;
-                if (e.r.bias) {
-                    v = acc[i][j] * scale + bias[i];
+                f32x4 v = acc[i][j] * scale + bias[i];
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) v[u] -= lse;
-                } else {
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) v[u] = __builtin_fmaf(acc[i][j][u], scale, -lse);
-                }
-#pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = exp2_fast(PLANES == 3 ? v[u] * LOG2E : v[u]);
-                if (left_out) {
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) v[u] = __builtin_fminf(v[u], most);
-                }
-                if (hit) {
+                for (int u = 0; u < 4; ++u)
+                    v[u] = __builtin_fminf(exp2_fast(PLANES == 3 ? (v[u] - lse) * LOG2E : v[u] - lse), most);
+                if (__any((unsigned)(at - i * 16) < 4u)) {
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
                         if (at == i * 16 + u) v[u] -= 1.f;
@@ -262,7 +250,7 @@ struct EntropyGradient {
                     for (int u = 0; u < 4; ++u)
                         if (m0 + i * 16 + g4 + u >= p.m) v[u] = 0.f;
                 }
-                if (e.sums) sum[i] += v;
+                sum[i] += v;
                 col[i] = v;
             }
             by_rows<TM>(

@@ -19,15 +19,15 @@ struct LinearArgs {
 };
 
 template <class T, int ACT>
-__device__ __forceinline__ void linear_finish(const LinearArgs<T> &e, f32x4 (&z)[2], const f32x4 (&residual)[2], long long at,
+__device__ __forceinline__ void linear_finish(const LinearArgs<T> &e, f32x4 (&z)[2], const Eight<T> &residual, long long at,
                                               int left)
 {
     if (e.pre) store_eight(e.pre + at, z, left, e.whole);
 #pragma unroll
     for (int u = 0; u < 8; ++u) z[u >> 2][u & 3] = activate<ACT>(z[u >> 2][u & 3]);
     if (e.residual) {
-        z[0] += residual[0];
-        z[1] += residual[1];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) z[u >> 2][u & 3] += (float)residual.v[u];
     }
     store_eight(e.y + at, z, left, e.whole);
 }
@@ -48,9 +48,6 @@ struct LinearEpilogue {
             bias[i] = f32x4{0.f, 0.f, 0.f, 0.f};
             if (e.bias && m < p.m) bias[i] = load_four(e.bias + m, (int)(p.m - m), e.whole);
         }
-        struct Eight {
-            f32x4 v[2];
-        };
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             f32x4 col[TM];
@@ -59,14 +56,12 @@ struct LinearEpilogue {
             by_rows<TM>(
                 region, col, lane,
                 [&](int r, int c) {
-                    Eight o = {};
                     const long long n = n0 + j * 16 + r, m = m0 + c;
-                    if (e.residual && n < p.n && m < p.m) load_eight(e.residual + n * p.m + m, (int)(p.m - m), e.whole, o.v);
-                    return o;
+                    return e.residual && n < p.n && m < p.m ? read_eight(e.residual + n * p.m + m, (int)(p.m - m), e.whole) : Eight<T>{};
                 },
-                [&](int r, int c, f32x4 (&v)[2], const Eight &o) {
+                [&](int r, int c, f32x4 (&v)[2], const Eight<T> &o) {
                     const long long n = n0 + j * 16 + r, m = m0 + c;
-                    if (n < p.n && m < p.m) linear_finish<T, ACT>(e, v, o.v, n * p.m + m, (int)(p.m - m));
+                    if (n < p.n && m < p.m) linear_finish<T, ACT>(e, v, o, n * p.m + m, (int)(p.m - m));
                 });
         }
     }
@@ -81,7 +76,8 @@ __global__ __launch_bounds__(256) void linear_finish_kernel(LinearArgs<T> e, con
     for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < rows * per_row; t += (long long)gridDim.x * 256) {
         const long long n = t / per_row;
         const int m = (int)(t - n * per_row) * 8, left = width - m;
-        f32x4 z[2], v[2], r[2] = {};
+        f32x4 z[2], v[2];
+        Eight<T> r{};
         load_eight(part + n * ldp + m, 8, true, z);
         for (int u = 1; u < splits; ++u) {
             load_eight(part + u * stride + n * ldp + m, 8, true, v);
@@ -93,7 +89,7 @@ __global__ __launch_bounds__(256) void linear_finish_kernel(LinearArgs<T> e, con
             z[0] += v[0];
             z[1] += v[1];
         }
-        if (e.residual) load_eight(e.residual + n * width + m, left, e.whole, r);
+        if (e.residual) r = read_eight(e.residual + n * width + m, left, e.whole);
         linear_finish<T, ACT>(e, z, r, n * width + m, left);
     }
 }

@@ -67,6 +67,29 @@ __device__ __forceinline__ void load_eight(const T *p, int left, bool whole, f32
     r[0] = load_four(p, left, whole);
     r[1] = load_four(p + 4, left - 4, whole);
 }
+// The same as they are in memory.
+template <class T>
+struct Eight {
+    T v[8];
+};
+template <class T>
+__device__ __forceinline__ Eight<T> read_eight(const T *p, int left, bool whole)
+{
+    Eight<T> r;
+    if (whole && left >= 8) {
+        typedef T piece __attribute__((ext_vector_type(16 / sizeof(T))));
+#pragma unroll
+        for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+            const piece q = ((const piece *)p)[h];
+#pragma unroll
+            for (int e = 0; e < 16 / (int)sizeof(T); ++e) r.v[h * (16 / (int)sizeof(T)) + e] = q[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.v[e] = e < left ? p[e] : (T)0.f;
+    }
+    return r;
+}
 template <class T>
 __device__ __forceinline__ void store_eight(T *p, const f32x4 (&v)[2], int left, bool whole)
 {
@@ -202,22 +225,18 @@ struct PartialEpilogue {
             f32x4 col[TM];
 #pragma unroll
             for (int i = 0; i < TM; ++i) col[i] = acc[i][j];
-            struct Eight {
-                f32x4 v[2];
-            };
             by_rows<TM>(
                 region, col, lane,
                 [&](int r, int c) {
-                    Eight o = {};
                     const long long n = n0 + j * 16 + r;
-                    if (e.add && n < p.n && m0 + c < p.m) load_eight(first + n * e.ldp + c, 8, true, o.v);
-                    return o;
+                    return e.add && n < p.n && m0 + c < p.m ? read_eight(first + n * e.ldp + c, 8, true) : Eight<float>{};
                 },
-                [&](int r, int c, f32x4 (&v)[2], const Eight &o) {
+                [&](int r, int c, f32x4 (&v)[2], const Eight<float> &o) {
                     const long long n = n0 + j * 16 + r;
                     if (n >= p.n || m0 + c >= p.m) return;
-                    const f32x4 w[2] = {v[0] + o.v[0], v[1] + o.v[1]};
-                    store_eight(first + n * e.ldp + c, w, 8, true);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) v[u >> 2][u & 3] += o.v[u];
+                    store_eight(first + n * e.ldp + c, v, 8, true);
                 });
         }
     }

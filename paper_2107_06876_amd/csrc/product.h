@@ -173,21 +173,26 @@ struct Nothing {};
 template <int TM, class Ahead, class Store>
 __device__ __forceinline__ void by_rows(char *region, const f32x4 (&v)[TM], int lane, Ahead ahead, Store store)
 {
-    constexpr int PITCH = RowRegion<TM>::PITCH, ROW = 2 * TM, PIECES = 16 * ROW;
+    constexpr int PITCH = RowRegion<TM>::PITCH, ROW = 2 * TM, PIECES = 16 * ROW, S = (PIECES + 63) / 64;
     float *f = (float *)region;
-    auto next = ahead(lane / ROW, lane % ROW * 8);
+    decltype(ahead(0, 0)) early[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        const int q = s * 64 + lane;
+        if (PIECES % 64 == 0 || q < PIECES) early[s] = ahead(q / ROW, q % ROW * 8);
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i) *(f32x4 *)(f + (lane & 15) * PITCH + i * 16 + 4 * (lane >> 4)) = v[i];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // LDS serves a wavefront in order
     __builtin_amdgcn_wave_barrier();
 #pragma unroll 1   // a loop: unrolled, epilogues with an activation no longer fit beside unrolled accumulators
     for (int q = lane; q < PIECES; q += 64) {
-        const auto now = next;
-        if (q + 64 < PIECES) next = ahead((q + 64) / ROW, (q + 64) % ROW * 8);
         f32x4 w[2];
         w[0] = *(const f32x4 *)(f + q / ROW * PITCH + q % ROW * 8);
         w[1] = *(const f32x4 *)(f + q / ROW * PITCH + q % ROW * 8 + 4);
-        store(q / ROW, q % ROW * 8, w, now);
+        store(q / ROW, q % ROW * 8, w, early[0]);
+#pragma unroll
+        for (int s = 0; s + 1 < S; ++s) early[s] = early[s + 1];
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
