@@ -5,7 +5,7 @@ and a linear layer with the residual; the loss is the cross entropy of every nod
 scale 1 / lambda.  The gradients are formed by the operators' backward calls, layer by layer, and applied by plain
 gradient descent.  At the end the encoded graphs of every pair are compared by a batch of transport problems.
 
-    python examples/train_encoder.py [--graphs 64] [--steps 30] [--bf16]
+    python examples/train_encoder.py [--graphs 64] [--steps 60] [--bf16]
 """
 import argparse
 import os
@@ -69,7 +69,7 @@ def graphs(count, d_in, classes, device, dtype, seed=2):
             torch.from_numpy(target).to(device))
 
 
-def train(count=64, steps=30, d_in=32, d=32, heads=4, classes=1000, lam=0.5, rate=0.3, dtype=torch.float32,
+def train(count=64, steps=30, d_in=32, d=32, heads=4, classes=1000, lam=0.5, rate=0.05, dtype=torch.float32,
           device="cuda:0", say=print):
     """Returns (losses of all steps, transport distances of the pairs (2 p, 2 p + 1))."""
     x, off, host_off, target = graphs(count, d_in, classes, device, dtype)
@@ -86,7 +86,8 @@ def train(count=64, steps=30, d_in=32, d=32, heads=4, classes=1000, lam=0.5, rat
         grads, _ = model.backward(dy)
         for name, w in model.weights.items():
             w -= (rate * grads[name].float()).to(w.dtype)
-        vocabulary -= (rate * x.shape[0] / 10.0 * dvoc.float()).to(vocabulary.dtype)
+        # a word is the target of one row in `classes`: its gradient is so much smaller
+        vocabulary -= (0.1 * rate * classes * dvoc.float()).to(vocabulary.dtype)
         losses.append(float((loss * weight).sum()))
         if step % 10 == 0 or step == steps - 1:
             say("step %d: loss %.4f" % (step, losses[-1]), flush=True)
@@ -98,7 +99,7 @@ def train(count=64, steps=30, d_in=32, d=32, heads=4, classes=1000, lam=0.5, rat
     X, Y = y[torch.cat(left).to(device)].contiguous(), y[torch.cat(right).to(device)].contiguous()
     ends = [np.concatenate([[0], np.cumsum([len(t) for t in side])]).astype(np.int64) for side in (left, right)]
     ones = [torch.ones(t.shape[0], device=device) for t in (X, Y)]
-    h = lcn.lcn_build_batched(X, Y, ends[0], ends[1], np.full(pairs, 0.2, dtype=np.float32), lcn.COST_EUCLID, lcn.MODE_DENSE,
+    h = lcn.lcn_build_batched(X, Y, ends[0], ends[1], np.full(pairs, lam, dtype=np.float32), lcn.COST_EUCLID, lcn.MODE_DENSE,
                               del_cost_x=ones[0], del_cost_y=ones[1])
     lcn.sinkhorn_run(h, 50)
     distances, _ = lcn.lcn_batched_results(h)
@@ -109,7 +110,7 @@ def train(count=64, steps=30, d_in=32, d=32, heads=4, classes=1000, lam=0.5, rat
 if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--graphs", type=int, default=64)
-    ap.add_argument("--steps", type=int, default=30)
+    ap.add_argument("--steps", type=int, default=60)
     ap.add_argument("--bf16", action="store_true")
     a = ap.parse_args()
     train(a.graphs, a.steps, dtype=torch.bfloat16 if a.bf16 else torch.float32)

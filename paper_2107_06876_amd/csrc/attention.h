@@ -85,6 +85,13 @@ __device__ __forceinline__ SetRange range_of(const AttentionArgs &a, int p)
 
 constexpr float LOG2_E = 1.4426950408889634f, LN_2 = 0.6931471805599453f;
 
+// log(2^m s), m times a log(2) in two parts
+__device__ __forceinline__ float natural_log(float m, float s)
+{
+    if (m == -__builtin_huge_valf()) return s == s ? m : s;   // no key; or scores that are not numbers
+    return __builtin_fmaf(m, LN_2, __builtin_fmaf(m, -1.9046542e-9f, logf(s)));
+}
+
 // How q . k becomes a score.  PLAIN: a positive multiple.  CAPPED (bf16 tensors, scale > 0, cap up to MOST_CAP, no slopes):
 // cap tanh(scale q.k / cap) = cap - 2 cap r with r = 1 / (e^(2 scale q.k / cap) + 1), off by about 2^-23 of the cap, far
 // below the rounding of P; no score is above the cap, so that is the reference of the exponentials: P' = 2^(-2 cap r
@@ -95,10 +102,11 @@ constexpr float MOST_CAP = 40.f;
 // Four scores at a time, times log2(e); PLAIN: not yet scaled, `unit` scales them.
 template <class T, int SHAPE>
 struct Scores {
-    float unit, scale, cap, inv_cap, slope;
+    float unit, natural, scale, cap, inv_cap, slope;
     __device__ __forceinline__ void init(const AttentionArgs &a, int head)
     {
         unit = SHAPE == PLAIN ? a.scale * LOG2_E : 1.f;
+        natural = a.scale;
         scale = a.scale * LOG2_E;
         cap = a.cap * LOG2_E;
         inv_cap = SHAPE == CAPPED ? 2.f * LOG2_E * a.scale / a.cap : SHAPE == SHAPED && a.cap > 0.f ? a.scale / a.cap : 0.f;
@@ -129,7 +137,7 @@ struct Scores {
             for (int e = 0; e < 4; ++e) z[e] -= slope * __builtin_fabsf(far + (float)(STEP * e));
         }
     }
-    // P of four q . k for a query (key) with lse (times log2(e)), and the factor of the cap in dS (CAPPED: without its 4)
+    // P of four q . k for a query (key) with lse (by lse_in()), and the factor of the cap in dS (CAPPED: without its 4)
     template <int STEP>
     __device__ __forceinline__ void weigh(f32x4 &z, int ahead, f32x4 lse, f32x4 &cut) const
     {
@@ -143,8 +151,18 @@ struct Scores {
         } else {
             shape<STEP>(z, ahead, &cut);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) z[e] = exp2_fast(z[e] * unit - lse[e]);
+            for (int e = 0; e < 4; ++e) z[e] = weight(z[e], lse[e]);
         }
+    }
+    // e^(score - lse), lse in the units of lse_in(): float tensors take the difference before they change its unit, so that
+    // it is rounded at its own size and not at that of lse times log2(e)
+    static __device__ __forceinline__ float lse_in(float lse) { return sizeof(T) == 4 ? lse : lse * LOG2_E; }
+    __device__ __forceinline__ float weight(float z, float lse) const
+    {
+        if constexpr (sizeof(T) == 4)
+            return exp2_fast((SHAPE == PLAIN ? __builtin_fmaf(z, natural, -lse) : __builtin_fmaf(z, LN_2, -lse)) * LOG2_E);
+        else
+            return exp2_fast(z * unit - lse);
     }
     // what dS is still to be multiplied with
     __device__ __forceinline__ float rest(const AttentionArgs &a) const { return SHAPE == CAPPED ? 4.f * a.scale : a.scale; }
@@ -393,7 +411,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
             if (d0 < a.dim) store_four(out + d0, o[d][u] * inv, a.dim - d0, VEC);
         }
         const float reference = SHAPE == CAPPED ? score.cap : top[u] * score.unit;
-        if (g == 0) a.lse[w.head * a.total_q + n] = (reference + log2f(total)) * LN_2;
+        if (g == 0) a.lse[w.head * a.total_q + n] = natural_log(reference, total);
     }
 }
 
@@ -616,7 +634,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a)
     T *out = (T *)a.o + row * a.dim;
     if (lane < a.dim) out[lane] = (T)(v0 * inv);
     if (lane + 64 < a.dim) out[lane + 64] = (T)(v1 * inv);
-    if (lane == 0) a.lse[head * a.total_q + n] = (most + log2f(total)) * LN_2;
+    if (lane == 0) a.lse[head * a.total_q + n] = natural_log(most, total);
 }
 
 // ---- backward -------------------------------------------------------------------
@@ -678,7 +696,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
                 for (int e = 0; e < 8; ++e) delta[u] += (float)f[e] * (float)fo[u][c][e];
             }
         }
-        lse[u] = in ? a.lse_in[w.head * a.total_q + n] * LOG2_E : 0.f;
+        lse[u] = in ? Scores<T, SHAPE>::lse_in(a.lse_in[w.head * a.total_q + n]) : 0.f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) dq[d][u] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -858,7 +876,7 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
     };
     auto landed = [&](int, auto which) {
         if (tid < BQ) {
-            lds_lse[decltype(which)::value][tid] = next_lse * LOG2_E;
+            lds_lse[decltype(which)::value][tid] = Scores<T, SHAPE>::lse_in(next_lse);
             lds_delta[decltype(which)::value][tid] = next_delta;
         }
     };

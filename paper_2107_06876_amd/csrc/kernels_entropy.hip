@@ -199,6 +199,7 @@ struct EntropyGradient {
         __bf16 *g;
         long long ldg, plane;   // elements
         float *sums;         // [tile of rows][word of the piece], nullable
+        float *rest;         // [row]: what rounding takes from the target's G, nullable
     };
     template <int TM, int TN, int WM, int WN>
     static __device__ void run(const Args &e, const ProductArgs &p, f32x4 (&acc)[TM][TN], long long m0, long long n0, int,
@@ -242,7 +243,11 @@ struct EntropyGradient {
                 if (__any((unsigned)(at - i * 16) < 4u)) {
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
-                        if (at == i * 16 + u) v[u] -= 1.f;
+                        if (at == i * 16 + u) {
+                            v[u] -= 1.f;
+                            const float all = v[u] * grad;
+                            if (PLANES == 1 && e.rest) e.rest[n] = all - (float)(__bf16)all;
+                        }
                 }
                 v *= grad;
                 if (edge) {
@@ -297,6 +302,37 @@ struct EntropyGradient {
     }
 };
 
+// dx = scale (the sums of G W + what rounding took from the target's G times its word).  The target's G is most of a row's: its
+// rounding to bf16 would be as large in dx as that of dx itself, and the same for all of the row.
+__global__ __launch_bounds__(256) void entropy_finish_kernel(const float *__restrict__ part, int splits, long long stride,
+                                                             long long rows, int dim, long long ldp, float scale,
+                                                             const float *__restrict__ rest, const int64_t *__restrict__ target,
+                                                             const __bf16 *__restrict__ w, int vocab, __bf16 *__restrict__ out,
+                                                             int whole)
+{
+    const int per_row = (dim + 7) / 8;
+    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < rows * per_row; t += (long long)gridDim.x * 256) {
+        const long long n = t / per_row;
+        const int c = (int)(t - n * per_row) * 8;
+        f32x4 v[2], o[2];
+        load_eight(part + n * ldp + c, 8, true, v);
+        for (int s = 1; s < splits; ++s) {
+            load_eight(part + s * stride + n * ldp + c, 8, true, o);
+            v[0] += o[0];
+            v[1] += o[1];
+        }
+        const int64_t at = target[n];
+        if (at >= 0 && at < vocab) {
+            load_eight(w + at * dim + c, dim - c, whole, o);
+            v[0] += o[0] * rest[n];
+            v[1] += o[1] * rest[n];
+        }
+        v[0] *= scale;
+        v[1] *= scale;
+        store_eight(out + n * dim + c, v, dim - c, whole);
+    }
+}
+
 // ---- host ---------------------------------------------------------------------
 
 constexpr int FEW_ROWS = 8, FEW_GROUPS = 1024;
@@ -350,7 +386,7 @@ struct EntropyBackward {
     int32_t piece;                // words
     int planes;                   // of G
     void *xp, *xz, *wp, *g;       // xz: x with zeros in the rows without a target
-    float *part_dx, *part_dw, *sums;
+    float *part_dx, *part_dw, *sums, *rest;
     size_t bytes;
 };
 static EntropyBackward entropy_backward_space(char *ws, int64_t rows, int32_t vocab, int32_t dim, int32_t dtype)
@@ -374,6 +410,7 @@ static EntropyBackward entropy_backward_space(char *ws, int64_t rows, int32_t vo
     b.part_dx = (float *)c.take((size_t)b.dx.splits * rows * padded(dim) * 4);
     b.part_dw = (float *)c.take(partial_bytes(b.dw, dim, piece));
     b.sums = (float *)c.take((size_t)(row_tiles(b.scores, rows, dtype)) * piece * 4);
+    b.rest = (float *)c.take(b.planes == 1 ? (size_t)rows * 4 : 0);
     b.bytes = c.used;
     return b;
 }
@@ -430,10 +467,10 @@ static lcn_status entropy_as(const T *x, const T *w, const float *bias, const in
 
 template <int PLANES>
 static hipError_t launch_gradient(const ProductPlan &plan, const ProductArgs &p, const EntropyRow &r, long long first,
-                                  const float *lse, const float *grad, void *g, long long ldg, float *sums, hipStream_t s)
+                                  const float *lse, const float *grad, void *g, long long ldg, float *sums, float *rest, hipStream_t s)
 {
     return launch_planned<PLANES == 3 ? 3 : 1, false, false, EntropyGradient<PLANES>>(plan, p,
-                                                                 {r, first, lse, grad, (__bf16 *)g, ldg, p.n * ldg, sums}, s);
+                                                                 {r, first, lse, grad, (__bf16 *)g, ldg, p.n * ldg, sums, rest}, s);
 }
 
 static lcn_status entropy_backward_as(const void *x, const void *w, const float *bias, const int64_t *target, const float *lse,
@@ -449,7 +486,9 @@ static lcn_status entropy_backward_as(const void *x, const void *w, const float 
     Operand xz{};
     if (dw) xz = add_masked(jobs, x, rows, dim, dtype, target, b.xz);
     OPCHK(launch_planes(jobs, dtype, s));
-    const bool one = b.piece >= vocab;
+    const bool rounded = dx && b.planes == 1, one = b.piece >= vocab && !rounded;
+    float *rest = rounded ? b.rest : nullptr;
+    if (rounded) OPCHK(launch_zero(rest, (size_t)rows * 4, s));
     for (int64_t first = 0; first < vocab; first += b.piece) {
         const int words = (int)(vocab - first < b.piece ? vocab - first : b.piece);
         const Operand here{(const char *)wo.p + first * wo.ld * 2, wo.plane, wo.ld};
@@ -463,9 +502,9 @@ static lcn_status entropy_backward_as(const void *x, const void *w, const float 
         p.n = (int)rows;
         p.k = dim;
         float *sums = dbias ? b.sums : nullptr;
-        OPCHK(b.planes == 3   ? launch_gradient<3>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, s)
-              : b.planes == 2 ? launch_gradient<2>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, s)
-                              : launch_gradient<1>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, s));
+        OPCHK(b.planes == 3   ? launch_gradient<3>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, rest, s)
+              : b.planes == 2 ? launch_gradient<2>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, rest, s)
+                              : launch_gradient<1>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, rest, s));
         if (dbias) {
             const int parts = (int)(row_tiles(b.scores, rows, dtype));
             OPCHK(launch_column_sums(sums, parts, words, LCN_F32, dbias + first, s));
@@ -490,7 +529,13 @@ static lcn_status entropy_backward_as(const void *x, const void *w, const float 
             OPCHK((launch_scaled<true, true>(b.dw, p, scale, dtype, (char *)dw + (size_t)first * dim * size, b.part_dw, s)));
         }
     }
-    if (dx && !one)
+    if (rounded) {
+        const long long groups = (rows * ((dim + 7) / 8) + 255) / 256, ldp = padded(dim);
+        hipLaunchKernelGGL(entropy_finish_kernel, dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(256), 0, s, b.part_dx,
+                           b.dx.splits, rows * ldp, (long long)rows, dim, ldp, scale, rest, target, (const __bf16 *)w, vocab,
+                           (__bf16 *)dx, whole_rows<__bf16>((const void *)((uintptr_t)dx | (uintptr_t)w), dim));
+        OPCHK(hipGetLastError());
+    } else if (dx && !one)
         OPCHK(launch_add_partials(b.part_dx, b.dx.splits, rows, dim, padded(dim), scale, dtype, dx, s));
     return LCN_OK;
 }
