@@ -33,16 +33,17 @@ struct AttentionArgs {
     void *o;                    // read in the backward pass
     float *lse;                 // [head][query]
     // keys split over workgroups: chunks of `chunk` keys, `rows` = max_q * (heads / kv_heads)
-    int chunk, rows;
-    float *part_o;              // [chunk][kv head][row][dim]
-    float2 *part_ml;            // [chunk][kv head][row]: maximum (times log2(e)) and sum
+    int chunk, rows;            // part: [chunk][key head][row][dim], part_top: [chunk][key head][row]
     // backward
     const void *d_o;
     const float *lse_in;
     float *delta;               // [head][query]
     void *dq, *dk, *dv;
-    int splits;                 // workgroups that share the heads of a key head
-    float *part_kv;             // [split][dk, dv][key][key head][dim], where splits > 1
+    // sums shared by several workgroups, where there are few tiles, and joined by a second launch
+    int key_splits;             // of a query tile's keys (forward, dq)
+    int splits;                 // of a key tile's queries (dk, dv)
+    float *part;                // forward, dq: [split][query][head][dim]; dk, dv: [split][dk, dv][key][key head][dim]
+    float2 *part_top;           // forward: [split][query][head], maximum (times log2(e)) and sum
 };
 
 // The last set p of `sets` with below(p), which holds for the first ones; 0 where it holds for none.  All lanes search.
@@ -178,6 +179,12 @@ __device__ __forceinline__ float minus_infinity() { return -__builtin_huge_valf(
 // The accumulators are in general registers from here on.  Without, the compiler (AMD clang 22, ROCm 7.2) has left out the wait between the
 // last matrix instruction and a read of its result behind a branch (attention_chunk_kernel: a wait of 1 to 6 cycles
 // where 8 are due, wrong scores); in one stretch of code it puts it in.
+template <int N>
+__device__ __forceinline__ void settle(f32x4 (&z)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(z[i]));
+}
 template <int N, int M>
 __device__ __forceinline__ void settle(f32x4 (&z)[N][M])
 {
@@ -206,7 +213,14 @@ __device__ __forceinline__ long long die_run(long long id, long long total)
 struct QueryTile {
     SetRange s;
     int head, kv, first, shift, prefix, last;   // last: behind the last key that any query of the tile sees
+    int split;
     bool any;
+    // this workgroup's steps of BK keys
+    template <int BK>
+    __device__ __forceinline__ int step(const AttentionArgs &a, int which) const
+    {
+        return (int)((long long)((last + BK - 1) / BK) * which / a.key_splits);
+    }
 };
 template <int BQ>
 __device__ __forceinline__ QueryTile query_tile(const AttentionArgs &a)
@@ -217,7 +231,8 @@ __device__ __forceinline__ QueryTile query_tile(const AttentionArgs &a)
     // their keys in its cache, and long and short tiles alike.
     w.head = (int)(blockIdx.x % a.heads);
     w.kv = w.head / group;
-    const long long tile = a.tiles - 1 - blockIdx.x / a.heads;   // causal: the long ones first
+    w.split = (int)(blockIdx.x / a.heads % a.key_splits);
+    const long long tile = a.tiles - 1 - blockIdx.x / a.heads / a.key_splits;   // causal: the long ones first
     const int p = set_of_tile(a.q_off, a.sets, BQ, tile);
     w.s = range_of(a, p);
     const long long b0 = (tile - (w.s.q0 / BQ + p)) * BQ;
@@ -234,28 +249,28 @@ __device__ __forceinline__ QueryTile query_tile(const AttentionArgs &a)
     return w;
 }
 
-// Steps 0 .. steps - 1 with two buffers in turn: step t + 1 is on its way while t is worked on.  fetch(t, which),
+// Steps begin .. end - 1 with two buffers in turn: step t + 1 is on its way while t is worked on.  fetch(t, which),
 // landed(t, which): what is left to do when step t's loads have arrived (before all wavefronts meet), work(t, which).
 template <class Fetch, class Landed, class Work>
-__device__ __forceinline__ void two_buffers(int steps, Fetch fetch, Landed landed, Work work)
+__device__ __forceinline__ void two_buffers(int begin, int end, Fetch fetch, Landed landed, Work work)
 {
     auto arrived = [&](int t, auto which) {
         __builtin_amdgcn_s_waitcnt(0x0f70);
         landed(t, which);
         __syncthreads();
     };
-    if (steps <= 0) return;
-    fetch(0, Buffer<0>());
-    int t = 0;
-    for (; t + 2 <= steps; t += 2) {
+    if (begin >= end) return;
+    fetch(begin, Buffer<0>());
+    int t = begin;
+    for (; t + 2 <= end; t += 2) {
         arrived(t, Buffer<0>());
         fetch(t + 1, Buffer<1>());
         work(t, Buffer<0>());
         arrived(t + 1, Buffer<1>());
-        if (t + 2 < steps) fetch(t + 2, Buffer<0>());
+        if (t + 2 < end) fetch(t + 2, Buffer<0>());
         work(t + 1, Buffer<1>());
     }
-    if (t < steps) {
+    if (t < end) {
         arrived(t, Buffer<0>());
         work(t, Buffer<0>());
     }
@@ -383,18 +398,38 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
                 }
             sum[u] += add;
         }
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            if (QT == 1 && 2 * c >= tiles) break;
+        if constexpr (sizeof(T) == 4) {
+            // float: the step's sum by itself, so that long sums are rounded once a step
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
-                const typename Frag<T>::type fv = L::columns(lds_v, c * 32, d * 16, lane);
+                f32x4 t4[QT];
 #pragma unroll
-                for (int u = 0; u < QT; ++u) mma(o[d][u], fv, fp[c][u]);
+                for (int u = 0; u < QT; ++u) t4[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    if (QT == 1 && 2 * c >= tiles) break;
+                    const typename Frag<T>::type fv = L::columns(lds_v, c * 32, d * 16, lane);
+#pragma unroll
+                    for (int u = 0; u < QT; ++u) mma(t4[u], fv, fp[c][u]);
+                }
+                settle(t4);
+#pragma unroll
+                for (int u = 0; u < QT; ++u) o[d][u] += t4[u];
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                if (QT == 1 && 2 * c >= tiles) break;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    const typename Frag<T>::type fv = L::columns(lds_v, c * 32, d * 16, lane);
+#pragma unroll
+                    for (int u = 0; u < QT; ++u) mma(o[d][u], fv, fp[c][u]);
+                }
             }
         }
     };
-    two_buffers((w.last + BK - 1) / BK, fetch, [](int, auto) {}, work);
+    two_buffers(w.step<BK>(a, w.split), w.step<BK>(a, w.split + 1), fetch, [](int, auto) {}, work);
     settle_loop();
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
@@ -403,6 +438,18 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
         total += __shfl_xor(total, 32);
         if (qi[u] >= s.nq) continue;
         const long long n = s.q0 + qi[u];
+        const float reference = SHAPE == CAPPED ? score.cap : top[u] * score.unit;
+        if (a.key_splits > 1) {
+            const long long row = (w.split * a.total_q + n) * a.heads + w.head;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                const int d0 = d * 16 + 4 * g;
+                if (d0 < a.dim) store_four(a.part + row * a.dim + d0, o[d][u], a.dim - d0, VEC);
+            }
+            // (capped: without keys there is no maximum either)
+            if (g == 0) a.part_top[row] = make_float2(total == 0.f ? minus_infinity() : reference, total);
+            continue;
+        }
         const float inv = total > 0.f || total != total ? 1.f / total : 0.f;   // no key: zero
         T *out = (T *)a.o + (n * a.heads + w.head) * a.dim;
 #pragma unroll
@@ -410,9 +457,34 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
             const int d0 = d * 16 + 4 * g;
             if (d0 < a.dim) store_four(out + d0, o[d][u] * inv, a.dim - d0, VEC);
         }
-        const float reference = SHAPE == CAPPED ? score.cap : top[u] * score.unit;
         if (g == 0) a.lse[w.head * a.total_q + n] = natural_log(reference, total);
     }
+}
+
+// Joins the splits of a query and head, a wavefront each, in their order.
+template <class T>
+__global__ __launch_bounds__(256) void attention_join_splits_kernel(AttentionArgs a)
+{
+    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), n = row / a.heads, all = a.total_q * a.heads;
+    const int head = (int)(row % a.heads), lane = threadIdx.x & 63;
+    if (n >= a.total_q || n < a.q_off[0] || n >= a.q_off[a.sets]) return;
+    float most = minus_infinity();
+    for (int s = 0; s < a.key_splits; ++s) most = fmaxf(most, a.part_top[s * all + row].x);
+    float total = 0.f, v0 = 0.f, v1 = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < a.key_splits; ++s) {
+        const float2 ml = a.part_top[s * all + row];
+        const float keep = ml.x == minus_infinity() ? (ml.y == ml.y ? 0.f : ml.y) : exp2_fast(ml.x - most);
+        const float *o = a.part + (s * all + row) * a.dim;
+        total += ml.y * keep;
+        if (lane < a.dim) v0 += o[lane] * keep;
+        if (lane + 64 < a.dim) v1 += o[lane + 64] * keep;
+    }
+    const float inv = total > 0.f || total != total ? 1.f / total : 0.f;   // no key: zero
+    T *out = (T *)a.o + row * a.dim;
+    if (lane < a.dim) out[lane] = (T)(v0 * inv);
+    if (lane + 64 < a.dim) out[lane + 64] = (T)(v1 * inv);
+    if (lane == 0) a.lse[head * a.total_q + n] = natural_log(most, total);
 }
 
 // Few queries per set (new tokens): the keys of a set are cut into chunks, a workgroup per chunk and key head, so that every
@@ -586,9 +658,9 @@ __global__ __launch_bounds__(WAVES * 64) void attention_chunk_kernel(AttentionAr
             float v = 0.f;
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) v += all[((long long)w * QT * 16 + r) * DP + d];
-            a.part_o[(first + r) * a.dim + d] = v;
+            a.part[(first + r) * a.dim + d] = v;
         }
-        if (lane == 0) a.part_ml[first + r] = make_float2(most, total);
+        if (lane == 0) a.part_top[first + r] = make_float2(most, total);
     }
 }
 
@@ -607,14 +679,14 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a)
     const int chunks = (s.nk + a.chunk - 1) / a.chunk;
     const long long stride = (long long)a.kv_heads * a.rows, at = (first * a.kv_heads + kv) * a.rows + r;
     float most = minus_infinity();
-    for (int c = lane; c < chunks; c += 64) most = fmaxf(most, a.part_ml[at + c * stride].x);
+    for (int c = lane; c < chunks; c += 64) most = fmaxf(most, a.part_top[at + c * stride].x);
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) most = fmaxf(most, __shfl_xor(most, x));
     float total = 0.f, v0 = 0.f, v1 = 0.f;
     for (int c0 = 0; c0 < chunks; c0 += 64) {   // a lane has the weight of a chunk
         float keep = 0.f, sum = 0.f;
         if (c0 + lane < chunks) {
-            const float2 ml = a.part_ml[at + (c0 + lane) * stride];
+            const float2 ml = a.part_top[at + (c0 + lane) * stride];
             keep = ml.x == minus_infinity() ? (ml.y == ml.y ? 0.f : ml.y) : exp2_fast(ml.x - most);
             sum = ml.y * keep;
         }
@@ -625,7 +697,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a)
 #pragma unroll 8
         for (int c = 0; c < count; ++c) {
             const float k = __shfl(keep, c);
-            const float *o = a.part_o + (at + (c0 + c) * stride) * a.dim;
+            const float *o = a.part + (at + (c0 + c) * stride) * a.dim;
             if (lane < a.dim) v0 += o[lane] * k;
             if (lane + 64 < a.dim) v1 += o[lane + 64] * k;
         }
@@ -650,6 +722,26 @@ __global__ __launch_bounds__(256) void attention_delta_kernel(const T *__restric
 #pragma unroll
     for (int x = 8; x > 0; x >>= 1) s += __shfl_xor(s, x, 16);
     if ((threadIdx.x & 15) == 0) delta[(r % heads) * total_q + r / heads] = s;
+}
+
+// sum[u] += a b[u]; float: the product by itself, so that a long sum is rounded once for 32 of its terms
+template <class T, int N>
+__device__ __forceinline__ void add_product(f32x4 (&sum)[N], typename Frag<T>::type a, const typename Frag<T>::type (&b)[N])
+{
+    if constexpr (sizeof(T) == 4) {
+        f32x4 t[N];
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            t[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+            mma(t[u], a, b[u]);
+        }
+        settle(t);
+#pragma unroll
+        for (int u = 0; u < N; ++u) sum[u] += t[u];
+    } else {
+#pragma unroll
+        for (int u = 0; u < N; ++u) mma(sum[u], a, b[u]);
+    }
 }
 
 // dq: like the forward pass; dS = P (dP - delta) cut, dq = scale sum_j dS_ij k_j.
@@ -745,9 +837,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
                 }
             }
     };
-    const int steps = (w.last + BK - 1) / BK;
     if (exact) {
-        two_buffers(steps, fetch, [](int, auto) {}, [&](int t, auto which) {
+        two_buffers(0, (w.last + BK - 1) / BK, fetch, [](int, auto) {}, [&](int t, auto which) {
             const char *lds_k = decltype(which)::value ? lds1 : lds0, *lds_v = lds_k + BK * L::PITCH;
             if (QT == 1 && w_first >= s.nq) return;
 #pragma unroll
@@ -769,9 +860,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
     for (int u = 0; u < QT; ++u) {
         delta[u] += __shfl_xor(delta[u], 16);
         delta[u] += __shfl_xor(delta[u], 32);
-        if (g == 0 && qi[u] < s.nq) a.delta[w.head * a.total_q + s.q0 + qi[u]] = delta[u];
+        if (g == 0 && qi[u] < s.nq && w.split == 0) a.delta[w.head * a.total_q + s.q0 + qi[u]] = delta[u];
     }
-    two_buffers(steps, fetch, [](int, auto) {}, [&](int t, auto which) {
+    two_buffers(w.step<BK>(a, w.split), w.step<BK>(a, w.split + 1), fetch, [](int, auto) {}, [&](int t, auto which) {
         const char *lds_k = decltype(which)::value ? lds1 : lds0, *lds_v = lds_k + BK * L::PITCH;
         if (QT == 1 && w_first >= s.nq) return;   // short sets: see the forward kernel
 #pragma unroll
@@ -792,8 +883,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
                 const typename Frag<T>::type fk = L::columns(lds_k, h * 32, d * 16, lane);
-#pragma unroll
-                for (int u = 0; u < QT; ++u) mma(dq[d][u], fk, fs[u]);
+                add_product<T>(dq[d], fk, fs);
             }
         }
     });
@@ -801,17 +891,22 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         if (qi[u] >= s.nq) continue;
-        T *out = (T *)a.dq + ((s.q0 + qi[u]) * a.heads + w.head) * a.dim;
+        const long long at = ((s.q0 + qi[u]) * a.heads + w.head) * a.dim;
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             const int d0 = d * 16 + 4 * g;
-            if (d0 < a.dim) store_four(out + d0, dq[d][u] * score.rest(a), a.dim - d0, VEC);
+            if (d0 >= a.dim) continue;
+            const f32x4 v = dq[d][u] * score.rest(a);
+            if (a.key_splits > 1)
+                store_four(a.part + w.split * a.total_q * a.heads * a.dim + at + d0, v, a.dim - d0, VEC);
+            else
+                store_four((T *)a.dq + at + d0, v, a.dim - d0, VEC);
         }
     }
 }
 
 // dk, dv: four wavefronts of 16 KT keys each go over the queries of all heads that share the key head, BQ at a
-// time; dv = P^T do, dk = scale dS^T q.  With few tiles the heads are dealt to a.splits workgroups, whose sums a second launch adds.
+// time; dv = P^T do, dk = scale dS^T q.  With few tiles the steps are dealt to a.splits workgroups, whose sums a second launch adds.
 template <class T, int DP, int KT, bool VEC, int SHAPE>
 __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
 {
@@ -824,8 +919,6 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
     const int group = a.heads / a.kv_heads;
     const int share = (int)(blockIdx.x % a.splits), kv = (int)(blockIdx.x / a.splits % a.kv_heads);
     const long long tile = blockIdx.x / (a.splits * a.kv_heads);
-    // this workgroup's heads of the group
-    const int h_first = group * share / a.splits, h_count = group * (share + 1) / a.splits - h_first;
     const int p = set_of_tile(a.k_off, a.sets, BK, tile);
     const SetRange s = range_of(a, p);
     const long long b0 = (tile - (s.k0 / BK + p)) * BK;
@@ -862,7 +955,7 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
     float next_lse = 0.f, next_delta = 0.f;
     auto fetch = [&](int t, auto which) {
         char *lds = decltype(which)::value ? lds1 : lds0;
-        const int head = kv * group + h_first + t / each, i0 = begin + t % each * BQ;
+        const int head = kv * group + t / each, i0 = begin + t % each * BQ;
         const T *qp = (const T *)a.q + (s.q0 + i0) * a.q_token + head * a.q_head;
         const T *op = (const T *)a.d_o + ((s.q0 + i0) * a.heads + head) * a.dim;
         if (tid < BQ) {
@@ -882,7 +975,7 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
     };
     auto work = [&](int t, auto which) {
         const char *lds_q = decltype(which)::value ? lds1 : lds0, *lds_o = lds_q + BQ * L::PITCH;
-        const int head = kv * group + h_first + t / each;
+        const int head = kv * group + t / each;
         Scores<T, SHAPE> score;
         score.init(a, head);
         if (KT == 1 && w_last - 15 >= s.nk) return;   // short sets: no key of this wavefront, no query of the 32
@@ -938,15 +1031,14 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
             for (int d = 0; d < DT; ++d) {
                 const typename Frag<T>::type fo = L::columns(lds_o, h * 32, d * 16, lane);
                 const typename Frag<T>::type fq = L::columns(lds_q, h * 32, d * 16, lane);
-#pragma unroll
-                for (int u = 0; u < KT; ++u) {
-                    mma(dv[d][u], fo, fp[u]);
-                    mma(dk[d][u], fq, fs[u]);
-                }
+                add_product<T>(dv[d], fo, fp);
+                add_product<T>(dk[d], fq, fs);
             }
         }
     };
-    two_buffers(h_count * each, fetch, landed, work);
+    // this workgroup's share of the steps
+    const long long steps = (long long)group * each;
+    two_buffers((int)(steps * share / a.splits), (int)(steps * (share + 1) / a.splits), fetch, landed, work);
     settle_loop();
     const float rest = Scores<T, SHAPE>().rest(a);
 #pragma unroll
@@ -959,8 +1051,8 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
             if (d0 >= a.dim) continue;
             if (a.splits > 1) {
                 const long long all = a.total_k * a.kv_heads * a.dim;
-                store_four(a.part_kv + 2 * share * all + at + d0, dk[d][u] * rest, a.dim - d0, VEC);
-                store_four(a.part_kv + (2 * share + 1) * all + at + d0, dv[d][u], a.dim - d0, VEC);
+                store_four(a.part + 2 * share * all + at + d0, dk[d][u] * rest, a.dim - d0, VEC);
+                store_four(a.part + (2 * share + 1) * all + at + d0, dv[d][u], a.dim - d0, VEC);
             } else {
                 store_four((T *)a.dk + at + d0, dk[d][u] * rest, a.dim - d0, VEC);
                 store_four((T *)a.dv + at + d0, dv[d][u], a.dim - d0, VEC);
@@ -969,25 +1061,25 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
     }
 }
 
-// dk and dv from the sums of `splits` workgroups, in their order: a thread adds four values
+// A gradient (blockIdx.y = 0, 1: of two) from the sums of `splits` workgroups, in their order: a thread adds four values of the
+// `width` of a token.  Tokens in no set are not written.
 template <class T>
-__global__ __launch_bounds__(256) void attention_add_kernel(AttentionArgs a, int whole)
+__global__ __launch_bounds__(256) void attention_add_kernel(const float *part, int splits, long long tokens, long long width,
+                                                            const int64_t *off, int sets, T *out0, T *out1, int whole)
 {
-    const long long all = a.total_k * a.kv_heads * a.dim, fours = (all + 3) / 4;
-    const long long begin = a.k_off[0] < 0 ? 0 : a.k_off[0], end = a.k_off[a.sets] < a.total_k ? a.k_off[a.sets] : a.total_k;
-    const long long width = (long long)a.kv_heads * a.dim;
-    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < 2 * fours; t += (long long)gridDim.x * 256) {
-        const int which = t >= fours;
-        const long long i = (t - which * fours) * 4;
-        T *out = (T *)(which ? a.dv : a.dk);
+    const long long all = tokens * width, stride = all * gridDim.y, fours = (all + 3) / 4;
+    const long long begin = off[0] < 0 ? 0 : off[0] * width, end = (off[sets] < tokens ? off[sets] : tokens) * width;
+    T *out = blockIdx.y ? out1 : out0;
+    part += blockIdx.y * all;
+    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < fours; t += (long long)gridDim.x * 256) {
+        const long long i = t * 4;
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < a.splits; ++s)
-            v += load_four(a.part_kv + (2 * s + which) * all + i, all - i < 4 ? (int)(all - i) : 4, whole);
-        if (i >= begin * width && i + 4 <= end * width) {
+        for (int s = 0; s < splits; ++s) v += load_four(part + s * stride + i, all - i < 4 ? (int)(all - i) : 4, whole);
+        if (i >= begin && i + 4 <= end) {
             store_four(out + i, v, 4, whole);
-        } else {   // keys in no set are not written
+        } else {
             for (int e = 0; e < 4; ++e)
-                if (i + e >= begin * width && i + e < end * width) out[i + e] = (T)v[e];
+                if (i + e >= begin && i + e < end) out[i + e] = (T)v[e];
         }
     }
 }

@@ -13,8 +13,8 @@ static bool attention_desc_fits(const lcn_attention_desc *d)
     const int64_t strides[6] = {d->q_token, d->q_head, d->k_token, d->k_head, d->v_token, d->v_head};
     for (int i = 0; i < 6; ++i)
         if (strides[i] < 0 || strides[i] > (1 << 22)) return false;
-    // a launch has a workgroup per tile of 64 tokens and head
-    if ((d->total_q / 64 + d->num_sets) * (int64_t)d->heads > 0x7fffffff) return false;
+    // a launch has a workgroup per tile of 64 tokens and head (split only where there are few), or a wavefront per token and head
+    if ((d->total_q / 64 + d->num_sets) * (int64_t)d->heads > 0x7fffffff || d->total_q * d->heads / 4 > 0x7ffffff0) return false;
     if ((d->total_k / 64 + d->num_sets) * (int64_t)d->heads > 0x7fffffff) return false;
     return d->num_sets == 0 || (d->q_off && d->k_off);
 }
@@ -74,39 +74,57 @@ static int chunk_of(const lcn_attention_desc *d)
     const int64_t chunk = (keys + 127) / 128 * 128;
     return (int)(chunk < 128 ? 128 : chunk > 2048 ? 2048 : chunk);
 }
-struct ChunkSpace {
-    int chunk, rows;
-    float *part_o;
-    float2 *part_ml;
+// Into how many workgroups a tile's other side is split so that there are some 512 of them: `tiles` there are, `length` is the
+// average length of a set's other side, and a share has at least 256 of it (4 sets of 145 queries and 4300 keys, 2 float
+// heads of 32, forward and all gradients: 119 us, with whole tiles 556 us).
+static int shares(int64_t tiles, int64_t length)
+{
+    const int64_t wanted = tiles > 0 ? (512 + tiles - 1) / tiles : 1, most = length / 256;
+    const int64_t n = wanted < most ? wanted : most;
+    return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+}
+static int key_splits(const lcn_attention_desc *d)
+{
+    if (d->num_sets == 0) return 1;
+    const int64_t tiles = (d->total_q / 128 + d->num_sets) * d->heads;
+    return shares(tiles, d->total_k / d->num_sets);
+}
+// dk and dv: twice as many, since the query heads of a key head are its other side as well, and a causal set's first
+// keys have twice the average length
+static int query_splits(const lcn_attention_desc *d)
+{
+    if (d->num_sets == 0) return 1;
+    const int64_t tiles = (d->total_k / 128 + d->num_sets) * d->kv_heads;
+    return shares((tiles + 1) / 2, d->total_q / d->num_sets * (d->heads / d->kv_heads));
+}
+
+struct ForwardSpace {
+    int chunk, rows, key_splits;
+    float *part;
+    float2 *part_top;
     size_t bytes;
 };
-static ChunkSpace chunk_space(char *ws, const lcn_attention_desc *d)
+static ForwardSpace forward_space(char *ws, const lcn_attention_desc *d)
 {
     Carver c{ws};
-    ChunkSpace f{};
+    ForwardSpace f{};
     f.chunk = chunk_of(d);
+    f.key_splits = 1;
+    size_t n = 0;
     if (f.chunk) {
         f.rows = (int)(d->max_q * (d->heads / d->kv_heads));
-        const size_t n = (size_t)(d->total_k / f.chunk + d->num_sets) * d->kv_heads * f.rows;
-        f.part_o = (float *)c.take(n * d->head_dim * 4);
-        f.part_ml = (float2 *)c.take(n * 8);
+        n = (size_t)(d->total_k / f.chunk + d->num_sets) * d->kv_heads * f.rows;
+    } else if ((f.key_splits = key_splits(d)) > 1) {
+        n = (size_t)f.key_splits * d->total_q * d->heads;
     }
+    f.part = (float *)c.take(n * d->head_dim * 4);
+    f.part_top = (float2 *)c.take(n * 8);
     f.bytes = c.used;
     return f;
 }
-
-// Workgroups that share the query heads of a key head in the dk, dv kernel: enough for four times the compute units (a causal
-// set's first keys take twice the average time, and sets differ), since the sums of each are written and read once more.
-static int kv_splits(const lcn_attention_desc *d)
-{
-    const int64_t tiles = (d->total_k / 128 + d->num_sets) * d->kv_heads;
-    const int group = d->heads / d->kv_heads;
-    const int64_t wanted = (1024 + tiles - 1) / tiles;
-    return (int)(wanted < group ? wanted : group);
-}
 struct GradSpace {
-    float *delta, *part_kv;
-    int splits;
+    float *delta, *part;   // part: for dq, then for dk and dv
+    int key_splits, splits;
     size_t bytes;
 };
 static GradSpace grad_space(char *ws, const lcn_attention_desc *d)
@@ -114,8 +132,11 @@ static GradSpace grad_space(char *ws, const lcn_attention_desc *d)
     Carver c{ws};
     GradSpace f;
     f.delta = (float *)c.take((size_t)d->heads * (size_t)d->total_q * 4);
-    f.splits = d->num_sets ? kv_splits(d) : 1;
-    f.part_kv = (float *)c.take(f.splits > 1 ? (size_t)f.splits * 2 * (size_t)d->total_k * d->kv_heads * d->head_dim * 4 : 0);
+    f.key_splits = key_splits(d);
+    f.splits = query_splits(d);
+    const size_t q = f.key_splits > 1 ? (size_t)f.key_splits * d->total_q * d->heads : 0;
+    const size_t k = f.splits > 1 ? (size_t)f.splits * 2 * d->total_k * d->kv_heads : 0;
+    f.part = (float *)c.take((q > k ? q : k) * d->head_dim * 4);
     f.bytes = c.used;
     return f;
 }
@@ -129,7 +150,7 @@ extern "C" {
 lcn_status lcn_attention_workspace_bytes(const lcn_attention_desc *desc, int32_t backward, size_t *bytes)
 {
     if (!bytes || !attention_desc_fits(desc)) return LCN_ERR_INVALID_ARG;
-    *bytes = backward ? grad_space(nullptr, desc).bytes : chunk_space(nullptr, desc).bytes;
+    *bytes = backward ? grad_space(nullptr, desc).bytes : forward_space(nullptr, desc).bytes;
     return LCN_OK;
 }
 
@@ -145,19 +166,22 @@ lcn_status lcn_attention(const lcn_attention_desc *desc, const void *q, const vo
     const void *more[1] = {o};
     const bool vec = pieces(a, desc->dtype == LCN_F32 ? 4 : 2, more, 1);
     const int shape = shape_of(a);
-    const ChunkSpace f = chunk_space((char *)workspace, desc);
+    const ForwardSpace f = forward_space((char *)workspace, desc);
+    if (f.bytes && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < f.bytes)) return LCN_ERR_ALLOC;
+    a.key_splits = f.key_splits;
     if (f.chunk) {
-        if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < f.bytes) return LCN_ERR_ALLOC;
         a.chunk = f.chunk;
         a.rows = f.rows;
-        a.part_o = f.part_o;
-        a.part_ml = f.part_ml;
+        a.part = f.part;
+        a.part_top = f.part_top;
         if (desc->dtype == LCN_F32)
             OPCHK(attention_by_chunks<float>(a, vec, shape, (hipStream_t)hip_stream));
         else
             OPCHK(attention_by_chunks<__bf16>(a, vec, shape, (hipStream_t)hip_stream));
         return LCN_OK;
     }
+    a.part = f.part;
+    a.part_top = f.part_top;
     if (desc->dtype == LCN_F32)
         OPCHK(attention_forward<float>(a, vec, shape, (hipStream_t)hip_stream));
     else
@@ -181,8 +205,9 @@ lcn_status lcn_attention_backward(const lcn_attention_desc *desc, const void *q,
     a.o = const_cast<void *>(o);
     a.lse_in = lse;
     a.delta = f.delta;
+    a.key_splits = f.key_splits;
     a.splits = f.splits;
-    a.part_kv = f.part_kv;
+    a.part = f.part;
     a.dq = dq;
     a.dk = dk;
     a.dv = dv;

@@ -16,7 +16,7 @@ static hipError_t forward_one(AttentionArgs a, hipStream_t s)
 {
     const long long tiles = tiles_of(a.total_q, a.sets, 64 * QT);
     a.tiles = (int)tiles;
-    hipLaunchKernelGGL((attention_forward_kernel<T, DP, QT, VEC, SHAPE>), dim3((unsigned)(tiles * a.heads)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((attention_forward_kernel<T, DP, QT, VEC, SHAPE>), dim3((unsigned)(tiles * a.heads * a.key_splits)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 template <class T, int DP, int QT, bool DQ, bool VEC, int SHAPE>
@@ -25,7 +25,7 @@ static hipError_t backward_one(AttentionArgs a, hipStream_t s)
     if constexpr (DQ) {
         const long long tiles = tiles_of(a.total_q, a.sets, 64 * QT);
         a.tiles = (int)tiles;
-        hipLaunchKernelGGL((attention_dq_kernel<T, DP, QT, VEC, SHAPE>), dim3((unsigned)(tiles * a.heads)), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((attention_dq_kernel<T, DP, QT, VEC, SHAPE>), dim3((unsigned)(tiles * a.heads * a.key_splits)), dim3(256), 0, s, a);
     } else {
         const long long tiles = tiles_of(a.total_k, a.sets, 64 * QT);
         a.tiles = (int)tiles;
@@ -72,7 +72,10 @@ static hipError_t by_size(const AttentionArgs &a, bool vec, int shape, hipStream
 template <class T>
 hipError_t attention_forward(AttentionArgs a, bool vec, int shape, hipStream_t s)
 {
-    return by_size<T, FORWARD>(a, vec, shape, s);
+    const hipError_t e = by_size<T, FORWARD>(a, vec, shape, s);
+    if (e != hipSuccess || a.key_splits == 1) return e;
+    hipLaunchKernelGGL(attention_join_splits_kernel<T>, dim3((unsigned)((a.total_q * a.heads + 3) / 4)), dim3(256), 0, s, a);
+    return hipGetLastError();
 }
 template <class T, int DP, int QT>
 static hipError_t chunks_one(const AttentionArgs &a, bool vec, int shape, hipStream_t s)
@@ -104,11 +107,22 @@ hipError_t attention_by_chunks(AttentionArgs a, bool vec, int shape, hipStream_t
     return hipGetLastError();
 }
 template <class T>
+static hipError_t add_sums(const AttentionArgs &a, int splits, long long tokens, long long width, const int64_t *off, void *out0,
+                           void *out1, bool whole, hipStream_t s)
+{
+    const long long groups = (tokens * width / 4 + 255) / 256 + 1;
+    hipLaunchKernelGGL(attention_add_kernel<T>, dim3((unsigned)(groups < 4096 ? groups : 4096), out1 ? 2 : 1), dim3(256), 0, s,
+                       a.part, splits, tokens, width, off, a.sets, (T *)out0, (T *)out1, whole ? 1 : 0);
+    return hipGetLastError();
+}
+template <class T>
 hipError_t attention_backward(AttentionArgs a, bool vec, int shape, hipStream_t s)
 {
     hipError_t e = hipSuccess;
     if (a.total_q > 0 && a.dq) {
         e = by_size<T, GRAD_Q>(a, vec, shape, s);
+        if (e == hipSuccess && a.key_splits > 1)
+            e = add_sums<T>(a, a.key_splits, a.total_q, (long long)a.heads * a.dim, a.q_off, a.dq, nullptr, vec, s);
     } else if (a.total_q > 0) {
         const long long rows = a.total_q * a.heads;
         hipLaunchKernelGGL(attention_delta_kernel<T>, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, s, (const T *)a.o,
@@ -118,9 +132,7 @@ hipError_t attention_backward(AttentionArgs a, bool vec, int shape, hipStream_t 
     if (e != hipSuccess || !a.dk || a.total_k == 0) return e;
     e = by_size<T, GRAD_KV>(a, vec, shape, s);
     if (e != hipSuccess || a.splits == 1) return e;
-    const long long groups = (a.total_k * a.kv_heads * a.dim / 2 + 255) / 256;
-    hipLaunchKernelGGL(attention_add_kernel<T>, dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(256), 0, s, a, vec ? 1 : 0);
-    return hipGetLastError();
+    return add_sums<T>(a, a.splits, a.total_k, (long long)a.kv_heads * a.dim, a.k_off, a.dk, a.dv, vec, s);
 }
 
 }  // namespace lcn

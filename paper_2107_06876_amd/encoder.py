@@ -202,8 +202,6 @@ def _attention_desc(q, k, v, q_off, k_off, scale, causal, prefix, slopes, cap, m
     if q_off.dim() != 1 or q_off.shape[0] < 1:
         raise ValueError("q_off: expected num_sets + 1 offsets")
     sets = q_off.shape[0] - 1
-    if causal is False and prefix is not None:
-        raise ValueError("prefix: only a causal mask has one")
 
     def strides(t):   # of a dimension with one entry: any
         dense = t.shape[1] * t.shape[2]
@@ -232,7 +230,7 @@ def lcn_attention(q, k, v, q_off, k_off, scale=None, causal=False, prefix=None, 
                   workspace=None):
     """(o, lse): attention of the queries of every set to the keys of the same set.  q: (tokens, heads, dim), k and v:
     (tokens, key heads, dim), views with strides are taken; q_off, k_off: int64 offsets of the sets on the device; scale:
-    1 / sqrt(dim) where None; prefix: int32 per set; slopes: float32 per head; max_q: the largest number of queries of
+    1 / sqrt(dim) where None; prefix: int32 per set (read if causal); slopes: float32 per head; max_q: the largest number of queries of
     a set, where known.  o is dense like q, lse float32 (heads, tokens); queries in no set are left as they are."""
     d = _attention_desc(q, k, v, q_off, k_off, scale, causal, prefix, slopes, cap, max_q)
     dev = q.device

@@ -200,6 +200,22 @@ def test_other_tokens_hold_anything(nq, dtype):
         assert torch.equal(dk[s], grads[1][s]) and torch.equal(dv[s], grads[2][s])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("how", [dict(), dict(causal=True, prefix=[900, 0]), dict(cap=5.0), dict(slopes=[0.01, 0.2], cap=60.0)])
+def test_few_tiles_over_long_sets(how, dtype):
+    """Few tiles: the keys of a query tile and the queries of a key tile are split over workgroups."""
+    check([150, 20], [3000, 1111], 2, 1, 32, dtype, **how)
+    check([2100, 700], [60, 500], 2, 2, 64, dtype, **how)
+
+
+def test_a_prefix_without_a_causal_mask_changes_nothing():
+    g = generator(30)
+    q, off_ = normal(g, 90, 2, 32), offsets([40, 50])
+    a = lcn.lcn_attention(q, q, q, off_, off_)
+    b = lcn.lcn_attention(q, q, q, off_, off_, prefix=torch.tensor([5, 7], dtype=torch.int32, device=DEV))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
 def test_differences():
     """<do, o> along a direction changes as the gradients say (central differences of the float path)."""
     g = generator(24)
@@ -278,7 +294,7 @@ def test_refusals():
     k = torch.ones(6, 2, 32, device=DEV)
     for bad in (dict(q=q.half()), dict(k=k.bfloat16()), dict(v=k[:5]), dict(q=q.transpose(1, 2)), dict(q=q[:, :3]), dict(q=q.cpu()),
                 dict(q_off=o.int()), dict(k_off=offsets([3, 3])), dict(slopes=torch.ones(3, device=DEV)), dict(q=q[0]),
-                dict(prefix=torch.ones(1, dtype=torch.int32, device=DEV)), dict(k=k[:1].expand(6, 2, 32))):
+                dict(prefix=torch.ones(2, dtype=torch.int32, device=DEV)), dict(k=k[:1].expand(6, 2, 32))):
         args = dict(dict(q=q, k=k, v=k, q_off=o, k_off=o), **bad)
         with pytest.raises(ValueError):
             lcn.lcn_attention(**args)
