@@ -372,7 +372,7 @@ static EntropySpace entropy_space(char *ws, int64_t rows, int32_t vocab, int32_t
     if (rows <= FEW_ROWS) {
         f.part = (float2 *)c.take((size_t)few_groups(vocab) * rows * 8);
     } else {
-        f.plan = plan_product(vocab, rows, dim, planes_of(dtype), false);
+        f.plan = plan_product(vocab, rows, dim, planes_of(dtype), false, false);
         f.part = (float2 *)c.take((size_t)((vocab + tile_m(f.plan.tile) - 1) / tile_m(f.plan.tile)) * rows * 8);
         f.xp = c.take(planes_bytes(rows, dim, planes_of(dtype)));
         f.wp = c.take(planes_bytes(vocab, dim, planes_of(dtype)));
@@ -400,9 +400,9 @@ static EntropyBackward entropy_backward_space(char *ws, int64_t rows, int32_t vo
     int64_t piece = ((vocab + pieces - 1) / pieces + 255) & ~(int64_t)255;   // pieces of about one size
     if (piece > vocab) piece = vocab;
     b.piece = (int32_t)piece;
-    b.scores = plan_product(piece, rows, dim, planes_of(dtype), false);
-    b.dx = plan_product(dim, rows, piece, planes, true);
-    b.dw = plan_product(dim, piece, rows, planes, true);
+    b.scores = plan_product(piece, rows, dim, planes_of(dtype), false, false);
+    b.dx = plan_product(dim, rows, piece, planes, true, true);
+    b.dw = plan_product(dim, piece, rows, planes, true, true);
     b.xp = c.take(planes_bytes(rows, dim, planes_of(dtype)));
     b.xz = c.take(planes_bytes(rows, dim, planes_of(dtype)));
     b.wp = c.take(planes_bytes(vocab, dim, planes_of(dtype)));

@@ -288,7 +288,7 @@ static LinearForward linear_forward_space(char *ws, int64_t rows, int32_t d_in, 
 {
     Carver c{ws};
     LinearForward f;
-    f.plan = plan_product(d_out, rows, d_in, planes_of(dtype), true);
+    f.plan = plan_product(d_out, rows, d_in, planes_of(dtype), true, true);
     f.xp = c.take(planes_bytes(rows, d_in, planes_of(dtype)));
     f.wp = c.take(planes_bytes(d_out, d_in, planes_of(dtype)));
     f.part = (float *)c.take(partial_bytes(f.plan, d_out, rows));
@@ -308,8 +308,8 @@ static LinearBackward linear_backward_space(char *ws, int64_t rows, int32_t d_in
     Carver c{ws};
     LinearBackward b;
     b.planes = gradient_planes(rows, dtype);
-    b.dx = plan_product(d_in, rows, d_out, b.planes, true);
-    b.dw = plan_product(d_in, d_out, rows, b.planes, true);
+    b.dx = plan_product(d_in, rows, d_out, b.planes, true, true);
+    b.dw = plan_product(d_in, d_out, rows, b.planes, true, true);
     // enough workgroups to fill the chip, at most 256 partial sums per column
     b.rows_each = (int)((((rows + 255) / 256) + 31) & ~31LL);
     b.groups = (int)((rows + b.rows_each - 1) / b.rows_each);

@@ -109,7 +109,10 @@ hipError_t launch_add_partials(const float *part, int splits, long long n, int m
 // that the shape reaches on large products (bf16: 256 x 256 1.25 PFLOP/s, 128 x 128 1.1, 64 x 64 0.7; three planes, six
 // products counted: 256 x 128 1.4, 320 x 64 1.1, 128 x 128 1.03, 64 x 64 1.2); two steps stand for a workgroup's start and epilogue; the chip takes 256 workgroups of the large shapes at a
 // time and several times as many small ones; the partial sums of a split are written and read once at the rate of memory.
-ProductPlan plan_product(long long m, long long n, long long k, int planes, bool may_split)
+//
+// Columns behind the last whole tile cost a tile's time, and often a round of them: where that is estimated to be more than
+// 3 us and a launch of 64 x 64 tiles, they get that (a bf16 training step of 16391 rows, 1024 to 4096: 711 us, else 784).
+ProductPlan plan_product(long long m, long long n, long long k, int planes, bool may_split, bool may_tail)
 {
     struct Shape {
         int resident;
@@ -119,24 +122,30 @@ ProductPlan plan_product(long long m, long long n, long long k, int planes, bool
     static const Shape three[TILE_COUNT] = {{1, 2.3}, {1, 1.56}, {3, 1.0}, {1, 1.81}};
     const Shape *shape = planes == 3 ? three : one;
     const long long steps = planes == 3 ? (k + 31) / 32 : (k + 63) / 64 * planes;
-    ProductPlan best{TILE_256, 1};
+    auto launch_us = [&](int t, long long columns, int splits) {
+        const int bm = tile_m(t), bn = tile_n(t, planes);
+        const long long groups = ((m + bm - 1) / bm) * ((columns + bn - 1) / bn) * splits, room = 256 * shape[t].resident;
+        const double rounds = (double)((groups + room - 1) / room);
+        double us = rounds * shape[t].step_us * ((double)((steps + splits - 1) / splits) + 2.0);
+        if (groups < room) {   // fewer to share a compute unit with
+            const double share = (double)((groups + 255) / 256) / shape[t].resident;
+            us *= share > 0.5 ? share : 0.5 + 0.5 * share;
+        }
+        return us;
+    };
+    ProductPlan best{TILE_256, 1, false};
     double least = 1e300;
     for (int t = 0; t < TILE_COUNT; ++t) {
-        const int bm = tile_m(t), bn = tile_n(t, planes);
-        const long long tiles = ((m + bm - 1) / bm) * ((n + bn - 1) / bn);
+        const long long rest = n % tile_n(t, planes);
         for (int splits = 1; splits <= 64; splits += splits < 16 ? 1 : 16) {
             if (splits > 1 && (!may_split || steps / splits < 4)) break;
-            const long long groups = tiles * splits, room = 256 * shape[t].resident;
-            const double rounds = (double)((groups + room - 1) / room);
-            double us = rounds * shape[t].step_us * ((double)((steps + splits - 1) / splits) + 2.0);
-            if (groups < room) {   // fewer to share a compute unit with
-                const double share = (double)((groups + 255) / 256) / shape[t].resident;
-                us *= share > 0.5 ? share : 0.5 + 0.5 * share;
-            }
-            if (splits > 1) us += 3.0 + (double)splits * m * n * 8e-6 / 4.0;
-            if (us < least) {
-                least = us;
-                best = ProductPlan{t, splits};
+            for (int tail = 0; tail <= (may_tail && t != TILE_64 && rest && n > rest ? 1 : 0); ++tail) {
+                double us = tail ? launch_us(t, n - rest, splits) + 3.0 + launch_us(TILE_64, rest, splits) : launch_us(t, n, splits);
+                if (splits > 1) us += 3.0 + (double)splits * m * n * 8e-6 / 4.0;
+                if (us < least) {
+                    least = us;
+                    best = ProductPlan{t, splits, tail != 0};
+                }
             }
         }
     }

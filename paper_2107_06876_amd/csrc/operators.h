@@ -203,8 +203,9 @@ hipError_t launch_add_partials(const float *part, int splits, long long n, int m
 struct ProductPlan {
     int tile;      // index of the tile shape, see launch_planned
     int splits;
+    bool tail;     // columns behind the last whole tile: by small tiles, in a launch of their own
 };
-ProductPlan plan_product(long long m, long long n, long long k, int planes, bool may_split);
+ProductPlan plan_product(long long m, long long n, long long k, int planes, bool may_split, bool may_tail);
 
 // A float product's partial sums: [split][n][ldp]; `add` adds to what is there.
 struct PartialEpilogue {
@@ -283,24 +284,36 @@ inline int tile_n(int tile, int planes)
     return tile == TILE_256 ? 256 : tile == TILE_64 ? 64 : 128;
 }
 template <int NP, bool ACOL, bool BCOL, class Epi>
-hipError_t launch_planned(const ProductPlan &plan, ProductArgs p, const typename Epi::Args &e, hipStream_t s)
+hipError_t launch_tiles(int tile, const ProductArgs &p, const typename Epi::Args &e, hipStream_t s)
 {
-    p.splits = plan.splits;
     if constexpr (NP == 3) {
-        switch (plan.tile) {
+        switch (tile) {
         case TILE_256: return launch_product<256, 128, 32, 4, 2, 3, ACOL, BCOL, Epi>(p, e, s);
         case TILE_320: return launch_product<320, 64, 32, 4, 2, 3, ACOL, BCOL, Epi>(p, e, s);
         case TILE_128: return launch_product<128, 128, 32, 2, 2, 3, ACOL, BCOL, Epi>(p, e, s);
         default: return launch_product<64, 64, 32, 2, 2, 3, ACOL, BCOL, Epi>(p, e, s);
         }
     } else {
-        switch (plan.tile) {
+        switch (tile) {
         case TILE_256: return launch_product<256, 256, 64, 2, 4, 1, ACOL, BCOL, Epi>(p, e, s);
         case TILE_320: return launch_product<320, 128, 64, 4, 2, 1, ACOL, BCOL, Epi>(p, e, s);
         case TILE_128: return launch_product<128, 128, 64, 2, 2, 1, ACOL, BCOL, Epi>(p, e, s);
         default: return launch_product<64, 64, 64, 2, 2, 1, ACOL, BCOL, Epi>(p, e, s);
         }
     }
+}
+template <int NP, bool ACOL, bool BCOL, class Epi>
+hipError_t launch_planned(const ProductPlan &plan, ProductArgs p, const typename Epi::Args &e, hipStream_t s)
+{
+    const int whole = p.n - p.n % tile_n(plan.tile, NP);
+    p.splits = plan.splits;
+    p.n_first = 0;
+    p.n_last = plan.tail && whole ? whole : p.n;
+    const hipError_t st = launch_tiles<NP, ACOL, BCOL, Epi>(plan.tile, p, e, s);
+    if (st != hipSuccess || p.n_last == p.n) return st;
+    p.n_first = whole;
+    p.n_last = p.n;
+    return launch_tiles<NP, ACOL, BCOL, Epi>(TILE_64, p, e, s);
 }
 
 // out[n][m] = scale * product, in one launch or as partial sums in `part` that a second launch adds up.

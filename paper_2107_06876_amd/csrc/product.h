@@ -38,6 +38,7 @@ struct ProductArgs {
     int planes;          // 1; 2: two of the second operand; 3: three of both
     int splits;          // workgroups that share a tile's k
     int tiles_m, tiles_n;
+    int n_first, n_last;   // the columns of a launch
 };
 
 typedef __attribute__((address_space(3))) void lds_void;
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs p, 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int tm, tn;
     tile_of(p, blockIdx.x, tm, tn);
-    const long long m0 = (long long)tm * BM, n0 = (long long)tn * BN;
+    const long long m0 = (long long)tm * BM, n0 = p.n_first + (long long)tn * BN;
     const int wm = (wave % WM) * (BM / WM), wn = (wave / WM) * (BN / WN);
 
     const int at_a = fragment_place<BM, BK, ACOL>(lane), at_b = fragment_place<BN, BK, BCOL>(lane);
@@ -321,7 +322,7 @@ template <int BM, int BN, int BK, int WM, int WN, int NP, bool ACOL, bool BCOL, 
 hipError_t launch_product(ProductArgs p, const typename Epi::Args &e, hipStream_t s)
 {
     p.tiles_m = (p.m + BM - 1) / BM;
-    p.tiles_n = (p.n + BN - 1) / BN;
+    p.tiles_n = (p.n_last - p.n_first + BN - 1) / BN;
     hipLaunchKernelGGL((product_kernel<BM, BN, BK, WM, WN, NP, ACOL, BCOL, Epi>), dim3((unsigned)(p.tiles_m * p.tiles_n), p.splits),
                        dim3(WM * WN * 64), 0, s, p, e);
     return hipGetLastError();
