@@ -390,7 +390,7 @@ typedef enum { LCN_ACT_NONE = 0, LCN_ACT_TANH = 1, LCN_ACT_RELU = 2, LCN_ACT_GEL
  * d_out.  pre (nullable): the fp32 values z = x W^T + bias for the backward pass,
  * rows x d_out.  GELU is z Phi(z) with the error function, SILU z / (1 + e^-z).
  * Sizes: 0 <= rows <= 2^30, 1 <= d_in, d_out <= 2^20.  Up to 8 rows need no
- * workspace. */
+ * workspace, nor do narrow layers (the call says 0 bytes). */
 lcn_status lcn_linear_workspace_bytes(int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype, int32_t backward,
                                       size_t *bytes);
 lcn_status lcn_linear(const void *x, const void *W, const void *bias, const void *residual, int64_t rows, int32_t d_in,

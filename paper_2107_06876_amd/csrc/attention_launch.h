@@ -8,9 +8,6 @@ namespace lcn {
 // Tiles of B tokens that sets with `total` tokens can have (see set_of_tile).
 inline long long tiles_of(long long total, int sets, int B) { return total / B + sets; }
 
-// Sets of up to 64 tokens on average: wavefronts of 16 instead of 32 queries (or keys) each, so that a set fills a workgroup.
-inline bool short_sets(long long total, int sets) { return total <= 64LL * sets; }
-
 template <class T, int DP, int QT, bool VEC, int SHAPE>
 static hipError_t forward_one(AttentionArgs a, hipStream_t s)
 {
@@ -54,19 +51,31 @@ static hipError_t by_form(const AttentionArgs &a, bool vec, int shape, hipStream
     }
     return one<T, DP, QT, WHAT, true, SHAPED>(a, s);
 }
+// A wavefront has 16 or 32 queries (dk and dv: keys).  32 halve the reads of LDS, 16 take half of the registers, so that two
+// wavefronts share a SIMD, fill a tile of half the size and leave out what lies behind a short set's end.  Measured, 16 / 32,
+// four heads of 32, 64, 128 on sets of 500 tokens and of 2000 (some 32 000 in all), us:
+//   dk, dv bf16   saves 12, 53, 0 / 76, 166, 0 of the whole backward pass    -> always 16
+//   dk, dv float  saves 67, 112, 122 / 189, 195, -205                         -> 32 for wide heads in long sets alone
+//   dq bf16       saves 8, 13, -7 / 8, 0, -79; float 41, 86, 122 / 20, 39, -131   -> wide heads: 32 in long sets
+//   forward bf16  33, 46, 84 / 32, 49, 74 and 95, 138, 262 / 76, 115, 178; float 98, 190, 462 / 118, 247, 452 and
+//                 346, 712, 1706 / 339, 725, 1357                              -> 32 in long sets, bf16 wide heads from 65 on
 template <class T, int WHAT>
 static hipError_t by_size(const AttentionArgs &a, bool vec, int shape, hipStream_t s)
 {
-    const bool few = WHAT == GRAD_KV ? short_sets(a.total_k, a.sets) : short_sets(a.total_q, a.sets);
-    // wide bf16 heads: with 16 keys a wavefront two share a SIMD (249 registers instead of 424), which is worth more than
-    // the fewer reads of LDS (packed documents of 16 heads of 128: dk and dv in 745 instead of 827 us)
-    constexpr bool narrow_keys = WHAT == GRAD_KV && sizeof(T) == 2;
-    if (a.dim <= 32) return few ? by_form<T, 32, 1, WHAT>(a, vec, shape, s) : by_form<T, 32, 2, WHAT>(a, vec, shape, s);
-    if (a.dim <= 64) return few ? by_form<T, 64, 1, WHAT>(a, vec, shape, s) : by_form<T, 64, 2, WHAT>(a, vec, shape, s);
-    if constexpr (narrow_keys)
+    constexpr bool wide_type = sizeof(T) == 4;
+    const long long total = WHAT == GRAD_KV ? a.total_k : a.total_q;
+    const bool up_to_512 = total <= 512LL * a.sets, up_to_64 = total <= 64LL * a.sets;
+    if constexpr (WHAT != FORWARD) {
+        if (a.dim <= 32) return by_form<T, 32, 1, WHAT>(a, vec, shape, s);
+        if (a.dim <= 64) return by_form<T, 64, 1, WHAT>(a, vec, shape, s);
+    } else {
+        if (a.dim <= 32) return up_to_512 ? by_form<T, 32, 1, WHAT>(a, vec, shape, s) : by_form<T, 32, 2, WHAT>(a, vec, shape, s);
+        if (a.dim <= 64) return up_to_512 ? by_form<T, 64, 1, WHAT>(a, vec, shape, s) : by_form<T, 64, 2, WHAT>(a, vec, shape, s);
+    }
+    if constexpr (WHAT == GRAD_KV && !wide_type)
         return by_form<T, 128, 1, WHAT>(a, vec, shape, s);
     else
-        return few ? by_form<T, 128, 1, WHAT>(a, vec, shape, s) : by_form<T, 128, 2, WHAT>(a, vec, shape, s);
+        return (wide_type ? up_to_512 : up_to_64) ? by_form<T, 128, 1, WHAT>(a, vec, shape, s) : by_form<T, 128, 2, WHAT>(a, vec, shape, s);
 }
 
 template <class T>

@@ -107,7 +107,8 @@ hipError_t launch_add_partials(const float *part, int splits, long long n, int m
 
 // The tile shape and the split with the least estimated time.  A workgroup's step costs its tile's area at the rate
 // that the shape reaches on large products (bf16: 256 x 256 1.25 PFLOP/s, 128 x 128 1.1, 64 x 64 0.7; three planes, six
-// products counted: 256 x 128 1.4, 320 x 64 1.1, 128 x 128 1.03, 64 x 64 1.2); two steps stand for a workgroup's start and epilogue; the chip takes 256 workgroups of the large shapes at a
+// products counted: 256 x 128 1.4, 320 x 64 1.1, 128 x 128 0.92, 64 x 64 1.0); two steps stand for a workgroup's start and epilogue,
+// three where these are 256 x 128 in three planes; the chip takes 256 workgroups of the large shapes at a
 // time and several times as many small ones; the partial sums of a split are written and read once at the rate of memory.
 //
 // Columns behind the last whole tile cost a tile's time, and often a round of them: where that is estimated to be more than
@@ -119,14 +120,14 @@ ProductPlan plan_product(long long m, long long n, long long k, int planes, bool
         double step_us;   // of one workgroup's step with the chip full: 64 values of k, or 32 in three planes
     };
     static const Shape one[TILE_COUNT] = {{1, 1.8}, {2, 1.03}, {4, 0.77}, {1, 1.25}};
-    static const Shape three[TILE_COUNT] = {{1, 2.3}, {1, 1.56}, {3, 1.0}, {1, 1.81}};
+    static const Shape three[TILE_COUNT] = {{1, 2.3}, {1, 1.75}, {3, 1.2}, {1, 1.81}};
     const Shape *shape = planes == 3 ? three : one;
     const long long steps = planes == 3 ? (k + 31) / 32 : (k + 63) / 64 * planes;
     auto launch_us = [&](int t, long long columns, int splits) {
         const int bm = tile_m(t), bn = tile_n(t, planes);
         const long long groups = ((m + bm - 1) / bm) * ((columns + bn - 1) / bn) * splits, room = 256 * shape[t].resident;
         const double rounds = (double)((groups + room - 1) / room);
-        double us = rounds * shape[t].step_us * ((double)((steps + splits - 1) / splits) + 2.0);
+        double us = rounds * shape[t].step_us * ((double)((steps + splits - 1) / splits) + (planes == 3 && t == TILE_256 ? 3.0 : 2.0));
         if (groups < room) {   // fewer to share a compute unit with
             const double share = (double)((groups + 255) / 256) / shape[t].resident;
             us *= share > 0.5 ? share : 0.5 + 0.5 * share;
