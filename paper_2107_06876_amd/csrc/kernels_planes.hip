@@ -107,7 +107,7 @@ hipError_t launch_add_partials(const float *part, int splits, long long n, int m
 
 // The tile shape and the split with the least estimated time.  A workgroup's step costs its tile's area at the rate
 // that the shape reaches on large products (bf16: 256 x 256 1.25 PFLOP/s, 128 x 128 1.1, 64 x 64 0.7; three planes, six
-// products counted: 256 x 128 1.4, 320 x 64 1.1, 128 x 128 0.92, 64 x 64 1.0); two steps stand for a workgroup's start and epilogue,
+// products counted: 256 x 128 1.4, 320 x 64 1.1, 128 x 128 0.87, 64 x 64 1.0); two steps stand for a workgroup's start and epilogue,
 // three where these are 256 x 128 in three planes; the chip takes 256 workgroups of the large shapes at a
 // time and several times as many small ones; the partial sums of a split are written and read once at the rate of memory.
 //
@@ -120,7 +120,7 @@ ProductPlan plan_product(long long m, long long n, long long k, int planes, bool
         double step_us;   // of one workgroup's step with the chip full: 64 values of k, or 32 in three planes
     };
     static const Shape one[TILE_COUNT] = {{1, 1.8}, {2, 1.03}, {4, 0.77}, {1, 1.25}};
-    static const Shape three[TILE_COUNT] = {{1, 2.3}, {1, 1.75}, {3, 1.2}, {1, 1.81}};
+    static const Shape three[TILE_COUNT] = {{1, 2.3}, {1, 1.85}, {3, 1.2}, {1, 1.81}};
     const Shape *shape = planes == 3 ? three : one;
     const long long steps = planes == 3 ? (k + 31) / 32 : (k + 63) / 64 * planes;
     auto launch_us = [&](int t, long long columns, int splits) {

@@ -14,6 +14,11 @@
 // 128-bit reads of `rows` tiles nor the transposing 64-bit reads of `columns` tiles meet in a bank.
 //
 // The accumulators' row index (four consecutive values in a lane) is m: outputs are stored with m contiguous.
+//
+// Bound by the matrix instruction while k is long: 8192^3 in bf16 1.25 PFLOP/s (the library's product there 1.14), in three
+// planes 233 TFLOP/s of float products (library 154).  With short k the epilogue counts, which nothing overlaps (a
+// workgroup of the largest shape fills a compute unit): bf16, 16384 rows, 4096 -> 1024 values 1.3 PFLOP/s, 1024 -> 4096
+// 0.95, k = 300 0.72.  A resident workgroup that loads its next tile during the epilogue was 1 to 3 % faster and spilled; not kept.
 #pragma once
 
 #include <hip/hip_runtime.h>
