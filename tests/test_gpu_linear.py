@@ -76,6 +76,11 @@ def test_large_tiles(dtype):
     check(5000, 512, 2050, "silu", dtype)
 
 
+@pytest.mark.parametrize("rows,d_in,dtype", [(4103, 1024, BF16), (2053, 512, F32)])
+def test_rows_behind_the_last_large_tile(rows, d_in, dtype):
+    check(rows, d_in, 4096, "gelu", dtype)
+
+
 def test_values_of_every_size_in_float():
     """Products of float values from 1e-18 to 1e18 are as exact as in single precision; the largest ones do not overflow."""
     g = generator(11)
