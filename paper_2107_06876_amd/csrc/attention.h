@@ -29,6 +29,7 @@ struct AttentionArgs {
     int causal;
     float scale, cap;
     int tiles;                  // of queries (forward, dq) or keys (dk, dv), over all sets
+    unsigned groups;            // workgroups with work, see group_number()
     // forward
     void *o;                    // read in the backward pass
     float *lse;                 // [head][query]
@@ -229,10 +230,13 @@ __device__ __forceinline__ QueryTile query_tile(const AttentionArgs &a)
     const int group = a.heads / a.kv_heads;
     // Heads are numbered fastest: workgroups are dealt to the eight dies in turn, so a die has the same heads of all tiles, and
     // their keys in its cache, and long and short tiles alike.
-    w.head = (int)(blockIdx.x % a.heads);
+    const unsigned id = group_number();
+    w.any = false;
+    if (id >= a.groups) return w;
+    w.head = (int)(id % a.heads);
     w.kv = w.head / group;
-    w.split = (int)(blockIdx.x / a.heads % a.key_splits);
-    const long long tile = a.tiles - 1 - blockIdx.x / a.heads / a.key_splits;   // causal: the long ones first
+    w.split = (int)(id / a.heads % a.key_splits);
+    const long long tile = a.tiles - 1 - (long long)(id / a.heads / a.key_splits);   // causal: the long ones first
     const int p = set_of_tile(a.q_off, a.sets, BQ, tile);
     w.s = range_of(a, p);
     const long long b0 = (tile - (w.s.q0 / BQ + p)) * BQ;
@@ -468,7 +472,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
 template <class T>
 __global__ __launch_bounds__(256) void attention_join_splits_kernel(AttentionArgs a)
 {
-    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), n = row / a.heads, all = a.total_q * a.heads;
+    const long long row = (long long)group_number() * 4 + (threadIdx.x >> 6), n = row / a.heads, all = a.total_q * a.heads;
     const int head = (int)(row % a.heads), lane = threadIdx.x & 63;
     if (n >= a.total_q || n < a.q_off[0] || n >= a.q_off[a.sets]) return;
     float most = minus_infinity();
@@ -506,7 +510,8 @@ __global__ __launch_bounds__(WAVES * 64) void attention_chunk_kernel(AttentionAr
     static_assert(WAVES * BYTES >= WAVES * QT * DP * 16 * 4, "the wavefronts' sums fit");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
     const int group = a.heads / a.kv_heads;
-    const long long t = die_run(blockIdx.x, gridDim.x);
+    if (group_number() >= a.groups) return;
+    const long long t = die_run(group_number(), a.groups);
     const int kv = (int)(t / a.tiles);
     const long long tile = t % a.tiles;
     const int p = set_of_tile(a.k_off, a.sets, a.chunk, tile);
@@ -672,7 +677,7 @@ __global__ __launch_bounds__(WAVES * 64) void attention_chunk_kernel(AttentionAr
 template <class T>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a)
 {
-    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), n = row / a.heads;
+    const long long row = (long long)group_number() * 4 + (threadIdx.x >> 6), n = row / a.heads;
     const int head = (int)(row % a.heads), lane = threadIdx.x & 63, group = a.heads / a.kv_heads, kv = head / group;
     if (n >= a.total_q) return;
     const int p = last_set(a.sets, [&](int q) { return a.q_off[q] <= n; });
@@ -719,7 +724,7 @@ template <class T>
 __global__ __launch_bounds__(256) void attention_delta_kernel(const T *__restrict__ o, const T *__restrict__ d_o, long long total_q,
                                                               int heads, int dim, float *__restrict__ delta)
 {
-    const long long r = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
+    const long long r = (long long)group_number() * 16 + (threadIdx.x >> 4);
     if (r >= total_q * heads) return;
     float s = 0.f;
     for (int d = threadIdx.x & 15; d < dim; d += 16) s += (float)o[r * dim + d] * (float)d_o[r * dim + d];
@@ -924,8 +929,10 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
     __shared__ __align__(16) float lds_lse[2][BQ], lds_delta[2][BQ];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
     const int group = a.heads / a.kv_heads;
-    const int share = (int)(blockIdx.x % a.splits), kv = (int)(blockIdx.x / a.splits % a.kv_heads);
-    const long long tile = blockIdx.x / (a.splits * a.kv_heads);
+    const unsigned id = group_number();
+    if (id >= a.groups) return;
+    const int share = (int)(id % a.splits), kv = (int)(id / a.splits % a.kv_heads);
+    const long long tile = id / (a.splits * a.kv_heads);
     const int p = set_of_tile(a.k_off, a.sets, BK, tile);
     const SetRange s = range_of(a, p);
     const long long b0 = (tile - (s.k0 / BK + p)) * BK;

@@ -13,7 +13,7 @@ static bool attention_desc_fits(const lcn_attention_desc *d)
     const int64_t strides[6] = {d->q_token, d->q_head, d->k_token, d->k_head, d->v_token, d->v_head};
     for (int i = 0; i < 6; ++i)
         if (strides[i] < 0 || strides[i] > (1 << 22)) return false;
-    // a launch has a workgroup per tile of 64 tokens and head (split only where there are few), or a wavefront per token and head
+    // workgroups are numbered in 32 bits: one per tile of 64 tokens and head (split only where there are few), or a wavefront per token and head
     if ((d->total_q / 64 + d->num_sets) * (int64_t)d->heads > 0x7fffffff || d->total_q * d->heads / 4 > 0x7ffffff0) return false;
     if ((d->total_k / 64 + d->num_sets) * (int64_t)d->heads > 0x7fffffff) return false;
     return d->num_sets == 0 || (d->q_off && d->k_off);

@@ -13,7 +13,8 @@ static hipError_t forward_one(AttentionArgs a, hipStream_t s)
 {
     const long long tiles = tiles_of(a.total_q, a.sets, 64 * QT);
     a.tiles = (int)tiles;
-    hipLaunchKernelGGL((attention_forward_kernel<T, DP, QT, VEC, SHAPE>), dim3((unsigned)(tiles * a.heads * a.key_splits)), dim3(256), 0, s, a);
+    a.groups = (unsigned)(tiles * a.heads * a.key_splits);
+    hipLaunchKernelGGL((attention_forward_kernel<T, DP, QT, VEC, SHAPE>), grid_of(a.groups), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 template <class T, int DP, int QT, bool DQ, bool VEC, int SHAPE>
@@ -22,11 +23,13 @@ static hipError_t backward_one(AttentionArgs a, hipStream_t s)
     if constexpr (DQ) {
         const long long tiles = tiles_of(a.total_q, a.sets, 64 * QT);
         a.tiles = (int)tiles;
-        hipLaunchKernelGGL((attention_dq_kernel<T, DP, QT, VEC, SHAPE>), dim3((unsigned)(tiles * a.heads * a.key_splits)), dim3(256), 0, s, a);
+        a.groups = (unsigned)(tiles * a.heads * a.key_splits);
+        hipLaunchKernelGGL((attention_dq_kernel<T, DP, QT, VEC, SHAPE>), grid_of(a.groups), dim3(256), 0, s, a);
     } else {
         const long long tiles = tiles_of(a.total_k, a.sets, 64 * QT);
         a.tiles = (int)tiles;
-        hipLaunchKernelGGL((attention_dkv_kernel<T, DP, QT, VEC, SHAPE>), dim3((unsigned)(tiles * a.kv_heads * a.splits)), dim3(256), 0, s, a);
+        a.groups = (unsigned)(tiles * a.kv_heads * a.splits);
+        hipLaunchKernelGGL((attention_dkv_kernel<T, DP, QT, VEC, SHAPE>), grid_of(a.groups), dim3(256), 0, s, a);
     }
     return hipGetLastError();
 }
@@ -83,14 +86,14 @@ hipError_t attention_forward(AttentionArgs a, bool vec, int shape, hipStream_t s
 {
     const hipError_t e = by_size<T, FORWARD>(a, vec, shape, s);
     if (e != hipSuccess || a.key_splits == 1) return e;
-    hipLaunchKernelGGL(attention_join_splits_kernel<T>, dim3((unsigned)((a.total_q * a.heads + 3) / 4)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(attention_join_splits_kernel<T>, grid_of((a.total_q * a.heads + 3) / 4), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 template <class T, int DP, int QT>
 static hipError_t chunks_one(const AttentionArgs &a, bool vec, int shape, hipStream_t s)
 {
     constexpr int WAVES = DP * sizeof(T) > 256 ? 2 : 4;   // two buffers of each wavefront fit into LDS
-    const dim3 grid((unsigned)((long long)a.tiles * a.kv_heads)), block(WAVES * 64);
+    const dim3 grid = grid_of(a.groups), block(WAVES * 64);
     if (vec && shape == PLAIN)   // bound by memory: a cap needs no kernel of its own
         hipLaunchKernelGGL((attention_chunk_kernel<T, DP, QT, WAVES, true, PLAIN>), grid, block, 0, s, a);
     else if (vec)
@@ -110,9 +113,10 @@ template <class T>
 hipError_t attention_by_chunks(AttentionArgs a, bool vec, int shape, hipStream_t s)
 {
     a.tiles = (int)tiles_of(a.total_k, a.sets, a.chunk);
+    a.groups = (unsigned)((long long)a.tiles * a.kv_heads);
     hipError_t e = a.rows <= 16 ? chunks_by_dim<T, 1>(a, vec, shape, s) : chunks_by_dim<T, 2>(a, vec, shape, s);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)((a.total_q * a.heads + 3) / 4)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(attention_join_kernel<T>, grid_of((a.total_q * a.heads + 3) / 4), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 template <class T>
@@ -134,7 +138,7 @@ hipError_t attention_backward(AttentionArgs a, bool vec, int shape, hipStream_t 
             e = add_sums<T>(a, a.key_splits, a.total_q, (long long)a.heads * a.dim, a.q_off, a.dq, nullptr, vec, s);
     } else if (a.total_q > 0) {
         const long long rows = a.total_q * a.heads;
-        hipLaunchKernelGGL(attention_delta_kernel<T>, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, s, (const T *)a.o,
+        hipLaunchKernelGGL(attention_delta_kernel<T>, grid_of((rows + 15) / 16), dim3(256), 0, s, (const T *)a.o,
                            (const T *)a.d_o, a.total_q, a.heads, a.dim, a.delta);
         e = hipGetLastError();
     }

@@ -155,6 +155,16 @@ __device__ __forceinline__ float activate_slope(float z)
     return 1.f;
 }
 
+// ---- launches of many workgroups --------------------------------------------
+// A dimension of a grid has fewer than 2^32 threads; what is beyond is cut off without an error.  More workgroups than GRID_ROW
+// are laid out in rows of so many, which are numbered through (the last row may be longer than what is left).
+constexpr long long GRID_ROW = 1 << 22;
+inline dim3 grid_of(long long groups)
+{
+    return groups <= GRID_ROW ? dim3((unsigned)groups) : dim3((unsigned)GRID_ROW, (unsigned)((groups + GRID_ROW - 1) / GRID_ROW));
+}
+__device__ __forceinline__ unsigned group_number() { return blockIdx.y * gridDim.x + blockIdx.x; }
+
 // ---- planes (kernels_planes.hip) --------------------------------------------
 inline __host__ __device__ long long padded(long long d) { return (d + 7) & ~7LL; }
 inline int planes_of(int32_t dtype) { return dtype == LCN_F32 ? 3 : 1; }

@@ -306,3 +306,33 @@ def test_refusals():
     out, lse = lcn.lcn_attention(q, k, k, o, o)
     with pytest.raises(lcn.LcnError):
         lcn.lcn_attention_backward(q, k, k, out, lse, q, o, o, workspace=torch.empty(4, dtype=torch.uint8, device=DEV))
+
+
+def test_more_workgroups_than_a_launch_has_in_one_dimension():
+    """2^24 sets, nearly all empty: more than 2^32 threads."""
+    sets = 1 << 24
+    g = generator(35)
+    q, k, v, do = (normal(g, 300, 1, 32, dtype=BF16) for _ in range(4))
+    long_off = torch.zeros(sets + 1, dtype=torch.int64, device=DEV)
+    long_off[sets // 2 + 1:] = 100
+    long_off[sets:] = 300
+    short = offsets([100, 200])
+    want = lcn.lcn_attention(q, k, v, short, short)
+    got = lcn.lcn_attention(q, k, v, long_off, long_off)
+    for u, w in zip((*got, *lcn.lcn_attention_backward(q, k, v, *got, do, long_off, long_off)),
+                    (*want, *lcn.lcn_attention_backward(q, k, v, *want, do, short, short))):
+        assert torch.equal(u, w)
+
+
+def test_more_rows_to_join_than_a_launch_has_in_one_dimension():
+    """One query of 32 heads in each of more than 2^21 sets: the chunks of more than 2^26 rows are joined by a wavefront each."""
+    sets, heads, nk, dim = (1 << 21) + 77, 32, 128, 8
+    g = torch.Generator(device=DEV)
+    g.manual_seed(36)
+    q, k = (torch.randn(n, h, dim, generator=g, device=DEV, dtype=BF16) for n, h in ((sets, heads), (sets * nk, 1)))
+    steps = torch.arange(sets + 1, device=DEV)
+    o, lse = lcn.lcn_attention(q, k, k, steps, steps * nk, max_q=1)
+    for p in (0, 1, sets // 3, (1 << 21) - 1, 1 << 21, sets - 1):
+        part = slice(p * nk, (p + 1) * nk)
+        want = oracle(q[p:p + 1], k[part], k[part], q[p:p + 1], [1], [nk], dim ** -0.5)
+        assert off(o[p:p + 1], want[0]) <= bound(BF16, nk, 1) and off(lse[:, p:p + 1], want[1]) <= bound(F32, nk)
