@@ -389,7 +389,7 @@ typedef enum { LCN_ACT_NONE = 0, LCN_ACT_TANH = 1, LCN_ACT_RELU = 2, LCN_ACT_GEL
  * (nullable), residual rows x d_out (nullable; y may be the same memory), y rows x
  * d_out.  pre (nullable): the fp32 values z = x W^T + bias for the backward pass,
  * rows x d_out.  GELU is z Phi(z) with the error function, SILU z / (1 + e^-z).
- * Sizes: 0 <= rows <= 2^30, 1 <= d_in, d_out <= 2^20.  Up to 8 rows need no
+ * Sizes: 0 <= rows <= 2^30, 1 <= d_in, d_out <= 2^20, rows times either <= 2^42.  Up to 8 rows need no
  * workspace, nor do narrow layers (the call says 0 bytes). */
 lcn_status lcn_linear_workspace_bytes(int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype, int32_t backward,
                                       size_t *bytes);
@@ -411,8 +411,8 @@ lcn_status lcn_linear_backward(const void *x, const void *W, const float *pre, c
  * pairs under the row-normalised plan.  A row with a negative target has loss 0
  * (its lse is still formed) and adds nothing to any gradient, whatever its x
  * holds; a target >= vocab makes its loss NaN.  A bias of -inf takes a word out.
- * target: int64.  Sizes: 0 <= rows <= 2^30, 1 <= vocab <= 2^30, 1 <= dim <= 2^20;
- * scale finite. */
+ * target: int64.  Sizes: 0 <= rows <= 2^30, 1 <= vocab <= 2^30, 1 <= dim <= 2^20, the
+ * product of any two <= 2^42; scale finite. */
 lcn_status lcn_cross_entropy_workspace_bytes(int64_t rows, int32_t vocab, int32_t dim, int32_t dtype, int32_t backward,
                                              size_t *bytes);
 lcn_status lcn_cross_entropy(const void *x, const void *W, const float *bias, const int64_t *target, int64_t rows,

@@ -121,7 +121,7 @@ __global__ __launch_bounds__(256) void entropy_join_kernel(const float2 *__restr
 {
     __shared__ float2 sums[256];
     const int c = threadIdx.x % across, q = threadIdx.x / across, down = 256 / across;
-    const long long n = (long long)blockIdx.x * across + c;
+    const long long n = (long long)group_number() * across + c;
     float m = -__builtin_huge_valf(), s = 0.f;
     if (n < rows)
         for (int i = q; i < parts; i += down) {
@@ -348,7 +348,7 @@ constexpr size_t PIECE_BYTES = (size_t)128 << 20;
 static bool entropy_args_fit(int64_t rows, int32_t vocab, int32_t dim, int32_t dtype)
 {
     return rows >= 0 && rows <= MAX_ROWS && vocab >= 1 && vocab <= (int32_t)MAX_ROWS && dim >= 1 && dim <= MAX_WIDTH &&
-           (dtype == LCN_F32 || dtype == LCN_BF16);
+           sizes_fit(rows, vocab) && sizes_fit(rows, dim) && sizes_fit(vocab, dim) && (dtype == LCN_F32 || dtype == LCN_BF16);
 }
 static int few_groups(int32_t vocab)
 {
@@ -464,7 +464,7 @@ static lcn_status entropy_as(const T *x, const T *w, const float *bias, const in
         parts = (vocab + tile_m(f.plan.tile) - 1) / tile_m(f.plan.tile);
         across = 16;
     }
-    hipLaunchKernelGGL(entropy_join_kernel, dim3((unsigned)((rows + across - 1) / across)), dim3(256), 0, s, f.part, parts,
+    hipLaunchKernelGGL(entropy_join_kernel, grid_of((rows + across - 1) / across), dim3(256), 0, s, f.part, parts,
                        (long long)rows, e, f.at_target, loss, lse, across);
     OPCHK(hipGetLastError());
     return LCN_OK;

@@ -287,7 +287,7 @@ static hipError_t launch_narrow(const LinearArgs<T> &e, const T *x, const T *w, 
 static bool linear_args_fit(int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype)
 {
     return rows >= 0 && rows <= MAX_ROWS && d_in >= 1 && d_in <= MAX_WIDTH && d_out >= 1 && d_out <= MAX_WIDTH &&
-           (dtype == LCN_F32 || dtype == LCN_BF16);
+           sizes_fit(rows, d_in) && sizes_fit(rows, d_out) && (dtype == LCN_F32 || dtype == LCN_BF16);
 }
 
 struct LinearForward {

@@ -9,6 +9,9 @@ namespace lcn {
 // what the host takes for granted about sizes: offsets within a tile stay below 2^31 bytes
 constexpr int32_t MAX_WIDTH = 1 << 20;
 constexpr int64_t MAX_ROWS = (int64_t)1 << 30;
+// a product's tiles are numbered in 31 bits: 64 x 64 of them at least in a result of up to 2^42 values
+constexpr int64_t MAX_AREA = (int64_t)1 << 42;
+inline bool sizes_fit(int64_t a, int64_t b) { return a * b <= MAX_AREA; }
 
 template <class T>
 struct Four;   // four consecutive values, one load or store
@@ -154,16 +157,6 @@ __device__ __forceinline__ float activate_slope(float z)
     }
     return 1.f;
 }
-
-// ---- launches of many workgroups --------------------------------------------
-// A dimension of a grid has fewer than 2^32 threads; what is beyond is cut off without an error.  More workgroups than GRID_ROW
-// are laid out in rows of so many, which are numbered through (the last row may be longer than what is left).
-constexpr long long GRID_ROW = 1 << 22;
-inline dim3 grid_of(long long groups)
-{
-    return groups <= GRID_ROW ? dim3((unsigned)groups) : dim3((unsigned)GRID_ROW, (unsigned)((groups + GRID_ROW - 1) / GRID_ROW));
-}
-__device__ __forceinline__ unsigned group_number() { return blockIdx.y * gridDim.x + blockIdx.x; }
 
 // ---- planes (kernels_planes.hip) --------------------------------------------
 inline __host__ __device__ long long padded(long long d) { return (d + 7) & ~7LL; }

@@ -26,6 +26,16 @@
 
 namespace lcn {
 
+// ---- launches of many workgroups --------------------------------------------
+// A dimension of a grid has fewer than 2^32 threads; what is beyond is cut off without an error.  More workgroups than GRID_ROW
+// are laid out in rows of so many, which are numbered through (the last row may be longer than what is left).
+constexpr long long GRID_ROW = 1 << 22;
+inline dim3 grid_of(long long groups)
+{
+    return groups <= GRID_ROW ? dim3((unsigned)groups) : dim3((unsigned)GRID_ROW, (unsigned)((groups + GRID_ROW - 1) / GRID_ROW));
+}
+__device__ __forceinline__ unsigned group_number() { return blockIdx.y * gridDim.x + blockIdx.x; }
+
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -42,7 +52,7 @@ struct ProductArgs {
     int m, n, k;         // k is padded by zeros up to a multiple of 8 in `rows` operands
     int planes;          // 1; 2: two of the second operand; 3: three of both
     int splits;          // workgroups that share a tile's k
-    int tiles_m, tiles_n;
+    int tiles_m, tiles_n;   // their product is below 2^31 (sizes_fit)
     int n_first, n_last;   // the columns of a launch
 };
 
@@ -215,8 +225,10 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs p, 
     __shared__ __align__(1024) char lds0[TILE > ROWS ? TILE : ROWS];
     __shared__ __align__(1024) char lds1[TILE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const unsigned id = blockIdx.z * gridDim.x + blockIdx.x;   // y: splits
+    if (id >= (unsigned)(p.tiles_m * p.tiles_n)) return;
     int tm, tn;
-    tile_of(p, blockIdx.x, tm, tn);
+    tile_of(p, (int)id, tm, tn);
     const long long m0 = (long long)tm * BM, n0 = p.n_first + (long long)tn * BN;
     const int wm = (wave % WM) * (BM / WM), wn = (wave / WM) * (BN / WN);
 
@@ -328,8 +340,9 @@ hipError_t launch_product(ProductArgs p, const typename Epi::Args &e, hipStream_
 {
     p.tiles_m = (p.m + BM - 1) / BM;
     p.tiles_n = (p.n_last - p.n_first + BN - 1) / BN;
-    hipLaunchKernelGGL((product_kernel<BM, BN, BK, WM, WN, NP, ACOL, BCOL, Epi>), dim3((unsigned)(p.tiles_m * p.tiles_n), p.splits),
-                       dim3(WM * WN * 64), 0, s, p, e);
+    const dim3 tiles = grid_of((long long)p.tiles_m * p.tiles_n);
+    hipLaunchKernelGGL((product_kernel<BM, BN, BK, WM, WN, NP, ACOL, BCOL, Epi>), dim3(tiles.x, p.splits, tiles.y), dim3(WM * WN * 64),
+                       0, s, p, e);
     return hipGetLastError();
 }
 

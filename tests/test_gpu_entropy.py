@@ -211,3 +211,18 @@ def test_refusals():
             lcn.lcn_cross_entropy(x, w, t, scale=scale)
     with pytest.raises(lcn.LcnError):
         lcn.lcn_cross_entropy(x, w, t, workspace=torch.empty(8, dtype=torch.uint8, device=DEV))
+
+
+def test_more_tiles_than_a_launch_has_in_one_dimension():
+    """2^20 rows against more than 2^19 words: more than 2^32 threads in one launch of the scores' tiles."""
+    g = generator(42)
+    rows, vocab, dim = 1 << 20, (1 << 19) + 300, 8
+    x, w = normal(g, rows, dim, dtype=BF16), normal(g, vocab, dim, dtype=BF16)
+    t = torch.randint(0, vocab, (rows,), generator=g).to(DEV)
+    loss, lse = lcn.lcn_cross_entropy(x, w, t)
+    some = torch.tensor([0, 1, 255, 256, 70000, 524287, 524288, rows - 257, rows - 1], device=DEV)
+    z = x[some].double() @ w.double().t().contiguous()
+    want = torch.logsumexp(z, 1)
+    assert torch.isfinite(loss).all()
+    # 2049 tiles of 256 words: sums of 32-bit partial sums
+    assert off(lse[some], want) <= bound(F32, vocab) and off(loss[some], want - z.gather(1, t[some, None])[:, 0]) <= bound(F32, vocab)

@@ -129,3 +129,13 @@ def test_tensors_that_are_not_on_a_device():
     q, o = torch.ones(4, 2, 8), torch.tensor([0, 4])
     with pytest.raises(ValueError):
         lcn.lcn_attention(q, q, q, o, o)
+
+
+@pytest.mark.parametrize("rows,a,b", [(1 << 30, 8, (1 << 12) + 1), (1 << 30, (1 << 12) + 1, 8), (1 << 23, 16, 1 << 20)])
+def test_results_with_more_tiles_than_are_numbered(lib, rows, a, b):
+    for f in (lib.lcn_linear_workspace_bytes, lambda rows, a, b, *more: lib.lcn_cross_entropy_workspace_bytes(rows, b, a, *more)):
+        for backward in (0, 1):
+            assert _bytes(f, rows, a, b, BF16, backward)[0] == ERR_INVALID_ARG
+            assert _bytes(f, rows // 2, a, b // 2 + 1 if b > a else b, BF16, backward)[0] == OK
+    assert lib.lcn_linear(FAKE, FAKE, None, None, rows, a, b, BF16, 0, FAKE, None, FAKE, 1 << 62, None) == ERR_INVALID_ARG
+    assert lib.lcn_cross_entropy(FAKE, FAKE, None, FAKE, rows, b, a, BF16, 1.0, FAKE, FAKE, FAKE, 1 << 62, None) == ERR_INVALID_ARG
