@@ -17,7 +17,13 @@
 
 namespace lcn {
 
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float LOG2E = 1.4426950408889634f;
+
+// A score, and e^(z - m).  Forward and backward pass form scores by the same operations in the same order, and differences
+// before they change the unit: a target with all the weight has z = m = lse, loss 0 and P = 1 to the last bit, where lse times
+// log2(e) and back would leave 2^-24 of the score in either direction, a gradient without meaning.
+__device__ __forceinline__ float score(float dot, float scale, float bias) { return __builtin_fmaf(dot, scale, bias); }
+__device__ __forceinline__ float exp_of(float difference) { return exp2_fast(difference * LOG2E); }
 
 struct EntropyRow {
     const float *bias;        // nullable
@@ -26,12 +32,11 @@ struct EntropyRow {
     int vocab;
 };
 
-// Maxima are kept times log2(e).  Joins (m, s) with another pair: the sum of exponentials relative to the larger
-// maximum.  -inf: nothing yet.
+// Joins (m, s) with another pair: the sum of exponentials relative to the larger maximum.  -inf: nothing yet.
 __device__ __forceinline__ void join(float &m, float &s, float om, float os)
 {
     const float top = fmaxf(m, om);
-    const float a = m == top ? 1.f : exp2_fast(m - top), b = om == top ? 1.f : exp2_fast(om - top);
+    const float a = m == top ? 1.f : exp_of(m - top), b = om == top ? 1.f : exp_of(om - top);
     s = s * a + os * b;
     m = top;
 }
@@ -54,30 +59,26 @@ struct EntropyForward {
             bias[i] = f32x4{0.f, 0.f, 0.f, 0.f};
             if (e.r.bias) bias[i] = load_four(e.r.bias + m0 + i * 16 + g4, (int)(p.m - (m0 + i * 16 + g4)), false);
         }
-        const float to_log2 = e.r.scale * LOG2E;
         const bool edge = m0 + TM * 16 > p.m;
-#pragma unroll
-        for (int i = 0; i < TM; ++i) bias[i] *= LOG2E;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             const long long n = n0 + j * 16 + (lane & 15);
             const long long t = n < p.n ? e.r.target[n] - (m0 + g4) : -1;
             const bool mine = t >= 0 && t < TM * 16 && (t & 15) < 4 && t + m0 + g4 < p.m;
+            float top = -__builtin_huge_valf();
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) acc[i][j][u] = score(acc[i][j][u], e.r.scale, bias[i][u]);
             if (__any(mine)) {   // the target is among this lane's words
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
-                        if (mine && t == i * 16 + u) {
-                            float z = acc[i][j][u] * e.r.scale;
-                            if (e.r.bias) z += e.r.bias[m0 + g4 + t];
-                            e.at_target[n] = z;
-                        }
+                        if (mine && t == i * 16 + u) e.at_target[n] = acc[i][j][u];
             }
-            float top = -__builtin_huge_valf();   // in units of log2(e)
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
-                acc[i][j] = acc[i][j] * to_log2 + bias[i];
                 if (edge) {
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
@@ -94,7 +95,7 @@ struct EntropyForward {
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int u = 0; u < 4; ++u) sum += exp2_fast(acc[i][j][u] - ref);
+                for (int u = 0; u < 4; ++u) sum += exp_of(acc[i][j][u] - ref);
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
             if (lane < 16) joined[(wave % WM) * (WN * TN * 16) + (wave / WM) * (TN * 16) + j * 16 + lane] = make_float2(top, sum);
@@ -138,11 +139,11 @@ __global__ __launch_bounds__(256) void entropy_join_kernel(const float2 *__restr
         }
     }
     if (q || n >= rows) return;
-    const float total = m * LN2 + logf(s);
+    const float rest = logf(s);
     const int64_t t = r.target[n];
-    lse[n] = total;
-    // no target: no loss; a target outside the vocabulary: not a number
-    loss[n] = t < 0 ? 0.f : t >= r.vocab ? __builtin_nanf("") : total - at_target[n];
+    lse[n] = m + rest;
+    // no target: no loss; a target outside the vocabulary: not a number; else without the rounding of lse
+    loss[n] = t < 0 ? 0.f : t >= r.vocab ? __builtin_nanf("") : (m - at_target[n]) + rest;
 }
 
 // Few rows: bound by reading W once.  A workgroup goes over a share of the words and leaves one pair per row.  One row, 20 000 words
@@ -171,15 +172,13 @@ __global__ __launch_bounds__(256) void entropy_few_kernel(EntropyRow e, const T 
         const float b0 = e.bias ? e.bias[f] : 0.f, b1 = e.bias && two ? e.bias[f + 1] : 0.f;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            float z0 = sum[0][r] * e.scale + b0, z1 = two ? sum[1][r] * e.scale + b1 : -__builtin_huge_valf();
+            const float z0 = score(sum[0][r], e.scale, b0), z1 = two ? score(sum[1][r], e.scale, b1) : -__builtin_huge_valf();
             if ((threadIdx.x & 15) == 0 && r < rows) {
                 if (t[r] == f) at_target[r] = z0;
                 if (t[r] == f + 1 && two) at_target[r] = z1;
             }
-            z0 *= LOG2E;
-            z1 *= LOG2E;
             const float top = fmaxf(m[r], fmaxf(z0, z1)), ref = top == -__builtin_huge_valf() ? 0.f : top;
-            s[r] = s[r] * exp2_fast(m[r] - ref) + exp2_fast(z0 - ref) + exp2_fast(z1 - ref);
+            s[r] = s[r] * exp_of(m[r] - ref) + exp_of(z0 - ref) + exp_of(z1 - ref);
             m[r] = top;
         }
     }
@@ -215,23 +214,20 @@ struct EntropyGradient {
         float *total = (float *)lds;   // [WN][BM]
         const long long wide = padded(p.m);   // G is read in pieces of eight words
         char *region = lds + wave * RowRegion<TM>::BYTES;
-        // float tensors: z - lse is formed before it is rounded to units of log2(e); for bf16 ones the rounding of both does
-        // not show, and scores come out of the product in these units
-        const float unit = PLANES == 3 ? 1.f : LOG2E, scale = e.r.scale * unit;
         const bool edge = m0 + TM * 16 > p.m;
         f32x4 bias[TM], sum[TM];
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const long long m = m0 + i * 16 + g4;
             bias[i] = sum[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (e.r.bias) bias[i] = load_four(e.r.bias + m, (int)(p.m - m), false) * unit;
+            if (e.r.bias) bias[i] = load_four(e.r.bias + m, (int)(p.m - m), false);
         }
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             const long long n = n0 + j * 16 + (lane & 15);
             const bool in = n < p.n;
             const long long t = in ? e.r.target[n] : -1;
-            const float lse = in ? e.lse[n] * unit : 0.f;
+            const float lse = in ? e.lse[n] : 0.f;
             // a row without a target adds nothing, whatever it holds: min(x, NaN) is x, min(NaN, 0) is 0
             const bool none = t < 0;
             const float grad = none ? 0.f : t >= e.r.vocab ? __builtin_nanf("") : e.grad[n];   // >= vocab: no such word
@@ -241,10 +237,9 @@ struct EntropyGradient {
             f32x4 col[TM];
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
-                f32x4 v = acc[i][j] * scale + bias[i];
+                f32x4 v;
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    v[u] = __builtin_fminf(exp2_fast(PLANES == 3 ? (v[u] - lse) * LOG2E : v[u] - lse), most);
+                for (int u = 0; u < 4; ++u) v[u] = __builtin_fminf(exp_of(score(acc[i][j][u], e.r.scale, bias[i][u]) - lse), most);
                 if (__any((unsigned)(at - i * 16) < 4u)) {
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
@@ -306,6 +301,54 @@ struct EntropyGradient {
         }
     }
 };
+
+// G of few rows, with the sums of entropy_few_kernel (a product's order of additions would give other scores than lse was
+// formed of).  A wavefront has eight words at a time, lane 2 r + which of 16 finishes row r of one of its group's two.  Words up
+// to `wide` are written, zeros behind the last.
+template <class T, int R, bool VEC>
+__global__ __launch_bounds__(256) void entropy_few_gradient_kernel(EntropyRow e, long long first, int words, int wide,
+                                                                   const T *__restrict__ x, const T *__restrict__ w, int rows,
+                                                                   int k, const float *__restrict__ lse,
+                                                                   const float *__restrict__ grad, __bf16 *__restrict__ g,
+                                                                   long long plane, float *__restrict__ dbias)
+{
+    const int lane = threadIdx.x & 15, r = lane >> 1, which = lane & 1;
+    const bool in = r < rows;
+    const long long t = in ? e.target[r] : -1;
+    // as in EntropyGradient: a row without a target adds nothing, a target behind the vocabulary is not a number
+    const bool none = t < 0;
+    const float own = none ? 0.f : t >= e.vocab ? __builtin_nanf("") : grad[r], most = none ? 0.f : __builtin_nanf("");
+    const float sum_of_row = in ? lse[r] : 0.f;
+    for (long long f = ((long long)blockIdx.x * 16 + (threadIdx.x >> 4)) * 2; f < wide; f += (long long)gridDim.x * 32) {
+        const long long f0 = f < words ? f : words - 1, f1 = f + 1 < words ? f + 1 : words - 1;
+        float sum[2][R];
+#pragma unroll
+        for (int u = 0; u < R; ++u) sum[0][u] = sum[1][u] = 0.f;
+        few_rows_dot<T, R, VEC>(w + f0 * k, w + f1 * k, x, rows, k, sum);
+        float dot = 0.f;
+#pragma unroll
+        for (int u = 0; u < R; ++u)
+            if (u == r) dot = which ? sum[1][u] : sum[0][u];
+        float v = 0.f;
+        if (in && f + which < words) {
+            v = __builtin_fminf(exp_of(score(dot, e.scale, e.bias ? e.bias[f + which] : 0.f) - sum_of_row), most);
+            if (!none && t - first == f + which) v -= 1.f;
+            v *= own;
+        }
+        float total = 0.f;
+#pragma unroll
+        for (int u = 0; u < R; ++u) total += __shfl(v, 2 * u + which, 16);
+        if (dbias && r == 0 && f + which < words) dbias[f + which] = total;
+        if (in) {
+            __bf16 a, b, c;
+            split_planes(v, a, b, c);
+            __bf16 *to = g + r * (long long)wide + f + which;
+            to[0] = a;
+            to[plane] = b;
+            if (sizeof(T) == 4) to[2 * plane] = c;
+        }
+    }
+}
 
 // dx = scale (the sums of G W + what rounding took from the target's G times its word).  The target's G is most of a row's: its
 // rounding to bf16 would be as large in dx as that of dx itself, and the same for all of the row.
@@ -432,6 +475,32 @@ static hipError_t launch_few(const EntropyRow &e, const T *x, const T *w, int ro
     return hipGetLastError();
 }
 
+template <class T, int R>
+static hipError_t launch_few_gradient(const EntropyRow &e, long long first, int words, const T *x, const T *w, int rows, int k,
+                                      const float *lse, const float *grad, void *g, float *dbias, hipStream_t s)
+{
+    const int wide = (int)padded(words);
+    const unsigned grid = (unsigned)few_groups(wide);
+    if (k % (16 / (int)sizeof(T)) == 0 && (((uintptr_t)x | (uintptr_t)w) & 15) == 0)   // as launch_few
+        hipLaunchKernelGGL((entropy_few_gradient_kernel<T, R, true>), dim3(grid), dim3(256), 0, s, e, first, words, wide, x, w, rows, k,
+                           lse, grad, (__bf16 *)g, (long long)rows * wide, dbias);
+    else
+        hipLaunchKernelGGL((entropy_few_gradient_kernel<T, R, false>), dim3(grid), dim3(256), 0, s, e, first, words, wide, x, w, rows,
+                           k, lse, grad, (__bf16 *)g, (long long)rows * wide, dbias);
+    return hipGetLastError();
+}
+template <class T>
+static hipError_t few_gradient(const EntropyRow &e, long long first, int words, const void *x, const void *w, int64_t rows, int k,
+                               const float *lse, const float *grad, void *g, float *dbias, hipStream_t s)
+{
+    const T *xt = (const T *)x, *wt = (const T *)w + first * k;
+    const int r = (int)rows;
+    return r == 1   ? launch_few_gradient<T, 1>(e, first, words, xt, wt, r, k, lse, grad, g, dbias, s)
+           : r == 2 ? launch_few_gradient<T, 2>(e, first, words, xt, wt, r, k, lse, grad, g, dbias, s)
+           : r <= 4 ? launch_few_gradient<T, 4>(e, first, words, xt, wt, r, k, lse, grad, g, dbias, s)
+                    : launch_few_gradient<T, 8>(e, first, words, xt, wt, r, k, lse, grad, g, dbias, s);
+}
+
 template <class T>
 static lcn_status entropy_as(const T *x, const T *w, const float *bias, const int64_t *target, int64_t rows, int32_t vocab,
                              int32_t dim, int32_t dtype, float scale, float *loss, float *lse, char *ws, size_t ws_bytes,
@@ -486,9 +555,10 @@ static lcn_status entropy_backward_as(const void *x, const void *w, const float 
     if (!ws || ((uintptr_t)ws & 255) || ws_bytes < b.bytes) return LCN_ERR_ALLOC;
     const size_t size = dtype == LCN_F32 ? 4 : 2;
     PlaneJobs jobs;
-    const Operand wo = add_operand(jobs, w, vocab, dim, dtype, b.wp);
-    const Operand xo = add_operand(jobs, x, rows, dim, dtype, b.xp);
-    Operand xz{};
+    const bool few = rows <= FEW_ROWS;
+    Operand wo{}, xo{}, xz{};
+    if (dx || !few) wo = add_operand(jobs, w, vocab, dim, dtype, b.wp);
+    if (!few) xo = add_operand(jobs, x, rows, dim, dtype, b.xp);
     if (dw) xz = add_masked(jobs, x, rows, dim, dtype, target, b.xz);
     OPCHK(launch_planes(jobs, dtype, s));
     const bool rounded = dx && b.planes == 1, one = b.piece >= vocab && !rounded;
@@ -507,10 +577,15 @@ static lcn_status entropy_backward_as(const void *x, const void *w, const float 
         p.n = (int)rows;
         p.k = dim;
         float *sums = dbias ? b.sums : nullptr;
-        OPCHK(b.planes == 3   ? launch_gradient<3>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, rest, s)
-              : b.planes == 2 ? launch_gradient<2>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, rest, s)
-                              : launch_gradient<1>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, rest, s));
-        if (dbias) {
+        if (few)
+            OPCHK(dtype == LCN_F32
+                      ? few_gradient<float>(r, first, words, x, w, rows, dim, lse, grad, b.g, dbias ? dbias + first : nullptr, s)
+                      : few_gradient<__bf16>(r, first, words, x, w, rows, dim, lse, grad, b.g, dbias ? dbias + first : nullptr, s));
+        else
+            OPCHK(b.planes == 3   ? launch_gradient<3>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, rest, s)
+                  : b.planes == 2 ? launch_gradient<2>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, rest, s)
+                                  : launch_gradient<1>(b.scores, p, r, first, lse, grad, b.g, g.ld, sums, rest, s));
+        if (dbias && !few) {
             const int parts = (int)(row_tiles(b.scores, rows, dtype));
             OPCHK(launch_column_sums(sums, parts, words, LCN_F32, dbias + first, s));
         }

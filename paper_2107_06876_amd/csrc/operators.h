@@ -337,7 +337,8 @@ inline size_t partial_bytes(const ProductPlan &plan, long long m, long long n)
 
 // ---- products with few rows: 16 lanes per row of W ---------------------------
 // sums[f][r] += W[f] . x[r] for two rows of W per group of 16 lanes and R rows of x (`rows` of them exist); every lane of
-// the group gets the sums.  Sums are in 32 bits.  VEC: rows of W and x are whole aligned 16-byte pieces.
+// the group gets the sums.  Sums are in 32 bits, of the same bits in every kernel that forms them (their order and the fused
+// multiply-adds are fixed here).  VEC: rows of W and x are whole aligned 16-byte pieces.
 template <class T, int R, bool VEC>
 __device__ __forceinline__ void few_rows_dot(const T *__restrict__ w0, const T *__restrict__ w1, const T *__restrict__ x,
                                              int rows, int k, float (&sum)[2][R])
@@ -363,8 +364,8 @@ __device__ __forceinline__ void few_rows_dot(const T *__restrict__ w0, const T *
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                sum[0][r] += (float)a[e] * (float)y[r][e];
-                sum[1][r] += (float)b[e] * (float)y[r][e];
+                sum[0][r] = __builtin_fmaf((float)a[e], (float)y[r][e], sum[0][r]);
+                sum[1][r] = __builtin_fmaf((float)b[e], (float)y[r][e], sum[1][r]);
             }
     }
 #pragma unroll

@@ -226,3 +226,33 @@ def test_more_tiles_than_a_launch_has_in_one_dimension():
     assert torch.isfinite(loss).all()
     # 2049 tiles of 256 words: sums of 32-bit partial sums
     assert off(lse[some], want) <= bound(F32, vocab) and off(loss[some], want - z.gather(1, t[some, None])[:, 0]) <= bound(F32, vocab)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [1, 3, 8, 30, 600])
+@pytest.mark.parametrize("bias", [False, True])
+def test_a_target_with_all_the_weight(rows, bias, dtype):
+    """Scores of several hundred, the target's far above all others: the loss is 0 and not below, and no gradient is left."""
+    g = generator(41, rows)
+    vocab, dim, scale = 400, 24, 400.0
+    w = normal(g, vocab, dim, dtype=dtype)
+    t = torch.randint(0, vocab, (rows,), generator=g).to(DEV)
+    x = w.double()[t]
+    x = (x * (0.9 + 0.1 * torch.rand(rows, 1, generator=g).to(DEV)) / (x * x).sum(1, keepdim=True)).to(dtype)
+    b = normal(g, vocab) if bias else None
+    grad = (0.5 + torch.rand(rows, generator=g)).to(DEV)
+    z = scale * (x.double() @ w.double().t().contiguous()) + (b.double() if bias else 0.0)
+    at = z.gather(1, t[:, None])[:, 0]
+    rest = z.scatter(1, t[:, None], -math.inf).max(1).values
+    far = at - rest > 40.0   # the others' weight is below 400 e^-40
+    t = torch.where(far, t, torch.full_like(t, -1))
+    assert far.sum() >= 0.8 * rows
+    loss, lse = lcn.lcn_cross_entropy(x, w, t, bias=b, scale=scale)
+    assert (loss >= 0).all() and loss.max().item() <= 2.0 ** -24
+    assert off(lse, torch.logsumexp(z, 1)) <= bound(F32, dim)
+    dx, dw, db = lcn.lcn_cross_entropy_backward(x, w, t, lse, grad, bias=b, scale=scale)
+    # one rounding of P = 1 in every row
+    step = 2.0 ** -24 * 1.5 * scale
+    assert dx.double().abs().max().item() <= step * w.double().abs().max().item()
+    assert dw.double().abs().max().item() <= step * x.double().abs().max().item() * rows
+    assert db is None or db.double().abs().max().item() <= 2.0 ** -24 * 1.5 * rows
