@@ -305,7 +305,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
     typename Frag<T>::type fq[QT][C];
     int qi[QT];
     f32x4 o[DT][QT];
-    float top[QT], sum[QT];   // top: in the score's units
+    // top: the maximum, in the score's units; ref: the same times log2(e), rounded once, what the exponentials are taken against.
+    // A query whose maximum stays is scaled by 2^(ref - ref) = 1, whatever the other queries do.
+    float top[QT], ref[QT], sum[QT];
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         qi[u] = w.first + (wave * QT + u) * 16 + (lane & 15);
@@ -313,7 +315,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
 #pragma unroll
         for (int c = 0; c < C; ++c) fq[u][c] = read_fragment<T, VEC>(row, 32 * c + 8 * g, a.dim);
         top[u] = minus_infinity();
-        sum[u] = 0.f;
+        ref[u] = sum[u] = 0.f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d][u] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -383,10 +385,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
                     for (int e = 0; e < 4; ++e) most = fmaxf(most, z[kt][u][e]);
                 most = fmaxf(most, __shfl_xor(most, 16));
                 most = fmaxf(most, __shfl_xor(most, 32));
-                const float ref = most == minus_infinity() ? 0.f : most * score.unit;
                 if (__any(most != top[u])) {   // else nothing is scaled down
-                    const float keep = exp2_fast(top[u] * score.unit - ref);
+                    float now = most == minus_infinity() ? 0.f : most * score.unit;
+                    asm volatile("" : "+v"(now));   // rounded here, not fused into the difference
+                    const float keep = top[u] == minus_infinity() ? 0.f : exp2_fast(ref[u] - now);
                     top[u] = most;
+                    ref[u] = now;
                     sum[u] *= keep;
 #pragma unroll
                     for (int d = 0; d < DT; ++d) o[d][u] *= keep;
@@ -394,7 +398,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
 #pragma unroll
                 for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) z[kt][u][e] = exp2_fast(z[kt][u][e] * score.unit - ref);
+                    for (int e = 0; e < 4; ++e) z[kt][u][e] = exp2_fast(z[kt][u][e] * score.unit - ref[u]);
             }
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt)
@@ -445,7 +449,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
         total += __shfl_xor(total, 32);
         if (qi[u] >= s.nq) continue;
         const long long n = s.q0 + qi[u];
-        const float reference = SHAPE == CAPPED ? score.cap : top[u] * score.unit;
+        const float reference = SHAPE == CAPPED ? score.cap : top[u] == minus_infinity() ? top[u] : ref[u];
         if (a.key_splits > 1) {
             const long long row = (w.split * a.total_q + n) * a.heads + w.head;
 #pragma unroll

@@ -336,3 +336,31 @@ def test_more_rows_to_join_than_a_launch_has_in_one_dimension():
         part = slice(p * nk, (p + 1) * nk)
         want = oracle(q[p:p + 1], k[part], k[part], q[p:p + 1], [1], [nk], dim ** -0.5)
         assert off(o[p:p + 1], want[0]) <= bound(BF16, nk, 1) and off(lse[:, p:p + 1], want[1]) <= bound(F32, nk)
+
+
+# ---- exactness ------------------------------------------------------------------
+
+
+def one_head(q, k, scale):
+    """lse in 64 bits of one head's queries against all keys, on the device."""
+    z = scale * (q.double() @ k.double().t().contiguous())
+    return torch.logsumexp(z, 1)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_long_row_of_scores_is_not_scaled_by_rounding(dim, dtype):
+    """8192 keys, scores of deviation 10: other queries' new maxima leave a query's sum alone.  q and k hold small whole numbers, so that
+    q . k is exact; what is left is a rounding of lse itself (2^-25 of the power of two above it) and the sum's, which are smaller
+    taken together than 2^-24 of the largest lse."""
+    g = generator(31, dim)
+    heads, nq, nk = 64, 1024, 8192   # so many tiles that no query's keys are split over workgroups
+    q = normal(g, nq, heads, dim, scale=10.0).round().to(dtype)
+    k = normal(g, nk, 1, dim).round().to(dtype)
+    _, lse = lcn.lcn_attention(q, k, k, offsets([nq]), offsets([nk]))
+    err, most = 0.0, 0.0
+    for h in (0, 17, 40, 63):
+        want = one_head(q[:, h], k[:, 0], dim ** -0.5)
+        err += (lse[h].double() - want).square().sum().item()
+        most = max(most, want.abs().max().item())
+    assert math.sqrt(err / (4 * nq)) <= 2.0 ** -24 * most
