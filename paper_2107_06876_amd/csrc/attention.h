@@ -96,8 +96,9 @@ __device__ __forceinline__ float natural_log(float m, float s)
 
 // How q . k becomes a score.  PLAIN: a positive multiple.  CAPPED (bf16 tensors, scale > 0, cap up to MOST_CAP, no slopes):
 // cap tanh(scale q.k / cap) = cap - 2 cap r with r = 1 / (e^(2 scale q.k / cap) + 1), off by about 2^-23 of the cap, far
-// below the rounding of P; no score is above the cap, so that is the reference of the exponentials: P' = 2^(-2 cap r
-// log2(e)) >= 2^-116 needs no running maximum, and the cap's derivative is 4 r (1 - r).  SHAPED: anything, by tanhf.
+// below the rounding of P; a score is between -cap and cap, so the exponentials need no running maximum: with 0 as their
+// reference P' is between 2^-58 and 2^58, and its products with small v and its sums over 2^30 keys keep their bits (with the cap
+// as reference it was down to 2^-116).  The cap's derivative is 4 r (1 - r).  SHAPED: anything, by tanhf.
 enum Shape { PLAIN = 0, CAPPED = 1, SHAPED = 2 };
 constexpr float MOST_CAP = 40.f;
 
@@ -360,7 +361,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
 #pragma unroll
                 for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) z[kt][u][e] = exp2_fast(score.under(z[kt][u][e]) * (-2.f * score.cap));
+                    for (int e = 0; e < 4; ++e) z[kt][u][e] = exp2_fast(__builtin_fmaf(score.under(z[kt][u][e]), -2.f * score.cap, score.cap));
                 if (!whole) {
 #pragma unroll
                     for (int kt = 0; kt < 4; ++kt)
@@ -449,7 +450,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
         total += __shfl_xor(total, 32);
         if (qi[u] >= s.nq) continue;
         const long long n = s.q0 + qi[u];
-        const float reference = SHAPE == CAPPED ? score.cap : top[u] == minus_infinity() ? top[u] : ref[u];
+        const float reference = SHAPE == CAPPED ? 0.f : top[u] == minus_infinity() ? top[u] : ref[u];
         if (a.key_splits > 1) {
             const long long row = (w.split * a.total_q + n) * a.heads + w.head;
 #pragma unroll

@@ -364,3 +364,22 @@ def test_a_long_row_of_scores_is_not_scaled_by_rounding(dim, dtype):
         err += (lse[h].double() - want).square().sum().item()
         most = max(most, want.abs().max().item())
     assert math.sqrt(err / (4 * nq)) <= 2.0 ** -24 * most
+
+
+@pytest.mark.parametrize("end", [1.0, -1.0])
+@pytest.mark.parametrize("cap", [30.0, 40.0])
+@pytest.mark.parametrize("how", [dict(), dict(causal=True, prefix=[40, 300])])
+def test_scores_at_either_end_of_the_cap(end, cap, how):
+    """All scores at +cap or at -cap and small v: the exponentials are not so small that v loses bits."""
+    g = generator(32)
+    lengths, dim = [100, 333], 64
+    n = sum(lengths)
+    q = (normal(g, n, 2, dim).abs() + 8.0).to(BF16)
+    k = (end * (normal(g, n, 1, dim).abs() + 8.0)).to(BF16)
+    v, do = normal(g, n, 1, dim, dtype=BF16, scale=2.0 ** -32), normal(g, n, 2, dim, dtype=BF16)
+    prefix = how.get("prefix")
+    args = dict(how, cap=cap, prefix=None if prefix is None else torch.tensor(prefix, dtype=torch.int32, device=DEV))
+    o, lse = lcn.lcn_attention(q, k, v, offsets(lengths), offsets(lengths), **args)
+    want = oracle(q, k, v, do, lengths, lengths, dim ** -0.5, how.get("causal", False), prefix, None, cap)
+    assert off(o, want[0]) <= bound(BF16, 333, 1) + 2.0 ** -21 * cap
+    assert off(lse, want[1]) <= bound(F32, 333)
