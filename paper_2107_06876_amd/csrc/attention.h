@@ -39,7 +39,7 @@ struct AttentionArgs {
     const void *d_o;
     const float *lse_in;
     float *delta;               // [head][query]
-    void *dq, *dk, *dv;
+    void *dq, *dk, *dv;         // dq: nullable, delta alone is formed then
     // sums shared by several workgroups, where there are few tiles, and joined by a second launch
     int key_splits;             // of a query tile's keys (forward, dq)
     int splits;                 // of a key tile's queries (dk, dv)
@@ -724,20 +724,6 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a)
 }
 
 // ---- backward -------------------------------------------------------------------
-// delta = do . o per query and head, where dq is not asked for: 16 lanes each
-template <class T>
-__global__ __launch_bounds__(256) void attention_delta_kernel(const T *__restrict__ o, const T *__restrict__ d_o, long long total_q,
-                                                              int heads, int dim, float *__restrict__ delta)
-{
-    const long long r = (long long)group_number() * 16 + (threadIdx.x >> 4);
-    if (r >= total_q * heads) return;
-    float s = 0.f;
-    for (int d = threadIdx.x & 15; d < dim; d += 16) s += (float)o[r * dim + d] * (float)d_o[r * dim + d];
-#pragma unroll
-    for (int x = 8; x > 0; x >>= 1) s += __shfl_xor(s, x, 16);
-    if ((threadIdx.x & 15) == 0) delta[(r % heads) * total_q + r / heads] = s;
-}
-
 // sum[u] += a b[u]; float: the product by itself, so that a long sum is rounded once for 32 of its terms
 template <class T, int N>
 __device__ __forceinline__ void add_product(f32x4 (&sum)[N], typename Frag<T>::type a, const typename Frag<T>::type (&b)[N])
@@ -760,8 +746,10 @@ __device__ __forceinline__ void add_product(f32x4 (&sum)[N], typename Frag<T>::t
 
 // dq: like the forward pass; dS = P (dP - delta) cut, dq = scale sum_j dS_ij k_j.
 // delta_i = do_i . o_i = sum_j P_ij dP_ij.  Where a tile sees up to EXACT_KEYS keys it is formed as the second sum, in a pass of
-// its own: o is large there, and its rounding to bf16 would count in dS as much as that of dS itself (with more keys o is
-// an average of many v, and small).  The delta that is used goes to a.delta for dk and dv.
+// its own: o is large there, and its rounding to bf16 would count in dS as much as that of dS itself.  With more keys do . o is
+// taken: o is an average of many v then, and small, unless a row's weight lies on few keys (steep slopes, large scores), whose dS
+// is off by a rounding of o as well; the first sum costs a pass over all keys.  The delta that is used goes to a.delta for dk and dv; where dq is not asked for that is all
+// that the kernel does, so that dk does not depend on it.
 // Bound as the forward pass is: the documents 425 us (0.63 PFLOP/s), the small float sets 56.
 constexpr int EXACT_KEYS = 256;
 template <class T, int DP, int QT, bool VEC, int SHAPE>
@@ -877,6 +865,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
         delta[u] += __shfl_xor(delta[u], 32);
         if (g == 0 && qi[u] < s.nq && w.split == 0) a.delta[w.head * a.total_q + s.q0 + qi[u]] = delta[u];
     }
+    if (!a.dq) return;
     two_buffers(w.step<BK>(a, w.split), w.step<BK>(a, w.split + 1), fetch, [](int, auto) {}, [&](int t, auto which) {
         const char *lds_k = decltype(which)::value ? lds1 : lds0, *lds_v = lds_k + BK * L::PITCH;
         if (QT == 1 && w_first >= s.nq) return;   // short sets: see the forward kernel

@@ -132,15 +132,11 @@ template <class T>
 hipError_t attention_backward(AttentionArgs a, bool vec, int shape, hipStream_t s)
 {
     hipError_t e = hipSuccess;
-    if (a.total_q > 0 && a.dq) {
+    if (a.total_q > 0) {
+        if (!a.dq) a.key_splits = 1;   // delta alone: formed by one workgroup of a tile
         e = by_size<T, GRAD_Q>(a, vec, shape, s);
         if (e == hipSuccess && a.key_splits > 1)
             e = add_sums<T>(a, a.key_splits, a.total_q, (long long)a.heads * a.dim, a.q_off, a.dq, nullptr, vec, s);
-    } else if (a.total_q > 0) {
-        const long long rows = a.total_q * a.heads;
-        hipLaunchKernelGGL(attention_delta_kernel<T>, grid_of((rows + 15) / 16), dim3(256), 0, s, (const T *)a.o,
-                           (const T *)a.d_o, a.total_q, a.heads, a.dim, a.delta);
-        e = hipGetLastError();
     }
     if (e != hipSuccess || !a.dk || a.total_k == 0) return e;
     e = by_size<T, GRAD_KV>(a, vec, shape, s);

@@ -383,3 +383,23 @@ def test_scores_at_either_end_of_the_cap(end, cap, how):
     want = oracle(q, k, v, do, lengths, lengths, dim ** -0.5, how.get("causal", False), prefix, None, cap)
     assert off(o, want[0]) <= bound(BF16, 333, 1) + 2.0 ** -21 * cap
     assert off(lse, want[1]) <= bound(F32, 333)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("how", [dict(), dict(causal=True, cap=5.0), dict(slopes=[0.1, 0.2])])
+def test_gradients_of_keys_without_those_of_queries(how, dtype):
+    """dk and dv, and dq, have the same bits whichever are asked for."""
+    g = generator(33)
+    nq, nk = [90, 140, 33, 700], [90, 140, 33, 900]
+    for dim, shift in ((64, 0), (20, 0), (64, 1)):
+        q, do = (normal(g, sum(nq), 2, dim, dtype=dtype, shift=shift) for _ in range(2))
+        k, v = (normal(g, sum(nk), 1, dim, dtype=dtype, shift=shift) for _ in range(2))
+        args = dict(how, slopes=None if "slopes" not in how else torch.tensor(how["slopes"], device=DEV))
+        qo, ko = offsets(nq), offsets(nk)
+        kept = lcn.lcn_attention(q, k, v, qo, ko, **args)
+        all_three = lcn.lcn_attention_backward(q, k, v, *kept, do, qo, ko, **args)
+        dq, none_k, none_v = lcn.lcn_attention_backward(q, k, v, *kept, do, qo, ko, with_kv=False, **args)
+        none_q, dk, dv = lcn.lcn_attention_backward(q, k, v, *kept, do, qo, ko, with_q=False, **args)
+        assert none_q is None and none_k is None and none_v is None
+        for u, w in zip((dq, dk, dv), all_three):
+            assert torch.equal(u, w)
