@@ -447,7 +447,7 @@ lcn_status lcn_cross_entropy_backward(const void *x, const void *W, const float 
  *           a head are contiguous); o, dy and the gradients are dense
  *   lse     fp32, heads x total_q
  * Sets may be empty.  Offsets that are not in order or outside 0 .. total are cut
- * to what exists; queries in no set are not written.  Sizes: num_sets <= 2^24,
+ * to what exists; queries in no set are not written unless `clear` says so.  Sizes: num_sets <= 2^24,
  * heads <= 1024 and a multiple of kv_heads, head_dim <= 128, totals <= 2^30.
  * slopes are constants (they get no gradient). */
 typedef struct {
@@ -464,6 +464,8 @@ typedef struct {
     const int32_t *prefix;    /* device, num_sets, nullable (0); read if causal */
     const float *slopes;      /* device, heads, nullable */
     int64_t q_token, q_head, k_token, k_head, v_token, v_head; /* strides in elements */
+    int32_t clear;            /* 1: tokens before the first and behind the last set get o = 0, lse = -inf and gradients of
+                                 zero; 0: these are not written */
 } lcn_attention_desc;
 lcn_status lcn_attention_workspace_bytes(const lcn_attention_desc *desc, int32_t backward, size_t *bytes);
 lcn_status lcn_attention(const lcn_attention_desc *desc, const void *q, const void *k, const void *v, void *o, float *lse,
@@ -472,7 +474,7 @@ lcn_status lcn_attention(const lcn_attention_desc *desc, const void *q, const vo
  * forward call:  dv = P^T dy,  dS = P .* (dy v^T - rowsum(dy .* o)) (times the cap's
  * derivative),  dq = scale dS k,  dk = scale dS^T q, dk and dv summed over the
  * query heads of a key head.  dq, or dk and dv together, may be NULL.  Gradients
- * of tokens in no set are not written. */
+ * of tokens in no set are not written unless `clear` says so. */
 lcn_status lcn_attention_backward(const lcn_attention_desc *desc, const void *q, const void *k, const void *v, const void *o,
                                   const float *lse, const void *dy, void *dq, void *dk, void *dv, void *workspace,
                                   size_t workspace_bytes, void *hip_stream);

@@ -29,7 +29,8 @@ struct AttentionArgs {
     int causal;
     float scale, cap;
     int tiles;                  // of queries (forward, dq) or keys (dk, dv), over all sets
-    unsigned groups;            // workgroups with work, see group_number()
+    unsigned groups;            // workgroups with work, see group_number(); where `clear` is set CLEARERS more follow
+    int clear;                  // tokens in no set: 0: not written, 1: zeros
     // forward
     void *o;                    // read in the backward pass
     float *lse;                 // [head][query]
@@ -281,6 +282,33 @@ __device__ __forceinline__ void two_buffers(int begin, int end, Fetch fetch, Lan
     }
 }
 
+// What stands in for tokens before the first and behind the last set: zeros in rows of `width` values, -inf in lse.  The workgroups
+// behind those with work share it; where every token is in a set there is nothing to do.
+constexpr unsigned CLEARERS = 64;
+template <class T, bool VEC>
+__device__ __forceinline__ void clear_others(const AttentionArgs &a, const int64_t *off, long long tokens, long long width, T *out0,
+                                             T *out1, float *lse)
+{
+    const unsigned nth = group_number() - a.groups;   // wraps around for those with work
+    if (!a.clear || !out0 || nth >= CLEARERS) return;
+    const long long first = off[0], last = off[a.sets];
+    const long long begin = first < 0 ? 0 : first < tokens ? first : tokens, end = last < begin ? begin : last < tokens ? last : tokens;
+    const long long others = begin + tokens - end;
+    constexpr int EACH = VEC ? 16 / (int)sizeof(T) : 1;
+    typedef T piece __attribute__((ext_vector_type(EACH)));
+    const long long step = CLEARERS * blockDim.x, mine = (long long)nth * blockDim.x + threadIdx.x, per_row = width / EACH;
+    for (long long t = mine; t < others * per_row; t += step) {
+        const long long at = (t < begin * per_row ? t : t + (end - begin) * per_row) * EACH;
+        *(piece *)(out0 + at) = piece{};
+        if (out1) *(piece *)(out1 + at) = piece{};
+    }
+    if (lse)
+        for (long long t = mine; t < others * a.heads; t += step) {
+            const long long n = t % others;
+            lse[t / others * tokens + (n < begin ? n : n + end - begin)] = minus_infinity();
+        }
+}
+
 // ---- forward -------------------------------------------------------------------
 // Four wavefronts of 16 QT queries each go over the set's keys, 64 at a time.  Bound by the vector instructions beside the
 // matrix ones: an exponential, a maximum and two conversions per score.  bf16, two sets of 8192, 16 heads of 64: 803 us,
@@ -295,7 +323,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
     __shared__ __align__(1024) char lds1[2 * BK * L::PITCH];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
     const QueryTile w = query_tile<BQ>(a);
-    if (!w.any) return;
+    if (!w.any) return clear_others<T, VEC>(a, a.q_off, a.total_q, (long long)a.heads * a.dim, (T *)a.o, nullptr, a.lse);
     const SetRange s = w.s;
     Scores<T, SHAPE> score;
     score.init(a, w.head);
@@ -473,13 +501,27 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
     }
 }
 
+// The row of a query and head that is in no set, by a wavefront.
+template <class T>
+__device__ __forceinline__ void clear_row(const AttentionArgs &a, long long row, int lane)
+{
+    T *out = (T *)a.o + row * a.dim;
+    if (lane < a.dim) out[lane] = (T)0.f;
+    if (lane + 64 < a.dim) out[lane + 64] = (T)0.f;
+    if (lane == 0) a.lse[row % a.heads * a.total_q + row / a.heads] = minus_infinity();
+}
+
 // Joins the splits of a query and head, a wavefront each, in their order.  Bound by memory, and small where splits are chosen.
 template <class T>
 __global__ __launch_bounds__(256) void attention_join_splits_kernel(AttentionArgs a)
 {
     const long long row = (long long)group_number() * 4 + (threadIdx.x >> 6), n = row / a.heads, all = a.total_q * a.heads;
     const int head = (int)(row % a.heads), lane = threadIdx.x & 63;
-    if (n >= a.total_q || n < a.q_off[0] || n >= a.q_off[a.sets]) return;
+    if (n >= a.total_q) return;
+    if (n < a.q_off[0] || n >= a.q_off[a.sets]) {
+        if (a.clear) clear_row<T>(a, row, lane);
+        return;
+    }
     float most = minus_infinity();
     for (int s = 0; s < a.key_splits; ++s) most = fmaxf(most, a.part_top[s * all + row].x);
     float total = 0.f, v0 = 0.f, v1 = 0.f;
@@ -688,6 +730,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a)
     const int p = last_set(a.sets, [&](int q) { return a.q_off[q] <= n; });
     const SetRange s = range_of(a, p);
     const long long i = n - s.q0, r = i * group + head % group;
+    if (a.clear && (n < a.q_off[0] || n >= a.q_off[a.sets])) return clear_row<T>(a, row, lane);
     if (i < 0 || i >= s.nq || r >= a.rows) return;
     const long long first = s.k0 / a.chunk + p;
     const int chunks = (s.nk + a.chunk - 1) / a.chunk;
@@ -761,7 +804,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
     __shared__ __align__(1024) char lds1[2 * BK * L::PITCH];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
     const QueryTile w = query_tile<BQ>(a);
-    if (!w.any) return;
+    if (!w.any) return clear_others<T, VEC>(a, a.q_off, a.total_q, (long long)a.heads * a.dim, (T *)a.dq, nullptr, nullptr);
     const SetRange s = w.s;
     Scores<T, SHAPE> score;
     score.init(a, w.head);
@@ -924,7 +967,8 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
     const int group = a.heads / a.kv_heads;
     const unsigned id = group_number();
-    if (id >= a.groups) return;
+    if (id >= a.groups)
+        return clear_others<T, VEC>(a, a.k_off, a.total_k, (long long)a.kv_heads * a.dim, (T *)a.dk, (T *)a.dv, nullptr);
     const int share = (int)(id % a.splits), kv = (int)(id / a.splits % a.kv_heads);
     const long long tile = id / (a.splits * a.kv_heads);
     const int p = set_of_tile(a.k_off, a.sets, BK, tile);
@@ -1070,10 +1114,11 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
 }
 
 // A gradient (blockIdx.y = 0, 1: of two) from the sums of `splits` workgroups, in their order: a thread adds four values of the
-// `width` of a token.  Tokens in no set are not written.
+// `width` of a token.  Tokens in no set are not written, or become zero (clear).
 template <class T>
 __global__ __launch_bounds__(256) void attention_add_kernel(const float *part, int splits, long long tokens, long long width,
-                                                            const int64_t *off, int sets, T *out0, T *out1, int whole)
+                                                            const int64_t *off, int sets, T *out0, T *out1, int whole,
+                                                            int clear)
 {
     const long long all = tokens * width, stride = all * gridDim.y, fours = (all + 3) / 4;
     const long long begin = off[0] < 0 ? 0 : off[0] * width, end = (off[sets] < tokens ? off[sets] : tokens) * width;
@@ -1086,8 +1131,10 @@ __global__ __launch_bounds__(256) void attention_add_kernel(const float *part, i
         if (i >= begin && i + 4 <= end) {
             store_four(out + i, v, 4, whole);
         } else {
-            for (int e = 0; e < 4; ++e)
-                if (i + e >= begin && i + e < end) out[i + e] = (T)v[e];
+            for (int e = 0; e < 4; ++e) {
+                const bool in = i + e >= begin && i + e < end;
+                if (in || (clear && i + e < all)) out[i + e] = in ? (T)v[e] : (T)0.f;
+            }
         }
     }
 }

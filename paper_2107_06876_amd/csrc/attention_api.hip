@@ -9,6 +9,7 @@ static bool attention_desc_fits(const lcn_attention_desc *d)
         d->total_k > MAX_ROWS || d->max_q < 0 || d->heads < 1 || d->heads > 1024 || d->kv_heads < 1 || d->heads % d->kv_heads ||
         d->head_dim < 1 || d->head_dim > 128 || (d->dtype != LCN_F32 && d->dtype != LCN_BF16))
         return false;
+    if (d->clear != 0 && d->clear != 1) return false;
     if (!(d->scale - d->scale == 0.f) || !(d->cap >= 0.f) || !(d->cap - d->cap == 0.f)) return false;
     const int64_t strides[6] = {d->q_token, d->q_head, d->k_token, d->k_head, d->v_token, d->v_head};
     for (int i = 0; i < 6; ++i)
@@ -44,6 +45,7 @@ static AttentionArgs args_of(const lcn_attention_desc *d, const void *q, const v
     a.causal = d->causal != 0;
     a.scale = d->scale;
     a.cap = d->cap;
+    a.clear = d->clear != 0;
     return a;
 }
 
@@ -98,6 +100,20 @@ static int query_splits(const lcn_attention_desc *d)
     if (d->num_sets == 0) return 1;
     const int64_t tiles = (d->total_k / 128 + d->num_sets) * d->kv_heads;
     return shares((tiles + 1) / 2, d->total_q / d->num_sets * (d->heads / d->kv_heads));
+}
+
+// -inf for the lse of queries where there is no set at all
+__global__ __launch_bounds__(256) void no_key_kernel(float *lse, long long count)
+{
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < count; i += (long long)gridDim.x * 256) lse[i] = minus_infinity();
+}
+static hipError_t clear_all(void *out, long long values, int32_t dtype, float *lse, long long rows, hipStream_t s)
+{
+    const hipError_t e = launch_zero(out, (size_t)values * (dtype == LCN_F32 ? 4 : 2), s);
+    if (e != hipSuccess || !lse || rows == 0) return e;
+    const long long groups = (rows + 255) / 256;
+    hipLaunchKernelGGL(no_key_kernel, dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(256), 0, s, lse, rows);
+    return hipGetLastError();
 }
 
 struct ForwardSpace {
@@ -160,8 +176,13 @@ lcn_status lcn_attention(const lcn_attention_desc *desc, const void *q, const vo
                          void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     if (!attention_desc_fits(desc)) return LCN_ERR_INVALID_ARG;
-    if (desc->num_sets == 0 || desc->total_q == 0) return LCN_OK;
+    if (desc->total_q == 0 || (desc->num_sets == 0 && !desc->clear)) return LCN_OK;
     if (!q || !o || !lse || (desc->total_k > 0 && (!k || !v))) return LCN_ERR_INVALID_ARG;
+    if (desc->num_sets == 0) {
+        const int64_t rows = desc->total_q * desc->heads;
+        OPCHK(clear_all(o, rows * desc->head_dim, desc->dtype, lse, rows, (hipStream_t)hip_stream));
+        return LCN_OK;
+    }
     AttentionArgs a = args_of(desc, q, k, v);
     a.o = o;
     a.lse = lse;
@@ -197,7 +218,14 @@ lcn_status lcn_attention_backward(const lcn_attention_desc *desc, const void *q,
 {
     if (!attention_desc_fits(desc) || !dk != !dv) return LCN_ERR_INVALID_ARG;
     hipStream_t s = (hipStream_t)hip_stream;
-    if (desc->num_sets == 0 || (!dq && !dk)) return LCN_OK;
+    if ((!dq && !dk) || (desc->num_sets == 0 && !desc->clear)) return LCN_OK;
+    if (desc->num_sets == 0) {
+        const int64_t rows_q = desc->total_q * desc->heads, rows_k = desc->total_k * desc->kv_heads;
+        if (dq) OPCHK(clear_all(dq, rows_q * desc->head_dim, desc->dtype, nullptr, 0, s));
+        if (dk) OPCHK(clear_all(dk, rows_k * desc->head_dim, desc->dtype, nullptr, 0, s));
+        if (dv) OPCHK(clear_all(dv, rows_k * desc->head_dim, desc->dtype, nullptr, 0, s));
+        return LCN_OK;
+    }
     if (desc->total_q > 0 && (!q || !o || !lse || !d_o)) return LCN_ERR_INVALID_ARG;
     if (desc->total_k > 0 && (!k || !v)) return LCN_ERR_INVALID_ARG;
     const GradSpace f = grad_space((char *)workspace, desc);

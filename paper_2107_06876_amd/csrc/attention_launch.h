@@ -5,6 +5,9 @@
 
 namespace lcn {
 
+// The grid of a.groups workgroups and, where they write their outputs themselves, of those that clear the others' (see clear_others).
+static dim3 grid_with_clearers(const AttentionArgs &a, bool own) { return grid_of((long long)a.groups + (a.clear && own ? CLEARERS : 0)); }
+
 // Tiles of B tokens that sets with `total` tokens can have (see set_of_tile).
 inline long long tiles_of(long long total, int sets, int B) { return total / B + sets; }
 
@@ -14,7 +17,8 @@ static hipError_t forward_one(AttentionArgs a, hipStream_t s)
     const long long tiles = tiles_of(a.total_q, a.sets, 64 * QT);
     a.tiles = (int)tiles;
     a.groups = (unsigned)(tiles * a.heads * a.key_splits);
-    hipLaunchKernelGGL((attention_forward_kernel<T, DP, QT, VEC, SHAPE>), grid_of(a.groups), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((attention_forward_kernel<T, DP, QT, VEC, SHAPE>), grid_with_clearers(a, a.key_splits == 1), dim3(256), 0, s,
+                       a);
     return hipGetLastError();
 }
 template <class T, int DP, int QT, bool DQ, bool VEC, int SHAPE>
@@ -24,12 +28,13 @@ static hipError_t backward_one(AttentionArgs a, hipStream_t s)
         const long long tiles = tiles_of(a.total_q, a.sets, 64 * QT);
         a.tiles = (int)tiles;
         a.groups = (unsigned)(tiles * a.heads * a.key_splits);
-        hipLaunchKernelGGL((attention_dq_kernel<T, DP, QT, VEC, SHAPE>), grid_of(a.groups), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((attention_dq_kernel<T, DP, QT, VEC, SHAPE>), grid_with_clearers(a, a.dq && a.key_splits == 1), dim3(256),
+                           0, s, a);
     } else {
         const long long tiles = tiles_of(a.total_k, a.sets, 64 * QT);
         a.tiles = (int)tiles;
         a.groups = (unsigned)(tiles * a.kv_heads * a.splits);
-        hipLaunchKernelGGL((attention_dkv_kernel<T, DP, QT, VEC, SHAPE>), grid_of(a.groups), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((attention_dkv_kernel<T, DP, QT, VEC, SHAPE>), grid_with_clearers(a, a.splits == 1), dim3(256), 0, s, a);
     }
     return hipGetLastError();
 }
@@ -125,7 +130,7 @@ static hipError_t add_sums(const AttentionArgs &a, int splits, long long tokens,
 {
     const long long groups = (tokens * width / 4 + 255) / 256 + 1;
     hipLaunchKernelGGL(attention_add_kernel<T>, dim3((unsigned)(groups < 4096 ? groups : 4096), out1 ? 2 : 1), dim3(256), 0, s,
-                       a.part, splits, tokens, width, off, a.sets, (T *)out0, (T *)out1, whole ? 1 : 0);
+                       a.part, splits, tokens, width, off, a.sets, (T *)out0, (T *)out1, whole ? 1 : 0, a.clear);
     return hipGetLastError();
 }
 template <class T>

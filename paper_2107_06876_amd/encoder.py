@@ -24,7 +24,8 @@ class AttentionDesc(ctypes.Structure):
                 ("total_k", ctypes.c_int64), ("max_q", ctypes.c_int64), ("q_off", ctypes.c_void_p),
                 ("k_off", ctypes.c_void_p), ("prefix", ctypes.c_void_p), ("slopes", ctypes.c_void_p),
                 ("q_token", ctypes.c_int64), ("q_head", ctypes.c_int64), ("k_token", ctypes.c_int64),
-                ("k_head", ctypes.c_int64), ("v_token", ctypes.c_int64), ("v_head", ctypes.c_int64)]
+                ("k_head", ctypes.c_int64), ("v_token", ctypes.c_int64), ("v_head", ctypes.c_int64),
+                ("clear", ctypes.c_int32)]
 
 
 def _library():
@@ -215,7 +216,7 @@ def _attention_desc(q, k, v, q_off, k_off, scale, causal, prefix, slopes, cap, m
                          _tensor(q_off, "q_off", (sets + 1,), torch.int64, dev),
                          _tensor(k_off, "k_off", (sets + 1,), torch.int64, dev),
                          _tensor(prefix, "prefix", (sets,), torch.int32, dev),
-                         _tensor(slopes, "slopes", (q.shape[1],), torch.float32, dev), *strides(q), *strides(k), *strides(v))
+                         _tensor(slopes, "slopes", (q.shape[1],), torch.float32, dev), *strides(q), *strides(k), *strides(v), 1)
 
 
 def _attention_space(desc, backward, workspace, device):
@@ -231,7 +232,7 @@ def lcn_attention(q, k, v, q_off, k_off, scale=None, causal=False, prefix=None, 
     """(o, lse): attention of the queries of every set to the keys of the same set.  q: (tokens, heads, dim), k and v:
     (tokens, key heads, dim), views with strides are taken; q_off, k_off: int64 offsets of the sets on the device; scale:
     1 / sqrt(dim) where None; prefix: int32 per set (read if causal); slopes: float32 per head; max_q: the largest number of queries of
-    a set, where known.  o is dense like q, lse float32 (heads, tokens); queries in no set are left as they are."""
+    a set, where known.  o is dense like q, lse float32 (heads, tokens); queries in no set have 0 and -inf."""
     d = _attention_desc(q, k, v, q_off, k_off, scale, causal, prefix, slopes, cap, max_q)
     dev = q.device
     o = torch.empty(q.shape, dtype=q.dtype, device=dev)
@@ -244,7 +245,7 @@ def lcn_attention(q, k, v, q_off, k_off, scale=None, causal=False, prefix=None, 
 def lcn_attention_backward(q, k, v, o, lse, dy, q_off, k_off, scale=None, causal=False, prefix=None, slopes=None, cap=0.0,
                            max_q=0, with_q=True, with_kv=True, workspace=None):
     """(dq, dk, dv) for a given dy, the gradient of o; o and lse as lcn_attention returned them, the rest as it was
-    given.  Gradients are dense; those that are not asked for are None."""
+    given.  Gradients are dense, zero for tokens in no set; those that are not asked for are None."""
     d = _attention_desc(q, k, v, q_off, k_off, scale, causal, prefix, slopes, cap, max_q)
     dev = q.device
     shape = tuple(q.shape)

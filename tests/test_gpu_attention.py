@@ -403,3 +403,53 @@ def test_gradients_of_keys_without_those_of_queries(how, dtype):
         assert none_q is None and none_k is None and none_v is None
         for u, w in zip((dq, dk, dv), all_three):
             assert torch.equal(u, w)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("max_q", [0, 2])
+@pytest.mark.parametrize("nq,nk", [([1, 2, 1], [300, 900, 5]), ([70, 200], [70, 200])])
+def test_tokens_in_no_set(nq, nk, max_q, dtype):
+    """Before the first and behind the last set: o and all gradients are zero, lse is -inf."""
+    if max(nq) > 2:
+        max_q = 0
+    g = generator(34)
+    before, behind = 37, 150
+    q, do = (normal(g, before + sum(nq) + behind, 4, 64, dtype=dtype) for _ in range(2))
+    k, v = (normal(g, before + sum(nk) + behind, 2, 64, dtype=dtype) for _ in range(2))
+    qo, ko = offsets(nq) + before, offsets(nk) + before
+    for t in (q, k):   # what torch hands out next has been used
+        for _ in range(4):
+            torch.full(t.shape, 7.0, dtype=dtype, device=DEV)
+    torch.full((4, q.shape[0]), 7.0, device=DEV)
+    o, lse = lcn.lcn_attention(q, k, v, qo, ko, max_q=max_q)
+    dq, dk, dv = lcn.lcn_attention_backward(q, k, v, o, lse, do, qo, ko, max_q=max_q)
+    for t, n in ((o, sum(nq)), (dq, sum(nq)), (dk, sum(nk)), (dv, sum(nk))):
+        assert not t[:before].any() and not t[before + n:].any() and t[before:before + n].any()
+    assert (lse[:, :before] == -math.inf).all() and (lse[:, before + sum(nq):] == -math.inf).all()
+    none = torch.zeros(1, dtype=torch.int64, device=DEV)   # no sets at all
+    o, lse = lcn.lcn_attention(q, k, v, none, none, max_q=max_q)
+    grads = lcn.lcn_attention_backward(q, k, v, o, lse, do, none, none, max_q=max_q)
+    assert not o.any() and (lse == -math.inf).all() and not any(t.any() for t in grads)
+
+
+def test_tokens_in_no_set_of_a_caller_that_keeps_them():
+    """Without `clear` the C entry points leave such tokens' memory alone: two calls may share an output."""
+    import ctypes
+    from paper_2107_06876_amd import encoder
+    g = generator(38)
+    q, do = (normal(g, 200, 2, 64) for _ in range(2))
+    o, dq, dk, dv = (torch.full_like(q, 7.0) for _ in range(4))
+    lse = torch.full((2, 200), 7.0, device=DEV)
+    off_ = torch.tensor([30, 100, 150], device=DEV)
+    for clear in (0, 1):
+        d = encoder._attention_desc(q, q, q, off_, off_, None, False, None, None, 0.0, 0)
+        d.clear = clear
+        for back in (0, 1):
+            at, size, space = encoder._attention_space(d, back, None, q.device)
+            more = ((o, lse, do, dq, dk, dv) if back else (o, lse))
+            encoder._call("lcn_attention_backward" if back else "lcn_attention", q.device, ctypes.byref(d), q.data_ptr(), q.data_ptr(),
+                          q.data_ptr(), *(t.data_ptr() for t in more), at, size)
+        for t in (o, dq, dk, dv):
+            assert (t[:30] == 7.0 * (1 - clear)).all() and (t[150:] == 7.0 * (1 - clear)).all() and (t[30:150] != 7.0).any()
+        left = -math.inf if clear else 7.0
+        assert (lse[:, :30] == left).all() and (lse[:, 150:] == left).all() and torch.isfinite(lse[:, 30:150]).all()
