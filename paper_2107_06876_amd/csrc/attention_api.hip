@@ -64,6 +64,11 @@ static int shape_of(const AttentionArgs &a)
     return a.cap == 0.f ? PLAIN : a.cap <= MOST_CAP ? CAPPED : SHAPED;
 }
 
+// Rows of a set's chunks: no set has more queries than there are.
+static int64_t chunk_rows(const lcn_attention_desc *d)
+{
+    return (d->max_q < d->total_q ? d->max_q : d->total_q) * (d->heads / d->kv_heads);
+}
 // Where a set has few queries, its keys are split over workgroups: up to 32 rows (queries times the heads that share a key
 // head) fit a wavefront.  Chunks of keys are so long that there are some eight workgroups per compute unit, from 128 keys (a
 // step of a workgroup's wavefronts) to 2048.  0: not split, as also where a set has less than 128 keys on average.
@@ -71,7 +76,7 @@ static int shape_of(const AttentionArgs &a)
 // sets of 1000 keys: 22 (21), 38 (41); one query for 256 sets of 128 keys: 15 (16), 28 (54).
 static int chunk_of(const lcn_attention_desc *d)
 {
-    const int64_t rows = d->max_q * (d->heads / d->kv_heads);
+    const int64_t rows = chunk_rows(d);
     if (d->max_q == 0 || rows > 32 || d->total_k < 128LL * d->num_sets) return 0;
     const int64_t keys = d->total_k * d->kv_heads / 2048;
     const int64_t chunk = (keys + 127) / 128 * 128;
@@ -130,7 +135,7 @@ static ForwardSpace forward_space(char *ws, const lcn_attention_desc *d)
     f.key_splits = 1;
     size_t n = 0;
     if (f.chunk) {
-        f.rows = (int)(d->max_q * (d->heads / d->kv_heads));
+        f.rows = (int)chunk_rows(d);
         n = (size_t)(d->total_k / f.chunk + d->num_sets) * d->kv_heads * f.rows;
     } else if ((f.key_splits = key_splits(d)) > 1) {
         n = (size_t)f.key_splits * d->total_q * d->heads;

@@ -139,3 +139,17 @@ def test_results_with_more_tiles_than_are_numbered(lib, rows, a, b):
             assert _bytes(f, rows // 2, a, b // 2 + 1 if b > a else b, BF16, backward)[0] == OK
     assert lib.lcn_linear(FAKE, FAKE, None, None, rows, a, b, BF16, 0, FAKE, None, FAKE, 1 << 62, None) == ERR_INVALID_ARG
     assert lib.lcn_cross_entropy(FAKE, FAKE, None, FAKE, rows, b, a, BF16, 1.0, FAKE, FAKE, FAKE, 1 << 62, None) == ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(4, 2), (4, 1), (8, 1)])
+def test_a_largest_number_of_queries_beyond_all_queries(lib, heads, kv_heads):
+    """max_q says no more than total_q does; times the heads of a group it must not wrap around."""
+    def space(max_q):
+        out = ctypes.c_size_t(0)
+        assert lib.lcn_attention_workspace_bytes(_desc(heads=heads, kv_heads=kv_heads, total_q=3, total_k=600, max_q=max_q), 0,
+                                                 ctypes.byref(out)) == OK
+        return out.value
+    want = space(3)
+    assert want > 0
+    for max_q in (4, 1 << 20, 1 << 59, 1 << 61, 1 << 62, (1 << 63) - 1):
+        assert space(max_q) == want
