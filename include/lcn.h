@@ -459,13 +459,13 @@ typedef struct {
     int64_t total_q, total_k; /* tokens in q and in k, v */
     int64_t max_q;            /* the largest number of queries of a set where the caller knows it, else 0: with
                                  few queries per set the keys are then split over workgroups.  A set must
-                                 not have more (what is beyond is not written) */
+                                 not have more (what is beyond may not be computed; see `clear`) */
     const int64_t *q_off, *k_off; /* device, num_sets + 1 each */
     const int32_t *prefix;    /* device, num_sets, nullable (0); read if causal */
     const float *slopes;      /* device, heads, nullable */
     int64_t q_token, q_head, k_token, k_head, v_token, v_head; /* strides in elements */
     int32_t clear;            /* 1: tokens before the first and behind the last set get o = 0, lse = -inf and gradients of
-                                 zero; 0: these are not written */
+                                 zero, queries beyond max_q that are not computed get NaN; 0: these are not written */
 } lcn_attention_desc;
 lcn_status lcn_attention_workspace_bytes(const lcn_attention_desc *desc, int32_t backward, size_t *bytes);
 lcn_status lcn_attention(const lcn_attention_desc *desc, const void *q, const void *k, const void *v, void *o, float *lse,

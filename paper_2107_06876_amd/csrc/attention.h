@@ -501,14 +501,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
     }
 }
 
-// The row of a query and head that is in no set, by a wavefront.
+// The row of a query and head that is not computed, by a wavefront: it gets `value`, and this lse.
 template <class T>
-__device__ __forceinline__ void clear_row(const AttentionArgs &a, long long row, int lane)
+__device__ __forceinline__ void clear_row(const AttentionArgs &a, long long row, int lane, float value, float lse)
 {
     T *out = (T *)a.o + row * a.dim;
-    if (lane < a.dim) out[lane] = (T)0.f;
-    if (lane + 64 < a.dim) out[lane + 64] = (T)0.f;
-    if (lane == 0) a.lse[row % a.heads * a.total_q + row / a.heads] = minus_infinity();
+    if (lane < a.dim) out[lane] = (T)value;
+    if (lane + 64 < a.dim) out[lane + 64] = (T)value;
+    if (lane == 0) a.lse[row % a.heads * a.total_q + row / a.heads] = lse;
 }
 
 // Joins the splits of a query and head, a wavefront each, in their order.  Bound by memory, and small where splits are chosen.
@@ -519,7 +519,7 @@ __global__ __launch_bounds__(256) void attention_join_splits_kernel(AttentionArg
     const int head = (int)(row % a.heads), lane = threadIdx.x & 63;
     if (n >= a.total_q) return;
     if (n < a.q_off[0] || n >= a.q_off[a.sets]) {
-        if (a.clear) clear_row<T>(a, row, lane);
+        if (a.clear) clear_row<T>(a, row, lane, 0.f, minus_infinity());
         return;
     }
     float most = minus_infinity();
@@ -730,8 +730,12 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a)
     const int p = last_set(a.sets, [&](int q) { return a.q_off[q] <= n; });
     const SetRange s = range_of(a, p);
     const long long i = n - s.q0, r = i * group + head % group;
-    if (a.clear && (n < a.q_off[0] || n >= a.q_off[a.sets])) return clear_row<T>(a, row, lane);
-    if (i < 0 || i >= s.nq || r >= a.rows) return;
+    if (a.clear && (n < a.q_off[0] || n >= a.q_off[a.sets])) return clear_row<T>(a, row, lane, 0.f, minus_infinity());
+    if (i < 0 || i >= s.nq) return;
+    if (r >= a.rows) {   // the set has more than max_q queries
+        if (a.clear) clear_row<T>(a, row, lane, __builtin_nanf(""), __builtin_nanf(""));
+        return;
+    }
     const long long first = s.k0 / a.chunk + p;
     const int chunks = (s.nk + a.chunk - 1) / a.chunk;
     const long long stride = (long long)a.kv_heads * a.rows, at = (first * a.kv_heads + kv) * a.rows + r;

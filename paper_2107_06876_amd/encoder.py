@@ -232,7 +232,8 @@ def lcn_attention(q, k, v, q_off, k_off, scale=None, causal=False, prefix=None, 
     """(o, lse): attention of the queries of every set to the keys of the same set.  q: (tokens, heads, dim), k and v:
     (tokens, key heads, dim), views with strides are taken; q_off, k_off: int64 offsets of the sets on the device; scale:
     1 / sqrt(dim) where None; prefix: int32 per set (read if causal); slopes: float32 per head; max_q: the largest number of queries of
-    a set, where known.  o is dense like q, lse float32 (heads, tokens); queries in no set have 0 and -inf."""
+    a set, where known.  o is dense like q, lse float32 (heads, tokens); queries in no set have 0 and -inf,
+    those that a max_q below the truth leaves out NaN."""
     d = _attention_desc(q, k, v, q_off, k_off, scale, causal, prefix, slopes, cap, max_q)
     dev = q.device
     o = torch.empty(q.shape, dtype=q.dtype, device=dev)

@@ -453,3 +453,19 @@ def test_tokens_in_no_set_of_a_caller_that_keeps_them():
             assert (t[:30] == 7.0 * (1 - clear)).all() and (t[150:] == 7.0 * (1 - clear)).all() and (t[30:150] != 7.0).any()
         left = -math.inf if clear else 7.0
         assert (lse[:, :30] == left).all() and (lse[:, 150:] == left).all() and torch.isfinite(lse[:, 30:150]).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_more_queries_than_max_q_says(dtype):
+    """What a hint below the truth leaves out is not a number, and not what the memory held."""
+    g = generator(39)
+    q, k = normal(g, 8, 4, 64, dtype=dtype), normal(g, 2000, 2, 64, dtype=dtype)
+    qo, ko = offsets([2, 5, 1]), offsets([700, 800, 500])
+    for _ in range(4):
+        torch.full(q.shape, 7.0, dtype=dtype, device=DEV)
+        torch.full((4, 8), 7.0, device=DEV)
+    o, lse = lcn.lcn_attention(q, k, k, qo, ko, max_q=2)
+    want, l = lcn.lcn_attention(q, k, k, qo, ko, max_q=5)
+    kept = torch.tensor([0, 1, 2, 3, 7], device=DEV)
+    assert torch.equal(o[kept], want[kept]) and torch.equal(lse[:, kept], l[:, kept])
+    assert torch.isnan(o[4:7]).all() and torch.isnan(lse[:, 4:7]).all()
