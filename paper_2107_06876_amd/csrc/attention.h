@@ -662,6 +662,13 @@ __global__ __launch_bounds__(WAVES * 64) void attention_chunk_kernel(AttentionAr
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     };
+    // The buffer has been read: the next loads into it come behind the last read, by a wait and not by the order in which the
+    // instructions that use what was read happen to stand.
+    auto read = [&]() {
+        __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
     constexpr int STEP = WAVES * BK;
     int j0 = k_first + wave * BK;
     if (j0 < k_end) fetch(j0, lds0);
@@ -670,14 +677,12 @@ __global__ __launch_bounds__(WAVES * 64) void attention_chunk_kernel(AttentionAr
         if (second) fetch(j0 + STEP, lds1);
         arrived(second);
         work(j0, lds0);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // the buffer has been read
-        __builtin_amdgcn_wave_barrier();
+        read();
         if (!second) break;
         if (third) fetch(j0 + 2 * STEP, lds0);
         arrived(third);
         work(j0 + STEP, lds1);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        read();
     }
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
