@@ -469,3 +469,44 @@ def test_more_queries_than_max_q_says(dtype):
     kept = torch.tensor([0, 1, 2, 3, 7], device=DEV)
     assert torch.equal(o[kept], want[kept]) and torch.equal(lse[:, kept], l[:, kept])
     assert torch.isnan(o[4:7]).all() and torch.isnan(lse[:, 4:7]).all()
+
+
+# ---- forms that the tests above leave out ------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dim,shift", [(1, 0), (20, 0), (100, 0), (64, 1), (128, 1)])
+@pytest.mark.parametrize("how", [dict(), dict(causal=True, prefix=[4, 2500, 0, 500])])
+def test_new_tokens_without_whole_pieces(how, dim, shift, dtype):
+    """Keys split over workgroups, read one value at a time: odd widths and addresses, also behind a prefix."""
+    check([1, 3, 2, 3], [129, 3000, 64, 700], 8, 2, dim, dtype, shift=shift, max_q=3, **how)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("how", [dict(causal=True, prefix=[900, 0, 1]), dict(causal=True, prefix=[1000, 3, 650], cap=20.0, slopes=[0.01] * 8)])
+def test_new_tokens_behind_a_prefix(how, dtype):
+    check([4, 2, 1], [1000, 400, 700], 8, 2, 64, dtype, max_q=4, **how)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dim,shift", [(33, 0), (7, 0), (64, 1), (65, 3)])
+@pytest.mark.parametrize("how", [dict(), dict(causal=True)])
+def test_few_tiles_without_whole_pieces(how, dim, shift, dtype):
+    """Sums of several workgroups whose rows are no whole pieces, and whose number is odd."""
+    check([151], [3001], 1, 1, dim, dtype, shift=shift, **how)
+    check([2501], [151], 3, 1, dim, dtype, shift=shift, **how)
+
+
+@pytest.mark.parametrize("dim", [32, 64, 128])
+@pytest.mark.parametrize("cap", [3.0, 30.0, 39.5, 50.0])
+@pytest.mark.parametrize("how", [dict(), dict(causal=True), dict(causal=True, prefix=[20, 400, 0])])
+def test_capped_documents(how, cap, dim):
+    """Caps on whole rows of bf16, under all masks and at all widths."""
+    check([90, 500, 33], [90, 500, 33], 4, 1, dim, BF16, cap=cap, size=2.0, **how)
+    check([90, 140, 33], [300, 700, 33], 2, 2, dim, BF16, cap=cap, **how)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_peaked_softmax_over_many_keys(dtype):
+    """Steep slopes: the weight of a row lies on few of its 1000 keys, and o is as large as one v."""
+    check([1000], [1000], 2, 1, 64, dtype, causal=True, slopes=[4.0, 1.0])

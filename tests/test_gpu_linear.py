@@ -185,3 +185,30 @@ def test_refusals():
         lcn.lcn_linear(torch.ones(99, 6, device=DEV), w, workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
     with pytest.raises(lcn.LcnError):   # an activation's gradient needs z
         lcn.lcn_linear_backward(x, w, None, torch.ones(4, 3, device=DEV), activation=lcn.ACT_TANH)
+
+
+# ---- forms that the tests above leave out ------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("rows,d_in,d_out", [(128, 8, 64), (300, 64, 200), (1000, 40, 33), (777, 128, 64), (515, 96, 20)])
+def test_narrow_layers(rows, d_in, d_out, act, dtype):
+    """Few inputs and outputs, rows of whole pieces: up to 32, 64 and 128 inputs, every activation."""
+    check(rows, d_in, d_out, act, dtype)
+    check(rows, d_in, d_out, act, dtype, bias=False, residual=False)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("act", ["none", "gelu"])
+@pytest.mark.parametrize("rows,shift", [(5, 0), (300, 0), (700, 0), (300, 1)])
+def test_single_gradients(rows, shift, act, dtype):
+    """dx, dw and db have the same bits whichever are asked for."""
+    g = generator(16, rows)
+    x, w = normal(g, rows, 72, dtype=dtype, shift=shift), normal(g, 136, 72, dtype=dtype, shift=shift)
+    dy, z = normal(g, rows, 136, dtype=dtype, shift=shift), normal(g, rows, 136)
+    want = lcn.lcn_linear_backward(x, w, z, dy, activation=ACTS[act])
+    for asked in ((1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 1, 0), (1, 0, 1), (0, 1, 1), (0, 0, 0)):
+        got = lcn.lcn_linear_backward(x, w, z, dy, activation=ACTS[act], with_x=asked[0], with_w=asked[1], with_bias=asked[2])
+        for a, u, v in zip(asked, got, want):
+            assert torch.equal(u, v) if a else u is None

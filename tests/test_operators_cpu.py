@@ -153,3 +153,12 @@ def test_a_largest_number_of_queries_beyond_all_queries(lib, heads, kv_heads):
     assert want > 0
     for max_q in (4, 1 << 20, 1 << 59, 1 << 61, 1 << 62, (1 << 63) - 1):
         assert space(max_q) == want
+
+
+def test_backward_workspaces_of_a_cross_entropy(lib):
+    for dtype in (F32, BF16):
+        for rows, dim, vocab in ((1, 16, 16), (20, 300, 600), (5000, 300, 20000), (70000, 1024, 4096)):
+            st, n = _bytes(lib.lcn_cross_entropy_workspace_bytes, rows, vocab, dim, dtype, 1)
+            assert st == OK and n > 0
+            assert lib.lcn_cross_entropy_backward(FAKE, FAKE, None, FAKE, FAKE, FAKE, rows, vocab, dim, dtype, 1.0, FAKE, FAKE, FAKE,
+                                                  FAKE, n - 1, None) == ERR_ALLOC
