@@ -43,3 +43,24 @@ def normal(g, *shape, dtype=F32, scale=1.0, shift=0):
     flat = torch.zeros(n + shift, dtype=dtype, device=DEV)
     flat[shift:] = (scale * torch.randn(n, generator=g)).to(dtype).to(DEV)
     return flat[shift:].view(*shape)
+
+
+# One rounding to bf16 by its statistics: half a unit in the last place is spread evenly, 2^-7 / sqrt(12) of the power of two below a
+# value, which in the 2-norm over normally distributed ones is 0.734 to 0.737 of them, whatever their deviation (0.65 to 0.69 over
+# values spread evenly, or evenly over octaves).  Independent roundings add in squares: two are 1.41 of one, so that a bound of 1.1
+# tells one from two, and two from three.
+ROUNDING = 0.737 * 2.0 ** -7 / math.sqrt(12.0)
+
+
+def roundings(n):
+    """The 2-norm of n independent roundings to bf16, with a tenth of room."""
+    return 1.1 * ROUNDING * math.sqrt(n)
+
+
+def farthest(got, want):
+    """The largest error of a value of bf16 tensors over what it may be: 2^-8 of the value (its own rounding) and 2^-6.5 of the root
+    mean square of its row (last dimension): 7 deviations of a sum whose terms were each rounded once."""
+    got, want = got.double(), want.double()
+    assert got.shape == want.shape and torch.isfinite(got).all()
+    row = want.square().mean(-1, keepdim=True).sqrt()
+    return ((got - want).abs() / (2.0 ** -8 * want.abs() + 2.0 ** -6.5 * row + 1e-30)).max().item()
