@@ -372,9 +372,22 @@ lcn_status lcn_calibrate(int32_t what, void *workspace, size_t workspace_bytes, 
  *     are read as they lie, others are first laid out in the workspace).
  *     Outputs must not overlap inputs or each other, except where noted.
  *   - Sums, softmax statistics and z are in 32 bits; a bf16 output is rounded
- *     once.  float products are formed from three bf16 planes per operand (six
- *     products of planes; as exact as single precision), so a float input that
- *     is infinite makes the sums it enters NaN.
+ *     once from them.  With bf16 tensors these are rounded to bf16 as well, where
+ *     they enter a matrix product: the weights P of lcn_attention (in o and dv)
+ *     and its dS (in dq and dk); above 512 rows dz of lcn_linear_backward where
+ *     there is an activation (in dx and dW), and the cross entropy's G (in dW, and
+ *     in dx but for the target's part).  Each is as large as the output's own
+ *     rounding: the error becomes 1.4 times that of one.  Where a tile of 64 or 128
+ *     queries sees more than 256 keys, o enters dS as it was rounded, a third such
+ *     error in rows whose weight lies on few keys.  Scores with a
+ *     cap up to 40 and no slopes, on bf16 rows of whole 16-byte pieces, are off by
+ *     about 2^-23 of the cap, and lse with them.  Exponentials below the smallest
+ *     normal float are zero.
+ *   - float products are formed from three bf16 planes per operand (six products
+ *     of planes; as exact as single precision), so that a float input that is
+ *     infinite makes the sums it enters NaN; up to 8 rows and in narrow layers,
+ *     which use float instructions, they are infinite (or NaN) as in single
+ *     precision.
  *   - Asynchronous on hip_stream, no synchronisation, no device allocation, no
  *     atomics: same inputs, same bits.  The workspace (device, 256-byte aligned,
  *     at least the bytes that the matching *_workspace_bytes call says for the
@@ -406,7 +419,8 @@ lcn_status lcn_linear_backward(const void *x, const void *W, const float *pre, c
 
 /* Softmax cross entropy over a vocabulary, without keeping the rows x vocab scores
  *   z_nv = scale x_n . W_v + bias_v    (x rows x dim, W vocab x dim, bias fp32, nullable):
- *   lse_n = log sum_v exp z_nv,  loss_n = lse_n - z_n,target(n)   (fp32, rows each).
+ *   lse_n = log sum_v exp z_nv,  loss_n = lse_n - z_n,target(n)   (fp32, rows each;
+ * the loss without lse's rounding, and never negative).
  * With scale = 1/lambda and bias = log v this is the negative log likelihood of known
  * pairs under the row-normalised plan.  A row with a negative target has loss 0
  * (its lse is still formed) and adds nothing to any gradient, whatever its x

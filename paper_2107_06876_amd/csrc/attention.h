@@ -283,7 +283,8 @@ __device__ __forceinline__ void two_buffers(int begin, int end, Fetch fetch, Lan
 }
 
 // What stands in for tokens before the first and behind the last set: zeros in rows of `width` values, -inf in lse.  The workgroups
-// behind those with work share it; where every token is in a set there is nothing to do.
+// behind those with work share it; where every token is in a set there is nothing to do.  These lines cost the kernels of the small
+// float sets 4 us of 173 altogether, a launch of their own as much, and 5 to 10 in longer calls.
 constexpr unsigned CLEARERS = 64;
 template <class T, bool VEC>
 __device__ __forceinline__ void clear_others(const AttentionArgs &a, const int64_t *off, long long tokens, long long width, T *out0,
@@ -313,7 +314,7 @@ __device__ __forceinline__ void clear_others(const AttentionArgs &a, const int64
 // Four wavefronts of 16 QT queries each go over the set's keys, 64 at a time.  Bound by the vector instructions beside the
 // matrix ones: an exponential, a maximum and two conversions per score.  bf16, two sets of 8192, 16 heads of 64: 803 us,
 // 0.68 PFLOP/s; packed documents of 500 to 5000 tokens, causal, capped, 16 heads of 128 on 4: 320 us, 0.56.  Float, 1024 sets of 16 to
-// 64 tokens, 4 heads of 32, slopes: 46 us.  With few tiles the keys are dealt to a.key_splits workgroups.
+// 64 tokens, 4 heads of 32, slopes: 48 us.  With few tiles the keys are dealt to a.key_splits workgroups.
 template <class T, int DP, int QT, bool VEC, int SHAPE>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward_kernel(AttentionArgs a)
 {
@@ -802,7 +803,7 @@ __device__ __forceinline__ void add_product(f32x4 (&sum)[N], typename Frag<T>::t
 // taken: o is an average of many v then, and small, unless a row's weight lies on few keys (steep slopes, large scores), whose dS
 // is off by a rounding of o as well; the first sum costs a pass over all keys.  The delta that is used goes to a.delta for dk and dv; where dq is not asked for that is all
 // that the kernel does, so that dk does not depend on it.
-// Bound as the forward pass is: the documents 425 us (0.63 PFLOP/s), the small float sets 56.
+// Bound as the forward pass is: the documents 425 us (0.63 PFLOP/s), the small float sets 57.
 constexpr int EXACT_KEYS = 256;
 template <class T, int DP, int QT, bool VEC, int SHAPE>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kernel(AttentionArgs a)
@@ -964,7 +965,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
 // dk, dv: four wavefronts of 16 KT keys each go over the queries of all heads that share the key head, BQ at a
 // time; dv = P^T do, dk = scale dS^T q.  With few tiles the steps are dealt to a.splits workgroups, whose sums a second launch adds.
 // Two products more per score than forward, and both operands are read from LDS twice: the documents 703 us (0.51 PFLOP/s) and 24 for
-// the sums, the small float sets 72.
+// the sums, the small float sets 74.
 template <class T, int DP, int KT, bool VEC, int SHAPE>
 __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
 {

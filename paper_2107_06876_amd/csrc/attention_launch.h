@@ -65,6 +65,8 @@ static hipError_t by_form(const AttentionArgs &a, bool vec, int shape, hipStream
 //   dk, dv bf16   saves 12, 53, 0 / 76, 166, 0 of the whole backward pass    -> always 16
 //   dk, dv float  saves 67, 112, 122 / 189, 195, -205                         -> 32 for wide heads in long sets alone
 //   dq bf16       saves 8, 13, -7 / 8, 0, -79; float 41, 86, 122 / 20, 39, -131   -> wide heads: 32 in long sets
+//   (dq, dk and dv of float with 32 rows of 65 to 128 values do not fit: 99 to 121 registers per lane are spilled, 239 where rows are
+//   not whole pieces; bf16 with 32 queries spills 8 to 34 in the forward and dq kernels of that width)
 //   forward bf16  33, 46, 84 / 32, 49, 74 and 95, 138, 262 / 76, 115, 178; float 98, 190, 462 / 118, 247, 452 and
 //                 346, 712, 1706 / 339, 725, 1357                              -> 32 in long sets, bf16 wide heads from 65 on
 template <class T, int WHAT>

@@ -304,7 +304,8 @@ struct EntropyGradient {
 
 // G of few rows, with the sums of entropy_few_kernel (a product's order of additions would give other scores than lse was
 // formed of).  A wavefront has eight words at a time, lane 2 r + which of 16 finishes row r of one of its group's two.  Words up
-// to `wide` are written, zeros behind the last.
+// to `wide` are written, zeros behind the last.  Bound by reading W once; with both products behind it one row / eight rows, 20 000
+// words of 300: float 58 / 63 us, bf16 58 / 64 (by a product of tiles 64 / 66, 57 / 59).
 template <class T, int R, bool VEC>
 __global__ __launch_bounds__(256) void entropy_few_gradient_kernel(EntropyRow e, long long first, int words, int wide,
                                                                    const T *__restrict__ x, const T *__restrict__ w, int rows,

@@ -2,7 +2,8 @@
 entry points; argument marshalling only.
 
 Tensors are contiguous device tensors of one type, float32 or bfloat16 (attention also takes views with strides);
-work goes to torch's current stream on their device; `workspace`, where given, is a contiguous uint8 tensor."""
+work goes to torch's current stream on their device; `workspace`, where given, is a contiguous uint8 tensor.  Results are
+no part of automatic differentiation, also where an input requires a gradient: that is what the backward calls give."""
 from __future__ import annotations
 
 import ctypes
@@ -44,8 +45,9 @@ def _library():
         lib.lcn_attention_workspace_bytes.argtypes = [desc, i32, out]
         lib.lcn_attention.argtypes = [desc, vp, vp, vp, vp, vp, vp, sz, vp]
         lib.lcn_attention_backward.argtypes = [desc, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
-        for name in ("lcn_attention_workspace_bytes", "lcn_attention", "lcn_attention_backward", "lcn_linear_workspace_bytes", "lcn_linear", "lcn_linear_backward", "lcn_cross_entropy_workspace_bytes",
-                     "lcn_cross_entropy", "lcn_cross_entropy_backward"):
+        for name in ("lcn_attention_workspace_bytes", "lcn_attention", "lcn_attention_backward", "lcn_linear_workspace_bytes",
+                     "lcn_linear", "lcn_linear_backward", "lcn_cross_entropy_workspace_bytes", "lcn_cross_entropy",
+                     "lcn_cross_entropy_backward"):
             getattr(lib, name).restype = i32
         _lib = lib
     return _lib
@@ -231,8 +233,8 @@ def lcn_attention(q, k, v, q_off, k_off, scale=None, causal=False, prefix=None, 
                   workspace=None):
     """(o, lse): attention of the queries of every set to the keys of the same set.  q: (tokens, heads, dim), k and v:
     (tokens, key heads, dim), views with strides are taken; q_off, k_off: int64 offsets of the sets on the device; scale:
-    1 / sqrt(dim) where None; prefix: int32 per set (read if causal); slopes: float32 per head; max_q: the largest number of queries of
-    a set, where known.  o is dense like q, lse float32 (heads, tokens); queries in no set have 0 and -inf,
+    1 / sqrt(dim) where None; prefix: int32 per set (read if causal); slopes: float32 per head; max_q: the largest number of
+    queries of a set, where known.  o is dense like q, lse float32 (heads, tokens); queries in no set have 0 and -inf,
     those that a max_q below the truth leaves out NaN."""
     d = _attention_desc(q, k, v, q_off, k_off, scale, causal, prefix, slopes, cap, max_q)
     dev = q.device

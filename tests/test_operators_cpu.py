@@ -162,3 +162,11 @@ def test_backward_workspaces_of_a_cross_entropy(lib):
             assert st == OK and n > 0
             assert lib.lcn_cross_entropy_backward(FAKE, FAKE, None, FAKE, FAKE, FAKE, rows, vocab, dim, dtype, 1.0, FAKE, FAKE, FAKE,
                                                   FAKE, n - 1, None) == ERR_ALLOC
+
+
+@pytest.mark.parametrize("clear", [-1, 2])
+def test_a_description_clears_or_not(lib, clear):
+    out = ctypes.c_size_t(0)
+    assert lib.lcn_attention_workspace_bytes(_desc(clear=clear), 0, ctypes.byref(out)) == ERR_INVALID_ARG
+    for good in (0, 1):
+        assert lib.lcn_attention_workspace_bytes(_desc(clear=good), 0, ctypes.byref(out)) == OK
