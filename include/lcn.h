@@ -493,6 +493,24 @@ lcn_status lcn_attention_backward(const lcn_attention_desc *desc, const void *q,
                                   const float *lse, const void *dy, void *dq, void *dk, void *dv, void *workspace,
                                   size_t workspace_bytes, void *hip_stream);
 
+/* Layer norm of every row of x, rows x dim: with the mean and the variance of the row,
+ *   y = (x - mean) rstd weight + bias,  rstd = 1 / sqrt(mean of (x - mean)^2 + eps).
+ * weight, bias (dim, of type dtype) are nullable (1 and 0); mean, rstd (fp32, rows;
+ * nullable): what the backward pass takes.  y may be x.  A row that holds a value that is not
+ * finite becomes NaN.  Sizes: 0 <= rows <= 2^30, 1 <= dim <= 2^20, their product <= 2^42; eps
+ * finite and >= 0 (0: rows of equal values become NaN).  No workspace. */
+lcn_status lcn_layer_norm(const void *x, const void *weight, const void *bias, int64_t rows, int32_t dim, int32_t dtype, float eps,
+                          void *y, float *mean, float *rstd, void *hip_stream);
+/* Its gradients for a given dy: with xhat = (x - mean) rstd and g = dy .* weight,
+ *   dx = rstd (g - rowmean(g) - xhat rowmean(g .* xhat)) + around,
+ *   dweight = sum over rows of dy .* xhat,  dbias = sum over rows of dy.
+ * around (nullable, rows x dim): the gradient that reaches x past the norm, as a residual's.
+ * dx may be around.  dx, dweight, dbias are nullable. */
+lcn_status lcn_layer_norm_workspace_bytes(int64_t rows, int32_t dim, int32_t dtype, size_t *bytes);   /* of the backward pass */
+lcn_status lcn_layer_norm_backward(const void *x, const void *weight, const float *mean, const float *rstd, const void *dy,
+                                   const void *around, int64_t rows, int32_t dim, int32_t dtype, void *dx, void *dweight,
+                                   void *dbias, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 void lcn_destroy(lcn_handle h); /* frees host memory only; the workspace is the caller's */
 const char *lcn_status_string(int32_t status);
 

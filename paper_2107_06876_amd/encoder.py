@@ -45,9 +45,12 @@ def _library():
         lib.lcn_attention_workspace_bytes.argtypes = [desc, i32, out]
         lib.lcn_attention.argtypes = [desc, vp, vp, vp, vp, vp, vp, sz, vp]
         lib.lcn_attention_backward.argtypes = [desc, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.lcn_layer_norm.argtypes = [vp, vp, vp, i64, i32, i32, f32, vp, vp, vp, vp]
+        lib.lcn_layer_norm_workspace_bytes.argtypes = [i64, i32, i32, out]
+        lib.lcn_layer_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i32, i32, vp, vp, vp, vp, sz, vp]
         for name in ("lcn_attention_workspace_bytes", "lcn_attention", "lcn_attention_backward", "lcn_linear_workspace_bytes",
                      "lcn_linear", "lcn_linear_backward", "lcn_cross_entropy_workspace_bytes", "lcn_cross_entropy",
-                     "lcn_cross_entropy_backward"):
+                     "lcn_cross_entropy_backward", "lcn_layer_norm", "lcn_layer_norm_workspace_bytes", "lcn_layer_norm_backward"):
             getattr(lib, name).restype = i32
         _lib = lib
     return _lib
@@ -183,6 +186,44 @@ def lcn_cross_entropy_backward(x, w, target, lse, grad_loss, bias=None, scale=1.
           _tensor(target, "target", (rows,), torch.int64, dev), _tensor(lse, "lse", (rows,), torch.float32, dev),
           _tensor(grad_loss, "grad_loss", (rows,), torch.float32, dev), rows, vocab, dim, dtype, float(scale), _address(dx),
           _address(dw), _address(db), at, size)
+    return dx, dw, db
+
+
+def _rows(x):
+    """Rows, width and type of a contiguous device matrix."""
+    dtype = _TYPES.get(x.dtype)
+    if dtype is None or x.dim() != 2 or not x.is_cuda or not x.is_contiguous() or x.shape[1] == 0:
+        raise ValueError("x: expected a contiguous float32 or bfloat16 matrix on a device")
+    return x.shape[0], x.shape[1], dtype
+
+
+def lcn_layer_norm(x, weight=None, bias=None, eps=1e-5, keep_stats=False, out=None):
+    """(x - mean) / sqrt(variance + eps) weight + bias, row by row; with keep_stats also mean and 1 / sqrt(variance + eps) in
+    float32, which lcn_layer_norm_backward takes.  out may be x."""
+    rows, dim, dtype = _rows(x)
+    dev = x.device
+    y = torch.empty_like(x) if out is None else out
+    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=dev) if keep_stats else (None, None)
+    _call("lcn_layer_norm", dev, x.data_ptr(), _tensor(weight, "weight", (dim,), x.dtype, dev),
+          _tensor(bias, "bias", (dim,), x.dtype, dev), rows, dim, dtype, float(eps), _tensor(y, "out", (rows, dim), x.dtype, dev),
+          _address(mean), _address(rstd))
+    return (y, mean, rstd) if keep_stats else y
+
+
+def lcn_layer_norm_backward(x, weight, mean, rstd, dy, around=None, with_x=True, with_weight=True, with_bias=True,
+                            workspace=None):
+    """(dx, dweight, dbias) for a given dy; mean and rstd as lcn_layer_norm kept them; around: the gradient that reaches x past
+    the norm, added to dx.  Gradients that are not asked for are None."""
+    rows, dim, dtype = _rows(x)
+    dev = x.device
+    dx = torch.empty_like(x) if with_x else None
+    dw = torch.empty(dim, dtype=x.dtype, device=dev) if with_weight else None
+    db = torch.empty(dim, dtype=x.dtype, device=dev) if with_bias else None
+    at, size, space = _space("lcn_layer_norm_workspace_bytes", (rows, dim, dtype), workspace, dev)
+    _call("lcn_layer_norm_backward", dev, x.data_ptr(), _tensor(weight, "weight", (dim,), x.dtype, dev),
+          _tensor(mean, "mean", (rows,), torch.float32, dev), _tensor(rstd, "rstd", (rows,), torch.float32, dev),
+          _tensor(dy, "dy", (rows, dim), x.dtype, dev), _tensor(around, "around", (rows, dim), x.dtype, dev), rows, dim, dtype,
+          _address(dx), _address(dw), _address(db), at, size)
     return dx, dw, db
 
 

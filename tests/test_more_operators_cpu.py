@@ -1,0 +1,63 @@
+"""Host-side checks that need no GPU of the operators that complete a layer: sizes, refusals before any device work, workspaces."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2107_06876_amd as lcn
+from paper_2107_06876_amd import encoder
+from paper_2107_06876_amd.binding import BF16, ERR_ALLOC, ERR_INVALID_ARG, F32, OK
+
+FAKE = 256 * 1024   # never read: the calls below are refused before any device work
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return encoder._library()
+
+
+def _bytes(f, *sizes):
+    out = ctypes.c_size_t(0)
+    return f(*sizes, ctypes.byref(out)), out.value
+
+
+# ---- layer norm ------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("rows,dim,dtype", [(-1, 4, F32), (4, 0, F32), (4, 4, 7), (4, (1 << 20) + 1, F32), ((1 << 30) + 1, 4, BF16),
+                                            (1 << 30, (1 << 12) + 1, BF16)])
+def test_norm_sizes_out_of_range(lib, rows, dim, dtype):
+    assert _bytes(lib.lcn_layer_norm_workspace_bytes, rows, dim, dtype)[0] == ERR_INVALID_ARG
+    assert lib.lcn_layer_norm(FAKE, FAKE, FAKE, rows, dim, dtype, 1e-5, FAKE, FAKE, FAKE, None) == ERR_INVALID_ARG
+    assert lib.lcn_layer_norm_backward(FAKE, FAKE, FAKE, FAKE, FAKE, None, rows, dim, dtype, FAKE, FAKE, FAKE, FAKE, 1 << 40,
+                                       None) == ERR_INVALID_ARG
+
+
+def test_norm_arguments(lib):
+    for at in (0, 7):
+        args = [FAKE, FAKE, FAKE, 20, 60, F32, 1e-5, FAKE, FAKE, FAKE, None]
+        args[at] = None
+        assert lib.lcn_layer_norm(*args) == ERR_INVALID_ARG
+    for eps in (-1e-9, float("nan"), float("inf")):
+        assert lib.lcn_layer_norm(FAKE, FAKE, FAKE, 20, 60, F32, eps, FAKE, FAKE, FAKE, None) == ERR_INVALID_ARG
+    good = [FAKE, FAKE, FAKE, FAKE, FAKE, None, 20, 60, F32, FAKE, FAKE, FAKE, FAKE, 1 << 40, None]
+    for at in (0, 2, 3, 4):
+        args = list(good)
+        args[at] = None
+        assert lib.lcn_layer_norm_backward(*args) == ERR_INVALID_ARG
+    st, n = _bytes(lib.lcn_layer_norm_workspace_bytes, 20, 60, F32)
+    assert st == OK and n > 0
+    for space, size in ((FAKE, n - 1), (None, n), (FAKE + 128, n)):
+        args = list(good)
+        args[12], args[13] = space, size
+        assert lib.lcn_layer_norm_backward(*args) == ERR_ALLOC
+    assert _bytes(lib.lcn_layer_norm_workspace_bytes, 0, 60, F32) == (OK, 0)
+    assert lib.lcn_layer_norm(None, None, None, 0, 60, F32, 1e-5, None, None, None, None) == OK
+    assert lib.lcn_layer_norm_backward(None, None, None, None, None, None, 20, 60, F32, None, None, None, None, 0, None) == OK
+
+
+def test_norm_of_tensors_that_are_not_on_a_device():
+    with pytest.raises(ValueError):
+        lcn.lcn_layer_norm(torch.ones(4, 6))
+    with pytest.raises(ValueError):
+        lcn.lcn_layer_norm_backward(torch.ones(4, 6), None, torch.ones(4), torch.ones(4), torch.ones(4, 6))
