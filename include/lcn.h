@@ -375,7 +375,7 @@ lcn_status lcn_calibrate(int32_t what, void *workspace, size_t workspace_bytes, 
  *     once from them.  With bf16 tensors these are rounded to bf16 as well, where
  *     they enter a matrix product: the weights P of lcn_attention (in o and dv)
  *     and its dS (in dq and dk); above 512 rows dz of lcn_linear_backward where
- *     there is an activation (in dx and dW), and the cross entropy's G (in dW, and
+ *     there is an activation and of lcn_gated_linear_backward (in dx and dW), and the cross entropy's G (in dW, and
  *     in dx but for the target's part).  Each is as large as the output's own
  *     rounding: the error becomes 1.4 times that of one.  Where a tile of 64 or 128
  *     queries sees more than 256 keys, o enters dS as it was rounded, a third such
@@ -492,6 +492,22 @@ lcn_status lcn_attention(const lcn_attention_desc *desc, const void *q, const vo
 lcn_status lcn_attention_backward(const lcn_attention_desc *desc, const void *q, const void *k, const void *v, const void *o,
                                   const float *lse, const void *dy, void *dq, void *dk, void *dv, void *workspace,
                                   size_t workspace_bytes, void *hip_stream);
+
+/* y = act(g) .* u with g = x Wg^T + bg and u = x Wu^T + bu: the gated half of a feed-forward block
+ * (its other half is lcn_linear).  x rows x d_in; W (2 d_out) x d_in, Wg above Wu; bias (bg before bu,
+ * 2 d_out; nullable); y rows x d_out.  pre (nullable): the fp32 values g and u for the backward pass,
+ * rows x (2 d_out), g before u in every row.  Sizes: 0 <= rows <= 2^30, 1 <= d_in <= 2^20, 1 <= d_out <= 2^19,
+ * rows times d_in or 2 d_out <= 2^42.  Up to 8 rows need no workspace (the call says 0 bytes). */
+lcn_status lcn_gated_linear_workspace_bytes(int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype, int32_t backward,
+                                            size_t *bytes);
+lcn_status lcn_gated_linear(const void *x, const void *W, const void *bias, int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype,
+                            int32_t activation, void *y, float *pre, void *workspace, size_t workspace_bytes, void *hip_stream);
+/* Its gradients for a given dy: with dz = [dy .* u .* act'(g) | dy .* act(g)],
+ *   dx = dz W (rows x d_in),  dW = dz^T x ((2 d_out) x d_in),  dbias = column sums of dz (2 d_out).
+ * dx, dW, dbias are nullable; x may be NULL if dW is, W if dx is. */
+lcn_status lcn_gated_linear_backward(const void *x, const void *W, const float *pre, const void *dy, int64_t rows, int32_t d_in,
+                                     int32_t d_out, int32_t dtype, int32_t activation, void *dx, void *dW, void *dbias,
+                                     void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* Layer norm of every row of x, rows x dim: with the mean and the variance of the row,
  *   y = (x - mean) rstd weight + bias,  rstd = 1 / sqrt(mean of (x - mean)^2 + eps).

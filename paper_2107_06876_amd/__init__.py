@@ -16,5 +16,5 @@ from .binding import (  # noqa: F401
     lcn_calibrate, CAL_COPY_GBS, CAL_READ_GBS, CAL_MFMA_BF16_TFLOPS, CAL_MFMA_F64_TFLOPS, CAL_LAUNCH_US)
 from .encoder import (  # noqa: F401
     ACT_GELU, ACT_NONE, ACT_RELU, ACT_SILU, ACT_TANH, lcn_attention, lcn_attention_backward,
-    lcn_cross_entropy, lcn_cross_entropy_backward, lcn_layer_norm, lcn_layer_norm_backward, lcn_linear,
-    lcn_linear_backward)
+    lcn_cross_entropy, lcn_cross_entropy_backward, lcn_gated_linear, lcn_gated_linear_backward, lcn_layer_norm,
+    lcn_layer_norm_backward, lcn_linear, lcn_linear_backward)

@@ -26,6 +26,7 @@ SOURCES = {
     "kernels_batched.hip": ["-ffp-contract=off"],  # bucket rule again
     "kernels_planes.hip": [],
     "kernels_linear.hip": [],
+    "kernels_gated.hip": [],
     "kernels_norm.hip": [],
     "kernels_entropy.hip": [],
     "kernels_attention_f32.hip": [],

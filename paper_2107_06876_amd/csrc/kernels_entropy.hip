@@ -384,7 +384,7 @@ __global__ __launch_bounds__(256) void entropy_finish_kernel(const float *__rest
 
 // ---- host ---------------------------------------------------------------------
 
-constexpr int FEW_ROWS = 8, FEW_GROUPS = 1024;
+constexpr int FEW_GROUPS = 1024;
 // G of a piece of the vocabulary takes at most this much of the workspace: what is written stays in the last-level cache until
 // both products have read it (8192 rows against 200 000 words: 6.11 ms; with 64 MiB 7.23, with 256 MiB 6.46, with 512 MiB 6.23)
 constexpr size_t PIECE_BYTES = (size_t)128 << 20;

@@ -244,25 +244,6 @@ __global__ __launch_bounds__(256) void slope_kernel(const T *__restrict__ dy, co
 
 // ---- host ---------------------------------------------------------------------
 
-constexpr int FEW_ROWS = 8;
-
-template <int ACT>
-struct Activation {
-    static constexpr int value = ACT;
-};
-// calls f with the activation as a type
-template <class F>
-static hipError_t by_activation(int act, F f)
-{
-    switch (act) {
-    case LCN_ACT_TANH: return f(Activation<LCN_ACT_TANH>());
-    case LCN_ACT_RELU: return f(Activation<LCN_ACT_RELU>());
-    case LCN_ACT_GELU: return f(Activation<LCN_ACT_GELU>());
-    case LCN_ACT_SILU: return f(Activation<LCN_ACT_SILU>());
-    default: return f(Activation<LCN_ACT_NONE>());
-    }
-}
-
 // Where that is faster than the product of planes (us for 40 000 rows, narrow / product): float 64 -> 256 35 / 36, 32 -> 512
 // 39 / 49, 128 -> 64 23 / 28, 128 -> 128 37 / 32; bf16 64 -> 256 20 / 23, 32 -> 512 22 / 32, 128 -> 64 11 / 7; rows that are
 // not whole pieces, 50 -> 64, 26 / 21 and 21 / 12.

@@ -158,6 +158,26 @@ __device__ __forceinline__ float activate_slope(float z)
     return 1.f;
 }
 
+// up to so many rows a layer takes dot products of its own (few_rows_dot) instead of the matrix instruction
+constexpr int FEW_ROWS = 8;
+
+template <int ACT>
+struct Activation {
+    static constexpr int value = ACT;
+};
+// calls f with the activation as a type
+template <class F>
+hipError_t by_activation(int act, F f)
+{
+    switch (act) {
+    case LCN_ACT_TANH: return f(Activation<LCN_ACT_TANH>());
+    case LCN_ACT_RELU: return f(Activation<LCN_ACT_RELU>());
+    case LCN_ACT_GELU: return f(Activation<LCN_ACT_GELU>());
+    case LCN_ACT_SILU: return f(Activation<LCN_ACT_SILU>());
+    default: return f(Activation<LCN_ACT_NONE>());
+    }
+}
+
 // ---- planes (kernels_planes.hip) --------------------------------------------
 inline __host__ __device__ long long padded(long long d) { return (d + 7) & ~7LL; }
 inline int planes_of(int32_t dtype) { return dtype == LCN_F32 ? 3 : 1; }

@@ -45,12 +45,16 @@ def _library():
         lib.lcn_attention_workspace_bytes.argtypes = [desc, i32, out]
         lib.lcn_attention.argtypes = [desc, vp, vp, vp, vp, vp, vp, sz, vp]
         lib.lcn_attention_backward.argtypes = [desc, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.lcn_gated_linear_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, out]
+        lib.lcn_gated_linear.argtypes = [vp, vp, vp, i64, i32, i32, i32, i32, vp, vp, vp, sz, vp]
+        lib.lcn_gated_linear_backward.argtypes = [vp, vp, vp, vp, i64, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
         lib.lcn_layer_norm.argtypes = [vp, vp, vp, i64, i32, i32, f32, vp, vp, vp, vp]
         lib.lcn_layer_norm_workspace_bytes.argtypes = [i64, i32, i32, out]
         lib.lcn_layer_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i32, i32, vp, vp, vp, vp, sz, vp]
         for name in ("lcn_attention_workspace_bytes", "lcn_attention", "lcn_attention_backward", "lcn_linear_workspace_bytes",
                      "lcn_linear", "lcn_linear_backward", "lcn_cross_entropy_workspace_bytes", "lcn_cross_entropy",
-                     "lcn_cross_entropy_backward", "lcn_layer_norm", "lcn_layer_norm_workspace_bytes", "lcn_layer_norm_backward"):
+                     "lcn_cross_entropy_backward", "lcn_layer_norm", "lcn_layer_norm_workspace_bytes", "lcn_layer_norm_backward",
+                     "lcn_gated_linear_workspace_bytes", "lcn_gated_linear", "lcn_gated_linear_backward"):
             getattr(lib, name).restype = i32
         _lib = lib
     return _lib
@@ -186,6 +190,41 @@ def lcn_cross_entropy_backward(x, w, target, lse, grad_loss, bias=None, scale=1.
           _tensor(target, "target", (rows,), torch.int64, dev), _tensor(lse, "lse", (rows,), torch.float32, dev),
           _tensor(grad_loss, "grad_loss", (rows,), torch.float32, dev), rows, vocab, dim, dtype, float(scale), _address(dx),
           _address(dw), _address(db), at, size)
+    return dx, dw, db
+
+
+def _gates(x, w):
+    """Rows, outputs, inputs and type of a gated layer: w has the rows of Wg above as many of Wu."""
+    rows, both, d_in, dtype = _matrices(x, w, "d_in")
+    if both % 2:
+        raise ValueError("w: expected the rows of Wg above as many of Wu")
+    return rows, both // 2, d_in, dtype
+
+
+def lcn_gated_linear(x, w, bias=None, activation=ACT_SILU, keep_pre=False, out=None, workspace=None):
+    """act(x Wg^T + bg) (x Wu^T + bu) as a (rows, d_out) tensor; w: (2 d_out, d_in), Wg above Wu, bias: (2 d_out).  With
+    keep_pre also both factors' arguments in float32, (rows, 2 d_out), which lcn_gated_linear_backward takes."""
+    rows, d_out, d_in, dtype = _gates(x, w)
+    dev = x.device
+    y = torch.empty((rows, d_out), dtype=x.dtype, device=dev) if out is None else out
+    pre = torch.empty((rows, 2 * d_out), dtype=torch.float32, device=dev) if keep_pre else None
+    at, size, space = _space("lcn_gated_linear_workspace_bytes", (rows, d_in, d_out, dtype, 0), workspace, dev)
+    _call("lcn_gated_linear", dev, x.data_ptr(), w.data_ptr(), _tensor(bias, "bias", (2 * d_out,), x.dtype, dev), rows, d_in, d_out,
+          dtype, int(activation), _tensor(y, "out", (rows, d_out), x.dtype, dev), _address(pre), at, size)
+    return (y, pre) if keep_pre else y
+
+
+def lcn_gated_linear_backward(x, w, pre, dy, activation=ACT_SILU, with_bias=True, with_x=True, with_w=True, workspace=None):
+    """(dx, dw, dbias) for a given dy; pre: what lcn_gated_linear kept.  Gradients that are not asked for are None."""
+    rows, d_out, d_in, dtype = _gates(x, w)
+    dev = x.device
+    dx = torch.empty_like(x) if with_x else None
+    dw = torch.empty_like(w) if with_w else None
+    db = torch.empty(2 * d_out, dtype=x.dtype, device=dev) if with_bias else None
+    at, size, space = _space("lcn_gated_linear_workspace_bytes", (rows, d_in, d_out, dtype, 1), workspace, dev)
+    _call("lcn_gated_linear_backward", dev, x.data_ptr(), w.data_ptr(), _tensor(pre, "pre", (rows, 2 * d_out), torch.float32, dev),
+          _tensor(dy, "dy", (rows, d_out), x.dtype, dev), rows, d_in, d_out, dtype, int(activation), _address(dx), _address(dw),
+          _address(db), at, size)
     return dx, dw, db
 
 

@@ -1,0 +1,207 @@
+"""lcn_gated_linear and lcn_gated_linear_backward against the formulas in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import paper_2107_06876_amd as lcn
+from operator_checks import BF16, DEV, F32, bound, farthest, generator, normal, off, roundings
+
+pytestmark = pytest.mark.gpu
+
+ACTS = {"none": lcn.ACT_NONE, "tanh": lcn.ACT_TANH, "relu": lcn.ACT_RELU, "gelu": lcn.ACT_GELU, "silu": lcn.ACT_SILU}
+FUNCTIONS = dict(none=lambda z: z * 1.0, tanh=torch.tanh, relu=torch.relu, gelu=torch.nn.functional.gelu,
+                 silu=torch.nn.functional.silu)
+
+
+def oracle(x, w, b, dy, act):
+    """y, [g | u], dx, dw, db in 64 bits."""
+    x, w, dy = x.double(), w.double(), dy.double()
+    d = w.shape[0] // 2
+    z = x @ w.t().contiguous()
+    if b is not None:
+        z = z + b.double()
+    z = z.detach().requires_grad_(True)
+    y = FUNCTIONS[act](z[:, :d]) * z[:, d:]
+    (dz,) = torch.autograd.grad(y, z, dy)
+    return y.detach(), z.detach(), dz @ w, dz.t().contiguous() @ x, dz.sum(0)
+
+
+def inputs(rows, d_in, d_out, dtype, shift=0):
+    g = generator(rows, d_in, d_out)
+    return (normal(g, rows, d_in, dtype=dtype, shift=shift), normal(g, 2 * d_out, d_in, dtype=dtype, scale=d_in ** -0.5, shift=shift),
+            normal(g, 2 * d_out, dtype=dtype, scale=0.3, shift=shift), normal(g, rows, d_out, dtype=dtype, shift=shift))
+
+
+def check(rows, d_in, d_out, act, dtype, bias=True, shift=0):
+    """g and u are off by the error of a sum of d_in terms each, y by both and (through act) once more; dz as y, rounded to bf16 on
+    its way into the products."""
+    print("gated", rows, d_in, d_out, act, dtype, bias, shift, flush=True)
+    x, w, b, dy = inputs(rows, d_in, d_out, dtype, shift)
+    b = b if bias else None
+    y, z = lcn.lcn_gated_linear(x, w, bias=b, activation=ACTS[act], keep_pre=True)
+    assert torch.equal(y, lcn.lcn_gated_linear(x, w, bias=b, activation=ACTS[act]))
+    dx, dw, db = lcn.lcn_gated_linear_backward(x, w, z, dy, activation=ACTS[act], with_bias=bias)
+    ey, ez, edx, edw, edb = oracle(x, w, b, dy, act)
+    own = 3 * bound(F32, d_in)
+    if act == "relu":   # its slope jumps: a g within the rounding of 0 may have either slope (it has one in expectation 1e-6 of places)
+        near = (ez[:, :d_out].abs() <= 2.0 ** -20).sum().item()
+        own += math.sqrt(near / ez[:, :d_out].numel())
+    assert off(z, ez) <= bound(F32, d_in)
+    assert off(y, ey) <= own + bound(dtype, 1)
+    assert off(dx, edx) <= own + bound(dtype, 2 * d_out, 1)
+    assert off(dw, edw) <= own + bound(dtype, rows, 1)
+    assert (db is None) == (not bias)
+    if bias:
+        assert off(db, edb) <= own + bound(dtype, rows)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,d_in,d_out", [
+    (1, 300, 20), (1, 1, 1), (2, 64, 64), (3, 17, 129), (7, 33, 5), (8, 128, 1), (9, 128, 1), (9, 1, 7), (40, 300, 32), (63, 72, 65),
+    (64, 64, 32), (257, 301, 130), (1000, 32, 64), (129, 2048, 257), (3000, 300, 512), (17, 4104, 12), (100, 40, 31), (65, 48, 100),
+    (700, 56, 33), (515, 96, 20), (300, 64, 200), (130, 1000, 66)])
+def test_sizes(rows, d_in, d_out, dtype):
+    check(rows, d_in, d_out, "silu", dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("rows,d_in,d_out", [(5, 96, 136), (300, 96, 136), (777, 32, 64)])
+def test_activations(act, rows, d_in, d_out, dtype):
+    check(rows, d_in, d_out, act, dtype)
+    check(rows, d_in, d_out, act, dtype, bias=False)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [3, 200])
+def test_addresses_of_one_element(rows, dtype):
+    check(rows, 64, 64, "gelu", dtype, shift=1)
+    check(rows, 64, 62, "none", dtype, shift=1)
+    check(rows, 64, 64, "silu", dtype, shift=4)
+
+
+@pytest.mark.parametrize("rows,d_in,d_out,dtype", [(5000, 512, 1026, BF16), (4103, 1024, 2048, BF16), (2053, 512, 2048, F32),
+                                                   (3000, 200, 1025, F32)])
+def test_large_tiles(rows, d_in, d_out, dtype):
+    check(rows, d_in, d_out, "silu", dtype)
+
+
+@pytest.mark.parametrize("rows", [12, 300, 512, 700, 4103])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_roundings_of_bf16(act, rows):
+    """y and db are rounded once; dz is rounded as well on its way into dx and dw, above 512 rows."""
+    d_in, d_out = (264, 520) if rows < 4000 else (512, 2048)
+    x, w, b, dy = inputs(rows, d_in, d_out, BF16)
+    y, z = lcn.lcn_gated_linear(x, w, bias=b, activation=ACTS[act], keep_pre=True)
+    got = (y, *lcn.lcn_gated_linear_backward(x, w, z, dy, activation=ACTS[act]))
+    want = oracle(x, w, b, dy, act)
+    once = 1 if rows <= 512 else 2
+    # y and dz are products of values with many sizes, spread more evenly over octaves: 1.1 covers that
+    for u, v, n in zip(got, (want[0], *want[2:]), (1, once, once, 1)):
+        assert off(u, v) <= roundings(n) and farthest(u, v) <= 1.0
+
+
+def test_not_a_number_stays_in_its_row():
+    for dtype in (F32, BF16):
+        for rows in (4, 100, 300):
+            x, w, b, _ = inputs(rows, 40, 24, dtype)
+            x[2, 7] = math.nan
+            y = lcn.lcn_gated_linear(x, w, bias=b, activation=lcn.ACT_SILU)
+            assert torch.isnan(y[2]).all() and torch.isfinite(y[:2]).all() and torch.isfinite(y[3:]).all()
+            x, w, b, _ = inputs(rows, 40, 24, dtype)
+            w[24 + 5, 3] = math.nan   # a row of Wu: one output
+            y = lcn.lcn_gated_linear(x, w, bias=b, activation=lcn.ACT_SILU)
+            assert torch.isnan(y[:, 5]).all() and torch.isfinite(y[:, :5]).all() and torch.isfinite(y[:, 6:]).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,d_out,shift", [(5, 136, 0), (300, 136, 0), (700, 136, 0), (300, 135, 0), (300, 136, 1)])
+def test_single_gradients_and_same_bits(rows, d_out, shift, dtype):
+    """dx, dw and db have the same bits whichever are asked for, and from call to call."""
+    x, w, b, dy = inputs(rows, 72, d_out, dtype, shift)
+    _, z = lcn.lcn_gated_linear(x, w, bias=b, keep_pre=True)
+    want = lcn.lcn_gated_linear_backward(x, w, z, dy)
+    for asked in ((1, 1, 1), (1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 1, 0), (1, 0, 1), (0, 1, 1), (0, 0, 0)):
+        got = lcn.lcn_gated_linear_backward(x, w, z, dy, with_x=asked[0], with_w=asked[1], with_bias=asked[2])
+        for a, u, v in zip(asked, got, want):
+            assert torch.equal(u, v) if a else u is None
+
+
+def test_differences():
+    """<dy, y> changes along a direction as the gradients say (central differences of the float path)."""
+    g = generator(14)
+    x, w, b, dy = inputs(30, 20, 25, F32)
+    for act in ("silu", "gelu", "tanh", "none"):
+        _, pre = lcn.lcn_gated_linear(x, w, bias=b, activation=ACTS[act], keep_pre=True)
+        grads = lcn.lcn_gated_linear_backward(x, w, pre, dy, activation=ACTS[act])
+        for at, grad in enumerate(grads):
+            step = normal(g, *grad.shape)
+            h = 1e-3
+            val = []
+            for sign in (1, -1):
+                args = [x, w, b]
+                args[at] = args[at] + sign * h * step
+                val.append((lcn.lcn_gated_linear(args[0], args[1], bias=args[2], activation=ACTS[act]).double() * dy.double()).sum())
+            want = (grad.double() * step.double()).sum().item()
+            # the third derivative times h^2, and the rounding of the values over h
+            room = 2e-4 * grad.double().norm().item() * step.double().norm().item()
+            assert abs((val[0] - val[1]).item() / (2 * h) - want) <= room
+
+
+def test_no_rows():
+    w, x = torch.ones(10, 4, device=DEV), torch.empty(0, 4, device=DEV)
+    y, pre = lcn.lcn_gated_linear(x, w, keep_pre=True)
+    assert y.shape == (0, 5) and pre.shape == (0, 10)
+    dx, dw, db = lcn.lcn_gated_linear_backward(x, w, pre, y)
+    assert dx.shape == (0, 4) and not dw.any() and not db.any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,d_in,d_out", [(6, 128, 256), (600, 128, 256), (900, 32, 64), (70, 2048, 40)])
+def test_other_stream_and_graph(rows, d_in, d_out, dtype):
+    x, w, b, dy = inputs(rows, d_in, d_out, dtype)
+
+    def both():
+        y, pre = lcn.lcn_gated_linear(x, w, bias=b, keep_pre=True)
+        return (y, pre, *lcn.lcn_gated_linear_backward(x, w, pre, dy))
+
+    want = both()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = both()
+    side.synchronize()
+    for u, v in zip(got, want):
+        assert torch.equal(u, v)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both()
+    for _ in range(3):
+        for t in got:
+            t.fill_(-7.0)
+        both()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for u, v in zip(got, want):
+            assert torch.equal(u, v)
+
+
+def test_refusals():
+    x, w = torch.ones(4, 6, device=DEV), torch.ones(8, 6, device=DEV)
+    for bad in (dict(x=x.t()), dict(x=x.half()), dict(x=x.bfloat16()), dict(w=torch.ones(8, 5, device=DEV)), dict(w=w[:7]),
+                dict(x=x.cpu()), dict(bias=torch.ones(4, device=DEV)), dict(bias=torch.ones(8, device=DEV, dtype=BF16)),
+                dict(out=torch.ones(4, 8, device=DEV)), dict(x=x[0])):
+        with pytest.raises(ValueError):
+            lcn.lcn_gated_linear(**dict(dict(x=x, w=w), **bad))
+    with pytest.raises(lcn.LcnError):
+        lcn.lcn_gated_linear(x, w, activation=9)
+    with pytest.raises(lcn.LcnError):   # a workspace that is too small
+        lcn.lcn_gated_linear(torch.ones(99, 6, device=DEV), w, workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
+    pre = torch.ones(4, 8, device=DEV)
+    for bad in (dict(pre=pre[:, :4]), dict(pre=pre.bfloat16()), dict(dy=pre)):
+        with pytest.raises(ValueError):
+            lcn.lcn_gated_linear_backward(**dict(dict(x=x, w=w, pre=pre, dy=torch.ones(4, 4, device=DEV)), **bad))
+    with pytest.raises(lcn.LcnError):   # the gradient needs g and u
+        lcn.lcn_gated_linear_backward(x, w, None, torch.ones(4, 4, device=DEV))

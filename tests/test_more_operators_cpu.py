@@ -61,3 +61,58 @@ def test_norm_of_tensors_that_are_not_on_a_device():
         lcn.lcn_layer_norm(torch.ones(4, 6))
     with pytest.raises(ValueError):
         lcn.lcn_layer_norm_backward(torch.ones(4, 6), None, torch.ones(4), torch.ones(4), torch.ones(4, 6))
+
+
+# ---- gated layer -----------------------------------------------------------------
+
+
+@pytest.mark.parametrize("rows,d_in,d_out,dtype", [
+    (-1, 4, 4, F32), (4, 0, 4, F32), (4, 4, 0, F32), (4, 4, 4, 7), (4, (1 << 20) + 1, 4, F32), (4, 4, (1 << 19) + 1, F32),
+    ((1 << 30) + 1, 4, 4, BF16), (1 << 30, 8, (1 << 11) + 1, BF16), (1 << 30, (1 << 12) + 1, 8, BF16)])
+def test_gated_sizes_out_of_range(lib, rows, d_in, d_out, dtype):
+    for backward in (0, 1):
+        assert _bytes(lib.lcn_gated_linear_workspace_bytes, rows, d_in, d_out, dtype, backward)[0] == ERR_INVALID_ARG
+    assert lib.lcn_gated_linear(FAKE, FAKE, None, rows, d_in, d_out, dtype, 0, FAKE, None, FAKE, 1 << 62, None) == ERR_INVALID_ARG
+    assert lib.lcn_gated_linear_backward(FAKE, FAKE, FAKE, FAKE, rows, d_in, d_out, dtype, 0, FAKE, FAKE, None, FAKE, 1 << 62,
+                                         None) == ERR_INVALID_ARG
+
+
+def test_gated_arguments(lib):
+    good = [FAKE, FAKE, None, 20, 600, 600, F32, 4, FAKE, None, FAKE, 1 << 40, None]
+    for at in (0, 1, 8):
+        bad = list(good)
+        bad[at] = None
+        assert lib.lcn_gated_linear(*bad) == ERR_INVALID_ARG
+    for act in (-1, 5):
+        bad = list(good)
+        bad[7] = act
+        assert lib.lcn_gated_linear(*bad) == ERR_INVALID_ARG
+    good = [FAKE, FAKE, FAKE, FAKE, 20, 60, 60, F32, 4, FAKE, FAKE, None, FAKE, 1 << 40, None]
+    for at in range(4):
+        bad = list(good)
+        bad[at] = None
+        assert lib.lcn_gated_linear_backward(*bad) == ERR_INVALID_ARG
+    bad = list(good)
+    bad[8] = 5
+    assert lib.lcn_gated_linear_backward(*bad) == ERR_INVALID_ARG
+    assert lib.lcn_gated_linear_backward(None, None, None, None, 20, 60, 60, F32, 4, None, None, None, None, 0, None) == OK
+
+
+def test_gated_workspaces(lib):
+    for dtype in (F32, BF16):
+        for rows, a, b in ((1, 16, 16), (20, 300, 600), (5000, 300, 20000), (70000, 1024, 4096)):
+            st, n = _bytes(lib.lcn_gated_linear_workspace_bytes, rows, a, b, dtype, 0)
+            assert st == OK and (n == 0) == (rows <= 8)
+            if n:
+                assert lib.lcn_gated_linear(FAKE, FAKE, None, rows, a, b, dtype, 4, FAKE, None, FAKE, n - 1, None) == ERR_ALLOC
+                assert lib.lcn_gated_linear(FAKE, FAKE, None, rows, a, b, dtype, 4, FAKE, None, FAKE + 64, n, None) == ERR_ALLOC
+            st, n = _bytes(lib.lcn_gated_linear_workspace_bytes, rows, a, b, dtype, 1)
+            assert st == OK and n > 0
+            assert lib.lcn_gated_linear_backward(FAKE, FAKE, FAKE, FAKE, rows, a, b, dtype, 4, FAKE, FAKE, None, FAKE, n - 1,
+                                                 None) == ERR_ALLOC
+    assert _bytes(lib.lcn_gated_linear_workspace_bytes, 0, 4, 4, F32, 1) == (OK, 0)
+
+
+def test_gated_tensors_that_are_not_on_a_device():
+    with pytest.raises(ValueError):
+        lcn.lcn_gated_linear(torch.ones(4, 6), torch.ones(4, 6))
