@@ -527,6 +527,23 @@ lcn_status lcn_layer_norm_backward(const void *x, const void *weight, const floa
                                    const void *around, int64_t rows, int32_t dim, int32_t dtype, void *dx, void *dweight,
                                    void *dbias, void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* Orthogonalisation of `count` matrices G, rows x cols each, one behind the other: from
+ *   X = G / (|G| + eps), |G| the Frobenius norm of the matrix,
+ * `steps` times, step i with (a, b, c) = coefficients[3 i .. 3 i + 2] (host memory, read during the call),
+ *   A = X X^T,  X = a X + (b A + c A^2) X       (with more rows than columns: of the transposed matrix);
+ * out = scale X.  The singular vectors stay, a singular value s becomes a s + b s^3 + c s^5 in a step.
+ * (3.4445, -4.7750, 2.0315) five times brings most of them to 0.7 .. 1.2, for updates of weight matrices;
+ * (1.875, -1.25, 0.375) often enough brings them to 1: the nearest orthogonal map to a correlation of two embeddings.
+ * X and all sums are held to 24 bits, also with bf16 tensors, and out is rounded once.  A G that holds a
+ * value that is not finite makes its whole result NaN, and so does G = 0 with eps = 0.  out may be g.
+ * LCN_ERR_INVALID_ARG for coefficients that let singular values in 0 .. 1 grow beyond 4, or a + b s^2 + c s^4 beyond
+ * 64, in any step.  Sizes: 0 <= count <= 2^20, 1 <= rows, cols <= 2^20, the smaller of them <= 32768, count * rows *
+ * cols <= 2^40; 1 <= steps <= 64; eps >= 0 and scale finite. */
+lcn_status lcn_orthogonalise_workspace_bytes(int64_t count, int32_t rows, int32_t cols, int32_t dtype, size_t *bytes);
+lcn_status lcn_orthogonalise(const void *g, int64_t count, int32_t rows, int32_t cols, int32_t dtype, int32_t steps,
+                             const float *coefficients, float eps, float scale, void *out, void *workspace, size_t workspace_bytes,
+                             void *hip_stream);
+
 void lcn_destroy(lcn_handle h); /* frees host memory only; the workspace is the caller's */
 const char *lcn_status_string(int32_t status);
 

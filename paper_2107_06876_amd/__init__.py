@@ -15,6 +15,6 @@ from .binding import (  # noqa: F401
     lcn_backward_scratch_bytes, lcn_plan_rows, lcn_deletion_costs, lcn_head_lambdas, lcn_last_error_counts, lcn_backward_static,
     lcn_calibrate, CAL_COPY_GBS, CAL_READ_GBS, CAL_MFMA_BF16_TFLOPS, CAL_MFMA_F64_TFLOPS, CAL_LAUNCH_US)
 from .encoder import (  # noqa: F401
-    ACT_GELU, ACT_NONE, ACT_RELU, ACT_SILU, ACT_TANH, lcn_attention, lcn_attention_backward,
+    ACT_GELU, ACT_NONE, ACT_RELU, ACT_SILU, ACT_TANH, ORTHOGONAL_MAP, ORTHOGONAL_UPDATE, lcn_attention, lcn_attention_backward,
     lcn_cross_entropy, lcn_cross_entropy_backward, lcn_gated_linear, lcn_gated_linear_backward, lcn_layer_norm,
-    lcn_layer_norm_backward, lcn_linear, lcn_linear_backward)
+    lcn_layer_norm_backward, lcn_linear, lcn_linear_backward, lcn_orthogonalise)

@@ -28,6 +28,7 @@ SOURCES = {
     "kernels_linear.hip": [],
     "kernels_gated.hip": [],
     "kernels_norm.hip": [],
+    "kernels_orthogonal.hip": [],
     "kernels_entropy.hip": [],
     "kernels_attention_f32.hip": [],
     "kernels_attention_bf16.hip": [],

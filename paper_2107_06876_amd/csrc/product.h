@@ -7,6 +7,9 @@
 // whose rate is 1/16.  Two planes of the second operand alone (two products) serve where a rounding of it to one would
 // show in the result.
 //
+// Values whose range is known can be two planes of fp16 instead: x1 = fp16(x), x2 = fp16(x - x1) leave 2^-24 |x| where x2 is no
+// subnormal, and the three products but x2 y2 are as exact as a single-precision one, at half the cost of six.
+//
 // An operand is stored either with k contiguous (`rows`: A[m][k] at m * ld + k) or with its own index contiguous
 // (`columns`: A[k][m] at k * ld + m).  Tiles of 32 or 64 values of k go from memory straight into LDS (16 bytes a lane; what is
 // outside the operand is read as zero by the buffer's bounds), two tiles of LDS in turn, so that the next tile is on its
@@ -40,6 +43,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 struct Operand {
     const void *p;     // first plane, 16-byte aligned
@@ -161,6 +165,11 @@ __device__ __forceinline__ f32x4 mfma_bf16(bf16x8 a, bf16x8 b, f32x4 c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
+// the same for a register's bits as fp16
+__device__ __forceinline__ f32x4 mfma_f16(bf16x8 a, bf16x8 b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
 
 // The tile that a workgroup works on.  Workgroups are dealt to the eight dies in turn: a die gets a run of
 // consecutive tiles, and tiles follow each other in strips of four along n, so that the tiles in flight on a die share
@@ -214,7 +223,7 @@ __device__ __forceinline__ void by_rows(char *region, const f32x4 (&v)[TM], int 
     __builtin_amdgcn_wave_barrier();
 }
 
-// WM x WN wavefronts of 64, each BM/WM x BN/WN of the tile; NP: 3 planes of both operands at a time, or 1.  Epi: struct with Args and
+// WM x WN wavefronts of 64, each BM/WM x BN/WN of the tile; NP: planes of both operands at a time, 1, 3 or 2 of fp16.  Epi: struct with Args and
 // run<TM, TN, WM, WN>(args, product args, acc, m0, n0, split, lds, tile) for the wavefront's accumulators.
 template <int BM, int BN, int BK, int WM, int WN, int NP, bool ACOL, bool BCOL, class Epi>
 __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs p, typename Epi::Args e)
@@ -239,7 +248,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs p, 
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    const int ksteps = (p.k + BK - 1) / BK, pairs = NP == 3 ? 1 : p.planes;
+    const int ksteps = (p.k + BK - 1) / BK, pairs = NP > 1 ? 1 : p.planes;
     const int all = ksteps * pairs, per = (all + p.splits - 1) / p.splits;
     const int first = (int)blockIdx.y * per, last = first + per < all ? first + per : all;
 
@@ -249,11 +258,11 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs p, 
     load_b.init(p.b, n0, p.n, wave, lane);
     int pair = first / ksteps, step = first - pair * ksteps;   // of the next fetch
     auto fetch = [&](char *lds) {
-        if constexpr (NP == 3) {
+        if constexpr (NP > 1) {
 #pragma unroll
-            for (int u = 0; u < 3; ++u) {
+            for (int u = 0; u < NP; ++u) {
                 load_a.load(u * p.a.plane, step, p.k, lds + u * ABYTES, wave);
-                load_b.load(u * p.b.plane, step, p.k, lds + 3 * ABYTES + u * BBYTES, wave);
+                load_b.load(u * p.b.plane, step, p.k, lds + NP * ABYTES + u * BBYTES, wave);
             }
             ++step;
         } else {   // two planes of B: the second one first
@@ -297,6 +306,25 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs p, 
                     for (int j = 0; j < TN; ++j) t[j] = mfma_bf16(a[0], b[1][j], t[j]);
 #pragma unroll
                     for (int j = 0; j < TN; ++j) acc[i][j] = mfma_bf16(a[0], b[0][j], acc[i][j]) + t[j];
+                }
+            } else if constexpr (NP == 2) {
+                bf16x8 b[2][TN];
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+                        b[u][j] = load_fragment<BN, BK, BCOL>(lds + 2 * ABYTES + u * BBYTES, pb, wn + j * 16, kk);
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+                    bf16x8 a[2];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) a[u] = load_fragment<BM, BK, ACOL>(lds + u * ABYTES, pa, wm + i * 16, kk);
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = mfma_f16(a[1], b[0][j], acc[i][j]);
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = mfma_f16(a[0], b[1][j], acc[i][j]);
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = mfma_f16(a[0], b[0][j], acc[i][j]);
                 }
             } else {
                 bf16x8 a[TM], b[TN];

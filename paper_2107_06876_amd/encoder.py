@@ -48,13 +48,16 @@ def _library():
         lib.lcn_gated_linear_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, out]
         lib.lcn_gated_linear.argtypes = [vp, vp, vp, i64, i32, i32, i32, i32, vp, vp, vp, sz, vp]
         lib.lcn_gated_linear_backward.argtypes = [vp, vp, vp, vp, i64, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+        lib.lcn_orthogonalise_workspace_bytes.argtypes = [i64, i32, i32, i32, out]
+        lib.lcn_orthogonalise.argtypes = [vp, i64, i32, i32, i32, i32, vp, f32, f32, vp, vp, sz, vp]
         lib.lcn_layer_norm.argtypes = [vp, vp, vp, i64, i32, i32, f32, vp, vp, vp, vp]
         lib.lcn_layer_norm_workspace_bytes.argtypes = [i64, i32, i32, out]
         lib.lcn_layer_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i32, i32, vp, vp, vp, vp, sz, vp]
         for name in ("lcn_attention_workspace_bytes", "lcn_attention", "lcn_attention_backward", "lcn_linear_workspace_bytes",
                      "lcn_linear", "lcn_linear_backward", "lcn_cross_entropy_workspace_bytes", "lcn_cross_entropy",
                      "lcn_cross_entropy_backward", "lcn_layer_norm", "lcn_layer_norm_workspace_bytes", "lcn_layer_norm_backward",
-                     "lcn_gated_linear_workspace_bytes", "lcn_gated_linear", "lcn_gated_linear_backward"):
+                     "lcn_gated_linear_workspace_bytes", "lcn_gated_linear", "lcn_gated_linear_backward",
+                     "lcn_orthogonalise_workspace_bytes", "lcn_orthogonalise"):
             getattr(lib, name).restype = i32
         _lib = lib
     return _lib
@@ -226,6 +229,36 @@ def lcn_gated_linear_backward(x, w, pre, dy, activation=ACT_SILU, with_bias=True
           _tensor(dy, "dy", (rows, d_out), x.dtype, dev), rows, d_in, d_out, dtype, int(activation), _address(dx), _address(dw),
           _address(db), at, size)
     return dx, dw, db
+
+
+ORTHOGONAL_UPDATE, ORTHOGONAL_MAP = (3.4445, -4.7750, 2.0315), (1.875, -1.25, 0.375)
+
+
+def _coefficients(steps, coefficients):
+    """The (a, b, c) of every step as an array of floats: one triple for all steps, or one for each."""
+    flat = [float(v) for c in coefficients for v in (c if isinstance(c, (tuple, list)) else (c,))]
+    if len(flat) == 3:
+        flat = flat * steps
+    if len(flat) != 3 * steps:
+        raise ValueError("coefficients: expected (a, b, c), or such a triple for each of %d steps" % steps)
+    return (ctypes.c_float * len(flat))(*flat)
+
+
+def lcn_orthogonalise(g, steps=5, coefficients=ORTHOGONAL_UPDATE, eps=1e-7, scale=1.0, out=None, workspace=None):
+    """scale X, with X = g / (|g| + eps) and then `steps` times X = a X + (b A + c A^2) X, A = X X^T, where g is a matrix or a
+    (count, rows, cols) batch of them; coefficients: (a, b, c), or a sequence of one such triple per step.  out may be g."""
+    dtype = _TYPES.get(g.dtype)
+    if dtype is None or g.dim() not in (2, 3) or not g.is_cuda or not g.is_contiguous() or 0 in g.shape[-2:]:
+        raise ValueError("g: expected a contiguous float32 or bfloat16 matrix, or a batch of them, on a device")
+    steps = int(steps)
+    if steps < 1:
+        raise ValueError("steps: expected at least one")
+    dev, (rows, cols), count = g.device, g.shape[-2:], g.shape[0] if g.dim() == 3 else 1
+    x = torch.empty_like(g) if out is None else out
+    at, size, space = _space("lcn_orthogonalise_workspace_bytes", (count, rows, cols, dtype), workspace, dev)
+    _call("lcn_orthogonalise", dev, g.data_ptr(), count, rows, cols, dtype, steps, _coefficients(steps, coefficients), float(eps),
+          float(scale), _tensor(x, "out", g.shape, g.dtype, dev), at, size)
+    return x
 
 
 def _rows(x):

@@ -116,3 +116,61 @@ def test_gated_workspaces(lib):
 def test_gated_tensors_that_are_not_on_a_device():
     with pytest.raises(ValueError):
         lcn.lcn_gated_linear(torch.ones(4, 6), torch.ones(4, 6))
+
+
+# ---- orthogonalisation -----------------------------------------------------------
+
+
+def _triples(*c):
+    return (ctypes.c_float * len(c))(*c)
+
+
+UPDATE = _triples(*(3.4445, -4.7750, 2.0315) * 5)
+
+
+@pytest.mark.parametrize("count,rows,cols,dtype", [
+    (-1, 4, 4, F32), (1, 0, 4, F32), (1, 4, 0, F32), (1, 4, 4, 7), ((1 << 20) + 1, 4, 4, F32), (1, (1 << 20) + 1, 4, F32),
+    (1, 4, (1 << 20) + 1, F32), (1, 32769, 32769, BF16), (1 << 20, 1 << 10, (1 << 10) + 1, BF16)])
+def test_orthogonal_sizes_out_of_range(lib, count, rows, cols, dtype):
+    assert _bytes(lib.lcn_orthogonalise_workspace_bytes, count, rows, cols, dtype)[0] == ERR_INVALID_ARG
+    assert lib.lcn_orthogonalise(FAKE, count, rows, cols, dtype, 5, UPDATE, 1e-7, 1.0, FAKE, FAKE, 1 << 62, None) == ERR_INVALID_ARG
+
+
+def test_orthogonal_arguments(lib):
+    good = [FAKE, 1, 200, 600, F32, 5, UPDATE, 1e-7, 1.0, FAKE, FAKE, 0, None]
+    for at, value in ((0, None), (6, None), (9, None), (5, 0), (5, 65), (7, -1.0), (7, float("nan")), (7, float("inf")),
+                      (8, float("inf")), (8, float("nan"))):
+        bad = list(good)
+        bad[at] = value
+        assert lib.lcn_orthogonalise(*bad) == ERR_INVALID_ARG
+    for c in (_triples(4.1, 0.0, 0.0), _triples(float("nan"), 0.0, 0.0), _triples(1.0, float("inf"), 0.0), _triples(70.0, -1000.0, 1000.0),
+              _triples(0.0, 0.0, 4.5), _triples(3.0, -8.0, 12.0)):
+        bad = list(good)
+        bad[5], bad[6] = 1, c
+        assert lib.lcn_orthogonalise(*bad) == ERR_INVALID_ARG
+    # values that a first step lets grow are seen by the next: 2 s four times over leaves 16
+    bad = list(good)
+    bad[5], bad[6] = 4, _triples(*(2.0, 0.0, 0.0) * 4)
+    assert lib.lcn_orthogonalise(*bad) == ERR_INVALID_ARG
+    for c in (_triples(4.0, 0.0, 0.0), _triples(3.4445, -4.7750, 2.0315), _triples(1.5, -0.5, 0.0), _triples(0.0, 0.0, 0.0)):
+        ok = list(good)
+        ok[5], ok[6] = 1, c
+        assert lib.lcn_orthogonalise(*ok) == ERR_ALLOC
+
+
+def test_orthogonal_workspaces(lib):
+    for dtype in (F32, BF16):
+        for count, rows, cols in ((1, 20, 60), (8, 96, 32), (1, 300, 300), (4, 8192, 1024)):
+            st, n = _bytes(lib.lcn_orthogonalise_workspace_bytes, count, rows, cols, dtype)
+            assert st == OK
+            if n:
+                for space, size in ((FAKE, n - 1), (None, n), (FAKE + 64, n)):
+                    assert lib.lcn_orthogonalise(FAKE, count, rows, cols, dtype, 5, UPDATE, 1e-7, 1.0, FAKE, space, size,
+                                                 None) == ERR_ALLOC
+    assert _bytes(lib.lcn_orthogonalise_workspace_bytes, 0, 4, 4, F32) == (OK, 0)
+    assert lib.lcn_orthogonalise(None, 0, 4, 4, F32, 5, UPDATE, 1e-7, 1.0, None, None, 0, None) == OK
+
+
+def test_orthogonal_tensors_that_are_not_on_a_device():
+    with pytest.raises(ValueError):
+        lcn.lcn_orthogonalise(torch.ones(4, 6))
