@@ -4,8 +4,10 @@
 //   dx = rstd (g - mean of g - xhat mean of (g xhat)) + around,  g = dy w,  xhat = (x - mean) rstd
 //   dw = sum over rows of dy xhat,  db = sum over rows of dy
 //
-// A workgroup per row, which reads it three times (the variance is formed from differences to the mean); the sums over
-// rows by a kernel of their own.
+// Bound by memory: a row is read once and stays in registers (so its variance is formed from differences to its mean), by as
+// many lanes as hold it in 16-byte pieces: 4 to 64, so that a wavefront has several narrow rows, or a workgroup.  Backward, a
+// thread keeps its columns from row to row and adds up dw and db for them; a workgroup leaves one partial sum per column.
+// Rows too long for that are read by a workgroup in a loop, several times, with the sums over rows in a kernel of their own.
 #include "operators.h"
 
 namespace lcn {
@@ -14,6 +16,191 @@ template <class T, int V>
 struct Piece {
     typedef T type __attribute__((ext_vector_type(V)));
 };
+
+// Sums over the L lanes (or the workgroup's 256 threads) that share a row, in each of them.  `lds`: 4 values of the workgroup's
+// own, others from one call to the next (whoever is late still reads the last call's).
+template <int L>
+__device__ __forceinline__ float sum_over(float a, float *lds)
+{
+    constexpr int W = L < 64 ? L : 64;
+#pragma unroll
+    for (int o = W / 2; o > 0; o >>= 1) a += __shfl_xor(a, o, W);
+    if constexpr (L > 64) {
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = a;
+        __syncthreads();
+        a = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    }
+    return a;
+}
+
+// L lanes have a row, C pieces of V values each.
+template <class T, int V, int L, int C>
+__global__ __launch_bounds__(256) void norm_kernel(const T *x, const T *__restrict__ w, const T *__restrict__ b, long long rows,
+                                                   int dim, float eps, T *y,   // y may be x
+                                                   float *__restrict__ mean_out, float *__restrict__ rstd_out)
+{
+    typedef typename Piece<T, V>::type piece;
+    __shared__ float lds[2][4];
+    const int lane = threadIdx.x % L, units = dim / V;
+    const long long r = (long long)group_number() * (256 / L) + threadIdx.x / L;
+    if (L > 64 && r >= rows) return;
+    const bool here = r < rows;
+    piece p[C];
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int u = c * L + lane;
+        p[c] = here && u < units ? ((const piece *)(x + r * dim))[u] : piece{};
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum += (float)p[c][e];
+    const float mean = sum_over<L>(sum, lds[0]) / (float)dim;
+    float square = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+        if (c * L + lane < units)
+#pragma unroll
+            for (int e = 0; e < V; ++e) square += ((float)p[c][e] - mean) * ((float)p[c][e] - mean);
+    const float rstd = 1.f / sqrtf(sum_over<L>(square, lds[1]) / (float)dim + eps);
+    if (!here) return;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int u = c * L + lane;
+        if (u >= units) break;
+        piece o, pw, pb;
+        if (w) pw = ((const piece *)w)[u];
+        if (b) pb = ((const piece *)b)[u];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            float v = ((float)p[c][e] - mean) * rstd;
+            if (w) v *= (float)pw[e];
+            if (b) v += (float)pb[e];
+            o[e] = (T)v;
+        }
+        ((piece *)(y + r * dim))[u] = o;
+    }
+    if (lane == 0) {
+        if (mean_out) mean_out[r] = mean;
+        if (rstd_out) rstd_out[r] = rstd;
+    }
+}
+
+// Rows g, g + gridDim.x, ... (256 / L at a time) for workgroup g: dx (nullable), and the workgroup's sums of dy xhat and dy for
+// every column at part[g][0 .. 1] (nullable).  With one or two pieces per lane the next row is requested before this one is
+// worked on.
+template <class T, int V, int L, int C>
+__global__ __launch_bounds__(256) void norm_grad_kernel(const T *__restrict__ x, const T *__restrict__ w,
+                                                        const float *__restrict__ mean_in, const float *__restrict__ rstd_in,
+                                                        const T *__restrict__ dy, const T *around, long long rows, int dim,
+                                                        T *dx,   // dx may be around
+                                                        float *__restrict__ part)
+{
+    typedef typename Piece<T, V>::type piece;
+    constexpr int PER = 256 / L, WIDTH = L * C * V;
+    constexpr bool AHEAD = C <= 2;
+    __shared__ float lds[2][2][4];
+    __shared__ float columns[L > 64 ? 1 : 4 * WIDTH];
+    const int lane = threadIdx.x % L, units = dim / V;
+    const long long step = (long long)gridDim.x * PER;
+    struct Row {
+        piece x[C], dy[C], around[C];
+        float mean, rstd;
+    };
+    auto read = [&](long long r) {
+        Row t;
+        const bool here = r < rows;
+        t.mean = here ? mean_in[r] : 0.f;
+        t.rstd = here ? rstd_in[r] : 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int u = c * L + lane;
+            const bool in = here && u < units;
+            t.x[c] = in ? ((const piece *)(x + r * dim))[u] : piece{};
+            t.dy[c] = in ? ((const piece *)(dy + r * dim))[u] : piece{};
+            t.around[c] = in && around ? ((const piece *)(around + r * dim))[u] : piece{};
+        }
+        return t;
+    };
+    piece pw[C];
+    float dw[C][V], db[C][V];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        pw[c] = w && c * L + lane < units ? ((const piece *)w)[c * L + lane] : piece{};
+#pragma unroll
+        for (int e = 0; e < V; ++e) dw[c][e] = db[c][e] = 0.f;
+    }
+    // every thread makes the same number of rounds: the sums over a workgroup wait for all of it
+    long long r = (long long)blockIdx.x * PER + threadIdx.x / L;
+    int turn = 0;
+    Row next{};
+    if (AHEAD) next = read(r);
+    for (long long first = (long long)blockIdx.x * PER; first < rows; first += step, r += step, turn ^= 1) {
+        Row t = AHEAD ? next : read(r);
+        if (AHEAD && first + step < rows) next = read(r + step);
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float d = (float)t.dy[c][e], h = ((float)t.x[c][e] - t.mean) * t.rstd, g = w ? d * (float)pw[c][e] : d;
+                s1 += g;
+                s2 += g * h;
+                dw[c][e] += d * h;
+                db[c][e] += d;
+            }
+        if (!dx) continue;
+        s1 = sum_over<L>(s1, lds[turn][0]) / (float)dim;
+        s2 = sum_over<L>(s2, lds[turn][1]) / (float)dim;
+        if (r >= rows) continue;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int u = c * L + lane;
+            if (u >= units) break;
+            piece o;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float d = (float)t.dy[c][e], h = ((float)t.x[c][e] - t.mean) * t.rstd, g = w ? d * (float)pw[c][e] : d;
+                float v = t.rstd * (g - s1 - h * s2);
+                if (around) v += (float)t.around[c][e];
+                o[e] = (T)v;
+            }
+            ((piece *)(dx + r * dim))[u] = o;
+        }
+    }
+    if (!part) return;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float(&v)[C][V] = which ? db : dw;
+        float *to = part + ((long long)blockIdx.x * 2 + which) * dim;
+        if constexpr (L > 64) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (c * L + lane < units) to[(c * L + lane) * V + e] = v[c][e];
+        } else {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+#pragma unroll
+                    for (int o = L; o < 64; o <<= 1) v[c][e] += __shfl_xor(v[c][e], o);
+            __syncthreads();
+            if ((threadIdx.x & 63) < L)
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) columns[(threadIdx.x >> 6) * WIDTH + (c * L + lane) * V + e] = v[c][e];
+            __syncthreads();
+            for (int i = threadIdx.x; i < dim; i += 256)
+                to[i] = (columns[i] + columns[WIDTH + i]) + (columns[2 * WIDTH + i] + columns[3 * WIDTH + i]);
+        }
+    }
+}
+
+// ---- rows that no workgroup holds in registers ---------------------------------
 
 // The sums of a and b over the workgroup, in every thread.
 __device__ __forceinline__ void sum_over_group(float &a, float &b, float (*lds)[2])
@@ -37,7 +224,7 @@ __device__ __forceinline__ void sum_over_group(float &a, float &b, float (*lds)[
 }
 
 template <class T, int V>
-__global__ __launch_bounds__(256) void norm_kernel(const T *x, const T *__restrict__ w, const T *__restrict__ b,
+__global__ __launch_bounds__(256) void norm_long_kernel(const T *x, const T *__restrict__ w, const T *__restrict__ b,
                                                    long long rows, int dim, float eps, T *y,   // y may be x
                                                    float *__restrict__ mean_out, float *__restrict__ rstd_out)
 {
@@ -84,7 +271,7 @@ __global__ __launch_bounds__(256) void norm_kernel(const T *x, const T *__restri
 }
 
 template <class T, int V>
-__global__ __launch_bounds__(256) void norm_dx_kernel(const T *__restrict__ x, const T *__restrict__ w,
+__global__ __launch_bounds__(256) void norm_long_dx_kernel(const T *__restrict__ x, const T *__restrict__ w,
                                                       const float *__restrict__ mean_in, const float *__restrict__ rstd_in,
                                                       const T *__restrict__ dy, const T *around, long long rows,
                                                       int dim, T *dx)   // dx may be around
@@ -149,22 +336,23 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(const T *__restrict__
     }
 }
 
-// Adds up the partial sums of dw (columns 0 .. dim - 1) and db (the dim behind): 32 columns per workgroup, 8 threads each,
-// in a fixed order.
+// Adds up the partial sums of dw (columns 0 .. dim - 1) and db (the dim behind): 16 columns per workgroup, 16 threads each, in a
+// fixed order.
 template <class T>
 __global__ __launch_bounds__(256) void norm_join_kernel(const float *__restrict__ part, int parts, int dim, T *__restrict__ dw,
                                                         T *__restrict__ db)
 {
-    __shared__ float sums[8][33];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), q = threadIdx.x >> 5, width = 2 * dim;
+    __shared__ float sums[16][17];
+    const int c = blockIdx.x * 16 + (threadIdx.x & 15), q = threadIdx.x >> 4, width = 2 * dim;
     float v = 0.f;
     if (c < width)
-        for (int r = q; r < parts; r += 8) v += part[(long long)r * width + c];
-    sums[q][threadIdx.x & 31] = v;
+#pragma unroll 8
+        for (int r = q; r < parts; r += 16) v += part[(long long)r * width + c];
+    sums[q][threadIdx.x & 15] = v;
     __syncthreads();
     if (q || c >= width) return;
 #pragma unroll
-    for (int u = 1; u < 8; ++u) v += sums[u][threadIdx.x];
+    for (int u = 1; u < 16; ++u) v += sums[u][threadIdx.x];
     if (c < dim) {
         if (dw) dw[c] = (T)v;
     } else if (db) {
@@ -180,8 +368,9 @@ static bool norm_args_fit(int64_t rows, int32_t dim, int32_t dtype)
            (dtype == LCN_F32 || dtype == LCN_BF16);
 }
 
-// Workgroups that share the rows of the sums of dw and db, each with partial sums of its own.
-static int norm_groups(int64_t rows) { return (int)(rows < 256 ? rows : 256); }
+// Partial sums of dw and db: one per workgroup that shares the rows.  As many workgroups as keep memory busy; more cost their
+// sums' way through memory.
+static int norm_groups(int64_t rows) { return (int)(rows < 512 ? rows : 512); }
 static size_t norm_backward_space(int64_t rows, int32_t dim)
 {
     return ((size_t)norm_groups(rows) * 2 * dim * 4 + 255) & ~(size_t)255;
@@ -201,13 +390,61 @@ static hipError_t by_width(uintptr_t addresses, int32_t dim, F f)
     return f(Width<1>());
 }
 
+// Calls f with the lanes that share a row of `units` pieces and the pieces of each as a type; false: a row is too long for that.
+// With many rows a row gets few lanes with several pieces each (more loads of a wavefront at once, sums over fewer lanes), as many
+// slots as it has pieces or little more; with few rows it gets all the lanes that it can use.  20 000 rows of 300, forward and
+// backward, us: 16 x 5 lanes x pieces float 9 + 19, bf16 7 + 14; 64 x 2 11 + 19, 9 + 19; of 301 (single values), 64 x 5 12 + 20 and
+// 10 + 19, 256 x 2 22 + 45 and 21 + 45; 16 391 of 2048 in bf16, 64 x 4 23 + 39, 256 x 1 28 + 49; of 4096, 64 x 8 46 + 117,
+// 256 x 2 43 + 83; 40 000 float rows of 256, 32 x 2 15 + 25, 64 x 1 16 + 25.
+template <int L, int C>
+struct Lanes {
+    static constexpr int lanes = L, pieces = C;
+};
+template <int V, class F>
+static bool by_lanes(int units, int64_t rows, hipError_t &st, F f)
+{
+    const bool many = rows >= 2048;
+    if (many && units > 32 && units <= 64) {
+        st = f(Lanes<32, 2>());
+    } else if (many && units > 64 && units <= 80) {
+        st = f(Lanes<16, 5>());
+    } else if (many && units > 80 && units <= 96) {
+        st = f(Lanes<32, 3>());
+    } else if (many && units > 128 && units <= 256) {
+        st = f(Lanes<64, 4>());
+    } else if (many && V == 1 && units > 256 && units <= 512) {   // single values: a wavefront's registers hold them easily
+        st = units <= 320 ? f(Lanes<64, V == 1 ? 5 : 4>()) : f(Lanes<64, V == 1 ? 8 : 4>());
+    } else {
+        st = units <= 4      ? f(Lanes<4, 1>())
+             : units <= 8    ? f(Lanes<8, 1>())
+             : units <= 16   ? f(Lanes<16, 1>())
+             : units <= 32   ? f(Lanes<32, 1>())
+             : units <= 64   ? f(Lanes<64, 1>())
+             : units <= 128  ? f(Lanes<64, 2>())
+             : units <= 256  ? f(Lanes<256, 1>())
+             : units <= 512  ? f(Lanes<256, 2>())
+             : units <= 1024 ? f(Lanes<256, 4>())
+             : units <= 2048 ? f(Lanes<256, 8>())
+                             : hipSuccess;
+    }
+    return units <= 2048;
+}
+
 template <class T>
 static lcn_status norm_as(const T *x, const T *w, const T *b, int64_t rows, int32_t dim, float eps, T *y, float *mean,
                           float *rstd, hipStream_t s)
 {
     OPCHK(by_width<T>((uintptr_t)x | (uintptr_t)w | (uintptr_t)b | (uintptr_t)y, dim, [&](auto v) {
-        hipLaunchKernelGGL((norm_kernel<T, decltype(v)::value>), grid_of(rows), dim3(256), 0, s, x, w, b, (long long)rows, dim, eps,
-                           y, mean, rstd);
+        constexpr int V = decltype(v)::value;
+        hipError_t st;
+        if (by_lanes<V>(dim / V, rows, st, [&](auto l) {
+                constexpr int L = decltype(l)::lanes, C = decltype(l)::pieces;
+                hipLaunchKernelGGL((norm_kernel<T, V, L, C>), grid_of((rows + 256 / L - 1) / (256 / L)), dim3(256), 0, s, x, w, b,
+                                   (long long)rows, dim, eps, y, mean, rstd);
+                return hipGetLastError();
+            }))
+            return st;
+        hipLaunchKernelGGL((norm_long_kernel<T, V>), grid_of(rows), dim3(256), 0, s, x, w, b, (long long)rows, dim, eps, y, mean, rstd);
         return hipGetLastError();
     }));
     return LCN_OK;
@@ -218,21 +455,31 @@ static lcn_status norm_backward_as(const T *x, const T *w, const float *mean, co
                                    int64_t rows, int32_t dim, T *dx, T *dw, T *db, float *part, hipStream_t s)
 {
     const uintptr_t all = (uintptr_t)x | (uintptr_t)w | (uintptr_t)dy | (uintptr_t)around | (uintptr_t)dx;
-    if (dx)
-        OPCHK(by_width<T>(all, dim, [&](auto v) {
-            hipLaunchKernelGGL((norm_dx_kernel<T, decltype(v)::value>), grid_of(rows), dim3(256), 0, s, x, w, mean, rstd, dy, around,
-                               (long long)rows, dim, dx);
-            return hipGetLastError();
-        }));
-    if (!dw && !db) return LCN_OK;
-    const int groups = norm_groups(rows);
-    OPCHK(by_width<T>((uintptr_t)x | (uintptr_t)dy, dim, [&](auto v) {
+    const int most = norm_groups(rows);
+    const bool sums = dw || db;
+    int groups = most;
+    OPCHK(by_width<T>(all, dim, [&](auto v) {
         constexpr int V = decltype(v)::value;
+        hipError_t st;
+        if (by_lanes<V>(dim / V, rows, st, [&](auto l) {
+                constexpr int L = decltype(l)::lanes, C = decltype(l)::pieces;
+                const int64_t needed = (rows + 256 / L - 1) / (256 / L);
+                groups = (int)(needed < most ? needed : most);
+                hipLaunchKernelGGL((norm_grad_kernel<T, V, L, C>), dim3((unsigned)groups), dim3(256), 0, s, x, w, mean, rstd, dy, around,
+                                   (long long)rows, dim, dx, sums ? part : nullptr);
+                return hipGetLastError();
+            }))
+            return st;
+        if (dx) hipLaunchKernelGGL((norm_long_dx_kernel<T, V>), grid_of(rows), dim3(256), 0, s, x, w, mean, rstd, dy, around,
+                                   (long long)rows, dim, dx);
+        st = hipGetLastError();
+        if (st != hipSuccess || !sums) return st;
         hipLaunchKernelGGL((norm_columns_kernel<T, V>), dim3((unsigned)((dim / V + 255) / 256), (unsigned)groups), dim3(256), 0, s, x,
                            mean, rstd, dy, (long long)rows, dim, part);
         return hipGetLastError();
     }));
-    hipLaunchKernelGGL(norm_join_kernel<T>, dim3((unsigned)((2 * dim + 31) / 32)), dim3(256), 0, s, part, groups, dim, dw, db);
+    if (!sums) return LCN_OK;
+    hipLaunchKernelGGL(norm_join_kernel<T>, dim3((unsigned)((2 * dim + 15) / 16)), dim3(256), 0, s, part, groups, dim, dw, db);
     OPCHK(hipGetLastError());
     return LCN_OK;
 }

@@ -79,7 +79,8 @@ def test_addresses_of_one_element(dim, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("rows,dim", [(30000, 32), (20000, 300), (5000, 2048)])
+@pytest.mark.parametrize("rows,dim", [(30000, 32), (20000, 300), (5000, 2048), (2048, 60), (2049, 129), (2200, 333), (2100, 350), (3001, 301),
+                                      (2050, 1200), (2300, 200), (2111, 500), (2048, 4096)])
 def test_many_rows(rows, dim, dtype):
     check(rows, dim, dtype)
 
