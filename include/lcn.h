@@ -495,17 +495,20 @@ lcn_status lcn_attention_backward(const lcn_attention_desc *desc, const void *q,
 
 /* y = act(g) .* u with g = x Wg^T + bg and u = x Wu^T + bu: the gated half of a feed-forward block
  * (its other half is lcn_linear).  x rows x d_in; W (2 d_out) x d_in, Wg above Wu; bias (bg before bu,
- * 2 d_out; nullable); y rows x d_out.  pre (nullable): the fp32 values g and u for the backward pass,
- * rows x (2 d_out), g before u in every row.  Sizes: 0 <= rows <= 2^30, 1 <= d_in <= 2^20, 1 <= d_out <= 2^19,
- * rows times d_in or 2 d_out <= 2^42.  Up to 8 rows need no workspace (the call says 0 bytes). */
+ * 2 d_out; nullable); y rows x d_out.  kept (nullable, 16-byte aligned, as many bytes as the call below
+ * says): g and u for the backward pass, in a layout of the library's own: floats with float tensors; with bf16
+ * tensors 16 bits a value, within 2^-14 of the power of two above the largest of eight neighbours.
+ * Sizes: 0 <= rows <= 2^30, 1 <= d_in <= 2^20, 1 <= d_out <= 2^19, rows times d_in or 2 d_out <= 2^42.  Up to 8
+ * rows need no workspace (the call says 0 bytes). */
 lcn_status lcn_gated_linear_workspace_bytes(int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype, int32_t backward,
                                             size_t *bytes);
+lcn_status lcn_gated_linear_kept_bytes(int64_t rows, int32_t d_out, int32_t dtype, size_t *bytes);
 lcn_status lcn_gated_linear(const void *x, const void *W, const void *bias, int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype,
-                            int32_t activation, void *y, float *pre, void *workspace, size_t workspace_bytes, void *hip_stream);
+                            int32_t activation, void *y, void *kept, void *workspace, size_t workspace_bytes, void *hip_stream);
 /* Its gradients for a given dy: with dz = [dy .* u .* act'(g) | dy .* act(g)],
  *   dx = dz W (rows x d_in),  dW = dz^T x ((2 d_out) x d_in),  dbias = column sums of dz (2 d_out).
  * dx, dW, dbias are nullable; x may be NULL if dW is, W if dx is. */
-lcn_status lcn_gated_linear_backward(const void *x, const void *W, const float *pre, const void *dy, int64_t rows, int32_t d_in,
+lcn_status lcn_gated_linear_backward(const void *x, const void *W, const void *kept, const void *dy, int64_t rows, int32_t d_in,
                                      int32_t d_out, int32_t dtype, int32_t activation, void *dx, void *dW, void *dbias,
                                      void *workspace, size_t workspace_bytes, void *hip_stream);
 

@@ -3,33 +3,198 @@
 // Backward: dz = [dy u act'(g) | dy act(g)] once (as planes of bf16, with the column sums that are the biases' gradients), then
 // dx = dz W and dW = dz^T x, which are two products because g's and u's halves lie in one matrix.
 //
-// Rounding: g, u, sums and activations are in 32 bits; with bf16 tensors y, dz, dx, dW and db are rounded once each, the kept g
-// and u are not (as bf16 each would add an error to dz of the size of dz's own rounding).
+// Rounding: g, u, sums and activations are in 32 bits; with bf16 tensors y, dz, dx, dW and db are rounded once each.  What is
+// kept of g and u for the backward pass is 16 bits a value for bf16 tensors, with 14 bits of significand for the largest of eight
+// (below); as bf16 each would add an error to dz of the size of dz's own rounding, as floats they are half of what moves.
 #include "operators.h"
 
 namespace lcn {
+
+// ---- what is kept of g and u: rows x 2 (g, u) x padded(d_out), in pieces of eight values ----
+// Float: as they are.  bf16 tensors: eight 16-bit words, of which the upper 15 bits are a value's multiple of a power of two and the
+// lowest is a bit of the piece's exponent code, so that a piece is 16 bytes.  The code is the largest value's exponent field (15 at
+// least): multiples are rounded to half of 2^-14 of the power of two above the largest value, 1.8e-5 of it in the root mean square where
+// bf16 leaves 1.6e-3 of each value.  Code 255, with a value that is not finite: the words are bf16, but for their lowest bits.
+template <class T>
+struct Keep;
+template <>
+struct Keep<float> {
+    typedef float type;
+    static __device__ __forceinline__ void store(float *p, const f32x4 (&v)[2])
+    {
+        ((f32x4 *)p)[0] = v[0];
+        ((f32x4 *)p)[1] = v[1];
+    }
+    static __device__ __forceinline__ void load(const float *p, f32x4 (&v)[2])
+    {
+        v[0] = ((const f32x4 *)p)[0];
+        v[1] = ((const f32x4 *)p)[1];
+    }
+};
+template <>
+struct Keep<__bf16> {
+    typedef unsigned short type;
+    typedef unsigned words __attribute__((ext_vector_type(4)));   // values 2 i and 2 i + 1 of the piece
+    static __device__ __forceinline__ void store(unsigned short *p, const f32x4 (&v)[2])
+    {
+        unsigned top = 15u << 23;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = v[e >> 2][e & 3];
+            const unsigned b = __builtin_bit_cast(unsigned, x) & 0x7fffffffu;
+            top = b > top ? b : top;
+        }
+        const unsigned code = top >> 23;
+        words w;
+        if (code < 255) {
+            // multiples of up to 16383: 2^(140 - code) 16383 / 16384; adding 3 * 2^22 leaves them in the lowest bits, rounded
+            const float scale = __builtin_bit_cast(float, (267u - code) << 23) * (16383.f / 16384.f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float a = __builtin_fmaf(v[i >> 1][(i & 1) * 2], scale, 12582912.f);
+                const float b = __builtin_fmaf(v[i >> 1][(i & 1) * 2 + 1], scale, 12582912.f);
+                w[i] = (__builtin_bit_cast(unsigned, a) << 1 & 0xfffeu) | __builtin_bit_cast(unsigned, b) << 17;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const unsigned short a = __builtin_bit_cast(unsigned short, (__bf16)v[i >> 1][(i & 1) * 2]);
+                const unsigned short b = __builtin_bit_cast(unsigned short, (__bf16)v[i >> 1][(i & 1) * 2 + 1]);
+                w[i] = (a & 0xfffeu) | (b & 0xfffeu) << 16;
+            }
+        }
+        const unsigned bits = (code & 15u) | (code & 0xf0u) << 12;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] |= bits >> i & 0x10001u;
+        *(words *)p = w;
+    }
+    static __device__ __forceinline__ void load(const unsigned short *p, f32x4 (&v)[2])
+    {
+        const words w = *(const words *)p;
+        unsigned bits = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bits |= (w[i] & 0x10001u) << i;
+        const unsigned code = (bits & 15u) | (bits >> 12 & 0xf0u);
+        // 2^(code - 141), the words being twice the multiples
+        const float scale = __builtin_bit_cast(float, (code - 14u) << 23) * (16384.f / 16383.f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned one = w[i] & 0xfffeu, two = w[i] & 0xfffe0000u;
+            v[i >> 1][(i & 1) * 2] = (float)(short)one * scale;
+            v[i >> 1][(i & 1) * 2 + 1] = (float)((int)two >> 16) * scale;
+        }
+        if (code == 255)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[i >> 1][(i & 1) * 2] = __builtin_bit_cast(float, (w[i] & 0xfffeu) << 16);
+                v[i >> 1][(i & 1) * 2 + 1] = __builtin_bit_cast(float, w[i] & 0xfffe0000u);
+            }
+    }
+};
+
+// act(g), and its slope.  With bf16 tensors the sigmoid is the exponential and reciprocal instructions alone, each within 2^-22: the
+// kernels here are bound by such operations otherwise (gated_slope_kernel 192 us instead of 138 for 16391 x 4096).
+template <class T>
+__device__ __forceinline__ float sigmoid(float z)
+{
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_rcpf(1.f + exp2_fast(z * -1.44269504088896341f));
+    return 1.f / (1.f + expf(-z));
+}
+template <class T, int ACT>
+__device__ __forceinline__ float gate(float g)
+{
+    if constexpr (ACT == LCN_ACT_SILU) return g * sigmoid<T>(g);
+    return activate<ACT>(g);
+}
+template <class T, int ACT>
+__device__ __forceinline__ void gate_and_slope(float g, float &a, float &slope)
+{
+    if constexpr (ACT == LCN_ACT_SILU) {
+        const float f = sigmoid<T>(g);
+        a = g * f;
+        slope = __builtin_fmaf(a, 1.f - f, f);
+    } else if constexpr (ACT == LCN_ACT_TANH) {
+        a = tanhf(g);
+        slope = 1.f - a * a;
+    } else if constexpr (ACT == LCN_ACT_GELU) {
+        const float f = 0.5f * (1.f + erff(g * 0.70710678118654752f));
+        a = g * f;
+        slope = f + g * expf(-0.5f * g * g) * 0.39894228040143268f;
+    } else {
+        a = activate<ACT>(g);
+        slope = activate_slope<ACT>(g);
+    }
+}
 
 template <class T>
 struct GatedArgs {
     const T *bias;   // 2 width
     T *y;
-    float *pre;      // rows x 2 width, nullable
-    int act, whole;  // whole: rows of y, bias and pre, and their halves, are whole 16-byte pieces
+    typename Keep<T>::type *kept;   // nullable
+    int act, whole;  // whole: rows of y and both halves of bias are whole 16-byte pieces
 };
 
-// eight outputs from g and u, which have their biases: y and pre at row n, column m
+// eight outputs from g and u, which have their biases: at row n, column m (a multiple of 8)
 template <class T, int ACT>
 __device__ __forceinline__ void gated_finish(const GatedArgs<T> &e, f32x4 (&g)[2], const f32x4 (&u)[2], long long n, int m, int width)
 {
-    const int left = width - m;
-    if (e.pre) {
-        store_eight(e.pre + n * 2 * width + m, g, left, e.whole);
-        store_eight(e.pre + (n * 2 + 1) * width + m, u, left, e.whole);
+    if (e.kept) {
+        const long long dp = padded(width);
+        Keep<T>::store(e.kept + n * 2 * dp + m, g);
+        Keep<T>::store(e.kept + (n * 2 + 1) * dp + m, u);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) g[i >> 2][i & 3] = activate<ACT>(g[i >> 2][i & 3]) * u[i >> 2][i & 3];
-    store_eight(e.y + n * width + m, g, left, e.whole);
+    for (int i = 0; i < 8; ++i) g[i >> 2][i & 3] = gate<T, ACT>(g[i >> 2][i & 3]) * u[i >> 2][i & 3];
+    store_eight(e.y + n * width + m, g, width - m, e.whole);
 }
+
+// The product's epilogue: subtiles of 16 rows are g's and u's in turn.  A wavefront's 16 columns n go through LDS row by row, as in
+// by_rows, and a lane takes up eight consecutive values of g and the eight of u that belong to them.
+template <class T, int ACT>
+struct GatedEpilogue {
+    typedef GatedArgs<T> Args;
+    template <int TM, int TN, int WM, int WN>
+    static __device__ void run(const Args &e, const ProductArgs &p, f32x4 (&acc)[TM][TN], long long m0, long long n0, int,
+                               char *lds, int, int)
+    {
+        static_assert(TM % 2 == 0, "whole pairs");
+        constexpr int PITCH = RowRegion<TM>::PITCH;
+        const int lane = threadIdx.x & 63;
+        float *f = (float *)(lds + (threadIdx.x >> 6) * RowRegion<TM>::BYTES);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i) *(f32x4 *)(f + (lane & 15) * PITCH + i * 16 + 4 * (lane >> 4)) = acc[i][j];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // LDS serves a wavefront in order
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+            for (int q = lane; q < 16 * TM; q += 64) {
+                const int r = q / TM, c = q % TM * 8, m = (int)m0 + c;
+                const long long n = n0 + j * 16 + r;
+                if (n >= p.n || m >= p.m) continue;
+                const float *at = f + r * PITCH + (c >> 4) * 32 + (c & 15);
+                f32x4 g[2], u[2], b[2];
+                g[0] = *(const f32x4 *)at;
+                g[1] = *(const f32x4 *)(at + 4);
+                u[0] = *(const f32x4 *)(at + 16);
+                u[1] = *(const f32x4 *)(at + 20);
+                if (e.bias) {
+                    load_eight(e.bias + m, p.m - m, e.whole, b);
+                    g[0] += b[0];
+                    g[1] += b[1];
+                    load_eight(e.bias + p.m + m, p.m - m, e.whole, b);
+                    u[0] += b[0];
+                    u[1] += b[1];
+                }
+                gated_finish<T, ACT>(e, g, u, n, m, p.m);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+};
+template <class T, int ACT>
+constexpr bool paired_rows<GatedEpilogue<T, ACT>> = true;
 
 // from the sums of [g | u] in memory, `splits` partial ones each
 template <class T, int ACT>
@@ -60,41 +225,51 @@ __global__ __launch_bounds__(256) void gated_finish_kernel(GatedArgs<T> e, const
     }
 }
 
-// Few rows: bound by reading W once; 16 lanes read a row of Wg and the one of Wu that belongs to it.
+// Few rows: bound by reading W once; 16 lanes read a row of Wg and the one of Wu that belongs to it, a workgroup has 16 outputs.
 template <class T, int R, bool VEC>
 __global__ __launch_bounds__(256) void gated_few_kernel(GatedArgs<T> e, const T *__restrict__ x, const T *__restrict__ w, int rows,
                                                         int k, int width)
 {
-    const int f = (int)(blockIdx.x * 16 + (threadIdx.x >> 4));
-    if (f >= width) return;
+    __shared__ float z[R][2][16];
+    const int group = threadIdx.x >> 4, f = (int)blockIdx.x * 16 + group, lane = threadIdx.x & 15;
+    const int fr = f < width ? f : width - 1;
     float sum[2][R];
 #pragma unroll
     for (int r = 0; r < R; ++r) sum[0][r] = sum[1][r] = 0.f;
-    few_rows_dot<T, R, VEC>(w + (long long)f * k, w + (long long)(width + f) * k, x, rows, k, sum);
-    const int r = threadIdx.x & 15;   // lane r finishes one value
-    if (r >= rows) return;
-    float g = 0.f, u = 0.f;
+    few_rows_dot<T, R, VEC>(w + (long long)fr * k, w + (long long)(width + fr) * k, x, rows, k, sum);
+    float g = 0.f, u = 0.f;   // lane r finishes one value
 #pragma unroll
     for (int i = 0; i < R; ++i)
-        if (i == r) {
+        if (i == lane) {
             g = sum[0][i];
             u = sum[1][i];
         }
     if (e.bias) {
-        g += (float)e.bias[f];
-        u += (float)e.bias[width + f];
+        g += (float)e.bias[fr];
+        u += (float)e.bias[width + fr];
     }
-    if (e.pre) {
-        e.pre[(long long)r * 2 * width + f] = g;
-        e.pre[((long long)r * 2 + 1) * width + f] = u;
+    if (e.kept && lane < R) {
+        z[lane][0][group] = f < width ? g : 0.f;
+        z[lane][1][group] = f < width ? u : 0.f;
     }
-    switch (e.act) {
-    case LCN_ACT_TANH: g = activate<LCN_ACT_TANH>(g); break;
-    case LCN_ACT_RELU: g = activate<LCN_ACT_RELU>(g); break;
-    case LCN_ACT_GELU: g = activate<LCN_ACT_GELU>(g); break;
-    case LCN_ACT_SILU: g = activate<LCN_ACT_SILU>(g); break;
+    if (lane < rows && f < width) {
+        switch (e.act) {
+        case LCN_ACT_TANH: g = gate<T, LCN_ACT_TANH>(g); break;
+        case LCN_ACT_RELU: g = gate<T, LCN_ACT_RELU>(g); break;
+        case LCN_ACT_GELU: g = gate<T, LCN_ACT_GELU>(g); break;
+        case LCN_ACT_SILU: g = gate<T, LCN_ACT_SILU>(g); break;
+        }
+        e.y[(long long)lane * width + f] = (T)(g * u);
     }
-    e.y[(long long)r * width + f] = (T)(g * u);
+    if (!e.kept) return;
+    __syncthreads();
+    // two pieces of g and two of u for every row
+    const int r = threadIdx.x >> 2, half = threadIdx.x >> 1 & 1, m = (int)blockIdx.x * 16 + (threadIdx.x & 1) * 8;
+    if (r >= rows || m >= width) return;
+    f32x4 v[2];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = z[r][half][(threadIdx.x & 1) * 8 + i];
+    Keep<T>::store(e.kept + ((long long)r * 2 + half) * padded(width) + m, v);
 }
 
 template <class T, int R>
@@ -109,43 +284,48 @@ static hipError_t launch_few(const GatedArgs<T> &e, const T *x, const T *w, int 
 }
 
 // dz as planes (dst: nullable; rows of dp values, zero behind 2 width), and the sums over this workgroup's rows for every column
-// (part: nullable).  32 pieces of eight columns of either half x 8 rows at a time.
-template <class T, int ACT>
-__global__ __launch_bounds__(256) void gated_slope_kernel(const T *__restrict__ dy, const float *__restrict__ pre, long long rows,
-                                                          int width, int dp, int rows_each, int whole, int planes,
+// (part: nullable).  C pieces of eight columns of either half x 256 / C rows at a time.
+template <class T, int ACT, int C, int PLANES>
+__global__ __launch_bounds__(256) void gated_slope_kernel(const T *__restrict__ dy, const typename Keep<T>::type *__restrict__ kept,
+                                                          long long rows, int width, int dp, int rows_each, int whole,
                                                           __bf16 *__restrict__ dst, float *__restrict__ part)
 {
-    __shared__ float sums[8][32][17];
-    const int c = threadIdx.x & 31, q = threadIdx.x >> 5, k = ((int)blockIdx.x * 32 + c) * 8, left = width - k;
+    constexpr int R = 256 / C;
+    __shared__ float sums[R][C][17];
+    const int c = threadIdx.x % C, q = threadIdx.x / C, k = ((int)blockIdx.x * C + c) * 8, left = width - k, wp = (int)padded(width);
     const long long plane = rows * dp, r0 = (long long)blockIdx.y * rows_each;
     float total[2][8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) total[0][e] = total[1][e] = 0.f;
     if (k < width)
-        for (long long r = r0 + q; r < r0 + rows_each && r < rows; r += 8) {
+        for (long long r = r0 + q; r < r0 + rows_each && r < rows; r += R) {
             f32x4 d[2], z[2][2];
             load_eight(dy + r * width + k, left, whole, d);
-            load_eight(pre + r * 2 * width + k, left, whole, z[0]);
-            load_eight(pre + (r * 2 + 1) * width + k, left, whole, z[1]);
-            bf16x8 o[2][3];
+            Keep<T>::load(kept + r * 2 * wp + k, z[0]);
+            Keep<T>::load(kept + (r * 2 + 1) * wp + k, z[1]);
+            bf16x8 o[2][PLANES];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float v = d[e >> 2][e & 3], g = z[0][e >> 2][e & 3];
-                const float y[2] = {e < left ? v * z[1][e >> 2][e & 3] * activate_slope<ACT>(g) : 0.f, e < left ? v * activate<ACT>(g) : 0.f};
+            for (int e = 0; e < 8; ++e) {   // what is behind a row's end is zero in dy and kept
+                const float v = d[e >> 2][e & 3];
+                float a, slope;
+                gate_and_slope<T, ACT>(z[0][e >> 2][e & 3], a, slope);
+                const float y[2] = {v * z[1][e >> 2][e & 3] * slope, v * a};
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    __bf16 a, b, f;
                     total[h][e] += y[h];
-                    split_planes(y[h], a, b, f);
-                    o[h][0][e] = a;
-                    o[h][1][e] = b;
-                    o[h][2][e] = f;
+                    if constexpr (PLANES == 1) {
+                        o[h][0][e] = (__bf16)y[h];
+                    } else {
+                        __bf16 p[3];
+                        split_planes(y[h], p[0], p[1], p[2]);
+#pragma unroll
+                        for (int u = 0; u < PLANES; ++u) o[h][u][e] = p[u];
+                    }
                 }
             }
             if (dst) {
 #pragma unroll
-                for (int p = 0; p < 3; ++p) {
-                    if (p >= planes) break;
+                for (int p = 0; p < PLANES; ++p) {
                     __bf16 *first = dst + p * plane + r * dp + k;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
@@ -169,17 +349,13 @@ __global__ __launch_bounds__(256) void gated_slope_kernel(const T *__restrict__ 
         sums[q][c][8 + e] = total[1][e];
     }
     __syncthreads();
-    // thread: column threadIdx.x of the 256, in both halves
-    const int cc = threadIdx.x >> 3, e = threadIdx.x & 7, col = (int)blockIdx.x * 256 + threadIdx.x;
-    float v[2] = {0.f, 0.f};
+    // a thread adds up a column of either half
+    for (int i = threadIdx.x; i < C * 16; i += 256) {
+        const int h = i / (C * 8), cc = i % (C * 8) >> 3, e = i & 7, col = (int)blockIdx.x * C * 8 + i % (C * 8);
+        float v = 0.f;
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-        v[0] += sums[u][cc][e];
-        v[1] += sums[u][cc][8 + e];
-    }
-    if (col < width) {
-        part[(long long)blockIdx.y * 2 * width + col] = v[0];
-        part[((long long)blockIdx.y * 2 + 1) * width + col] = v[1];
+        for (int u = 0; u < R; ++u) v += sums[u][cc][h * 8 + e];
+        if (col < width) part[((long long)blockIdx.y * 2 + h) * width + col] = v;
     }
 }
 
@@ -191,28 +367,60 @@ static bool gated_args_fit(int64_t rows, int32_t d_in, int32_t d_out, int32_t dt
            sizes_fit(rows, d_in) && sizes_fit(rows, 2 * (int64_t)d_out) && (dtype == LCN_F32 || dtype == LCN_BF16);
 }
 
+// A product by large tiles and, where columns behind the last whole one get small tiles (plan_product), these as a product of their
+// own, whose k may be split: 7 columns behind 16384, k = 8192: 64 us in one piece of k, 16 in 16.
+struct Columns {
+    ProductPlan main, rest;
+    long long whole, n;
+    float *part, *part_rest;
+};
+static Columns plan_columns(Carver &c, long long m, long long n, long long k, int planes, bool may_320)
+{
+    Columns r{};
+    r.main = plan_product(m, n, k, planes, true, true, may_320);
+    r.n = r.whole = n;
+    if (r.main.tail) {
+        r.main.tail = false;
+        r.whole = n - n % tile_n(r.main.tile, planes);
+        r.rest = plan_product(m, n - r.whole, k, planes, true, false, may_320);
+    }
+    r.part = (float *)c.take(partial_bytes(r.main, m, r.whole));
+    r.part_rest = r.whole < n ? (float *)c.take(partial_bytes(r.rest, m, n - r.whole)) : nullptr;
+    return r;
+}
+// calls f(first column, columns, plan, partial sums) for both
+template <class F>
+static hipError_t by_columns(const Columns &c, F f)
+{
+    const hipError_t st = f((long long)0, (int)c.whole, c.main, c.part);
+    return st != hipSuccess || c.whole == c.n ? st : f(c.whole, (int)(c.n - c.whole), c.rest, c.part_rest);
+}
+static Operand from_column(Operand o, long long n)
+{
+    o.p = (const char *)o.p + n * o.ld * 2;
+    return o;
+}
+
 struct GatedForward {
     void *xp, *wp;
-    float *part;
-    ProductPlan plan;
+    Columns y;
     size_t bytes;
 };
 static GatedForward gated_forward_space(char *ws, int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype)
 {
     Carver c{ws};
     GatedForward f;
-    f.plan = plan_product(2 * d_out, rows, d_in, planes_of(dtype), true, true);
     f.xp = c.take(planes_bytes(rows, d_in, planes_of(dtype)));
     f.wp = c.take(planes_bytes(2 * d_out, d_in, planes_of(dtype)));
-    f.part = (float *)c.take((size_t)f.plan.splits * (size_t)rows * (size_t)padded(2 * d_out) * 4);
+    f.y = plan_columns(c, 2 * d_out, rows, d_in, planes_of(dtype), false);
     f.bytes = c.used;
     return f;
 }
 
 struct GatedBackward {
     void *xp, *wp, *dz;
-    float *part_dx, *part_dw, *sums;
-    ProductPlan dx, dw;
+    float *sums;
+    Columns dx, dw;
     int planes, groups, rows_each;   // planes of dz
     size_t bytes;
 };
@@ -222,16 +430,14 @@ static GatedBackward gated_backward_space(char *ws, int64_t rows, int32_t d_in, 
     GatedBackward b;
     const int32_t wide = 2 * d_out;
     b.planes = gradient_planes(rows, dtype);
-    b.dx = plan_product(d_in, rows, wide, b.planes, true, true);
-    b.dw = plan_product(d_in, wide, rows, b.planes, true, true);
     // enough workgroups to fill the chip, at most 256 partial sums per column
     b.rows_each = (int)((((rows + 255) / 256) + 31) & ~31LL);
     b.groups = (int)((rows + b.rows_each - 1) / b.rows_each);
     b.xp = c.take(planes_bytes(rows, d_in, planes_of(dtype)));
     b.wp = c.take(planes_bytes(wide, d_in, planes_of(dtype)));
     b.dz = c.take(planes_bytes(rows, wide, b.planes));
-    b.part_dx = (float *)c.take(partial_bytes(b.dx, d_in, rows));
-    b.part_dw = (float *)c.take(partial_bytes(b.dw, d_in, wide));
+    b.dx = plan_columns(c, d_in, rows, wide, b.planes, true);
+    b.dw = plan_columns(c, d_in, wide, rows, b.planes, true);
     b.sums = (float *)c.take((size_t)b.groups * wide * 4);
     b.bytes = c.used;
     return b;
@@ -239,9 +445,9 @@ static GatedBackward gated_backward_space(char *ws, int64_t rows, int32_t d_in, 
 
 template <class T>
 static lcn_status gated_as(const T *x, const T *w, const T *bias, int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype,
-                           int32_t act, T *y, float *pre, char *ws, size_t ws_bytes, hipStream_t s)
+                           int32_t act, T *y, typename Keep<T>::type *kept, char *ws, size_t ws_bytes, hipStream_t s)
 {
-    GatedArgs<T> e{bias, y, pre, act, 0};
+    GatedArgs<T> e{bias, y, kept, act, 0};
     if (rows <= FEW_ROWS) {
         const int r = (int)rows;
         OPCHK(r == 1   ? launch_few<T, 1>(e, x, w, r, d_in, d_out, s)
@@ -250,7 +456,7 @@ static lcn_status gated_as(const T *x, const T *w, const T *bias, int64_t rows, 
                        : launch_few<T, 8>(e, x, w, r, d_in, d_out, s));
         return LCN_OK;
     }
-    e.whole = whole_rows<T>((const void *)((uintptr_t)y | (uintptr_t)bias | (uintptr_t)pre), d_out);
+    e.whole = whole_rows<T>((const void *)((uintptr_t)y | (uintptr_t)bias), d_out);
     const GatedForward f = gated_forward_space(ws, rows, d_in, d_out, dtype);
     if (!ws || ((uintptr_t)ws & 255) || ws_bytes < f.bytes) return LCN_ERR_ALLOC;
     ProductArgs p{};
@@ -258,33 +464,59 @@ static lcn_status gated_as(const T *x, const T *w, const T *bias, int64_t rows, 
     p.a = add_operand(jobs, w, 2 * d_out, d_in, dtype, f.wp);
     p.b = add_operand(jobs, x, rows, d_in, dtype, f.xp);
     OPCHK(launch_planes(jobs, dtype, s));
-    p.m = 2 * d_out;
-    p.n = (int)rows;
     p.k = d_in;
     p.planes = planes_of(dtype);
-    const long long ldp = padded(2 * d_out), groups = (rows * ((d_out + 7) / 8) + 255) / 256;
-    OPCHK((launch_planned<sizeof(T) == 4 ? 3 : 1, false, false, PartialEpilogue>(f.plan, p, {f.part, ldp, rows * ldp, 0}, s)));
-    OPCHK(by_activation(act, [&](auto a) {
-        hipLaunchKernelGGL((gated_finish_kernel<T, decltype(a)::value>), dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(256), 0,
-                           s, e, f.part, f.plan.splits, rows * ldp, (long long)rows, d_out, ldp);
-        return hipGetLastError();
+    OPCHK(by_columns(f.y, [&](long long first, int n, const ProductPlan &plan, float *part) {
+        constexpr int NP = sizeof(T) == 4 ? 3 : 1;
+        ProductArgs q = p;
+        GatedArgs<T> to = e;
+        q.b = from_column(p.b, first);
+        q.n = n;
+        to.y += first * d_out;
+        if (to.kept) to.kept += first * 2 * padded(d_out);
+        if (plan.splits == 1) {
+            q.m = d_out;
+            return by_activation(act, [&](auto a) {
+                return launch_planned<NP, false, false, GatedEpilogue<T, decltype(a)::value>>(plan, q, to, s);
+            });
+        }
+        q.m = 2 * d_out;
+        const long long ldp = padded(2 * d_out), groups = ((long long)n * ((d_out + 7) / 8) + 255) / 256;
+        const hipError_t st = launch_planned<NP, false, false, PartialEpilogue>(plan, q, {part, ldp, n * ldp, 0}, s);
+        if (st != hipSuccess) return st;
+        return by_activation(act, [&](auto a) {
+            hipLaunchKernelGGL((gated_finish_kernel<T, decltype(a)::value>), dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(256),
+                               0, s, to, part, plan.splits, n * ldp, (long long)n, d_out, ldp);
+            return hipGetLastError();
+        });
     }));
     return LCN_OK;
 }
 
 template <class T>
-static lcn_status gated_backward_as(const T *x, const T *w, const float *pre, const T *dy, int64_t rows, int32_t d_in, int32_t d_out,
+static lcn_status gated_backward_as(const T *x, const T *w, const typename Keep<T>::type *kept, const T *dy, int64_t rows, int32_t d_in, int32_t d_out,
                                     int32_t dtype, int32_t act, T *dx, T *dw, T *dbias, char *ws, size_t ws_bytes, hipStream_t s)
 {
     const GatedBackward b = gated_backward_space(ws, rows, d_in, d_out, dtype);
     if (!ws || ((uintptr_t)ws & 255) || ws_bytes < b.bytes) return LCN_ERR_ALLOC;
     const int32_t wide = 2 * d_out;
-    const int dp = (int)padded(wide), whole = whole_rows<T>((const void *)((uintptr_t)dy | (uintptr_t)pre), d_out);
+    const int dp = (int)padded(wide), whole = whole_rows<T>(dy, d_out);
     OPCHK(by_activation(act, [&](auto a) {
-        hipLaunchKernelGGL((gated_slope_kernel<T, decltype(a)::value>), dim3((unsigned)((d_out + 255) / 256), (unsigned)b.groups),
-                           dim3(256), 0, s, dy, pre, (long long)rows, d_out, dp, b.rows_each, whole, b.planes,
-                           dx || dw ? (__bf16 *)b.dz : nullptr, dbias ? b.sums : nullptr);
-        return hipGetLastError();
+        constexpr int ACT = decltype(a)::value;
+        auto launch = [&](auto kernel, int pieces) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((d_out + pieces * 8 - 1) / (pieces * 8)), (unsigned)b.groups), dim3(256), 0, s, dy,
+                               kept, (long long)rows, d_out, dp, b.rows_each, whole,
+                               dx || dw ? (__bf16 *)b.dz : nullptr, dbias ? b.sums : nullptr);
+            return hipGetLastError();
+        };
+        constexpr int MOST = sizeof(T) == 4 ? 3 : 2;
+        if (b.planes == 1)
+            return d_out <= 64    ? launch(gated_slope_kernel<T, ACT, 8, 1>, 8)
+                   : d_out <= 128 ? launch(gated_slope_kernel<T, ACT, 16, 1>, 16)
+                                  : launch(gated_slope_kernel<T, ACT, 32, 1>, 32);
+        return d_out <= 64    ? launch(gated_slope_kernel<T, ACT, 8, MOST>, 8)
+               : d_out <= 128 ? launch(gated_slope_kernel<T, ACT, 16, MOST>, 16)
+                              : launch(gated_slope_kernel<T, ACT, 32, MOST>, 32);
     }));
     if (dbias) OPCHK(launch_column_sums(b.sums, b.groups, wide, dtype, dbias, s));
     ProductArgs p{};
@@ -295,18 +527,25 @@ static lcn_status gated_backward_as(const T *x, const T *w, const float *pre, co
     OPCHK(launch_planes(jobs, dtype, s));
     p.planes = b.planes;
     p.m = d_in;
-    p.b = plane_operand(b.dz, rows, wide);
+    const Operand dz = plane_operand(b.dz, rows, wide);
     if (dx) {
         p.a = wo;
-        p.n = (int)rows;
         p.k = wide;
-        OPCHK((launch_scaled<true, false>(b.dx, p, 1.f, dtype, dx, b.part_dx, s)));
+        OPCHK(by_columns(b.dx, [&](long long first, int n, const ProductPlan &plan, float *part) {
+            p.b = from_column(dz, first);
+            p.n = n;
+            return launch_scaled<true, false>(plan, p, 1.f, dtype, dx + first * d_in, part, s);
+        }));
     }
     if (dw) {
         p.a = xo;
-        p.n = wide;
         p.k = (int)rows;
-        OPCHK((launch_scaled<true, true>(b.dw, p, 1.f, dtype, dw, b.part_dw, s)));
+        OPCHK(by_columns(b.dw, [&](long long first, int n, const ProductPlan &plan, float *part) {
+            p.b = dz;   // its columns are the result's
+            p.b.p = (const char *)p.b.p + first * 2;
+            p.n = n;
+            return launch_scaled<true, true>(plan, p, 1.f, dtype, dw + first * d_in, part, s);
+        }));
     }
     return LCN_OK;
 }
@@ -316,6 +555,13 @@ static lcn_status gated_backward_as(const T *x, const T *w, const float *pre, co
 using namespace lcn;
 
 extern "C" {
+
+lcn_status lcn_gated_linear_kept_bytes(int64_t rows, int32_t d_out, int32_t dtype, size_t *bytes)
+{
+    if (!bytes || !gated_args_fit(rows, 1, d_out, dtype)) return LCN_ERR_INVALID_ARG;
+    *bytes = (size_t)rows * 2 * (size_t)padded(d_out) * (dtype == LCN_F32 ? 4 : 2);
+    return LCN_OK;
+}
 
 lcn_status lcn_gated_linear_workspace_bytes(int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype, int32_t backward,
                                             size_t *bytes)
@@ -329,20 +575,20 @@ lcn_status lcn_gated_linear_workspace_bytes(int64_t rows, int32_t d_in, int32_t 
 }
 
 lcn_status lcn_gated_linear(const void *x, const void *W, const void *bias, int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype,
-                            int32_t activation, void *y, float *pre, void *workspace, size_t workspace_bytes, void *hip_stream)
+                            int32_t activation, void *y, void *kept, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     if (!gated_args_fit(rows, d_in, d_out, dtype) || activation < LCN_ACT_NONE || activation > LCN_ACT_SILU)
         return LCN_ERR_INVALID_ARG;
     if (rows == 0) return LCN_OK;
-    if (!x || !W || !y) return LCN_ERR_INVALID_ARG;
+    if (!x || !W || !y || ((uintptr_t)kept & 15)) return LCN_ERR_INVALID_ARG;
     if (dtype == LCN_F32)
-        return gated_as((const float *)x, (const float *)W, (const float *)bias, rows, d_in, d_out, dtype, activation, (float *)y, pre,
-                        (char *)workspace, workspace_bytes, (hipStream_t)hip_stream);
-    return gated_as((const __bf16 *)x, (const __bf16 *)W, (const __bf16 *)bias, rows, d_in, d_out, dtype, activation, (__bf16 *)y, pre,
-                    (char *)workspace, workspace_bytes, (hipStream_t)hip_stream);
+        return gated_as((const float *)x, (const float *)W, (const float *)bias, rows, d_in, d_out, dtype, activation, (float *)y,
+                        (float *)kept, (char *)workspace, workspace_bytes, (hipStream_t)hip_stream);
+    return gated_as((const __bf16 *)x, (const __bf16 *)W, (const __bf16 *)bias, rows, d_in, d_out, dtype, activation, (__bf16 *)y,
+                    (unsigned short *)kept, (char *)workspace, workspace_bytes, (hipStream_t)hip_stream);
 }
 
-lcn_status lcn_gated_linear_backward(const void *x, const void *W, const float *pre, const void *dy, int64_t rows, int32_t d_in,
+lcn_status lcn_gated_linear_backward(const void *x, const void *W, const void *kept, const void *dy, int64_t rows, int32_t d_in,
                                      int32_t d_out, int32_t dtype, int32_t activation, void *dx, void *dW, void *dbias,
                                      void *workspace, size_t workspace_bytes, void *hip_stream)
 {
@@ -356,11 +602,11 @@ lcn_status lcn_gated_linear_backward(const void *x, const void *W, const float *
         if (dbias) OPCHK(launch_zero(dbias, (size_t)2 * d_out * e, s));
         return LCN_OK;
     }
-    if (!dy || !pre || (dx && !W) || (dW && !x)) return LCN_ERR_INVALID_ARG;
+    if (!dy || !kept || ((uintptr_t)kept & 15) || (dx && !W) || (dW && !x)) return LCN_ERR_INVALID_ARG;
     if (dtype == LCN_F32)
-        return gated_backward_as((const float *)x, (const float *)W, pre, (const float *)dy, rows, d_in, d_out, dtype, activation,
+        return gated_backward_as((const float *)x, (const float *)W, (const float *)kept, (const float *)dy, rows, d_in, d_out, dtype, activation,
                                  (float *)dx, (float *)dW, (float *)dbias, (char *)workspace, workspace_bytes, s);
-    return gated_backward_as((const __bf16 *)x, (const __bf16 *)W, pre, (const __bf16 *)dy, rows, d_in, d_out, dtype, activation,
+    return gated_backward_as((const __bf16 *)x, (const __bf16 *)W, (const unsigned short *)kept, (const __bf16 *)dy, rows, d_in, d_out, dtype, activation,
                              (__bf16 *)dx, (__bf16 *)dW, (__bf16 *)dbias, (char *)workspace, workspace_bytes, s);
 }
 

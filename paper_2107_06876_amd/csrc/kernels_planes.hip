@@ -84,6 +84,7 @@ __global__ __launch_bounds__(256) void add_partials_kernel(const float *__restri
         const long long r = t / per_row;
         const int c = (int)(t - r * per_row) * 4;
         f32x4 v = *(const f32x4 *)(part + r * ldp + c);
+#pragma unroll 8   // loads ahead of the sums
         for (int u = 1; u < splits; ++u) v += *(const f32x4 *)(part + u * stride + r * ldp + c);
         store_four(out + r * m + c, v * scale, m - c, whole);
     }
@@ -113,7 +114,7 @@ hipError_t launch_add_partials(const float *part, int splits, long long n, int m
 //
 // Columns behind the last whole tile cost a tile's time, and often a round of them: where that is estimated to be more than
 // 3 us and a launch of 64 x 64 tiles, they get that (a bf16 training step of 16391 rows, 1024 to 4096: 711 us, else 784).
-ProductPlan plan_product(long long m, long long n, long long k, int planes, bool may_split, bool may_tail)
+ProductPlan plan_product(long long m, long long n, long long k, int planes, bool may_split, bool may_tail, bool may_320)
 {
     struct Shape {
         int resident;
@@ -137,6 +138,7 @@ ProductPlan plan_product(long long m, long long n, long long k, int planes, bool
     ProductPlan best{TILE_256, 1, false};
     double least = 1e300;
     for (int t = 0; t < TILE_COUNT; ++t) {
+        if (t == TILE_320 && !may_320) continue;
         const long long rest = n % tile_n(t, planes);
         for (int splits = 1; splits <= 64; splits += splits < 16 ? 1 : 16) {
             if (splits > 1 && (!may_split || steps / splits < 4)) break;
@@ -189,6 +191,7 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const float *__restric
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), q = threadIdx.x >> 5;
     float v = 0.f;
     if (c < width)
+#pragma unroll 8
         for (int r = q; r < parts; r += 8) v += part[(long long)r * width + c];
     sums[q][threadIdx.x & 31] = v;
     __syncthreads();

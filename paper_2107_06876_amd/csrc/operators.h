@@ -228,7 +228,7 @@ struct ProductPlan {
     int splits;
     bool tail;     // columns behind the last whole tile: by small tiles, in a launch of their own
 };
-ProductPlan plan_product(long long m, long long n, long long k, int planes, bool may_split, bool may_tail);
+ProductPlan plan_product(long long m, long long n, long long k, int planes, bool may_split, bool may_tail, bool may_320 = true);
 
 // A float product's partial sums: [split][n][ldp]; `add` adds to what is there.
 struct PartialEpilogue {
@@ -312,14 +312,18 @@ hipError_t launch_tiles(int tile, const ProductArgs &p, const typename Epi::Args
     if constexpr (NP == 3) {
         switch (tile) {
         case TILE_256: return launch_product<256, 128, 32, 4, 2, 3, ACOL, BCOL, Epi>(p, e, s);
-        case TILE_320: return launch_product<320, 64, 32, 4, 2, 3, ACOL, BCOL, Epi>(p, e, s);
+        case TILE_320:   // 80 rows of a wavefront are no whole pairs
+            if constexpr (paired_rows<Epi>) return hipErrorInvalidValue;
+            else return launch_product<320, 64, 32, 4, 2, 3, ACOL, BCOL, Epi>(p, e, s);
         case TILE_128: return launch_product<128, 128, 32, 2, 2, 3, ACOL, BCOL, Epi>(p, e, s);
         default: return launch_product<64, 64, 32, 2, 2, 3, ACOL, BCOL, Epi>(p, e, s);
         }
     } else {
         switch (tile) {
         case TILE_256: return launch_product<256, 256, 64, 2, 4, 1, ACOL, BCOL, Epi>(p, e, s);
-        case TILE_320: return launch_product<320, 128, 64, 4, 2, 1, ACOL, BCOL, Epi>(p, e, s);
+        case TILE_320:
+            if constexpr (paired_rows<Epi>) return hipErrorInvalidValue;
+            else return launch_product<320, 128, 64, 4, 2, 1, ACOL, BCOL, Epi>(p, e, s);
         case TILE_128: return launch_product<128, 128, 64, 2, 2, 1, ACOL, BCOL, Epi>(p, e, s);
         default: return launch_product<64, 64, 64, 2, 2, 1, ACOL, BCOL, Epi>(p, e, s);
         }

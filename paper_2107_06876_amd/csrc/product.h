@@ -73,8 +73,13 @@ __device__ __forceinline__ int columns_swizzle(int k)
     return (((k >> 1) & 1) | ((k >> 2) & 2)) << 1;
 }
 
+// Whether an epilogue takes the rows of the first operand in pairs: the matrix has 2 m rows, row i and row m + i belong together, and
+// of every 32 rows of a tile 16 are rows i .. i + 15 and 16 are rows m + i .. m + i + 15, so that a lane gets both.
+template <class Epi>
+constexpr bool paired_rows = false;
+
 // One operand's part of the tiles of a workgroup: W indices from i0, BK values of k at a time, into LDS.
-template <int W, int BK, bool COLUMNS, int THREADS>
+template <int W, int BK, bool COLUMNS, int THREADS, bool PAIRED = false>
 struct TileLoader {
     static constexpr int PIECES = W * BK / 8, LOADS = (PIECES + THREADS - 1) / THREADS;   // 16 bytes each
     static_assert(PIECES % 64 == 0, "whole wavefronts of pieces");
@@ -83,6 +88,7 @@ struct TileLoader {
     // the permutation does not see.
     static constexpr bool EVEN = THREADS % ROW == 0 && THREADS / ROW % 16 == 0;
     static constexpr int KEPT = EVEN ? 1 : LOADS;
+    static_assert(!PAIRED || (!COLUMNS && (LOADS == 1 || THREADS / ROW % 32 == 0)), "a wavefront's loads are all of one half");
     const char *first;        // the workgroup's first index, k = 0, first plane
     long long k_bytes;        // from one tile's k to the next
     unsigned row_bytes, tail; // from a row to the next; bytes of the last row that are read
@@ -95,14 +101,15 @@ struct TileLoader {
         const int left = count - (int)i0;
         row_bytes = (unsigned)(o.ld * 2);
         first = (const char *)o.p + (COLUMNS ? i0 : i0 * o.ld) * 2;
+        if (PAIRED && (wave * (64 / ROW) >> 4) & 1) first += count * o.ld * 2;
         k_bytes = COLUMNS ? (long long)BK * o.ld * 2 : BK * 2;
-        rows = left < W ? left : W;
+        rows = left < W / (PAIRED ? 2 : 1) ? left : W / (PAIRED ? 2 : 1);
         tail = (unsigned)(((left + 7) & ~7) * 2);
 #pragma unroll
         for (int u = 0; u < KEPT; ++u) {
             const int c = (u * (THREADS / 64) + wave) * 64 + lane, row = c / ROW;
             const int piece = (c % ROW) ^ (COLUMNS ? columns_swizzle<W>(row) : rows_swizzle<BK>(row));
-            off[u] = (unsigned)row * row_bytes + (unsigned)piece * 16;
+            off[u] = (unsigned)(PAIRED ? (row >> 5) * 16 + (row & 15) : row) * row_bytes + (unsigned)piece * 16;
             need[u] = piece * 8;
             if (COLUMNS && piece * 8 >= left) off[u] = 0x80000000u;   // outside, also with rows added
         }
@@ -121,7 +128,7 @@ struct TileLoader {
             if (PIECES % THREADS && (u * (THREADS / 64) + wave) * 64 >= PIECES) break;
             unsigned o = off[EVEN ? 0 : u];
             if (!COLUMNS) o = need[EVEN ? 0 : u] < left ? o : 0x80000000u;
-            if (EVEN) o += u * (THREADS / ROW) * row_bytes;
+            if (EVEN) o += u * (THREADS / ROW) / (PAIRED ? 2 : 1) * row_bytes;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (lds_void *)(lds + (u * (THREADS / 64) + wave) * 1024), 16, (int)o,
                                                      0, 0, 0);
         }
@@ -238,7 +245,8 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs p, 
     if (id >= (unsigned)(p.tiles_m * p.tiles_n)) return;
     int tm, tn;
     tile_of(p, (int)id, tm, tn);
-    const long long m0 = (long long)tm * BM, n0 = p.n_first + (long long)tn * BN;
+    constexpr int PAIR = paired_rows<Epi> ? 2 : 1;   // rows of the tile that make an index m
+    const long long m0 = (long long)tm * (BM / PAIR), n0 = p.n_first + (long long)tn * BN;
     const int wm = (wave % WM) * (BM / WM), wn = (wave / WM) * (BN / WN);
 
     const int at_a = fragment_place<BM, BK, ACOL>(lane), at_b = fragment_place<BN, BK, BCOL>(lane);
@@ -252,7 +260,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs p, 
     const int all = ksteps * pairs, per = (all + p.splits - 1) / p.splits;
     const int first = (int)blockIdx.y * per, last = first + per < all ? first + per : all;
 
-    TileLoader<BM, BK, ACOL, THREADS> load_a;
+    TileLoader<BM, BK, ACOL, THREADS, paired_rows<Epi>> load_a;
     TileLoader<BN, BK, BCOL, THREADS> load_b;
     load_a.init(p.a, m0, p.m, wave, lane);
     load_b.init(p.b, n0, p.n, wave, lane);
@@ -360,13 +368,14 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs p, 
         }
     }
     __syncthreads();
-    Epi::template run<TM, TN, WM, WN>(e, p, acc, m0 + wm, n0 + wn, (int)blockIdx.y, lds0, tm, tn);
+    Epi::template run<TM, TN, WM, WN>(e, p, acc, m0 + wm / PAIR, n0 + wn, (int)blockIdx.y, lds0, tm, tn);
 }
 
 template <int BM, int BN, int BK, int WM, int WN, int NP, bool ACOL, bool BCOL, class Epi>
 hipError_t launch_product(ProductArgs p, const typename Epi::Args &e, hipStream_t s)
 {
-    p.tiles_m = (p.m + BM - 1) / BM;
+    constexpr int M = BM / (paired_rows<Epi> ? 2 : 1);
+    p.tiles_m = (p.m + M - 1) / M;
     p.tiles_n = (p.n_last - p.n_first + BN - 1) / BN;
     const dim3 tiles = grid_of((long long)p.tiles_m * p.tiles_n);
     hipLaunchKernelGGL((product_kernel<BM, BN, BK, WM, WN, NP, ACOL, BCOL, Epi>), dim3(tiles.x, p.splits, tiles.y), dim3(WM * WN * 64),

@@ -46,6 +46,7 @@ def _library():
         lib.lcn_attention.argtypes = [desc, vp, vp, vp, vp, vp, vp, sz, vp]
         lib.lcn_attention_backward.argtypes = [desc, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         lib.lcn_gated_linear_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, out]
+        lib.lcn_gated_linear_kept_bytes.argtypes = [i64, i32, i32, out]
         lib.lcn_gated_linear.argtypes = [vp, vp, vp, i64, i32, i32, i32, i32, vp, vp, vp, sz, vp]
         lib.lcn_gated_linear_backward.argtypes = [vp, vp, vp, vp, i64, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
         lib.lcn_orthogonalise_workspace_bytes.argtypes = [i64, i32, i32, i32, out]
@@ -56,7 +57,8 @@ def _library():
         for name in ("lcn_attention_workspace_bytes", "lcn_attention", "lcn_attention_backward", "lcn_linear_workspace_bytes",
                      "lcn_linear", "lcn_linear_backward", "lcn_cross_entropy_workspace_bytes", "lcn_cross_entropy",
                      "lcn_cross_entropy_backward", "lcn_layer_norm", "lcn_layer_norm_workspace_bytes", "lcn_layer_norm_backward",
-                     "lcn_gated_linear_workspace_bytes", "lcn_gated_linear", "lcn_gated_linear_backward",
+                     "lcn_gated_linear_workspace_bytes", "lcn_gated_linear_kept_bytes", "lcn_gated_linear",
+                     "lcn_gated_linear_backward",
                      "lcn_orthogonalise_workspace_bytes", "lcn_orthogonalise"):
             getattr(lib, name).restype = i32
         _lib = lib
@@ -76,8 +78,8 @@ def _tensor(t, name, shape, dtype, device):
 _sizes = {}   # bytes of workspace by call and sizes
 
 
-def _space(call, sizes, workspace, device):
-    """The address and size of a workspace, and the tensor that holds it."""
+def _bytes(call, sizes):
+    """What a call that says how many bytes are needed for these sizes says."""
     need = _sizes.get((call, sizes))
     if need is None:
         out = ctypes.c_size_t(0)
@@ -87,7 +89,12 @@ def _space(call, sizes, workspace, device):
         if len(_sizes) > 4096:
             _sizes.clear()
         need = _sizes[(call, sizes)] = out.value
-    return _workspace(need, workspace, device)
+    return need
+
+
+def _space(call, sizes, workspace, device):
+    """The address and size of a workspace, and the tensor that holds it."""
+    return _workspace(_bytes(call, sizes), workspace, device)
 
 
 def _workspace(need, workspace, device):
@@ -206,11 +213,11 @@ def _gates(x, w):
 
 def lcn_gated_linear(x, w, bias=None, activation=ACT_SILU, keep_pre=False, out=None, workspace=None):
     """act(x Wg^T + bg) (x Wu^T + bu) as a (rows, d_out) tensor; w: (2 d_out, d_in), Wg above Wu, bias: (2 d_out).  With
-    keep_pre also both factors' arguments in float32, (rows, 2 d_out), which lcn_gated_linear_backward takes."""
+    keep_pre also what lcn_gated_linear_backward takes of both sums, as bytes."""
     rows, d_out, d_in, dtype = _gates(x, w)
     dev = x.device
     y = torch.empty((rows, d_out), dtype=x.dtype, device=dev) if out is None else out
-    pre = torch.empty((rows, 2 * d_out), dtype=torch.float32, device=dev) if keep_pre else None
+    pre = torch.empty(_bytes("lcn_gated_linear_kept_bytes", (rows, d_out, dtype)), dtype=torch.uint8, device=dev) if keep_pre else None
     at, size, space = _space("lcn_gated_linear_workspace_bytes", (rows, d_in, d_out, dtype, 0), workspace, dev)
     _call("lcn_gated_linear", dev, x.data_ptr(), w.data_ptr(), _tensor(bias, "bias", (2 * d_out,), x.dtype, dev), rows, d_in, d_out,
           dtype, int(activation), _tensor(y, "out", (rows, d_out), x.dtype, dev), _address(pre), at, size)
@@ -225,9 +232,9 @@ def lcn_gated_linear_backward(x, w, pre, dy, activation=ACT_SILU, with_bias=True
     dw = torch.empty_like(w) if with_w else None
     db = torch.empty(2 * d_out, dtype=x.dtype, device=dev) if with_bias else None
     at, size, space = _space("lcn_gated_linear_workspace_bytes", (rows, d_in, d_out, dtype, 1), workspace, dev)
-    _call("lcn_gated_linear_backward", dev, x.data_ptr(), w.data_ptr(), _tensor(pre, "pre", (rows, 2 * d_out), torch.float32, dev),
-          _tensor(dy, "dy", (rows, d_out), x.dtype, dev), rows, d_in, d_out, dtype, int(activation), _address(dx), _address(dw),
-          _address(db), at, size)
+    kept = _tensor(pre, "pre", (_bytes("lcn_gated_linear_kept_bytes", (rows, d_out, dtype)),), torch.uint8, dev)
+    _call("lcn_gated_linear_backward", dev, x.data_ptr(), w.data_ptr(), kept, _tensor(dy, "dy", (rows, d_out), x.dtype, dev), rows, d_in,
+          d_out, dtype, int(activation), _address(dx), _address(dw), _address(db), at, size)
     return dx, dw, db
 
 
@@ -275,7 +282,8 @@ def lcn_layer_norm(x, weight=None, bias=None, eps=1e-5, keep_stats=False, out=No
     rows, dim, dtype = _rows(x)
     dev = x.device
     y = torch.empty_like(x) if out is None else out
-    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=dev) if keep_stats else (None, None)
+    mean = torch.empty(rows, dtype=torch.float32, device=dev) if keep_stats else None
+    rstd = torch.empty(rows, dtype=torch.float32, device=dev) if keep_stats else None
     _call("lcn_layer_norm", dev, x.data_ptr(), _tensor(weight, "weight", (dim,), x.dtype, dev),
           _tensor(bias, "bias", (dim,), x.dtype, dev), rows, dim, dtype, float(eps), _tensor(y, "out", (rows, dim), x.dtype, dev),
           _address(mean), _address(rstd))

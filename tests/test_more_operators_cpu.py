@@ -98,6 +98,19 @@ def test_gated_arguments(lib):
     assert lib.lcn_gated_linear_backward(None, None, None, None, 20, 60, 60, F32, 4, None, None, None, None, 0, None) == OK
 
 
+def test_gated_kept(lib):
+    """Rows of both sums in whole pieces of eight: floats, or 16 bits a value; aligned."""
+    f = lib.lcn_gated_linear_kept_bytes
+    assert _bytes(f, 10, 24, F32) == (OK, 10 * 2 * 24 * 4) and _bytes(f, 10, 20, BF16) == (OK, 10 * 2 * 24 * 2)
+    assert _bytes(f, 0, 20, BF16) == (OK, 0)
+    for rows, d_out, dtype in ((-1, 4, F32), (4, 0, F32), (4, 4, 3), (4, (1 << 19) + 1, F32), (1 << 30, (1 << 11) + 1, BF16)):
+        assert _bytes(f, rows, d_out, dtype)[0] == ERR_INVALID_ARG
+    args = [FAKE, FAKE, None, 20, 600, 600, F32, 4, FAKE, FAKE + 8, FAKE, 1 << 40, None]
+    assert lib.lcn_gated_linear(*args) == ERR_INVALID_ARG
+    args = [FAKE, FAKE, FAKE + 8, FAKE, 20, 60, 60, F32, 4, FAKE, FAKE, None, FAKE, 1 << 40, None]
+    assert lib.lcn_gated_linear_backward(*args) == ERR_INVALID_ARG
+
+
 def test_gated_workspaces(lib):
     for dtype in (F32, BF16):
         for rows, a, b in ((1, 16, 16), (20, 300, 600), (5000, 300, 20000), (70000, 1024, 4096)):
