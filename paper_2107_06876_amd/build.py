@@ -29,6 +29,7 @@ SOURCES = {
     "kernels_gated.hip": [],
     "kernels_norm.hip": [],
     "kernels_orthogonal.hip": [],
+    "kernels_pair.hip": [],
     "kernels_entropy.hip": [],
     "kernels_attention_f32.hip": [],
     "kernels_attention_bf16.hip": [],

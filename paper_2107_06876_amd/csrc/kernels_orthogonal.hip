@@ -5,140 +5,63 @@
 //
 // Every product is one of two planes of fp16 (product.h): the singular values are bounded by the polynomials, and with them every
 // value of X, A and B, so that powers of two in front keep them in fp16's range.  Planes and sums are as exact as single precision,
-// which is needed: what rounding adds in the first steps grows as the smallest singular values do, up to a per step.
-#include "operators.h"
+// which is needed: what rounding adds in the first steps grows as the smallest singular values do, up to a per step.  bf16 matrices
+// are one plane in the first step, exactly.
+//
+// Long bf16 matrices take several steps on A alone, which is small: with B_1, B_2, ... as they come, A <- A B^2 and X <- B_r .. B_1 X
+// at the end of such a stage.  A then has to tell sigma^2 from the largest one's rounding, 2^-24, where X tells sigma: a stage's
+// polynomials grow by 64 at most, so that a singular value whose result they decide is 1/64 of the largest at least, its square
+// off by 64^2 2^-24 = 2^-12 of itself in the worst case, which a bf16 result has room for.  4 matrices of 8192 x 1024, 5 steps: 14
+// products of 1024^3 at 33 us in place of three of A and of X, at 130 and 170.
+//
+// A and B are symmetric, and so are the products of two polynomials of one A: tiles on and below the diagonal are computed, and
+// written twice.  A is a product with a long k and few tiles: k is split over workgroups, whose sums a second launch adds.
+#include "orthogonal.h"
 
 namespace lcn {
 
-// The largest singular value of X that a step may leave, the largest of a + b t + c t^2 in its way, and what X, A and B are
-// multiplied with: values up to 32 768 of fp16's 65 504.
-constexpr double MOST_X = 4.0, MOST_POLY = 64.0;
-constexpr float SCALE_X = 8192.f, SCALE_A = 2048.f, SCALE_B = 512.f;
-
-typedef _Float16 f16;
-
-// A matrix in two planes: rows of `ld` values, ld a multiple of 8, zeros behind a row's values
-struct Planes {
-    f16 *p;
-    long long plane, ld;   // values from a plane to the next, from a row to the next
-};
-
-__device__ __forceinline__ void store_planes(const Planes &o, long long at, const f32x4 (&v)[2])
-{
-    f16x8 hi, lo;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float x = v[e >> 2][e & 3];
-        hi[e] = (f16)x;
-        lo[e] = (f16)(x - (float)hi[e]);
-    }
-    *(f16x8 *)(o.p + at) = hi;
-    *(f16x8 *)(o.p + o.plane + at) = lo;
-}
-
-// planes of factor * the product (A, and X in between)
-struct PlanesEpilogue {
-    struct Args {
-        Planes out;
-        float factor;
-    };
-    template <int TM, int TN, int WM, int WN>
-    static __device__ void run(const Args &e, const ProductArgs &p, f32x4 (&acc)[TM][TN], long long m0, long long n0, int, char *lds,
-                               int, int)
-    {
-        const int lane = threadIdx.x & 63;
-        char *region = lds + (threadIdx.x >> 6) * RowRegion<TM>::BYTES;
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            f32x4 col[TM];
-#pragma unroll
-            for (int i = 0; i < TM; ++i) col[i] = acc[i][j] * e.factor;
-            by_rows<TM>(
-                region, col, lane, [](int, int) { return Nothing{}; },
-                [&](int r, int c, f32x4 (&v)[2], Nothing) {
-                    const long long n = n0 + j * 16 + r, m = m0 + c;
-                    if (n < p.n && m < p.m) store_planes(e.out, n * e.out.ld + m, v);
-                });
-        }
-    }
-};
-
-// planes of factor * the product + linear * A + constant on the diagonal (B)
-struct PolynomialEpilogue {
-    struct Args {
-        Planes out, gram;
-        float factor, linear, constant;
-    };
-    template <int TM, int TN, int WM, int WN>
-    static __device__ void run(const Args &e, const ProductArgs &p, f32x4 (&acc)[TM][TN], long long m0, long long n0, int, char *lds,
-                               int, int)
-    {
-        const int lane = threadIdx.x & 63;
-        char *region = lds + (threadIdx.x >> 6) * RowRegion<TM>::BYTES;
-        struct Two {
-            f16x8 hi, lo;
-        };
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            f32x4 col[TM];
-#pragma unroll
-            for (int i = 0; i < TM; ++i) col[i] = acc[i][j] * e.factor;
-            by_rows<TM>(
-                region, col, lane,
-                [&](int r, int c) {
-                    const long long n = n0 + j * 16 + r, m = m0 + c;
-                    Two t{};
-                    if (n < p.n && m < p.m) {
-                        t.hi = *(const f16x8 *)(e.gram.p + n * e.gram.ld + m);
-                        t.lo = *(const f16x8 *)(e.gram.p + e.gram.plane + n * e.gram.ld + m);
-                    }
-                    return t;
-                },
-                [&](int r, int c, f32x4 (&v)[2], const Two &t) {
-                    const long long n = n0 + j * 16 + r, m = m0 + c;
-                    if (n >= p.n || m >= p.m) return;
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        float x = v[u >> 2][u & 3] + e.linear * ((float)t.hi[u] + (float)t.lo[u]);
-                        if (m + u == n) x += e.constant;
-                        v[u >> 2][u & 3] = x;
-                    }
-                    store_planes(e.out, n * e.out.ld + m, v);
-                });
-        }
-    }
-};
-
 // Partial sums of squares of a matrix (blockIdx.y), in 64 bits: squares of floats leave their own range.
-constexpr int NORM_GROUPS = 64;
-template <class T>
+template <class T, bool VEC>
 __global__ __launch_bounds__(256) void squares_kernel(const T *__restrict__ g, long long size, double *__restrict__ part)
 {
+    constexpr int V = VEC ? 16 / (int)sizeof(T) : 1;
+    typedef T piece __attribute__((ext_vector_type(V)));
     __shared__ double sums[4];
-    const T *p = g + blockIdx.y * size;
+    const piece *p = (const piece *)(g + blockIdx.y * size);
+    const long long pieces = size / V;
     double v = 0.0;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < size; i += (long long)NORM_GROUPS * 256) {
-        const double x = (double)(float)p[i];
-        v += x * x;
+#pragma unroll 4
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (long long)NORM_GROUPS * 256) {
+        const piece x = p[i];
+#pragma unroll
+        for (int e = 0; e < V; ++e) v = __builtin_fma((double)(float)x[e], (double)(float)x[e], v);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
     if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = v;
     __syncthreads();
-    if (threadIdx.x == 0) part[blockIdx.y * NORM_GROUPS + blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
+    if (threadIdx.x == 0) part[blockIdx.y * NORM_GROUPS + blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
 }
 
-// X = SCALE_X G / (|G| + eps) in planes; matrix blockIdx.y
+// Matrix blockIdx.y.  float: SCALE_X G / (|G| + eps) in two planes.  bf16: G times the power of two that brings |G| to between
+// SCALE_X / 2 and SCALE_X, in one plane, which holds it exactly, and what is left of the factor in `ratio`.
 template <class T>
 __global__ __launch_bounds__(256) void normalise_kernel(const T *__restrict__ g, const double *__restrict__ part, int rows, int cols,
-                                                        float eps, int whole, Planes out)
+                                                        float eps, int whole, Planes out, float *__restrict__ ratio)
 {
     double sum = 0.0;
     for (int i = 0; i < NORM_GROUPS; ++i) sum += part[blockIdx.y * NORM_GROUPS + i];
-    const double inv = (double)SCALE_X / (sqrt(sum) + (double)eps);
+    const double norm = sqrt(sum), inv = (double)SCALE_X / (norm + (double)eps);
+    int shift = 0;
+    if (sizeof(T) == 2 && norm > 0.0 && norm < __builtin_huge_val()) {
+        int e;
+        (void)frexp(norm, &e);   // norm = 0.5 .. 1 times 2^e
+        shift = 13 - e;
+    }
+    if (sizeof(T) == 2 && blockIdx.x == 0 && threadIdx.x == 0) ratio[blockIdx.y] = (float)ldexp(inv, -shift);
     const int per_row = (int)(out.ld / 8);
     const T *src = g + (long long)blockIdx.y * rows * cols;
-    out.p += (long long)blockIdx.y * rows * out.ld;
+    f16 *dst = out.p + (long long)blockIdx.y * rows * out.ld;
     const long long pieces = (long long)rows * per_row;
     for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < pieces; t += (long long)gridDim.x * 256) {
         const long long r = t / per_row;
@@ -146,8 +69,102 @@ __global__ __launch_bounds__(256) void normalise_kernel(const T *__restrict__ g,
         f32x4 v[2];
         load_eight(src + r * cols + k, cols - k, whole, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e >> 2][e & 3] = k + e < cols ? (float)((double)v[e >> 2][e & 3] * inv) : 0.f;
-        store_planes(out, t * 8, v);
+        for (int e = 0; e < 8; ++e) {
+            const float x = v[e >> 2][e & 3];
+            v[e >> 2][e & 3] = k + e >= cols ? 0.f : sizeof(T) == 2 ? __builtin_ldexpf(x, shift) : (float)((double)x * inv);
+        }
+        if (sizeof(T) == 2) {
+            f16x8 o;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = (f16)v[e >> 2][e & 3];
+            *(f16x8 *)(dst + t * 8) = o;
+        } else {
+            store_planes(Planes{dst, out.plane, out.ld}, t * 8, v);
+        }
+    }
+}
+
+// ---- small matrices --------------------------------------------------------------
+// All steps of a matrix in one workgroup, X, A and B as floats in LDS, on the float matrix instruction (its operands and sums are
+// single precision as they are).  X lies with its longer side as rows.  Bound by the chain of its products: 8 matrices of 96 x 32,
+// 5 steps: see below.
+template <class T, int D, int ROWS>
+__global__ __launch_bounds__(512) void orthogonal_small_kernel(const T *__restrict__ g, int rows, int cols, int steps, SmallSteps c,
+                                                               float eps, float scale, T *out)   // out may be g
+{
+    typedef Tile<float, D> L;
+    constexpr int N = D / 16;
+    __shared__ __align__(1024) char xs[ROWS * D * 4];
+    __shared__ __align__(1024) char as[D * D * 4];
+    __shared__ __align__(1024) char bs[D * D * 4];
+    __shared__ double sums[8];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = lane >> 4;
+    const bool wide = rows < cols;
+    const int hi = wide ? cols : rows, lo = wide ? rows : cols, blocks = (hi + 31) / 32 * 2;   // of 16 rows, whole chunks of 32 for A
+    const T *src = g + (long long)blockIdx.x * rows * cols;
+    auto at = [](char *lds, int r, int k) -> float & { return *(float *)(lds + L::place(r, k >> 2) + (k & 3) * 4); };
+    double sum = 0.0;
+    for (int i = tid; i < blocks * 16 * D; i += 512) at(xs, i / D, i % D) = 0.f;
+    __syncthreads();
+    for (int i = tid; i < rows * cols; i += 512) {
+        const float v = (float)src[i];
+        const int r = i / cols, k = i - r * cols;
+        at(xs, wide ? k : r, wide ? r : k) = v;
+        sum += (double)v * v;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    sum = ((sums[0] + sums[1]) + (sums[2] + sums[3])) + ((sums[4] + sums[5]) + (sums[6] + sums[7]));
+    const double inv = 1.0 / (sqrt(sum) + (double)eps);
+    for (int i = tid; i < rows * cols; i += 512) {
+        const int r = i / lo, k = i - r * lo;
+        at(xs, r, k) = (float)((double)at(xs, r, k) * inv);
+    }
+    for (int s = 0; s < steps; ++s) {
+        __syncthreads();
+        for (int b = wave; b < N * N; b += 8) {   // A[i][j]: sum over the rows of X
+            const int i = b / N * 16, j = b % N * 16;
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+            for (int r = 0; r < blocks * 16; r += 32) mma(acc, L::columns(xs, r, i, lane), L::columns(xs, r, j, lane));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) at(as, i + 4 * grp + e, j + (lane & 15)) = acc[e];
+        }
+        __syncthreads();
+        for (int b = wave; b < N * N; b += 8) {   // B = a + b A + c A A
+            const int i = b / N * 16, j = b % N * 16;
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) mma(acc, L::rows(as, i, k, lane), L::rows(as, j, k, lane));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int m = i + 4 * grp + e, n = j + (lane & 15);
+                at(bs, m, n) = c.c[s][2] * acc[e] + c.c[s][1] * at(as, m, n) + (m == n ? c.c[s][0] : 0.f);
+            }
+        }
+        __syncthreads();
+        for (int b = wave; b < blocks; b += 8) {   // X <- X B, 16 rows of a wavefront's own
+            f32x4 acc[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) {
+                const Frag<float>::type x = L::rows(xs, b * 16, k, lane);
+#pragma unroll
+                for (int j = 0; j < N; ++j) mma(acc[j], x, L::rows(bs, j * 16, k, lane));
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) at(xs, b * 16 + 4 * grp + e, j * 16 + (lane & 15)) = acc[j][e];
+        }
+    }
+    __syncthreads();
+    T *dst = out + (long long)blockIdx.x * rows * cols;
+    for (int i = tid; i < rows * cols; i += 512) {
+        const int r = i / cols, k = i - r * cols;
+        dst[i] = (T)(at(xs, wide ? k : r, wide ? r : k) * scale);
     }
 }
 
@@ -160,17 +177,19 @@ static bool orthogonal_args_fit(int64_t count, int32_t rows, int32_t cols, int32
            (double)count * rows * cols <= (double)((int64_t)1 << 40) && (dtype == LCN_F32 || dtype == LCN_BF16);
 }
 
-// Whether every step keeps the singular values, which start at 1 or less, within the bounds above.
-static bool coefficients_fit(int32_t steps, const float *c)
+// Whether every step keeps the singular values, which start at 1 or less, within the bounds of orthogonal.h; poly: the largest
+// value of every step's polynomial on the way.
+static bool coefficients_fit(int32_t steps, const float *c, double *poly)
 {
     double s = 1.0;
     for (int i = 0; i < steps; ++i) {
         const double k[3] = {c[3 * i], c[3 * i + 1], c[3 * i + 2]}, top = s * s;
-        double most = 0.0, poly = 0.0;
+        double most = 0.0;
+        poly[i] = 0.0;
         auto at = [&](double t) {   // a singular value sqrt(t), if it can occur
             if (!(t >= 0.0) || t > top) return;
             const double q = __builtin_fabs(k[0] + t * (k[1] + t * k[2]));
-            if (!(q <= poly)) poly = q;
+            if (!(q <= poly[i])) poly[i] = q;
             if (!(q * __builtin_sqrt(t) <= most)) most = q * __builtin_sqrt(t);
         };
         at(0.0);
@@ -183,101 +202,168 @@ static bool coefficients_fit(int32_t steps, const float *c)
             at((-3.0 * k[1] - __builtin_sqrt(d)) / (10.0 * k[2]));
         }
         at(-k[0] / (3.0 * k[1]));   // the same without c
-        if (!(most <= MOST_X) || !(poly <= MOST_POLY)) return false;
+        if (!(most <= MOST_X) || !(poly[i] <= MOST_POLY)) return false;
         s = most;
     }
     return true;
 }
 
+static bool small(int32_t rows, int32_t cols)
+{
+    const int32_t lo = rows < cols ? rows : cols, hi = rows < cols ? cols : rows;
+    return (lo <= 32 && hi <= 512) || (lo <= 64 && hi <= 256);
+}
+
+template <class T>
+static lcn_status small_as(const T *g, int64_t count, int32_t rows, int32_t cols, int32_t steps, const float *c, float eps, float scale,
+                           T *out, hipStream_t s)
+{
+    SmallSteps k{};
+    for (int i = 0; i < steps; ++i)
+        for (int e = 0; e < 3; ++e) k.c[i][e] = c[3 * i + e];
+    const int32_t lo = rows < cols ? rows : cols;
+    if (lo <= 32)
+        hipLaunchKernelGGL((orthogonal_small_kernel<T, 32, 512>), dim3((unsigned)count), dim3(512), 0, s, g, rows, cols, steps, k, eps,
+                           scale, out);
+    else
+        hipLaunchKernelGGL((orthogonal_small_kernel<T, 64, 256>), dim3((unsigned)count), dim3(512), 0, s, g, rows, cols, steps, k, eps,
+                           scale, out);
+    OPCHK(hipGetLastError());
+    return LCN_OK;
+}
+
+// Whether steps are taken on A alone.
+static bool by_stages(int32_t rows, int32_t cols, int32_t dtype)
+{
+    const int64_t lo = rows < cols ? rows : cols, hi = rows < cols ? cols : rows;
+    return dtype == LCN_BF16 && hi >= 4 * lo;
+}
+
 struct OrthogonalSpace {
-    f16 *x[2], *gram, *poly;
+    f16 *x[2], *gram, *next, *poly[3];   // next, poly[1 ..]: by stages
     double *part;
+    float *ratio, *sums;
     long long size, ld, lo, ldg;   // values of a plane of X and its row; of A and its row
+    PairPlan plan_gram, plan_poly, plan_apply;
     size_t bytes;
 };
-static OrthogonalSpace orthogonal_space(char *ws, int64_t count, int32_t rows, int32_t cols)
+static OrthogonalSpace orthogonal_space(char *ws, int64_t count, int32_t rows, int32_t cols, int32_t dtype)
 {
     Carver c{ws};
     OrthogonalSpace o;
+    const bool bf16 = dtype == LCN_BF16;
+    const int32_t hi = rows < cols ? cols : rows;
     o.ld = padded(cols);
     o.size = count * rows * o.ld;
     o.lo = rows < cols ? rows : cols;
     o.ldg = padded(o.lo);
+    o.plan_gram = plan_pair(o.lo, o.lo, hi, count, true, bf16);
+    o.plan_poly = plan_pair(o.lo, o.lo, o.lo, count, true, bf16);
+    o.plan_apply = plan_pair(cols, rows, o.lo, count, false, bf16);
     for (int i = 0; i < 2; ++i) o.x[i] = (f16 *)c.take((size_t)o.size * 4);
-    o.gram = (f16 *)c.take((size_t)(count * o.lo * o.ldg) * 4);
-    o.poly = (f16 *)c.take((size_t)(count * o.lo * o.ldg) * 4);
+    const size_t square = (size_t)(count * o.lo * o.ldg) * 4;
+    const bool more = by_stages(rows, cols, dtype);
+    o.gram = (f16 *)c.take(square);
+    for (int i = 0; i < 3; ++i) o.poly[i] = i == 0 || more ? (f16 *)c.take(square) : nullptr;
+    o.next = more ? (f16 *)c.take(square) : nullptr;
     o.part = (double *)c.take((size_t)count * NORM_GROUPS * 8);
+    o.ratio = (float *)c.take((size_t)count * 4);
+    const size_t one = pair_part_bytes(o.plan_gram, o.lo, count), two = pair_part_bytes(o.plan_poly, o.lo, count);
+    o.sums = (float *)c.take(one > two ? one : two);
     o.bytes = c.used;
     return o;
 }
 
-template <bool ACOL, bool BCOL, class Epi>
-static hipError_t launch_pair(ProductArgs p, const typename Epi::Args &e, hipStream_t s)
-{
-    p.planes = 2;
-    p.splits = 1;
-    p.n_first = 0;
-    p.n_last = p.n;
-    const long long large = ((p.m + 255LL) / 256) * ((p.n + 255) / 256), mid = ((p.m + 127LL) / 128) * ((p.n + 127) / 128);
-    if (large >= 256) return launch_product<256, 256, 32, 2, 4, 2, ACOL, BCOL, Epi>(p, e, s);
-    if (mid >= 256) return launch_product<128, 128, 32, 2, 2, 2, ACOL, BCOL, Epi>(p, e, s);
-    return launch_product<64, 64, 32, 2, 2, 2, ACOL, BCOL, Epi>(p, e, s);
-}
-
 template <class T>
-static lcn_status orthogonal_as(const T *g, int64_t count, int32_t rows, int32_t cols, int32_t steps, const float *c, float eps,
-                                float scale, T *out, char *ws, size_t ws_bytes, hipStream_t s)
+static lcn_status orthogonal_as(const T *g, int64_t count, int32_t rows, int32_t cols, int32_t dtype, int32_t steps, const float *c,
+                                const double *most, float eps, float scale, T *out, char *ws, size_t ws_bytes, hipStream_t s)
 {
-    OrthogonalSpace o = orthogonal_space(ws, count, rows, cols);
+    const OrthogonalSpace o = orthogonal_space(ws, count, rows, cols, dtype);
     if (!ws || ((uintptr_t)ws & 255) || ws_bytes < o.bytes) return LCN_ERR_ALLOC;
-    const bool wide = rows <= cols;
     const int n = (int)o.lo;
     Planes x[2] = {{o.x[0], o.size, o.ld}, {o.x[1], o.size, o.ld}};
-    const Planes gram{o.gram, count * n * o.ldg, o.ldg}, poly{o.poly, count * n * o.ldg, o.ldg};
-    const long long groups = ((long long)rows * (o.ld / 8) + 255) / 256;
+    auto square = [&](f16 *p) { return Planes{p, count * n * o.ldg, o.ldg}; };
+    const long long groups = ((long long)rows * (o.ld / 8) + 255) / 256, size = (long long)rows * cols;
+    const bool vec = ((uintptr_t)g & 15) == 0 && size % (16 / (int)sizeof(T)) == 0;
     for (int64_t first = 0; first < count; first += 32768) {   // a grid's second dimension
         const unsigned some = (unsigned)(count - first < 32768 ? count - first : 32768);
-        hipLaunchKernelGGL(squares_kernel<T>, dim3(NORM_GROUPS, some), dim3(256), 0, s, g + first * rows * cols, (long long)rows * cols,
-                           o.part + first * NORM_GROUPS);
+        if (vec)
+            hipLaunchKernelGGL((squares_kernel<T, true>), dim3(NORM_GROUPS, some), dim3(256), 0, s, g + first * size, size,
+                               o.part + first * NORM_GROUPS);
+        else
+            hipLaunchKernelGGL((squares_kernel<T, false>), dim3(NORM_GROUPS, some), dim3(256), 0, s, g + first * size, size,
+                               o.part + first * NORM_GROUPS);
         OPCHK(hipGetLastError());
         Planes to = x[0];
         to.p += first * rows * o.ld;
-        hipLaunchKernelGGL(normalise_kernel<T>, dim3((unsigned)(groups < 1024 ? groups : 1024), some), dim3(256), 0, s,
-                           g + first * rows * cols, o.part + first * NORM_GROUPS, rows, cols, eps, whole_rows<T>(g, cols), to);
+        hipLaunchKernelGGL(normalise_kernel<T>, dim3((unsigned)(groups < 1024 ? groups : 1024), some), dim3(256), 0, s, g + first * size,
+                           o.part + first * NORM_GROUPS, rows, cols, eps, whole_rows<T>(g, cols), to, o.ratio + first);
         OPCHK(hipGetLastError());
     }
-    auto operand = [](const Planes &m, long long at) { return Operand{m.p + at, m.plane * 2, m.ld}; };
-    auto from = [](Planes m, long long at) {
-        m.p += at;
-        return m;
+    auto operand = [](const Planes &m) { return Operand{m.p, m.plane * 2, m.ld}; };
+    const long long x_batch = rows * o.ld, g_batch = n * o.ldg;
+    const bool wide = rows <= cols;
+    constexpr int FULL = sizeof(T) == 2 ? PAIR_TWO : PAIR_FLOAT;
+    // out = factor * product (+ linear * gram + constant), of symmetric matrices
+    auto multiply = [&](f16 *left, f16 *right, f16 *out, float factor, f16 *gram, float linear, float constant) {
+        PairArgs p{};
+        p.batches = (int)count;
+        p.part = o.sums;
+        p.a = operand(square(left));
+        p.b = operand(square(right));
+        p.a_batch = p.b_batch = g_batch * 2;
+        p.m = p.n = p.k = n;
+        return launch_gram(o.plan_poly, p, {square(out), g_batch, square(gram), factor, linear, constant, nullptr}, true, FULL, s);
     };
-    for (int i = 0; i < steps; ++i) {
-        const float a = c[3 * i], b = c[3 * i + 1], k = c[3 * i + 2];
-        for (int64_t u = 0; u < count; ++u) {
-            const long long ax = u * rows * o.ld, ag = u * n * o.ldg;
-            ProductArgs p{};
-            p.a = p.b = operand(x[0], ax);
-            p.m = p.n = n;
-            p.k = wide ? cols : rows;
-            const PlanesEpilogue::Args ga{from(gram, ag), SCALE_A / (SCALE_X * SCALE_X)};
-            OPCHK(wide ? launch_pair<false, false, PlanesEpilogue>(p, ga, s) : launch_pair<true, true, PlanesEpilogue>(p, ga, s));
-            p.a = p.b = operand(gram, ag);
-            p.k = n;
-            OPCHK(launch_pair<false, false, PolynomialEpilogue>(
-                p, {from(poly, ag), from(gram, ag), SCALE_B * k / (SCALE_A * SCALE_A), SCALE_B * b / SCALE_A, SCALE_B * a}, s));
-            // wide: out[r][c] = sum over k of X[k][c] B[r][k];  tall: sum over k of B[c][k] X[r][k]
-            p.m = cols;
-            p.n = rows;
-            p.a = wide ? operand(x[0], ax) : operand(poly, ag);
-            p.b = wide ? operand(poly, ag) : operand(x[0], ax);
-            if (i + 1 < steps) {
-                const PlanesEpilogue::Args xa{from(x[1], ax), 1.f / SCALE_B};
-                OPCHK(wide ? launch_pair<true, false, PlanesEpilogue>(p, xa, s) : launch_pair<false, false, PlanesEpilogue>(p, xa, s));
-            } else {
-                const typename ScaledEpilogue<T>::Args xa{out + u * rows * cols, cols, scale / (SCALE_B * SCALE_X), whole_rows<T>(out, cols)};
-                OPCHK(wide ? launch_pair<true, false, ScaledEpilogue<T>>(p, xa, s) : launch_pair<false, false, ScaledEpilogue<T>>(p, xa, s));
+    for (int i = 0; i < steps;) {
+        // the steps of this stage: as many as the polynomials' growth allows
+        int stage = 1;
+        if (by_stages(rows, cols, dtype))
+            for (double growth = most[i]; i + stage < steps && growth * most[i + stage] <= MOST_POLY; ++stage) growth *= most[i + stage];
+        const bool first = sizeof(T) == 2 && i == 0;   // X is one plane, and lacks its ratio
+        const float *ratio = first ? o.ratio : nullptr;
+        PairArgs p{};
+        p.batches = (int)count;
+        p.part = o.sums;
+        p.a = p.b = operand(x[0]);
+        p.a_batch = p.b_batch = x_batch * 2;
+        p.m = p.n = n;
+        p.k = wide ? cols : rows;
+        OPCHK(launch_gram(o.plan_gram, p, {square(o.gram), g_batch, Planes{}, SCALE_A / (SCALE_X * SCALE_X), 0.f, 0.f, ratio}, wide,
+                          first ? PAIR_ONE : FULL, s));
+        int now = 0, all = 0;   // of o.poly: this step's B, and the product of the stage's
+        for (int r = 0; r < stage; ++r) {
+            const float *k = c + 3 * (i + r);
+            if (r) {   // A <- A B B
+                OPCHK(multiply(o.gram, o.poly[now], o.next, 1.f / SCALE_B, nullptr, 0.f, 0.f));
+                OPCHK(multiply(o.next, o.poly[now], o.gram, 1.f / SCALE_B, nullptr, 0.f, 0.f));
             }
+            int to = 0;
+            while (r && (to == now || to == all)) ++to;
+            OPCHK(multiply(o.gram, o.gram, o.poly[to], SCALE_B * k[2] / (SCALE_A * SCALE_A), o.gram, SCALE_B * k[1] / SCALE_A, SCALE_B * k[0]));
+            if (r) {
+                const int together = 3 - to - all;   // neither of them; the last step's B is no longer needed
+                OPCHK(multiply(o.poly[to], o.poly[all], o.poly[together], 1.f / SCALE_B, nullptr, 0.f, 0.f));
+                all = together;
+            }
+            now = to;
         }
+        // wide: out[r][c] = sum over k of X[k][c] B[r][k];  tall: sum over k of B[c][k] X[r][k]
+        const Operand poly = operand(square(o.poly[all]));
+        p.m = cols;
+        p.n = rows;
+        p.k = n;
+        p.a = wide ? operand(x[0]) : poly;
+        p.b = wide ? poly : operand(x[0]);
+        p.a_batch = (wide ? x_batch : g_batch) * 2;
+        p.b_batch = (wide ? g_batch : x_batch) * 2;
+        const int how = first ? PAIR_ONE : FULL;
+        i += stage;
+        if (i < steps)
+            OPCHK(launch_apply(o.plan_apply, p, {x[1], x_batch, 1.f / SCALE_B, ratio}, wide, how, s));
+        else
+            OPCHK(launch_apply_last(o.plan_apply, p, {out, size, cols, scale / (SCALE_B * SCALE_X), ratio, whole_rows<T>(out, cols)},
+                                    wide, how, s));
         const Planes t = x[0];
         x[0] = x[1];
         x[1] = t;
@@ -294,7 +380,7 @@ extern "C" {
 lcn_status lcn_orthogonalise_workspace_bytes(int64_t count, int32_t rows, int32_t cols, int32_t dtype, size_t *bytes)
 {
     if (!bytes || !orthogonal_args_fit(count, rows, cols, dtype)) return LCN_ERR_INVALID_ARG;
-    *bytes = count == 0 ? 0 : orthogonal_space(nullptr, count, rows, cols).bytes;
+    *bytes = count == 0 || small(rows, cols) ? 0 : orthogonal_space(nullptr, count, rows, cols, dtype).bytes;
     return LCN_OK;
 }
 
@@ -302,16 +388,23 @@ lcn_status lcn_orthogonalise(const void *g, int64_t count, int32_t rows, int32_t
                              const float *coefficients, float eps, float scale, void *out, void *workspace, size_t workspace_bytes,
                              void *hip_stream)
 {
-    if (!orthogonal_args_fit(count, rows, cols, dtype) || steps < 1 || steps > 64 || !coefficients || !(eps >= 0.f) || eps > 3.4e38f ||
-        !(__builtin_fabsf(scale) <= 3.4e38f) || !coefficients_fit(steps, coefficients))
+    double poly[MOST_STEPS];
+    if (!orthogonal_args_fit(count, rows, cols, dtype) || steps < 1 || steps > MOST_STEPS || !coefficients || !(eps >= 0.f) || eps > 3.4e38f ||
+        !(__builtin_fabsf(scale) <= 3.4e38f) || !coefficients_fit(steps, coefficients, poly))
         return LCN_ERR_INVALID_ARG;
     if (count == 0) return LCN_OK;
     if (!g || !out) return LCN_ERR_INVALID_ARG;
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (small(rows, cols)) {
+        if (dtype == LCN_F32)
+            return small_as((const float *)g, count, rows, cols, steps, coefficients, eps, scale, (float *)out, s);
+        return small_as((const __bf16 *)g, count, rows, cols, steps, coefficients, eps, scale, (__bf16 *)out, s);
+    }
     if (dtype == LCN_F32)
-        return orthogonal_as((const float *)g, count, rows, cols, steps, coefficients, eps, scale, (float *)out, (char *)workspace,
-                             workspace_bytes, (hipStream_t)hip_stream);
-    return orthogonal_as((const __bf16 *)g, count, rows, cols, steps, coefficients, eps, scale, (__bf16 *)out, (char *)workspace,
-                         workspace_bytes, (hipStream_t)hip_stream);
+        return orthogonal_as((const float *)g, count, rows, cols, dtype, steps, coefficients, poly, eps, scale, (float *)out,
+                             (char *)workspace, workspace_bytes, s);
+    return orthogonal_as((const __bf16 *)g, count, rows, cols, dtype, steps, coefficients, poly, eps, scale, (__bf16 *)out, (char *)workspace,
+                         workspace_bytes, s);
 }
 
 }  // extern "C"

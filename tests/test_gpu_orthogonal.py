@@ -126,14 +126,14 @@ def test_batches(count, rows, cols, dtype):
             assert off(x[i], want) <= room + (2.0 ** -8 if dtype == BF16 else 0.0)
 
 
-@pytest.mark.parametrize("rows,cols", [(64, 64), (300, 500), (900, 600), (1500, 1024)])
+@pytest.mark.parametrize("rows,cols", [(64, 64), (300, 500), (900, 600), (1500, 1024), (100, 800), (1200, 128), (4100, 520)])
 def test_one_rounding_of_bf16(rows, cols):
     g = gradient(3, rows, cols, BF16)
     assert off(lcn.lcn_orthogonalise(g), oracle(g, 5, UPDATE)[0]) <= roundings(1)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("rows,cols", [(96, 60), (400, 300)])
+@pytest.mark.parametrize("rows,cols", [(96, 60), (400, 300), (900, 100)])
 def test_few_directions(rows, cols, dtype):
     """A gradient of 6 samples has 6 singular values beside those of its rounding, which grow the most: also they come out."""
     g = generator(9, rows, cols)
@@ -216,7 +216,8 @@ def test_refusals():
         with pytest.raises(ValueError):
             lcn.lcn_orthogonalise(g, **bad)
     for bad in (dict(steps=65), dict(eps=-1.0), dict(eps=math.nan), dict(scale=math.inf), dict(coefficients=(math.nan, 0.0, 0.0)),
-                dict(coefficients=(5.0, 0.0, 0.0)), dict(coefficients=(100.0, -300.0, 200.0)),
-                dict(workspace=torch.empty(16, dtype=torch.uint8, device=DEV))):
+                dict(coefficients=(5.0, 0.0, 0.0)), dict(coefficients=(100.0, -300.0, 200.0))):
         with pytest.raises(lcn.LcnError):
             lcn.lcn_orthogonalise(g, **bad)
+    with pytest.raises(lcn.LcnError):   # a workspace that is too small
+        lcn.lcn_orthogonalise(torch.ones(300, 300, device=DEV), workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
