@@ -27,6 +27,7 @@ SOURCES = {
     "kernels_planes.hip": [],
     "kernels_linear.hip": [],
     "kernels_gated.hip": [],
+    "kernels_gated_narrow.hip": [],
     "kernels_norm.hip": [],
     "kernels_orthogonal.hip": [],
     "kernels_pair.hip": [],

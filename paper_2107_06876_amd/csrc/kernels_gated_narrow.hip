@@ -1,0 +1,299 @@
+// The gated layer with few inputs and outputs on many rows: bound by reading rows and writing them, so nothing is laid out first.
+//
+// Forward, a workgroup has 32 outputs, their rows of Wg and Wu in registers, and a wavefront goes over rows 16 at a time, straight
+// from memory into the matrix instruction.  Backward, all in one launch: a wavefront forms dz of 16 rows in the order that the
+// instruction takes for dx = dz W, W from LDS, and turns it around in LDS for its part of dW = dz^T x, which stays in registers from
+// row to row, as db does; a workgroup leaves its sums, which a second launch adds.  The float instruction serves bf16 tensors as
+// well: dz and all sums are in 32 bits.
+#include "gated.h"
+
+namespace lcn {
+
+constexpr int NARROW = 64;   // inputs, outputs
+
+template <class T, int KP, int ACT, bool KEPT>
+__global__ __launch_bounds__(256) void gated_narrow_kernel(GatedArgs<T> e, const T *__restrict__ x, const T *__restrict__ w,
+                                                           long long rows, int k, int width)
+{
+    constexpr int C = KP / 32;
+    const int lane = threadIdx.x & 63, g = lane >> 4, m0 = (int)blockIdx.y * 32, wp = (int)padded(width);
+    typename Frag<T>::type fw[2][2][C];   // of Wg and Wu
+    f32x4 bias[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int m = m0 + i * 16 + (lane & 15), mb = m0 + i * 16 + 4 * g;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                fw[h][i][c] = read_fragment<T, true>(m < width ? w + (long long)(h * width + m) * k : nullptr, 32 * c + 8 * g, k);
+            bias[h][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (e.bias && mb < width) bias[h][i] = load_four(e.bias + h * width + mb, width - mb, e.whole);
+        }
+    const long long tiles = (rows + 15) / 16, step = (long long)gridDim.x * 4;
+    for (long long t = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); t < tiles; t += step) {
+        const long long n = t * 16 + (lane & 15);
+        const T *row = n < rows ? x + n * k : nullptr;
+        f32x4 z[2][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) z[h][i] = bias[h][i];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const typename Frag<T>::type fx = read_fragment<T, true>(row, 32 * c + 8 * g, k);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) mma(z[h][i], fw[h][i][c], fx);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int m = m0 + i * 16 + 4 * g;   // four values; a piece of eight has those of the lane 16 before or behind as well
+            if constexpr (KEPT) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if constexpr (sizeof(T) == 4) {
+                        if (n < rows && m < wp) *(f32x4 *)(e.kept + (n * 2 + h) * wp + m) = z[h][i];
+                    } else {
+                        f32x4 v[2], other;
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) other[u] = __shfl_xor(z[h][i][u], 16);
+                        v[0] = g & 1 ? other : z[h][i];
+                        v[1] = g & 1 ? z[h][i] : other;
+                        if (!(g & 1) && n < rows && m < wp) Keep<T>::store(e.kept + (n * 2 + h) * wp + m, v);
+                    }
+                }
+            }
+            if (n >= rows || m >= width) continue;
+            f32x4 y;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) y[u] = gate<T, ACT>(z[0][i][u]) * z[1][i][u];
+            store_four(e.y + n * width + m, y, width - m, e.whole);
+        }
+    }
+}
+
+// D tiles of 16 inputs, C chunks of 32 outputs
+template <class T, int ACT, int D, int C>
+__global__ __launch_bounds__(256) void gated_narrow_grad_kernel(const T *__restrict__ x, const T *__restrict__ w,
+                                                                const typename Keep<T>::type *__restrict__ kept,
+                                                                const T *__restrict__ dy, long long rows, int d_in, int width,
+                                                                T *__restrict__ dx, float *__restrict__ part, int whole, int whole_dx)
+{
+    // pitches: rows 8 (of W) and 1 (of dz) apart begin 16 banks apart
+    constexpr int WP = D * 16 + 2, ZP = C * 64 + 16, K = C * 64;
+    __shared__ __align__(16) float lds_w[K * WP];         // rows of Wg, then of Wu from C * 32 on
+    __shared__ __align__(16) float lds_z[4 * 16 * ZP];    // a wavefront's dz
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, l = lane & 15, wp = (int)padded(width);
+    for (int i = tid; i < K * D * 16; i += 256) {
+        const int k = i / (D * 16), c = i % (D * 16), h = k / (C * 32), m = k % (C * 32);
+        lds_w[k * WP + c] = m < width && c < d_in ? (float)w[(long long)(h * width + m) * d_in + c] : 0.f;
+    }
+    __syncthreads();
+    float *z = lds_z + wave * 16 * ZP;
+    f32x4 dw[2 * C * 2][D];
+    float db[2][C][8];
+#pragma unroll
+    for (int i = 0; i < 4 * C; ++i)
+#pragma unroll
+        for (int t = 0; t < D; ++t) dw[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int u = 0; u < 8; ++u) db[0][c][u] = db[1][c][u] = 0.f;
+    const long long tiles = (rows + 15) / 16;
+    for (long long tile = (long long)blockIdx.x * 4 + wave; tile < tiles; tile += (long long)gridDim.x * 4) {
+        const long long n = tile * 16 + l;
+        float xs[4][D];   // x of rows 4 s + g, for dW
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int t = 0; t < D; ++t) {
+                const long long r = tile * 16 + 4 * s + g;
+                xs[s][t] = part && r < rows && t * 16 + l < d_in ? (float)x[r * d_in + t * 16 + l] : 0.f;
+            }
+        f32x4 out[D];
+#pragma unroll
+        for (int t = 0; t < D; ++t) out[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int m = 32 * c + 8 * g;
+            f32x4 d[2], a[2], b[2];
+            d[0] = d[1] = a[0] = a[1] = b[0] = b[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (n < rows && m < width) {
+                load_eight(dy + n * width + m, width - m, whole, d);
+                Keep<T>::load(kept + n * 2 * wp + m, a);
+                Keep<T>::load(kept + (n * 2 + 1) * wp + m, b);
+            }
+            Frag<float>::type f[2];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float v = d[u >> 2][u & 3];
+                float act, slope;
+                gate_and_slope<T, ACT>(a[u >> 2][u & 3], act, slope);
+                f[0][u] = v * b[u >> 2][u & 3] * slope;
+                f[1][u] = v * act;
+                db[0][c][u] += f[0][u];
+                db[1][c][u] += f[1][u];
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k0 = h * C * 32 + m;
+                if (dx)
+#pragma unroll
+                    for (int t = 0; t < D; ++t) {
+                        Frag<float>::type fw;
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) fw[u] = lds_w[(k0 + u) * WP + t * 16 + l];
+                        mma(out[t], fw, f[h]);
+                    }
+#pragma unroll
+                for (int u = 0; u < 8; u += 4) *(f32x4 *)(z + l * ZP + k0 + u) = f32x4{f[h][u], f[h][u + 1], f[h][u + 2], f[h][u + 3]};
+            }
+        }
+        if (dx && n < rows)
+#pragma unroll
+            for (int t = 0; t < D; ++t)
+                if (t * 16 + 4 * g < d_in) store_four(dx + n * d_in + t * 16 + 4 * g, out[t], d_in - t * 16 - 4 * g, whole_dx);
+        if (!part) continue;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // LDS serves a wavefront in order
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < 4 * C; ++i)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const float v = z[(4 * s + g) * ZP + i * 16 + l];
+#pragma unroll
+                for (int t = 0; t < D; ++t) dw[i][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, xs[s][t], dw[i][t], 0, 0, 0);
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    if (!part) return;
+    // dw[i][t]: row k = 16 i + 4 g + e, column 16 t + l.  The four wavefronts' sums one after another, in LDS, then db behind them.
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) db[h][c][u] += __shfl_xor(db[h][c][u], o, 16);
+    __syncthreads();
+    float *sum = lds_w, *sum_b = lds_z;
+    for (int v = 0; v < 4; ++v) {
+        if (wave == v) {
+#pragma unroll
+            for (int i = 0; i < 4 * C; ++i)
+#pragma unroll
+                for (int t = 0; t < D; ++t)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        float *at = sum + (16 * i + 4 * g + q) * WP + 16 * t + l;
+                        *at = v ? *at + dw[i][t][q] : dw[i][t][q];
+                    }
+            if (l == 0)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int c = 0; c < C; ++c)
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) {
+                            float *at = sum_b + h * C * 32 + 32 * c + 8 * g + u;
+                            *at = v ? *at + db[h][c][u] : db[h][c][u];
+                        }
+        }
+        __syncthreads();
+    }
+    float *to = part + (long long)blockIdx.x * 2 * width * (d_in + 1);
+    for (int i = tid; i < 2 * width * d_in; i += 256) {
+        const int k = i / d_in, c = i - k * d_in, h = k >= width, m = k - h * width;
+        to[i] = sum[(h * C * 32 + m) * WP + c];
+    }
+    for (int i = tid; i < 2 * width; i += 256) to[2 * width * d_in + i] = sum_b[(i >= width) * C * 32 + i - (i >= width) * width];
+}
+
+// adds up the workgroups' sums: values 0 .. first - 1 are dw, the others db; 16 values per workgroup, 16 threads each, in a fixed order
+template <class T>
+__global__ __launch_bounds__(256) void gated_narrow_join_kernel(const float *__restrict__ part, int parts, int first, int all,
+                                                                T *__restrict__ dw, T *__restrict__ db)
+{
+    __shared__ float sums[16][17];
+    const int c = blockIdx.x * 16 + (threadIdx.x & 15), q = threadIdx.x >> 4;
+    float v = 0.f;
+    if (c < all)
+#pragma unroll 8
+        for (int r = q; r < parts; r += 16) v += part[(long long)r * all + c];
+    sums[q][threadIdx.x & 15] = v;
+    __syncthreads();
+    if (q || c >= all) return;
+#pragma unroll
+    for (int u = 1; u < 16; ++u) v += sums[u][threadIdx.x];
+    if (c < first) {
+        if (dw) dw[c] = (T)v;
+    } else if (db) {
+        db[c - first] = (T)v;
+    }
+}
+
+// ---- host ---------------------------------------------------------------------
+
+bool gated_narrow(const void *x, const void *w, int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype)
+{
+    return rows >= 128 && d_in <= NARROW && d_out <= NARROW && d_in % (dtype == LCN_F32 ? 4 : 8) == 0 &&
+           (((uintptr_t)x | (uintptr_t)w) & 15) == 0;
+}
+
+int gated_narrow_groups(int64_t rows)
+{
+    const int64_t groups = (rows + 63) / 64;
+    return (int)(groups < 256 ? groups : 256);
+}
+
+template <class T>
+hipError_t launch_gated_narrow(const GatedArgs<T> &e, const T *x, const T *w, int64_t rows, int32_t d_in, int32_t d_out, hipStream_t s)
+{
+    const long long groups = (rows + 63) / 64, tiles = (d_out + 31) / 32, most = 2048 / tiles;
+    const dim3 grid((unsigned)(groups < most ? groups : most), (unsigned)tiles);
+    return by_activation(e.act, [&](auto a) {
+        constexpr int ACT = decltype(a)::value;
+        auto launch = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, e, x, w, (long long)rows, d_in, d_out);
+            return hipGetLastError();
+        };
+        if (e.kept) return d_in <= 32 ? launch(gated_narrow_kernel<T, 32, ACT, true>) : launch(gated_narrow_kernel<T, 64, ACT, true>);
+        return d_in <= 32 ? launch(gated_narrow_kernel<T, 32, ACT, false>) : launch(gated_narrow_kernel<T, 64, ACT, false>);
+    });
+}
+template hipError_t launch_gated_narrow(const GatedArgs<float> &, const float *, const float *, int64_t, int32_t, int32_t, hipStream_t);
+template hipError_t launch_gated_narrow(const GatedArgs<__bf16> &, const __bf16 *, const __bf16 *, int64_t, int32_t, int32_t, hipStream_t);
+
+template <class T>
+hipError_t launch_gated_narrow_backward(const T *x, const T *w, const typename Keep<T>::type *kept, const T *dy, int64_t rows, int32_t d_in,
+                                        int32_t d_out, int32_t act, T *dx, T *dw, T *db, float *part, hipStream_t s)
+{
+    const int groups = gated_narrow_groups(rows), first = 2 * d_out * d_in, all = first + 2 * d_out;
+    const bool sums = dw || db;
+    const int whole = whole_rows<T>(dy, d_out);
+    const hipError_t st = by_activation(act, [&](auto a) {
+        constexpr int ACT = decltype(a)::value;
+        auto launch = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, s, x, w, kept, dy, (long long)rows, d_in, d_out, dx,
+                               sums ? part : nullptr, whole, whole_rows<T>(dx, d_in));
+            return hipGetLastError();
+        };
+        if (d_out <= 32)
+            return d_in <= 32 ? launch(gated_narrow_grad_kernel<T, ACT, 2, 1>) : launch(gated_narrow_grad_kernel<T, ACT, 4, 1>);
+        return d_in <= 32 ? launch(gated_narrow_grad_kernel<T, ACT, 2, 2>) : launch(gated_narrow_grad_kernel<T, ACT, 4, 2>);
+    });
+    if (st != hipSuccess || !sums) return st;
+    hipLaunchKernelGGL(gated_narrow_join_kernel<T>, dim3((unsigned)((all + 15) / 16)), dim3(256), 0, s, part, groups, first, all, dw, db);
+    return hipGetLastError();
+}
+template hipError_t launch_gated_narrow_backward(const float *, const float *, const float *, const float *, int64_t, int32_t, int32_t,
+                                                 int32_t, float *, float *, float *, float *, hipStream_t);
+template hipError_t launch_gated_narrow_backward(const __bf16 *, const __bf16 *, const unsigned short *, const __bf16 *, int64_t, int32_t,
+                                                 int32_t, int32_t, __bf16 *, __bf16 *, __bf16 *, float *, hipStream_t);
+
+}  // namespace lcn

@@ -400,6 +400,7 @@ template <int L, int C>
 struct Lanes {
     static constexpr int lanes = L, pieces = C;
 };
+constexpr int longest(int v) { return v == 1 ? 8192 : 2048; }
 template <int V, class F>
 static bool by_lanes(int units, int64_t rows, hipError_t &st, F f)
 {
@@ -425,9 +426,10 @@ static bool by_lanes(int units, int64_t rows, hipError_t &st, F f)
              : units <= 512  ? f(Lanes<256, 2>())
              : units <= 1024 ? f(Lanes<256, 4>())
              : units <= 2048 ? f(Lanes<256, 8>())
+             : units <= longest(V) ? (units <= 4096 ? f(Lanes<256, V == 1 ? 16 : 8>()) : f(Lanes<256, V == 1 ? 32 : 8>()))
                              : hipSuccess;
     }
-    return units <= 2048;
+    return units <= longest(V);
 }
 
 template <class T>

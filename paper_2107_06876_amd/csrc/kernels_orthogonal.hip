@@ -88,14 +88,21 @@ __global__ __launch_bounds__(256) void normalise_kernel(const T *__restrict__ g,
 // All steps of a matrix in one workgroup, X, A and B as floats in LDS, on the float matrix instruction (its operands and sums are
 // single precision as they are).  X lies with its longer side as rows.  Bound by the chain of its products: 8 matrices of 96 x 32,
 // 5 steps: see below.
+// a product's eight instructions in two chains
+__device__ __forceinline__ void mma_two(f32x4 (&c)[2], const Frag<float>::type &a, const Frag<float>::type &b)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c[e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c[e & 1], 0, 0, 0);
+}
+
 template <class T, int D, int ROWS>
 __global__ __launch_bounds__(512) void orthogonal_small_kernel(const T *__restrict__ g, int rows, int cols, int steps, SmallSteps c,
                                                                float eps, float scale, T *out)   // out may be g
 {
     typedef Tile<float, D> L;
-    constexpr int N = D / 16;
+    constexpr int N = D / 16, PARTS = 8 / (N * N) > 1 ? 8 / (N * N) : 1;   // A's sums over parts of the rows, so that all wavefronts work
     __shared__ __align__(1024) char xs[ROWS * D * 4];
-    __shared__ __align__(1024) char as[D * D * 4];
+    __shared__ __align__(1024) char as[PARTS][D * D * 4];
     __shared__ __align__(1024) char bs[D * D * 4];
     __shared__ double sums[8];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = lane >> 4;
@@ -124,23 +131,31 @@ __global__ __launch_bounds__(512) void orthogonal_small_kernel(const T *__restri
     }
     for (int s = 0; s < steps; ++s) {
         __syncthreads();
-        for (int b = wave; b < N * N; b += 8) {   // A[i][j]: sum over the rows of X
-            const int i = b / N * 16, j = b % N * 16;
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-            for (int r = 0; r < blocks * 16; r += 32) mma(acc, L::columns(xs, r, i, lane), L::columns(xs, r, j, lane));
+        for (int b = wave; b < N * N * PARTS; b += 8) {   // A[i][j]: sum over the rows of X
+            const int part = b / (N * N), i = b % (N * N) / N * 16, j = b % N * 16;
+            f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+            for (int r = part * 32; r < blocks * 16; r += 32 * PARTS) mma_two(acc, L::columns(xs, r, i, lane), L::columns(xs, r, j, lane));
+            acc[0] += acc[1];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) at(as, i + 4 * grp + e, j + (lane & 15)) = acc[e];
+            for (int e = 0; e < 4; ++e) at(as[part], i + 4 * grp + e, j + (lane & 15)) = acc[0][e];
         }
         __syncthreads();
         for (int b = wave; b < N * N; b += 8) {   // B = a + b A + c A A
             const int i = b / N * 16, j = b % N * 16;
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+            auto rows_of_a = [&](int r, int k) {
+                Frag<float>::type f = L::rows(as[0], r, k, lane);
+                if (PARTS > 1) f += L::rows(as[PARTS - 1], r, k, lane);
+                return f;
+            };
+            f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-            for (int k = 0; k < D / 32; ++k) mma(acc, L::rows(as, i, k, lane), L::rows(as, j, k, lane));
+            for (int k = 0; k < D / 32; ++k) mma_two(acc, rows_of_a(i, k), rows_of_a(j, k));
+            acc[0] += acc[1];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int m = i + 4 * grp + e, n = j + (lane & 15);
-                at(bs, m, n) = c.c[s][2] * acc[e] + c.c[s][1] * at(as, m, n) + (m == n ? c.c[s][0] : 0.f);
+                const float one = PARTS > 1 ? at(as[0], m, n) + at(as[PARTS - 1], m, n) : at(as[0], m, n);
+                at(bs, m, n) = c.c[s][2] * acc[0][e] + c.c[s][1] * one + (m == n ? c.c[s][0] : 0.f);
             }
         }
         __syncthreads();

@@ -376,7 +376,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void pair_join_kernel(PairArgs p, G
 PairPlan plan_pair(long long m, long long n, long long k, long long batches, bool symmetric, bool bf16)
 {
     static const int resident[PAIR_SHAPES] = {1, 2, 1};
-    static const double alone_us[PAIR_SHAPES] = {2.4, 0.85, 0.32}, full_us[PAIR_SHAPES] = {2.6, 1.55, 0.37};
+    static const double alone_us[PAIR_SHAPES] = {2.4, 0.85, 0.32}, full_us[PAIR_SHAPES] = {2.6, 1.35, 0.37};
     PairPlan best{PAIR_64, 1};
     double least = 1e300;
     for (int t = bf16 ? 0 : 1; t < PAIR_SHAPES; ++t) {
@@ -389,7 +389,7 @@ PairPlan plan_pair(long long m, long long n, long long k, long long batches, boo
             const long long rounds = groups / room, rest = groups % room;
             double us = (double)rounds * (full_us[t] * (double)each + 4.0);
             if (rest) us += (rest <= 256 ? alone_us[t] : full_us[t]) * (double)each + 4.0;
-            if (splits > 1) us += 5.0 + (double)groups * w * w * 8e-6 / 3.0;
+            if (splits > 1) us += 5.0 + (double)groups * w * w * 8e-6 / 4.0;
             if (us < least) {
                 least = us;
                 best = PairPlan{t, splits};

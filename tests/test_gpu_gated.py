@@ -89,6 +89,28 @@ def test_large_tiles(rows, d_in, d_out, dtype):
     check(rows, d_in, d_out, "silu", dtype)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("rows,d_in,d_out", [(128, 8, 64), (300, 64, 40), (1000, 40, 33), (777, 32, 64), (515, 56, 20), (129, 16, 1),
+                                             (4099, 64, 64), (20000, 32, 31)])
+def test_narrow_layers(rows, d_in, d_out, act, dtype):
+    """Few inputs and outputs: up to 32 and 64 of either, every activation; dz is not rounded there."""
+    check(rows, d_in, d_out, act, dtype)
+    check(rows, d_in, d_out, act, dtype, bias=False)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,d_in,d_out", [(300, 32, 64), (1000, 64, 33)])
+def test_single_gradients_of_narrow_layers(rows, d_in, d_out, dtype):
+    x, w, b, dy = inputs(rows, d_in, d_out, dtype)
+    _, z = lcn.lcn_gated_linear(x, w, bias=b, keep_pre=True)
+    want = lcn.lcn_gated_linear_backward(x, w, z, dy)
+    for asked in ((1, 1, 1), (1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 1, 0), (1, 0, 1), (0, 1, 1), (0, 0, 0)):
+        got = lcn.lcn_gated_linear_backward(x, w, z, dy, with_x=asked[0], with_w=asked[1], with_bias=asked[2])
+        for a, u, v in zip(asked, got, want):
+            assert torch.equal(u, v) if a else u is None
+
+
 @pytest.mark.parametrize("rows", [12, 300, 512, 700, 4103])
 @pytest.mark.parametrize("act", ["silu", "gelu"])
 def test_roundings_of_bf16(act, rows):

@@ -58,7 +58,7 @@ def check(rows, dim, dtype, affine=True, around=True, shift=0):
 @pytest.mark.parametrize("rows,dim", [
     (1, 16), (1, 2048), (2, 3), (5, 7), (3, 33), (64, 32), (1000, 32), (700, 40), (257, 63), (130, 64), (300, 100), (333, 129),
     (515, 300), (200, 301), (100, 512), (77, 1000), (64, 1024), (65, 1025), (50, 2048), (37, 2051), (33, 4096), (12, 8192),
-    (7, 8193), (9, 16384), (3, 20000), (2, 70001)])
+    (7, 8193), (2100, 5281), (2053, 3333), (9, 8191), (9, 16384), (3, 20000), (2, 70001)])
 def test_sizes(rows, dim, dtype):
     check(rows, dim, dtype)
 
