@@ -31,22 +31,28 @@ __global__ __launch_bounds__(256) void gated_narrow_kernel(GatedArgs<T> e, const
             if (e.bias && mb < width) bias[h][i] = load_four(e.bias + h * width + mb, width - mb, e.whole);
         }
     const long long tiles = (rows + 15) / 16, step = (long long)gridDim.x * 4;
-    for (long long t = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); t < tiles; t += step) {
+    typename Frag<T>::type fx[C];
+    auto read = [&](long long t) {
         const long long n = t * 16 + (lane & 15);
-        const T *row = n < rows ? x + n * k : nullptr;
+#pragma unroll
+        for (int c = 0; c < C; ++c) fx[c] = read_fragment<T, true>(n < rows ? x + n * k : nullptr, 32 * c + 8 * g, k);
+    };
+    long long t = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    read(t);
+    for (; t < tiles; t += step) {
+        const long long n = t * 16 + (lane & 15);
         f32x4 z[2][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 2; ++i) z[h][i] = bias[h][i];
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const typename Frag<T>::type fx = read_fragment<T, true>(row, 32 * c + 8 * g, k);
+        for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) mma(z[h][i], fw[h][i][c], fx);
-        }
+                for (int i = 0; i < 2; ++i) mma(z[h][i], fw[h][i][c], fx[c]);
+        read(t + step);   // the next rows, while these are finished
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int m = m0 + i * 16 + 4 * g;   // four values; a piece of eight has those of the lane 16 before or behind as well
@@ -86,9 +92,12 @@ __global__ __launch_bounds__(256) void gated_narrow_grad_kernel(const T *__restr
     __shared__ __align__(16) float lds_w[K * WP];         // rows of Wg, then of Wu from C * 32 on
     __shared__ __align__(16) float lds_z[4 * 16 * ZP];    // a wavefront's dz
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, l = lane & 15, wp = (int)padded(width);
-    for (int i = tid; i < K * D * 16; i += 256) {
-        const int k = i / (D * 16), c = i % (D * 16), h = k / (C * 32), m = k % (C * 32);
-        lds_w[k * WP + c] = m < width && c < d_in ? (float)w[(long long)(h * width + m) * d_in + c] : 0.f;
+#pragma unroll
+    for (int u = 0; u < K * D * 4 / 256; ++u) {   // d_in is a multiple of four, W aligned to as many values
+        const int i = u * 256 + tid, k = i / (D * 4), c = i % (D * 4) * 4, h = k / (C * 32), m = k % (C * 32);
+        const f32x4 v = m < width ? load_four(w + (h * width + m) * d_in + c, d_in - c, true) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) lds_w[k * WP + c + e] = v[e];
     }
     __syncthreads();
     float *z = lds_z + wave * 16 * ZP;
@@ -102,37 +111,51 @@ __global__ __launch_bounds__(256) void gated_narrow_grad_kernel(const T *__restr
     for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int u = 0; u < 8; ++u) db[0][c][u] = db[1][c][u] = 0.f;
-    const long long tiles = (rows + 15) / 16;
-    for (long long tile = (long long)blockIdx.x * 4 + wave; tile < tiles; tile += (long long)gridDim.x * 4) {
+    const long long tiles = (rows + 15) / 16, step = (long long)gridDim.x * 4;
+    struct Rows {
+        f32x4 d[C][2], a[C][2], b[C][2];   // of row l: dy, g and u
+        float x[4][D];                     // of rows 4 s + g, for dW
+    };
+    auto read = [&](long long tile, Rows &v) {
         const long long n = tile * 16 + l;
-        float xs[4][D];   // x of rows 4 s + g, for dW
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int m = 32 * c + 8 * g;
+            v.d[c][0] = v.d[c][1] = v.a[c][0] = v.a[c][1] = v.b[c][0] = v.b[c][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (n < rows && m < width) {
+                load_eight(dy + n * width + m, width - m, whole, v.d[c]);
+                Keep<T>::load(kept + n * 2 * wp + m, v.a[c]);
+                Keep<T>::load(kept + (n * 2 + 1) * wp + m, v.b[c]);
+            }
+        }
 #pragma unroll
         for (int s = 0; s < 4; ++s)
 #pragma unroll
             for (int t = 0; t < D; ++t) {
                 const long long r = tile * 16 + 4 * s + g;
-                xs[s][t] = part && r < rows && t * 16 + l < d_in ? (float)x[r * d_in + t * 16 + l] : 0.f;
+                v.x[s][t] = part && r < rows && t * 16 + l < d_in ? (float)x[r * d_in + t * 16 + l] : 0.f;
             }
+    };
+    long long tile = (long long)blockIdx.x * 4 + wave;
+    Rows next;
+    read(tile, next);
+    for (; tile < tiles; tile += step) {
+        const long long n = tile * 16 + l;
+        const Rows now = next;
+        read(tile + step, next);   // while these rows are worked on
         f32x4 out[D];
 #pragma unroll
         for (int t = 0; t < D; ++t) out[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int m = 32 * c + 8 * g;
-            f32x4 d[2], a[2], b[2];
-            d[0] = d[1] = a[0] = a[1] = b[0] = b[1] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (n < rows && m < width) {
-                load_eight(dy + n * width + m, width - m, whole, d);
-                Keep<T>::load(kept + n * 2 * wp + m, a);
-                Keep<T>::load(kept + (n * 2 + 1) * wp + m, b);
-            }
             Frag<float>::type f[2];
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                const float v = d[u >> 2][u & 3];
+                const float v = now.d[c][u >> 2][u & 3];
                 float act, slope;
-                gate_and_slope<T, ACT>(a[u >> 2][u & 3], act, slope);
-                f[0][u] = v * b[u >> 2][u & 3] * slope;
+                gate_and_slope<T, ACT>(now.a[c][u >> 2][u & 3], act, slope);
+                f[0][u] = v * now.b[c][u >> 2][u & 3] * slope;
                 f[1][u] = v * act;
                 db[0][c][u] += f[0][u];
                 db[1][c][u] += f[1][u];
@@ -165,13 +188,14 @@ __global__ __launch_bounds__(256) void gated_narrow_grad_kernel(const T *__restr
             for (int s = 0; s < 4; ++s) {
                 const float v = z[(4 * s + g) * ZP + i * 16 + l];
 #pragma unroll
-                for (int t = 0; t < D; ++t) dw[i][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, xs[s][t], dw[i][t], 0, 0, 0);
+                for (int t = 0; t < D; ++t) dw[i][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, now.x[s][t], dw[i][t], 0, 0, 0);
             }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
     if (!part) return;
-    // dw[i][t]: row k = 16 i + 4 g + e, column 16 t + l.  The four wavefronts' sums one after another, in LDS, then db behind them.
+    // dw[i][t]: row k = 16 i + 4 g + e, column 16 t + l.  Two wavefronts leave their sums in LDS, the other two add theirs.
+    __shared__ float lds_b[2][K];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -180,38 +204,43 @@ __global__ __launch_bounds__(256) void gated_narrow_grad_kernel(const T *__restr
             for (int u = 0; u < 8; ++u)
 #pragma unroll
                 for (int o = 8; o > 0; o >>= 1) db[h][c][u] += __shfl_xor(db[h][c][u], o, 16);
-    __syncthreads();
-    float *sum = lds_w, *sum_b = lds_z;
-    for (int v = 0; v < 4; ++v) {
-        if (wave == v) {
-#pragma unroll
-            for (int i = 0; i < 4 * C; ++i)
-#pragma unroll
-                for (int t = 0; t < D; ++t)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        float *at = sum + (16 * i + 4 * g + q) * WP + 16 * t + l;
-                        *at = v ? *at + dw[i][t][q] : dw[i][t][q];
-                    }
-            if (l == 0)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int c = 0; c < C; ++c)
-#pragma unroll
-                        for (int u = 0; u < 8; ++u) {
-                            float *at = sum_b + h * C * 32 + 32 * c + 8 * g + u;
-                            *at = v ? *at + db[h][c][u] : db[h][c][u];
-                        }
-        }
+    static_assert(K * WP <= 4 * 16 * ZP, "a second place for dW's sums");
+    float *sum = wave & 1 ? lds_z : lds_w;
+    for (int turn = 0; turn < 2; ++turn) {
         __syncthreads();
+        if (wave >> 1 != turn) continue;
+#pragma unroll
+        for (int i = 0; i < 4 * C; ++i)
+#pragma unroll
+            for (int t = 0; t < D; ++t)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float *at = sum + (16 * i + 4 * g + q) * WP + 16 * t + l;
+                    *at = turn ? *at + dw[i][t][q] : dw[i][t][q];
+                }
+        if (l == 0)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        float *at = lds_b[wave & 1] + h * C * 32 + 32 * c + 8 * g + u;
+                        *at = turn ? *at + db[h][c][u] : db[h][c][u];
+                    }
     }
+    __syncthreads();
+    // rows of dW as they lie in memory, without those that are padding
     float *to = part + (long long)blockIdx.x * 2 * width * (d_in + 1);
-    for (int i = tid; i < 2 * width * d_in; i += 256) {
-        const int k = i / d_in, c = i - k * d_in, h = k >= width, m = k - h * width;
-        to[i] = sum[(h * C * 32 + m) * WP + c];
+#pragma unroll 4
+    for (int i = tid; i < K * D * 16; i += 256) {
+        const int k = i / (D * 16), c = i % (D * 16), h = k / (C * 32), m = k % (C * 32);
+        if (m < width && c < d_in) to[(h * width + m) * d_in + c] = lds_w[k * WP + c] + lds_z[k * WP + c];
     }
-    for (int i = tid; i < 2 * width; i += 256) to[2 * width * d_in + i] = sum_b[(i >= width) * C * 32 + i - (i >= width) * width];
+    for (int k = tid; k < K; k += 256) {
+        const int h = k / (C * 32), m = k % (C * 32);
+        if (m < width) to[2 * width * d_in + h * width + m] = lds_b[0][k] + lds_b[1][k];
+    }
 }
 
 // adds up the workgroups' sums: values 0 .. first - 1 are dw, the others db; 16 values per workgroup, 16 threads each, in a fixed order
@@ -248,13 +277,16 @@ bool gated_narrow(const void *x, const void *w, int64_t rows, int32_t d_in, int3
 int gated_narrow_groups(int64_t rows)
 {
     const int64_t groups = (rows + 63) / 64;
-    return (int)(groups < 256 ? groups : 256);
+    return (int)(groups < 256 ? groups : 256);   // one to a compute unit: 512 take 38 us instead of 31
 }
 
 template <class T>
 hipError_t launch_gated_narrow(const GatedArgs<T> &e, const T *x, const T *w, int64_t rows, int32_t d_in, int32_t d_out, hipStream_t s)
 {
-    const long long groups = (rows + 63) / 64, tiles = (d_out + 31) / 32, most = 2048 / tiles;
+    const long long groups = (rows + 63) / 64, tiles = (d_out + 31) / 32;
+    // a wavefront has W's rows to bring first: 256, 512 and 2048 workgroups for 40 961 rows, 32 -> 64, float 14, 15 and 17 us, bf16 11, 9
+    // and 10
+    const long long most = (sizeof(T) == 4 ? 256 : 512) / tiles;
     const dim3 grid((unsigned)(groups < most ? groups : most), (unsigned)tiles);
     return by_activation(e.act, [&](auto a) {
         constexpr int ACT = decltype(a)::value;

@@ -85,101 +85,180 @@ __global__ __launch_bounds__(256) void normalise_kernel(const T *__restrict__ g,
 }
 
 // ---- small matrices --------------------------------------------------------------
-// All steps of a matrix in one workgroup, X, A and B as floats in LDS, on the float matrix instruction (its operands and sums are
-// single precision as they are).  X lies with its longer side as rows.  Bound by the chain of its products: 8 matrices of 96 x 32,
-// 5 steps: see below.
-// a product's eight instructions in two chains
-__device__ __forceinline__ void mma_two(f32x4 (&c)[2], const Frag<float>::type &a, const Frag<float>::type &b)
-{
-#pragma unroll
-    for (int e = 0; e < 8; ++e) c[e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c[e & 1], 0, 0, 0);
-}
-
+// All steps of a matrix in one workgroup, X, A and B in planes in LDS.  X lies with its longer side as rows, and results are turned
+// so that a lane writes four neighbours.  Bound by the chain of its products and barriers: 8 matrices of 96 x 32, 5 steps, 9.5 us,
+// 3.6 of them start, loads and stores (on the float instruction 14.3); 8 of 256 x 64, 30 us (75).
 template <class T, int D, int ROWS>
 __global__ __launch_bounds__(512) void orthogonal_small_kernel(const T *__restrict__ g, int rows, int cols, int steps, SmallSteps c,
-                                                               float eps, float scale, T *out)   // out may be g
+                                                               float eps, float scale, int whole, T *out)   // out may be g
 {
-    typedef Tile<float, D> L;
-    constexpr int N = D / 16, PARTS = 8 / (N * N) > 1 ? 8 / (N * N) : 1;   // A's sums over parts of the rows, so that all wavefronts work
-    __shared__ __align__(1024) char xs[ROWS * D * 4];
-    __shared__ __align__(1024) char as[PARTS][D * D * 4];
-    __shared__ __align__(1024) char bs[D * D * 4];
+    typedef Tile<__bf16, D> L;   // of any 16-bit values
+    constexpr int N = D / 16;
+    __shared__ __align__(1024) char xs[2][ROWS * D * 2];
+    __shared__ __align__(1024) char as[2][D * D * 2];
+    __shared__ __align__(1024) char bs[2][D * D * 2];
     __shared__ double sums[8];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = lane >> 4, l = lane & 15;
     const bool wide = rows < cols;
     const int hi = wide ? cols : rows, lo = wide ? rows : cols, blocks = (hi + 31) / 32 * 2;   // of 16 rows, whole chunks of 32 for A
     const T *src = g + (long long)blockIdx.x * rows * cols;
-    auto at = [](char *lds, int r, int k) -> float & { return *(float *)(lds + L::place(r, k >> 2) + (k & 3) * 4); };
+    auto place = [](int r, int k) { return L::place(r, k >> 3) + (k & 7) * 2; };
+    auto store = [&](char (*to)[D * D * 2], int r, int k, f32x4 v) {
+        f16x4 h, s;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            h[e] = (f16)v[e];
+            s[e] = (f16)(v[e] - (float)h[e]);
+        }
+        *(f16x4 *)(to[0] + place(r, k)) = h;
+        *(f16x4 *)(to[1] + place(r, k)) = s;
+    };
+    // a product of two planes each: the small ones in `low`
+    auto multiply = [](f32x4 &sum, f32x4 &low, const bf16x8(&a)[2], const bf16x8(&b)[2]) {
+        low = mfma_f16(a[1], b[0], low);
+        sum = mfma_f16(a[0], b[0], sum);
+        low = mfma_f16(a[0], b[1], low);
+    };
+    const f32x4 none = {0.f, 0.f, 0.f, 0.f};
+    // Pieces of eight neighbours in memory: of a row of X, or of a column of it where G is wide; X[r][k] is the first of them.
+    constexpr int ROW = D / 8, COLUMN = ROWS / 8;
+    const int limit = wide ? lo * COLUMN : blocks * 16 * ROW;
+    auto row_of = [&](int i) { return wide ? i % COLUMN * 8 : i / ROW; };
+    auto col_of = [&](int i) { return wide ? i / COLUMN : i % ROW * 8; };
+    auto left_of = [&](int i) { return wide ? hi - row_of(i) : row_of(i) < hi ? lo - col_of(i) : 0; };
+    auto index_of = [&](int i) { return wide ? col_of(i) * cols + row_of(i) : row_of(i) * cols + col_of(i); };
     double sum = 0.0;
-    for (int i = tid; i < blocks * 16 * D; i += 512) at(xs, i / D, i % D) = 0.f;
-    __syncthreads();
-    for (int i = tid; i < rows * cols; i += 512) {
-        const float v = (float)src[i];
-        const int r = i / cols, k = i - r * cols;
-        at(xs, wide ? k : r, wide ? r : k) = v;
-        sum += (double)v * v;
+    for (int i = tid; i < limit; i += 512) {
+        f32x4 v[2];
+        load_eight(src + index_of(i), left_of(i), whole, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = __builtin_fma((double)v[e >> 2][e & 3], (double)v[e >> 2][e & 3], sum);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
     if (lane == 0) sums[wave] = sum;
     __syncthreads();
     sum = ((sums[0] + sums[1]) + (sums[2] + sums[3])) + ((sums[4] + sums[5]) + (sums[6] + sums[7]));
-    const double inv = 1.0 / (sqrt(sum) + (double)eps);
-    for (int i = tid; i < rows * cols; i += 512) {
-        const int r = i / lo, k = i - r * lo;
-        at(xs, r, k) = (float)((double)at(xs, r, k) * inv);
+    const double inv = (double)SCALE_X / (sqrt(sum) + (double)eps);
+    const float factor = (float)inv;
+    const bool plain = inv > 1e-30 && inv < 1e30;   // neither it nor a value times it leaves a float's range
+    if (wide)   // what no piece below fills
+        for (int i = tid; i < blocks * 16 * ROW; i += 512)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) *(f16x8 *)(xs[u] + L::place(i / ROW, i % ROW)) = f16x8{};
+    __syncthreads();
+    for (int i = tid; i < limit; i += 512) {
+        const int r = row_of(i), k = col_of(i);
+        f32x4 v[2];
+        f16x8 h, q;
+        load_eight(src + index_of(i), left_of(i), whole, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = v[e >> 2][e & 3], y = plain ? x * factor : (float)((double)x * inv);
+            h[e] = (f16)y;
+            q[e] = (f16)(y - (float)h[e]);
+        }
+        if (!wide) {
+            *(f16x8 *)(xs[0] + place(r, k)) = h;
+            *(f16x8 *)(xs[1] + place(r, k)) = q;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (r + e < hi) {
+                    *(f16 *)(xs[0] + place(r + e, k)) = h[e];
+                    *(f16 *)(xs[1] + place(r + e, k)) = q[e];
+                }
+        }
     }
     for (int s = 0; s < steps; ++s) {
         __syncthreads();
-        for (int b = wave; b < N * N * PARTS; b += 8) {   // A[i][j]: sum over the rows of X
-            const int part = b / (N * N), i = b % (N * N) / N * 16, j = b % N * 16;
-            f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-            for (int r = part * 32; r < blocks * 16; r += 32 * PARTS) mma_two(acc, L::columns(xs, r, i, lane), L::columns(xs, r, j, lane));
-            acc[0] += acc[1];
+        for (int b = wave; b < N * N; b += 8) {   // A[i][j]: sum over the rows of X
+            const int i = b / N * 16, j = b % N * 16;
+            f32x4 acc = none, low = none;
+            for (int r = 0; r < blocks * 16; r += 32) {
+                bf16x8 x[2], y[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) at(as[part], i + 4 * grp + e, j + (lane & 15)) = acc[0][e];
+                for (int u = 0; u < 2; ++u) {
+                    x[u] = L::columns(xs[u], r, i, lane);
+                    y[u] = L::columns(xs[u], r, j, lane);
+                }
+                multiply(acc, low, x, y);
+            }
+            store(as, j + l, i + 4 * grp, (acc + low) * (SCALE_A / (SCALE_X * SCALE_X)));
         }
         __syncthreads();
+        const float square = SCALE_B * c.c[s][2] / (SCALE_A * SCALE_A), linear = SCALE_B * c.c[s][1] / SCALE_A;
         for (int b = wave; b < N * N; b += 8) {   // B = a + b A + c A A
             const int i = b / N * 16, j = b % N * 16;
-            auto rows_of_a = [&](int r, int k) {
-                Frag<float>::type f = L::rows(as[0], r, k, lane);
-                if (PARTS > 1) f += L::rows(as[PARTS - 1], r, k, lane);
-                return f;
-            };
-            f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+            f32x4 acc = none, low = none;
 #pragma unroll
-            for (int k = 0; k < D / 32; ++k) mma_two(acc, rows_of_a(i, k), rows_of_a(j, k));
-            acc[0] += acc[1];
+            for (int k = 0; k < D / 32; ++k) {
+                bf16x8 x[2], y[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int m = i + 4 * grp + e, n = j + (lane & 15);
-                const float one = PARTS > 1 ? at(as[0], m, n) + at(as[PARTS - 1], m, n) : at(as[0], m, n);
-                at(bs, m, n) = c.c[s][2] * acc[0][e] + c.c[s][1] * one + (m == n ? c.c[s][0] : 0.f);
+                for (int u = 0; u < 2; ++u) {
+                    x[u] = L::rows(as[u], i, k, lane);
+                    y[u] = L::rows(as[u], j, k, lane);
+                }
+                multiply(acc, low, x, y);
             }
+            const int n = j + l, m = i + 4 * grp;
+            const f16x4 h = *(const f16x4 *)(as[0] + place(n, m)), q = *(const f16x4 *)(as[1] + place(n, m));
+            f32x4 v = (acc + low) * square;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += linear * ((float)h[e] + (float)q[e]) + (m + e == n ? SCALE_B * c.c[s][0] : 0.f);
+            store(bs, n, m, v);
         }
         __syncthreads();
         for (int b = wave; b < blocks; b += 8) {   // X <- X B, 16 rows of a wavefront's own
-            f32x4 acc[N];
+            f32x4 acc[N], low[N];
 #pragma unroll
-            for (int j = 0; j < N; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < N; ++j) acc[j] = low[j] = none;
 #pragma unroll
             for (int k = 0; k < D / 32; ++k) {
-                const Frag<float>::type x = L::rows(xs, b * 16, k, lane);
+                bf16x8 x[2], y[2];
 #pragma unroll
-                for (int j = 0; j < N; ++j) mma(acc[j], x, L::rows(bs, j * 16, k, lane));
+                for (int u = 0; u < 2; ++u) x[u] = L::rows(xs[u], b * 16, k, lane);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) y[u] = L::rows(bs[u], j * 16, k, lane);
+                    multiply(acc[j], low[j], y, x);
+                }
             }
 #pragma unroll
-            for (int j = 0; j < N; ++j)
+            for (int j = 0; j < N; ++j) {
+                const f32x4 v = (acc[j] + low[j]) * (1.f / SCALE_B);
+                f16x4 h, q;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) at(xs, b * 16 + 4 * grp + e, j * 16 + (lane & 15)) = acc[j][e];
+                for (int e = 0; e < 4; ++e) {
+                    h[e] = (f16)v[e];
+                    q[e] = (f16)(v[e] - (float)h[e]);
+                }
+                *(f16x4 *)(xs[0] + place(b * 16 + l, j * 16 + 4 * grp)) = h;
+                *(f16x4 *)(xs[1] + place(b * 16 + l, j * 16 + 4 * grp)) = q;
+            }
         }
     }
     __syncthreads();
     T *dst = out + (long long)blockIdx.x * rows * cols;
-    for (int i = tid; i < rows * cols; i += 512) {
-        const int r = i / cols, k = i - r * cols;
-        dst[i] = (T)(at(xs, wide ? k : r, wide ? r : k) * scale);
+    for (int i = tid; i < limit; i += 512) {
+        const int r = row_of(i), k = col_of(i);
+        f16x8 h, q;
+        if (!wide) {
+            h = *(const f16x8 *)(xs[0] + place(r, k));
+            q = *(const f16x8 *)(xs[1] + place(r, k));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (r + e < hi) {
+                    h[e] = *(const f16 *)(xs[0] + place(r + e, k));
+                    q[e] = *(const f16 *)(xs[1] + place(r + e, k));
+                }
+        }
+        f32x4 v[2];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e >> 2][e & 3] = ((float)h[e] + (float)q[e]) * (scale / SCALE_X);
+        store_eight(dst + index_of(i), v, left_of(i), whole);
     }
 }
 
@@ -236,13 +315,13 @@ static lcn_status small_as(const T *g, int64_t count, int32_t rows, int32_t cols
     SmallSteps k{};
     for (int i = 0; i < steps; ++i)
         for (int e = 0; e < 3; ++e) k.c[i][e] = c[3 * i + e];
-    const int32_t lo = rows < cols ? rows : cols;
+    const int32_t lo = rows < cols ? rows : cols, whole = whole_rows<T>((const void *)((uintptr_t)g | (uintptr_t)out), cols);
     if (lo <= 32)
         hipLaunchKernelGGL((orthogonal_small_kernel<T, 32, 512>), dim3((unsigned)count), dim3(512), 0, s, g, rows, cols, steps, k, eps,
-                           scale, out);
+                           scale, whole, out);
     else
         hipLaunchKernelGGL((orthogonal_small_kernel<T, 64, 256>), dim3((unsigned)count), dim3(512), 0, s, g, rows, cols, steps, k, eps,
-                           scale, out);
+                           scale, whole, out);
     OPCHK(hipGetLastError());
     return LCN_OK;
 }

@@ -42,11 +42,10 @@ struct Count {
     static constexpr int value = N;
 };
 
-typedef f16 f16x4 __attribute__((ext_vector_type(4)));
-
+template <bool SYM>   // false: of few tiles all are computed, which costs no time and saves writing twice
 struct GramEpilogue {
     typedef GramArgs Args;
-    static constexpr bool SYMMETRIC = true;
+    static constexpr bool SYMMETRIC = SYM, ROWS = false;   // ROWS: goes through LDS row by row
     // What the result needs of `gram`, requested before the product where there is room for it
     template <int TM, int TN>
     struct Early {
@@ -112,7 +111,7 @@ struct GramEpilogue {
                     *(f16x4 *)(hi + at) = x;
                     *(f16x4 *)(lo + at) = y;
                 }
-                if (mirror && n < ld) {   // also zeros behind the rows' ends
+                if (SYM && mirror && n < ld) {   // also zeros behind the rows' ends
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
                         if (m + u < p.m) {
@@ -127,7 +126,7 @@ struct GramEpilogue {
 
 struct ApplyEpilogue {
     typedef ApplyArgs Args;
-    static constexpr bool SYMMETRIC = false;
+    static constexpr bool SYMMETRIC = false, ROWS = true;
     template <int TM, int TN>
     struct Early {};
     template <int TM, int TN>
@@ -156,7 +155,7 @@ struct ApplyEpilogue {
 template <class T>
 struct LastEpilogue {
     typedef LastArgs Args;
-    static constexpr bool SYMMETRIC = false;
+    static constexpr bool SYMMETRIC = false, ROWS = true;
     template <int TM, int TN>
     struct Early {};
     template <int TM, int TN>
@@ -188,7 +187,7 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN == 4 ? 1 : BM == 128 ? 4 : 2) v
 {
     constexpr int THREADS = WM * WN * 64, TM = BM / WM / 16, TN = BN / WN / 16;
     constexpr int ABYTES = BM * BK * 2, BBYTES = BN * BK * 2, STAGE = PA * ABYTES + PB * BBYTES;
-    constexpr int ROWS = Epi::SYMMETRIC ? 0 : WM * WN * RowRegion<TM>::BYTES;
+    constexpr int ROWS = Epi::ROWS ? WM * WN * RowRegion<TM>::BYTES : 0;
     typedef TileLoader<BM, BK, ACOL, THREADS> LoadA;
     typedef TileLoader<BN, BK, BCOL, THREADS> LoadB;
     static_assert(LoadA::PIECES % THREADS == 0 && LoadB::PIECES % THREADS == 0, "a wavefront's loads of a tile are counted");
@@ -340,7 +339,7 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN == 4 ? 1 : BM == 128 ? 4 : 2) v
         return;
     }
     __syncthreads();
-    Epi::template run<TM, TN>(e, p, acc, wanted, m0 + wm, n0 + wn, batch, tm != tn, lds0 + (Epi::SYMMETRIC ? 0 : wave * RowRegion<TM>::BYTES));
+    Epi::template run<TM, TN>(e, p, acc, wanted, m0 + wm, n0 + wn, batch, tm != tn, lds0 + (Epi::ROWS ? wave * RowRegion<TM>::BYTES : 0));
 }
 
 // adds up the partial sums of a symmetric product, tile by tile in the order that pair_kernel left them
@@ -363,9 +362,10 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void pair_join_kernel(PairArgs p, G
         for (int i = 0; i < TM; ++i) acc[i][0] += from[(i * TN + j) * THREADS + tid];
     }
     const int m0 = tm * BM + (wave % WM) * (BM / WM), n0 = tn * BN + (wave / WM) * (BN / WN) + j * 16;
-    GramEpilogue::Early<TM, 1> wanted{};
-    GramEpilogue::early<TM, 1>(e, p, wanted, m0, n0, batch);
-    GramEpilogue::run<TM, 1>(e, p, acc, wanted, m0, n0, batch, tm != tn, nullptr);
+    typedef GramEpilogue<true> Epi;
+    Epi::Early<TM, 1> wanted{};
+    Epi::early<TM, 1>(e, p, wanted, m0, n0, batch);
+    Epi::run<TM, 1>(e, p, acc, wanted, m0, n0, batch, tm != tn, nullptr);
 }
 
 // ---- host ---------------------------------------------------------------------
@@ -427,16 +427,24 @@ static hipError_t launch_tile(const PairPlan &plan, const PairArgs &p, const typ
     return plan.shape == PAIR_128 ? launch_pair<128, 32, 2, 4, 2, ACOL, BCOL, PA, PB, LOW, Epi>(plan, p, e, s)
                                   : launch_pair<64, 64, 2, 2, 4, ACOL, BCOL, PA, PB, LOW, Epi>(plan, p, e, s);
 }
+template <bool ACOL, bool BCOL, int PA, int PB, bool LOW>
+static hipError_t launch_symmetric(const PairPlan &plan, const PairArgs &p, const GramArgs &e, hipStream_t s)
+{
+    const long long t = (p.n + 63) / 64;
+    if (plan.shape == PAIR_64 && plan.splits == 1 && t * t * p.batches <= 256)
+        return launch_pair<64, 64, 2, 2, 4, ACOL, BCOL, PA, PB, LOW, GramEpilogue<false>>(plan, p, e, s);
+    return launch_tile<ACOL, BCOL, PA, PB, LOW, GramEpilogue<true>>(plan, p, e, s);
+}
 
 hipError_t launch_gram(const PairPlan &plan, const PairArgs &p, const GramArgs &e, bool wide, int planes, hipStream_t s)
 {
     if (wide)
-        return planes == PAIR_ONE   ? launch_tile<false, false, 1, 1, false, GramEpilogue>(plan, p, e, s)
-               : planes == PAIR_TWO ? launch_tile<false, false, 2, 2, false, GramEpilogue>(plan, p, e, s)
-                                    : launch_tile<false, false, 2, 2, true, GramEpilogue>(plan, p, e, s);
-    return planes == PAIR_ONE   ? launch_tile<true, true, 1, 1, false, GramEpilogue>(plan, p, e, s)
-           : planes == PAIR_TWO ? launch_tile<true, true, 2, 2, false, GramEpilogue>(plan, p, e, s)
-                                : launch_tile<true, true, 2, 2, true, GramEpilogue>(plan, p, e, s);
+        return planes == PAIR_ONE   ? launch_symmetric<false, false, 1, 1, false>(plan, p, e, s)
+               : planes == PAIR_TWO ? launch_symmetric<false, false, 2, 2, false>(plan, p, e, s)
+                                    : launch_symmetric<false, false, 2, 2, true>(plan, p, e, s);
+    return planes == PAIR_ONE   ? launch_symmetric<true, true, 1, 1, false>(plan, p, e, s)
+           : planes == PAIR_TWO ? launch_symmetric<true, true, 2, 2, false>(plan, p, e, s)
+                                : launch_symmetric<true, true, 2, 2, true>(plan, p, e, s);
 }
 
 template <bool ACOL, bool BCOL, int PA, int PB, class Epi>

@@ -10,6 +10,7 @@ namespace lcn {
 
 typedef _Float16 f16;
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
+typedef f16 f16x4 __attribute__((ext_vector_type(4)));
 
 // the same for a register's bits as fp16
 __device__ __forceinline__ f32x4 mfma_f16(bf16x8 a, bf16x8 b, f32x4 c)
