@@ -243,8 +243,9 @@ static bool gated_args_fit(int64_t rows, int32_t d_in, int32_t d_out, int32_t dt
            sizes_fit(rows, d_in) && sizes_fit(rows, 2 * (int64_t)d_out) && (dtype == LCN_F32 || dtype == LCN_BF16);
 }
 
-// A product by large tiles and, where columns behind the last whole one get small tiles (plan_product), these as a product of their
-// own, whose k may be split: 7 columns behind 16384, k = 8192: 64 us in one piece of k, 16 in 16.
+// A product in two launches where that is estimated to be faster: whole rounds of workgroups of one shape, and the columns behind
+// them by another, whose k may be split.  20 000 float rows: 1024 -> 300, 111 us by 64 x 64 tiles in three rounds, 105 as one round of
+// 320 x 64 and the rest; 16391 bf16 rows, 8192 -> 1024: the 7 rows behind 16384 took 64 us in one piece of k, 12 in 32.
 struct Columns {
     ProductPlan main, rest;
     long long whole, n;
@@ -253,12 +254,24 @@ struct Columns {
 static Columns plan_columns(Carver &c, long long m, long long n, long long k, int planes, bool may_320)
 {
     Columns r{};
-    r.main = plan_product(m, n, k, planes, true, true, may_320);
+    r.main = plan_product(m, n, k, planes, true, false, may_320);
     r.n = r.whole = n;
-    if (r.main.tail) {
-        r.main.tail = false;
-        r.whole = n - n % tile_n(r.main.tile, planes);
-        r.rest = plan_product(m, n - r.whole, k, planes, true, false, may_320);
+    double least = r.main.us;
+    for (int t = 0; t < TILE_COUNT; ++t) {
+        if (t == TILE_320 && !may_320) continue;
+        const long long across = (m + tile_m(t) - 1) / tile_m(t), round = product_room(t, planes) / across * tile_n(t, planes);
+        const long long tiles = n - n % tile_n(t, planes);   // whole tiles, and whole rounds of them
+        for (long long whole : {tiles, round > 0 ? n - n % round : 0}) {
+            if (whole <= 0 || whole >= n) continue;
+            const ProductPlan rest = plan_product(m, n - whole, k, planes, true, false, may_320);
+            const double us = product_us(t, m, whole, k, planes, 1) + 3.0 + rest.us;
+            if (us < least) {
+                least = us;
+                r.main = ProductPlan{t, 1, false, us};
+                r.rest = rest;
+                r.whole = whole;
+            }
+        }
     }
     r.part = (float *)c.take(partial_bytes(r.main, m, r.whole));
     r.part_rest = r.whole < n ? (float *)c.take(partial_bytes(r.rest, m, n - r.whole)) : nullptr;

@@ -106,49 +106,58 @@ hipError_t launch_add_partials(const float *part, int splits, long long n, int m
     return hipGetLastError();
 }
 
-// The tile shape and the split with the least estimated time.  A workgroup's step costs its tile's area at the rate
+struct Shape {
+    int resident;
+    double step_us;   // of one workgroup's step with the chip full: 64 values of k, or 32 in three planes
+};
+static const Shape &shape_of(int tile, int planes)
+{
+    static const Shape one[TILE_COUNT] = {{1, 1.8}, {2, 1.03}, {4, 0.77}, {1, 1.25}};
+    static const Shape three[TILE_COUNT] = {{1, 2.3}, {1, 1.85}, {3, 1.2}, {1, 1.81}};
+    return (planes == 3 ? three : one)[tile];
+}
+long long product_room(int tile, int planes) { return 256LL * shape_of(tile, planes).resident; }
+static long long product_steps(long long k, int planes) { return planes == 3 ? (k + 31) / 32 : (k + 63) / 64 * planes; }
+
+// The estimated time of a launch.  A workgroup's step costs its tile's area at the rate
 // that the shape reaches on large products (bf16: 256 x 256 1.25 PFLOP/s, 128 x 128 1.1, 64 x 64 0.7; three planes, six
 // products counted: 256 x 128 1.4, 320 x 64 1.1, 128 x 128 0.87, 64 x 64 1.0); two steps stand for a workgroup's start and epilogue,
 // three where these are 256 x 128 in three planes; the chip takes 256 workgroups of the large shapes at a
-// time and several times as many small ones; the partial sums of a split are written and read once at the rate of memory.
+// time and several times as many small ones.
+double product_us(int tile, long long m, long long columns, long long k, int planes, int splits)
+{
+    const Shape &shape = shape_of(tile, planes);
+    const long long steps = product_steps(k, planes);
+    const int bm = tile_m(tile), bn = tile_n(tile, planes);
+    const long long groups = ((m + bm - 1) / bm) * ((columns + bn - 1) / bn) * splits, room = 256 * shape.resident;
+    const double rounds = (double)((groups + room - 1) / room);
+    double us = rounds * shape.step_us * ((double)((steps + splits - 1) / splits) + (planes == 3 && tile == TILE_256 ? 3.0 : 2.0));
+    if (groups < room) {   // fewer to share a compute unit with
+        const double share = (double)((groups + 255) / 256) / shape.resident;
+        us *= share > 0.5 ? share : 0.5 + 0.5 * share;
+    }
+    return us;
+}
+
+// The tile shape and the split with the least estimated time; the partial sums of a split are written and read once at the rate of
+// memory.
 //
 // Columns behind the last whole tile cost a tile's time, and often a round of them: where that is estimated to be more than
 // 3 us and a launch of 64 x 64 tiles, they get that (a bf16 training step of 16391 rows, 1024 to 4096: 711 us, else 784).
 ProductPlan plan_product(long long m, long long n, long long k, int planes, bool may_split, bool may_tail, bool may_320)
 {
-    struct Shape {
-        int resident;
-        double step_us;   // of one workgroup's step with the chip full: 64 values of k, or 32 in three planes
-    };
-    static const Shape one[TILE_COUNT] = {{1, 1.8}, {2, 1.03}, {4, 0.77}, {1, 1.25}};
-    static const Shape three[TILE_COUNT] = {{1, 2.3}, {1, 1.85}, {3, 1.2}, {1, 1.81}};
-    const Shape *shape = planes == 3 ? three : one;
-    const long long steps = planes == 3 ? (k + 31) / 32 : (k + 63) / 64 * planes;
-    auto launch_us = [&](int t, long long columns, int splits) {
-        const int bm = tile_m(t), bn = tile_n(t, planes);
-        const long long groups = ((m + bm - 1) / bm) * ((columns + bn - 1) / bn) * splits, room = 256 * shape[t].resident;
-        const double rounds = (double)((groups + room - 1) / room);
-        double us = rounds * shape[t].step_us * ((double)((steps + splits - 1) / splits) + (planes == 3 && t == TILE_256 ? 3.0 : 2.0));
-        if (groups < room) {   // fewer to share a compute unit with
-            const double share = (double)((groups + 255) / 256) / shape[t].resident;
-            us *= share > 0.5 ? share : 0.5 + 0.5 * share;
-        }
-        return us;
-    };
-    ProductPlan best{TILE_256, 1, false};
-    double least = 1e300;
+    const long long steps = product_steps(k, planes);
+    ProductPlan best{TILE_256, 1, false, 1e300};
     for (int t = 0; t < TILE_COUNT; ++t) {
         if (t == TILE_320 && !may_320) continue;
         const long long rest = n % tile_n(t, planes);
         for (int splits = 1; splits <= 64; splits += splits < 16 ? 1 : 16) {
             if (splits > 1 && (!may_split || steps / splits < 4)) break;
             for (int tail = 0; tail <= (may_tail && t != TILE_64 && rest && n > rest ? 1 : 0); ++tail) {
-                double us = tail ? launch_us(t, n - rest, splits) + 3.0 + launch_us(TILE_64, rest, splits) : launch_us(t, n, splits);
+                double us = tail ? product_us(t, m, n - rest, k, planes, splits) + 3.0 + product_us(TILE_64, m, rest, k, planes, splits)
+                                 : product_us(t, m, n, k, planes, splits);
                 if (splits > 1) us += 3.0 + (double)splits * m * n * 8e-6 / 4.0;
-                if (us < least) {
-                    least = us;
-                    best = ProductPlan{t, splits, tail != 0};
-                }
+                if (us < best.us) best = ProductPlan{t, splits, tail != 0, us};
             }
         }
     }

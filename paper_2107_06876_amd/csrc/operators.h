@@ -227,7 +227,11 @@ struct ProductPlan {
     int tile;      // index of the tile shape, see launch_planned
     int splits;
     bool tail;     // columns behind the last whole tile: by small tiles, in a launch of their own
+    double us;     // estimated
 };
+// workgroups of a tile shape that are on the chip at a time; the estimated time of a launch without partial sums' way
+long long product_room(int tile, int planes);
+double product_us(int tile, long long m, long long columns, long long k, int planes, int splits);
 ProductPlan plan_product(long long m, long long n, long long k, int planes, bool may_split, bool may_tail, bool may_320 = true);
 
 // A float product's partial sums: [split][n][ldp]; `add` adds to what is there.
