@@ -516,7 +516,7 @@ lcn_status lcn_gated_linear_backward(const void *x, const void *W, const void *k
  *   y = (x - mean) rstd weight + bias,  rstd = 1 / sqrt(mean of (x - mean)^2 + eps).
  * weight, bias (dim, of type dtype) are nullable (1 and 0); mean, rstd (fp32, rows;
  * nullable): what the backward pass takes.  y may be x.  A row that holds a value that is not
- * finite becomes NaN.  Sizes: 0 <= rows <= 2^30, 1 <= dim <= 2^20, their product <= 2^42; eps
+ * finite becomes NaN; where squares leave a float's range (differences from 1e19 on) rstd is 0.  Sizes: 0 <= rows <= 2^30, 1 <= dim <= 2^20, their product <= 2^42; eps
  * finite and >= 0 (0: rows of equal values become NaN).  No workspace. */
 lcn_status lcn_layer_norm(const void *x, const void *weight, const void *bias, int64_t rows, int32_t dim, int32_t dtype, float eps,
                           void *y, float *mean, float *rstd, void *hip_stream);
@@ -541,7 +541,8 @@ lcn_status lcn_layer_norm_backward(const void *x, const void *weight, const floa
  * value that is not finite makes its whole result NaN, and so does G = 0 with eps = 0.  out may be g.
  * LCN_ERR_INVALID_ARG for coefficients that let singular values in 0 .. 1 grow beyond 4, or a + b s^2 + c s^4 beyond
  * 64, in any step.  Sizes: 0 <= count <= 2^20, 1 <= rows, cols <= 2^20, the smaller of them <= 32768, count * rows *
- * cols <= 2^40; 1 <= steps <= 64; eps >= 0 and scale finite. */
+ * cols <= 2^40, fewer than 2^31 tiles of 64 x 64; 1 <= steps <= 64; eps >= 0 and scale finite.  Matrices of up to
+ * 32 x 512 or 64 x 256 values, either way round, need no workspace (the call says 0 bytes). */
 lcn_status lcn_orthogonalise_workspace_bytes(int64_t count, int32_t rows, int32_t cols, int32_t dtype, size_t *bytes);
 lcn_status lcn_orthogonalise(const void *g, int64_t count, int32_t rows, int32_t cols, int32_t dtype, int32_t steps,
                              const float *coefficients, float eps, float scale, void *out, void *workspace, size_t workspace_bytes,

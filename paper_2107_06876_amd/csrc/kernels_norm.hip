@@ -57,13 +57,17 @@ __global__ __launch_bounds__(256) void norm_kernel(const T *x, const T *__restri
 #pragma unroll
         for (int e = 0; e < V; ++e) sum += (float)p[c][e];
     const float mean = sum_over<L>(sum, lds[0]) / (float)dim;
-    float square = 0.f;
+    float square = 0.f;   // of differences over sqrt(dim): the sum leaves a float's range where the variance does, not before
+    const float share = 1.f / sqrtf((float)dim);
 #pragma unroll
     for (int c = 0; c < C; ++c)
         if (c * L + lane < units)
 #pragma unroll
-            for (int e = 0; e < V; ++e) square += ((float)p[c][e] - mean) * ((float)p[c][e] - mean);
-    const float rstd = 1.f / sqrtf(sum_over<L>(square, lds[1]) / (float)dim + eps);
+            for (int e = 0; e < V; ++e) {
+                const float d = ((float)p[c][e] - mean) * share;
+                square += d * d;
+            }
+    const float rstd = 1.f / sqrtf(sum_over<L>(square, lds[1]) + eps);
     if (!here) return;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -243,13 +247,17 @@ __global__ __launch_bounds__(256) void norm_long_kernel(const T *x, const T *__r
     sum_over_group(sum, none, lds);
     const float mean = sum / (float)dim;
     float square = 0.f;
+    const float share = 1.f / sqrtf((float)dim);
     for (int u = threadIdx.x; u < units; u += 256) {
         const piece p = row[u];
 #pragma unroll
-        for (int e = 0; e < V; ++e) square += ((float)p[e] - mean) * ((float)p[e] - mean);
+        for (int e = 0; e < V; ++e) {
+            const float d = ((float)p[e] - mean) * share;
+            square += d * d;
+        }
     }
     sum_over_group(square, none, lds);
-    const float rstd = 1.f / sqrtf(square / (float)dim + eps);
+    const float rstd = 1.f / sqrtf(square + eps);
     for (int u = threadIdx.x; u < units; u += 256) {
         const piece p = row[u];
         piece o, pw, pb;

@@ -268,7 +268,9 @@ static bool orthogonal_args_fit(int64_t count, int32_t rows, int32_t cols, int32
 {
     const int32_t lo = rows < cols ? rows : cols;
     return count >= 0 && count <= (1 << 20) && rows >= 1 && cols >= 1 && rows <= MAX_WIDTH && cols <= MAX_WIDTH && lo <= 32768 &&
-           (double)count * rows * cols <= (double)((int64_t)1 << 40) && (dtype == LCN_F32 || dtype == LCN_BF16);
+           (double)count * rows * cols <= (double)((int64_t)1 << 40) &&
+           count * ((rows + 63) / 64) * ((cols + 63) / 64) < (int64_t)1 << 31 &&   // a product's tiles are numbered in 31 bits
+           (dtype == LCN_F32 || dtype == LCN_BF16);
 }
 
 // Whether every step keeps the singular values, which start at 1 or less, within the bounds of orthogonal.h; poly: the largest

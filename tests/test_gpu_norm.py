@@ -155,6 +155,31 @@ def test_in_place(dim, dtype):
     assert lcn.lcn_layer_norm(x, w, b, out=x) is x and torch.equal(x, want)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,dim", [(45, 32), (2100, 300), (45, 301), (3000, 2048), (33, 9000)])
+def test_dx_in_place_of_the_gradient_around(rows, dim, dtype):
+    """dx may be the memory of `around` (the C entry point; the binding's dx is new)."""
+    from paper_2107_06876_amd import encoder
+    x, w, b, dy, around = inputs(rows, dim, dtype)
+    _, mean, rstd = lcn.lcn_layer_norm(x, w, b, keep_stats=True)
+    want, dw, db = lcn.lcn_layer_norm_backward(x, w, mean, rstd, dy, around=around)
+    sizes = (rows, dim, 0 if dtype == F32 else 1)
+    space = torch.empty(encoder._bytes("lcn_layer_norm_workspace_bytes", sizes), dtype=torch.uint8, device=DEV)
+    got = torch.empty(2, dim, dtype=dtype, device=DEV)
+    encoder._call("lcn_layer_norm_backward", x.device, x.data_ptr(), w.data_ptr(), mean.data_ptr(), rstd.data_ptr(), dy.data_ptr(),
+                  around.data_ptr(), *sizes, around.data_ptr(), got[0].data_ptr(), got[1].data_ptr(), space.data_ptr(), space.numel())
+    assert torch.equal(around, want) and torch.equal(got[0], dw) and torch.equal(got[1], db)
+
+
+def test_values_of_every_size():
+    """A row's size drops out, up to eps on one side and the range of squares on the other."""
+    x, w, b, _, _ = inputs(40, 300, F32)
+    want = lcn.lcn_layer_norm(x, w, b, eps=0.0)
+    for size in (1e-15, 1e-6, 1e6, 1e18):
+        assert off(lcn.lcn_layer_norm(x * size, w, b, eps=0.0), want) <= 4 * bound(F32, 300)
+    assert off(lcn.lcn_layer_norm(x * 1e25, w, b), b.expand(40, 300)) == 0.0
+
+
 @pytest.mark.parametrize("dim", [64, 300, 4096])
 def test_roundings_of_bf16(dim):
     x, w, b, dy, around = inputs(2000, dim, BF16)

@@ -143,7 +143,8 @@ UPDATE = _triples(*(3.4445, -4.7750, 2.0315) * 5)
 
 @pytest.mark.parametrize("count,rows,cols,dtype", [
     (-1, 4, 4, F32), (1, 0, 4, F32), (1, 4, 0, F32), (1, 4, 4, 7), ((1 << 20) + 1, 4, 4, F32), (1, (1 << 20) + 1, 4, F32),
-    (1, 4, (1 << 20) + 1, F32), (1, 32769, 32769, BF16), (1 << 20, 1 << 10, (1 << 10) + 1, BF16)])
+    (1, 4, (1 << 20) + 1, F32), (1, 32769, 32769, BF16), (1 << 20, 1 << 10, (1 << 10) + 1, BF16),
+    (1 << 20, 1, 1 << 17, BF16)])
 def test_orthogonal_sizes_out_of_range(lib, count, rows, cols, dtype):
     assert _bytes(lib.lcn_orthogonalise_workspace_bytes, count, rows, cols, dtype)[0] == ERR_INVALID_ARG
     assert lib.lcn_orthogonalise(FAKE, count, rows, cols, dtype, 5, UPDATE, 1e-7, 1.0, FAKE, FAKE, 1 << 62, None) == ERR_INVALID_ARG
