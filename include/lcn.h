@@ -363,8 +363,9 @@ lcn_status lcn_calibrate(int32_t what, void *workspace, size_t workspace_bytes, 
 
 /* ---- operators that produce and train the points ---------------------------
  * Layers and a loss for the model behind X and Y: a matrix product with its
- * epilogue, attention inside the sets of a ragged batch, and softmax cross
- * entropy against a large vocabulary of points.  They need no handle.
+ * epilogue, attention inside the sets of a ragged batch, layer norm, a gated
+ * layer, and softmax cross entropy against a large vocabulary of points; and
+ * orthogonal updates of its weights.  They need no handle.
  *
  *   - Tensors are device memory, row-major and dense unless a stride is named,
  *     of type `dtype` where no other is; any alignment that the type has (with
@@ -375,8 +376,8 @@ lcn_status lcn_calibrate(int32_t what, void *workspace, size_t workspace_bytes, 
  *     once from them.  With bf16 tensors these are rounded to bf16 as well, where
  *     they enter a matrix product: the weights P of lcn_attention (in o and dv)
  *     and its dS (in dq and dk); above 512 rows dz of lcn_linear_backward where
- *     there is an activation and of lcn_gated_linear_backward (in dx and dW), and the cross entropy's G (in dW, and
- *     in dx but for the target's part).  Each is as large as the output's own
+ *     there is an activation and of lcn_gated_linear_backward (in dx and dW), and
+ *     the cross entropy's G (in dW, and in dx but for the target's part).  Each is as large as the output's own
  *     rounding: the error becomes 1.4 times that of one.  Where a tile of 64 or 128
  *     queries sees more than 256 keys, o enters dS as it was rounded, a third such
  *     error in rows whose weight lies on few keys.  Scores with a
