@@ -6,7 +6,7 @@
 // Every product is one of two planes of fp16 (product.h): the singular values are bounded by the polynomials, and with them every
 // value of X, A and B, so that powers of two in front keep them in fp16's range.  Planes and sums are as exact as single precision,
 // which is needed: what rounding adds in the first steps grows as the smallest singular values do, up to a per step.  bf16 matrices
-// are one plane in the first step, exactly.
+// are one plane in the first step.
 //
 // Long bf16 matrices take several steps on A alone, which is small: with B_1, B_2, ... as they come, A <- A B^2 and X <- B_r .. B_1 X
 // at the end of such a stage.  A then has to tell sigma^2 from the largest one's rounding, 2^-24, where X tells sigma: a stage's
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256) void squares_kernel(const T *__restrict__ g, l
 }
 
 // Matrix blockIdx.y.  float: SCALE_X G / (|G| + eps) in two planes.  bf16: G times the power of two that brings |G| to between
-// SCALE_X / 2 and SCALE_X, in one plane, which holds it exactly, and what is left of the factor in `ratio`.
+// SCALE_X / 2 and SCALE_X, in one plane, which holds it (values below 2^-30 |G| to 2^-38 |G|), and what is left of the factor in `ratio`.
 template <class T>
 __global__ __launch_bounds__(256) void normalise_kernel(const T *__restrict__ g, const double *__restrict__ part, int rows, int cols,
                                                         float eps, int whole, Planes out, float *__restrict__ ratio)

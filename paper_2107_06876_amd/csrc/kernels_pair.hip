@@ -6,6 +6,8 @@
 // four buffers, fragments ahead in registers and other orders of k were no faster, 64 x 64 tiles 34 to 38).
 // 64 x 64 tiles, 64 values of k at a time in four buffers: products of few tiles, where what counts is the way from memory
 // (1024^3: 13 us; as 128 x 128 25, with 32 values of k at a time 17).
+// 32 x 32 tiles, the same: of even fewer, where what counts is what a workgroup has to bring (300^3: 4.9 us, as 64 x 64 7.0, with 128
+// values of k at a time 4.8; 896^3, symmetric: 11, as 64 x 64 10).
 #include "orthogonal.h"
 
 namespace lcn {
@@ -375,8 +377,8 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void pair_join_kernel(PairArgs p, G
 // The largest tile has no room for sums of a float's precision.
 PairPlan plan_pair(long long m, long long n, long long k, long long batches, bool symmetric, bool bf16)
 {
-    static const int resident[PAIR_SHAPES] = {1, 2, 1};
-    static const double alone_us[PAIR_SHAPES] = {2.4, 0.85, 0.32}, full_us[PAIR_SHAPES] = {2.6, 1.35, 0.37};
+    static const int resident[PAIR_SHAPES] = {1, 2, 1, 2};
+    static const double alone_us[PAIR_SHAPES] = {2.4, 0.85, 0.32, 0.2}, full_us[PAIR_SHAPES] = {2.6, 1.35, 0.37, 0.25};
     PairPlan best{PAIR_64, 1};
     double least = 1e300;
     for (int t = bf16 ? 0 : 1; t < PAIR_SHAPES; ++t) {
@@ -424,15 +426,17 @@ static hipError_t launch_tile(const PairPlan &plan, const PairArgs &p, const typ
 {
     if constexpr (!LOW)
         if (plan.shape == PAIR_256) return launch_pair<256, 32, 2, 4, 2, ACOL, BCOL, PA, PB, LOW, Epi>(plan, p, e, s);
-    return plan.shape == PAIR_128 ? launch_pair<128, 32, 2, 4, 2, ACOL, BCOL, PA, PB, LOW, Epi>(plan, p, e, s)
-                                  : launch_pair<64, 64, 2, 2, 4, ACOL, BCOL, PA, PB, LOW, Epi>(plan, p, e, s);
+    return plan.shape == PAIR_128  ? launch_pair<128, 32, 2, 4, 2, ACOL, BCOL, PA, PB, LOW, Epi>(plan, p, e, s)
+           : plan.shape == PAIR_64 ? launch_pair<64, 64, 2, 2, 4, ACOL, BCOL, PA, PB, LOW, Epi>(plan, p, e, s)
+                                   : launch_pair<32, 64, 2, 2, 4, ACOL, BCOL, PA, PB, LOW, Epi>(plan, p, e, s);
 }
 template <bool ACOL, bool BCOL, int PA, int PB, bool LOW>
 static hipError_t launch_symmetric(const PairPlan &plan, const PairArgs &p, const GramArgs &e, hipStream_t s)
 {
-    const long long t = (p.n + 63) / 64;
-    if (plan.shape == PAIR_64 && plan.splits == 1 && t * t * p.batches <= 256)
-        return launch_pair<64, 64, 2, 2, 4, ACOL, BCOL, PA, PB, LOW, GramEpilogue<false>>(plan, p, e, s);
+    const long long w = pair_tile_of(plan.shape), t = (p.n + w - 1) / w;
+    if (plan.shape >= PAIR_64 && plan.splits == 1 && t * t * p.batches <= 256)
+        return plan.shape == PAIR_64 ? launch_pair<64, 64, 2, 2, 4, ACOL, BCOL, PA, PB, LOW, GramEpilogue<false>>(plan, p, e, s)
+                                     : launch_pair<32, 64, 2, 2, 4, ACOL, BCOL, PA, PB, LOW, GramEpilogue<false>>(plan, p, e, s);
     return launch_tile<ACOL, BCOL, PA, PB, LOW, GramEpilogue<true>>(plan, p, e, s);
 }
 

@@ -59,8 +59,8 @@ struct PairArgs {
 enum { PAIR_ONE = 0, PAIR_TWO = 1, PAIR_FLOAT = 2 };
 
 // tile shapes
-enum { PAIR_256 = 0, PAIR_128 = 1, PAIR_64 = 2, PAIR_SHAPES = 3 };
-inline int pair_tile_of(int shape) { return shape == PAIR_256 ? 256 : shape == PAIR_128 ? 128 : 64; }
+enum { PAIR_256 = 0, PAIR_128 = 1, PAIR_64 = 2, PAIR_32 = 3, PAIR_SHAPES = 4 };
+inline int pair_tile_of(int shape) { return shape == PAIR_256 ? 256 : shape == PAIR_128 ? 128 : shape == PAIR_64 ? 64 : 32; }
 struct PairPlan {
     int shape, splits;   // workgroups that share a tile's k
 };

@@ -68,6 +68,7 @@ template <int W>
 __device__ __forceinline__ int columns_swizzle(int k)
 {
     if (W % 128 == 0) return ((k & 3) | ((k >> 1) & 4)) << 1;
+    if (W % 64) return (k >> 3 & 1) << 1;
     return (((k >> 1) & 1) | ((k >> 2) & 2)) << 1;
 }
 
@@ -157,8 +158,8 @@ __device__ __forceinline__ bf16x8 load_fragment(const char *lds, int at, int i, 
             s16x4 h[2];
             bf16x8 v;
         } f;
-        static_assert(W % 64 == 0, "a row of the tile is whole units of 128 bytes");
-        constexpr int LOW = W % 128 == 0 ? 255 : 127;   // what the permutation moves within
+        static_assert(W == 32 || W % 64 == 0, "a row of the tile is whole units of 128 bytes, or half a one");
+        constexpr int LOW = W % 128 == 0 ? 255 : W % 64 == 0 ? 127 : 63;   // what the permutation moves within
         const char *q = lds + (at ^ (i * 2 & LOW)) + (i * 2 & ~LOW) + kk * 32 * (W * 2);
         f.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)q);
         f.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(q + 4 * (W * 2)));
