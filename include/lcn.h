@@ -499,8 +499,8 @@ lcn_status lcn_attention_backward(const lcn_attention_desc *desc, const void *q,
  * 2 d_out; nullable); y rows x d_out.  kept (nullable, 16-byte aligned, as many bytes as the call below
  * says): g and u for the backward pass, in a layout of the library's own: floats with float tensors; with bf16
  * tensors 16 bits a value, within 2^-14 of the power of two above the largest of eight neighbours.
- * Sizes: 0 <= rows <= 2^30, 1 <= d_in <= 2^20, 1 <= d_out <= 2^19, rows times d_in or 2 d_out <= 2^42.  Up to 8
- * rows need no workspace (the call says 0 bytes). */
+ * Sizes: 0 <= rows <= 2^30, 1 <= d_in <= 2^20, 1 <= d_out <= 2^19, rows times d_in or 2 d_out <= 2^42.  The
+ * forward pass needs no workspace for up to 8 rows and in narrow layers (the call says 0 bytes). */
 lcn_status lcn_gated_linear_workspace_bytes(int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype, int32_t backward,
                                             size_t *bytes);
 lcn_status lcn_gated_linear_kept_bytes(int64_t rows, int32_t d_out, int32_t dtype, size_t *bytes);
@@ -517,8 +517,9 @@ lcn_status lcn_gated_linear_backward(const void *x, const void *W, const void *k
  *   y = (x - mean) rstd weight + bias,  rstd = 1 / sqrt(mean of (x - mean)^2 + eps).
  * weight, bias (dim, of type dtype) are nullable (1 and 0); mean, rstd (fp32, rows;
  * nullable): what the backward pass takes.  y may be x.  A row that holds a value that is not
- * finite becomes NaN; where squares leave a float's range (differences from 1e19 on) rstd is 0.  Sizes: 0 <= rows <= 2^30, 1 <= dim <= 2^20, their product <= 2^42; eps
- * finite and >= 0 (0: rows of equal values become NaN).  No workspace. */
+ * finite becomes NaN; where squares leave a float's range (differences from 1e19 on) rstd is 0.
+ * Sizes: 0 <= rows <= 2^30, 1 <= dim <= 2^20, their product <= 2^42; eps finite and >= 0
+ * (0: rows of equal values become NaN).  No workspace. */
 lcn_status lcn_layer_norm(const void *x, const void *weight, const void *bias, int64_t rows, int32_t dim, int32_t dtype, float eps,
                           void *y, float *mean, float *rstd, void *hip_stream);
 /* Its gradients for a given dy: with xhat = (x - mean) rstd and g = dy .* weight,

@@ -485,7 +485,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
                 const int d0 = d * 16 + 4 * g;
-                if (d0 < a.dim) store_four(a.part + row * a.dim + d0, o[d][u], a.dim - d0, VEC);
+                if (d0 < a.dim) store_four(a.part + row * a.dim + d0, o[d][u], a.dim - d0);
             }
             // (capped: without keys there is no maximum either)
             if (g == 0) a.part_top[row] = make_float2(total == 0.f ? minus_infinity() : reference, total);
@@ -496,7 +496,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_forward
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             const int d0 = d * 16 + 4 * g;
-            if (d0 < a.dim) store_four(out + d0, o[d][u] * inv, a.dim - d0, VEC);
+            if (d0 < a.dim) store_four(out + d0, o[d][u] * inv, a.dim - d0);
         }
         if (g == 0) a.lse[w.head * a.total_q + n] = natural_log(reference, total);
     }
@@ -955,9 +955,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
             if (d0 >= a.dim) continue;
             const f32x4 v = dq[d][u] * score.rest(a);
             if (a.key_splits > 1)
-                store_four(a.part + w.split * a.total_q * a.heads * a.dim + at + d0, v, a.dim - d0, VEC);
+                store_four(a.part + w.split * a.total_q * a.heads * a.dim + at + d0, v, a.dim - d0);
             else
-                store_four((T *)a.dq + at + d0, v, a.dim - d0, VEC);
+                store_four((T *)a.dq + at + d0, v, a.dim - d0);
         }
     }
 }
@@ -1113,11 +1113,11 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
             if (d0 >= a.dim) continue;
             if (a.splits > 1) {
                 const long long all = a.total_k * a.kv_heads * a.dim;
-                store_four(a.part + 2 * share * all + at + d0, dk[d][u] * rest, a.dim - d0, VEC);
-                store_four(a.part + (2 * share + 1) * all + at + d0, dv[d][u], a.dim - d0, VEC);
+                store_four(a.part + 2 * share * all + at + d0, dk[d][u] * rest, a.dim - d0);
+                store_four(a.part + (2 * share + 1) * all + at + d0, dv[d][u], a.dim - d0);
             } else {
-                store_four((T *)a.dk + at + d0, dk[d][u] * rest, a.dim - d0, VEC);
-                store_four((T *)a.dv + at + d0, dv[d][u], a.dim - d0, VEC);
+                store_four((T *)a.dk + at + d0, dk[d][u] * rest, a.dim - d0);
+                store_four((T *)a.dv + at + d0, dv[d][u], a.dim - d0);
             }
         }
     }
@@ -1127,8 +1127,7 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(AttentionArgs a)
 // `width` of a token.  Tokens in no set are not written, or become zero (clear).
 template <class T>
 __global__ __launch_bounds__(256) void attention_add_kernel(const float *part, int splits, long long tokens, long long width,
-                                                            const int64_t *off, int sets, T *out0, T *out1, int whole,
-                                                            int clear)
+                                                            const int64_t *off, int sets, T *out0, T *out1, int clear)
 {
     const long long all = tokens * width, stride = all * gridDim.y, fours = (all + 3) / 4;
     const long long begin = off[0] < 0 ? 0 : off[0] * width, end = (off[sets] < tokens ? off[sets] : tokens) * width;
@@ -1137,9 +1136,9 @@ __global__ __launch_bounds__(256) void attention_add_kernel(const float *part, i
     for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < fours; t += (long long)gridDim.x * 256) {
         const long long i = t * 4;
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < splits; ++s) v += load_four(part + s * stride + i, all - i < 4 ? (int)(all - i) : 4, whole);
+        for (int s = 0; s < splits; ++s) v += load_four(part + s * stride + i, all - i < 4 ? (int)(all - i) : 4);
         if (i >= begin && i + 4 <= end) {
-            store_four(out + i, v, 4, whole);
+            store_four(out + i, v, 4);
         } else {
             for (int e = 0; e < 4; ++e) {
                 const bool in = i + e >= begin && i + e < end;

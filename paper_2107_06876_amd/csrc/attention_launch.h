@@ -128,11 +128,11 @@ hipError_t attention_by_chunks(AttentionArgs a, bool vec, int shape, hipStream_t
 }
 template <class T>
 static hipError_t add_sums(const AttentionArgs &a, int splits, long long tokens, long long width, const int64_t *off, void *out0,
-                           void *out1, bool whole, hipStream_t s)
+                           void *out1, hipStream_t s)
 {
     const long long groups = (tokens * width / 4 + 255) / 256 + 1;
     hipLaunchKernelGGL(attention_add_kernel<T>, dim3((unsigned)(groups < 4096 ? groups : 4096), out1 ? 2 : 1), dim3(256), 0, s,
-                       a.part, splits, tokens, width, off, a.sets, (T *)out0, (T *)out1, whole ? 1 : 0, a.clear);
+                       a.part, splits, tokens, width, off, a.sets, (T *)out0, (T *)out1, a.clear);
     return hipGetLastError();
 }
 template <class T>
@@ -143,12 +143,12 @@ hipError_t attention_backward(AttentionArgs a, bool vec, int shape, hipStream_t 
         if (!a.dq) a.key_splits = 1;   // delta alone: formed by one workgroup of a tile
         e = by_size<T, GRAD_Q>(a, vec, shape, s);
         if (e == hipSuccess && a.key_splits > 1)
-            e = add_sums<T>(a, a.key_splits, a.total_q, (long long)a.heads * a.dim, a.q_off, a.dq, nullptr, vec, s);
+            e = add_sums<T>(a, a.key_splits, a.total_q, (long long)a.heads * a.dim, a.q_off, a.dq, nullptr, s);
     }
     if (e != hipSuccess || !a.dk || a.total_k == 0) return e;
     e = by_size<T, GRAD_KV>(a, vec, shape, s);
     if (e != hipSuccess || a.splits == 1) return e;
-    return add_sums<T>(a, a.splits, a.total_k, (long long)a.kv_heads * a.dim, a.k_off, a.dk, a.dv, vec, s);
+    return add_sums<T>(a, a.splits, a.total_k, (long long)a.kv_heads * a.dim, a.k_off, a.dk, a.dv, s);
 }
 
 }  // namespace lcn

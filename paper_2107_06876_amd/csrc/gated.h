@@ -126,11 +126,11 @@ struct GatedArgs {
     const T *bias;   // 2 width
     T *y;
     typename Keep<T>::type *kept;   // nullable
-    int act, whole;  // whole: rows of y and both halves of bias are whole 16-byte pieces
+    int act;
 };
 
-// Narrow layers (kernels_gated_narrow.hip): up to 64 inputs and outputs, on many rows that are whole 16-byte pieces.
-bool gated_narrow(const void *x, const void *w, int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype);
+// Narrow layers (kernels_gated_narrow.hip): up to 64 inputs and outputs, on many rows.
+bool gated_narrow(int64_t rows, int32_t d_in, int32_t d_out);
 // workgroups of the backward pass, each of which leaves partial sums of dW and db, 2 d_out (d_in + 1) floats
 int gated_narrow_groups(int64_t rows);
 template <class T>

@@ -57,7 +57,7 @@ struct EntropyForward {
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             bias[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (e.r.bias) bias[i] = load_four(e.r.bias + m0 + i * 16 + g4, (int)(p.m - (m0 + i * 16 + g4)), false);
+            if (e.r.bias) bias[i] = load_four(e.r.bias + m0 + i * 16 + g4, (int)(p.m - (m0 + i * 16 + g4)));
         }
         const bool edge = m0 + TM * 16 > p.m;
 #pragma unroll
@@ -220,7 +220,7 @@ struct EntropyGradient {
         for (int i = 0; i < TM; ++i) {
             const long long m = m0 + i * 16 + g4;
             bias[i] = sum[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (e.r.bias) bias[i] = load_four(e.r.bias + m, (int)(p.m - m), false);
+            if (e.r.bias) bias[i] = load_four(e.r.bias + m, (int)(p.m - m));
         }
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
@@ -356,29 +356,28 @@ __global__ __launch_bounds__(256) void entropy_few_gradient_kernel(EntropyRow e,
 __global__ __launch_bounds__(256) void entropy_finish_kernel(const float *__restrict__ part, int splits, long long stride,
                                                              long long rows, int dim, long long ldp, float scale,
                                                              const float *__restrict__ rest, const int64_t *__restrict__ target,
-                                                             const __bf16 *__restrict__ w, int vocab, __bf16 *__restrict__ out,
-                                                             int whole)
+                                                             const __bf16 *__restrict__ w, int vocab, __bf16 *__restrict__ out)
 {
     const int per_row = (dim + 7) / 8;
     for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < rows * per_row; t += (long long)gridDim.x * 256) {
         const long long n = t / per_row;
         const int c = (int)(t - n * per_row) * 8;
         f32x4 v[2], o[2];
-        load_eight(part + n * ldp + c, 8, true, v);
+        load_eight(part + n * ldp + c, 8, v);
         for (int s = 1; s < splits; ++s) {
-            load_eight(part + s * stride + n * ldp + c, 8, true, o);
+            load_eight(part + s * stride + n * ldp + c, 8, o);
             v[0] += o[0];
             v[1] += o[1];
         }
         const int64_t at = target[n];
         if (at >= 0 && at < vocab) {
-            load_eight(w + at * dim + c, dim - c, whole, o);
+            load_eight(w + at * dim + c, dim - c, o);
             v[0] += o[0] * rest[n];
             v[1] += o[1] * rest[n];
         }
         v[0] *= scale;
         v[1] *= scale;
-        store_eight(out + n * dim + c, v, dim - c, whole);
+        store_eight(out + n * dim + c, v, dim - c);
     }
 }
 
@@ -614,7 +613,7 @@ static lcn_status entropy_backward_as(const void *x, const void *w, const float 
         const long long groups = (rows * ((dim + 7) / 8) + 255) / 256, ldp = padded(dim);
         hipLaunchKernelGGL(entropy_finish_kernel, dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(256), 0, s, b.part_dx,
                            b.dx.splits, rows * ldp, (long long)rows, dim, ldp, scale, rest, target, (const __bf16 *)w, vocab,
-                           (__bf16 *)dx, whole_rows<__bf16>((const void *)((uintptr_t)dx | (uintptr_t)w), dim));
+                           (__bf16 *)dx);
         OPCHK(hipGetLastError());
     } else if (dx && !one)
         OPCHK(launch_add_partials(b.part_dx, b.dx.splits, rows, dim, padded(dim), scale, dtype, dx, s));

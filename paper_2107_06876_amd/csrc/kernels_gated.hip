@@ -24,7 +24,7 @@ __device__ __forceinline__ void gated_finish(const GatedArgs<T> &e, f32x4 (&g)[2
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) g[i >> 2][i & 3] = gate<T, ACT>(g[i >> 2][i & 3]) * u[i >> 2][i & 3];
-    store_eight(e.y + n * width + m, g, width - m, e.whole);
+    store_eight(e.y + n * width + m, g, width - m);
 }
 
 // The product's epilogue: subtiles of 16 rows are g's and u's in turn.  A wavefront's 16 columns n go through LDS row by row, as in
@@ -58,10 +58,10 @@ struct GatedEpilogue {
                 u[0] = *(const f32x4 *)(at + 16);
                 u[1] = *(const f32x4 *)(at + 20);
                 if (e.bias) {
-                    load_eight(e.bias + m, p.m - m, e.whole, b);
+                    load_eight(e.bias + m, p.m - m, b);
                     g[0] += b[0];
                     g[1] += b[1];
-                    load_eight(e.bias + p.m + m, p.m - m, e.whole, b);
+                    load_eight(e.bias + p.m + m, p.m - m, b);
                     u[0] += b[0];
                     u[1] += b[1];
                 }
@@ -80,7 +80,7 @@ template <class T, int ACT>
 __global__ __launch_bounds__(256) void gated_finish_kernel(GatedArgs<T> e, const float *__restrict__ part, int splits,
                                                            long long stride, long long rows, int width, long long ldp)
 {
-    const int per_row = (width + 7) / 8, whole_half = width % 4 == 0;
+    const int per_row = (width + 7) / 8;
     for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < rows * per_row; t += (long long)gridDim.x * 256) {
         const long long n = t / per_row;
         const int m = (int)(t - n * per_row) * 8, left = width - m;
@@ -88,14 +88,14 @@ __global__ __launch_bounds__(256) void gated_finish_kernel(GatedArgs<T> e, const
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const float *p = part + n * ldp + h * width + m;
-            load_eight(p, left, whole_half, z[h]);
+            load_eight(p, left, z[h]);
             for (int s = 1; s < splits; ++s) {
-                load_eight(p + s * stride, left, whole_half, v);
+                load_eight(p + s * stride, left, v);
                 z[h][0] += v[0];
                 z[h][1] += v[1];
             }
             if (e.bias) {
-                load_eight(e.bias + h * width + m, left, e.whole, v);
+                load_eight(e.bias + h * width + m, left, v);
                 z[h][0] += v[0];
                 z[h][1] += v[1];
             }
@@ -104,8 +104,64 @@ __global__ __launch_bounds__(256) void gated_finish_kernel(GatedArgs<T> e, const
     }
 }
 
+template <int N>
+struct Number {
+    static constexpr int value = N;
+};
+// The dot products of rows w0 and w1 with R rows of x (`rows` of them exist), shared by 16 lanes, in each of them: in pieces of 16
+// bytes wherever rows lie, several of them requested before the first is worked on.  One row, 4096 -> 2 x 4096 bf16, 16 us with a
+// compiler's order of the loads, 11.5 so; eight 26 and 23; one, 2047 -> 2 x 8191, 24 value by value and 13.
+template <class T, int R>
+__device__ __forceinline__ void dot_of_rows(const T *__restrict__ w0, const T *__restrict__ w1, const T *__restrict__ x, int rows, int k,
+                                            float (&sum)[2][R])
+{
+    constexpr int V = 16 / (int)sizeof(T), AHEAD = R <= 2 ? 4 : 2;
+    typedef T piece __attribute__((ext_vector_type(V)));
+    typedef T any __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+    const int lane = threadIdx.x & 15, whole = k - k % V;
+    auto add = [&](int c, auto count) {
+        constexpr int U = decltype(count)::value;
+        piece a[U], b[U], y[U][R];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            a[u] = *(const any *)(w0 + c + u * 16 * V);
+            b[u] = *(const any *)(w1 + c + u * 16 * V);
+#pragma unroll
+            for (int r = 0; r < R; ++r) y[u][r] = *(const any *)(x + (long long)(r < rows ? r : 0) * k + c + u * 16 * V);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    sum[0][r] = __builtin_fmaf((float)a[u][e], (float)y[u][r][e], sum[0][r]);
+                    sum[1][r] = __builtin_fmaf((float)b[u][e], (float)y[u][r][e], sum[1][r]);
+                }
+    };
+    int c = lane * V;
+    for (; c + (AHEAD - 1) * 16 * V < whole; c += AHEAD * 16 * V) add(c, Number<AHEAD>());
+    for (; c < whole; c += 16 * V) add(c, Number<1>());
+    if (whole + lane < k) {   // behind the last whole piece
+        const float a = (float)w0[whole + lane], b = (float)w1[whole + lane];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float y = (float)x[(long long)(r < rows ? r : 0) * k + whole + lane];
+            sum[0][r] = __builtin_fmaf(a, y, sum[0][r]);
+            sum[1][r] = __builtin_fmaf(b, y, sum[1][r]);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) sum[f][r] += __shfl_xor(sum[f][r], o, 16);
+}
+
 // Few rows: bound by reading W once; 16 lanes read a row of Wg and the one of Wu that belongs to it, a workgroup has 16 outputs.
-template <class T, int R, bool VEC>
+template <class T, int R>
 __global__ __launch_bounds__(256) void gated_few_kernel(GatedArgs<T> e, const T *__restrict__ x, const T *__restrict__ w, int rows,
                                                         int k, int width)
 {
@@ -115,7 +171,7 @@ __global__ __launch_bounds__(256) void gated_few_kernel(GatedArgs<T> e, const T 
     float sum[2][R];
 #pragma unroll
     for (int r = 0; r < R; ++r) sum[0][r] = sum[1][r] = 0.f;
-    few_rows_dot<T, R, VEC>(w + (long long)fr * k, w + (long long)(width + fr) * k, x, rows, k, sum);
+    dot_of_rows<T, R>(w + (long long)fr * k, w + (long long)(width + fr) * k, x, rows, k, sum);
     float g = 0.f, u = 0.f;   // lane r finishes one value
 #pragma unroll
     for (int i = 0; i < R; ++i)
@@ -155,10 +211,7 @@ template <class T, int R>
 static hipError_t launch_few(const GatedArgs<T> &e, const T *x, const T *w, int rows, int k, int width, hipStream_t s)
 {
     const unsigned grid = (unsigned)((width + 15) / 16);
-    if (k % (16 / (int)sizeof(T)) == 0 && (((uintptr_t)x | (uintptr_t)w) & 15) == 0)
-        hipLaunchKernelGGL((gated_few_kernel<T, R, true>), dim3(grid), dim3(256), 0, s, e, x, w, rows, k, width);
-    else
-        hipLaunchKernelGGL((gated_few_kernel<T, R, false>), dim3(grid), dim3(256), 0, s, e, x, w, rows, k, width);
+    hipLaunchKernelGGL((gated_few_kernel<T, R>), dim3(grid), dim3(256), 0, s, e, x, w, rows, k, width);
     return hipGetLastError();
 }
 
@@ -166,7 +219,7 @@ static hipError_t launch_few(const GatedArgs<T> &e, const T *x, const T *w, int 
 // (part: nullable).  C pieces of eight columns of either half x 256 / C rows at a time.
 template <class T, int ACT, int C, int PLANES>
 __global__ __launch_bounds__(256) void gated_slope_kernel(const T *__restrict__ dy, const typename Keep<T>::type *__restrict__ kept,
-                                                          long long rows, int width, int dp, int rows_each, int whole,
+                                                          long long rows, int width, int dp, int rows_each,
                                                           __bf16 *__restrict__ dst, float *__restrict__ part)
 {
     constexpr int R = 256 / C;
@@ -179,7 +232,7 @@ __global__ __launch_bounds__(256) void gated_slope_kernel(const T *__restrict__ 
     if (k < width)
         for (long long r = r0 + q; r < r0 + rows_each && r < rows; r += R) {
             f32x4 d[2], z[2][2];
-            load_eight(dy + r * width + k, left, whole, d);
+            load_eight(dy + r * width + k, left, d);
             Keep<T>::load(kept + r * 2 * wp + k, z[0]);
             Keep<T>::load(kept + (r * 2 + 1) * wp + k, z[1]);
             bf16x8 o[2][PLANES];
@@ -208,8 +261,9 @@ __global__ __launch_bounds__(256) void gated_slope_kernel(const T *__restrict__ 
                     __bf16 *first = dst + p * plane + r * dp + k;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        if (width % 8 == 0) {
-                            *(bf16x8 *)(first + h * width) = o[h][p];
+                        if (left >= 8) {
+                            typedef bf16x8 any __attribute__((aligned(2)));
+                            *(any *)(first + h * width) = o[h][p];
                         } else {
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
@@ -332,7 +386,7 @@ static GatedBackward gated_backward_space(char *ws, int64_t rows, int32_t d_in, 
     b.dw = plan_columns(c, d_in, wide, rows, b.planes, true);
     b.sums = (float *)c.take((size_t)b.groups * wide * 4);
     b.narrow = (float *)b.xp;   // in place of all others
-    const size_t sums = gated_narrow(nullptr, nullptr, rows, d_in, d_out, dtype) ? (size_t)gated_narrow_groups(rows) * wide * (d_in + 1) * 4 : 0;
+    const size_t sums = gated_narrow(rows, d_in, d_out) ? (size_t)gated_narrow_groups(rows) * wide * (d_in + 1) * 4 : 0;
     b.bytes = c.used > sums ? c.used : sums;
     return b;
 }
@@ -341,7 +395,7 @@ template <class T>
 static lcn_status gated_as(const T *x, const T *w, const T *bias, int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype,
                            int32_t act, T *y, typename Keep<T>::type *kept, char *ws, size_t ws_bytes, hipStream_t s)
 {
-    GatedArgs<T> e{bias, y, kept, act, 0};
+    GatedArgs<T> e{bias, y, kept, act};
     if (rows <= FEW_ROWS) {
         const int r = (int)rows;
         OPCHK(r == 1   ? launch_few<T, 1>(e, x, w, r, d_in, d_out, s)
@@ -350,8 +404,7 @@ static lcn_status gated_as(const T *x, const T *w, const T *bias, int64_t rows, 
                        : launch_few<T, 8>(e, x, w, r, d_in, d_out, s));
         return LCN_OK;
     }
-    e.whole = whole_rows<T>((const void *)((uintptr_t)y | (uintptr_t)bias), d_out);
-    if (gated_narrow(x, w, rows, d_in, d_out, dtype)) {
+    if (gated_narrow(rows, d_in, d_out)) {
         OPCHK(launch_gated_narrow(e, x, w, rows, d_in, d_out, s));
         return LCN_OK;
     }
@@ -397,17 +450,17 @@ static lcn_status gated_backward_as(const T *x, const T *w, const typename Keep<
 {
     const GatedBackward b = gated_backward_space(ws, rows, d_in, d_out, dtype);
     if (!ws || ((uintptr_t)ws & 255) || ws_bytes < b.bytes) return LCN_ERR_ALLOC;
-    if (gated_narrow(x, w, rows, d_in, d_out, dtype) && x && w) {
+    if (gated_narrow(rows, d_in, d_out) && x && w) {
         OPCHK(launch_gated_narrow_backward(x, w, kept, dy, rows, d_in, d_out, act, dx, dw, dbias, b.narrow, s));
         return LCN_OK;
     }
     const int32_t wide = 2 * d_out;
-    const int dp = (int)padded(wide), whole = whole_rows<T>(dy, d_out);
+    const int dp = (int)padded(wide);
     OPCHK(by_activation(act, [&](auto a) {
         constexpr int ACT = decltype(a)::value;
         auto launch = [&](auto kernel, int pieces) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)((d_out + pieces * 8 - 1) / (pieces * 8)), (unsigned)b.groups), dim3(256), 0, s, dy,
-                               kept, (long long)rows, d_out, dp, b.rows_each, whole,
+                               kept, (long long)rows, d_out, dp, b.rows_each,
                                dx || dw ? (__bf16 *)b.dz : nullptr, dbias ? b.sums : nullptr);
             return hipGetLastError();
         };
@@ -470,7 +523,7 @@ lcn_status lcn_gated_linear_workspace_bytes(int64_t rows, int32_t d_in, int32_t 
 {
     if (!bytes || !gated_args_fit(rows, d_in, d_out, dtype)) return LCN_ERR_INVALID_ARG;
     *bytes = 0;
-    if (rows == 0 || (!backward && rows <= FEW_ROWS)) return LCN_OK;
+    if (rows == 0 || (!backward && (rows <= FEW_ROWS || gated_narrow(rows, d_in, d_out)))) return LCN_OK;
     *bytes = backward ? gated_backward_space(nullptr, rows, d_in, d_out, dtype).bytes
                       : gated_forward_space(nullptr, rows, d_in, d_out, dtype).bytes;
     return LCN_OK;

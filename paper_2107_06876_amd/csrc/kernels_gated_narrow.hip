@@ -12,6 +12,18 @@ namespace lcn {
 
 constexpr int NARROW = 64;   // inputs, outputs
 
+// values d0 .. d0 + 7 of a row (nullptr: zeros)
+template <class T>
+__device__ __forceinline__ typename Frag<T>::type fragment_of(const T *row, int d0, int dim)
+{
+    typename Frag<T>::type f;
+    Eight<T> v{};
+    if (row && d0 < dim) v = read_eight(row + d0, dim - d0);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = v.v[e];
+    return f;
+}
+
 template <class T, int KP, int ACT, bool KEPT>
 __global__ __launch_bounds__(256) void gated_narrow_kernel(GatedArgs<T> e, const T *__restrict__ x, const T *__restrict__ w,
                                                            long long rows, int k, int width)
@@ -27,16 +39,16 @@ __global__ __launch_bounds__(256) void gated_narrow_kernel(GatedArgs<T> e, const
             const int m = m0 + i * 16 + (lane & 15), mb = m0 + i * 16 + 4 * g;
 #pragma unroll
             for (int c = 0; c < C; ++c)
-                fw[h][i][c] = read_fragment<T, true>(m < width ? w + (long long)(h * width + m) * k : nullptr, 32 * c + 8 * g, k);
+                fw[h][i][c] = fragment_of(m < width ? w + (long long)(h * width + m) * k : (const T *)nullptr, 32 * c + 8 * g, k);
             bias[h][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (e.bias && mb < width) bias[h][i] = load_four(e.bias + h * width + mb, width - mb, e.whole);
+            if (e.bias && mb < width) bias[h][i] = load_four(e.bias + h * width + mb, width - mb);
         }
     const long long tiles = (rows + 15) / 16, step = (long long)gridDim.x * 4;
     typename Frag<T>::type fx[C];
     auto read = [&](long long t) {
         const long long n = t * 16 + (lane & 15);
 #pragma unroll
-        for (int c = 0; c < C; ++c) fx[c] = read_fragment<T, true>(n < rows ? x + n * k : nullptr, 32 * c + 8 * g, k);
+        for (int c = 0; c < C; ++c) fx[c] = fragment_of(n < rows ? x + n * k : (const T *)nullptr, 32 * c + 8 * g, k);
     };
     long long t = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
     read(t);
@@ -76,7 +88,7 @@ __global__ __launch_bounds__(256) void gated_narrow_kernel(GatedArgs<T> e, const
             f32x4 y;
 #pragma unroll
             for (int u = 0; u < 4; ++u) y[u] = gate<T, ACT>(z[0][i][u]) * z[1][i][u];
-            store_four(e.y + n * width + m, y, width - m, e.whole);
+            store_four(e.y + n * width + m, y, width - m);
         }
     }
 }
@@ -86,7 +98,7 @@ template <class T, int ACT, int D, int C>
 __global__ __launch_bounds__(256) void gated_narrow_grad_kernel(const T *__restrict__ x, const T *__restrict__ w,
                                                                 const typename Keep<T>::type *__restrict__ kept,
                                                                 const T *__restrict__ dy, long long rows, int d_in, int width,
-                                                                T *__restrict__ dx, float *__restrict__ part, int whole, int whole_dx)
+                                                                T *__restrict__ dx, float *__restrict__ part)
 {
     // pitches: rows 8 (of W) and 1 (of dz) apart begin 16 banks apart
     constexpr int WP = D * 16 + 2, ZP = C * 64 + 16, K = C * 64;
@@ -94,9 +106,9 @@ __global__ __launch_bounds__(256) void gated_narrow_grad_kernel(const T *__restr
     __shared__ __align__(16) float lds_z[4 * 16 * ZP];    // a wavefront's dz
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, l = lane & 15, wp = (int)padded(width);
 #pragma unroll
-    for (int u = 0; u < K * D * 4 / 256; ++u) {   // d_in is a multiple of four, W aligned to as many values
+    for (int u = 0; u < K * D * 4 / 256; ++u) {
         const int i = u * 256 + tid, k = i / (D * 4), c = i % (D * 4) * 4, h = k / (C * 32), m = k % (C * 32);
-        const f32x4 v = m < width ? load_four(w + (h * width + m) * d_in + c, d_in - c, true) : f32x4{0.f, 0.f, 0.f, 0.f};
+        const f32x4 v = m < width ? load_four(w + (h * width + m) * d_in + c, d_in - c) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int e = 0; e < 4; ++e) lds_w[k * WP + c + e] = v[e];
     }
@@ -124,7 +136,7 @@ __global__ __launch_bounds__(256) void gated_narrow_grad_kernel(const T *__restr
             const int m = 32 * c + 8 * g;
             v.d[c][0] = v.d[c][1] = v.a[c][0] = v.a[c][1] = v.b[c][0] = v.b[c][1] = f32x4{0.f, 0.f, 0.f, 0.f};
             if (n < rows && m < width) {
-                load_eight(dy + n * width + m, width - m, whole, v.d[c]);
+                load_eight(dy + n * width + m, width - m, v.d[c]);
                 Keep<T>::load(kept + n * 2 * wp + m, v.a[c]);
                 Keep<T>::load(kept + (n * 2 + 1) * wp + m, v.b[c]);
             }
@@ -179,7 +191,7 @@ __global__ __launch_bounds__(256) void gated_narrow_grad_kernel(const T *__restr
         if (dx && n < rows)
 #pragma unroll
             for (int t = 0; t < D; ++t)
-                if (t * 16 + 4 * g < d_in) store_four(dx + n * d_in + t * 16 + 4 * g, out[t], d_in - t * 16 - 4 * g, whole_dx);
+                if (t * 16 + 4 * g < d_in) store_four(dx + n * d_in + t * 16 + 4 * g, out[t], d_in - t * 16 - 4 * g);
         if (!part) continue;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // LDS serves a wavefront in order
         __builtin_amdgcn_wave_barrier();
@@ -269,11 +281,7 @@ __global__ __launch_bounds__(256) void gated_narrow_join_kernel(const float *__r
 
 // ---- host ---------------------------------------------------------------------
 
-bool gated_narrow(const void *x, const void *w, int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype)
-{
-    return rows >= 128 && d_in <= NARROW && d_out <= NARROW && d_in % (dtype == LCN_F32 ? 4 : 8) == 0 &&
-           (((uintptr_t)x | (uintptr_t)w) & 15) == 0;
-}
+bool gated_narrow(int64_t rows, int32_t d_in, int32_t d_out) { return rows >= 128 && d_in <= NARROW && d_out <= NARROW; }
 
 int gated_narrow_groups(int64_t rows)
 {
@@ -308,12 +316,11 @@ hipError_t launch_gated_narrow_backward(const T *x, const T *w, const typename K
 {
     const int groups = gated_narrow_groups(rows), first = 2 * d_out * d_in, all = first + 2 * d_out;
     const bool sums = dw || db;
-    const int whole = whole_rows<T>(dy, d_out);
     const hipError_t st = by_activation(act, [&](auto a) {
         constexpr int ACT = decltype(a)::value;
         auto launch = [&](auto kernel) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, s, x, w, kept, dy, (long long)rows, d_in, d_out, dx,
-                               sums ? part : nullptr, whole, whole_rows<T>(dx, d_in));
+                               sums ? part : nullptr);
             return hipGetLastError();
         };
         if (d_out <= 32)

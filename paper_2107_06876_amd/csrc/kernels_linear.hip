@@ -17,21 +17,21 @@ struct LinearArgs {
     const T *bias, *residual;
     T *y;
     float *pre;
-    int act, whole;   // whole: rows of y, residual, bias and pre are whole 16-byte pieces
+    int act;
 };
 
 template <class T, int ACT>
 __device__ __forceinline__ void linear_finish(const LinearArgs<T> &e, f32x4 (&z)[2], const Eight<T> &residual, long long at,
                                               int left)
 {
-    if (e.pre) store_eight(e.pre + at, z, left, e.whole);
+    if (e.pre) store_eight(e.pre + at, z, left);
 #pragma unroll
     for (int u = 0; u < 8; ++u) z[u >> 2][u & 3] = activate<ACT>(z[u >> 2][u & 3]);
     if (e.residual) {
 #pragma unroll
         for (int u = 0; u < 8; ++u) z[u >> 2][u & 3] += (float)residual.v[u];
     }
-    store_eight(e.y + at, z, left, e.whole);
+    store_eight(e.y + at, z, left);
 }
 
 template <class T, int ACT>
@@ -48,7 +48,7 @@ struct LinearEpilogue {
         for (int i = 0; i < TM; ++i) {
             const long long m = m0 + i * 16 + 4 * (lane >> 4);
             bias[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (e.bias && m < p.m) bias[i] = load_four(e.bias + m, (int)(p.m - m), e.whole);
+            if (e.bias && m < p.m) bias[i] = load_four(e.bias + m, (int)(p.m - m));
         }
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
@@ -59,7 +59,7 @@ struct LinearEpilogue {
                 region, col, lane,
                 [&](int r, int c) {
                     const long long n = n0 + j * 16 + r, m = m0 + c;
-                    return e.residual && n < p.n && m < p.m ? read_eight(e.residual + n * p.m + m, (int)(p.m - m), e.whole) : Eight<T>{};
+                    return e.residual && n < p.n && m < p.m ? read_eight(e.residual + n * p.m + m, (int)(p.m - m)) : Eight<T>{};
                 },
                 [&](int r, int c, f32x4 (&v)[2], const Eight<T> &o) {
                     const long long n = n0 + j * 16 + r, m = m0 + c;
@@ -80,18 +80,18 @@ __global__ __launch_bounds__(256) void linear_finish_kernel(LinearArgs<T> e, con
         const int m = (int)(t - n * per_row) * 8, left = width - m;
         f32x4 z[2], v[2];
         Eight<T> r{};
-        load_eight(part + n * ldp + m, 8, true, z);
+        load_eight(part + n * ldp + m, 8, z);
         for (int u = 1; u < splits; ++u) {
-            load_eight(part + u * stride + n * ldp + m, 8, true, v);
+            load_eight(part + u * stride + n * ldp + m, 8, v);
             z[0] += v[0];
             z[1] += v[1];
         }
         if (e.bias) {
-            load_eight(e.bias + m, left, e.whole, v);
+            load_eight(e.bias + m, left, v);
             z[0] += v[0];
             z[1] += v[1];
         }
-        if (e.residual) r = read_eight(e.residual + n * width + m, left, e.whole);
+        if (e.residual) r = read_eight(e.residual + n * width + m, left);
         linear_finish<T, ACT>(e, z, r, n * width + m, left);
     }
 }
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(256) void linear_narrow_kernel(LinearArgs<T> e, con
 #pragma unroll
         for (int c = 0; c < C; ++c) fw[i][c] = read_fragment<T, VEC>(m < width ? w + (long long)m * k : nullptr, 32 * c + 8 * g, k);
         bias[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (e.bias && mb < width) bias[i] = load_four(e.bias + mb, width - mb, e.whole);
+        if (e.bias && mb < width) bias[i] = load_four(e.bias + mb, width - mb);
     }
     const long long tiles = (rows + 15) / 16, step = (long long)gridDim.x * 4;
     for (long long t = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); t < tiles; t += step) {
@@ -180,12 +180,12 @@ __global__ __launch_bounds__(256) void linear_narrow_kernel(LinearArgs<T> e, con
             const int m = m0 + i * 16 + 4 * g;
             if (m >= width) continue;
             const long long at = n * width + m;
-            if (e.pre) store_four(e.pre + at, acc[i], width - m, e.whole);
+            if (e.pre) store_four(e.pre + at, acc[i], width - m);
             f32x4 y;
 #pragma unroll
             for (int u = 0; u < 4; ++u) y[u] = activate<ACT>(acc[i][u]);
-            if (e.residual) y += load_four(e.residual + at, width - m, e.whole);
-            store_four(e.y + at, y, width - m, e.whole);
+            if (e.residual) y += load_four(e.residual + at, width - m);
+            store_four(e.y + at, y, width - m);
         }
     }
 }
@@ -194,7 +194,7 @@ __global__ __launch_bounds__(256) void linear_narrow_kernel(LinearArgs<T> e, con
 // 32 pieces of eight columns x 8 rows at a time.  Bound by memory: 16391 x 4096, bf16, GELU: 130 us, 4.1 TB/s (a copy: 4.4).
 template <class T, int ACT>
 __global__ __launch_bounds__(256) void slope_kernel(const T *__restrict__ dy, const float *__restrict__ pre, long long rows,
-                                                    int width, int dp, int rows_each, int whole,
+                                                    int width, int dp, int rows_each,
                                                     int planes, __bf16 *__restrict__ dst, float *__restrict__ part)
 {
     __shared__ float sums[8][32][9];
@@ -206,10 +206,10 @@ __global__ __launch_bounds__(256) void slope_kernel(const T *__restrict__ dy, co
     if (k < dp)
         for (long long r = r0 + q; r < r0 + rows_each && r < rows; r += 8) {
             f32x4 v[2];
-            load_eight(dy + r * width + k, width - k, whole, v);
+            load_eight(dy + r * width + k, width - k, v);
             if constexpr (ACT != LCN_ACT_NONE) {
                 f32x4 z[2];
-                load_eight(pre + r * width + k, width - k, whole, z);
+                load_eight(pre + r * width + k, width - k, z);
 #pragma unroll
                 for (int u = 0; u < 8; ++u) v[u >> 2][u & 3] *= activate_slope<ACT>(z[u >> 2][u & 3]);
             }
@@ -321,7 +321,7 @@ static lcn_status linear_as(const T *x, const T *w, const T *bias, const T *resi
                             int32_t d_out, int32_t dtype, int32_t act, T *y, float *pre, char *ws, size_t ws_bytes,
                             hipStream_t s)
 {
-    LinearArgs<T> e{bias, residual, y, pre, act, 0};
+    LinearArgs<T> e{bias, residual, y, pre, act};
     if (rows <= FEW_ROWS) {
         const int r = (int)rows;
         hipError_t st = r == 1   ? launch_few<T, 1>(e, x, w, r, d_in, d_out, s)
@@ -331,7 +331,6 @@ static lcn_status linear_as(const T *x, const T *w, const T *bias, const T *resi
         OPCHK(st);
         return LCN_OK;
     }
-    e.whole = whole_rows<T>((const void *)((uintptr_t)y | (uintptr_t)bias | (uintptr_t)residual | (uintptr_t)pre), d_out);
     if (narrow(rows, d_in, d_out, dtype)) {
         const bool vec = whole_rows<T>((const void *)((uintptr_t)x | (uintptr_t)w), d_in);
         constexpr int MOST = sizeof(T) == 4 ? 128 : 64;
@@ -384,10 +383,9 @@ static lcn_status linear_backward_as(const T *x, const T *w, const float *pre, c
     }
     if (!as_is || dbias) {
         const int dp = (int)padded(d_out);
-        const int whole = whole_rows<T>((const void *)((uintptr_t)dy | (uintptr_t)pre), d_out);
         OPCHK(by_activation(act, [&](auto a) {
             hipLaunchKernelGGL((slope_kernel<T, decltype(a)::value>), dim3((unsigned)((dp + 255) / 256), (unsigned)b.groups),
-                               dim3(256), 0, s, dy, pre, (long long)rows, d_out, dp, b.rows_each, whole, b.planes,
+                               dim3(256), 0, s, dy, pre, (long long)rows, d_out, dp, b.rows_each, b.planes,
                                as_is ? nullptr : (__bf16 *)b.dz, dbias ? b.sums : nullptr);
             return hipGetLastError();
         }));

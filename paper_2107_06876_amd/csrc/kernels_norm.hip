@@ -14,10 +14,43 @@
 
 namespace lcn {
 
+// V neighbours of a row, from its value c on.  TAIL: wherever they lie, and of a row's last piece only those that exist.
 template <class T, int V>
 struct Piece {
     typedef T type __attribute__((ext_vector_type(V)));
+    typedef T any __attribute__((ext_vector_type(V), aligned(sizeof(T))));
 };
+template <class T, int V, bool TAIL>
+__device__ __forceinline__ typename Piece<T, V>::type load_piece(const T *row, int c, int dim)
+{
+    typedef typename Piece<T, V>::type piece;
+    if constexpr (TAIL) {
+        if (c + V > dim) {
+            piece v{};
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (c + e < dim) v[e] = row[c + e];
+            return v;
+        }
+        return *(const typename Piece<T, V>::any *)(row + c);
+    }
+    return *(const piece *)(row + c);
+}
+template <class T, int V, bool TAIL>
+__device__ __forceinline__ void store_piece(T *p, int left, typename Piece<T, V>::type v)
+{
+    if constexpr (TAIL) {
+        if (left < V) {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (e < left) p[e] = v[e];
+        } else {
+            *(typename Piece<T, V>::any *)p = v;
+        }
+    } else {
+        *(typename Piece<T, V>::type *)p = v;
+    }
+}
 
 // Sums over the L lanes (or the workgroup's 256 threads) that share a row, in each of them.  `lds`: 4 values of the workgroup's
 // own, others from one call to the next (whoever is late still reads the last call's).
@@ -36,14 +69,14 @@ __device__ __forceinline__ float sum_over(float a, float *lds)
 }
 
 // L lanes have a row, C pieces of V values each.
-template <class T, int V, int L, int C>
+template <class T, int V, bool TAIL, int L, int C>
 __global__ __launch_bounds__(256) void norm_kernel(const T *x, const T *__restrict__ w, const T *__restrict__ b, long long rows,
                                                    int dim, float eps, T *y,   // y may be x
                                                    float *__restrict__ mean_out, float *__restrict__ rstd_out)
 {
     typedef typename Piece<T, V>::type piece;
     __shared__ float lds[2][4];
-    const int lane = threadIdx.x % L, units = dim / V;
+    const int lane = threadIdx.x % L, units = TAIL ? (dim + V - 1) / V : dim / V;
     const long long r = (long long)group_number() * (256 / L) + threadIdx.x / L;
     if (L > 64 && r >= rows) return;
     const bool here = r < rows;
@@ -52,7 +85,7 @@ __global__ __launch_bounds__(256) void norm_kernel(const T *x, const T *__restri
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int u = c * L + lane;
-        p[c] = here && u < units ? ((const piece *)(x + r * dim))[u] : piece{};
+        p[c] = here && u < units ? load_piece<T, V, TAIL>(x + r * dim, u * V, dim) : piece{};
     }
 #pragma unroll
     for (int c = 0; c < C; ++c)
@@ -67,7 +100,7 @@ __global__ __launch_bounds__(256) void norm_kernel(const T *x, const T *__restri
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float d = ((float)p[c][e] - mean) * share;
-                square += d * d;
+                if (!TAIL || (c * L + lane) * V + e < dim) square += d * d;
             }
     const float rstd = 1.f / sqrtf(sum_over<L>(square, lds[1]) + eps);
     if (!here) return;
@@ -76,8 +109,8 @@ __global__ __launch_bounds__(256) void norm_kernel(const T *x, const T *__restri
         const int u = c * L + lane;
         if (u >= units) break;
         piece o, pw, pb;
-        if (w) pw = ((const piece *)w)[u];
-        if (b) pb = ((const piece *)b)[u];
+        if (w) pw = load_piece<T, V, TAIL>(w, u * V, dim);
+        if (b) pb = load_piece<T, V, TAIL>(b, u * V, dim);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             float v = ((float)p[c][e] - mean) * rstd;
@@ -85,7 +118,7 @@ __global__ __launch_bounds__(256) void norm_kernel(const T *x, const T *__restri
             if (b) v += (float)pb[e];
             o[e] = (T)v;
         }
-        ((piece *)(y + r * dim))[u] = o;
+        store_piece<T, V, TAIL>(y + r * dim + u * V, dim - u * V, o);
     }
     if (lane == 0) {
         if (mean_out) mean_out[r] = mean;
@@ -96,7 +129,7 @@ __global__ __launch_bounds__(256) void norm_kernel(const T *x, const T *__restri
 // Rows g, g + gridDim.x, ... (256 / L at a time) for workgroup g: dx (nullable), and the workgroup's sums of dy xhat and dy for
 // every column at part[g][0 .. 1] (nullable).  With one or two pieces per lane the next row is requested before this one is
 // worked on.
-template <class T, int V, int L, int C>
+template <class T, int V, bool TAIL, int L, int C>
 __global__ __launch_bounds__(256) void norm_grad_kernel(const T *__restrict__ x, const T *__restrict__ w,
                                                         const float *__restrict__ mean_in, const float *__restrict__ rstd_in,
                                                         const T *__restrict__ dy, const T *around, long long rows, int dim,
@@ -108,7 +141,7 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const T *__restrict__ x,
     constexpr bool AHEAD = C <= 2;
     __shared__ float lds[2][2][4];
     __shared__ float columns[L > 64 ? 1 : 4 * WIDTH];
-    const int lane = threadIdx.x % L, units = dim / V;
+    const int lane = threadIdx.x % L, units = TAIL ? (dim + V - 1) / V : dim / V;
     const long long step = (long long)gridDim.x * PER;
     struct Row {
         piece x[C], dy[C], around[C];
@@ -123,9 +156,9 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const T *__restrict__ x,
         for (int c = 0; c < C; ++c) {
             const int u = c * L + lane;
             const bool in = here && u < units;
-            t.x[c] = in ? ((const piece *)(x + r * dim))[u] : piece{};
-            t.dy[c] = in ? ((const piece *)(dy + r * dim))[u] : piece{};
-            t.around[c] = in && around ? ((const piece *)(around + r * dim))[u] : piece{};
+            t.x[c] = in ? load_piece<T, V, TAIL>(x + r * dim, u * V, dim) : piece{};
+            t.dy[c] = in ? load_piece<T, V, TAIL>(dy + r * dim, u * V, dim) : piece{};
+            t.around[c] = in && around ? load_piece<T, V, TAIL>(around + r * dim, u * V, dim) : piece{};
         }
         return t;
     };
@@ -133,7 +166,7 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const T *__restrict__ x,
     float dw[C][V], db[C][V];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        pw[c] = w && c * L + lane < units ? ((const piece *)w)[c * L + lane] : piece{};
+        pw[c] = w && c * L + lane < units ? load_piece<T, V, TAIL>(w, (c * L + lane) * V, dim) : piece{};
 #pragma unroll
         for (int e = 0; e < V; ++e) dw[c][e] = db[c][e] = 0.f;
     }
@@ -172,7 +205,7 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const T *__restrict__ x,
                 if (around) v += (float)t.around[c][e];
                 o[e] = (T)v;
             }
-            ((piece *)(dx + r * dim))[u] = o;
+            store_piece<T, V, TAIL>(dx + r * dim + u * V, dim - u * V, o);
         }
     }
     if (!part) return;
@@ -185,7 +218,7 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const T *__restrict__ x,
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int e = 0; e < V; ++e)
-                    if (c * L + lane < units) to[(c * L + lane) * V + e] = v[c][e];
+                    if (TAIL ? (c * L + lane) * V + e < dim : c * L + lane < units) to[(c * L + lane) * V + e] = v[c][e];
         } else {
 #pragma unroll
             for (int c = 0; c < C; ++c)
@@ -229,7 +262,7 @@ __device__ __forceinline__ void sum_over_group(float &a, float &b, float (*lds)[
     }
 }
 
-template <class T, int V>
+template <class T, int V, bool TAIL>
 __global__ __launch_bounds__(256) void norm_long_kernel(const T *x, const T *__restrict__ w, const T *__restrict__ b,
                                                    long long rows, int dim, float eps, T *y,   // y may be x
                                                    float *__restrict__ mean_out, float *__restrict__ rstd_out)
@@ -238,11 +271,11 @@ __global__ __launch_bounds__(256) void norm_long_kernel(const T *x, const T *__r
     __shared__ float lds[4][2];
     const long long r = group_number();
     if (r >= rows) return;
-    const int units = dim / V;
-    const piece *row = (const piece *)(x + r * dim);
+    const int units = TAIL ? (dim + V - 1) / V : dim / V;
+    const T *row = x + r * dim;
     float sum = 0.f, none = 0.f;
     for (int u = threadIdx.x; u < units; u += 256) {
-        const piece p = row[u];
+        const piece p = load_piece<T, V, TAIL>(row, u * V, dim);
 #pragma unroll
         for (int e = 0; e < V; ++e) sum += (float)p[e];
     }
@@ -251,20 +284,20 @@ __global__ __launch_bounds__(256) void norm_long_kernel(const T *x, const T *__r
     float square = 0.f;
     const float share = 1.f / sqrtf((float)dim);
     for (int u = threadIdx.x; u < units; u += 256) {
-        const piece p = row[u];
+        const piece p = load_piece<T, V, TAIL>(row, u * V, dim);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const float d = ((float)p[e] - mean) * share;
-            square += d * d;
+            if (!TAIL || u * V + e < dim) square += d * d;
         }
     }
     sum_over_group(square, none, lds);
     const float rstd = 1.f / sqrtf(square + eps);
     for (int u = threadIdx.x; u < units; u += 256) {
-        const piece p = row[u];
+        const piece p = load_piece<T, V, TAIL>(row, u * V, dim);
         piece o, pw, pb;
-        if (w) pw = ((const piece *)w)[u];
-        if (b) pb = ((const piece *)b)[u];
+        if (w) pw = load_piece<T, V, TAIL>(w, u * V, dim);
+        if (b) pb = load_piece<T, V, TAIL>(b, u * V, dim);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             float v = ((float)p[e] - mean) * rstd;
@@ -272,7 +305,7 @@ __global__ __launch_bounds__(256) void norm_long_kernel(const T *x, const T *__r
             if (b) v += (float)pb[e];
             o[e] = (T)v;
         }
-        ((piece *)(y + r * dim))[u] = o;
+        store_piece<T, V, TAIL>(y + r * dim + u * V, dim - u * V, o);
     }
     if (threadIdx.x == 0) {
         if (mean_out) mean_out[r] = mean;
@@ -280,7 +313,7 @@ __global__ __launch_bounds__(256) void norm_long_kernel(const T *x, const T *__r
     }
 }
 
-template <class T, int V>
+template <class T, int V, bool TAIL>
 __global__ __launch_bounds__(256) void norm_long_dx_kernel(const T *__restrict__ x, const T *__restrict__ w,
                                                       const float *__restrict__ mean_in, const float *__restrict__ rstd_in,
                                                       const T *__restrict__ dy, const T *around, long long rows,
@@ -290,48 +323,55 @@ __global__ __launch_bounds__(256) void norm_long_dx_kernel(const T *__restrict__
     __shared__ float lds[4][2];
     const long long r = group_number();
     if (r >= rows) return;
-    const int units = dim / V;
-    const piece *px = (const piece *)(x + r * dim), *pd = (const piece *)(dy + r * dim), *pw = (const piece *)w;
-    const piece *pa = (const piece *)(around + r * dim);
+    const int units = TAIL ? (dim + V - 1) / V : dim / V;
+    x += r * dim, dy += r * dim, dx += r * dim;
+    if (around) around += r * dim;
     const float mean = mean_in[r], rstd = rstd_in[r];
     float s1 = 0.f, s2 = 0.f;
-    for (int u = threadIdx.x; u < units; u += 256)
+    for (int u = threadIdx.x; u < units; u += 256) {
+        const piece px = load_piece<T, V, TAIL>(x, u * V, dim), pd = load_piece<T, V, TAIL>(dy, u * V, dim);
+        piece pw;
+        if (w) pw = load_piece<T, V, TAIL>(w, u * V, dim);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const float g = (float)pd[u][e] * (w ? (float)pw[u][e] : 1.f);
+            const float g = (float)pd[e] * (w ? (float)pw[e] : 1.f);
             s1 += g;
-            s2 += g * (((float)px[u][e] - mean) * rstd);
+            s2 += g * (((float)px[e] - mean) * rstd);
         }
+    }
     sum_over_group(s1, s2, lds);
     s1 /= (float)dim;
     s2 /= (float)dim;
     for (int u = threadIdx.x; u < units; u += 256) {
-        piece o;
+        const piece px = load_piece<T, V, TAIL>(x, u * V, dim), pd = load_piece<T, V, TAIL>(dy, u * V, dim);
+        piece pw, pa, o;
+        if (w) pw = load_piece<T, V, TAIL>(w, u * V, dim);
+        if (around) pa = load_piece<T, V, TAIL>(around, u * V, dim);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const float g = (float)pd[u][e] * (w ? (float)pw[u][e] : 1.f);
-            float v = rstd * (g - s1 - ((float)px[u][e] - mean) * rstd * s2);
-            if (around) v += (float)pa[u][e];
+            const float g = (float)pd[e] * (w ? (float)pw[e] : 1.f);
+            float v = rstd * (g - s1 - ((float)px[e] - mean) * rstd * s2);
+            if (around) v += (float)pa[e];
             o[e] = (T)v;
         }
-        ((piece *)(dx + r * dim))[u] = o;
+        store_piece<T, V, TAIL>(dx + u * V, dim - u * V, o);
     }
 }
 
 // part[g][0][c], part[g][1][c]: the sums of dy xhat and of dy over the rows r = g, g + gridDim.y, ...; a thread has V columns
-template <class T, int V>
+template <class T, int V, bool TAIL>
 __global__ __launch_bounds__(256) void norm_columns_kernel(const T *__restrict__ x, const float *__restrict__ mean,
                                                            const float *__restrict__ rstd, const T *__restrict__ dy,
                                                            long long rows, int dim, float *__restrict__ part)
 {
     typedef typename Piece<T, V>::type piece;
     const int u = (int)(blockIdx.x * 256 + threadIdx.x);
-    if (u >= dim / V) return;
+    if (u >= (TAIL ? (dim + V - 1) / V : dim / V)) return;
     float dw[V], db[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) dw[e] = db[e] = 0.f;
     for (long long r = blockIdx.y; r < rows; r += gridDim.y) {
-        const piece px = ((const piece *)(x + r * dim))[u], pd = ((const piece *)(dy + r * dim))[u];
+        const piece px = load_piece<T, V, TAIL>(x + r * dim, u * V, dim), pd = load_piece<T, V, TAIL>(dy + r * dim, u * V, dim);
         const float m = mean[r], s = rstd[r];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
@@ -341,6 +381,7 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(const T *__restrict__
     }
 #pragma unroll
     for (int e = 0; e < V; ++e) {
+        if (TAIL && u * V + e >= dim) break;
         part[((long long)blockIdx.y * 2) * dim + u * V + e] = dw[e];
         part[((long long)blockIdx.y * 2 + 1) * dim + u * V + e] = db[e];
     }
@@ -386,18 +427,22 @@ static size_t norm_backward_space(int64_t rows, int32_t dim)
     return ((size_t)norm_groups(rows) * 2 * dim * 4 + 255) & ~(size_t)255;
 }
 
-// calls f with the values of a load as a type: 16 bytes, 8 (bf16) or one value, as `addresses` and dim allow
-template <int V>
+// Calls f with the values of a load as a type: 16 bytes, or 8 (bf16), where rows are whole ones of those, aligned; else single
+// values in short rows and 16 bytes wherever they lie in long ones.  us forward + backward, singly / in 16 bytes: 20 000 rows of 301,
+// float 13 + 21 / 13 + 23, bf16 12 + 20 / 14 + 27; 40 000 of 75, float 11 + 16 / 12 + 24; 8000 of 1001, bf16 15 + 30 / 13 + 25; of 4097,
+// bf16 48 + 363 / 31 + 89; of 2050, float 27 + 158 / 27 + 55.
+template <int V, bool TAIL>
 struct Width {
     static constexpr int value = V;
+    static constexpr bool tail = TAIL;
 };
 template <class T, class F>
 static hipError_t by_width(uintptr_t addresses, int32_t dim, F f)
 {
     constexpr int MOST = 16 / (int)sizeof(T);
-    if (dim % MOST == 0 && addresses % 16 == 0) return f(Width<MOST>());
-    if (MOST == 8 && dim % 4 == 0 && addresses % 8 == 0) return f(Width<4>());
-    return f(Width<1>());
+    if (dim % MOST == 0 && addresses % 16 == 0) return f(Width<MOST, false>());
+    if (MOST == 8 && dim % 4 == 0 && addresses % 8 == 0) return f(Width<4, false>());
+    return dim <= 512 ? f(Width<1, false>()) : f(Width<MOST, true>());
 }
 
 // Calls f with the lanes that share a row of `units` pieces and the pieces of each as a type; false: a row is too long for that.
@@ -410,9 +455,9 @@ template <int L, int C>
 struct Lanes {
     static constexpr int lanes = L, pieces = C;
 };
-constexpr int longest(int v) { return v == 1 ? 8192 : 2048; }
-template <int V, class F>
-static bool by_lanes(int units, int64_t rows, hipError_t &st, F f)
+constexpr int LONGEST = 2048;
+template <class F>
+static bool by_lanes(int units, bool singly, int64_t rows, hipError_t &st, F f)
 {
     const bool many = rows >= 2048;
     if (many && units > 32 && units <= 64) {
@@ -423,8 +468,8 @@ static bool by_lanes(int units, int64_t rows, hipError_t &st, F f)
         st = f(Lanes<32, 3>());
     } else if (many && units > 128 && units <= 256) {
         st = f(Lanes<64, 4>());
-    } else if (many && V == 1 && units > 256 && units <= 512) {   // single values: a wavefront's registers hold them easily
-        st = units <= 320 ? f(Lanes<64, V == 1 ? 5 : 4>()) : f(Lanes<64, V == 1 ? 8 : 4>());
+    } else if (many && units > 256 && singly) {   // single values: a wavefront's registers hold them easily
+        st = units <= 320 ? f(Lanes<64, 5>()) : f(Lanes<64, 8>());
     } else {
         st = units <= 4      ? f(Lanes<4, 1>())
              : units <= 8    ? f(Lanes<8, 1>())
@@ -435,11 +480,10 @@ static bool by_lanes(int units, int64_t rows, hipError_t &st, F f)
              : units <= 256  ? f(Lanes<256, 1>())
              : units <= 512  ? f(Lanes<256, 2>())
              : units <= 1024 ? f(Lanes<256, 4>())
-             : units <= 2048 ? f(Lanes<256, 8>())
-             : units <= longest(V) ? (units <= 4096 ? f(Lanes<256, V == 1 ? 16 : 8>()) : f(Lanes<256, V == 1 ? 32 : 8>()))
+             : units <= LONGEST ? f(Lanes<256, 8>())
                              : hipSuccess;
     }
-    return units <= longest(V);
+    return units <= LONGEST;
 }
 
 template <class T>
@@ -448,15 +492,16 @@ static lcn_status norm_as(const T *x, const T *w, const T *b, int64_t rows, int3
 {
     OPCHK(by_width<T>((uintptr_t)x | (uintptr_t)w | (uintptr_t)b | (uintptr_t)y, dim, [&](auto v) {
         constexpr int V = decltype(v)::value;
+        constexpr bool TAIL = decltype(v)::tail;
         hipError_t st;
-        if (by_lanes<V>(dim / V, rows, st, [&](auto l) {
+        if (by_lanes((dim + V - 1) / V, V == 1, rows, st, [&](auto l) {
                 constexpr int L = decltype(l)::lanes, C = decltype(l)::pieces;
-                hipLaunchKernelGGL((norm_kernel<T, V, L, C>), grid_of((rows + 256 / L - 1) / (256 / L)), dim3(256), 0, s, x, w, b,
+                hipLaunchKernelGGL((norm_kernel<T, V, TAIL, L, C>), grid_of((rows + 256 / L - 1) / (256 / L)), dim3(256), 0, s, x, w, b,
                                    (long long)rows, dim, eps, y, mean, rstd);
                 return hipGetLastError();
             }))
             return st;
-        hipLaunchKernelGGL((norm_long_kernel<T, V>), grid_of(rows), dim3(256), 0, s, x, w, b, (long long)rows, dim, eps, y, mean, rstd);
+        hipLaunchKernelGGL((norm_long_kernel<T, V, TAIL>), grid_of(rows), dim3(256), 0, s, x, w, b, (long long)rows, dim, eps, y, mean, rstd);
         return hipGetLastError();
     }));
     return LCN_OK;
@@ -472,21 +517,22 @@ static lcn_status norm_backward_as(const T *x, const T *w, const float *mean, co
     int groups = most;
     OPCHK(by_width<T>(all, dim, [&](auto v) {
         constexpr int V = decltype(v)::value;
+        constexpr bool TAIL = decltype(v)::tail;
         hipError_t st;
-        if (by_lanes<V>(dim / V, rows, st, [&](auto l) {
+        if (by_lanes((dim + V - 1) / V, V == 1, rows, st, [&](auto l) {
                 constexpr int L = decltype(l)::lanes, C = decltype(l)::pieces;
                 const int64_t needed = (rows + 256 / L - 1) / (256 / L);
                 groups = (int)(needed < most ? needed : most);
-                hipLaunchKernelGGL((norm_grad_kernel<T, V, L, C>), dim3((unsigned)groups), dim3(256), 0, s, x, w, mean, rstd, dy, around,
+                hipLaunchKernelGGL((norm_grad_kernel<T, V, TAIL, L, C>), dim3((unsigned)groups), dim3(256), 0, s, x, w, mean, rstd, dy, around,
                                    (long long)rows, dim, dx, sums ? part : nullptr);
                 return hipGetLastError();
             }))
             return st;
-        if (dx) hipLaunchKernelGGL((norm_long_dx_kernel<T, V>), grid_of(rows), dim3(256), 0, s, x, w, mean, rstd, dy, around,
+        if (dx) hipLaunchKernelGGL((norm_long_dx_kernel<T, V, TAIL>), grid_of(rows), dim3(256), 0, s, x, w, mean, rstd, dy, around,
                                    (long long)rows, dim, dx);
         st = hipGetLastError();
         if (st != hipSuccess || !sums) return st;
-        hipLaunchKernelGGL((norm_columns_kernel<T, V>), dim3((unsigned)((dim / V + 255) / 256), (unsigned)groups), dim3(256), 0, s, x,
+        hipLaunchKernelGGL((norm_columns_kernel<T, V, TAIL>), dim3((unsigned)(((dim + V - 1) / V + 255) / 256), (unsigned)groups), dim3(256), 0, s, x,
                            mean, rstd, dy, (long long)rows, dim, part);
         return hipGetLastError();
     }));

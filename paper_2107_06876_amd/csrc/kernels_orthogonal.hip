@@ -47,7 +47,7 @@ __global__ __launch_bounds__(256) void squares_kernel(const T *__restrict__ g, l
 // SCALE_X / 2 and SCALE_X, in one plane, which holds it (values below 2^-30 |G| to 2^-38 |G|), and what is left of the factor in `ratio`.
 template <class T>
 __global__ __launch_bounds__(256) void normalise_kernel(const T *__restrict__ g, const double *__restrict__ part, int rows, int cols,
-                                                        float eps, int whole, Planes out, float *__restrict__ ratio)
+                                                        float eps, Planes out, float *__restrict__ ratio)
 {
     double sum = 0.0;
     for (int i = 0; i < NORM_GROUPS; ++i) sum += part[blockIdx.y * NORM_GROUPS + i];
@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256) void normalise_kernel(const T *__restrict__ g,
         const long long r = t / per_row;
         const int k = (int)(t - r * per_row) * 8;
         f32x4 v[2];
-        load_eight(src + r * cols + k, cols - k, whole, v);
+        load_eight(src + r * cols + k, cols - k, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float x = v[e >> 2][e & 3];
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256) void normalise_kernel(const T *__restrict__ g,
 // 3.6 of them start, loads and stores (on the float instruction 14.3); 8 of 256 x 64, 30 us (75).
 template <class T, int D, int ROWS>
 __global__ __launch_bounds__(512) void orthogonal_small_kernel(const T *__restrict__ g, int rows, int cols, int steps, SmallSteps c,
-                                                               float eps, float scale, int whole, T *out)   // out may be g
+                                                               float eps, float scale, T *out)   // out may be g
 {
     typedef Tile<__bf16, D> L;   // of any 16-bit values
     constexpr int N = D / 16;
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(512) void orthogonal_small_kernel(const T *__restri
     double sum = 0.0;
     for (int i = tid; i < limit; i += 512) {
         f32x4 v[2];
-        load_eight(src + index_of(i), left_of(i), whole, v);
+        load_eight(src + index_of(i), left_of(i), v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum = __builtin_fma((double)v[e >> 2][e & 3], (double)v[e >> 2][e & 3], sum);
     }
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(512) void orthogonal_small_kernel(const T *__restri
         const int r = row_of(i), k = col_of(i);
         f32x4 v[2];
         f16x8 h, q;
-        load_eight(src + index_of(i), left_of(i), whole, v);
+        load_eight(src + index_of(i), left_of(i), v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float x = v[e >> 2][e & 3], y = plain ? x * factor : (float)((double)x * inv);
@@ -258,7 +258,7 @@ __global__ __launch_bounds__(512) void orthogonal_small_kernel(const T *__restri
         f32x4 v[2];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e >> 2][e & 3] = ((float)h[e] + (float)q[e]) * (scale / SCALE_X);
-        store_eight(dst + index_of(i), v, left_of(i), whole);
+        store_eight(dst + index_of(i), v, left_of(i));
     }
 }
 
@@ -317,13 +317,13 @@ static lcn_status small_as(const T *g, int64_t count, int32_t rows, int32_t cols
     SmallSteps k{};
     for (int i = 0; i < steps; ++i)
         for (int e = 0; e < 3; ++e) k.c[i][e] = c[3 * i + e];
-    const int32_t lo = rows < cols ? rows : cols, whole = whole_rows<T>((const void *)((uintptr_t)g | (uintptr_t)out), cols);
+    const int32_t lo = rows < cols ? rows : cols;
     if (lo <= 32)
         hipLaunchKernelGGL((orthogonal_small_kernel<T, 32, 512>), dim3((unsigned)count), dim3(512), 0, s, g, rows, cols, steps, k, eps,
-                           scale, whole, out);
+                           scale, out);
     else
         hipLaunchKernelGGL((orthogonal_small_kernel<T, 64, 256>), dim3((unsigned)count), dim3(512), 0, s, g, rows, cols, steps, k, eps,
-                           scale, whole, out);
+                           scale, out);
     OPCHK(hipGetLastError());
     return LCN_OK;
 }
@@ -393,7 +393,7 @@ static lcn_status orthogonal_as(const T *g, int64_t count, int32_t rows, int32_t
         Planes to = x[0];
         to.p += first * rows * o.ld;
         hipLaunchKernelGGL(normalise_kernel<T>, dim3((unsigned)(groups < 1024 ? groups : 1024), some), dim3(256), 0, s, g + first * size,
-                           o.part + first * NORM_GROUPS, rows, cols, eps, whole_rows<T>(g, cols), to, o.ratio + first);
+                           o.part + first * NORM_GROUPS, rows, cols, eps, to, o.ratio + first);
         OPCHK(hipGetLastError());
     }
     auto operand = [](const Planes &m) { return Operand{m.p, m.plane * 2, m.ld}; };
@@ -458,7 +458,7 @@ static lcn_status orthogonal_as(const T *g, int64_t count, int32_t rows, int32_t
         if (i < steps)
             OPCHK(launch_apply(o.plan_apply, p, {x[1], x_batch, 1.f / SCALE_B, ratio}, wide, how, s));
         else
-            OPCHK(launch_apply_last(o.plan_apply, p, {out, size, cols, scale / (SCALE_B * SCALE_X), ratio, whole_rows<T>(out, cols)},
+            OPCHK(launch_apply_last(o.plan_apply, p, {out, size, cols, scale / (SCALE_B * SCALE_X), ratio},
                                     wide, how, s));
         const Planes t = x[0];
         x[0] = x[1];

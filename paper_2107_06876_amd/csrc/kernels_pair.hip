@@ -177,7 +177,7 @@ struct LastEpilogue {
                 region, col, lane, [](int, int) { return Nothing{}; },
                 [&](int r, int c, f32x4 (&v)[2], Nothing) {
                     const int n = n0 + j * 16 + r, m = m0 + c;
-                    if (n < p.n && m < p.m) store_eight(out + n * e.ld + m, v, p.m - m, e.whole);
+                    if (n < p.n && m < p.m) store_eight(out + n * e.ld + m, v, p.m - m);
                 });
         }
     }

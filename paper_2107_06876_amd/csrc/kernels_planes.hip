@@ -19,8 +19,7 @@ __global__ __launch_bounds__(256) void planes_kernel(PlaneJobs jobs)
         const int k = (int)(t - r * per_row) * 8;
         const T *p = (const T *)j.src + r * j.d + k;
         f32x4 v[2];
-        v[0] = load_four(p, j.d - k, j.vec);
-        v[1] = load_four(p + 4, j.d - k - 4, j.vec);
+        load_eight(p, j.d - k, v);
         if (j.target && j.target[r] < 0) v[0] = v[1] = f32x4{0.f, 0.f, 0.f, 0.f};
         bf16x8 o[3];
 #pragma unroll
@@ -41,7 +40,6 @@ __global__ __launch_bounds__(256) void planes_kernel(PlaneJobs jobs)
 
 Operand add_masked(PlaneJobs &jobs, const void *p, long long rows, int d, int32_t dtype, const int64_t *target, void *space)
 {
-    const size_t e = dtype == LCN_F32 ? 4 : 2;
     const long long groups = (rows * (padded(d) / 8) + 255) / 256;
     PlaneJobs::Job &j = jobs.job[jobs.count];
     j.src = p;
@@ -50,7 +48,6 @@ Operand add_masked(PlaneJobs &jobs, const void *p, long long rows, int d, int32_
     j.rows = rows;
     j.d = d;
     j.dp = (int)padded(d);
-    j.vec = d % 4 == 0 && ((uintptr_t)p & (4 * e - 1)) == 0;
     j.end = (jobs.count ? jobs.job[jobs.count - 1].end : 0) + (unsigned)(groups < 8192 ? groups : 8192);
     ++jobs.count;
     return plane_operand(space, rows, d);
@@ -77,7 +74,7 @@ hipError_t launch_planes(const PlaneJobs &jobs, int32_t dtype, hipStream_t s)
 template <class T>
 __global__ __launch_bounds__(256) void add_partials_kernel(const float *__restrict__ part, int splits, long long stride,
                                                            long long n, int m, long long ldp, float scale,
-                                                           T *__restrict__ out, int whole)
+                                                           T *__restrict__ out)
 {
     const int per_row = (m + 3) / 4;
     for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < n * per_row; t += (long long)gridDim.x * 256) {
@@ -86,7 +83,7 @@ __global__ __launch_bounds__(256) void add_partials_kernel(const float *__restri
         f32x4 v = *(const f32x4 *)(part + r * ldp + c);
 #pragma unroll 8   // loads ahead of the sums
         for (int u = 1; u < splits; ++u) v += *(const f32x4 *)(part + u * stride + r * ldp + c);
-        store_four(out + r * m + c, v * scale, m - c, whole);
+        store_four(out + r * m + c, v * scale, m - c);
     }
 }
 
@@ -95,14 +92,12 @@ hipError_t launch_add_partials(const float *part, int splits, long long n, int m
 {
     const long long groups = (n * ((m + 3) / 4) + 255) / 256;
     const unsigned grid = (unsigned)(groups < 8192 ? groups : 8192);
-    const size_t e = dtype == LCN_F32 ? 4 : 2;
-    const int whole = m % 4 == 0 && ((uintptr_t)out & (4 * e - 1)) == 0;
     if (dtype == LCN_F32)
         hipLaunchKernelGGL(add_partials_kernel<float>, dim3(grid), dim3(256), 0, s, part, splits, n * ldp, n, m, ldp, scale,
-                           (float *)out, whole);
+                           (float *)out);
     else
         hipLaunchKernelGGL(add_partials_kernel<__bf16>, dim3(grid), dim3(256), 0, s, part, splits, n * ldp, n, m, ldp, scale,
-                           (__bf16 *)out, whole);
+                           (__bf16 *)out);
     return hipGetLastError();
 }
 
@@ -177,8 +172,8 @@ hipError_t launch_scaled(const ProductPlan &plan, const ProductArgs &p, float sc
         return launch_add_partials(part, plan.splits, p.n, p.m, ldp, scale, dtype, out, s);
     }
     if (dtype == LCN_F32)
-        return launch_planned<3, ACOL, BCOL, ScaledEpilogue<float>>(plan, p, {(float *)out, p.m, scale, whole_rows<float>(out, p.m)}, s);
-    return launch_planned<1, ACOL, BCOL, ScaledEpilogue<__bf16>>(plan, p, {(__bf16 *)out, p.m, scale, whole_rows<__bf16>(out, p.m)}, s);
+        return launch_planned<3, ACOL, BCOL, ScaledEpilogue<float>>(plan, p, {(float *)out, p.m, scale}, s);
+    return launch_planned<1, ACOL, BCOL, ScaledEpilogue<__bf16>>(plan, p, {(__bf16 *)out, p.m, scale}, s);
 }
 template hipError_t launch_scaled<true, false>(const ProductPlan &, const ProductArgs &, float, int32_t, void *, float *,
                                                hipStream_t);

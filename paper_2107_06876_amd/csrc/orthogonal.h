@@ -93,7 +93,6 @@ struct LastArgs {
     long long batch, ld;
     float factor;
     const float *ratio;
-    int whole;
 };
 // wide: both operands lie with k contiguous, else with their own index
 hipError_t launch_gram(const PairPlan &plan, const PairArgs &p, const GramArgs &e, bool wide, int planes, hipStream_t s);

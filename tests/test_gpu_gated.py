@@ -100,6 +100,21 @@ def test_narrow_layers(rows, d_in, d_out, act, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,d_in,d_out", [(300, 33, 64), (5000, 61, 50), (129, 1, 3), (128, 63, 1), (4097, 31, 63), (200, 30, 7)])
+def test_narrow_layers_of_odd_widths(rows, d_in, d_out, dtype):
+    """Rows that are no whole pieces, from addresses that are none either."""
+    check(rows, d_in, d_out, "silu", dtype)
+    check(rows, d_in, d_out, "tanh", dtype, bias=False, shift=1)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,d_in,d_out", [(1, 2047, 333), (2, 1025, 100), (4, 519, 61), (8, 2051, 77), (3, 7, 9), (1, 129, 16)])
+def test_few_rows_of_odd_widths(rows, d_in, d_out, dtype):
+    check(rows, d_in, d_out, "silu", dtype)
+    check(rows, d_in, d_out, "gelu", dtype, shift=1)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("rows,d_in,d_out", [(300, 32, 64), (1000, 64, 33)])
 def test_single_gradients_of_narrow_layers(rows, d_in, d_out, dtype):
     x, w, b, dy = inputs(rows, d_in, d_out, dtype)

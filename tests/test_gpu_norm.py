@@ -85,6 +85,18 @@ def test_many_rows(rows, dim, dtype):
     check(rows, dim, dtype)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,dim", [(2100, 513), (300, 515), (2050, 767), (70, 1023), (2048, 2049), (40, 4099), (20, 8190), (9, 8195), (5, 16385)])
+def test_long_rows_of_odd_widths(rows, dim, dtype):
+    """Pieces of 16 bytes wherever they lie, of the last one only what exists; with what stands behind the last row left as it was."""
+    check(rows, dim, dtype)
+    y = check(rows, dim, dtype, shift=1)[0]
+    x, w, b, _, _ = inputs(rows, dim, dtype, shift=1)
+    room = torch.full((rows * dim + 64,), 7.0, dtype=dtype, device=DEV)
+    assert torch.equal(lcn.lcn_layer_norm(x, w, b, eps=EPS, out=room[:rows * dim].view(rows, dim)), y)
+    assert (room[rows * dim:] == 7.0).all()
+
+
 def test_only_a_weight_or_only_a_bias():
     x, w, b, dy, _ = inputs(50, 96, F32)
     assert off(lcn.lcn_layer_norm(x, w), oracle(x, w, None, dy, None)[0]) <= bound(F32, 96)

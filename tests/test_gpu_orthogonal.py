@@ -74,6 +74,13 @@ def test_long_matrices(rows, cols, dtype):
     check(rows, cols, dtype)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(640, 640), (621, 707), (100, 4000), (35, 600), (5001, 161), (300, 300), (900, 890), (33, 1037)])
+def test_small_tiles(rows, cols, dtype):
+    """Few tiles: all of a symmetric product, its half written twice, sums split over workgroups."""
+    check(rows, cols, dtype)
+
+
 @pytest.mark.parametrize("rows,cols", [(2048, 2304), (2311, 1100)])
 def test_large_tiles(rows, cols):
     check(rows, cols, BF16, steps=3)
