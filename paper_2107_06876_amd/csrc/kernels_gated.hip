@@ -303,6 +303,9 @@ static bool gated_args_fit(int64_t rows, int32_t d_in, int32_t d_out, int32_t dt
 // A product in two launches where that is estimated to be faster: whole rounds of workgroups of one shape, and the columns behind
 // them by another, whose k may be split.  20 000 float rows: 1024 -> 300, 111 us by 64 x 64 tiles in three rounds, 105 as one round of
 // 320 x 64 and the rest; 16391 bf16 rows, 8192 -> 1024: the 7 rows behind 16384 took 64 us in one piece of k, 12 in 32.
+// More than 640 tiles of 64 x 64 are taken as 15 % slower than product_us says (with the gates' epilogue, and on rows that are no whole
+// lines): by them / by larger ones, us, dx of 4000 rows, 4006 -> 1001 bf16, 72 / 57, of 2048, 4096 -> 2048, 58 / 49; y of 9001, 517 -> 301
+// float 66 / 52; of 512 tiles, dz and dx of 2048, 2048 -> 1024 bf16, 31 / 35.
 struct Columns {
     ProductPlan main, rest;
     long long whole, n;
@@ -313,15 +316,24 @@ static Columns plan_columns(Carver &c, long long m, long long n, long long k, in
     Columns r{};
     r.main = plan_product(m, n, k, planes, true, false, may_320);
     r.n = r.whole = n;
-    double least = r.main.us;
+    auto weighed = [&](int t, double us, long long columns) {
+        return t == TILE_64 && (m + 63) / 64 * ((columns + 63) / 64) > 640 ? 1.15 * us : us;
+    };
+    double least = weighed(r.main.tile, r.main.us, n);
     for (int t = 0; t < TILE_COUNT; ++t) {
         if (t == TILE_320 && !may_320) continue;
+        const double alone = weighed(t, product_us(t, m, n, k, planes, 1), n);
+        if (alone < least) {
+            least = alone;
+            r.main = ProductPlan{t, 1, false, alone};
+            r.whole = n;
+        }
         const long long across = (m + tile_m(t) - 1) / tile_m(t), round = product_room(t, planes) / across * tile_n(t, planes);
         const long long tiles = n - n % tile_n(t, planes);   // whole tiles, and whole rounds of them
         for (long long whole : {tiles, round > 0 ? n - n % round : 0}) {
             if (whole <= 0 || whole >= n) continue;
             const ProductPlan rest = plan_product(m, n - whole, k, planes, true, false, may_320);
-            const double us = product_us(t, m, whole, k, planes, 1) + 3.0 + rest.us;
+            const double us = weighed(t, product_us(t, m, whole, k, planes, 1), whole) + 3.0 + rest.us;
             if (us < least) {
                 least = us;
                 r.main = ProductPlan{t, 1, false, us};
@@ -376,8 +388,12 @@ static GatedBackward gated_backward_space(char *ws, int64_t rows, int32_t d_in, 
     GatedBackward b;
     const int32_t wide = 2 * d_out;
     b.planes = gradient_planes(rows, dtype);
-    // enough workgroups to fill the chip, at most 256 partial sums per column
-    b.rows_each = (int)((((rows + 255) / 256) + 31) & ~31LL);
+    // workgroups of dz: 256 columns each, and so many rows that there are some ten to a compute unit, with up to 512 partial sums per
+    // column (13 502 rows of 211 in bf16: 211 workgroups 25 us, 422 16; 2000 of 512 floats, 126 13, 500 8; 16 391 of 4096 in bf16, 2736 138,
+    // 3648 144)
+    const int64_t blocks = (d_out + 255) / 256, most = blocks > 20 ? 128 : blocks > 5 ? 2720 / blocks : 512;
+    const int64_t unit = d_out <= 64 ? 32 : d_out <= 128 ? 16 : 8;   // rows at a time
+    b.rows_each = (int)(((rows + most - 1) / most + unit - 1) / unit * unit);
     b.groups = (int)((rows + b.rows_each - 1) / b.rows_each);
     b.xp = c.take(planes_bytes(rows, d_in, planes_of(dtype)));
     b.wp = c.take(planes_bytes(wide, d_in, planes_of(dtype)));
