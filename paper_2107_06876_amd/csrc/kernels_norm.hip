@@ -7,8 +7,8 @@
 // Bound by memory: a row is read once and stays in registers (so its variance is formed from differences to its mean), by as
 // many lanes as hold it in 16-byte pieces: 4 to 64, so that a wavefront has several narrow rows, or a workgroup.  Backward, a
 // thread keeps its columns from row to row and adds up dw and db for them; a workgroup leaves one partial sum per column.
-// 16 391 rows of 4096 bf16 values: forward 50 us (5.4 TB/s), backward 106 (3.8 TB/s: three streams in, one out) and 7 for the
-// join; 40 961 rows of 32 floats 4.5 and 6.5 + 3, of which a launch
+// 16 391 rows of 4096 bf16 values: forward 43 to 51 us (5.3 TB/s or more), backward 92 to 107 (5.0 TB/s: three streams in, one
+// out) and 7 for the join; 40 961 rows of 32 floats 4.5 and 6.5 + 3, of which a launch
 // is 2.5.  Rows too long for that are read by a workgroup in a loop, several times, with the sums over rows in a kernel of their own.
 #include "operators.h"
 
