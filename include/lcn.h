@@ -500,7 +500,7 @@ lcn_status lcn_attention_backward(const lcn_attention_desc *desc, const void *q,
  * says): g and u for the backward pass, in a layout of the library's own: floats with float tensors; with bf16
  * tensors 16 bits a value, within 2^-14 of the power of two above the largest of eight neighbours.
  * Sizes: 0 <= rows <= 2^30, 1 <= d_in <= 2^20, 1 <= d_out <= 2^19, rows times d_in or 2 d_out <= 2^42.  The
- * forward pass needs no workspace for up to 8 rows and in narrow layers (the call says 0 bytes). */
+ * forward pass needs no workspace for few rows and in narrow layers (the call says 0 bytes). */
 lcn_status lcn_gated_linear_workspace_bytes(int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype, int32_t backward,
                                             size_t *bytes);
 lcn_status lcn_gated_linear_kept_bytes(int64_t rows, int32_t d_out, int32_t dtype, size_t *bytes);

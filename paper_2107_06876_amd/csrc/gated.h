@@ -131,7 +131,10 @@ struct GatedArgs {
 
 // Narrow layers (kernels_gated_narrow.hip): up to 64 inputs and outputs, on many rows.
 bool gated_narrow(int64_t rows, int32_t d_in, int32_t d_out);
-// workgroups of the backward pass, each of which leaves partial sums of dW and db, 2 d_out (d_in + 1) floats
+// Some rows of floats (the same file), more than FEW_ROWS.
+bool gated_some(int64_t rows, int32_t d_in, int32_t dtype);
+hipError_t launch_gated_some(const GatedArgs<float> &e, const float *x, const float *w, int rows, int d_in, int d_out, hipStream_t s);
+// workgroups of the backward pass of narrow layers, each of which leaves partial sums of dW and db, 2 d_out (d_in + 1) floats
 int gated_narrow_groups(int64_t rows);
 template <class T>
 hipError_t launch_gated_narrow(const GatedArgs<T> &e, const T *x, const T *w, int64_t rows, int32_t d_in, int32_t d_out, hipStream_t s);

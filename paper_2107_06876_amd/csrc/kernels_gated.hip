@@ -420,6 +420,11 @@ static lcn_status gated_as(const T *x, const T *w, const T *bias, int64_t rows, 
                        : launch_few<T, 8>(e, x, w, r, d_in, d_out, s));
         return LCN_OK;
     }
+    if constexpr (sizeof(T) == 4)
+        if (gated_some(rows, d_in, dtype)) {
+            OPCHK(launch_gated_some(e, x, w, (int)rows, d_in, d_out, s));
+            return LCN_OK;
+        }
     if (gated_narrow(rows, d_in, d_out)) {
         OPCHK(launch_gated_narrow(e, x, w, rows, d_in, d_out, s));
         return LCN_OK;
@@ -539,7 +544,7 @@ lcn_status lcn_gated_linear_workspace_bytes(int64_t rows, int32_t d_in, int32_t 
 {
     if (!bytes || !gated_args_fit(rows, d_in, d_out, dtype)) return LCN_ERR_INVALID_ARG;
     *bytes = 0;
-    if (rows == 0 || (!backward && (rows <= FEW_ROWS || gated_narrow(rows, d_in, d_out)))) return LCN_OK;
+    if (rows == 0 || (!backward && (rows <= FEW_ROWS || gated_some(rows, d_in, dtype) || gated_narrow(rows, d_in, d_out)))) return LCN_OK;
     *bytes = backward ? gated_backward_space(nullptr, rows, d_in, d_out, dtype).bytes
                       : gated_forward_space(nullptr, rows, d_in, d_out, dtype).bytes;
     return LCN_OK;

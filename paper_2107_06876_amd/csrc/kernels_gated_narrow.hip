@@ -11,6 +11,7 @@
 namespace lcn {
 
 constexpr int NARROW = 64;   // inputs, outputs
+constexpr int SOME_ROWS = 64;
 
 // values d0 .. d0 + 7 of a row (nullptr: zeros)
 template <class T>
@@ -90,6 +91,68 @@ __global__ __launch_bounds__(256) void gated_narrow_kernel(GatedArgs<T> e, const
             for (int u = 0; u < 4; ++u) y[u] = gate<T, ACT>(z[0][i][u]) * z[1][i][u];
             store_four(e.y + n * width + m, y, width - m);
         }
+    }
+}
+
+// Some rows, up to 16 N of floats: bound by reading W once, which through planes is read, written and read.  A workgroup has 16 outputs;
+// its wavefronts share k, 32 values of it at a time straight from memory into the float instruction, and add up through LDS.  us, so /
+// through planes: 16 rows, 576 -> 4096, 7 / 27, 64 15 / 27; 16, 4096 -> 1024, 32 / 41, 32 44 / 41; 64, 1024 -> 8192, 34 / 55, 2048 -> 2048 37 / 37.
+template <int ACT, int N>
+__global__ __launch_bounds__(256) void gated_some_kernel(GatedArgs<float> e, const float *__restrict__ x, const float *__restrict__ w,
+                                                         int rows, int k, int width)
+{
+    __shared__ f32x4 sums[4][2][N][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, g = lane >> 4, m0 = (int)blockIdx.x * 16, wp = (int)padded(width);
+    const float *rw[2], *rx[N];   // nullptr: a row of zeros
+#pragma unroll
+    for (int h = 0; h < 2; ++h) rw[h] = m0 + l < width ? w + (long long)(h * width + m0 + l) * k : nullptr;
+#pragma unroll
+    for (int t = 0; t < N; ++t) rx[t] = t * 16 + l < rows ? x + (long long)(t * 16 + l) * k : nullptr;
+    struct Chunk {
+        Frag<float>::type w[2], x[N];
+    };
+    auto read = [&](int c, Chunk &v) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) v.w[h] = fragment_of(rw[h], 32 * c + 8 * g, k);
+#pragma unroll
+        for (int t = 0; t < N; ++t) v.x[t] = fragment_of(rx[t], 32 * c + 8 * g, k);
+    };
+    f32x4 z[2][N];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < N; ++t) z[h][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int chunks = (k + 31) / 32;
+    Chunk next;
+    read(wave, next);   // zeros behind k
+    for (int c = wave; c < chunks; c += 4) {
+        const Chunk now = next;
+        read(c + 4, next);   // while this one is worked on
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int t = 0; t < N; ++t) mma(z[h][t], now.w[h], now.x[t]);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < N; ++t) sums[wave][h][t][lane] = z[h][t];
+    __syncthreads();
+    const int m = m0 + 4 * g;
+    for (int t = wave; t < N; t += 4) {
+        const int n = t * 16 + l;
+        if (n >= rows || m >= wp) continue;
+        f32x4 v[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            v[h] = (sums[0][h][t][lane] + sums[1][h][t][lane]) + (sums[2][h][t][lane] + sums[3][h][t][lane]);
+            if (e.bias && m < width) v[h] += load_four(e.bias + h * width + m, width - m);
+            if (e.kept) *(f32x4 *)(e.kept + (n * 2LL + h) * wp + m) = v[h];
+        }
+        if (m >= width) continue;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[0][u] = gate<float, ACT>(v[0][u]) * v[1][u];
+        store_four(e.y + (long long)n * width + m, v[0], width - m);
     }
 }
 
@@ -280,6 +343,23 @@ __global__ __launch_bounds__(256) void gated_narrow_join_kernel(const float *__r
 }
 
 // ---- host ---------------------------------------------------------------------
+
+bool gated_some(int64_t rows, int32_t d_in, int32_t dtype)
+{
+    return dtype == LCN_F32 && rows <= SOME_ROWS && (rows <= 16 ? 1 : rows <= 32 ? 2 : 4) * (int64_t)d_in <= 4096;
+}
+
+hipError_t launch_gated_some(const GatedArgs<float> &e, const float *x, const float *w, int rows, int d_in, int d_out, hipStream_t s)
+{
+    return by_activation(e.act, [&](auto a) {
+        constexpr int ACT = decltype(a)::value;
+        auto launch = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((d_out + 15) / 16)), dim3(256), 0, s, e, x, w, rows, d_in, d_out);
+            return hipGetLastError();
+        };
+        return rows <= 16 ? launch(gated_some_kernel<ACT, 1>) : rows <= 32 ? launch(gated_some_kernel<ACT, 2>) : launch(gated_some_kernel<ACT, 4>);
+    });
+}
 
 bool gated_narrow(int64_t rows, int32_t d_in, int32_t d_out) { return rows >= 128 && d_in <= NARROW && d_out <= NARROW; }
 

@@ -114,6 +114,21 @@ def test_few_rows_of_odd_widths(rows, d_in, d_out, dtype):
     check(rows, d_in, d_out, "gelu", dtype, shift=1)
 
 
+@pytest.mark.parametrize("rows", [9, 16, 17, 31, 32, 33, 48, 49, 64, 65])
+@pytest.mark.parametrize("d_in,d_out", [(1, 1), (33, 17), (96, 136), (301, 15), (130, 1025), (1024, 16), (1025, 40)])
+def test_some_rows(rows, d_in, d_out):
+    """Tiles of 16 rows and outputs that are not full, k that four wavefronts share unevenly or not at all."""
+    check(rows, d_in, d_out, "silu", F32)
+    check(rows, d_in, d_out, "gelu", F32, bias=False, shift=1)
+
+
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_activations_of_some_rows(act, dtype):
+    check(20, 100, 50, act, dtype)
+    check(12, 2056, 24, act, dtype, bias=False)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("rows,d_in,d_out", [(300, 32, 64), (1000, 64, 33)])
 def test_single_gradients_of_narrow_layers(rows, d_in, d_out, dtype):

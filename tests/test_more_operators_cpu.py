@@ -115,7 +115,7 @@ def test_gated_workspaces(lib):
     for dtype in (F32, BF16):
         for rows, a, b in ((1, 16, 16), (20, 300, 600), (5000, 300, 20000), (70000, 1024, 4096)):
             st, n = _bytes(lib.lcn_gated_linear_workspace_bytes, rows, a, b, dtype, 0)
-            assert st == OK and (n == 0) == (rows <= 8)
+            assert st == OK and (n == 0) == (rows <= 8 or (rows == 20 and dtype == F32))   # those that read W as it lies
             if n:
                 assert lib.lcn_gated_linear(FAKE, FAKE, None, rows, a, b, dtype, 4, FAKE, None, FAKE, n - 1, None) == ERR_ALLOC
                 assert lib.lcn_gated_linear(FAKE, FAKE, None, rows, a, b, dtype, 4, FAKE, None, FAKE + 64, n, None) == ERR_ALLOC
