@@ -386,7 +386,7 @@ lcn_status lcn_calibrate(int32_t what, void *workspace, size_t workspace_bytes, 
  *     normal float are zero.
  *   - float products are formed from three bf16 planes per operand (six products
  *     of planes; as exact as single precision), so that a float input that is
- *     infinite makes the sums it enters NaN; up to 8 rows and in narrow layers,
+ *     infinite makes the sums it enters NaN; for few rows and in narrow layers,
  *     which use float instructions, they are infinite (or NaN) as in single
  *     precision.
  *   - Asynchronous on hip_stream, no synchronisation, no device allocation, no
