@@ -450,7 +450,8 @@ static hipError_t by_width(uintptr_t addresses, int32_t dim, F f)
 // slots as it has pieces or little more; with few rows it gets all the lanes that it can use.  20 000 rows of 300, forward and
 // backward, us: 16 x 5 lanes x pieces float 9 + 19, bf16 7 + 14; 64 x 2 11 + 19, 9 + 19; of 301 (single values), 64 x 5 12 + 20 and
 // 10 + 19, 256 x 2 22 + 45 and 21 + 45; 16 391 of 2048 in bf16, 64 x 4 23 + 39, 256 x 1 28 + 49; of 4096, 64 x 8 46 + 117,
-// 256 x 2 43 + 83; 40 000 float rows of 256, 32 x 2 15 + 25, 64 x 1 16 + 25.
+// 256 x 2 43 + 83; 40 000 float rows of 256, 32 x 2 15 + 25, 64 x 1 16 + 25;
+// backward, 4000 float rows of 4097, 256 x 6 52, 256 x 8 78; 8000 bf16 rows of 5000, 256 x 3 59, 256 x 4 62.
 template <int L, int C>
 struct Lanes {
     static constexpr int lanes = L, pieces = C;
@@ -479,7 +480,9 @@ static bool by_lanes(int units, bool singly, int64_t rows, hipError_t &st, F f)
              : units <= 128  ? f(Lanes<64, 2>())
              : units <= 256  ? f(Lanes<256, 1>())
              : units <= 512  ? f(Lanes<256, 2>())
+             : units <= 768  ? f(Lanes<256, 3>())
              : units <= 1024 ? f(Lanes<256, 4>())
+             : units <= 1536 ? f(Lanes<256, 6>())
              : units <= LONGEST ? f(Lanes<256, 8>())
                              : hipSuccess;
     }
