@@ -457,34 +457,44 @@ struct Lanes {
     static constexpr int lanes = L, pieces = C;
 };
 constexpr int LONGEST = 2048;
-template <class F>
-static bool by_lanes(int units, bool singly, int64_t rows, hipError_t &st, F f)
+template <int V, bool TAIL, class F>
+static bool by_lanes(int units, int64_t rows, hipError_t &st, F f)
 {
     const bool many = rows >= 2048;
-    if (many && units > 32 && units <= 64) {
-        st = f(Lanes<32, 2>());
-    } else if (many && units > 64 && units <= 80) {
+    if constexpr (V == 1)   // up to 512 single values: a wavefront's registers hold them easily
+        if (many && units > 256) {
+            st = units <= 320 ? f(Lanes<64, 5>()) : f(Lanes<64, 8>());
+            return true;
+        }
+    if constexpr (!TAIL) {   // with TAIL a row has more than 64 pieces
+        if (many && units > 32 && units <= 64) {
+            st = f(Lanes<32, 2>());
+            return true;
+        }
+        if (units <= 64) {
+            st = units <= 4    ? f(Lanes<4, 1>())
+                 : units <= 8  ? f(Lanes<8, 1>())
+                 : units <= 16 ? f(Lanes<16, 1>())
+                 : units <= 32 ? f(Lanes<32, 1>())
+                               : f(Lanes<64, 1>());
+            return true;
+        }
+    }
+    if (many && units <= 80) {
         st = f(Lanes<16, 5>());
-    } else if (many && units > 80 && units <= 96) {
+    } else if (many && units <= 96) {
         st = f(Lanes<32, 3>());
     } else if (many && units > 128 && units <= 256) {
         st = f(Lanes<64, 4>());
-    } else if (many && units > 256 && singly) {   // single values: a wavefront's registers hold them easily
-        st = units <= 320 ? f(Lanes<64, 5>()) : f(Lanes<64, 8>());
+    } else if (units <= 512) {
+        st = units <= 128 ? f(Lanes<64, 2>()) : units <= 256 ? f(Lanes<256, 1>()) : f(Lanes<256, 2>());
     } else {
-        st = units <= 4      ? f(Lanes<4, 1>())
-             : units <= 8    ? f(Lanes<8, 1>())
-             : units <= 16   ? f(Lanes<16, 1>())
-             : units <= 32   ? f(Lanes<32, 1>())
-             : units <= 64   ? f(Lanes<64, 1>())
-             : units <= 128  ? f(Lanes<64, 2>())
-             : units <= 256  ? f(Lanes<256, 1>())
-             : units <= 512  ? f(Lanes<256, 2>())
-             : units <= 768  ? f(Lanes<256, 3>())
-             : units <= 1024 ? f(Lanes<256, 4>())
-             : units <= 1536 ? f(Lanes<256, 6>())
-             : units <= LONGEST ? f(Lanes<256, 8>())
-                             : hipSuccess;
+        if constexpr (V == 1) return false;   // none so long
+        else if (units <= LONGEST)
+            st = units <= 768    ? f(Lanes<256, 3>())
+                 : units <= 1024 ? f(Lanes<256, 4>())
+                 : units <= 1536 ? f(Lanes<256, 6>())
+                                 : f(Lanes<256, 8>());
     }
     return units <= LONGEST;
 }
@@ -497,14 +507,15 @@ static lcn_status norm_as(const T *x, const T *w, const T *b, int64_t rows, int3
         constexpr int V = decltype(v)::value;
         constexpr bool TAIL = decltype(v)::tail;
         hipError_t st;
-        if (by_lanes((dim + V - 1) / V, V == 1, rows, st, [&](auto l) {
+        if (by_lanes<V, TAIL>((dim + V - 1) / V, rows, st, [&](auto l) {
                 constexpr int L = decltype(l)::lanes, C = decltype(l)::pieces;
                 hipLaunchKernelGGL((norm_kernel<T, V, TAIL, L, C>), grid_of((rows + 256 / L - 1) / (256 / L)), dim3(256), 0, s, x, w, b,
                                    (long long)rows, dim, eps, y, mean, rstd);
                 return hipGetLastError();
             }))
             return st;
-        hipLaunchKernelGGL((norm_long_kernel<T, V, TAIL>), grid_of(rows), dim3(256), 0, s, x, w, b, (long long)rows, dim, eps, y, mean, rstd);
+        if constexpr (V > 1)
+            hipLaunchKernelGGL((norm_long_kernel<T, V, TAIL>), grid_of(rows), dim3(256), 0, s, x, w, b, (long long)rows, dim, eps, y, mean, rstd);
         return hipGetLastError();
     }));
     return LCN_OK;
@@ -522,7 +533,7 @@ static lcn_status norm_backward_as(const T *x, const T *w, const float *mean, co
         constexpr int V = decltype(v)::value;
         constexpr bool TAIL = decltype(v)::tail;
         hipError_t st;
-        if (by_lanes((dim + V - 1) / V, V == 1, rows, st, [&](auto l) {
+        if (by_lanes<V, TAIL>((dim + V - 1) / V, rows, st, [&](auto l) {
                 constexpr int L = decltype(l)::lanes, C = decltype(l)::pieces;
                 const int64_t needed = (rows + 256 / L - 1) / (256 / L);
                 groups = (int)(needed < most ? needed : most);
@@ -531,12 +542,14 @@ static lcn_status norm_backward_as(const T *x, const T *w, const float *mean, co
                 return hipGetLastError();
             }))
             return st;
-        if (dx) hipLaunchKernelGGL((norm_long_dx_kernel<T, V, TAIL>), grid_of(rows), dim3(256), 0, s, x, w, mean, rstd, dy, around,
-                                   (long long)rows, dim, dx);
-        st = hipGetLastError();
-        if (st != hipSuccess || !sums) return st;
-        hipLaunchKernelGGL((norm_columns_kernel<T, V, TAIL>), dim3((unsigned)(((dim + V - 1) / V + 255) / 256), (unsigned)groups), dim3(256), 0, s, x,
-                           mean, rstd, dy, (long long)rows, dim, part);
+        if constexpr (V > 1) {
+            if (dx) hipLaunchKernelGGL((norm_long_dx_kernel<T, V, TAIL>), grid_of(rows), dim3(256), 0, s, x, w, mean, rstd, dy, around,
+                                       (long long)rows, dim, dx);
+            st = hipGetLastError();
+            if (st != hipSuccess || !sums) return st;
+            hipLaunchKernelGGL((norm_columns_kernel<T, V, TAIL>), dim3((unsigned)(((dim + V - 1) / V + 255) / 256), (unsigned)groups), dim3(256), 0, s, x,
+                               mean, rstd, dy, (long long)rows, dim, part);
+        }
         return hipGetLastError();
     }));
     if (!sums) return LCN_OK;
