@@ -498,7 +498,8 @@ lcn_status lcn_attention_backward(const lcn_attention_desc *desc, const void *q,
  * (its other half is lcn_linear).  x rows x d_in; W (2 d_out) x d_in, Wg above Wu; bias (bg before bu,
  * 2 d_out; nullable); y rows x d_out.  kept (nullable, 16-byte aligned, as many bytes as the call below
  * says): g and u for the backward pass, in a layout of the library's own: floats with float tensors; with bf16
- * tensors 16 bits a value, within 2^-14 of the power of two above the largest of eight neighbours.
+ * tensors 16 bits a value, within 2^-11 of each, 2^-10 where eight neighbours are more than 2^13 apart or some are zero, 2^-7
+ * where they are more than 2^27 apart or one is not finite.
  * Sizes: 0 <= rows <= 2^30, 1 <= d_in <= 2^20, 1 <= d_out <= 2^19, rows times d_in or 2 d_out <= 2^42.  The
  * forward pass needs no workspace for few rows and in narrow layers (the call says 0 bytes). */
 lcn_status lcn_gated_linear_workspace_bytes(int64_t rows, int32_t d_in, int32_t d_out, int32_t dtype, int32_t backward,

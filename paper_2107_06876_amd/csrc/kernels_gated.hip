@@ -7,8 +7,8 @@
 // the rate of a copy, dx 250, dW 285) and by reading W on few (one row, 2048 -> 8192, bf16: 11 us for 67 MB).
 //
 // Rounding: g, u, sums and activations are in 32 bits; with bf16 tensors y, dz, dx, dW and db are rounded once each.  What is
-// kept of g and u for the backward pass is 16 bits a value for bf16 tensors, with 14 bits of significand for the largest of eight
-// (below); as bf16 each would add an error to dz of the size of dz's own rounding, as floats they are half of what moves.
+// kept of g and u for the backward pass is 16 bits a value for bf16 tensors, 11 of significand (gated.h); as bf16 each would add
+// an error to dz of the size of dz's own rounding, as floats they are half of what moves.
 #include "gated.h"
 
 namespace lcn {

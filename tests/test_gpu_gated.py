@@ -200,6 +200,64 @@ def test_what_is_kept_may_be_infinite(rows):
         assert torch.isfinite(dx[3:]).all()
 
 
+def column_sizes(kind, d_out):
+    """Factors of columns: one of eight far above its neighbours, or 2^-20 to 2^20 in any order."""
+    s = torch.ones(d_out, device=DEV)
+    if kind == "any":
+        return (2.0 ** torch.linspace(-20, 20, d_out)[torch.randperm(d_out, generator=generator(d_out))]).to(DEV)
+    s[3::8] = 2.0 ** kind
+    return s
+
+
+@pytest.mark.parametrize("kind", [0, 6, 10, 13, 16, 24, 40, -12, -30, -60, "any"])
+@pytest.mark.parametrize("rows,d_out", [(3, 40), (3, 37), (20, 64), (300, 37), (300, 200), (700, 520)])
+def test_what_is_kept_is_near_each_value(rows, d_out, kind):
+    """u and g, which db is for a dy of 1 in one row and no activation: kept within 2^-10 of each value, whatever its neighbours are
+    (2^-7 where they are more than 2^27 apart), formed in sums of 48 terms and rounded once in db."""
+    x, w, b, dy = inputs(rows, 48, d_out, BF16)
+    s = column_sizes(kind, d_out)
+    w = (w.float() * torch.cat((s, s))[:, None]).bfloat16()
+    _, pre = lcn.lcn_gated_linear(x, w, activation=lcn.ACT_NONE, keep_pre=True)
+    z = x.double() @ w.double().t().contiguous()
+    terms = x.double().abs() @ w.double().abs().t().contiguous()
+    for r in {0, 1, rows // 2, rows - 1}:
+        dy.zero_()
+        dy[r] = 1.0
+        db = lcn.lcn_gated_linear_backward(x, w, pre, dy, activation=lcn.ACT_NONE)[2].double()
+        want = torch.cat((z[r, d_out:], z[r, :d_out]))
+        near = 2.0 ** -24 * 48 * torch.cat((terms[r, d_out:], terms[r, :d_out]))
+        # a piece's largest and least value, which decide how it is kept
+        some = torch.nn.functional.pad(z[r].view(2, d_out), (0, -d_out % 8)).abs().view(2, -1, 8)
+        apart = some.amax(2) / torch.where(some == 0.0, math.inf, some).amin(2) > 2.0 ** 27
+        far = apart.flip(0)[:, :, None].expand(-1, -1, 8).reshape(2, -1)[:, :d_out].flatten()
+        room = want.abs() * (2.0 ** -8 + torch.where(far, 2.0 ** -7, 2.0 ** -10)) * (1 + 2.0 ** -7) + 2 * near
+        assert ((db - want).abs() <= room).all(), ((db - want).abs() / room).max()
+
+
+@pytest.mark.parametrize("act,gates", [("none", True), ("silu", False)])
+@pytest.mark.parametrize("rows,d_out", [(3, 40), (20, 64), (300, 37), (300, 200), (700, 520)])
+@pytest.mark.parametrize("kind", [6, 10, 13, 16, "any"])
+def test_gradients_beside_larger_columns(kind, rows, d_out, act, gates):
+    """Rows of dW and db are as exact beside columns that are larger as elsewhere.  g and u are kept within `kept` of each value; dz is
+    rounded once above 512 rows, dW and db are rounded once.  The rows of x are nearly at right angles (few rows) or their errors
+    independent (many): 1.25 covers what adds up in dW.  In db the errors of its terms are independent, 0.43 of their bound
+    in the root mean square, of u and through the slope: 3 covers five deviations."""
+    x, w, _, dy = inputs(rows, 48, d_out, BF16)
+    s = column_sizes(kind, d_out)
+    w = (w.float() * torch.cat((s if gates else torch.ones_like(s), s))[:, None]).bfloat16()
+    _, pre = lcn.lcn_gated_linear(x, w, activation=ACTS[act], keep_pre=True)
+    _, dw, db = lcn.lcn_gated_linear_backward(x, w, pre, dy, activation=ACTS[act])
+    want = oracle(x, w, None, dy, act)
+    kept = 2.0 ** -7 if kind == "any" else 2.0 ** -10
+    for i in range(2 * d_out):
+        assert off(dw[i], want[3][i]) <= 2.5 * 2.0 ** -8 + 1.25 * kept, i
+    g, u, d = want[1][:, :d_out].detach().requires_grad_(True), want[1][:, d_out:], dy.double()
+    a = FUNCTIONS[act](g)
+    (slope,) = torch.autograd.grad(a.sum(), g)
+    dz = torch.cat((d * u * slope, d * a.detach()), 1)
+    assert ((db.double() - want[4]).abs() <= 2.0 ** -8 * want[4].abs() + 3 * kept * dz.norm(dim=0)).all()
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("rows,d_out,shift", [(5, 136, 0), (300, 136, 0), (700, 136, 0), (300, 135, 0), (300, 136, 1)])
 def test_single_gradients_and_same_bits(rows, d_out, shift, dtype):
