@@ -518,7 +518,8 @@ lcn_status lcn_gated_linear_backward(const void *x, const void *W, const void *k
  *   y = (x - mean) rstd weight + bias,  rstd = 1 / sqrt(mean of (x - mean)^2 + eps).
  * weight, bias (dim, of type dtype) are nullable (1 and 0); mean, rstd (fp32, rows;
  * nullable): what the backward pass takes.  y may be x.  A row that holds a value that is not
- * finite becomes NaN; where squares leave a float's range (differences from 1e19 on) rstd is 0.
+ * finite becomes NaN; where the variance leaves a float's range (differences from 1e19 on) rstd is 0 and y the bias, for values
+ * of up to 2^127.
  * Sizes: 0 <= rows <= 2^30, 1 <= dim <= 2^20, their product <= 2^42; eps finite and >= 0
  * (0: rows of equal values become NaN).  No workspace. */
 lcn_status lcn_layer_norm(const void *x, const void *weight, const void *bias, int64_t rows, int32_t dim, int32_t dtype, float eps,

@@ -68,6 +68,11 @@ __device__ __forceinline__ float sum_over(float a, float *lds)
     return a;
 }
 
+// A power of two from 1 / (2 dim) on, below 1 / dim: a sum of `dim` finite values times it stays in a float's range, as their mean does.
+__device__ __forceinline__ float share_of(int dim) { return __builtin_ldexpf(1.f, __builtin_clz(dim) - 32); }
+// x - mean, halved, so that it stays in that range as well: what it is multiplied with is doubled, and the product has the same bits.
+__device__ __forceinline__ float half_less(float x, float half_mean) { return __builtin_fmaf(x, 0.5f, -half_mean); }
+
 // L lanes have a row, C pieces of V values each.
 template <class T, int V, bool TAIL, int L, int C>
 __global__ __launch_bounds__(256) void norm_kernel(const T *x, const T *__restrict__ w, const T *__restrict__ b, long long rows,
@@ -82,6 +87,7 @@ __global__ __launch_bounds__(256) void norm_kernel(const T *x, const T *__restri
     const bool here = r < rows;
     piece p[C];
     float sum = 0.f;
+    const float part = share_of(dim);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int u = c * L + lane;
@@ -90,19 +96,19 @@ __global__ __launch_bounds__(256) void norm_kernel(const T *x, const T *__restri
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int e = 0; e < V; ++e) sum += (float)p[c][e];
-    const float mean = sum_over<L>(sum, lds[0]) / (float)dim;
+        for (int e = 0; e < V; ++e) sum = __builtin_fmaf((float)p[c][e], part, sum);
+    const float mean = sum_over<L>(sum, lds[0]) / ((float)dim * part), half = 0.5f * mean;
     float square = 0.f;   // of differences over sqrt(dim): the sum leaves a float's range where the variance does, not before
-    const float share = 1.f / sqrtf((float)dim);
+    const float share = 2.f / sqrtf((float)dim);
 #pragma unroll
     for (int c = 0; c < C; ++c)
         if (c * L + lane < units)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float d = ((float)p[c][e] - mean) * share;
+                const float d = half_less((float)p[c][e], half) * share;
                 if (!TAIL || (c * L + lane) * V + e < dim) square += d * d;
             }
-    const float rstd = 1.f / sqrtf(sum_over<L>(square, lds[1]) + eps);
+    const float rstd = 1.f / sqrtf(sum_over<L>(square, lds[1]) + eps), twice = 2.f * rstd;
     if (!here) return;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -113,7 +119,7 @@ __global__ __launch_bounds__(256) void norm_kernel(const T *x, const T *__restri
         if (b) pb = load_piece<T, V, TAIL>(b, u * V, dim);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            float v = ((float)p[c][e] - mean) * rstd;
+            float v = half_less((float)p[c][e], half) * twice;
             if (w) v *= (float)pw[e];
             if (b) v += (float)pb[e];
             o[e] = (T)v;
@@ -145,12 +151,12 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const T *__restrict__ x,
     const long long step = (long long)gridDim.x * PER;
     struct Row {
         piece x[C], dy[C], around[C];
-        float mean, rstd;
+        float half, rstd;   // half of the mean
     };
     auto read = [&](long long r) {
         Row t;
         const bool here = r < rows;
-        t.mean = here ? mean_in[r] : 0.f;
+        t.half = here ? 0.5f * mean_in[r] : 0.f;
         t.rstd = here ? rstd_in[r] : 0.f;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
@@ -178,12 +184,13 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const T *__restrict__ x,
     for (long long first = (long long)blockIdx.x * PER; first < rows; first += step, r += step, turn ^= 1) {
         Row t = AHEAD ? next : read(r);
         if (AHEAD && first + step < rows) next = read(r + step);
+        const float twice = 2.f * t.rstd;
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float d = (float)t.dy[c][e], h = ((float)t.x[c][e] - t.mean) * t.rstd, g = w ? d * (float)pw[c][e] : d;
+                const float d = (float)t.dy[c][e], h = half_less((float)t.x[c][e], t.half) * twice, g = w ? d * (float)pw[c][e] : d;
                 s1 += g;
                 s2 += g * h;
                 dw[c][e] += d * h;
@@ -200,7 +207,7 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const T *__restrict__ x,
             piece o;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float d = (float)t.dy[c][e], h = ((float)t.x[c][e] - t.mean) * t.rstd, g = w ? d * (float)pw[c][e] : d;
+                const float d = (float)t.dy[c][e], h = half_less((float)t.x[c][e], t.half) * twice, g = w ? d * (float)pw[c][e] : d;
                 float v = t.rstd * (g - s1 - h * s2);
                 if (around) v += (float)t.around[c][e];
                 o[e] = (T)v;
@@ -273,26 +280,27 @@ __global__ __launch_bounds__(256) void norm_long_kernel(const T *x, const T *__r
     if (r >= rows) return;
     const int units = TAIL ? (dim + V - 1) / V : dim / V;
     const T *row = x + r * dim;
+    const float part = share_of(dim);
     float sum = 0.f, none = 0.f;
     for (int u = threadIdx.x; u < units; u += 256) {
         const piece p = load_piece<T, V, TAIL>(row, u * V, dim);
 #pragma unroll
-        for (int e = 0; e < V; ++e) sum += (float)p[e];
+        for (int e = 0; e < V; ++e) sum = __builtin_fmaf((float)p[e], part, sum);
     }
     sum_over_group(sum, none, lds);
-    const float mean = sum / (float)dim;
+    const float mean = sum / ((float)dim * part), half = 0.5f * mean;
     float square = 0.f;
-    const float share = 1.f / sqrtf((float)dim);
+    const float share = 2.f / sqrtf((float)dim);
     for (int u = threadIdx.x; u < units; u += 256) {
         const piece p = load_piece<T, V, TAIL>(row, u * V, dim);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const float d = ((float)p[e] - mean) * share;
+            const float d = half_less((float)p[e], half) * share;
             if (!TAIL || u * V + e < dim) square += d * d;
         }
     }
     sum_over_group(square, none, lds);
-    const float rstd = 1.f / sqrtf(square + eps);
+    const float rstd = 1.f / sqrtf(square + eps), twice = 2.f * rstd;
     for (int u = threadIdx.x; u < units; u += 256) {
         const piece p = load_piece<T, V, TAIL>(row, u * V, dim);
         piece o, pw, pb;
@@ -300,7 +308,7 @@ __global__ __launch_bounds__(256) void norm_long_kernel(const T *x, const T *__r
         if (b) pb = load_piece<T, V, TAIL>(b, u * V, dim);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            float v = ((float)p[e] - mean) * rstd;
+            float v = half_less((float)p[e], half) * twice;
             if (w) v *= (float)pw[e];
             if (b) v += (float)pb[e];
             o[e] = (T)v;
@@ -326,7 +334,7 @@ __global__ __launch_bounds__(256) void norm_long_dx_kernel(const T *__restrict__
     const int units = TAIL ? (dim + V - 1) / V : dim / V;
     x += r * dim, dy += r * dim, dx += r * dim;
     if (around) around += r * dim;
-    const float mean = mean_in[r], rstd = rstd_in[r];
+    const float half = 0.5f * mean_in[r], rstd = rstd_in[r], twice = 2.f * rstd;
     float s1 = 0.f, s2 = 0.f;
     for (int u = threadIdx.x; u < units; u += 256) {
         const piece px = load_piece<T, V, TAIL>(x, u * V, dim), pd = load_piece<T, V, TAIL>(dy, u * V, dim);
@@ -336,7 +344,7 @@ __global__ __launch_bounds__(256) void norm_long_dx_kernel(const T *__restrict__
         for (int e = 0; e < V; ++e) {
             const float g = (float)pd[e] * (w ? (float)pw[e] : 1.f);
             s1 += g;
-            s2 += g * (((float)px[e] - mean) * rstd);
+            s2 += g * (half_less((float)px[e], half) * twice);
         }
     }
     sum_over_group(s1, s2, lds);
@@ -350,7 +358,7 @@ __global__ __launch_bounds__(256) void norm_long_dx_kernel(const T *__restrict__
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const float g = (float)pd[e] * (w ? (float)pw[e] : 1.f);
-            float v = rstd * (g - s1 - ((float)px[e] - mean) * rstd * s2);
+            float v = rstd * (g - s1 - half_less((float)px[e], half) * twice * s2);
             if (around) v += (float)pa[e];
             o[e] = (T)v;
         }
@@ -372,10 +380,10 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(const T *__restrict__
     for (int e = 0; e < V; ++e) dw[e] = db[e] = 0.f;
     for (long long r = blockIdx.y; r < rows; r += gridDim.y) {
         const piece px = load_piece<T, V, TAIL>(x + r * dim, u * V, dim), pd = load_piece<T, V, TAIL>(dy + r * dim, u * V, dim);
-        const float m = mean[r], s = rstd[r];
+        const float half = 0.5f * mean[r], twice = 2.f * rstd[r];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            dw[e] += (float)pd[e] * (((float)px[e] - m) * s);
+            dw[e] += (float)pd[e] * (half_less((float)px[e], half) * twice);
             db[e] += (float)pd[e];
         }
     }

@@ -192,6 +192,29 @@ def test_values_of_every_size():
     assert off(lcn.lcn_layer_norm(x * 1e25, w, b), b.expand(40, 300)) == 0.0
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,dim", [(5, 16), (70, 300), (2050, 300), (9, 301), (2100, 513), (33, 4096), (2048, 4096), (5, 9000), (3, 20001)])
+def test_rows_up_to_the_largest_values(rows, dim, dtype):
+    """Sums and differences of finite rows leave a float's range where the mean and the variance do, not before: y is the bias, the mean
+    is off by the roundings of its sum, and what reaches x is the gradient around."""
+    g = generator(rows, dim)
+    w, b, dy, around = (normal(g, *shape, dtype=dtype) for shape in ((dim,), (dim,), (rows, dim), (rows, dim)))
+    sign = torch.randint(0, 2, (rows, dim), generator=g).to(DEV) * 2.0 - 1.0
+    one = torch.ones(rows, dim, device=DEV)
+    one[:, dim // 2] = -1.0
+    for x in (sign * 1e36, sign * 3.3e38, one * 3.3e38, one.abs() * 1e36, one.abs() * 3.3e38, one.abs() * -3.3e38):
+        x = x.to(dtype)
+        assert torch.isfinite(x).all()
+        y, mean, rstd = lcn.lcn_layer_norm(x, w, b, eps=EPS, keep_stats=True)
+        assert torch.equal(y, b.expand(rows, dim))
+        largest = x.double().abs().amax(1)
+        assert ((mean.double() - x.double().mean(1)).abs() <= largest * (dim * 2.0 ** -24)).all()
+        if (x[0] != x[0, 0]).any():
+            assert not rstd.any()
+            dx, dw, db = lcn.lcn_layer_norm_backward(x, w, mean, rstd, dy, around=around)
+            assert torch.equal(dx, around) and not dw.any() and off(db, dy.double().sum(0)) <= bound(dtype, rows)
+
+
 @pytest.mark.parametrize("dim", [64, 300, 4096])
 def test_roundings_of_bf16(dim):
     x, w, b, dy, around = inputs(2000, dim, BF16)
