@@ -70,6 +70,9 @@ __device__ __forceinline__ float sum_over(float a, float *lds)
 
 // A power of two from 1 / (2 dim) on, below 1 / dim: a sum of `dim` finite values times it stays in a float's range, as their mean does.
 __device__ __forceinline__ float share_of(int dim) { return __builtin_ldexpf(1.f, __builtin_clz(dim) - 32); }
+// A power of two whose square times dim is from 1 / 8 on, below 1 / 2: differences times it have a sum of squares that stays in a
+// float's range where the variance does, with no rounding of a factor's own (1 / sqrt(dim) is off by 1e-7 in the variance).
+__device__ __forceinline__ float root_share_of(int dim) { return __builtin_ldexpf(1.f, -((34 - __builtin_clz(dim)) / 2)); }
 // x - mean, halved, so that it stays in that range as well: what it is multiplied with is doubled, and the product has the same bits.
 __device__ __forceinline__ float half_less(float x, float half_mean) { return __builtin_fmaf(x, 0.5f, -half_mean); }
 
@@ -98,17 +101,17 @@ __global__ __launch_bounds__(256) void norm_kernel(const T *x, const T *__restri
 #pragma unroll
         for (int e = 0; e < V; ++e) sum = __builtin_fmaf((float)p[c][e], part, sum);
     const float mean = sum_over<L>(sum, lds[0]) / ((float)dim * part), half = 0.5f * mean;
-    float square = 0.f;   // of differences over sqrt(dim): the sum leaves a float's range where the variance does, not before
-    const float share = 2.f / sqrtf((float)dim);
+    float square = 0.f;
+    const float root = root_share_of(dim), mean_part = mean * root;
 #pragma unroll
     for (int c = 0; c < C; ++c)
         if (c * L + lane < units)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float d = half_less((float)p[c][e], half) * share;
+                const float d = __builtin_fmaf((float)p[c][e], root, -mean_part);
                 if (!TAIL || (c * L + lane) * V + e < dim) square += d * d;
             }
-    const float rstd = 1.f / sqrtf(sum_over<L>(square, lds[1]) + eps), twice = 2.f * rstd;
+    const float rstd = 1.f / sqrtf(sum_over<L>(square, lds[1]) / ((float)dim * root * root) + eps), twice = 2.f * rstd;
     if (!here) return;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -290,17 +293,17 @@ __global__ __launch_bounds__(256) void norm_long_kernel(const T *x, const T *__r
     sum_over_group(sum, none, lds);
     const float mean = sum / ((float)dim * part), half = 0.5f * mean;
     float square = 0.f;
-    const float share = 2.f / sqrtf((float)dim);
+    const float root = root_share_of(dim), mean_part = mean * root;
     for (int u = threadIdx.x; u < units; u += 256) {
         const piece p = load_piece<T, V, TAIL>(row, u * V, dim);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const float d = half_less((float)p[e], half) * share;
+            const float d = __builtin_fmaf((float)p[e], root, -mean_part);
             if (!TAIL || u * V + e < dim) square += d * d;
         }
     }
     sum_over_group(square, none, lds);
-    const float rstd = 1.f / sqrtf(square + eps), twice = 2.f * rstd;
+    const float rstd = 1.f / sqrtf(square / ((float)dim * root * root) + eps), twice = 2.f * rstd;
     for (int u = threadIdx.x; u < units; u += 256) {
         const piece p = load_piece<T, V, TAIL>(row, u * V, dim);
         piece o, pw, pb;

@@ -215,6 +215,17 @@ def test_rows_up_to_the_largest_values(rows, dim, dtype):
             assert torch.equal(dx, around) and not dw.any() and off(db, dy.double().sum(0)) <= bound(dtype, rows)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,dim", [(3, 2), (70, 6), (2050, 24), (70, 300), (2050, 300), (9, 302), (2100, 514), (33, 1000), (5, 3002), (5, 9000),
+                                      (3, 20002)])
+def test_a_variance_of_one(rows, dim, dtype):
+    """Rows of 1 and -1: every sum is exact, and so are the variance, rstd and y."""
+    x = torch.ones(rows, dim, dtype=dtype, device=DEV)
+    x[:, ::2] = -1.0
+    y, mean, rstd = lcn.lcn_layer_norm(x, eps=0.0, keep_stats=True)
+    assert torch.equal(y, x) and not mean.any() and (rstd == 1.0).all()
+
+
 @pytest.mark.parametrize("dim", [64, 300, 4096])
 def test_roundings_of_bf16(dim):
     x, w, b, dy, around = inputs(2000, dim, BF16)
