@@ -183,6 +183,70 @@ def test_in_place_scaled_and_same_bits(rows, cols, dtype):
     assert lcn.lcn_orthogonalise(g, out=g) is g and torch.equal(g, want)
 
 
+# ---- long bf16 matrices, whose steps are taken on A alone, several to a stage ----
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 6, 7, 12, 13])
+@pytest.mark.parametrize("rows,cols", [(900, 100), (100, 800), (70, 1030)])
+def test_steps_and_coefficients_of_long_matrices(rows, cols, steps):
+    check(rows, cols, BF16, steps=steps)
+    check(rows, cols, BF16, steps=steps, coefficients=MAP)
+    check(rows, cols, BF16, steps=steps, coefficients=[UPDATE if i % 2 else MAP for i in range(steps)])
+    check(rows, cols, BF16, steps=steps, coefficients=[MAP if i % 3 else UPDATE for i in range(steps)])
+    check(rows, cols, BF16, steps=steps, coefficients=(1.5, -0.5, 0.0))
+
+
+@pytest.mark.parametrize("count,rows,cols", [(4, 900, 100), (3, 100, 800), (5, 1200, 128), (3, 65, 500), (3, 2500, 600)])
+def test_batches_of_long_matrices(count, rows, cols):
+    """Matrices of different sizes each have their own factor; one of zeros stays so, also beside others."""
+    g = torch.stack([gradient(i, rows, cols, BF16) * 10.0 ** (3 * i - 6) for i in range(count)])
+    g[count // 2] = 0.0
+    for steps, coefficients in ((5, UPDATE), (9, MAP)):
+        x = lcn.lcn_orthogonalise(g, steps=steps, coefficients=coefficients)
+        assert not x[count // 2].any()
+        for i in range(count):
+            if i != count // 2:
+                want, room = oracle(g[i], steps, coefficients)
+                assert off(x[i], want) <= room + 2.0 ** -8
+
+
+@pytest.mark.parametrize("rows,cols", [(900, 100), (100, 800)])
+def test_what_is_not_finite_stays_in_its_long_matrix(rows, cols):
+    g = torch.stack([gradient(i, rows, cols, BF16) for i in range(5)])
+    for steps, coefficients in ((5, UPDATE), (1, UPDATE), (6, MAP)):
+        want = lcn.lcn_orthogonalise(g, steps=steps, coefficients=coefficients)
+        bad = g.clone()
+        bad[1, 3, 5], bad[2, 0, 0], bad[4, rows - 1, cols - 1] = math.nan, -math.inf, math.inf
+        x = lcn.lcn_orthogonalise(bad, steps=steps, coefficients=coefficients)
+        for i in range(5):
+            assert torch.isnan(x[i]).all() if i in (1, 2, 4) else torch.equal(x[i], want[i])
+    zero = torch.zeros(2, rows, cols, dtype=BF16, device=DEV)
+    assert torch.isnan(lcn.lcn_orthogonalise(zero, eps=0.0)).all() and not lcn.lcn_orthogonalise(zero).any()
+
+
+@pytest.mark.parametrize("rows,cols", [(900, 100), (100, 800), (4100, 520)])
+def test_long_matrices_in_place_scaled_and_same_bits(rows, cols):
+    g = torch.stack([gradient(i, rows, cols, BF16) for i in range(3)])
+    want = lcn.lcn_orthogonalise(g, steps=7, coefficients=MAP)
+    assert torch.equal(want, lcn.lcn_orthogonalise(g, steps=7, coefficients=MAP))
+    for i in range(3):   # and of each alone
+        assert off(lcn.lcn_orthogonalise(g[i], steps=7, coefficients=MAP), want[i].double()) <= 2.0 ** -8
+    assert off(lcn.lcn_orthogonalise(g, steps=7, coefficients=MAP, scale=-0.25), -0.25 * want) == 0.0
+    assert lcn.lcn_orthogonalise(g, steps=7, coefficients=MAP, out=g) is g and torch.equal(g, want)
+
+
+@pytest.mark.parametrize("rows,cols", [(900, 100), (100, 800)])
+def test_sizes_of_every_order_of_long_matrices(rows, cols):
+    """bf16 has a float's range: the factor of a matrix is a power of two and the rest.  (The least values, 2^-31, lose bits as
+    subnormals at 2^-100: what is compared with is the matrix that is left.)"""
+    base = gradient(4, rows, cols, BF16)
+    for power in (-100, -60, 60, 120):
+        g = base * 2.0 ** power
+        left = (g.double() * 2.0 ** -power).bfloat16()
+        assert torch.equal(left.double() * 2.0 ** power, g.double())
+        assert torch.equal(lcn.lcn_orthogonalise(g, eps=0.0), lcn.lcn_orthogonalise(left, eps=0.0))
+
+
 def test_no_matrices():
     assert lcn.lcn_orthogonalise(torch.empty(0, 4, 5, device=DEV)).shape == (0, 4, 5)
 
