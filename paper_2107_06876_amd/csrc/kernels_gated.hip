@@ -486,10 +486,11 @@ static lcn_status gated_backward_as(const T *x, const T *w, const typename Keep<
             return hipGetLastError();
         };
         constexpr int MOST = sizeof(T) == 4 ? 3 : 2;
-        if (b.planes == 1)
-            return d_out <= 64    ? launch(gated_slope_kernel<T, ACT, 8, 1>, 8)
-                   : d_out <= 128 ? launch(gated_slope_kernel<T, ACT, 16, 1>, 16)
-                                  : launch(gated_slope_kernel<T, ACT, 32, 1>, 32);
+        if constexpr (MOST == 2)
+            if (b.planes == 1)
+                return d_out <= 64    ? launch(gated_slope_kernel<T, ACT, 8, 1>, 8)
+                       : d_out <= 128 ? launch(gated_slope_kernel<T, ACT, 16, 1>, 16)
+                                      : launch(gated_slope_kernel<T, ACT, 32, 1>, 32);
         return d_out <= 64    ? launch(gated_slope_kernel<T, ACT, 8, MOST>, 8)
                : d_out <= 128 ? launch(gated_slope_kernel<T, ACT, 16, MOST>, 16)
                               : launch(gated_slope_kernel<T, ACT, 32, MOST>, 32);
