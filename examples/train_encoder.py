@@ -3,9 +3,9 @@
 Nodes of ragged graphs go through a tanh layer, attention inside their own graph (near nodes of the order count more)
 and a linear layer with the residual, and with --hidden through a gated feed-forward block behind a layer norm; the loss
 is the cross entropy of every node against a vocabulary of prototypes at scale 1 / lambda.  The gradients are formed by the
-operators' backward calls, layer by layer, and applied by plain gradient descent, with --orthogonal those of matrices as
-the orthogonal matrices nearest to them.  At the end the encoded graphs of every pair are compared by a batch of transport
-problems.
+operators' backward calls, layer by layer, and applied by plain gradient descent, with --orthogonal those of matrices with
+their singular values brought to 0.7 .. 1.2.  At the end the encoded graphs of every pair are compared by a batch of
+transport problems.
 
     python examples/train_encoder.py [--graphs 64] [--steps 60] [--bf16] [--hidden 64] [--orthogonal]
 """

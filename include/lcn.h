@@ -540,9 +540,12 @@ lcn_status lcn_layer_norm_backward(const void *x, const void *weight, const floa
  *   A = X X^T,  X = a X + (b A + c A^2) X       (with more rows than columns: of the transposed matrix);
  * out = scale X.  The singular vectors stay, a singular value s becomes a s + b s^3 + c s^5 in a step.
  * (3.4445, -4.7750, 2.0315) five times brings most of them to 0.7 .. 1.2, for updates of weight matrices;
- * (1.875, -1.25, 0.375) often enough brings them to 1: the nearest orthogonal map to a correlation of two embeddings.
- * X and all sums are held to 24 bits, also with bf16 tensors, and out is rounded once.  A G that holds a
- * value that is not finite makes its whole result NaN, and so does G = 0 with eps = 0.  out may be g.
+ * (1.875, -1.25, 0.375) brings them to 1, a value s to within 2^-24 in 1.1 log2(|G| / s) + 3 steps (|G| / 1000: 14): with enough
+ * for the least of them, the nearest orthogonal map to a correlation of two embeddings; values that fewer steps leave below 1
+ * are directions that the map shrinks.
+ * X and all sums are held to 24 bits, also with bf16 tensors, and out is rounded once.  Long bf16 matrices (one side 4 times the
+ * other or more) take several steps at a time on A alone, which is off by an eighth of a bf16 rounding at most in the result.  A G that
+ * holds a value that is not finite makes its whole result NaN, and so does G = 0 with eps = 0.  out may be g.
  * LCN_ERR_INVALID_ARG for coefficients that let singular values in 0 .. 1 grow beyond 4, or a + b s^2 + c s^4 beyond
  * 64, in any step.  Sizes: 0 <= count <= 2^20, 1 <= rows, cols <= 2^20, the smaller of them <= 32768, count * rows *
  * cols <= 2^40, fewer than 2^31 tiles of 64 x 64; 1 <= steps <= 64; eps >= 0 and scale finite.  Matrices of up to

@@ -83,8 +83,7 @@ struct Tile {
 
 // Brings rows of a tensor into a tile.  VEC: 16-byte pieces of rows are aligned and whole; they go straight into LDS.
 // Otherwise values are read one by one.  What is outside (rows from `left` on, values from dim on) becomes zero.
-// REPEAT: rows from `left` on repeat the last one instead (left > 0), so that every load reads something: who waits for
-// loads by counting them need not know in which order loads end that are outside as a whole.
+// REPEAT: rows from `left` on repeat the last one instead (left > 0), so that every load reads something.
 template <class T, int DP, int ROWS, bool VEC, int THREADS, bool REPEAT = false>
 struct TileReader {
     typedef Tile<T, DP> L;

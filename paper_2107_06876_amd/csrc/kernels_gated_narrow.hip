@@ -5,7 +5,8 @@
 // instruction takes for dx = dz W, W from LDS, and turns it around in LDS for its part of dW = dz^T x, which stays in registers from
 // row to row, as db does; a workgroup leaves its sums, which a second launch adds.  The float instruction serves bf16 tensors as
 // well: dz and all sums are in 32 bits.  40 961 rows, 32 -> 64, float: 14 us and 29 + 4, where the products through planes took 73 in all
-// and more than the 31 MB at a copy's rate, 7, what bounds it is the chain from a row's load over two products and LDS to its stores.
+// and more than the 31 MB at a copy's rate, 7, what bounds it is the chain from a row's load over two products and LDS to its stores;
+// a wavefront has 2.5 tiles of rows, so that W's and the sums' fixed parts count, and reads W's fragments from LDS anew for each.
 #include "gated.h"
 
 namespace lcn {

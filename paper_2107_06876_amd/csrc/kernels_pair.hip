@@ -272,8 +272,9 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN == 4 ? 1 : BM == 128 ? 4 : 2) v
             }
         }
     };
-    // A tile is in LDS, of every wavefront, and every wavefront has read the tile before: loads are counted in order, those of
-    // `more` later tiles may be under way.
+    // A tile is in LDS, of every wavefront, and every wavefront has read the tile before: those of `more` later tiles may be under
+    // way.  Loads end in the order of their issue, as the counter is defined (the compiler's own waits rest on it), also those that are
+    // out of range as a whole: they go the same way and bring zeros.
     auto arrived = [&](auto more) {
         constexpr int MORE = decltype(more)::value * LOADS;
         static_assert(MORE < 64, "the counter");

@@ -253,7 +253,9 @@ def _coefficients(steps, coefficients):
 
 def lcn_orthogonalise(g, steps=5, coefficients=ORTHOGONAL_UPDATE, eps=1e-7, scale=1.0, out=None, workspace=None):
     """scale X, with X = g / (|g| + eps) and then `steps` times X = a X + (b A + c A^2) X, A = X X^T, where g is a matrix or a
-    (count, rows, cols) batch of them; coefficients: (a, b, c), or a sequence of one such triple per step.  out may be g."""
+    (count, rows, cols) batch of them; coefficients: (a, b, c), or a sequence of one such triple per step.  ORTHOGONAL_UPDATE brings most
+    singular values to 0.7 .. 1.2 in the 5 steps that are the default; ORTHOGONAL_MAP brings a value s to 1 in 1.1 log2(|g| / s) + 3 steps,
+    and to the polar factor with enough for the least.  out may be g."""
     dtype = _TYPES.get(g.dtype)
     if dtype is None or g.dim() not in (2, 3) or not g.is_cuda or not g.is_contiguous() or 0 in g.shape[-2:]:
         raise ValueError("g: expected a contiguous float32 or bfloat16 matrix, or a batch of them, on a device")
