@@ -236,6 +236,20 @@ def test_roundings_of_bf16(dim):
         assert off(u, v) <= roundings(1)
 
 
+@pytest.mark.parametrize("rows,dim", [(40961, 300), (30000, 1024), (8000, 4096)])
+def test_sums_over_rows_in_pairs(rows, dim):
+    """Sums of random terms: a sum in pairs adds one rounding's square to the error's with every doubling, a chain of m sums m / 2 of them.
+    Up to 512 workgroups have rows / 512 of them, in chains of up to 16 and then in pairs; their sums are added in
+    chains of 8, then in pairs: 6 doublings.  A rounding is 0.737 2^-23 / sqrt(12) in the 2-norm, and 1.15 leaves room for what it varies by."""
+    x, w, b, dy, _ = inputs(rows, dim, F32)
+    y, mean, rstd = lcn.lcn_layer_norm(x, w, b, keep_stats=True)
+    _, dw, db = lcn.lcn_layer_norm_backward(x, w, mean, rstd, dy, with_x=False)
+    chain = {300: 5, 1024: 15, 4096: 16}[dim] / 2   # of a thread's rows
+    pairs = {300: 4, 1024: 2, 4096: 0}[dim]         # lanes and wavefronts of a workgroup that share columns
+    doublings = chain + pairs + 4 + 6
+    assert off(db, dy.double().sum(0)) <= 1.15 * 0.737 * 2.0 ** -23 / math.sqrt(12.0) * math.sqrt(doublings)
+
+
 def test_differences():
     """<dy, y> changes along a direction as the gradients say (central differences of the float path)."""
     g = generator(5)
