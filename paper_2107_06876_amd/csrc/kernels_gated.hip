@@ -3,8 +3,8 @@
 // Backward: dz = [dy u act'(g) | dy act(g)] once (as planes of bf16, with the column sums that are the biases' gradients), then
 // dx = dz W and dW = dz^T x, which are two products because g's and u's halves lie in one matrix.
 //
-// Bound by the matrix instruction on many rows (16 391 rows, 1024 -> 4096, bf16: 310 us, of it some 50 of epilogue; backward dz 137, at
-// the rate of a copy, dx 250, dW 285) and by reading W on few (one row, 2048 -> 8192, bf16: 11 us for 67 MB).
+// Bound by the matrix instruction on many rows (16 391 rows, 1024 -> 4096, bf16: 337 us, of it some 60 of epilogue; backward dz 137, at
+// the rate of a copy, dx 257, dW 289) and by reading W on few (one row, 2048 -> 8192, bf16: 11 us for 67 MB).
 //
 // Rounding: g, u, sums and activations are in 32 bits; with bf16 tensors y, dz, dx, dW and db are rounded once each.  What is
 // kept of g and u for the backward pass is 16 bits a value for bf16 tensors, 11 of significand (gated.h); as bf16 each would add
