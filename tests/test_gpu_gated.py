@@ -271,6 +271,31 @@ def test_single_gradients_and_same_bits(rows, d_out, shift, dtype):
             assert torch.equal(u, v) if a else u is None
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,d_in,d_out", [(5, 96, 136), (300, 33, 64), (300, 96, 136), (700, 96, 130)])
+def test_operands_that_are_not_needed_may_be_missing(rows, d_in, d_out, dtype):
+    """x is read for dW only, and W for dx only (the C entry point)."""
+    from paper_2107_06876_amd import encoder
+    x, w, b, dy = inputs(rows, d_in, d_out, dtype)
+    _, z = lcn.lcn_gated_linear(x, w, bias=b, keep_pre=True)
+    dx, dw, db = lcn.lcn_gated_linear_backward(x, w, z, dy)
+    sizes = (rows, d_in, d_out, 0 if dtype == F32 else 1)
+    space = torch.empty(encoder._bytes("lcn_gated_linear_workspace_bytes", (*sizes, 1)), dtype=torch.uint8, device=DEV)
+    for with_x, with_w in ((True, False), (False, True), (False, False)):
+        got = [torch.full_like(t, 7.0) for t in (dx, dw, db)]
+        encoder._call("lcn_gated_linear_backward", x.device, x.data_ptr() if with_w else None, w.data_ptr() if with_x else None, z.data_ptr(),
+                      dy.data_ptr(), *sizes, ACTS["silu"], got[0].data_ptr() if with_x else None, got[1].data_ptr() if with_w else None,
+                      got[2].data_ptr(), space.data_ptr(), space.numel())
+        narrow_by_planes = rows >= 128 and d_in <= 64 and d_out <= 64
+        for u, v, asked in zip(got, (dx, dw, db), (with_x, with_w, True)):
+            if not asked:
+                assert (u == 7.0).all()
+            elif narrow_by_planes:   # another way to the same sums
+                assert off(u, v.double()) <= 2 * bound(dtype, max(rows, 2 * d_out), 1)
+            else:
+                assert torch.equal(u, v)
+
+
 def test_differences():
     """<dy, y> changes along a direction as the gradients say (central differences of the float path)."""
     g = generator(14)
